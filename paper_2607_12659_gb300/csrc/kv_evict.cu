@@ -1,0 +1,243 @@
+// Eviction from a cache by accumulated attention weight (jpi_kv_evict): two launches, the choice and
+// the move.
+//
+// The choice (k_kv_select), one block per layer, cache and KV head. The weights, as unsigned keys of
+// the same order (NaN 0, below everything), are searched for the need-th largest by three passes over
+// 11, 11 and 10 bits, a histogram in shared memory each: exact, whatever the distribution. Above the
+// threshold every row stays; of the rows equal to it the lowest, as many as are left. Each thread then
+// counts its run of consecutive rows, one block-wide scan gives every run its place, and the kept rows
+// come out ascending.
+//
+// The move (k_kv_gather): a block takes 64 bytes of every kept row of one cache, head and matrix, in
+// tiles of ascending rows: a tile is loaded whole, then stored. In place this needs no second buffer:
+// a row never moves up (row i goes to at most i) and what a tile overwrites lies in it or before it,
+// so it has been read. Bound by memory: every kept row is read and written once.
+
+#include "kv.h"
+
+namespace jpi {
+namespace {
+
+constexpr int SEL_THREADS = 1024;
+constexpr int SEL_BINS = 2048;
+
+// An unsigned key of the same order; NaN is 0, -0 equals 0.
+__device__ __forceinline__ uint32_t sort_key(float w) {
+    if (w != w) return 0u;
+    const uint32_t b = __float_as_uint(w + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// Exclusive sums of (x, y) over the block's threads in order; `tot` gets the whole sums.
+__device__ __forceinline__ uint2 block_scan(uint2 v, uint2* warp_sums, uint2* tot) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint2 s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, s.x, o), y = __shfl_up_sync(0xffffffffu, s.y, o);
+        if (lane >= o) {
+            s.x += x;
+            s.y += y;
+        }
+    }
+    if (lane == 31) warp_sums[warp] = s;
+    __syncthreads();
+    if (warp == 0) {
+        uint2 t = warp_sums[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, t.x, o), y = __shfl_up_sync(0xffffffffu, t.y, o);
+            if (lane >= o) {
+                t.x += x;
+                t.y += y;
+            }
+        }
+        warp_sums[lane] = t;
+    }
+    __syncthreads();
+    const uint2 before = warp ? warp_sums[warp - 1] : make_uint2(0, 0);
+    *tot = warp_sums[SEL_THREADS / 32 - 1];
+    __syncthreads();   // warp_sums may be used again
+    return make_uint2(before.x + s.x - v.x, before.y + s.y - v.y);
+}
+
+__global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, const int* length, int rows, int caches,
+                                                           int K, int keep, int sink, int recent, int dst_rows,
+                                                           float* w_out_all, int* kept_all) {
+    __shared__ uint32_t hist[SEL_BINS];
+    __shared__ uint2 warp_sums[SEL_THREADS / 32];
+    __shared__ uint32_t found[2];   // chosen bin, rows still needed within it
+    const int t = threadIdx.x;
+    const long long item = blockIdx.x;   // (layer, cache, head)
+    const int c = (int)((item / K) % caches);
+    const float* w = w_all + item * rows;
+    float* w_out = w_out_all + item * dst_rows;
+    int* kept = kept_all + item * keep;
+    const int n = min(max(length[c], 0), rows);
+    if (n <= keep) {
+        for (int i = t; i < keep; i += SEL_THREADS) {
+            kept[i] = i < n ? i : -1;
+            if (i < n && w_out != w) w_out[i] = w[i];
+        }
+        return;
+    }
+    // The need-th largest key of rows lo .. hi - 1 (need < hi - lo).
+    const int lo = sink, hi = n - recent;
+    uint32_t need = (uint32_t)(keep - sink - recent);
+    uint32_t prefix = 0, mask = 0;   // keys with (key & mask) == prefix are still candidates
+    if (need > 0) {
+        const int shifts[3] = {21, 10, 0};
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = shifts[pass];
+            const uint32_t bins = pass == 2 ? 1024u : 2048u;
+            hist[t] = 0;
+            hist[t + SEL_THREADS] = 0;
+            __syncthreads();
+            for (int i = lo + t; i < hi; i += SEL_THREADS) {
+                const uint32_t k = sort_key(w[i]);
+                if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+            }
+            __syncthreads();
+            // Bins from the top, two a thread.
+            const uint32_t b1 = SEL_BINS - 1 - 2 * t, n1 = hist[b1], n0 = hist[b1 - 1];
+            uint2 tot;
+            const uint32_t above = block_scan(make_uint2(n1 + n0, 0), warp_sums, &tot).x;
+            if (above < need && need <= above + n1) {
+                found[0] = b1;
+                found[1] = need - above;
+            } else if (above + n1 < need && need <= above + n1 + n0) {
+                found[0] = b1 - 1;
+                found[1] = need - above - n1;
+            }
+            __syncthreads();
+            prefix |= found[0] << shift;
+            mask |= (bins - 1) << shift;
+            need = found[1];
+            __syncthreads();
+        }
+    }
+    // Rows that stay: protected or above the threshold (x), and `need` of those equal to it (y).
+    const bool some = keep > sink + recent;
+    const int run = (n + SEL_THREADS - 1) / SEL_THREADS, r0 = min(n, t * run), r1 = min(n, r0 + run);
+    auto kind = [&](int i) -> uint2 {
+        if (i < lo || i >= hi) return make_uint2(1, 0);
+        const uint32_t k = sort_key(w[i]);
+        return make_uint2(some && k > prefix, some && k == prefix);
+    };
+    uint2 mine = make_uint2(0, 0);
+    for (int i = r0; i < r1; ++i) {
+        const uint2 x = kind(i);
+        mine.x += x.x;
+        mine.y += x.y;
+    }
+    uint2 tot;
+    uint2 at = block_scan(mine, warp_sums, &tot);
+    for (int i = r0; i < r1; ++i) {
+        const uint2 x = kind(i);
+        if (x.x || (x.y && at.y < need)) kept[at.x + min(at.y, need)] = i;
+        at.x += x.x;
+        at.y += x.y;
+    }
+    __syncthreads();
+    // The weights follow, in tiles: in place, a tile's stores come after its loads.
+    for (int i0 = 0; i0 < keep; i0 += SEL_THREADS) {
+        const int i = i0 + t;
+        const float x = i < keep ? w[kept[i]] : 0.f;
+        __syncthreads();
+        if (i < keep) w_out[i] = x;
+    }
+}
+
+struct GatherArgs {
+    const uint8_t *k, *v;
+    uint8_t *ok, *ov;
+    long long cs, rs, hs, ls;        // strides in bytes
+    long long ocs, ors, ohs, ols;
+    int caches, K, keep, chunks;     // chunks: 16-byte chunks of a row
+    const int* kept;
+    const int* length;
+    int* length_out;
+    int rows;
+    int in_place;
+};
+
+constexpr int GA_THREADS = 256;
+constexpr int GA_LANES = 4;                           // 16-byte chunks of a slice
+constexpr int GA_ROWS = GA_THREADS / GA_LANES;        // rows of one load
+constexpr int GA_UNROLL = 8;
+
+__global__ void __launch_bounds__(GA_THREADS) k_kv_gather(const __grid_constant__ GatherArgs a) {
+    const int item = blockIdx.y;   // (layer, cache, head)
+    const int h = item % a.K, c = (item / a.K) % a.caches, l = item / (a.K * a.caches);
+    const int slices = (a.chunks + GA_LANES - 1) / GA_LANES;
+    const bool is_v = (int)blockIdx.x >= slices;
+    const int ch = (blockIdx.x - (is_v ? slices : 0)) * GA_LANES + (threadIdx.x & (GA_LANES - 1));
+    const int r0 = threadIdx.x / GA_LANES;
+    const uint8_t* src = (is_v ? a.v : a.k) + l * a.ls + c * a.cs + h * a.hs + ch * 16;
+    uint8_t* dst = (is_v ? a.ov : a.ok) + l * a.ols + c * a.ocs + h * a.ohs + ch * 16;
+    const int* kept = a.kept + (long long)item * a.keep;
+    const bool mine = ch < a.chunks;
+    for (int i0 = (int)blockIdx.z * GA_ROWS * GA_UNROLL; i0 < a.keep; i0 += (int)gridDim.z * GA_ROWS * GA_UNROLL) {
+        uint4 x[GA_UNROLL];
+        bool move[GA_UNROLL];
+#pragma unroll
+        for (int u = 0; u < GA_UNROLL; ++u) {
+            const int i = i0 + u * GA_ROWS + r0;
+            const int r = i < a.keep && mine ? kept[i] : -1;
+            move[u] = r >= 0 && !(a.in_place && r == i);
+            if (move[u]) x[u] = *(const uint4*)(src + r * a.rs);
+        }
+        if (a.in_place) __syncthreads();
+#pragma unroll
+        for (int u = 0; u < GA_UNROLL; ++u)
+            if (move[u]) *(uint4*)(dst + (long long)(i0 + u * GA_ROWS + r0) * a.ors) = x[u];
+    }
+    // The choice has read the lengths: one thread of each cache's first block replaces its length.
+    if (blockIdx.x == 0 && blockIdx.z == 0 && l == 0 && h == 0 && threadIdx.x == 0)
+        a.length_out[c] = min(min(max(a.length[c], 0), a.rows), a.keep);
+}
+
+}  // namespace
+
+jpi_status launch_kv_evict(const jpi_kv_handle* h, const jpi_kv_cache& src, const float* w, const int* length, int layers,
+                           int caches, int keep, int sink, int recent, const jpi_kv_cache& dst, float* w_out,
+                           int* length_out, int* kept, cudaStream_t st) {
+    const int items = layers * caches * h->K;
+    k_kv_select<<<items, SEL_THREADS, 0, st>>>(w, length, src.rows, caches, h->K, keep, sink, recent, dst.rows, w_out, kept);
+    JPI_CUDA_TRY(cudaGetLastError());
+    const long long e = h->bf16 ? 2 : 4;
+    GatherArgs a = {};
+    a.k = (const uint8_t*)src.k;
+    a.v = (const uint8_t*)src.v;
+    a.ok = (uint8_t*)dst.k;
+    a.ov = (uint8_t*)dst.v;
+    a.cs = src.cache_stride * e;
+    a.rs = src.row_stride * e;
+    a.hs = src.head_stride * e;
+    a.ls = src.layer_stride * e;
+    a.ocs = dst.cache_stride * e;
+    a.ors = dst.row_stride * e;
+    a.ohs = dst.head_stride * e;
+    a.ols = dst.layer_stride * e;
+    a.caches = caches;
+    a.K = h->K;
+    a.keep = keep;
+    a.chunks = (int)(h->D * e / 16);
+    a.kept = kept;
+    a.length = length;
+    a.length_out = length_out;
+    a.rows = src.rows;
+    a.in_place = src.k == dst.k;
+    const int gx = 2 * ((a.chunks + GA_LANES - 1) / GA_LANES);
+    // Apart, the tiles of a slice are independent: more blocks where there are few slices.
+    int gz = 1;
+    if (!a.in_place) {
+        const int tiles = (keep + GA_ROWS * GA_UNROLL - 1) / (GA_ROWS * GA_UNROLL);
+        while (gz < tiles && gz < 64 && (long long)gx * items * gz < 8ll * h->num_sms) ++gz;
+    }
+    k_kv_gather<<<dim3(gx, items, gz), GA_THREADS, 0, st>>>(a);
+    JPI_CUDA_TRY(cudaGetLastError());
+    return JPI_OK;
+}
+
+}  // namespace jpi

@@ -1,0 +1,223 @@
+// Accumulated attention weight of cached keys (jpi_kv_weigh).
+//
+//   out[j] = decay in[j] + sum over rows r that see j of exp(s_rj - lse_r),  s_rj = scale q_r . k_j,
+// with lse from jpi_kv_attend, so that no maximum has to be found and keys are independent of each other.
+// A key's sum is formed by one block in a fixed order and written once: no atomics, no partial results in
+// global memory.
+//
+// bf16: a warp keeps 16 keys in registers as the rows of mma.sync and streams the query rows past them, 8 at
+// a time; a lane adds up the weights of its two keys, and the four lanes of a key and the warps that share it
+// are joined at the end. fp32 on CUDA cores: a key per lane.
+
+#include "kv_rows.cuh"
+
+#include <algorithm>
+
+namespace jpi {
+namespace {
+
+constexpr int WG_WARPS = 8;
+constexpr int WG_THREADS = 32 * WG_WARPS;
+
+struct WeighArgs {
+    KvCall c;
+    const float* lse;
+    float decay;
+    const float *pin, *oin;
+    float *pout, *oout;
+    int wr_p, wr_o;              // warps of a block that share its keys, each with every wr-th row tile
+    int tiles_p, tiles_o;        // key blocks per cache and head
+    long long blocks_p;
+};
+
+struct KeyPiece {
+    bool prefix;
+    int cache, kvh, tile, wr;
+    RowTile t;
+};
+__device__ __forceinline__ KeyPiece key_piece(const WeighArgs& a) {
+    KeyPiece x;
+    long long i = blockIdx.x;
+    x.prefix = i < a.blocks_p;
+    if (!x.prefix) i -= a.blocks_p;
+    const int tiles = x.prefix ? a.tiles_p : a.tiles_o;
+    x.wr = x.prefix ? a.wr_p : a.wr_o;
+    x.tile = (int)(i % tiles);
+    i /= tiles;
+    x.kvh = (int)(i % a.c.K);
+    x.cache = (int)(i / a.c.K);
+    const int toks = x.prefix ? a.c.batch / a.c.groups * a.c.tokens : a.c.tokens;
+    x.t.tok0 = (long long)x.cache * toks;
+    x.t.head0 = x.kvh * a.c.gq;
+    x.t.R = toks * a.c.gq;
+    x.t.r0 = 0;
+    return x;
+}
+// Rows of the piece's cache that hold keys: the prefix's length, or the most that a token of the request sees.
+__device__ __forceinline__ int live_keys(const WeighArgs& a, const KeyPiece& x, int* shared) {
+    const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
+    if (x.prefix) return min(max(s.len[x.cache], 0), s.rows);
+    if (threadIdx.x == 0) *shared = 0;
+    __syncthreads();
+    int n = 0;
+    for (int t = threadIdx.x; t < a.c.tokens; t += WG_THREADS) n = max(n, s.len[x.t.tok0 + t]);
+    n = __reduce_max_sync(0xffffffffu, n);
+    if ((threadIdx.x & 31) == 0) atomicMax(shared, n);
+    __syncthreads();
+    return min(*shared, s.rows);
+}
+__device__ __forceinline__ void write_weight(const WeighArgs& a, const KeyPiece& x, int key, float sum) {
+    const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
+    const float* in = x.prefix ? a.pin : a.oin;
+    float* out = x.prefix ? a.pout : a.oout;
+    const long long i = ((long long)x.cache * a.c.K + x.kvh) * s.rows + key;
+    out[i] = in && a.decay != 0.f ? fmaf(a.decay, in[i], sum) : sum;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_mma(const __grid_constant__ WeighArgs a) {
+    __shared__ float part[WG_WARPS][16];
+    __shared__ int top;
+    constexpr int NC = DP / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+    const KeyPiece x = key_piece(a);
+    const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
+    const int live = live_keys(a, x, &top);
+    const int kt = WG_WARPS / x.wr, key0 = (x.tile * kt + warp / x.wr) * 16, wrow = warp % x.wr;
+    float acc0 = 0.f, acc1 = 0.f;   // keys g and g + 8
+    if (key0 < live) {
+        uint4 kf[NC][2];
+        const __nv_bfloat16* kp = (const __nv_bfloat16*)s.k + x.cache * s.cs + x.kvh * s.hs + (long long)(key0 + g) * s.rs + 8 * j;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const bool in = 8 * (4 * i + j) < a.c.D;
+            kf[i][0] = kr_ld(kp + 32 * i, in && key0 + g < live);
+            kf[i][1] = kr_ld(kp + 8 * s.rs + 32 * i, in && key0 + g + 8 < live);
+        }
+        for (int rt = wrow * KR_ROWS; rt < x.t.R; rt += x.wr * KR_ROWS) {
+            const int rq = rt + g;
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + 8 * j;
+            if (rq < x.t.R) q += row_token(x.t, a.c.gq, rq) * a.c.q_stride + (long long)(x.t.head0 + rq % a.c.gq) * a.c.D;
+            float sc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const uint4 v = kr_ld(q + 32 * i, rq < x.t.R && 8 * (4 * i + j) < a.c.D);
+                kr_mma(sc, kf[i][0].x, kf[i][1].x, kf[i][0].y, kf[i][1].y, v.x, v.y);
+                kr_mma(sc, kf[i][0].z, kf[i][1].z, kf[i][0].w, kf[i][1].w, v.z, v.w);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = rt + 2 * j + e;
+                if (r >= x.t.R) continue;
+                const float ls = a.lse[row_index(x.t, a.c.gq, a.c.H, r)];
+                const int n = row_seen(a.c, x.prefix, x.cache, x.t, r);
+                if (ls == -INFINITY) continue;
+                if (key0 + g < n) acc0 += kr_ex2(fmaf(sc[e], a.c.scale, -ls) * KR_LOG2E);
+                if (key0 + g + 8 < n) acc1 += kr_ex2(fmaf(sc[2 + e], a.c.scale, -ls) * KR_LOG2E);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        acc0 += __shfl_xor_sync(0xffffffffu, acc0, o);
+        acc1 += __shfl_xor_sync(0xffffffffu, acc1, o);
+    }
+    if (j == 0) {
+        part[warp][g] = acc0;
+        part[warp][g + 8] = acc1;
+    }
+    __syncthreads();
+    if (wrow == 0 && lane < 16 && key0 + lane < live) {
+        float sum = part[warp][lane];
+        for (int i = 1; i < x.wr; ++i) sum += part[warp + i][lane];
+        write_weight(a, x, key0 + lane, sum);
+    }
+}
+
+__global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_f32(const __grid_constant__ WeighArgs a) {
+    __shared__ float part[WG_WARPS][32];
+    __shared__ int top;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const KeyPiece x = key_piece(a);
+    const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
+    const int live = live_keys(a, x, &top);
+    const int kt = WG_WARPS / x.wr, key = (x.tile * kt + warp / x.wr) * 32 + lane, wrow = warp % x.wr;
+    float acc = 0.f;
+    const float* kp = (const float*)s.k + x.cache * s.cs + x.kvh * s.hs + (long long)(key < live ? key : 0) * s.rs;
+    for (int rt = wrow * KR_ROWS; rt < x.t.R; rt += x.wr * KR_ROWS) {
+        float p[KR_ROWS];
+        const float* q[KR_ROWS];
+#pragma unroll
+        for (int r = 0; r < KR_ROWS; ++r) {
+            const int rr = min(rt + r, x.t.R - 1);
+            p[r] = 0.f;
+            q[r] = static_cast<const float*>(a.c.q) + row_token(x.t, a.c.gq, rr) * a.c.q_stride + (long long)(x.t.head0 + rr % a.c.gq) * a.c.D;
+        }
+        if (key < live)
+            for (int d = 0; d < a.c.D; d += 4) {
+                const float4 k = __ldg((const float4*)(kp + d));
+#pragma unroll
+                for (int r = 0; r < KR_ROWS; ++r) {
+                    const float4 v = __ldg((const float4*)(q[r] + d));
+                    p[r] = fmaf(v.x, k.x, fmaf(v.y, k.y, fmaf(v.z, k.z, fmaf(v.w, k.w, p[r]))));
+                }
+            }
+#pragma unroll
+        for (int r = 0; r < KR_ROWS; ++r) {
+            if (rt + r >= x.t.R) break;
+            const float ls = a.lse[row_index(x.t, a.c.gq, a.c.H, rt + r)];
+            const int n = row_seen(a.c, x.prefix, x.cache, x.t, rt + r);
+            if (key < n && ls != -INFINITY) acc += expf(fmaf(p[r], a.c.scale, -ls));
+        }
+    }
+    part[warp][lane] = acc;
+    __syncthreads();
+    if (wrow == 0 && key < live) {
+        float sum = acc;
+        for (int i = 1; i < x.wr; ++i) sum += part[warp + i][lane];
+        write_weight(a, x, key, sum);
+    }
+}
+
+// Warps that share a block's keys: as many as leave every SM a block, and each warp a row tile.
+int row_warps(const jpi_kv_handle* h, const KvCall& c, bool prefix, int keys, int* tiles) {
+    const KvSide& s = prefix ? c.prefix : c.own;
+    const long long R = (long long)(prefix ? c.batch / c.groups : 1) * c.tokens * c.gq;
+    const long long caches = (long long)(prefix ? c.groups : c.batch) * c.K, rt = (R + KR_ROWS - 1) / KR_ROWS;
+    int wr = 1;
+    auto count = [&](int w) { return (s.rows + keys * (WG_WARPS / w) - 1) / (keys * (WG_WARPS / w)); };
+    while (wr < WG_WARPS && wr * 2 <= rt && caches * count(wr) < h->num_sms) wr *= 2;
+    *tiles = s.rows ? count(wr) : 0;
+    return wr;
+}
+
+}  // namespace
+
+jpi_status launch_kv_weigh(jpi_kv_handle* h, const KvCall& c, const float* lse, float decay, const float* prefix_in,
+                           float* prefix_out, const float* own_in, float* own_out, cudaStream_t st) {
+    WeighArgs a;
+    a.c = c;
+    a.lse = lse;
+    a.decay = decay;
+    a.pin = prefix_in;
+    a.oin = own_in;
+    a.pout = prefix_out;
+    a.oout = own_out;
+    const int keys = h->bf16 ? 16 : 32;
+    a.wr_p = row_warps(h, c, true, keys, &a.tiles_p);
+    a.wr_o = row_warps(h, c, false, keys, &a.tiles_o);
+    a.blocks_p = (long long)c.groups * c.K * a.tiles_p;
+    const long long blocks = a.blocks_p + (long long)c.batch * c.K * a.tiles_o;
+    if (blocks > 0x7fffffffll) {
+        set_error("the call needs more than 2^31 blocks");
+        return JPI_ERR_SHAPE;
+    }
+    if (!h->bf16) k_kv_weigh_f32<<<(unsigned)blocks, WG_THREADS, 0, st>>>(a);
+    else if (h->D <= 64) k_kv_weigh_mma<64><<<(unsigned)blocks, WG_THREADS, 0, st>>>(a);
+    else if (h->D <= 128) k_kv_weigh_mma<128><<<(unsigned)blocks, WG_THREADS, 0, st>>>(a);
+    else k_kv_weigh_mma<256><<<(unsigned)blocks, WG_THREADS, 0, st>>>(a);
+    JPI_CUDA_TRY(cudaGetLastError());
+    return JPI_OK;
+}
+
+}  // namespace jpi

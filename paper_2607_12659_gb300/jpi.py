@@ -74,12 +74,25 @@ _SIGS = {
     "jpi_profile_op": [c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_void_p],
     "jpi_expert_forward_noalloc": [c_void_p, c_void_p, c_void_p, c_float, c_int, c_int, c_void_p,
                                    c_void_p, c_void_p],
+    # The KV-cache operators (include/jpi_kv.h); their structs and wrappers are in kv.py.
+    "jpi_kv_create": [c_void_p, c_void_p, POINTER(c_void_p)],
+    "jpi_kv_destroy": [c_void_p],
+    "jpi_kv_append": [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_void_p,
+                      c_int, c_int, c_void_p, c_void_p, c_void_p],
+    "jpi_kv_attend": [c_void_p, c_void_p, c_longlong, c_int, c_int, c_void_p, c_int, c_void_p, c_void_p, c_void_p,
+                      c_void_p, c_void_p, c_void_p],
+    "jpi_kv_weigh": [c_void_p, c_void_p, c_longlong, c_void_p, c_int, c_int, c_void_p, c_int, c_void_p, c_void_p,
+                     c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p],
+    "jpi_kv_evict": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p,
+                     c_void_p, c_void_p, c_void_p],
+    "jpi_kv_device_status": [c_void_p],
+    "jpi_kv_memory_usage": [c_void_p, POINTER(c_longlong)],
 }
 
 _lib = None
 
 
-LIB_HEADERS = ("jpi.h", "jpi_corr.h")   # the entry points libjpi.so exports
+LIB_HEADERS = ("jpi.h", "jpi_corr.h", "jpi_kv.h")   # the entry points libjpi.so exports
 
 
 def header_symbols(headers=LIB_HEADERS) -> list[str]:
