@@ -1,7 +1,7 @@
 """Builds the libraries in-tree for sm_103a with nvcc (no cmake, no torch build).
 
-``libjpi.so``: the action expert and the future correction module (every .cu directly under
-csrc/). Each translation unit compiles in parallel; the objects link into one shared library
+``libjpi.so``: the action expert, the future correction module (every .cu directly under csrc/)
+and the KV-cache operators (csrc/kv/). Each translation unit compiles in parallel; the objects link into one shared library
 with the CUDA runtime linked statically, so the library needs no libcuda at load time (the
 driver entry points are resolved at run time).
 
@@ -23,6 +23,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libjpi.so")
+KV_SRC = os.path.join(CSRC, "kv")
 PREFILL_SRC = os.path.join(CSRC, "prefill")
 PREFILL_LIB = os.path.join(PKG, "libjpi_prefill.so")
 PREFILL_BUILD_ERROR = None
@@ -43,7 +44,7 @@ def nvcc() -> str:
 
 
 def sources() -> list[str]:
-    return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
+    return sorted(os.path.join(d, f) for d in (CSRC, KV_SRC) for f in os.listdir(d) if f.endswith(".cu"))
 
 
 def _stale(obj: str, src: str) -> bool:
@@ -51,7 +52,7 @@ def _stale(obj: str, src: str) -> bool:
         return True
     t = os.path.getmtime(obj)
     inc = os.path.join(ROOT, "include")
-    deps = [src] + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
+    deps = [src] + [os.path.join(d, f) for d in (CSRC, KV_SRC) for f in os.listdir(d) if f.endswith((".h", ".cuh"))]
     deps += [os.path.join(inc, f) for f in os.listdir(inc) if f.endswith(".h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -105,7 +106,7 @@ def build_probe(force: bool = False) -> str:
 
 
 def build(verbose: bool = False, force: bool = False) -> str:
-    """Compile every .cu directly under csrc/ and link libjpi.so, then the prefill library;
+    """Compile every .cu directly under csrc/ and in csrc/kv/ and link libjpi.so, then the prefill library;
     returns libjpi.so's path."""
     os.makedirs(BUILD, exist_ok=True)
     cc = nvcc()

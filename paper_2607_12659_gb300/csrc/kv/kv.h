@@ -1,6 +1,6 @@
 // KV-cache operators (include/jpi_kv.h): the handle and the launchers of its kernels.
 #pragma once
-#include "jpi_internal.h"
+#include "../jpi_internal.h"
 #include "jpi_kv.h"
 
 struct jpi_kv_handle {

@@ -14,7 +14,7 @@
 #pragma once
 
 #include "kv.h"
-#include "ptx.h"
+#include "../ptx.h"
 
 namespace jpi {
 namespace {

@@ -17,8 +17,7 @@ import ctypes
 from ctypes import byref, c_float, c_int, c_longlong, c_void_p
 from dataclasses import dataclass
 
-from . import jpi
-from .jpi import JPI_BF16, JPI_FP32, OnStream, _check, _ptr, _stream, load
+from .jpi import _HERE, JPI_BF16, JPI_FP32, OnStream, _check, _ptr, _stream, load
 
 
 class jpi_kv_rope(ctypes.Structure):
@@ -110,14 +109,13 @@ class Rope:
 
 def cache_of(k, v=None, layers=False) -> jpi_kv_cache:
     """The jpi_kv_cache of tensors [caches][rows][KV heads][head dim], or with `layers` another dimension before them."""
-    n = 5 if layers else 4
-    if k.dim() != n or (v is not None and (v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype)):
+    s, n = k.stride(), 5 if layers else 4
+    if len(s) != n or (v is not None and (v.stride() != s or v.shape != k.shape or v.dtype is not k.dtype)):
         raise ValueError(f"k and v must be {n}-dimensional caches of one shape, type and strides")
-    if k.stride(-1) != 1 and k.shape[-1] > 1:
+    if s[-1] != 1 and k.shape[-1] > 1:
         raise ValueError("a head's elements must be contiguous")
-    st = k.stride()[-4:]
-    return jpi_kv_cache(k=k.data_ptr(), v=v.data_ptr() if v is not None else None, cache_stride=st[0], row_stride=st[1],
-                        head_stride=st[2], layer_stride=k.stride(0) if layers else 0, rows=k.shape[-3])
+    return jpi_kv_cache(k.data_ptr(), v.data_ptr() if v is not None else None, s[-4], s[-3], s[-2], s[0] if layers else 0,
+                        k.shape[-3])
 
 
 class KV:
@@ -130,9 +128,12 @@ class KV:
         self.cfg = jpi_kv_config(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, max_batch=max_batch,
                                  max_tokens=max_tokens, scale=scale,
                                  precision={"bf16": JPI_BF16, "fp32": JPI_FP32}[precision])
+        self.heads, self.kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
         self.dtype = torch.bfloat16 if precision == "bf16" else torch.float32
         self.handle = jpi_kv_create(self.cfg, rope.c() if rope is not None else None)
-        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.index = torch.cuda.current_device()
+        self.device = torch.device("cuda", self.index)
+        self._torch, self._int, self._float = torch, torch.int32, torch.float32
 
     def close(self):
         if self.handle:
@@ -145,128 +146,140 @@ class KV:
         except Exception:
             pass
 
-    # The C-ABI sees addresses only: what they point to is checked here.
-    def _data(self, name, t, shape=None, dtype=None):
-        if t is None:
-            return
-        if t.device != self.device:
+    # The C-ABI sees addresses only: what they point to is checked here. A call for one token lasts a few
+    # microseconds on the GPU, so the checks read each property of a tensor once.
+    def _data(self, name, t, dtype):
+        if t.get_device() != self.index:
             raise ValueError(f"{name} is on {t.device}, the handle on {self.device}")
-        if t.dtype != (dtype or self.dtype):
-            raise ValueError(f"{name} is {t.dtype}, not {dtype or self.dtype}")
-        if shape is not None and tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+        if t.dtype is not dtype:
+            raise ValueError(f"{name} is {t.dtype}, not {dtype}")
 
     def _whole(self, name, t, shape, dtype):
-        """A tensor that is taken (and written) as one contiguous block."""
-        self._data(name, t, shape, dtype)
-        if t is not None and not t.is_contiguous():
+        """The address of a tensor that is taken (and written) as one contiguous block."""
+        self._data(name, t, dtype)
+        if t.shape != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+        if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
+        return t.data_ptr()
 
     def _cache(self, name, k, v, n, layers=None):
-        K, D = self.cfg.n_kv_heads, self.cfg.head_dim
+        want = (self.kv_heads, self.head_dim)
         lead = (n,) if layers is None else (layers, n)
-        for part, t in (("k", k), ("v", v)):
+        for t in (k, v):
             if t is not None:
-                self._data(f"{name} {part}", t)
-                if tuple(t.shape) != (*lead, t.shape[len(lead)], K, D):
-                    raise ValueError(f"{name} {part} has shape {tuple(t.shape)}, not [{', '.join(map(str, lead))}][rows][{K}][{D}]")
+                self._data(name, t, self.dtype)
+                if t.shape[:-3] != lead or t.shape[-2:] != want:
+                    raise ValueError(f"{name} has shape {tuple(t.shape)}, not {lead} x rows x {want}")
         return cache_of(k, v, layers is not None)
 
     def _tokens(self, name, t, heads):
-        """(tensor, token stride): new tokens [batch][tokens][heads][D], one row of `stride` elements each."""
-        self._data(name, t, (*t.shape[:2], heads, self.cfg.head_dim))
-        B, T, _, D = t.shape
-        s = t.stride()
-        whole = s[3] == 1 and (s[2] == D or heads == 1)
+        """(tensor, address, token stride): new tokens [batch][tokens][heads][D], one row of `stride` elements each."""
+        self._data(name, t, self.dtype)
+        shape, s, at = t.shape, t.stride(), t.data_ptr()
+        if len(shape) != 4 or shape[2] != heads or shape[3] != self.head_dim:
+            raise ValueError(f"{name} has shape {tuple(shape)}, not [batch][tokens][{heads}][{self.head_dim}]")
+        B, T, _, D = shape
         stride = s[1] if T > 1 else s[0] if B > 1 else heads * D
-        if not whole or (B > 1 and T > 1 and s[0] != T * s[1]) or stride < heads * D or (stride * t.element_size()) % 16 \
-                or t.data_ptr() % 16:
+        if s[3] != 1 or (s[2] != D and heads > 1) or (B > 1 and T > 1 and s[0] != T * s[1]) or stride < heads * D \
+                or (stride * t.element_size()) % 16 or at % 16:
             t = t.contiguous()
-            stride = heads * D
-        return t, stride
+            at, stride = t.data_ptr(), heads * D
+        return t, at, stride
+
+    def _on(self, stream):
+        """Torch's side of a call on another stream than the current one (None: this one)."""
+        return None if stream is None else OnStream(stream, self.device)
+
+    def _run(self, fn, stream, args, on, reads, returns):
+        """The C call, with what it reads and returns kept by the stream that it runs on."""
+        if on is not None:
+            on.reads(*(t for t in reads if t is not None))
+            on.returns(*returns)
+        lib = load()
+        _check(getattr(lib, fn)(self.handle, *args, _stream(stream)), fn)
 
     def append(self, q, k, v, positions, rows, cache_k=None, cache_v=None, q_out=None, stream=None):
         """Codes q [B][T][H][D] and k [B][T][Hk][D] for `positions` (int32 [B][T]) and writes k and v into `rows`
         (int32 [B][T]; a row outside the cache marks padding) of the caches. Returns the coded queries. q, v, or k
         with v and the caches may be None."""
-        import torch
-        H, K, D = self.cfg.n_heads, self.cfg.n_kv_heads, self.cfg.head_dim
         if q is None and k is None:
             raise ValueError("neither q nor k is given")
-        B, T = (q if q is not None else k).shape[:2]
-        dev = self.device
-        with OnStream(stream, dev) as on:
-            args = []
-            for name, t, heads in (("q", q, H), ("k", k, K), ("v", v, K)):
+        on = self._on(stream)
+        with on or _HERE:
+            lead = (q if q is not None else k).shape[:2]
+            B, T = lead
+            args, fresh = [], []
+            reads = [q, k, v, positions, rows]
+            for name, t, heads in (("q", q, self.heads), ("k", k, self.kv_heads), ("v", v, self.kv_heads)):
                 if t is None:
-                    args += [None, 0]
+                    args += (None, 0)
                     continue
-                if tuple(t.shape[:2]) != (B, T):
+                if t.shape[:2] != lead:
                     raise ValueError(f"{name} has shape {tuple(t.shape)}, not [{B}][{T}]..")
-                on.reads(t)
-                args += self._tokens(name, t, heads)
-            self._whole("positions", positions, (B, T), torch.int32)
-            self._whole("rows", rows, (B, T), torch.int32)
-            on.reads(positions, rows)
-            cache = None
-            if k is not None:
-                if cache_k is None or (v is not None and cache_v is None):
-                    raise ValueError("k and v need the caches they go to")
-                cache = self._cache("cache", cache_k, cache_v if v is not None else None, B)
-                on.reads(cache_k, *(() if v is None else (cache_v,)))
+                t, at, stride = self._tokens(name, t, heads)
+                fresh.append(t)     # lives until the call is enqueued
+                args += (at, stride)
+            args += (self._whole("positions", positions, lead, self._int), self._whole("rows", rows, lead, self._int), B, T)
+            returns = []
             if q is None:
                 q_out = None
-            elif q_out is None:
-                q_out = torch.zeros((B, T, H, D), dtype=self.dtype, device=dev)
-                on.returns(q_out)
+                args.append(None)
             else:
-                self._whole("q_out", q_out, (B, T, H, D), self.dtype)
-                on.reads(q_out)
-        jpi_kv_append(self.handle, *args, positions, rows, B, T, q_out, cache, stream)
+                shape = (B, T, self.heads, self.head_dim)
+                if q_out is None:
+                    q_out = self._torch.zeros(shape, dtype=self.dtype, device=self.device)
+                    returns.append(q_out)
+                else:
+                    reads.append(q_out)
+                args.append(self._whole("q_out", q_out, shape, self.dtype))
+            if k is None:
+                args.append(None)
+            else:
+                if cache_k is None or (v is not None and cache_v is None):
+                    raise ValueError("k and v need the caches they go to")
+                args.append(byref(self._cache("cache", cache_k, cache_v if v is not None else None, B)))
+                reads += (cache_k, cache_v)
+            self._run("jpi_kv_append", stream, args, on, reads, returns)
         return q_out
 
-    def _sides(self, on, q, prefix, prefix_len, own, seen):
-        """(q, stride, B, T, prefix cache, groups, own cache) of attend and weigh; prefix and own are (k, v)."""
-        import torch
-        H = self.cfg.n_heads
+    def _sides(self, q, prefix, prefix_len, own, seen):
+        """(q, address, stride, B, T, [prefix, groups, prefix_len, own, seen] as arguments, prefix, own caches)."""
+        q, at, stride = self._tokens("q", q, self.heads)
         B, T = q.shape[:2]
-        on.reads(q)
-        q, stride = self._tokens("q", q, H)
         if (prefix is None) != (prefix_len is None) or (own is None) != (seen is None):
             raise ValueError("prefix goes with prefix_len, own with seen")
         p = o = None
-        groups = 1
+        args = [None, 1, None, None, None]
         if prefix is not None:
             groups = prefix[0].shape[0]
             p = self._cache("prefix", *prefix, groups)
-            self._whole("prefix_len", prefix_len, (groups,), torch.int32)
-            on.reads(prefix_len, *(t for t in prefix if t is not None))
+            args[:3] = byref(p), groups, self._whole("prefix_len", prefix_len, (groups,), self._int)
         if own is not None:
             o = self._cache("own", *own, B)
-            self._whole("seen", seen, (B, T), torch.int32)
-            on.reads(seen, *(t for t in own if t is not None))
-        return q, stride, B, T, p, groups, o
+            args[3:] = byref(o), self._whole("seen", seen, (B, T), self._int)
+        return q, at, stride, B, T, args, p, o
 
     def attend(self, q, prefix=None, prefix_len=None, own=None, seen=None, out=None, lse=None, stream=None):
         """Attention of q [B][T][H][D] over the first prefix_len[g] rows of prefix (k, v) [G][P][Hk][D], shared by each
         run of B / G requests, and the first seen[b][t] rows of own (k, v) [B][R][Hk][D]. Returns (out, lse)."""
-        import torch
-        H, D = self.cfg.n_heads, self.cfg.head_dim
-        with OnStream(stream, self.device) as on:
-            q, stride, B, T, p, groups, o = self._sides(on, q, prefix, prefix_len, own, seen)
+        on = self._on(stream)
+        with on or _HERE:
+            x, at, stride, B, T, sides, _, _ = self._sides(q, prefix, prefix_len, own, seen)
+            reads, returns = [q, prefix_len, seen, *(prefix or ()), *(own or ())], []
+            shape = (B, T, self.heads, self.head_dim)
             if out is None:
-                out = torch.empty((B, T, H, D), dtype=self.dtype, device=self.device)
-                on.returns(out)
+                out = self._torch.empty(shape, dtype=self.dtype, device=self.device)
+                returns.append(out)
             else:
-                self._whole("out", out, (B, T, H, D), self.dtype)
-                on.reads(out)
+                reads.append(out)
             if lse is None:
-                lse = torch.empty((B, T, H), dtype=torch.float32, device=self.device)
-                on.returns(lse)
+                lse = self._torch.empty(shape[:3], dtype=self._float, device=self.device)
+                returns.append(lse)
             else:
-                self._whole("lse", lse, (B, T, H), torch.float32)
-                on.reads(lse)
-        jpi_kv_attend(self.handle, q, stride, B, T, p, groups, prefix_len, o, seen, out, lse, stream)
+                reads.append(lse)
+            self._run("jpi_kv_attend", stream, (at, stride, B, T, *sides, self._whole("out", out, shape, self.dtype),
+                                                self._whole("lse", lse, shape[:3], self._float)), on, reads, returns)
         return out, lse
 
     def weigh(self, q, lse, prefix=None, prefix_len=None, own=None, seen=None, w_prefix=None, w_own=None, decay=1.0,
@@ -274,33 +287,32 @@ class KV:
         """Adds the attention weight that q's tokens and heads give to each key of `prefix` (keys [G][P][Hk][D]) and
         `own` (keys [B][R][Hk][D]) to decay times w_prefix [G][Hk][P] and w_own [B][Hk][R] (None: zeros). Returns
         the sums, in out_prefix and out_own (None: new ones, zero where a row holds no key)."""
-        import torch
-        H, K = self.cfg.n_heads, self.cfg.n_kv_heads
-        with OnStream(stream, self.device) as on:
-            q, stride, B, T, p, groups, o = self._sides(on, q, None if prefix is None else (prefix, None), prefix_len,
-                                                        None if own is None else (own, None), seen)
-            self._whole("lse", lse, (B, T, H), torch.float32)
-            on.reads(lse)
-            outs = []
-            for name, cache, n, w, out in (("prefix", p, groups, w_prefix, out_prefix), ("own", o, B, w_own, out_own)):
+        on = self._on(stream)
+        with on or _HERE:
+            x, at, stride, B, T, sides, p, o = self._sides(q, None if prefix is None else (prefix, None), prefix_len,
+                                                           None if own is None else (own, None), seen)
+            reads, returns = [q, lse, prefix, prefix_len, own, seen], []
+            args, outs = [], []
+            for name, cache, n, w, out in (("prefix", p, sides[1], w_prefix, out_prefix), ("own", o, B, w_own, out_own)):
                 if cache is None:
                     if w is not None or out is not None:
                         raise ValueError(f"weights of {name} without {name}")
-                    outs += [None, None]
+                    args += (None, None)
+                    outs.append(None)
                     continue
-                shape = (n, K, cache.rows)
-                if w is not None:
-                    self._whole(f"w_{name}", w, shape, torch.float32)
-                    on.reads(w)
+                shape = (n, self.kv_heads, cache.rows)
                 if out is None:
-                    out = torch.zeros(shape, dtype=torch.float32, device=self.device)
-                    on.returns(out)
+                    out = self._torch.zeros(shape, dtype=self._float, device=self.device)
+                    returns.append(out)
                 else:
-                    self._whole(f"out_{name}", out, shape, torch.float32)
-                    on.reads(out)
-                outs += [w, out]
-        jpi_kv_weigh(self.handle, q, stride, lse, B, T, p, groups, prefix_len, o, seen, decay, *outs, stream)
-        return outs[1], outs[3]
+                    reads.append(out)
+                reads.append(w)
+                args += (None if w is None else self._whole(f"w_{name}", w, shape, self._float),
+                         self._whole(f"out_{name}", out, shape, self._float))
+                outs.append(out)
+            self._run("jpi_kv_weigh", stream, (at, stride, self._whole("lse", lse, (B, T, self.heads), self._float), B, T,
+                                               *sides, decay, *args), on, reads, returns)
+        return outs[0], outs[1]
 
     def evict(self, k, v, w, length, keep, sink=0, recent=0, out_k=None, out_v=None, out_w=None, out_length=None,
               stream=None):
@@ -308,27 +320,24 @@ class KV:
         `recent`, the best of the others by w [L][N][Hk][R]. In place, or into out_k, out_v and out_w of at least `keep`
         rows; the new lengths go to out_length (None: `length` itself). Returns the rows kept, int32 [L][N][Hk][keep],
         -1 behind them."""
-        import torch
-        K = self.cfg.n_kv_heads
         outs = (out_k, out_v, out_w)
-        if any(t is None for t in outs) and any(t is not None for t in outs):
-            raise ValueError("out_k, out_v and out_w go together")
-        if out_k is None:
+        if any(t is None for t in outs):
+            if any(t is not None for t in outs):
+                raise ValueError("out_k, out_v and out_w go together")
             out_k, out_v, out_w = k, v, w
         if out_length is None:
             out_length = length
-        L, N, R = k.shape[:3]
-        with OnStream(stream, self.device) as on:
+        on = self._on(stream)
+        with on or _HERE:
+            L, N, R = k.shape[:3]
             src = self._cache("k, v", k, v, N, L)
             dst = self._cache("out", out_k, out_v, N, L)
-            self._whole("w", w, (L, N, K, R), torch.float32)
-            self._whole("out_w", out_w, (L, N, K, out_k.shape[2]), torch.float32)
-            self._whole("length", length, (N,), torch.int32)
-            self._whole("out_length", out_length, (N,), torch.int32)
-            on.reads(k, v, w, length, out_k, out_v, out_w, out_length)
-            kept = torch.empty((L, N, K, max(keep, 0)), dtype=torch.int32, device=self.device)
-            on.returns(kept)
-        jpi_kv_evict(self.handle, src, w, length, L, N, keep, sink, recent, dst, out_w, out_length, kept, stream)
+            kept = self._torch.empty((L, N, self.kv_heads, max(keep, 0)), dtype=self._int, device=self.device)
+            args = (byref(src), self._whole("w", w, (L, N, self.kv_heads, R), self._float),
+                    self._whole("length", length, (N,), self._int), L, N, keep, sink, recent, byref(dst),
+                    self._whole("out_w", out_w, (L, N, self.kv_heads, dst.rows), self._float),
+                    self._whole("out_length", out_length, (N,), self._int), kept.data_ptr())
+            self._run("jpi_kv_evict", stream, args, on, (k, v, w, length, out_k, out_v, out_w, out_length), (kept,))
         return kept
 
     def device_status(self):
