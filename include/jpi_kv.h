@@ -74,7 +74,7 @@ typedef struct jpi_kv_config {
     int head_dim;     /* D, at most 256; a multiple of 8 (JPI_BF16) or 4 (JPI_FP32)               */
     int max_batch;    /* most requests per call                                                   */
     int max_tokens;   /* most new tokens of one request per call                                  */
-    float scale;      /* of the attention scores; 0: 1 / sqrt(D)                                  */
+    float scale;      /* of the attention scores, 2^-32 .. 2^32; 0: 1 / sqrt(D)                   */
     jpi_precision precision;
 } jpi_kv_config;
 

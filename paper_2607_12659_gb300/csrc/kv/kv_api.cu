@@ -184,7 +184,8 @@ JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* ro
     if (cfg->max_batch < 1 || cfg->max_tokens < 1) return fail(JPI_ERR_INVALID_ARG, "max_batch and max_tokens must be >= 1");
     if (cfg->max_batch > 65535 || (long long)cfg->max_batch * cfg->max_tokens * cfg->n_heads > (1ll << 28))
         return fail(JPI_ERR_SHAPE, "maxima too large");
-    if (!(cfg->scale >= 0.f) || std::isinf(cfg->scale)) return fail(JPI_ERR_INVALID_ARG, "scale must be >= 0 and finite");
+    if (cfg->scale != 0.f && !(cfg->scale >= 0x1p-32f && cfg->scale <= 0x1p32f))
+        return fail(JPI_ERR_INVALID_ARG, "scale must be 0 or in 2^-32 .. 2^32");
     if (rope) JPI_TRY(check_rope(rope, cfg->head_dim));
     jpi_kv_handle* h = new (std::nothrow) jpi_kv_handle();
     if (!h) return fail(JPI_ERR_OOM, "host allocation failed");

@@ -13,6 +13,7 @@
 // values would overflow.
 
 #include "kv_rows.cuh"
+#include "kv_attend.h"
 
 #include <algorithm>
 
@@ -546,6 +547,7 @@ size_t kv_attend_ws_bytes(const jpi_kv_handle* h) {
 }
 
 jpi_status kv_attend_prepare(jpi_kv_handle* h) {
+    JPI_TRY(kv_prefix_prepare(h));
     return h->D <= 64 ? prepare_dim<64>() : h->D <= 128 ? prepare_dim<128>() : prepare_dim<256>();
 }
 
@@ -558,11 +560,20 @@ jpi_status launch_kv_attend(jpi_kv_handle* h, const KvCall& c, void* out, float*
     a.rows = (long long)c.batch * c.tokens * c.H;
     a.po = static_cast<float*>(h->ws);
     a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
+    // Many rows on one prefix go to the tensor-core tiles, its parts first.
+    int splits = 0;
+    const bool tiles = kv_prefix_splits(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), &splits);
+    if (tiles) {
+        a.p.blocks = 0;
+        a.p.splits = splits;
+    }
     if (a.p.blocks + a.o.blocks > 0x7fffffffll) {
         set_error("the call needs more than 2^31 blocks");
         return JPI_ERR_SHAPE;
     }
-    JPI_TRY(h->D <= 64 ? launch_parts<64>(h, a, st) : h->D <= 128 ? launch_parts<128>(h, a, st) : launch_parts<256>(h, a, st));
+    if (tiles) JPI_TRY(launch_kv_prefix_t5(h, c, splits, a.po, a.pml, st));
+    if (a.p.blocks + a.o.blocks > 0)
+        JPI_TRY(h->D <= 64 ? launch_parts<64>(h, a, st) : h->D <= 128 ? launch_parts<128>(h, a, st) : launch_parts<256>(h, a, st));
     const int parts = a.p.splits + a.o.splits;
     const size_t smem = (size_t)((parts + 3) & ~3) * 4 + CB_THREADS * 16;
     if (h->bf16)

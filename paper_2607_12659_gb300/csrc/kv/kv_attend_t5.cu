@@ -1,0 +1,516 @@
+// The prefix side of jpi_kv_attend on tcgen05: 128 query rows of a run (tokens x heads of one KV head) per
+// block over a range of the shared keys, in blocks of 64 keys.
+//   warp 0  one thread: K blocks by bulk tensor copies into a ring of NS slots
+//   warp 1  one thread: V blocks into a ring of their own
+//   warp 2  one thread: S_i = Q K_i^T (M = 128, N = 64, K = D) into one of two TMEM score buffers
+//   warp 3  one thread: O += P_i V_i (M = 128, N = D, K = 64), V read as an MN-major operand
+//   warps 4-11  two threads per query row (its TMEM lane), half of a block's keys each: maximum, 2^x,
+//           probabilities as bf16 to shared memory. O is rescaled only when a block's maximum passes the running one by
+//           more than 8 in log2 units, so that probabilities stay below 2^8.
+// The query rows are gathered by the softmax threads (a run's tokens may lie at any stride and a row
+// tile may begin and end inside a token's heads) straight into tensor memory, columns 384.., as the A operand of the
+// score products, which leaves all of shared memory to keys and values.
+//
+// Probabilities are rounded to bf16 once (2^-9 on average of independent signs): with 128 rows a block there is
+// no time for a second term as in the row kernel, and the result's own rounding to bf16 is as large.
+// The sum l takes them unrounded.
+//
+// Rows of the last key block past the prefix's end may hold anything: their scores are replaced, and their
+// values are cleared in shared memory before the product, since 0 times a NaN would reach every row.
+//
+// Each block leaves a part (unnormalised fp32 rows, (m, l)) for k_kv_combine: rows pass through shared memory
+// (the ring, free by then) and leave by one bulk copy each, contiguous in global memory.
+//
+// Every wait is bounded; a wait that gives up records an error in the handle's word, and its thread waits for
+// nothing more.
+
+#include "kv_rows.cuh"
+#include "kv_attend.h"
+
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+
+namespace jpi {
+namespace {
+
+constexpr int KP_ROWS = 128;
+constexpr int KP_KEYS = 64;
+constexpr int KP_THREADS = 384;
+constexpr uint64_t KP_WAIT_NS = 200ull * 1000 * 1000;
+constexpr float KP_RESCALE = 8.f;   // log2 units
+
+struct PrefixArgs {
+    KvCall c;
+    float c2;            // log2(e) * scale
+    int splits, tiles;   // key ranges, row tiles per run and KV head
+    int at_head, at_row, at_run;   // which of the maps' outer dimensions is which
+    float* po;           // [parts][rows][D]
+    float2* pml;         // [parts][rows]
+    long long rows;
+    int* err;
+};
+
+template <int DP>
+struct KpSmem {
+    static constexpr int NS = DP == 256 ? 3 : DP == 128 ? 5 : 8;
+    static constexpr int KVBYTES = KP_KEYS * DP * 2;
+    static constexpr int STAGE = 2 * KVBYTES;               // ring slot: K, then V
+    static constexpr int PBYTES = KP_ROWS * KP_KEYS * 2;
+    static constexpr int P_OFF = NS * STAGE;                // two P buffers
+    static constexpr int XM_OFF = P_OFF + 2 * PBYTES;       // [2 blocks][2 key halves][128 rows]
+    static constexpr int BAR_OFF = XM_OFF + 4 * KP_ROWS * 4;
+    static constexpr int BYTES = BAR_OFF + 64 + 8 * (4 * NS + 10);
+    static constexpr int OUT_LD = DP * 4 + 16;              // bytes of a staged output row: the pad spreads the banks
+    static_assert(KP_ROWS * OUT_LD <= P_OFF, "staged rows fit the ring");
+    static_assert(BYTES <= 227 * 1024, "fits an SM");
+    static constexpr uint32_t TMEM_O = 128, TMEM_Q = 384, TMEM_COLS = 512;
+};
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const void* tmap, uint64_t* bar, int x, int y, int z, int w) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(ptx::smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(ptx::smem_u32(bar))
+        : "memory");
+}
+// (a - m) c for two scores at a time.
+__device__ __forceinline__ void sub_scale2(float a, float b, uint64_t neg_m2, uint64_t c2, float& x, float& y) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(neg_m2));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(c2));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+}
+__device__ __forceinline__ uint64_t pair2(float a) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(v) : "f"(a));
+    return v;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_constant__ CUtensorMap kmap,
+                                                                const __grid_constant__ CUtensorMap vmap,
+                                                                const __grid_constant__ PrefixArgs a) {
+    using L = KpSmem<DP>;
+    constexpr int NS = L::NS, NDB = DP / 64;
+    constexpr uint32_t IDESC_S = ptx::idesc_bf16_f32(KP_ROWS, KP_KEYS);
+    constexpr uint32_t IDESC_PV = ptx::idesc_bf16_f32(KP_ROWS, DP) | (1u << 16);   // B MN-major
+    extern __shared__ __align__(1024) uint8_t kp_smem[];
+    uint8_t* stages = kp_smem;
+    uint8_t* ps = kp_smem + L::P_OFF;
+    float* xmax = (float*)(kp_smem + L::XM_OFF);
+    uint64_t* bars = (uint64_t*)(kp_smem + L::BAR_OFF);
+    uint64_t* sfull = bars;            // 2: score buffer ready
+    uint64_t* pfull = bars + 2;        // 2: P buffer written
+    uint64_t* odone = bars + 4;        // 2: P V of the block in P buffer b done
+    uint64_t* sfree = bars + 6;        // 2: score buffer has been read
+    uint64_t* qready = bars + 8;       // the query rows are in TMEM
+    uint64_t* kfull = bars + 9;        // NS each
+    uint64_t* vfull = kfull + NS;
+    uint64_t* kempty = vfull + NS;
+    uint64_t* vempty = kempty + NS;
+    uint32_t* tmem_slot = (uint32_t*)(vempty + NS);
+    int* flag = (int*)(tmem_slot + 1);
+
+    const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
+    // Row tiles fastest: the blocks that read the same keys run together.
+    long long w = blockIdx.x;
+    const int tile = (int)(w % a.tiles);
+    w /= a.tiles;
+    const int split = (int)(w % a.splits);
+    w /= a.splits;
+    const int kvh = (int)(w % a.c.K), run = (int)(w / a.c.K);
+    RowTile t;
+    const int toks = a.c.batch / a.c.groups * a.c.tokens;
+    t.tok0 = (long long)run * toks;
+    t.head0 = kvh * a.c.gq;
+    t.R = toks * a.c.gq;
+    t.r0 = tile * KP_ROWS;
+    const int len = min(max(a.c.prefix.len[run], 0), a.c.prefix.rows);
+    const int nb_all = (len + KP_KEYS - 1) / KP_KEYS;
+    const int blk0 = (int)((long long)split * nb_all / a.splits);
+    const int nb = (int)((long long)(split + 1) * nb_all / a.splits) - blk0;
+    if (nb == 0) {   // the prefix is shorter than its splits: the part weighs nothing
+        const int r = t.r0 + tid;
+        if (tid < KP_ROWS && r < t.R) a.pml[split * a.rows + row_index(t, a.c.gq, a.c.H, r)] = make_float2(-INFINITY, 0.f);
+        return;
+    }
+
+    if (warp == 1) {
+        ptx::tmem_alloc(tmem_slot, L::TMEM_COLS);
+        ptx::tmem_relinquish();
+    }
+    if (tid == 0) {
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(&sfull[b], 1);
+            ptx::mbar_init(&pfull[b], 256);
+            ptx::mbar_init(&odone[b], 1);
+            ptx::mbar_init(&sfree[b], 256);
+        }
+        ptx::mbar_init(qready, 256);
+        for (int s = 0; s < NS; ++s) {
+            ptx::mbar_init(&kfull[s], 1);
+            ptx::mbar_init(&vfull[s], 1);
+            ptx::mbar_init(&kempty[s], 1);
+            ptx::mbar_init(&vempty[s], 1);
+        }
+        ptx::fence_mbar_init();
+        *flag = 0;
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp <= 1) {
+        if (ptx::elect_one()) {
+            const bool is_v = warp == 1;
+            uint64_t* fullb = is_v ? vfull : kfull;
+            uint64_t* emptyb = is_v ? vempty : kempty;
+            const CUtensorMap* map = is_v ? &vmap : &kmap;
+            auto coord = [&](int dim, int row) { return dim == a.at_row ? row : dim == a.at_head ? kvh : run; };
+            int issued = 0;
+            for (int i = 0; i < nb; ++i) {
+                const int sl = i % NS;
+                if (i >= NS && !ptx::mbar_wait_bounded(&emptyb[sl], (i / NS - 1) & 1, KP_WAIT_NS)) {
+                    *flag = DEV_TIMEOUT_WEIGHTS;
+                    break;
+                }
+                uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0);
+                ptx::mbar_expect_tx(&fullb[sl], (uint32_t)L::KVBYTES);
+                const int key0 = (blk0 + i) * KP_KEYS;
+                for (int db = 0; db < NDB; ++db)
+                    tma_load_4d(base + db * (KP_KEYS * 128), map, &fullb[sl], db * 64, coord(0, key0), coord(1, key0),
+                                coord(2, key0));
+                issued = i + 1;
+            }
+            if (!ptx::ring_drain(fullb, NS, issued, KP_WAIT_NS)) *flag = DEV_TIMEOUT_WEIGHTS;
+        }
+    } else if (warp == 2) {
+        if (ptx::elect_one()) {
+            const uint32_t sb = ptx::smem_u32(stages);
+            bool good = ptx::mbar_wait_bounded(qready, 0, KP_WAIT_NS);
+            for (int i = 0; i < nb; ++i) {
+                const int sl = i % NS;
+                if (i >= 2 && good) good = ptx::mbar_wait_bounded(&sfree[i & 1], ((i - 2) >> 1) & 1, KP_WAIT_NS);
+                if (good) good = ptx::mbar_wait_bounded(&kfull[sl], (i / NS) & 1, KP_WAIT_NS);
+                ptx::tc_fence_after();
+                if (good) {
+                    const uint64_t kb = ptx::desc_sw128(sb + sl * L::STAGE);
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            ptx::mma_bf16_ta(tmem + (uint32_t)(64 * (i & 1)), tmem + L::TMEM_Q + (uint32_t)(8 * (4 * db + kk)),
+                                             ptx::desc_add(kb, db * (KP_KEYS * 128) + kk * 32), IDESC_S, (db | kk) != 0);
+                }
+                ptx::mma_commit(&sfull[i & 1]);
+                if (i + NS < nb) ptx::mma_commit(&kempty[sl]);
+            }
+            if (!good) *flag = DEV_TIMEOUT_MMA;
+        }
+    } else if (warp == 3) {
+        if (ptx::elect_one()) {
+            const uint32_t sb = ptx::smem_u32(stages), pb = ptx::smem_u32(ps);
+            bool good = true;
+            for (int i = 0; i < nb; ++i) {
+                const int sl = i % NS;
+                if (good) good = ptx::mbar_wait_bounded(&pfull[i & 1], (i >> 1) & 1, KP_WAIT_NS);
+                if (good) good = ptx::mbar_wait_bounded(&vfull[sl], (i / NS) & 1, KP_WAIT_NS);
+                ptx::tc_fence_after();
+                if (good) {
+                    const uint64_t vb = ptx::desc_sw128_mn(sb + sl * L::STAGE + L::KVBYTES, KP_KEYS * 128, 1024);
+                    const uint64_t pbi = ptx::desc_sw128(pb + (uint32_t)((i & 1) * L::PBYTES));
+#pragma unroll
+                    for (int kk = 0; kk < KP_KEYS / 16; ++kk)
+                        ptx::mma_bf16(tmem + L::TMEM_O, ptx::desc_add(pbi, kk * 32), ptx::desc_add(vb, kk * 16 * 128), IDESC_PV,
+                                      (i | kk) != 0);
+                }
+                if (i + NS < nb) ptx::mma_commit(&vempty[sl]);
+                ptx::mma_commit(&odone[i & 1]);
+            }
+            if (!good) *flag = DEV_TIMEOUT_MMA;
+        }
+    } else {
+        const int row = (warp & 3) * 32 + lane, half = (warp - 4) >> 2;
+        const int r = t.r0 + row;
+        const bool valid = r < t.R;
+        const int nvis = valid ? len : 0;
+        const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t pair_bar = 1 + (warp & 3);   // the two warps of these 32 rows
+        float m_used = -INFINITY, l = 0.f;          // m_used is the same in both threads of a row
+        bool good = true;
+        {
+            // Half of the query row to TMEM: column 32 db + 4 c + e holds elements 64 db + 8 c + 2 e, + 1.
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q);
+            if (valid) q += row_token(t, a.c.gq, r) * a.c.q_stride + (long long)(t.head0 + r % a.c.gq) * a.c.D;
+            constexpr int QW = DP / 32;   // 16-column groups (32 elements), half of them per thread
+#pragma unroll
+            for (int k = 0; k < QW / 2; ++k) {
+                const int gr = half * (QW / 2) + k;
+                uint32_t rq[16];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint4 v = kr_ld(q + 32 * gr + 8 * c, valid && 32 * gr + 8 * c < a.c.D);
+                    rq[4 * c] = v.x;
+                    rq[4 * c + 1] = v.y;
+                    rq[4 * c + 2] = v.z;
+                    rq[4 * c + 3] = v.w;
+                }
+                ptx::tmem_st_x16(lane_base + L::TMEM_Q + (uint32_t)(16 * gr), rq);
+            }
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(qready);
+        }
+        constexpr int HK = KP_KEYS / 2;   // keys per thread
+        const uint64_t c2 = pair2(a.c2);
+        const float rescale = KP_RESCALE / a.c2;
+        for (int i = 0; i < nb; ++i) {
+            if (good) good = ptx::mbar_wait_bounded(&sfull[i & 1], (i >> 1) & 1, KP_WAIT_NS);
+            ptx::tc_fence_after();
+            uint32_t s[2][16];
+            {
+                const uint32_t sa = lane_base + (uint32_t)(64 * (i & 1) + HK * half);
+                ptx::tmem_ld_x16(sa, s[0]);
+                ptx::tmem_ld_x16(sa + 16u, s[1]);
+                ptx::tmem_ld_wait();
+                ptx::tc_fence_before();
+                ptx::mbar_arrive(&sfree[i & 1]);
+            }
+            const int vis = nvis - (blk0 + i) * KP_KEYS - HK * half;   // keys of this half block the row sees
+            const bool full = __all_sync(0xffffffffu, vis >= HK);
+            if (!full) {
+#pragma unroll
+                for (int j = 0; j < HK; ++j)
+                    if (j >= vis) s[j >> 4][j & 15] = __float_as_uint(-INFINITY);
+            }
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int j = 0; j < HK; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j >> 4][j & 15]));
+            float mb = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            float* xm = xmax + (i & 1) * 2 * KP_ROWS + row;
+            xm[half * KP_ROWS] = mb;
+            ptx::named_bar_sync(pair_bar, 64);
+            mb = fmaxf(mb, xm[(1 - half) * KP_ROWS]);
+            const bool move = mb > m_used + rescale;
+            const float alpha = !move ? 1.f : m_used == -INFINITY ? 0.f : kr_ex2((m_used - mb) * a.c2);
+            // TMEM accesses are warp-collective: the warp rescales together (its half of the columns), lanes whose
+            // maximum stays put multiply by 1. O is settled once P V of the previous block is done.
+            if (__any_sync(0xffffffffu, move && i > 0 && m_used != -INFINITY)) {
+                if (good) good = ptx::mbar_wait_bounded(&odone[(i - 1) & 1], ((i - 1) >> 1) & 1, KP_WAIT_NS);
+                ptx::tc_fence_after();
+#pragma unroll 1
+                for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 16) {
+                    uint32_t ro[16];
+                    ptx::tmem_ld_x16(lane_base + L::TMEM_O + (uint32_t)c0, ro);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) ro[j] = __float_as_uint(__uint_as_float(ro[j]) * alpha);
+                    ptx::tmem_st_x16(lane_base + L::TMEM_O + (uint32_t)c0, ro);
+                }
+                ptx::tmem_st_wait();
+            }
+            if (move) {
+                l *= alpha;
+                m_used = mb;
+            }
+            // 2^((s - m) c): a hidden key's -inf gives 0, also while the row has seen none at all (m taken as 0).
+            const uint64_t neg_m = pair2(m_used == -INFINITY ? 0.f : -m_used);
+            float l4[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t pk[HK / 2];
+#pragma unroll
+            for (int k = 0; k < HK; k += 2) {
+                float p0, p1;
+                sub_scale2(__uint_as_float(s[k >> 4][k & 15]), __uint_as_float(s[k >> 4][(k + 1) & 15]), neg_m, c2, p0, p1);
+                p0 = kr_ex2(p0);
+                p1 = kr_ex2(p1);
+                l4[(k >> 1) & 3] += p0 + p1;
+                pk[k / 2] = kr_pack(p0, p1);
+            }
+            l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+            // P buffer i mod 2 is free once P V of block i - 2 is done.
+            if (i >= 2 && good) good = ptx::mbar_wait_bounded(&odone[i & 1], ((i - 2) >> 1) & 1, KP_WAIT_NS);
+            ptx::tc_fence_after();
+            uint4* prow = (uint4*)(ps + (i & 1) * L::PBYTES + row * 128);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                prow[(4 * half + c) ^ (row & 7)] = make_uint4(pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]);
+            const int live = len - (blk0 + i) * KP_KEYS;   // the same for the whole block
+            if (live < KP_KEYS) {
+                // Values of rows past the end, as they landed: cleared (a row's 16-byte pieces stay in the row).
+                const int sl = i % NS;
+                if (good) good = ptx::mbar_wait_bounded(&vfull[sl], (i / NS) & 1, KP_WAIT_NS);
+                uint8_t* vb = stages + sl * L::STAGE + L::KVBYTES;
+                for (int e = tid - 128; good && e < (KP_KEYS - live) * NDB * 8; e += 256) {
+                    const int key = live + e / (NDB * 8), p = e % (NDB * 8);
+                    *(uint4*)(vb + (p / 8) * (KP_KEYS * 128) + key * 128 + (p % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+            }
+            ptx::fence_proxy_async_smem();
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(&pfull[i & 1]);
+        }
+        // The row's sum: both halves, in order.
+        float* xl = xmax + (nb & 1) * 2 * KP_ROWS + row;   // not the buffer of the last block's maxima
+        xl[half * KP_ROWS] = l;
+        ptx::named_bar_sync(pair_bar, 64);
+        l = xl[0] + xl[KP_ROWS];
+        // Every P V is done, and with them every read of the ring.
+        if (nb >= 2 && good) good = ptx::mbar_wait_bounded(&odone[(nb - 2) & 1], ((nb - 2) >> 1) & 1, KP_WAIT_NS);
+        if (good) good = ptx::mbar_wait_bounded(&odone[(nb - 1) & 1], ((nb - 1) >> 1) & 1, KP_WAIT_NS);
+        ptx::tc_fence_after();
+        if (!good) *flag = DEV_TIMEOUT_MMA;
+        uint8_t* orow = kp_smem + row * L::OUT_LD;
+#pragma unroll 1
+        for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 32) {
+            uint32_t v[2][16];
+            ptx::tmem_ld_x16(lane_base + L::TMEM_O + (uint32_t)c0, v[0]);
+            ptx::tmem_ld_x16(lane_base + L::TMEM_O + (uint32_t)(c0 + 16), v[1]);
+            ptx::tmem_ld_wait();
+            if (good) {   // a wait that gave up may have left copies on their way into the ring
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    *(uint4*)(orow + (c0 + 4 * k) * 4) = make_uint4(v[k >> 2][4 * (k & 3)], v[k >> 2][4 * (k & 3) + 1],
+                                                                   v[k >> 2][4 * (k & 3) + 2], v[k >> 2][4 * (k & 3) + 3]);
+            }
+        }
+        ptx::fence_proxy_async_smem();
+        ptx::named_bar_sync(pair_bar, 64);
+        if (half == 0 && valid) {
+            const long long row_out = split * a.rows + row_index(t, a.c.gq, a.c.H, r);
+            a.pml[row_out] = make_float2(m_used, l);
+            if (good) {
+                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.po + row_out * a.c.D),
+                             "r"(ptx::smem_u32(orow)), "r"(a.c.D * 4)
+                             : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            }
+        }
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    if (tid == 0 && *flag != 0) atomicCAS(a.err, 0, *flag);
+    if (warp == 1) ptx::tmem_dealloc(tmem, L::TMEM_COLS);
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        cudaDriverEntryPointQueryResult q;
+        void* p = nullptr;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return (PFN_cuTensorMapEncodeTiled_v12000)p;
+    }();
+    return fn;
+}
+
+// The outer dimensions of the prefix's maps: heads, rows and runs by ascending stride, those of size 1 last. Maps
+// are documented for strides that are multiples of the one before, and below 2^40 bytes: false for a cache of other
+// strides, which the row kernel takes.
+struct MapDims {
+    cuuint64_t size[3], stride[3];
+    int at_head = 0, at_row = 0, at_run = 0;
+};
+bool map_dims(const KvCall& c, MapDims* m) {
+    struct Dim {
+        long long stride;
+        int size, id;
+    } d[3] = {{c.prefix.hs, c.K, 0}, {c.prefix.rs, c.prefix.rows, 1}, {c.prefix.cs, c.groups, 2}};
+    std::stable_sort(d, d + 3, [](const Dim& x, const Dim& y) {
+        if ((x.size > 1) != (y.size > 1)) return x.size > 1;
+        return x.size > 1 && x.stride < y.stride;
+    });
+    long long last = (c.D + 7) / 8 * 8;
+    for (int i = 0; i < 3; ++i) {
+        const long long st = d[i].size > 1 ? d[i].stride : last;
+        if (i > 0 && st % last) return false;
+        if (st >= (1ll << 39)) return false;
+        last = st;
+        m->size[i] = (cuuint64_t)d[i].size;
+        m->stride[i] = (cuuint64_t)st * 2;
+        (d[i].id == 0 ? m->at_head : d[i].id == 1 ? m->at_row : m->at_run) = i;
+    }
+    return true;
+}
+
+bool make_map(const KvCall& c, const MapDims& m, const void* base, CUtensorMap* map) {
+    auto enc = encode_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.D, m.size[0], m.size[1], m.size[2]};
+    cuuint32_t box[4] = {64, 1, 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    box[1 + m.at_row] = KP_KEYS;
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, m.stride, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DP>
+jpi_status launch_dim(const PrefixArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st) {
+    const long long blocks = (long long)a.tiles * a.splits * a.c.K * a.c.groups;
+    k_kv_prefix_t5<DP><<<(unsigned)blocks, KP_THREADS, KpSmem<DP>::BYTES, st>>>(km, vm, a);
+    JPI_CUDA_TRY(cudaGetLastError());
+    return JPI_OK;
+}
+
+}  // namespace
+
+jpi_status kv_prefix_prepare(jpi_kv_handle* h) {
+    if (!h->bf16 || h->D < 64) return JPI_OK;
+    if (!encode_fn()) {
+        set_error("cuTensorMapEncodeTiled is unavailable from the driver");
+        return JPI_ERR_CUDA;
+    }
+    if (h->D <= 64)
+        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<64>::BYTES));
+    else if (h->D <= 128)
+        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<128>::BYTES));
+    else
+        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<256>::BYTES));
+    return JPI_OK;
+}
+
+bool kv_prefix_splits(const jpi_kv_handle* h, const KvCall& c, long long room, int* splits) {
+    if (!h->bf16 || c.D < 64 || c.prefix.rows == 0) return false;
+    const long long R = (long long)(c.batch / c.groups) * c.tokens * c.gq;
+    if (R < 32) return false;
+    MapDims m;
+    if (!map_dims(c, &m)) return false;
+    const long long tiles = (R + KP_ROWS - 1) / KP_ROWS, blocks = tiles * c.K * c.groups;
+    const long long nb = (c.prefix.rows + KP_KEYS - 1) / KP_KEYS;
+    long long s = std::max(1ll, h->num_sms / blocks);
+    *splits = (int)std::max(1ll, std::min({s, room, nb}));
+    return blocks * *splits <= 0x7fffffffll;
+}
+
+jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, float* po, float2* pml, cudaStream_t st) {
+    PrefixArgs a;
+    a.c = c;
+    a.c2 = KR_LOG2E * c.scale;
+    a.splits = splits;
+    const long long R = (long long)(c.batch / c.groups) * c.tokens * c.gq;
+    a.tiles = (int)((R + KP_ROWS - 1) / KP_ROWS);
+    a.po = po;
+    a.pml = pml;
+    a.rows = (long long)c.batch * c.tokens * c.H;
+    a.err = h->dev_err;
+    MapDims m;
+    CUtensorMap km, vm;
+    if (!map_dims(c, &m) || !make_map(c, m, c.prefix.k, &km) || !make_map(c, m, c.prefix.v, &vm)) {
+        set_error("cuTensorMapEncodeTiled refused the prefix");
+        return JPI_ERR_CUDA;
+    }
+    a.at_head = m.at_head;
+    a.at_row = m.at_row;
+    a.at_run = m.at_run;
+    return c.D <= 64 ? launch_dim<64>(a, km, vm, st) : c.D <= 128 ? launch_dim<128>(a, km, vm, st) : launch_dim<256>(a, km, vm, st);
+}
+
+}  // namespace jpi

@@ -109,12 +109,14 @@ class Rope:
 
 def cache_of(k, v=None, layers=False) -> jpi_kv_cache:
     """The jpi_kv_cache of tensors [caches][rows][KV heads][head dim], or with `layers` another dimension before them."""
-    s, n = k.stride(), 5 if layers else 4
-    if len(s) != n or (v is not None and (v.stride() != s or v.shape != k.shape or v.dtype is not k.dtype)):
-        raise ValueError(f"k and v must be {n}-dimensional caches of one shape, type and strides")
+    s = k.stride()
+    if v is not None and (v.stride() != s or v.shape != k.shape or v.dtype is not k.dtype):
+        raise ValueError("k and v must be caches of one shape, type and strides")
+    if len(s) != (5 if layers else 4):
+        raise ValueError("a cache is [caches][rows][KV heads][head dim], with layers [layers] before that")
     if s[-1] != 1 and k.shape[-1] > 1:
         raise ValueError("a head's elements must be contiguous")
-    return jpi_kv_cache(k.data_ptr(), v.data_ptr() if v is not None else None, s[-4], s[-3], s[-2], s[0] if layers else 0,
+    return jpi_kv_cache(k.data_ptr(), None if v is None else v.data_ptr(), s[-4], s[-3], s[-2], s[0] if layers else 0,
                         k.shape[-3])
 
 
@@ -133,7 +135,7 @@ class KV:
         self.handle = jpi_kv_create(self.cfg, rope.c() if rope is not None else None)
         self.index = torch.cuda.current_device()
         self.device = torch.device("cuda", self.index)
-        self._torch, self._int, self._float = torch, torch.int32, torch.float32
+        self._torch, self._int, self._float, self._lib = torch, torch.int32, torch.float32, load()
 
     def close(self):
         if self.handle:
@@ -164,14 +166,15 @@ class KV:
         return t.data_ptr()
 
     def _cache(self, name, k, v, n, layers=None):
-        want = (self.kv_heads, self.head_dim)
-        lead = (n,) if layers is None else (layers, n)
-        for t in (k, v):
-            if t is not None:
-                self._data(name, t, self.dtype)
-                if t.shape[:-3] != lead or t.shape[-2:] != want:
-                    raise ValueError(f"{name} has shape {tuple(t.shape)}, not {lead} x rows x {want}")
-        return cache_of(k, v, layers is not None)
+        self._data(name, k, self.dtype)
+        if v is not None:
+            self._data(name, v, self.dtype)
+        c = cache_of(k, v, layers is not None)      # v has k's shape
+        shape = k.shape
+        if shape[-1] != self.head_dim or shape[-2] != self.kv_heads or shape[-4] != n or (layers is not None and shape[0] != layers):
+            raise ValueError(f"{name} has shape {tuple(shape)}, not {'' if layers is None else f'[{layers}]'}[{n}][rows]"
+                             f"[{self.kv_heads}][{self.head_dim}]")
+        return c
 
     def _tokens(self, name, t, heads):
         """(tensor, address, token stride): new tokens [batch][tokens][heads][D], one row of `stride` elements each."""
@@ -189,15 +192,19 @@ class KV:
 
     def _on(self, stream):
         """Torch's side of a call on another stream than the current one (None: this one)."""
-        return None if stream is None else OnStream(stream, self.device)
+        return _HERE if stream is None else OnStream(stream, self.device)
 
     def _run(self, fn, stream, args, on, reads, returns):
         """The C call, with what it reads and returns kept by the stream that it runs on."""
         if on is not None:
             on.reads(*(t for t in reads if t is not None))
             on.returns(*returns)
-        lib = load()
-        _check(getattr(lib, fn)(self.handle, *args, _stream(stream)), fn)
+            raw = _stream(stream)
+        else:
+            raw = self._torch._C._cuda_getCurrentRawStream(self.index)
+        status = getattr(self._lib, fn)(self.handle, *args, raw)
+        if status:
+            _check(status, fn)
 
     def append(self, q, k, v, positions, rows, cache_k=None, cache_v=None, q_out=None, stream=None):
         """Codes q [B][T][H][D] and k [B][T][Hk][D] for `positions` (int32 [B][T]) and writes k and v into `rows`
@@ -205,8 +212,7 @@ class KV:
         with v and the caches may be None."""
         if q is None and k is None:
             raise ValueError("neither q nor k is given")
-        on = self._on(stream)
-        with on or _HERE:
+        with self._on(stream) as on:
             lead = (q if q is not None else k).shape[:2]
             B, T = lead
             args, fresh = [], []
@@ -263,8 +269,7 @@ class KV:
     def attend(self, q, prefix=None, prefix_len=None, own=None, seen=None, out=None, lse=None, stream=None):
         """Attention of q [B][T][H][D] over the first prefix_len[g] rows of prefix (k, v) [G][P][Hk][D], shared by each
         run of B / G requests, and the first seen[b][t] rows of own (k, v) [B][R][Hk][D]. Returns (out, lse)."""
-        on = self._on(stream)
-        with on or _HERE:
+        with self._on(stream) as on:
             x, at, stride, B, T, sides, _, _ = self._sides(q, prefix, prefix_len, own, seen)
             reads, returns = [q, prefix_len, seen, *(prefix or ()), *(own or ())], []
             shape = (B, T, self.heads, self.head_dim)
@@ -287,8 +292,7 @@ class KV:
         """Adds the attention weight that q's tokens and heads give to each key of `prefix` (keys [G][P][Hk][D]) and
         `own` (keys [B][R][Hk][D]) to decay times w_prefix [G][Hk][P] and w_own [B][Hk][R] (None: zeros). Returns
         the sums, in out_prefix and out_own (None: new ones, zero where a row holds no key)."""
-        on = self._on(stream)
-        with on or _HERE:
+        with self._on(stream) as on:
             x, at, stride, B, T, sides, p, o = self._sides(q, None if prefix is None else (prefix, None), prefix_len,
                                                            None if own is None else (own, None), seen)
             reads, returns = [q, lse, prefix, prefix_len, own, seen], []
@@ -327,8 +331,7 @@ class KV:
             out_k, out_v, out_w = k, v, w
         if out_length is None:
             out_length = length
-        on = self._on(stream)
-        with on or _HERE:
+        with self._on(stream) as on:
             L, N, R = k.shape[:3]
             src = self._cache("k, v", k, v, N, L)
             dst = self._cache("out", out_k, out_v, N, L)
