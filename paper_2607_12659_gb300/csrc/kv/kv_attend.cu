@@ -5,12 +5,17 @@
 // cache. A prefix is read once for all its requests: their query rows are one matrix.
 //
 // The softmax is computed in parts: every part (a range of keys of one side) keeps a running maximum m and
-// sum l per row and an unnormalised output, all fp32, and k_kv_combine joins them,
+// sum l per row and an unnormalised output, all fp32, and they are joined as
 //   o = sum_s w_s O_s / sum_s w_s l_s,  w_s = exp(scale (m_s - M)),
 // in part order, so that a result does not depend on which block finished first. A part that saw no key
 // has m = -inf and weighs nothing; a row of only such parts is zero. Maxima are those of the unscaled
 // products, and the difference is scaled, not the product: log2(e) times a score near the type's largest
 // values would overflow.
+//
+// Two launches: the prefix's parts (many rows: kv_attend_t5.cu, few: the row kernels here), and the row kernel
+// over the requests' own rows, which joins a row's prefix parts to its own result and writes it. The second starts
+// while the first runs and waits for it only before that. Where a row has many prefix parts, or its own rows are
+// split too (few requests with long caches) or absent, k_kv_combine joins the parts over all SMs instead.
 
 #include "kv_rows.cuh"
 #include "kv_attend.h"
@@ -20,10 +25,12 @@
 namespace jpi {
 namespace {
 
-constexpr int AT_WARPS = 8;
+constexpr int AT_WARPS = 4;
 constexpr int AT_THREADS = 32 * AT_WARPS;
+constexpr int AT_JOIN = 4;   // most prefix parts that the own rows' kernel joins
 
-// How one side is dealt to blocks: `wr` warps of a block take different row tiles and 8 / wr different keys.
+// How one side is dealt to blocks: `wr` warps of a block take different row tiles and AT_WARPS / wr
+// different keys.
 struct SidePlan {
     int wr = 1, wk = AT_WARPS;
     int tiles = 0;        // blocks of wr row tiles per cache and KV head
@@ -38,6 +45,9 @@ struct AttendArgs {
     float2* pml;          // [parts][rows] (m, l), m unscaled
     float c2;             // log2(e) * scale
     long long rows;       // batch * tokens * H
+    void* out;
+    float* lse;
+    int late;             // parts that are another kernel's: wait for it before they are read
 };
 
 // The block's piece of work: side, cache, KV head, row tile and key split.
@@ -78,47 +88,145 @@ struct MergeSmem {
     static constexpr int BYTES = AT_WARPS * WARP_FLOATS * 4;
 };
 
-// Joins the key warps of each row tile (their outputs and (m, l) are in shared memory) and writes the part.
+// One row's elements as a warp holds them: lane's float4 i is d = 4 lane + 128 i.
 template <int DP>
+struct RowAcc {
+    static constexpr int NI = (DP + 127) / 128;
+    float4 o[NI];
+    float m, l;
+    __device__ __forceinline__ void add(float w, const float4 (&v)[NI]) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            o[i].x = fmaf(w, v[i].x, o[i].x);
+            o[i].y = fmaf(w, v[i].y, o[i].y);
+            o[i].z = fmaf(w, v[i].z, o[i].z);
+            o[i].w = fmaf(w, v[i].w, o[i].w);
+        }
+    }
+};
+
+// Joins parts first, first + step, .. of a row's `parts` to what `r` holds, all relative to the largest maximum
+// of the row (which r.m becomes). The loads of JOIN parts are in flight together: they are made whether the part
+// weighs anything or not (its memory is the workspace's), and a part of no weight, which may never have been
+// written, is replaced by zeros.
+template <int DP>
+__device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, long long row, int parts, int first, int step,
+                                           int lane) {
+    constexpr int NI = RowAcc<DP>::NI, JOIN = 16 / NI;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < parts) ml = __ldcg(&a.pml[lane * a.rows + row]);
+    float M = fmaxf(r.m, ml.x);
+    for (int p = 32 + lane; p < parts; p += 32) M = fmaxf(M, __ldcg(&a.pml[p * a.rows + row]).x);
+#pragma unroll
+    for (int e = 16; e > 0; e >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, e));
+    const float w0 = r.m == -INFINITY ? 0.f : kr_ex2((r.m - M) * a.c2);
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) r.o[i] = make_float4(r.o[i].x * w0, r.o[i].y * w0, r.o[i].z * w0, r.o[i].w * w0);
+    int d[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) d[i] = 4 * lane + 128 * i < a.c.D ? 4 * lane + 128 * i : 0;
+    for (int p0 = 0; p0 < parts; p0 += 32) {
+        if (p0 > 0) {
+            ml = make_float2(-INFINITY, 0.f);
+            if (p0 + lane < parts) ml = __ldcg(&a.pml[(p0 + lane) * a.rows + row]);
+        }
+        const float w = ml.x == -INFINITY ? 0.f : kr_ex2((ml.x - M) * a.c2);
+        if ((p0 + lane) % step == first) l += w * ml.y;   // (w = 0 past the parts)
+        const int n = min(32, parts - p0);
+        for (int k0 = first; k0 < n; k0 += JOIN * step) {   // step divides 32
+            float4 v[JOIN][NI];
+            float wk[JOIN];
+#pragma unroll
+            for (int k = 0; k < JOIN; ++k) {
+                const int q = min(k0 + k * step, n - 1);
+                const float* src = a.po + ((p0 + q) * a.rows + row) * a.c.D;
+                wk[k] = __shfl_sync(0xffffffffu, w, q);
+                if (k0 + k * step >= n) wk[k] = 0.f;
+#pragma unroll
+                for (int i = 0; i < NI; ++i) v[k][i] = __ldcg((const float4*)(src + d[i]));
+            }
+#pragma unroll
+            for (int k = 0; k < JOIN; ++k) {
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+                    if (wk[k] == 0.f) v[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                r.add(wk[k], v[k]);
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 16; e > 0; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
+    r.l = r.l * w0 + l;
+    r.m = M;
+}
+
+// The row's result from its joined sums.
+template <int DP, typename E>
+__device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>& r, long long row, int lane) {
+    const float inv = r.l > 0.f ? 1.f / r.l : 0.f;   // (a NaN sum comes with NaN outputs)
+    E* out = static_cast<E*>(a.out) + row * a.c.D;
+#pragma unroll
+    for (int i = 0; i < RowAcc<DP>::NI; ++i) {
+        const int d = 4 * lane + 128 * i;
+        if (d >= a.c.D) continue;
+        const float4 v = make_float4(r.o[i].x * inv, r.o[i].y * inv, r.o[i].z * inv, r.o[i].w * inv);
+        if constexpr (sizeof(E) == 2)
+            *(uint2*)(out + d) = make_uint2(kr_pack(v.x, v.y), kr_pack(v.z, v.w));
+        else
+            *(float4*)(out + d) = v;
+    }
+    if (lane == 0 && a.lse) a.lse[row] = r.m == -INFINITY ? -INFINITY : fmaf(r.m, a.c.scale, logf(r.l));
+}
+
+// Joins the key warps of each row tile (their outputs and (m, l) are in shared memory) and writes the part, or, where
+// the block's keys are the last of its rows, the result.
+template <int DP, typename E>
 __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece& x, const SidePlan& s, float* sm, int warp,
                                                 int lane) {
     using M = MergeSmem<DP>;
+    constexpr int NI = RowAcc<DP>::NI;
     __syncthreads();
+    const bool last = a.out != nullptr;
+    if (a.late) ptx::grid_dep_wait();
     // Every warp takes rows (its index among the key warps) + n nwk of its row tile.
     const float* tile = sm + (warp / s.wk) * s.wk * M::WARP_FLOATS;
     for (int rr = x.wk; rr < KR_ROWS; rr += x.nwk) {
         const int r = x.t.r0 + rr;
         if (r >= x.t.R) continue;
-        float m = -INFINITY;
-        for (int k = 0; k < x.nwk; ++k) m = fmaxf(m, tile[k * M::WARP_FLOATS + KR_ROWS * M::LD + 2 * rr]);
-        float l = 0.f;
-        const long long row = (long long)x.part * a.rows + row_index(x.t, a.c.gq, a.c.H, r);
-        float4 o[DP / 128 + (DP % 128 != 0)];
+        const long long row = row_index(x.t, a.c.gq, a.c.H, r);
+        RowAcc<DP> acc;
+        acc.m = -INFINITY;
+        acc.l = 0.f;
+        for (int k = 0; k < x.nwk; ++k) acc.m = fmaxf(acc.m, tile[k * M::WARP_FLOATS + KR_ROWS * M::LD + 2 * rr]);
 #pragma unroll
-        for (int i = 0; i < (DP + 127) / 128; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k = 0; k < x.nwk; ++k) {
             const float* f = tile + k * M::WARP_FLOATS;
             const float mk = f[KR_ROWS * M::LD + 2 * rr];
-            const float w = mk == -INFINITY ? 0.f : kr_ex2((mk - m) * a.c2);
-            l += w * f[KR_ROWS * M::LD + 2 * rr + 1];
+            if (mk == -INFINITY) continue;
+            const float w = kr_ex2((mk - acc.m) * a.c2);
+            acc.l += w * f[KR_ROWS * M::LD + 2 * rr + 1];
+            float4 v[NI];
 #pragma unroll
-            for (int i = 0; i < (DP + 127) / 128; ++i) {
+            for (int i = 0; i < NI; ++i) {
                 const int d = 4 * lane + 128 * i;
-                if (d < DP) {
-                    const float4 v = *(const float4*)(f + rr * M::LD + d);
-                    o[i].x = fmaf(w, v.x, o[i].x);
-                    o[i].y = fmaf(w, v.y, o[i].y);
-                    o[i].z = fmaf(w, v.z, o[i].z);
-                    o[i].w = fmaf(w, v.w, o[i].w);
-                }
+                v[i] = d < DP ? *(const float4*)(f + rr * M::LD + d) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
+            acc.add(w, v);
         }
-        if (lane == 0) a.pml[row] = make_float2(m, l);
-        if (m != -INFINITY) {
+        if (last) {
+            if (a.p.splits > 0) join_parts<DP>(a, acc, row, a.p.splits, 0, 1, lane);
+            write_row<DP, E>(a, acc, row, lane);
+            continue;
+        }
+        const long long at = x.part * a.rows + row;
+        if (lane == 0) a.pml[at] = make_float2(acc.m, acc.l);
+        if (acc.m != -INFINITY) {
 #pragma unroll
-            for (int i = 0; i < (DP + 127) / 128; ++i) {
+            for (int i = 0; i < NI; ++i) {
                 const int d = 4 * lane + 128 * i;
-                if (d < a.c.D) *(float4*)(a.po + row * a.c.D + d) = o[i];
+                if (d < a.c.D) *(float4*)(a.po + at * a.c.D + d) = acc.o[i];
             }
         }
     }
@@ -129,12 +237,13 @@ __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece
 // that its error stays that of fp32 sums: the products are bound by the loads of keys and values, and the
 // second term costs no time there.
 template <int DP>
-__global__ void __launch_bounds__(AT_THREADS, 1) k_kv_attend_mma(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(AT_THREADS, 2) k_kv_attend_mma(const __grid_constant__ AttendArgs a) {
     extern __shared__ __align__(16) float kv_smem[];
     constexpr int NC = DP / 32;    // chunk groups of a key
     constexpr int NV = DP / 64;    // chunk groups of a value row
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, j = lane & 3;
+    ptx::grid_dep_launch();
     const Piece x = piece_of(a, warp);
     const SidePlan& sp = x.prefix ? a.p : a.o;
     const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
@@ -307,7 +416,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_kv_attend_mma(const __grid_co
         ml[2] = m1;
         ml[3] = l1;
     }
-    merge_and_write<DP>(a, x, sp, kv_smem, warp, lane);
+    merge_and_write<DP, __nv_bfloat16>(a, x, sp, kv_smem, warp, lane);
 }
 
 // fp32 on CUDA cores: one warp = 8 query rows over 32-key blocks. Scores with a key per lane, the
@@ -316,6 +425,7 @@ template <int DP>
 __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_constant__ AttendArgs a) {
     extern __shared__ __align__(16) float kv_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    ptx::grid_dep_launch();
     const Piece x = piece_of(a, warp);
     const SidePlan& sp = x.prefix ? a.p : a.o;
     const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
@@ -425,73 +535,39 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
             f[KR_ROWS * MergeSmem<DP>::LD + 2 * r + 1] = l[r];
         }
     }
-    merge_and_write<DP>(a, x, sp, kv_smem, warp, lane);
+    merge_and_write<DP, float>(a, x, sp, kv_smem, warp, lane);
 }
 
-// Joins the parts of a row: one block per row, D / 4 threads per group of parts.
-constexpr int CB_THREADS = 128;
-template <typename E>
-__global__ void __launch_bounds__(CB_THREADS) k_kv_combine(const float* __restrict__ po, const float2* __restrict__ pml,
-                                                           long long rows, int parts, int D, float scale, E* out, float* lse) {
-    extern __shared__ __align__(16) float kv_smem[];   // [parts] weights, then [groups][D]
-    __shared__ float red[CB_THREADS / 32];
-    const int t = threadIdx.x;
-    const long long row = blockIdx.x;
-    float m = -INFINITY;
-    for (int p = t; p < parts; p += CB_THREADS) m = fmaxf(m, pml[p * rows + row].x);
+// Joins the parts of all rows: `wpr` warps (1, 2 or 4) a row, each with every wpr-th part.
+template <int DP, typename E>
+__global__ void __launch_bounds__(AT_THREADS) k_kv_combine(const __grid_constant__ AttendArgs a, int wpr) {
+    __shared__ float4 so[AT_WARPS][RowAcc<DP>::NI][32];
+    __shared__ float sl[AT_WARPS];
+    constexpr int NI = RowAcc<DP>::NI;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp % wpr;
+    const long long row = ((long long)blockIdx.x * AT_WARPS + warp) / wpr;
+    ptx::grid_dep_wait();
+    RowAcc<DP> acc;
+    acc.m = -INFINITY;
+    acc.l = 0.f;
 #pragma unroll
-    for (int e = 16; e > 0; e >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, e));
-    if ((t & 31) == 0) red[t >> 5] = m;
-    __syncthreads();
-    m = red[0];
+    for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row < a.rows) join_parts<DP>(a, acc, row, a.p.splits + a.o.splits, first, wpr, lane);
+    if (wpr > 1) {
 #pragma unroll
-    for (int i = 1; i < CB_THREADS / 32; ++i) m = fmaxf(m, red[i]);
-    __syncthreads();
-    float l = 0.f;
-    for (int p = t; p < parts; p += CB_THREADS) {
-        const float2 v = pml[p * rows + row];
-        const float w = v.x == -INFINITY ? 0.f : kr_ex2((v.x - m) * (KR_LOG2E * scale));
-        kv_smem[p] = w;
-        l += w * v.y;
-    }
-#pragma unroll
-    for (int e = 16; e > 0; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
-    if ((t & 31) == 0) red[t >> 5] = l;
-    __syncthreads();
-    l = red[0];
-#pragma unroll
-    for (int i = 1; i < CB_THREADS / 32; ++i) l += red[i];
-    if (t == 0 && lse) lse[row] = m == -INFINITY ? -INFINITY : fmaf(m, scale, logf(l));
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    const int lanes = D / 4, groups = CB_THREADS / lanes, gr = t / lanes, d = 4 * (t % lanes);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (gr < groups)
-        for (int p = gr; p < parts; p += groups) {
-            const float w = kv_smem[p];
-            if (w > 0.f) {
-                const float4 v = *(const float4*)(po + (p * rows + row) * D + d);
-                o.x = fmaf(w, v.x, o.x);
-                o.y = fmaf(w, v.y, o.y);
-                o.z = fmaf(w, v.z, o.z);
-                o.w = fmaf(w, v.w, o.w);
-            }
-        }
-    float4* sums = reinterpret_cast<float4*>(kv_smem + ((parts + 3) & ~3));
-    if (groups > 1) {
-        if (gr < groups) sums[gr * lanes + t % lanes] = o;
+        for (int i = 0; i < NI; ++i) so[warp][i][lane] = acc.o[i];
+        if (lane == 0) sl[warp] = acc.l;
         __syncthreads();
-        if (gr == 0)
-            for (int i = 1; i < groups; ++i) {
-                const float4 v = sums[i * lanes + t];
-                o = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
-            }
+        if (first != 0) return;
+        for (int k = 1; k < wpr; ++k) {
+            float4 v[NI];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) v[i] = so[warp + k][i][lane];
+            acc.add(1.f, v);
+            acc.l += sl[warp + k];
+        }
     }
-    if (gr == 0) {
-        if constexpr (sizeof(E) == 2)
-            *(uint2*)(out + row * D + d) = make_uint2(kr_pack(o.x * inv, o.y * inv), kr_pack(o.z * inv, o.w * inv));
-        else
-            *(float4*)(out + row * D + d) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    }
+    if (row < a.rows) write_row<DP, E>(a, acc, row, lane);
 }
 
 // Rows of partial outputs the workspace holds.
@@ -500,8 +576,8 @@ long long ws_rows(const jpi_kv_handle* h) {
     return 2 * rows + 512ll * h->num_sms;
 }
 
-// A side's key splits: enough blocks for the SMs, as long as a block keeps at least `least` keys and the parts
-// fit their half of the workspace.
+// A side's key splits: enough blocks for two on every SM, as long as a block keeps at least `least` keys a warp
+// and the parts fit their half of the workspace.
 SidePlan plan_side(const jpi_kv_handle* h, const KvCall& c, bool prefix, int least) {
     SidePlan s;
     const KvSide& side = prefix ? c.prefix : c.own;
@@ -515,22 +591,61 @@ SidePlan plan_side(const jpi_kv_handle* h, const KvCall& c, bool prefix, int lea
     s.tiles = (int)((rt + s.wr - 1) / s.wr);
     const long long blocks = (long long)caches * c.K * s.tiles, rows = (long long)c.batch * c.tokens * c.H;
     const long long room = std::max(1ll, (ws_rows(h) / 2) / rows);
-    long long splits = (h->num_sms + blocks - 1) / blocks;
+    long long splits = 2ll * h->num_sms / blocks;
     splits = std::min({splits, room, (long long)(side.rows + least * s.wk - 1) / (least * s.wk)});
     s.splits = (int)std::max(1ll, splits);
     s.blocks = blocks * s.splits;
     return s;
 }
 
-template <int DP>
-jpi_status launch_parts(const jpi_kv_handle* h, const AttendArgs& a, cudaStream_t st) {
-    const unsigned grid = (unsigned)(a.p.blocks + a.o.blocks);
-    if (h->bf16)
-        k_kv_attend_mma<DP><<<grid, AT_THREADS, MergeSmem<DP>::BYTES, st>>>(a);
-    else
-        k_kv_attend_f32<DP><<<grid, AT_THREADS, MergeSmem<DP>::BYTES, st>>>(a);
-    JPI_CUDA_TRY(cudaGetLastError());
+// A launch that starts while the one before it runs (and waits for it where it says so), or an ordinary one.
+template <typename... Params, typename... Args>
+jpi_status start(void (*kernel)(Params...), long long grid, int threads, size_t smem, bool early, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = early ? 1 : 0;
+    JPI_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     return JPI_OK;
+}
+
+template <int DP>
+jpi_status launch_dim(jpi_kv_handle* h, AttendArgs a, bool tiles, void* out, float* lse, cudaStream_t st) {
+    auto rows = [&](const AttendArgs& x, bool early) {
+        const long long grid = x.p.blocks + x.o.blocks;
+        return h->bf16 ? start(k_kv_attend_mma<DP>, grid, AT_THREADS, MergeSmem<DP>::BYTES, early, st, x)
+                       : start(k_kv_attend_f32<DP>, grid, AT_THREADS, MergeSmem<DP>::BYTES, early, st, x);
+    };
+    a.out = nullptr;
+    a.lse = lse;
+    a.late = 0;
+    // The own rows finish the call where they are not split.
+    const bool own_last = a.o.splits == 1 && a.p.splits <= AT_JOIN;
+    AttendArgs first = a;
+    if (tiles) first.p.blocks = 0;
+    if (own_last) first.o.blocks = 0;
+    if (tiles) JPI_TRY(launch_kv_prefix_t5(h, a.c, a.p.splits, a.po, a.pml, st));
+    const bool parts = first.p.blocks + first.o.blocks > 0;
+    if (parts) {
+        first.late = tiles;   // (it ends after the tiles, so that what waits for it has both)
+        JPI_TRY(rows(first, tiles));
+    }
+    a.out = out;
+    if (own_last) {
+        a.p.blocks = 0;
+        a.late = tiles || parts;
+        return rows(a, a.late);
+    }
+    const int n = a.p.splits + a.o.splits, wpr = n > 16 ? 4 : n > 4 ? 2 : 1;
+    const long long grid = (a.rows * wpr + AT_WARPS - 1) / AT_WARPS;
+    return h->bf16 ? start(k_kv_combine<DP, __nv_bfloat16>, grid, AT_THREADS, 0, true, st, a, wpr)
+                   : start(k_kv_combine<DP, float>, grid, AT_THREADS, 0, true, st, a, wpr);
 }
 
 template <int DP>
@@ -552,7 +667,7 @@ jpi_status kv_attend_prepare(jpi_kv_handle* h) {
 }
 
 jpi_status launch_kv_attend(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, cudaStream_t st) {
-    AttendArgs a;
+    AttendArgs a = {};
     a.c = c;
     a.p = plan_side(h, c, true, h->bf16 ? KR_KEYS : 32);
     a.o = plan_side(h, c, false, h->bf16 ? KR_KEYS : 32);
@@ -560,29 +675,16 @@ jpi_status launch_kv_attend(jpi_kv_handle* h, const KvCall& c, void* out, float*
     a.rows = (long long)c.batch * c.tokens * c.H;
     a.po = static_cast<float*>(h->ws);
     a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
-    // Many rows on one prefix go to the tensor-core tiles, its parts first.
+    // Many rows on one prefix go to the tensor-core tiles.
     int splits = 0;
     const bool tiles = kv_prefix_splits(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), &splits);
-    if (tiles) {
-        a.p.blocks = 0;
-        a.p.splits = splits;
-    }
+    if (tiles) a.p.splits = splits;
     if (a.p.blocks + a.o.blocks > 0x7fffffffll) {
         set_error("the call needs more than 2^31 blocks");
         return JPI_ERR_SHAPE;
     }
-    if (tiles) JPI_TRY(launch_kv_prefix_t5(h, c, splits, a.po, a.pml, st));
-    if (a.p.blocks + a.o.blocks > 0)
-        JPI_TRY(h->D <= 64 ? launch_parts<64>(h, a, st) : h->D <= 128 ? launch_parts<128>(h, a, st) : launch_parts<256>(h, a, st));
-    const int parts = a.p.splits + a.o.splits;
-    const size_t smem = (size_t)((parts + 3) & ~3) * 4 + CB_THREADS * 16;
-    if (h->bf16)
-        k_kv_combine<__nv_bfloat16><<<(unsigned)a.rows, CB_THREADS, smem, st>>>(a.po, a.pml, a.rows, parts, c.D, c.scale,
-                                                                                (__nv_bfloat16*)out, lse);
-    else
-        k_kv_combine<float><<<(unsigned)a.rows, CB_THREADS, smem, st>>>(a.po, a.pml, a.rows, parts, c.D, c.scale, (float*)out, lse);
-    JPI_CUDA_TRY(cudaGetLastError());
-    return JPI_OK;
+    return h->D <= 64 ? launch_dim<64>(h, a, tiles, out, lse, st)
+                      : h->D <= 128 ? launch_dim<128>(h, a, tiles, out, lse, st) : launch_dim<256>(h, a, tiles, out, lse, st);
 }
 
 }  // namespace jpi

@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
     int* flag = (int*)(tmem_slot + 1);
 
     const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
+    ptx::grid_dep_launch();
     // Row tiles fastest: the blocks that read the same keys run together.
     long long w = blockIdx.x;
     const int tile = (int)(w % a.tiles);
