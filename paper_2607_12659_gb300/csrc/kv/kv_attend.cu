@@ -652,6 +652,9 @@ template <int DP>
 jpi_status prepare_dim() {
     JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_mma<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
     JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
+    // The row kernel and the tiles share an SM: both ask for its largest shared memory.
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_mma<DP>, cudaFuncAttributePreferredSharedMemoryCarveout,
+                                      cudaSharedmemCarveoutMaxShared));
     return JPI_OK;
 }
 

@@ -1,6 +1,7 @@
 // The prefix side of jpi_kv_attend on tcgen05: 128 query rows of a run (tokens x heads of one KV head) per
 // block over a range of the shared keys, in blocks of 64 keys.
-//   warp 0  one thread: K blocks by bulk tensor copies into a ring of NS slots
+//   warp 0  one thread: K blocks by bulk tensor copies into a ring of NS slots (the first ones, of V too, before
+//           the block has set itself up)
 //   warp 1  one thread: V blocks into a ring of their own
 //   warp 2  one thread: S_i = Q K_i^T (M = 128, N = 64, K = D) into one of two TMEM score buffers
 //   warp 3  one thread: O += P_i V_i (M = 128, N = D, K = 64), V read as an MN-major operand
@@ -53,7 +54,7 @@ struct PrefixArgs {
 
 template <int DP>
 struct KpSmem {
-    static constexpr int NS = DP == 256 ? 3 : DP == 128 ? 5 : 8;
+    static constexpr int NS = DP == 256 ? 2 : DP == 128 ? 5 : 8;
     static constexpr int KVBYTES = KP_KEYS * DP * 2;
     static constexpr int STAGE = 2 * KVBYTES;               // ring slot: K, then V
     static constexpr int PBYTES = KP_ROWS * KP_KEYS * 2;
@@ -62,7 +63,7 @@ struct KpSmem {
     static constexpr int BAR_OFF = XM_OFF + 4 * KP_ROWS * 4;
     static constexpr int BYTES = BAR_OFF + 64 + 8 * (4 * NS + 10);
     static constexpr int OUT_LD = DP * 4 + 16;              // bytes of a staged output row: the pad spreads the banks
-    static_assert(KP_ROWS * OUT_LD <= P_OFF, "staged rows fit the ring");
+    static_assert(KP_ROWS * OUT_LD <= XM_OFF, "staged rows fit the ring and the P buffers");
     static_assert(BYTES <= 227 * 1024, "fits an SM");
     static constexpr uint32_t TMEM_O = 128, TMEM_Q = 384, TMEM_COLS = 512;
 };
@@ -116,33 +117,30 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
     const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
     ptx::grid_dep_launch();
     // Row tiles fastest: the blocks that read the same keys run together.
-    long long w = blockIdx.x;
-    const int tile = (int)(w % a.tiles);
-    w /= a.tiles;
-    const int split = (int)(w % a.splits);
-    w /= a.splits;
-    const int kvh = (int)(w % a.c.K), run = (int)(w / a.c.K);
-    RowTile t;
-    const int toks = a.c.batch / a.c.groups * a.c.tokens;
-    t.tok0 = (long long)run * toks;
-    t.head0 = kvh * a.c.gq;
-    t.R = toks * a.c.gq;
-    t.r0 = tile * KP_ROWS;
+    uint32_t w = blockIdx.x;
+    const int tile = (int)(w % (uint32_t)a.tiles);
+    w /= (uint32_t)a.tiles;
+    const int split = (int)(w % (uint32_t)a.splits);
+    w /= (uint32_t)a.splits;
+    const int kvh = (int)(w % (uint32_t)a.c.K), run = (int)(w / (uint32_t)a.c.K);
     const int len = min(max(a.c.prefix.len[run], 0), a.c.prefix.rows);
+    // This block's key blocks; none where the prefix is shorter than its splits: the part then weighs nothing.
     const int nb_all = (len + KP_KEYS - 1) / KP_KEYS;
     const int blk0 = (int)((long long)split * nb_all / a.splits);
     const int nb = (int)((long long)(split + 1) * nb_all / a.splits) - blk0;
-    if (nb == 0) {   // the prefix is shorter than its splits: the part weighs nothing
-        const int r = t.r0 + tid;
-        if (tid < KP_ROWS && r < t.R) a.pml[split * a.rows + row_index(t, a.c.gq, a.c.H, r)] = make_float2(-INFINITY, 0.f);
-        return;
-    }
-
-    if (warp == 1) {
-        ptx::tmem_alloc(tmem_slot, L::TMEM_COLS);
-        ptx::tmem_relinquish();
-    }
-    if (tid == 0) {
+    // Key (value) block i into its ring slot.
+    auto load = [&](bool is_v, int i) {
+        const int sl = i % NS, key0 = (blk0 + i) * KP_KEYS;
+        uint64_t* full = (is_v ? vfull : kfull) + sl;
+        uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0);
+        auto coord = [&](int dim) { return dim == a.at_row ? key0 : dim == a.at_head ? kvh : run; };
+        ptx::mbar_expect_tx(full, (uint32_t)L::KVBYTES);
+        for (int db = 0; db < NDB; ++db)
+            tma_load_4d(base + db * (KP_KEYS * 128), is_v ? &vmap : &kmap, full, db * 64, coord(0), coord(1), coord(2));
+    };
+    if (warp == 0 && ptx::elect_one()) {
+        ptx::prefetch_tmap(&kmap);
+        ptx::prefetch_tmap(&vmap);
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(&sfull[b], 1);
             ptx::mbar_init(&pfull[b], 256);
@@ -158,6 +156,49 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         }
         ptx::fence_mbar_init();
         *flag = 0;
+        // The first use of the ring needs nothing of the other warps.
+        for (int i = 0; i < NS && i < nb; ++i) {
+            load(false, i);
+            load(true, i);
+        }
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(tmem_slot, L::TMEM_COLS);
+        ptx::tmem_relinquish();
+    }
+    RowTile t;
+    const int toks = a.c.batch / a.c.groups * a.c.tokens;
+    t.tok0 = (long long)run * toks;
+    t.head0 = kvh * a.c.gq;
+    t.R = toks * a.c.gq;
+    t.r0 = tile * KP_ROWS;
+    // The softmax warps' query rows, on their way while the block sets itself up: 64-element blocks (warp - 4) / 4,
+    // + 2, of the rows of the warp's TMEM lanes.
+    constexpr int QN = (NDB + 1) / 2;
+    uint4 qv[QN][8];
+    if (warp >= 4) {
+        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q);
+        // Row 4 i + (lane / 8): its token and head, stepped by 4 rows.
+        int r = t.r0 + (warp & 3) * 32 + (lane >> 3);
+        int tok = r / a.c.gq, hd = r - tok * a.c.gq;
+        const int tok4 = 4 / a.c.gq, hd4 = 4 - tok4 * a.c.gq;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool in = r < t.R;
+            const __nv_bfloat16* row = q + (in ? (t.tok0 + tok) * a.c.q_stride + (long long)(t.head0 + hd) * a.c.D : 0);
+#pragma unroll
+            for (int k = 0; k < QN; ++k) {
+                const int d = 64 * (((warp - 4) >> 2) + 2 * k) + 8 * (lane & 7);
+                qv[k][i] = kr_ld(row + d, in && d < a.c.D);
+            }
+            r += 4;
+            tok += tok4;
+            hd += hd4;
+            if (hd >= a.c.gq) {
+                hd -= a.c.gq;
+                ++tok;
+            }
+        }
     }
     ptx::tc_fence_before();
     __syncthreads();
@@ -169,21 +210,13 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             const bool is_v = warp == 1;
             uint64_t* fullb = is_v ? vfull : kfull;
             uint64_t* emptyb = is_v ? vempty : kempty;
-            const CUtensorMap* map = is_v ? &vmap : &kmap;
-            auto coord = [&](int dim, int row) { return dim == a.at_row ? row : dim == a.at_head ? kvh : run; };
-            int issued = 0;
-            for (int i = 0; i < nb; ++i) {
-                const int sl = i % NS;
-                if (i >= NS && !ptx::mbar_wait_bounded(&emptyb[sl], (i / NS - 1) & 1, KP_WAIT_NS)) {
+            int issued = min(NS, nb);
+            for (int i = NS; i < nb; ++i) {
+                if (!ptx::mbar_wait_bounded(&emptyb[i % NS], (i / NS - 1) & 1, KP_WAIT_NS)) {
                     *flag = DEV_TIMEOUT_WEIGHTS;
                     break;
                 }
-                uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0);
-                ptx::mbar_expect_tx(&fullb[sl], (uint32_t)L::KVBYTES);
-                const int key0 = (blk0 + i) * KP_KEYS;
-                for (int db = 0; db < NDB; ++db)
-                    tma_load_4d(base + db * (KP_KEYS * 128), map, &fullb[sl], db * 64, coord(0, key0), coord(1, key0),
-                                coord(2, key0));
+                load(is_v, i);
                 issued = i + 1;
             }
             if (!ptx::ring_drain(fullb, NS, issued, KP_WAIT_NS)) *flag = DEV_TIMEOUT_WEIGHTS;
@@ -242,29 +275,35 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         const uint32_t pair_bar = 1 + (warp & 3);   // the two warps of these 32 rows
         float m_used = -INFINITY, l = 0.f;          // m_used is the same in both threads of a row
         bool good = true;
-        {
-            // Half of the query row to TMEM: column 32 db + 4 c + e holds elements 64 db + 8 c + 2 e, + 1.
-            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q);
-            if (valid) q += row_token(t, a.c.gq, r) * a.c.q_stride + (long long)(t.head0 + r % a.c.gq) * a.c.D;
-            constexpr int QW = DP / 32;   // 16-column groups (32 elements), half of them per thread
+        // The query rows were loaded 128 bytes of four rows an instruction: through the warp's 4 KB of the P buffers
+        // to a row per thread, then to TMEM (column 32 db + 4 c + e holds elements 64 db + 8 c + 2 e, + 1).
+        uint4* turn = (uint4*)(ps + (warp - 4) * 4096);
 #pragma unroll
-            for (int k = 0; k < QW / 2; ++k) {
-                const int gr = half * (QW / 2) + k;
-                uint32_t rq[16];
+        for (int k = 0; k < QN; ++k) {
+            const int db = half + 2 * k;
+            if (db < NDB) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint4 v = kr_ld(q + 32 * gr + 8 * c, valid && 32 * gr + 8 * c < a.c.D);
-                    rq[4 * c] = v.x;
-                    rq[4 * c + 1] = v.y;
-                    rq[4 * c + 2] = v.z;
-                    rq[4 * c + 3] = v.w;
+                for (int i = 0; i < 8; ++i) turn[(4 * i + (lane >> 3)) * 8 + ((lane & 7) ^ ((4 * i + (lane >> 3)) & 7))] = qv[k][i];
+                __syncwarp();
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    uint32_t rq[16];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint4 v = turn[lane * 8 + ((4 * hf + c) ^ (lane & 7))];
+                        rq[4 * c] = v.x;
+                        rq[4 * c + 1] = v.y;
+                        rq[4 * c + 2] = v.z;
+                        rq[4 * c + 3] = v.w;
+                    }
+                    ptx::tmem_st_x16(lane_base + L::TMEM_Q + (uint32_t)(32 * db + 16 * hf), rq);
                 }
-                ptx::tmem_st_x16(lane_base + L::TMEM_Q + (uint32_t)(16 * gr), rq);
+                __syncwarp();
             }
-            ptx::tmem_st_wait();
-            ptx::tc_fence_before();
-            ptx::mbar_arrive(qready);
         }
+        ptx::tmem_st_wait();
+        ptx::tc_fence_before();
+        ptx::mbar_arrive(qready);
         constexpr int HK = KP_KEYS / 2;   // keys per thread
         const uint64_t c2 = pair2(a.c2);
         const float rescale = KP_RESCALE / a.c2;
@@ -360,7 +399,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         l = xl[0] + xl[KP_ROWS];
         // Every P V is done, and with them every read of the ring.
         if (nb >= 2 && good) good = ptx::mbar_wait_bounded(&odone[(nb - 2) & 1], ((nb - 2) >> 1) & 1, KP_WAIT_NS);
-        if (good) good = ptx::mbar_wait_bounded(&odone[(nb - 1) & 1], ((nb - 1) >> 1) & 1, KP_WAIT_NS);
+        if (nb >= 1 && good) good = ptx::mbar_wait_bounded(&odone[(nb - 1) & 1], ((nb - 1) >> 1) & 1, KP_WAIT_NS);
         ptx::tc_fence_after();
         if (!good) *flag = DEV_TIMEOUT_MMA;
         uint8_t* orow = kp_smem + row * L::OUT_LD;
@@ -370,7 +409,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             ptx::tmem_ld_x16(lane_base + L::TMEM_O + (uint32_t)c0, v[0]);
             ptx::tmem_ld_x16(lane_base + L::TMEM_O + (uint32_t)(c0 + 16), v[1]);
             ptx::tmem_ld_wait();
-            if (good) {   // a wait that gave up may have left copies on their way into the ring
+            if (good && nb > 0) {   // a wait that gave up may have left copies on their way into the ring
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     *(uint4*)(orow + (c0 + 4 * k) * 4) = make_uint4(v[k >> 2][4 * (k & 3)], v[k >> 2][4 * (k & 3) + 1],
@@ -382,12 +421,12 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         if (half == 0 && valid) {
             const long long row_out = split * a.rows + row_index(t, a.c.gq, a.c.H, r);
             a.pml[row_out] = make_float2(m_used, l);
-            if (good) {
+            if (good && nb > 0) {
                 asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.po + row_out * a.c.D),
                              "r"(ptx::smem_u32(orow)), "r"(a.c.D * 4)
                              : "memory");
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             }
         }
     }
