@@ -12,13 +12,14 @@
 // products, and the difference is scaled, not the product: log2(e) times a score near the type's largest
 // values would overflow.
 //
-// Two launches: the prefix's parts (many rows: kv_attend_t5.cu, few: the row kernels here), and the row kernel
-// over the requests' own rows, which joins a row's prefix parts to its own result and writes it. The second starts
-// while the first runs and waits for it only before that. Where a row has many prefix parts, or its own rows are
-// split too (few requests with long caches) or absent, k_kv_combine joins the parts over all SMs instead.
+// Kernels: the row kernels here take both sides, 8 query rows a warp; many rows on one prefix (from 32) go to
+// tiles of 128 rows instead (kv_attend_t5.cu), bound by tensor cores and 2^x where the row kernel is bound by
+// memory, so the two share the SMs: the row kernel starts first with two blocks per SM, the tiles start while it
+// runs. k_kv_combine joins the parts, except where a row has only one.
 
 #include "kv_rows.cuh"
 #include "kv_attend.h"
+#include "kv_maps.h"
 
 #include <algorithm>
 
@@ -27,12 +28,11 @@ namespace {
 
 constexpr int AT_WARPS = 4;
 constexpr int AT_THREADS = 32 * AT_WARPS;
-constexpr int AT_JOIN = 4;   // most prefix parts that the own rows' kernel joins
 
-// How one side is dealt to blocks: `wr` warps of a block take different row tiles and AT_WARPS / wr
+// How one side is dealt to blocks: `wr` warps of a block take different row tiles, and each of those `wk` warps
 // different keys.
 struct SidePlan {
-    int wr = 1, wk = AT_WARPS;
+    int wr = 1, wk = 1;
     int tiles = 0;        // blocks of wr row tiles per cache and KV head
     int splits = 0;       // key ranges
     long long blocks = 0;
@@ -45,9 +45,9 @@ struct AttendArgs {
     float2* pml;          // [parts][rows] (m, l), m unscaled
     float c2;             // log2(e) * scale
     long long rows;       // batch * tokens * H
-    void* out;
+    void* out;            // rows of one part: the result itself, else null
     float* lse;
-    int late;             // parts that are another kernel's: wait for it before they are read
+    int* err;
 };
 
 // The block's piece of work: side, cache, KV head, row tile and key split.
@@ -57,18 +57,18 @@ struct Piece {
     RowTile t;
     int wk, nwk;
 };
-__device__ __forceinline__ Piece piece_of(const AttendArgs& a, int warp) {
+__device__ __forceinline__ Piece piece_of(const AttendArgs& a, long long piece, int warp) {
     Piece x;
-    long long i = blockIdx.x;
+    uint32_t i = (uint32_t)piece;
     x.prefix = i < a.p.blocks;
-    if (!x.prefix) i -= a.p.blocks;
+    if (!x.prefix) i -= (uint32_t)a.p.blocks;
     const SidePlan& s = x.prefix ? a.p : a.o;
-    x.split = (int)(i % s.splits);
-    i /= s.splits;
-    const int tile = (int)(i % s.tiles);
-    i /= s.tiles;
-    const int kvh = (int)(i % a.c.K);
-    x.cache = (int)(i / a.c.K);
+    x.split = (int)(i % (uint32_t)s.splits);
+    i /= (uint32_t)s.splits;
+    const int tile = (int)(i % (uint32_t)s.tiles);
+    i /= (uint32_t)s.tiles;
+    const int kvh = (int)(i % (uint32_t)a.c.K);
+    x.cache = (int)(i / (uint32_t)a.c.K);
     x.part = x.prefix ? x.split : a.p.splits + x.split;
     const int toks = x.prefix ? a.c.batch / a.c.groups * a.c.tokens : a.c.tokens;
     x.t.tok0 = (long long)x.cache * toks;
@@ -80,7 +80,8 @@ __device__ __forceinline__ Piece piece_of(const AttendArgs& a, int warp) {
     return x;
 }
 
-// Shared memory of one warp's share of the merge: 8 rows of DP outputs, then (m, l) per row.
+// Shared memory of one warp's share of the merge: 8 rows of DP outputs, then (m, l) per row. BYTES: of a block of
+// AT_WARPS warps, which holds the query fragments in it before.
 template <int DP>
 struct MergeSmem {
     static constexpr int LD = DP + 4;   // the row pad spreads the rows over the banks
@@ -182,13 +183,11 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>&
 // Joins the key warps of each row tile (their outputs and (m, l) are in shared memory) and writes the part, or, where
 // the block's keys are the last of its rows, the result.
 template <int DP, typename E>
-__device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece& x, const SidePlan& s, float* sm, int warp,
+__device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece& x, const SidePlan& s, const float* sm, int warp,
                                                 int lane) {
     using M = MergeSmem<DP>;
     constexpr int NI = RowAcc<DP>::NI;
     __syncthreads();
-    const bool last = a.out != nullptr;
-    if (a.late) ptx::grid_dep_wait();
     // Every warp takes rows (its index among the key warps) + n nwk of its row tile.
     const float* tile = sm + (warp / s.wk) * s.wk * M::WARP_FLOATS;
     for (int rr = x.wk; rr < KR_ROWS; rr += x.nwk) {
@@ -215,8 +214,7 @@ __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece
             }
             acc.add(w, v);
         }
-        if (last) {
-            if (a.p.splits > 0) join_parts<DP>(a, acc, row, a.p.splits, 0, 1, lane);
+        if (a.out) {
             write_row<DP, E>(a, acc, row, lane);
             continue;
         }
@@ -244,7 +242,7 @@ __global__ void __launch_bounds__(AT_THREADS, 2) k_kv_attend_mma(const __grid_co
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, j = lane & 3;
     ptx::grid_dep_launch();
-    const Piece x = piece_of(a, warp);
+    const Piece x = piece_of(a, blockIdx.x, warp);
     const SidePlan& sp = x.prefix ? a.p : a.o;
     const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
     const int D = a.c.D;
@@ -419,6 +417,275 @@ __global__ void __launch_bounds__(AT_THREADS, 2) k_kv_attend_mma(const __grid_co
     merge_and_write<DP, __nv_bfloat16>(a, x, sp, kv_smem, warp, lane);
 }
 
+// The same work for caches that bulk tensor copies can read (head dims from 64, see kv_maps.h): each warp
+// streams its 16 KB blocks of 16 (D = 256) to 64 (D = 64) keys through shared memory of its own, the next keys on
+// their way while this block's values are used and the other way round, and reads fragments with ldmatrix. Against loads
+// to registers this needs half the registers and no room in L1 for what is in flight, so that a block fits beside
+// the 128-row tiles on their SM. Blocks are persistent: piece blockIdx.x, + gridDim.x, ..
+constexpr int RT_WARPS = 2;
+constexpr int RT_THREADS = 32 * RT_WARPS;
+constexpr int RT_BLOCK = 16384;   // bytes of a warp's keys and values
+constexpr uint64_t RT_WAIT_NS = 200ull * 1000 * 1000;
+
+template <int DP>
+struct RtSmem {
+    static constexpr int KEYS = RT_BLOCK / (4 * DP);   // keys of a block
+    static constexpr int HALF = RT_BLOCK / 2;          // its keys, then its values
+    static constexpr int BAR_OFF = RT_WARPS * RT_BLOCK > RT_WARPS * MergeSmem<DP>::WARP_FLOATS * 4
+                                       ? RT_WARPS * RT_BLOCK
+                                       : RT_WARPS * MergeSmem<DP>::WARP_FLOATS * 4;
+    static constexpr int BYTES = BAR_OFF + 8 * 2 * RT_WARPS;
+};
+
+struct RtMaps {
+    CUtensorMap k[2], v[2];   // prefix, own
+    int3 at[2];
+};
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+
+template <int DP>
+__global__ void __launch_bounds__(RT_THREADS) k_kv_attend_rows(const __grid_constant__ RtMaps maps,
+                                                               const __grid_constant__ AttendArgs a) {
+    using L = RtSmem<DP>;
+    extern __shared__ __align__(1024) uint8_t rt_smem[];
+    constexpr int MT = L::KEYS / 16;   // 16-key tiles of a block
+    constexpr int ND = DP / 16;
+    const int warp = ptx::warp_index(), lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+    uint8_t* block = rt_smem + warp * RT_BLOCK;
+    const uint32_t ks = ptx::smem_u32(block), vs = ks + L::HALF;
+    uint64_t* bar = (uint64_t*)(rt_smem + L::BAR_OFF) + 2 * warp;   // keys, values
+    ptx::grid_dep_launch();
+    if (lane == 0) {
+        ptx::mbar_init(&bar[0], 1);
+        ptx::mbar_init(&bar[1], 1);
+        ptx::fence_mbar_init();
+    }
+    __syncwarp();
+    int asked[2] = {0, 0}, done[2] = {0, 0};   // copies asked for and waited for, of keys and of values
+    bool good = true;
+    const long long pieces = a.p.blocks + a.o.blocks;
+    for (long long piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const Piece x = piece_of(a, piece, warp);
+        const SidePlan& sp = x.prefix ? a.p : a.o;
+        const int side = x.prefix ? 0 : 1;
+        const int kvh = x.t.head0 / a.c.gq;
+        const int n0 = row_seen(a.c, x.prefix, x.cache, x.t, x.t.r0 + 2 * j);
+        const int n1 = row_seen(a.c, x.prefix, x.cache, x.t, x.t.r0 + 2 * j + 1);
+        int lim = max(n0, n1), low = 0x7fffffff;
+        if (x.t.r0 + 2 * j < x.t.R) low = n0;
+        if (x.t.r0 + 2 * j + 1 < x.t.R) low = min(low, n1);
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            lim = max(lim, __shfl_xor_sync(0xffffffffu, lim, o));
+            low = min(low, __shfl_xor_sync(0xffffffffu, low, o));
+        }
+        const int nb = (lim + L::KEYS - 1) / L::KEYS;
+        const int b0 = (int)((long long)nb * x.split / sp.splits), b1 = (int)((long long)nb * (x.split + 1) / sp.splits);
+        auto load = [&](int what, int blk) {
+            ++asked[what];
+            if (!ptx::elect_one()) return;
+            ptx::mbar_expect_tx(&bar[what], (uint32_t)L::HALF);
+            for (int db = 0; db < DP / 64; ++db)
+                kv_load_box(block + what * L::HALF + db * (L::KEYS * 128), what ? &maps.v[side] : &maps.k[side], &bar[what],
+                            db * 64, maps.at[side], kvh, blk * L::KEYS, x.cache);
+        };
+        const int first = b0 + x.wk;
+        if (first < b1 && good) {
+            load(0, first);
+            load(1, first);
+        }
+        // Query fragments: row g, elements 16 i + 2 j, + 1 and + 8, + 9.
+        uint32_t qf[ND][2];
+        {
+            const int r = x.t.r0 + g;
+            const bool in = r < x.t.R;
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + 2 * j;
+            if (in) q += row_token(x.t, a.c.gq, r) * a.c.q_stride + (long long)(x.t.head0 + r % a.c.gq) * a.c.D;
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    qf[i][e] = in && 16 * i + 8 * e < a.c.D ? __ldg((const uint32_t*)(q + 16 * i + 8 * e)) : 0u;
+        }
+        float o[ND][4];
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+        for (int blk = first; blk < b1 && good; blk += x.nwk) {
+            const int key0 = blk * L::KEYS;
+            good = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&bar[0], done[0] & 1, RT_WAIT_NS));
+            if (!good) break;
+            ++done[0];
+            float sc[MT][4];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[t][e] = 0.f;
+            const int kr = (lane & 7) + (lane & 8);   // key of this lane's matrix row; its chunk is 2 i + lane / 16
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const int ch = 2 * i + (lane >> 4);
+                    uint32_t f[4];
+                    ldsm4(f, ks + (ch >> 3) * (L::KEYS * 128) + (16 * t + kr) * 128 + (((ch & 7) ^ (kr & 7)) << 4));
+                    kr_mma(sc[t], f[0], f[1], f[2], f[3], qf[i][0], qf[i][1]);
+                }
+            __syncwarp();
+            if (blk + x.nwk < b1) load(0, blk + x.nwk);
+            // Keys g, g + 8 of each tile, rows 2 j, 2 j + 1; hidden scores are replaced, whatever they hold.
+            float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int key = key0 + 16 * t + g + 8 * e;
+                    if (key >= n0) sc[t][2 * e] = -INFINITY;
+                    if (key >= n1) sc[t][2 * e + 1] = -INFINITY;
+                    x0 = fmaxf(x0, sc[t][2 * e]);
+                    x1 = fmaxf(x1, sc[t][2 * e + 1]);
+                }
+            }
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) {
+                x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, d));
+                x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, d));
+            }
+            if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
+                const float y0 = fmaxf(m0, x0), y1 = fmaxf(m1, x1);
+                const float a0 = m0 == -INFINITY ? 0.f : kr_ex2((m0 - y0) * a.c2);
+                const float a1 = m1 == -INFINITY ? 0.f : kr_ex2((m1 - y1) * a.c2);
+                m0 = y0;
+                m1 = y1;
+                l0 *= a0;
+                l1 *= a1;
+#pragma unroll
+                for (int i = 0; i < ND; ++i) {
+                    o[i][0] *= a0;
+                    o[i][1] *= a1;
+                    o[i][2] *= a0;
+                    o[i][3] *= a1;
+                }
+            }
+            const float f0 = m0 == -INFINITY ? 0.f : m0, f1 = m1 == -INFINITY ? 0.f : m1;
+            uint32_t ph[MT][2], pe[MT][2];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float p0 = kr_ex2((sc[t][2 * e] - f0) * a.c2), p1 = kr_ex2((sc[t][2 * e + 1] - f1) * a.c2);
+                    l0 += p0;
+                    l1 += p1;
+                    const uint32_t h = kr_pack(p0, p1);
+                    const uint32_t r = kr_pack(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+                    ph[t][e] = kr_transpose(h);
+                    pe[t][e] = kr_transpose(r);
+                }
+            good = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&bar[1], done[1] & 1, RT_WAIT_NS));
+            if (!good) break;
+            ++done[1];
+            const int vr = (lane & 7) + ((lane >> 4) << 3);   // key of this lane's matrix row; its chunk is 2 i + bit 3
+            auto values = [&](int t, int i, uint32_t(&f)[4]) {
+                const int ch = 2 * i + ((lane >> 3) & 1);
+                ldsm4_t(f, vs + (ch >> 3) * (L::KEYS * 128) + (16 * t + vr) * 128 + (((ch & 7) ^ (vr & 7)) << 4));
+            };
+            // Values of keys from `n` on become zeros, whatever they hold (0 times a NaN is not 0).
+            auto mask = [&](int t, int n, uint32_t& lo, uint32_t& hi) {
+                const int key = key0 + 16 * t + 2 * j;
+                lo = (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
+                hi = (key + 8 < n ? 0xffffu : 0u) | (key + 9 < n ? 0xffff0000u : 0u);
+            };
+            // A block that some rows see only a part of, with an infinity or NaN among its values: row by row over the
+            // row's own keys (one row's would reach another).
+            bool odd = false;
+            if (low < min(key0 + L::KEYS, lim)) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    uint32_t lo, hi;
+                    mask(t, lim, lo, hi);
+                    for (int i = 0; i < ND; ++i) {
+                        uint32_t f[4];
+                        values(t, i, f);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t v = f[e] & (e < 2 ? lo : hi);
+                            odd = odd || (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+                        }
+                    }
+                }
+                odd = __any_sync(0xffffffffu, odd);
+            }
+            auto product = [&](int n, bool cut, int row) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    uint32_t lo = ~0u, hi = ~0u;
+                    if (cut) mask(t, n, lo, hi);
+                    const bool mine = row < 0 || g == row;
+                    const uint32_t h0 = mine ? ph[t][0] : 0u, h1 = mine ? ph[t][1] : 0u;
+                    const uint32_t e0 = mine ? pe[t][0] : 0u, e1 = mine ? pe[t][1] : 0u;
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) {
+                        uint32_t f[4];
+                        values(t, i, f);
+                        kr_mma(o[i], f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, h0, h1);
+                        kr_mma(o[i], f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, e0, e1);
+                    }
+                }
+            };
+            if (!odd) {
+                product(lim, key0 + L::KEYS > lim, -1);
+            } else {
+#pragma unroll 1
+                for (int r = 0; r < KR_ROWS; ++r) product(__shfl_sync(0xffffffffu, (r & 1) ? n1 : n0, r >> 1), true, r);
+            }
+            __syncwarp();
+            if (blk + x.nwk < b1) load(1, blk + x.nwk);
+        }
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, d);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, d);
+        }
+        // Copies that are still on their way (a wait gave up) land before their memory is used for anything else.
+        for (int what = 0; what < 2; ++what)
+            for (; done[what] < asked[what]; ++done[what]) (void)ptx::mbar_wait_bounded(&bar[what], done[what] & 1, RT_WAIT_NS);
+        __syncthreads();   // every warp is through with its blocks: their memory holds the merge now
+        float* f = (float*)rt_smem + warp * MergeSmem<DP>::WARP_FLOATS;
+        constexpr int LD = MergeSmem<DP>::LD;
+        if (good) {
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[(2 * j + (e & 1)) * LD + 16 * i + g + 8 * (e >> 1)] = o[i][e];
+        }
+        if (g == 0) {
+            float* ml = f + KR_ROWS * LD + 4 * j;
+            ml[0] = m0;
+            ml[1] = l0;
+            ml[2] = m1;
+            ml[3] = l1;
+        }
+        merge_and_write<DP, __nv_bfloat16>(a, x, sp, (const float*)rt_smem, warp, lane);
+        ptx::fence_proxy_async_smem();   // before the next piece's copies land where the merge was
+        __syncthreads();
+    }
+    if (!good && lane == 0) atomicCAS(a.err, 0, (int)DEV_TIMEOUT_WEIGHTS);
+}
+
 // fp32 on CUDA cores: one warp = 8 query rows over 32-key blocks. Scores with a key per lane, the
 // values with a lane per four elements of d.
 template <int DP>
@@ -426,7 +693,7 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
     extern __shared__ __align__(16) float kv_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     ptx::grid_dep_launch();
-    const Piece x = piece_of(a, warp);
+    const Piece x = piece_of(a, blockIdx.x, warp);
     const SidePlan& sp = x.prefix ? a.p : a.o;
     const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
     const int D = a.c.D;
@@ -576,84 +843,95 @@ long long ws_rows(const jpi_kv_handle* h) {
     return 2 * rows + 512ll * h->num_sms;
 }
 
-// A side's key splits: enough blocks for two on every SM, as long as a block keeps at least `least` keys a warp
-// and the parts fit their half of the workspace.
-SidePlan plan_side(const jpi_kv_handle* h, const KvCall& c, bool prefix, int least) {
+// A side's pieces for blocks of `warps` warps: key splits until there are `want` pieces in all, as long as a warp keeps
+// `least` keys and the parts fit their half of the workspace.
+SidePlan plan_side(const jpi_kv_handle* h, const KvCall& c, bool prefix, int warps, int least, long long want) {
     SidePlan s;
     const KvSide& side = prefix ? c.prefix : c.own;
     if (side.rows == 0) return s;
     const int caches = prefix ? c.groups : c.batch;
     const long long R = (long long)(prefix ? c.batch / c.groups : 1) * c.tokens * c.gq;
     const long long rt = (R + KR_ROWS - 1) / KR_ROWS;
-    s.wr = 1;
-    while (s.wr < AT_WARPS && s.wr < rt) s.wr *= 2;
-    s.wk = AT_WARPS / s.wr;
+    while (s.wr < warps && s.wr < rt) s.wr *= 2;
+    s.wk = warps / s.wr;
     s.tiles = (int)((rt + s.wr - 1) / s.wr);
     const long long blocks = (long long)caches * c.K * s.tiles, rows = (long long)c.batch * c.tokens * c.H;
     const long long room = std::max(1ll, (ws_rows(h) / 2) / rows);
-    long long splits = 2ll * h->num_sms / blocks;
-    splits = std::min({splits, room, (long long)(side.rows + least * s.wk - 1) / (least * s.wk)});
+    const long long splits = std::min({want / blocks, room, (long long)(side.rows + least * s.wk - 1) / (least * s.wk)});
     s.splits = (int)std::max(1ll, splits);
     s.blocks = blocks * s.splits;
     return s;
 }
 
-// A launch that starts while the one before it runs (and waits for it where it says so), or an ordinary one.
-template <typename... Params, typename... Args>
-jpi_status start(void (*kernel)(Params...), long long grid, int threads, size_t smem, bool early, cudaStream_t st, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = early ? 1 : 0;
-    JPI_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
-    return JPI_OK;
-}
-
 template <int DP>
-jpi_status launch_dim(jpi_kv_handle* h, AttendArgs a, bool tiles, void* out, float* lse, cudaStream_t st) {
-    auto rows = [&](const AttendArgs& x, bool early) {
-        const long long grid = x.p.blocks + x.o.blocks;
-        return h->bf16 ? start(k_kv_attend_mma<DP>, grid, AT_THREADS, MergeSmem<DP>::BYTES, early, st, x)
-                       : start(k_kv_attend_f32<DP>, grid, AT_THREADS, MergeSmem<DP>::BYTES, early, st, x);
-    };
-    a.out = nullptr;
+jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, cudaStream_t st) {
+    AttendArgs a = {};
+    a.c = c;
+    a.c2 = KR_LOG2E * c.scale;
+    a.rows = (long long)c.batch * c.tokens * c.H;
+    a.po = static_cast<float*>(h->ws);
+    a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
     a.lse = lse;
-    a.late = 0;
-    // The own rows finish the call where they are not split.
-    const bool own_last = a.o.splits == 1 && a.p.splits <= AT_JOIN;
-    AttendArgs first = a;
-    if (tiles) first.p.blocks = 0;
-    if (own_last) first.o.blocks = 0;
-    if (tiles) JPI_TRY(launch_kv_prefix_t5(h, a.c, a.p.splits, a.po, a.pml, st));
-    const bool parts = first.p.blocks + first.o.blocks > 0;
-    if (parts) {
-        first.late = tiles;   // (it ends after the tiles, so that what waits for it has both)
-        JPI_TRY(rows(first, tiles));
-    }
-    a.out = out;
-    if (own_last) {
+    a.err = h->dev_err;
+    int splits = 0;
+    const bool tiles = kv_prefix_splits(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), &splits);
+    // The row kernel: on bulk copies where both sides' strides allow them.
+    KvMapDims md[2];
+    const bool copies = h->bf16 && c.D >= 64 && kv_maps_available() &&
+                        (tiles || c.prefix.rows == 0 || kv_map_dims(c.prefix, c.K, c.D, c.groups, &md[0])) &&
+                        (c.own.rows == 0 || kv_map_dims(c.own, c.K, c.D, c.batch, &md[1]));
+    const int warps = copies ? RT_WARPS : AT_WARPS, least = copies ? RtSmem<DP>::KEYS : h->bf16 ? KR_KEYS : 32;
+    const long long want = 2ll * h->num_sms;
+    a.p = plan_side(h, c, true, warps, least, want);
+    a.o = plan_side(h, c, false, warps, least, want);
+    if (tiles) {
         a.p.blocks = 0;
-        a.late = tiles || parts;
-        return rows(a, a.late);
+        a.p.splits = splits;
     }
-    const int n = a.p.splits + a.o.splits, wpr = n > 16 ? 4 : n > 4 ? 2 : 1;
+    const int parts = a.p.splits + a.o.splits;
+    const long long pieces = a.p.blocks + a.o.blocks;
+    if (pieces > 0x7fffffffll) {
+        set_error("the call needs more than 2^31 blocks");
+        return JPI_ERR_SHAPE;
+    }
+    if (pieces > 0) {
+        AttendArgs r = a;
+        if (parts == 1) r.out = out;
+        if (copies) {
+            RtMaps m = {};
+            for (int i = 0; i < 2; ++i) {
+                const KvSide& s = i ? c.own : c.prefix;
+                if (s.rows == 0 || (i == 0 && tiles)) continue;
+                if (!kv_make_map(md[i], s.k, c.D, RtSmem<DP>::KEYS, &m.k[i]) || !kv_make_map(md[i], s.v, c.D, RtSmem<DP>::KEYS, &m.v[i])) {
+                    set_error("cuTensorMapEncodeTiled refused the %s", i ? "own rows" : "prefix");
+                    return JPI_ERR_CUDA;
+                }
+                m.at[i] = make_int3(md[i].at_head, md[i].at_row, md[i].at_cache);
+            }
+            const long long most = (tiles ? 2ll : 6ll) * h->num_sms;
+            JPI_TRY(kv_start(k_kv_attend_rows<DP>, std::min(pieces, most), RT_THREADS, RtSmem<DP>::BYTES, false, st, m, r));
+        } else if (h->bf16) {
+            JPI_TRY(kv_start(k_kv_attend_mma<DP>, pieces, AT_THREADS, MergeSmem<DP>::BYTES, false, st, r));
+        } else {
+            JPI_TRY(kv_start(k_kv_attend_f32<DP>, pieces, AT_THREADS, MergeSmem<DP>::BYTES, false, st, r));
+        }
+    }
+    if (tiles) JPI_TRY(launch_kv_prefix_t5(h, c, splits, a.po, a.pml, pieces > 0, st));
+    if (parts == 1 && pieces > 0) return JPI_OK;
+    a.out = out;
+    const int wpr = parts > 16 ? 4 : parts > 4 ? 2 : 1;
     const long long grid = (a.rows * wpr + AT_WARPS - 1) / AT_WARPS;
-    return h->bf16 ? start(k_kv_combine<DP, __nv_bfloat16>, grid, AT_THREADS, 0, true, st, a, wpr)
-                   : start(k_kv_combine<DP, float>, grid, AT_THREADS, 0, true, st, a, wpr);
+    return h->bf16 ? kv_start(k_kv_combine<DP, __nv_bfloat16>, grid, AT_THREADS, 0, true, st, a, wpr)
+                   : kv_start(k_kv_combine<DP, float>, grid, AT_THREADS, 0, true, st, a, wpr);
 }
 
 template <int DP>
 jpi_status prepare_dim() {
     JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_mma<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
     JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
-    // The row kernel and the tiles share an SM: both ask for its largest shared memory.
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_mma<DP>, cudaFuncAttributePreferredSharedMemoryCarveout,
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_rows<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, RtSmem<DP>::BYTES));
+    // All of its loads go to shared memory, and the 128-row tiles need the SM set up for the most of it.
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_rows<DP>, cudaFuncAttributePreferredSharedMemoryCarveout,
                                       cudaSharedmemCarveoutMaxShared));
     return JPI_OK;
 }
@@ -670,24 +948,8 @@ jpi_status kv_attend_prepare(jpi_kv_handle* h) {
 }
 
 jpi_status launch_kv_attend(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, cudaStream_t st) {
-    AttendArgs a = {};
-    a.c = c;
-    a.p = plan_side(h, c, true, h->bf16 ? KR_KEYS : 32);
-    a.o = plan_side(h, c, false, h->bf16 ? KR_KEYS : 32);
-    a.c2 = KR_LOG2E * c.scale;
-    a.rows = (long long)c.batch * c.tokens * c.H;
-    a.po = static_cast<float*>(h->ws);
-    a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
-    // Many rows on one prefix go to the tensor-core tiles.
-    int splits = 0;
-    const bool tiles = kv_prefix_splits(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), &splits);
-    if (tiles) a.p.splits = splits;
-    if (a.p.blocks + a.o.blocks > 0x7fffffffll) {
-        set_error("the call needs more than 2^31 blocks");
-        return JPI_ERR_SHAPE;
-    }
-    return h->D <= 64 ? launch_dim<64>(h, a, tiles, out, lse, st)
-                      : h->D <= 128 ? launch_dim<128>(h, a, tiles, out, lse, st) : launch_dim<256>(h, a, tiles, out, lse, st);
+    return h->D <= 64 ? launch_dim<64>(h, c, out, lse, st)
+                      : h->D <= 128 ? launch_dim<128>(h, c, out, lse, st) : launch_dim<256>(h, c, out, lse, st);
 }
 
 }  // namespace jpi

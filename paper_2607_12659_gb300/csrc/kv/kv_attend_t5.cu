@@ -6,7 +6,8 @@
 //   warp 2  one thread: S_i = Q K_i^T (M = 128, N = 64, K = D) into one of two TMEM score buffers
 //   warp 3  one thread: O += P_i V_i (M = 128, N = D, K = 64), V read as an MN-major operand
 //   warps 4-11  two threads per query row (its TMEM lane), half of a block's keys each: maximum, 2^x,
-//           probabilities as bf16 to shared memory. O is rescaled only when a block's maximum passes the running one by
+//           probabilities as bf16 back to tensor memory, over the scores they come from (the A operand of the
+//           second product: no shared memory, and room on the SM for blocks of the row kernel). O is rescaled only when a block's maximum passes the running one by
 //           more than 8 in log2 units, so that probabilities stay below 2^8.
 // The query rows are gathered by the softmax threads (a run's tokens may lie at any stride and a row
 // tile may begin and end inside a token's heads) straight into tensor memory, columns 384.., as the A operand of the
@@ -27,8 +28,7 @@
 
 #include "kv_rows.cuh"
 #include "kv_attend.h"
-
-#include <cudaTypedefs.h>
+#include "kv_maps.h"
 
 #include <algorithm>
 
@@ -45,7 +45,7 @@ struct PrefixArgs {
     KvCall c;
     float c2;            // log2(e) * scale
     int splits, tiles;   // key ranges, row tiles per run and KV head
-    int at_head, at_row, at_run;   // which of the maps' outer dimensions is which
+    int3 at;             // of the maps' outer dimensions: heads, rows, runs
     float* po;           // [parts][rows][D]
     float2* pml;         // [parts][rows]
     long long rows;
@@ -54,27 +54,21 @@ struct PrefixArgs {
 
 template <int DP>
 struct KpSmem {
-    static constexpr int NS = DP == 256 ? 2 : DP == 128 ? 5 : 8;
+    static constexpr int NS = DP == 256 ? 2 : 4;
     static constexpr int KVBYTES = KP_KEYS * DP * 2;
     static constexpr int STAGE = 2 * KVBYTES;               // ring slot: K, then V
-    static constexpr int PBYTES = KP_ROWS * KP_KEYS * 2;
-    static constexpr int P_OFF = NS * STAGE;                // two P buffers
-    static constexpr int XM_OFF = P_OFF + 2 * PBYTES;       // [2 blocks][2 key halves][128 rows]
+    static constexpr int OUT_LD = DP * 4 + 16;              // bytes of a staged output row: the pad spreads the banks
+    static constexpr int RING = NS * STAGE > KP_ROWS * OUT_LD ? NS * STAGE : KP_ROWS * OUT_LD;
+    static constexpr int XM_OFF = RING;                     // [2 blocks][2 key halves][128 rows]
     static constexpr int BAR_OFF = XM_OFF + 4 * KP_ROWS * 4;
     static constexpr int BYTES = BAR_OFF + 64 + 8 * (4 * NS + 10);
-    static constexpr int OUT_LD = DP * 4 + 16;              // bytes of a staged output row: the pad spreads the banks
-    static_assert(KP_ROWS * OUT_LD <= XM_OFF, "staged rows fit the ring and the P buffers");
+    // The query rows' way to a row per thread: 4 KB a warp in the last QS value slots, which are filled after it.
+    static constexpr int TURN = KVBYTES / 4096, QS = DP == 256 ? 1 : 2;
+    static_assert(QS < NS && TURN * QS >= (DP == 64 ? 4 : 8), "the query rows fit those slots");
     static_assert(BYTES <= 227 * 1024, "fits an SM");
     static constexpr uint32_t TMEM_O = 128, TMEM_Q = 384, TMEM_COLS = 512;
 };
 
-__device__ __forceinline__ void tma_load_4d(void* dst, const void* tmap, uint64_t* bar, int x, int y, int z, int w) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(ptx::smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(ptx::smem_u32(bar))
-        : "memory");
-}
 // (a - m) c for two scores at a time.
 __device__ __forceinline__ void sub_scale2(float a, float b, uint64_t neg_m2, uint64_t c2, float& x, float& y) {
     uint64_t v;
@@ -99,15 +93,13 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
     constexpr uint32_t IDESC_PV = ptx::idesc_bf16_f32(KP_ROWS, DP) | (1u << 16);   // B MN-major
     extern __shared__ __align__(1024) uint8_t kp_smem[];
     uint8_t* stages = kp_smem;
-    uint8_t* ps = kp_smem + L::P_OFF;
     float* xmax = (float*)(kp_smem + L::XM_OFF);
     uint64_t* bars = (uint64_t*)(kp_smem + L::BAR_OFF);
     uint64_t* sfull = bars;            // 2: score buffer ready
-    uint64_t* pfull = bars + 2;        // 2: P buffer written
-    uint64_t* odone = bars + 4;        // 2: P V of the block in P buffer b done
-    uint64_t* sfree = bars + 6;        // 2: score buffer has been read
-    uint64_t* qready = bars + 8;       // the query rows are in TMEM
-    uint64_t* kfull = bars + 9;        // NS each
+    uint64_t* pfull = bars + 2;        // 2: probabilities written over the score buffer
+    uint64_t* odone = bars + 4;        // 2: P V of the block in score buffer b done
+    uint64_t* qready = bars + 6;       // the query rows are in TMEM
+    uint64_t* kfull = bars + 7;        // NS each
     uint64_t* vfull = kfull + NS;
     uint64_t* kempty = vfull + NS;
     uint64_t* vempty = kempty + NS;
@@ -133,10 +125,9 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         const int sl = i % NS, key0 = (blk0 + i) * KP_KEYS;
         uint64_t* full = (is_v ? vfull : kfull) + sl;
         uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0);
-        auto coord = [&](int dim) { return dim == a.at_row ? key0 : dim == a.at_head ? kvh : run; };
         ptx::mbar_expect_tx(full, (uint32_t)L::KVBYTES);
         for (int db = 0; db < NDB; ++db)
-            tma_load_4d(base + db * (KP_KEYS * 128), is_v ? &vmap : &kmap, full, db * 64, coord(0), coord(1), coord(2));
+            kv_load_box(base + db * (KP_KEYS * 128), is_v ? &vmap : &kmap, full, db * 64, a.at, kvh, key0, run);
     };
     if (warp == 0 && ptx::elect_one()) {
         ptx::prefetch_tmap(&kmap);
@@ -145,7 +136,6 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             ptx::mbar_init(&sfull[b], 1);
             ptx::mbar_init(&pfull[b], 256);
             ptx::mbar_init(&odone[b], 1);
-            ptx::mbar_init(&sfree[b], 256);
         }
         ptx::mbar_init(qready, 256);
         for (int s = 0; s < NS; ++s) {
@@ -159,7 +149,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         // The first use of the ring needs nothing of the other warps.
         for (int i = 0; i < NS && i < nb; ++i) {
             load(false, i);
-            load(true, i);
+            if (i < NS - L::QS) load(true, i);
         }
     }
     if (warp == 1) {
@@ -211,7 +201,14 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             uint64_t* fullb = is_v ? vfull : kfull;
             uint64_t* emptyb = is_v ? vempty : kempty;
             int issued = min(NS, nb);
-            for (int i = NS; i < nb; ++i) {
+            bool good = true;
+            if (is_v) {
+                good = ptx::mbar_wait_bounded(qready, 0, KP_WAIT_NS);
+                if (!good) *flag = DEV_TIMEOUT_MMA;
+                if (!good) issued = min(NS - L::QS, nb);
+                for (int i = NS - L::QS; good && i < NS && i < nb; ++i) load(true, i);
+            }
+            for (int i = NS; good && i < nb; ++i) {
                 if (!ptx::mbar_wait_bounded(&emptyb[i % NS], (i / NS - 1) & 1, KP_WAIT_NS)) {
                     *flag = DEV_TIMEOUT_WEIGHTS;
                     break;
@@ -227,7 +224,8 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             bool good = ptx::mbar_wait_bounded(qready, 0, KP_WAIT_NS);
             for (int i = 0; i < nb; ++i) {
                 const int sl = i % NS;
-                if (i >= 2 && good) good = ptx::mbar_wait_bounded(&sfree[i & 1], ((i - 2) >> 1) & 1, KP_WAIT_NS);
+                // (its score buffer holds P_{i-2} until that product is done)
+                if (i >= 2 && good) good = ptx::mbar_wait_bounded(&odone[i & 1], ((i - 2) >> 1) & 1, KP_WAIT_NS);
                 if (good) good = ptx::mbar_wait_bounded(&kfull[sl], (i / NS) & 1, KP_WAIT_NS);
                 ptx::tc_fence_after();
                 if (good) {
@@ -246,7 +244,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         }
     } else if (warp == 3) {
         if (ptx::elect_one()) {
-            const uint32_t sb = ptx::smem_u32(stages), pb = ptx::smem_u32(ps);
+            const uint32_t sb = ptx::smem_u32(stages);
             bool good = true;
             for (int i = 0; i < nb; ++i) {
                 const int sl = i % NS;
@@ -255,11 +253,10 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
                 ptx::tc_fence_after();
                 if (good) {
                     const uint64_t vb = ptx::desc_sw128_mn(sb + sl * L::STAGE + L::KVBYTES, KP_KEYS * 128, 1024);
-                    const uint64_t pbi = ptx::desc_sw128(pb + (uint32_t)((i & 1) * L::PBYTES));
 #pragma unroll
                     for (int kk = 0; kk < KP_KEYS / 16; ++kk)
-                        ptx::mma_bf16(tmem + L::TMEM_O, ptx::desc_add(pbi, kk * 32), ptx::desc_add(vb, kk * 16 * 128), IDESC_PV,
-                                      (i | kk) != 0);
+                        ptx::mma_bf16_ta(tmem + L::TMEM_O, tmem + (uint32_t)(64 * (i & 1) + 8 * kk),
+                                         ptx::desc_add(vb, kk * 16 * 128), IDESC_PV, (i | kk) != 0);
                 }
                 if (i + NS < nb) ptx::mma_commit(&vempty[sl]);
                 ptx::mma_commit(&odone[i & 1]);
@@ -275,9 +272,10 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         const uint32_t pair_bar = 1 + (warp & 3);   // the two warps of these 32 rows
         float m_used = -INFINITY, l = 0.f;          // m_used is the same in both threads of a row
         bool good = true;
-        // The query rows were loaded 128 bytes of four rows an instruction: through the warp's 4 KB of the P buffers
+        // The query rows were loaded 128 bytes of four rows an instruction: through 4 KB of shared memory of the warp
         // to a row per thread, then to TMEM (column 32 db + 4 c + e holds elements 64 db + 8 c + 2 e, + 1).
-        uint4* turn = (uint4*)(ps + (warp - 4) * 4096);
+        const int wi = warp - 4;
+        uint4* turn = (uint4*)(stages + (NS - 1 - wi / L::TURN) * L::STAGE + L::KVBYTES + wi % L::TURN * 4096);
 #pragma unroll
         for (int k = 0; k < QN; ++k) {
             const int db = half + 2 * k;
@@ -302,6 +300,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             }
         }
         ptx::tmem_st_wait();
+        ptx::fence_proxy_async_smem();   // the slots' values land after these accesses
         ptx::tc_fence_before();
         ptx::mbar_arrive(qready);
         constexpr int HK = KP_KEYS / 2;   // keys per thread
@@ -316,8 +315,6 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
                 ptx::tmem_ld_x16(sa, s[0]);
                 ptx::tmem_ld_x16(sa + 16u, s[1]);
                 ptx::tmem_ld_wait();
-                ptx::tc_fence_before();
-                ptx::mbar_arrive(&sfree[i & 1]);
             }
             const int vis = nvis - (blk0 + i) * KP_KEYS - HK * half;   // keys of this half block the row sees
             const bool full = __all_sync(0xffffffffu, vis >= HK);
@@ -370,13 +367,10 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
                 pk[k / 2] = kr_pack(p0, p1);
             }
             l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-            // P buffer i mod 2 is free once P V of block i - 2 is done.
-            if (i >= 2 && good) good = ptx::mbar_wait_bounded(&odone[i & 1], ((i - 2) >> 1) & 1, KP_WAIT_NS);
-            ptx::tc_fence_after();
-            uint4* prow = (uint4*)(ps + (i & 1) * L::PBYTES + row * 128);
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                prow[(4 * half + c) ^ (row & 7)] = make_uint4(pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]);
+            // Over the scores of both halves: both threads of a row have read theirs (the barrier above). Column 16 half
+            // + e holds keys 32 half + 2 e, + 1.
+            ptx::tmem_st_x16(lane_base + (uint32_t)(64 * (i & 1) + 16 * half), pk);
+            ptx::tmem_st_wait();
             const int live = len - (blk0 + i) * KP_KEYS;   // the same for the whole block
             if (live < KP_KEYS) {
                 // Values of rows past the end, as they landed: cleared (a row's 16-byte pieces stay in the row).
@@ -387,8 +381,8 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
                     const int key = live + e / (NDB * 8), p = e % (NDB * 8);
                     *(uint4*)(vb + (p / 8) * (KP_KEYS * 128) + key * 128 + (p % 8) * 16) = make_uint4(0, 0, 0, 0);
                 }
+                ptx::fence_proxy_async_smem();
             }
-            ptx::fence_proxy_async_smem();
             ptx::tc_fence_before();
             ptx::mbar_arrive(&pfull[i & 1]);
         }
@@ -418,6 +412,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
         }
         ptx::fence_proxy_async_smem();
         ptx::named_bar_sync(pair_bar, 64);
+        ptx::grid_dep_wait();   // the row kernel that started before this one: what waits for this kernel has both
         if (half == 0 && valid) {
             const long long row_out = split * a.rows + row_index(t, a.c.gq, a.c.H, r);
             a.pml[row_out] = make_float2(m_used, l);
@@ -437,66 +432,18 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
     if (warp == 1) ptx::tmem_dealloc(tmem, L::TMEM_COLS);
 }
 
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
-        cudaDriverEntryPointQueryResult q;
-        void* p = nullptr;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-        return (PFN_cuTensorMapEncodeTiled_v12000)p;
-    }();
-    return fn;
-}
-
-// The outer dimensions of the prefix's maps: heads, rows and runs by ascending stride, those of size 1 last. Maps
-// are documented for strides that are multiples of the one before, and below 2^40 bytes: false for a cache of other
-// strides, which the row kernel takes.
-struct MapDims {
-    cuuint64_t size[3], stride[3];
-    int at_head = 0, at_row = 0, at_run = 0;
-};
-bool map_dims(const KvCall& c, MapDims* m) {
-    struct Dim {
-        long long stride;
-        int size, id;
-    } d[3] = {{c.prefix.hs, c.K, 0}, {c.prefix.rs, c.prefix.rows, 1}, {c.prefix.cs, c.groups, 2}};
-    std::stable_sort(d, d + 3, [](const Dim& x, const Dim& y) {
-        if ((x.size > 1) != (y.size > 1)) return x.size > 1;
-        return x.size > 1 && x.stride < y.stride;
-    });
-    long long last = (c.D + 7) / 8 * 8;
-    for (int i = 0; i < 3; ++i) {
-        const long long st = d[i].size > 1 ? d[i].stride : last;
-        if (i > 0 && st % last) return false;
-        if (st >= (1ll << 39)) return false;
-        last = st;
-        m->size[i] = (cuuint64_t)d[i].size;
-        m->stride[i] = (cuuint64_t)st * 2;
-        (d[i].id == 0 ? m->at_head : d[i].id == 1 ? m->at_row : m->at_run) = i;
-    }
-    return true;
-}
-
-bool make_map(const KvCall& c, const MapDims& m, const void* base, CUtensorMap* map) {
-    auto enc = encode_fn();
-    if (!enc) return false;
-    const cuuint64_t dims[4] = {(cuuint64_t)c.D, m.size[0], m.size[1], m.size[2]};
-    cuuint32_t box[4] = {64, 1, 1, 1};
-    const cuuint32_t estr[4] = {1, 1, 1, 1};
-    box[1 + m.at_row] = KP_KEYS;
-    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, m.stride, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+template <int DP>
+jpi_status launch_dim(const PrefixArgs& a, const CUtensorMap& km, const CUtensorMap& vm, bool early, cudaStream_t st) {
+    const long long blocks = (long long)a.tiles * a.splits * a.c.K * a.c.groups;
+    return kv_start(k_kv_prefix_t5<DP>, blocks, KP_THREADS, KpSmem<DP>::BYTES, early, st, km, vm, a);
 }
 
 template <int DP>
-jpi_status launch_dim(const PrefixArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st) {
-    const long long blocks = (long long)a.tiles * a.splits * a.c.K * a.c.groups;
-    k_kv_prefix_t5<DP><<<(unsigned)blocks, KP_THREADS, KpSmem<DP>::BYTES, st>>>(km, vm, a);
-    JPI_CUDA_TRY(cudaGetLastError());
+jpi_status prepare_dim() {
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<DP>::BYTES));
+    // An SM that runs a block of the row kernel takes one of these beside it only if both want it set up alike.
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<DP>, cudaFuncAttributePreferredSharedMemoryCarveout,
+                                      cudaSharedmemCarveoutMaxShared));
     return JPI_OK;
 }
 
@@ -504,25 +451,15 @@ jpi_status launch_dim(const PrefixArgs& a, const CUtensorMap& km, const CUtensor
 
 jpi_status kv_prefix_prepare(jpi_kv_handle* h) {
     if (!h->bf16 || h->D < 64) return JPI_OK;
-    if (!encode_fn()) {
-        set_error("cuTensorMapEncodeTiled is unavailable from the driver");
-        return JPI_ERR_CUDA;
-    }
-    if (h->D <= 64)
-        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<64>::BYTES));
-    else if (h->D <= 128)
-        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<128>::BYTES));
-    else
-        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<256>::BYTES));
-    return JPI_OK;
+    return h->D <= 64 ? prepare_dim<64>() : h->D <= 128 ? prepare_dim<128>() : prepare_dim<256>();
 }
 
 bool kv_prefix_splits(const jpi_kv_handle* h, const KvCall& c, long long room, int* splits) {
     if (!h->bf16 || c.D < 64 || c.prefix.rows == 0) return false;
     const long long R = (long long)(c.batch / c.groups) * c.tokens * c.gq;
     if (R < 32) return false;
-    MapDims m;
-    if (!map_dims(c, &m)) return false;
+    KvMapDims m;
+    if (!kv_map_dims(c.prefix, c.K, c.D, c.groups, &m)) return false;
     const long long tiles = (R + KP_ROWS - 1) / KP_ROWS, blocks = tiles * c.K * c.groups;
     const long long nb = (c.prefix.rows + KP_KEYS - 1) / KP_KEYS;
     long long s = std::max(1ll, h->num_sms / blocks);
@@ -530,7 +467,8 @@ bool kv_prefix_splits(const jpi_kv_handle* h, const KvCall& c, long long room, i
     return blocks * *splits <= 0x7fffffffll;
 }
 
-jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, float* po, float2* pml, cudaStream_t st) {
+jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, float* po, float2* pml, bool early,
+                               cudaStream_t st) {
     PrefixArgs a;
     a.c = c;
     a.c2 = KR_LOG2E * c.scale;
@@ -541,16 +479,16 @@ jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, fl
     a.pml = pml;
     a.rows = (long long)c.batch * c.tokens * c.H;
     a.err = h->dev_err;
-    MapDims m;
+    KvMapDims m;
     CUtensorMap km, vm;
-    if (!map_dims(c, &m) || !make_map(c, m, c.prefix.k, &km) || !make_map(c, m, c.prefix.v, &vm)) {
+    if (!kv_map_dims(c.prefix, c.K, c.D, c.groups, &m) || !kv_make_map(m, c.prefix.k, c.D, KP_KEYS, &km) ||
+        !kv_make_map(m, c.prefix.v, c.D, KP_KEYS, &vm)) {
         set_error("cuTensorMapEncodeTiled refused the prefix");
         return JPI_ERR_CUDA;
     }
-    a.at_head = m.at_head;
-    a.at_row = m.at_row;
-    a.at_run = m.at_run;
-    return c.D <= 64 ? launch_dim<64>(a, km, vm, st) : c.D <= 128 ? launch_dim<128>(a, km, vm, st) : launch_dim<256>(a, km, vm, st);
+    a.at = make_int3(m.at_head, m.at_row, m.at_cache);
+    return c.D <= 64 ? launch_dim<64>(a, km, vm, early, st)
+                     : c.D <= 128 ? launch_dim<128>(a, km, vm, early, st) : launch_dim<256>(a, km, vm, early, st);
 }
 
 }  // namespace jpi
