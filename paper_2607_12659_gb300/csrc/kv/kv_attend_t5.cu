@@ -5,9 +5,12 @@
 //   warp 1  one thread: V blocks into a ring of their own
 //   warp 2  one thread: S_i = Q K_i^T (M = 128, N = 64, K = D) into one of two TMEM score buffers
 //   warp 3  one thread: O += P_i V_i (M = 128, N = D, K = 64), V read as an MN-major operand
-//   warps 4-11  two threads per query row (its TMEM lane), half of a block's keys each: maximum, 2^x,
+//   warps 4-  groups of eight: two threads per query row (its TMEM lane), half of a block's keys each: maximum, 2^x,
 //           probabilities as bf16 back to tensor memory, over the scores they come from (the A operand of the
-//           second product: no shared memory, and room on the SM for blocks of the row kernel). O is rescaled only when a block's maximum passes the running one by
+//           second product: no shared memory, and room on the SM for blocks of the row kernel). To D = 128 a block's
+//           softmax takes twice as long as its products (1280 cycles for one group of warps, 610): two groups take the
+//           even and the odd blocks, each with a maximum, sum and output of its own, joined at the end. At D = 256 the
+//           products need that long, and tensor memory holds one output. O is rescaled only when a block's maximum passes the running one by
 //           more than 8 in log2 units, so that probabilities stay below 2^8.
 // The query rows are gathered by the softmax threads (a run's tokens may lie at any stride and a row
 // tile may begin and end inside a token's heads) straight into tensor memory, columns 384.., as the A operand of the
@@ -37,7 +40,7 @@ namespace {
 
 constexpr int KP_ROWS = 128;
 constexpr int KP_KEYS = 64;
-constexpr int KP_THREADS = 384;
+constexpr int KP_SOFT = 256;   // threads of a softmax group
 constexpr uint64_t KP_WAIT_NS = 200ull * 1000 * 1000;
 constexpr float KP_RESCALE = 8.f;   // log2 units
 
@@ -59,14 +62,21 @@ struct KpSmem {
     static constexpr int STAGE = 2 * KVBYTES;               // ring slot: K, then V
     static constexpr int OUT_LD = DP * 4 + 16;              // bytes of a staged output row: the pad spreads the banks
     static constexpr int RING = NS * STAGE > KP_ROWS * OUT_LD ? NS * STAGE : KP_ROWS * OUT_LD;
-    static constexpr int XM_OFF = RING;                     // [2 blocks][2 key halves][128 rows]
-    static constexpr int BAR_OFF = XM_OFF + 4 * KP_ROWS * 4;
-    static constexpr int BYTES = BAR_OFF + 64 + 8 * (4 * NS + 10);
+    static constexpr int NG = DP == 256 ? 1 : 2;            // softmax groups
+    static constexpr int THREADS = 128 + NG * KP_SOFT;
+    // Score buffers: a third where it fits, so that a group's next scores are there when it is through with the last
+    // (with two they wait for the product that reads the probabilities lying over them).
+    static constexpr int NB = DP == 256 ? 2 : 3;
+    static constexpr int XM_OFF = RING;                     // [groups][2 blocks][2 key halves][128 rows]
+    static constexpr int ML_OFF = XM_OFF + NG * 4 * KP_ROWS * 4;    // [groups][128 rows] (m, l)
+    static constexpr int BAR_OFF = ML_OFF + NG * KP_ROWS * 8;
+    static constexpr int BYTES = BAR_OFF + 8 * (3 * NB + NG + 1 + 4 * NS + 1);
     // The query rows' way to a row per thread: 4 KB a warp in the last QS value slots, which are filled after it.
     static constexpr int TURN = KVBYTES / 4096, QS = DP == 256 ? 1 : 2;
     static_assert(QS < NS && TURN * QS >= (DP == 64 ? 4 : 8), "the query rows fit those slots");
     static_assert(BYTES <= 227 * 1024, "fits an SM");
-    static constexpr uint32_t TMEM_O = 128, TMEM_Q = 384, TMEM_COLS = 512;
+    static constexpr uint32_t TMEM_O = NB * KP_KEYS, TMEM_Q = TMEM_O + NG * DP, TMEM_COLS = 512;
+    static_assert(TMEM_Q + DP / 2 <= TMEM_COLS, "scores, outputs and queries fit");
 };
 
 // (a - m) c for two scores at a time.
@@ -84,22 +94,24 @@ __device__ __forceinline__ uint64_t pair2(float a) {
 }
 
 template <int DP>
-__global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_constant__ CUtensorMap kmap,
+__global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const __grid_constant__ CUtensorMap kmap,
                                                                 const __grid_constant__ CUtensorMap vmap,
                                                                 const __grid_constant__ PrefixArgs a) {
     using L = KpSmem<DP>;
-    constexpr int NS = L::NS, NDB = DP / 64;
+    constexpr int NS = L::NS, NG = L::NG, NB = L::NB, NDB = DP / 64;
     constexpr uint32_t IDESC_S = ptx::idesc_bf16_f32(KP_ROWS, KP_KEYS);
     constexpr uint32_t IDESC_PV = ptx::idesc_bf16_f32(KP_ROWS, DP) | (1u << 16);   // B MN-major
     extern __shared__ __align__(1024) uint8_t kp_smem[];
     uint8_t* stages = kp_smem;
     float* xmax = (float*)(kp_smem + L::XM_OFF);
+    float2* ml = (float2*)(kp_smem + L::ML_OFF);
     uint64_t* bars = (uint64_t*)(kp_smem + L::BAR_OFF);
-    uint64_t* sfull = bars;            // 2: score buffer ready
-    uint64_t* pfull = bars + 2;        // 2: probabilities written over the score buffer
-    uint64_t* odone = bars + 4;        // 2: P V of the block in score buffer b done
-    uint64_t* qready = bars + 6;       // the query rows are in TMEM
-    uint64_t* kfull = bars + 7;        // NS each
+    uint64_t* sfull = bars;            // NB: score buffer ready
+    uint64_t* pfull = sfull + NB;      // NB: probabilities written over the score buffer
+    uint64_t* odone = pfull + NB;      // NB: P V of the block in score buffer b done
+    uint64_t* gdone = odone + NB;      // NG: P V of the group's block done
+    uint64_t* qready = gdone + NG;     // the query rows are in TMEM
+    uint64_t* kfull = qready + 1;      // NS each
     uint64_t* vfull = kfull + NS;
     uint64_t* kempty = vfull + NS;
     uint64_t* vempty = kempty + NS;
@@ -132,11 +144,12 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
     if (warp == 0 && ptx::elect_one()) {
         ptx::prefetch_tmap(&kmap);
         ptx::prefetch_tmap(&vmap);
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < NB; ++b) {
             ptx::mbar_init(&sfull[b], 1);
-            ptx::mbar_init(&pfull[b], 256);
+            ptx::mbar_init(&pfull[b], KP_SOFT);
             ptx::mbar_init(&odone[b], 1);
         }
+        for (int b = 0; b < NG; ++b) ptx::mbar_init(&gdone[b], 1);
         ptx::mbar_init(qready, 256);
         for (int s = 0; s < NS; ++s) {
             ptx::mbar_init(&kfull[s], 1);
@@ -166,7 +179,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
     // + 2, of the rows of the warp's TMEM lanes.
     constexpr int QN = (NDB + 1) / 2;
     uint4 qv[QN][8];
-    if (warp >= 4) {
+    if (warp >= 4 && warp < 12) {
         const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q);
         // Row 4 i + (lane / 8): its token and head, stepped by 4 rows.
         int r = t.r0 + (warp & 3) * 32 + (lane >> 3);
@@ -224,8 +237,8 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             bool good = ptx::mbar_wait_bounded(qready, 0, KP_WAIT_NS);
             for (int i = 0; i < nb; ++i) {
                 const int sl = i % NS;
-                // (its score buffer holds P_{i-2} until that product is done)
-                if (i >= 2 && good) good = ptx::mbar_wait_bounded(&odone[i & 1], ((i - 2) >> 1) & 1, KP_WAIT_NS);
+                // (its score buffer holds P_{i-NB} until that product is done)
+                if (i >= NB && good) good = ptx::mbar_wait_bounded(&odone[i % NB], (i / NB - 1) & 1, KP_WAIT_NS);
                 if (good) good = ptx::mbar_wait_bounded(&kfull[sl], (i / NS) & 1, KP_WAIT_NS);
                 ptx::tc_fence_after();
                 if (good) {
@@ -234,10 +247,10 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
                     for (int db = 0; db < NDB; ++db)
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk)
-                            ptx::mma_bf16_ta(tmem + (uint32_t)(64 * (i & 1)), tmem + L::TMEM_Q + (uint32_t)(8 * (4 * db + kk)),
+                            ptx::mma_bf16_ta(tmem + (uint32_t)(KP_KEYS * (i % NB)), tmem + L::TMEM_Q + (uint32_t)(8 * (4 * db + kk)),
                                              ptx::desc_add(kb, db * (KP_KEYS * 128) + kk * 32), IDESC_S, (db | kk) != 0);
                 }
-                ptx::mma_commit(&sfull[i & 1]);
+                ptx::mma_commit(&sfull[i % NB]);
                 if (i + NS < nb) ptx::mma_commit(&kempty[sl]);
             }
             if (!good) *flag = DEV_TIMEOUT_MMA;
@@ -248,70 +261,74 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             bool good = true;
             for (int i = 0; i < nb; ++i) {
                 const int sl = i % NS;
-                if (good) good = ptx::mbar_wait_bounded(&pfull[i & 1], (i >> 1) & 1, KP_WAIT_NS);
+                if (good) good = ptx::mbar_wait_bounded(&pfull[i % NB], (i / NB) & 1, KP_WAIT_NS);
                 if (good) good = ptx::mbar_wait_bounded(&vfull[sl], (i / NS) & 1, KP_WAIT_NS);
                 ptx::tc_fence_after();
                 if (good) {
                     const uint64_t vb = ptx::desc_sw128_mn(sb + sl * L::STAGE + L::KVBYTES, KP_KEYS * 128, 1024);
 #pragma unroll
                     for (int kk = 0; kk < KP_KEYS / 16; ++kk)
-                        ptx::mma_bf16_ta(tmem + L::TMEM_O, tmem + (uint32_t)(64 * (i & 1) + 8 * kk),
-                                         ptx::desc_add(vb, kk * 16 * 128), IDESC_PV, (i | kk) != 0);
+                        ptx::mma_bf16_ta(tmem + L::TMEM_O + (uint32_t)(i % NG * DP), tmem + (uint32_t)(KP_KEYS * (i % NB) + 8 * kk),
+                                         ptx::desc_add(vb, kk * 16 * 128), IDESC_PV, i >= NG || kk != 0);
                 }
                 if (i + NS < nb) ptx::mma_commit(&vempty[sl]);
-                ptx::mma_commit(&odone[i & 1]);
+                if (i + NB < nb) ptx::mma_commit(&odone[i % NB]);
+                ptx::mma_commit(&gdone[i % NG]);
             }
             if (!good) *flag = DEV_TIMEOUT_MMA;
         }
     } else {
-        const int row = (warp & 3) * 32 + lane, half = (warp - 4) >> 2;
+        const int grp = (warp - 4) >> 3, row = (warp & 3) * 32 + lane, half = ((warp - 4) >> 2) & 1;
         const int r = t.r0 + row;
         const bool valid = r < t.R;
         const int nvis = valid ? len : 0;
         const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t pair_bar = 1 + (warp & 3);   // the two warps of these 32 rows
+        const uint32_t out = lane_base + L::TMEM_O + (uint32_t)(grp * DP);
+        const uint32_t pair_bar = 1 + 4 * grp + (warp & 3);   // the two warps of these 32 rows
         float m_used = -INFINITY, l = 0.f;          // m_used is the same in both threads of a row
         bool good = true;
         // The query rows were loaded 128 bytes of four rows an instruction: through 4 KB of shared memory of the warp
         // to a row per thread, then to TMEM (column 32 db + 4 c + e holds elements 64 db + 8 c + 2 e, + 1).
-        const int wi = warp - 4;
-        uint4* turn = (uint4*)(stages + (NS - 1 - wi / L::TURN) * L::STAGE + L::KVBYTES + wi % L::TURN * 4096);
-#pragma unroll
-        for (int k = 0; k < QN; ++k) {
-            const int db = half + 2 * k;
-            if (db < NDB) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) turn[(4 * i + (lane >> 3)) * 8 + ((lane & 7) ^ ((4 * i + (lane >> 3)) & 7))] = qv[k][i];
-                __syncwarp();
-#pragma unroll
-                for (int hf = 0; hf < 2; ++hf) {
-                    uint32_t rq[16];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint4 v = turn[lane * 8 + ((4 * hf + c) ^ (lane & 7))];
-                        rq[4 * c] = v.x;
-                        rq[4 * c + 1] = v.y;
-                        rq[4 * c + 2] = v.z;
-                        rq[4 * c + 3] = v.w;
+        if (grp == 0) {
+            const int wi = warp - 4;
+            uint4* turn = (uint4*)(stages + (NS - 1 - wi / L::TURN) * L::STAGE + L::KVBYTES + wi % L::TURN * 4096);
+    #pragma unroll
+            for (int k = 0; k < QN; ++k) {
+                const int db = half + 2 * k;
+                if (db < NDB) {
+    #pragma unroll
+                    for (int i = 0; i < 8; ++i) turn[(4 * i + (lane >> 3)) * 8 + ((lane & 7) ^ ((4 * i + (lane >> 3)) & 7))] = qv[k][i];
+                    __syncwarp();
+    #pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        uint32_t rq[16];
+    #pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const uint4 v = turn[lane * 8 + ((4 * hf + c) ^ (lane & 7))];
+                            rq[4 * c] = v.x;
+                            rq[4 * c + 1] = v.y;
+                            rq[4 * c + 2] = v.z;
+                            rq[4 * c + 3] = v.w;
+                        }
+                        ptx::tmem_st_x16(lane_base + L::TMEM_Q + (uint32_t)(32 * db + 16 * hf), rq);
                     }
-                    ptx::tmem_st_x16(lane_base + L::TMEM_Q + (uint32_t)(32 * db + 16 * hf), rq);
+                    __syncwarp();
                 }
-                __syncwarp();
-            }
         }
-        ptx::tmem_st_wait();
-        ptx::fence_proxy_async_smem();   // the slots' values land after these accesses
-        ptx::tc_fence_before();
-        ptx::mbar_arrive(qready);
+            ptx::tmem_st_wait();
+            ptx::fence_proxy_async_smem();   // the slots' values land after these accesses
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(qready);
+        }
         constexpr int HK = KP_KEYS / 2;   // keys per thread
         const uint64_t c2 = pair2(a.c2);
         const float rescale = KP_RESCALE / a.c2;
-        for (int i = 0; i < nb; ++i) {
-            if (good) good = ptx::mbar_wait_bounded(&sfull[i & 1], (i >> 1) & 1, KP_WAIT_NS);
+        for (int i = grp; i < nb; i += NG) {
+            if (good) good = ptx::mbar_wait_bounded(&sfull[i % NB], (i / NB) & 1, KP_WAIT_NS);
             ptx::tc_fence_after();
             uint32_t s[2][16];
             {
-                const uint32_t sa = lane_base + (uint32_t)(64 * (i & 1) + HK * half);
+                const uint32_t sa = lane_base + (uint32_t)(KP_KEYS * (i % NB) + HK * half);
                 ptx::tmem_ld_x16(sa, s[0]);
                 ptx::tmem_ld_x16(sa + 16u, s[1]);
                 ptx::tmem_ld_wait();
@@ -327,25 +344,25 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
 #pragma unroll
             for (int j = 0; j < HK; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j >> 4][j & 15]));
             float mb = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            float* xm = xmax + (i & 1) * 2 * KP_ROWS + row;
+            float* xm = xmax + (2 * grp + (i / NG & 1)) * 2 * KP_ROWS + row;
             xm[half * KP_ROWS] = mb;
             ptx::named_bar_sync(pair_bar, 64);
             mb = fmaxf(mb, xm[(1 - half) * KP_ROWS]);
             const bool move = mb > m_used + rescale;
             const float alpha = !move ? 1.f : m_used == -INFINITY ? 0.f : kr_ex2((m_used - mb) * a.c2);
             // TMEM accesses are warp-collective: the warp rescales together (its half of the columns), lanes whose
-            // maximum stays put multiply by 1. O is settled once P V of the previous block is done.
-            if (__any_sync(0xffffffffu, move && i > 0 && m_used != -INFINITY)) {
-                if (good) good = ptx::mbar_wait_bounded(&odone[(i - 1) & 1], ((i - 1) >> 1) & 1, KP_WAIT_NS);
+            // maximum stays put multiply by 1. O is settled once P V of the group's previous block is done.
+            if (__any_sync(0xffffffffu, move && i >= NG && m_used != -INFINITY)) {
+                if (good) good = ptx::mbar_wait_bounded(&gdone[grp], (i / NG - 1) & 1, KP_WAIT_NS);
                 ptx::tc_fence_after();
 #pragma unroll 1
                 for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 16) {
                     uint32_t ro[16];
-                    ptx::tmem_ld_x16(lane_base + L::TMEM_O + (uint32_t)c0, ro);
+                    ptx::tmem_ld_x16(out + (uint32_t)c0, ro);
                     ptx::tmem_ld_wait();
 #pragma unroll
                     for (int j = 0; j < 16; ++j) ro[j] = __float_as_uint(__uint_as_float(ro[j]) * alpha);
-                    ptx::tmem_st_x16(lane_base + L::TMEM_O + (uint32_t)c0, ro);
+                    ptx::tmem_st_x16(out + (uint32_t)c0, ro);
                 }
                 ptx::tmem_st_wait();
             }
@@ -369,7 +386,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
             l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
             // Over the scores of both halves: both threads of a row have read theirs (the barrier above). Column 16 half
             // + e holds keys 32 half + 2 e, + 1.
-            ptx::tmem_st_x16(lane_base + (uint32_t)(64 * (i & 1) + 16 * half), pk);
+            ptx::tmem_st_x16(lane_base + (uint32_t)(KP_KEYS * (i % NB) + 16 * half), pk);
             ptx::tmem_st_wait();
             const int live = len - (blk0 + i) * KP_KEYS;   // the same for the whole block
             if (live < KP_KEYS) {
@@ -377,51 +394,85 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
                 const int sl = i % NS;
                 if (good) good = ptx::mbar_wait_bounded(&vfull[sl], (i / NS) & 1, KP_WAIT_NS);
                 uint8_t* vb = stages + sl * L::STAGE + L::KVBYTES;
-                for (int e = tid - 128; good && e < (KP_KEYS - live) * NDB * 8; e += 256) {
+                for (int e = (tid - 128) % KP_SOFT; good && e < (KP_KEYS - live) * NDB * 8; e += KP_SOFT) {
                     const int key = live + e / (NDB * 8), p = e % (NDB * 8);
                     *(uint4*)(vb + (p / 8) * (KP_KEYS * 128) + key * 128 + (p % 8) * 16) = make_uint4(0, 0, 0, 0);
                 }
                 ptx::fence_proxy_async_smem();
             }
             ptx::tc_fence_before();
-            ptx::mbar_arrive(&pfull[i & 1]);
+            ptx::mbar_arrive(&pfull[i % NB]);
         }
-        // The row's sum: both halves, in order.
-        float* xl = xmax + (nb & 1) * 2 * KP_ROWS + row;   // not the buffer of the last block's maxima
+        // The row's sum: both halves, in order, through the buffer that the last block's maxima are not in.
+        const int mine = (nb - grp + NG - 1) / NG;   // blocks of this group
+        float* xl = xmax + (2 * grp + (mine & 1)) * 2 * KP_ROWS + row;
         xl[half * KP_ROWS] = l;
         ptx::named_bar_sync(pair_bar, 64);
         l = xl[0] + xl[KP_ROWS];
-        // Every P V is done, and with them every read of the ring.
-        if (nb >= 2 && good) good = ptx::mbar_wait_bounded(&odone[(nb - 2) & 1], ((nb - 2) >> 1) & 1, KP_WAIT_NS);
-        if (nb >= 1 && good) good = ptx::mbar_wait_bounded(&odone[(nb - 1) & 1], ((nb - 1) >> 1) & 1, KP_WAIT_NS);
+        // Every P V of the block is done, and with them every read of the ring.
+        for (int b = 0; b < NG; ++b) {
+            const int of = (nb - b + NG - 1) / NG;   // blocks of group b
+            if (of > 0 && good) good = ptx::mbar_wait_bounded(&gdone[b], (of - 1) & 1, KP_WAIT_NS);
+        }
         ptx::tc_fence_after();
         if (!good) *flag = DEV_TIMEOUT_MMA;
+        // The groups' outputs are joined on the way: w_g = 2^((m_g - M) c).
+        float w = 1.f;
+        if (NG > 1) {
+            if (half == 0) ml[grp * KP_ROWS + row] = make_float2(m_used, l);
+            ptx::named_bar_sync(9, NG * KP_SOFT);
+            const float2 other = ml[(1 - grp) * KP_ROWS + row];
+            const float M = fmaxf(m_used, other.x);
+            w = m_used == -INFINITY ? 0.f : kr_ex2((m_used - M) * a.c2);
+            l = w * l + (other.x == -INFINITY ? 0.f : kr_ex2((other.x - M) * a.c2) * other.y);
+            m_used = M;
+        }
         uint8_t* orow = kp_smem + row * L::OUT_LD;
 #pragma unroll 1
-        for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 32) {
-            uint32_t v[2][16];
-            ptx::tmem_ld_x16(lane_base + L::TMEM_O + (uint32_t)c0, v[0]);
-            ptx::tmem_ld_x16(lane_base + L::TMEM_O + (uint32_t)(c0 + 16), v[1]);
-            ptx::tmem_ld_wait();
-            if (good && nb > 0) {   // a wait that gave up may have left copies on their way into the ring
+        for (int turn = 0; turn < NG; ++turn) {
+            if (turn == grp) {
+#pragma unroll 1
+                for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 32) {
+                    uint32_t v[2][16];
+                    ptx::tmem_ld_x16(out + (uint32_t)c0, v[0]);
+                    ptx::tmem_ld_x16(out + (uint32_t)(c0 + 16), v[1]);
+                    ptx::tmem_ld_wait();
+                    if (good && mine > 0) {   // a wait that gave up may have left copies on their way into the ring
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    *(uint4*)(orow + (c0 + 4 * k) * 4) = make_uint4(v[k >> 2][4 * (k & 3)], v[k >> 2][4 * (k & 3) + 1],
-                                                                   v[k >> 2][4 * (k & 3) + 2], v[k >> 2][4 * (k & 3) + 3]);
+                        for (int k = 0; k < 8; ++k) {
+                            float4* dst = (float4*)(orow + (c0 + 4 * k) * 4);
+                            float4 x = make_float4(__uint_as_float(v[k >> 2][4 * (k & 3)]), __uint_as_float(v[k >> 2][4 * (k & 3) + 1]),
+                                                   __uint_as_float(v[k >> 2][4 * (k & 3) + 2]), __uint_as_float(v[k >> 2][4 * (k & 3) + 3]));
+                            if (NG > 1) {
+                                x = make_float4(w * x.x, w * x.y, w * x.z, w * x.w);
+                                if (grp > 0) {
+                                    const float4 y = *dst;
+                                    x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+                                }
+                            }
+                            *dst = x;
+                        }
+                    }
+                }
             }
+            if (turn + 1 < NG) ptx::named_bar_sync(10, NG * KP_SOFT);
         }
-        ptx::fence_proxy_async_smem();
-        ptx::named_bar_sync(pair_bar, 64);
-        ptx::grid_dep_wait();   // the row kernel that started before this one: what waits for this kernel has both
-        if (half == 0 && valid) {
-            const long long row_out = split * a.rows + row_index(t, a.c.gq, a.c.H, r);
-            a.pml[row_out] = make_float2(m_used, l);
-            if (good && nb > 0) {
-                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.po + row_out * a.c.D),
-                             "r"(ptx::smem_u32(orow)), "r"(a.c.D * 4)
-                             : "memory");
-                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        if (grp < NG - 1) {
+            ptx::grid_dep_wait();
+        } else {
+            ptx::fence_proxy_async_smem();
+            ptx::named_bar_sync(pair_bar, 64);
+            ptx::grid_dep_wait();   // the row kernel that started before this one: what waits for this kernel has both
+            if (half == 0 && valid) {
+                const long long row_out = split * a.rows + row_index(t, a.c.gq, a.c.H, r);
+                a.pml[row_out] = make_float2(m_used, l);
+                if (good && nb > 0) {
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.po + row_out * a.c.D),
+                                 "r"(ptx::smem_u32(orow)), "r"(a.c.D * 4)
+                                 : "memory");
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                }
             }
         }
     }
@@ -435,7 +486,7 @@ __global__ void __launch_bounds__(KP_THREADS, 1) k_kv_prefix_t5(const __grid_con
 template <int DP>
 jpi_status launch_dim(const PrefixArgs& a, const CUtensorMap& km, const CUtensorMap& vm, bool early, cudaStream_t st) {
     const long long blocks = (long long)a.tiles * a.splits * a.c.K * a.c.groups;
-    return kv_start(k_kv_prefix_t5<DP>, blocks, KP_THREADS, KpSmem<DP>::BYTES, early, st, km, vm, a);
+    return kv_start(k_kv_prefix_t5<DP>, blocks, KpSmem<DP>::THREADS, KpSmem<DP>::BYTES, early, st, km, vm, a);
 }
 
 template <int DP>
