@@ -22,6 +22,25 @@ struct jpi_kv_handle {
 
 namespace jpi {
 
+// n / d for 0 <= n < 2^31 by a multiplication: with 2^s >= d > 2^(s-1) and m = floor(2^32 (2^s - d) / d) + 1,
+// n / d = (floor(m n / 2^32) + n) >> s.
+struct KvDiv {
+    uint32_t d = 1, m = 1, s = 0;
+    KvDiv() = default;
+    explicit KvDiv(uint32_t div) : d(div) {
+        while ((1ull << s) < div) ++s;
+        m = (uint32_t)(((1ull << 32) * ((1ull << s) - div)) / div + 1);
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
+    __device__ __forceinline__ uint32_t div(uint32_t n, uint32_t& rem) const {
+        const uint32_t q = div(n);
+        rem = n - q * d;
+        return q;
+    }
+#endif
+};
+
 // One side of a call's keys as the kernels read them: `n` caches of at most `rows` rows.
 struct KvSide {
     const void *k = nullptr, *v = nullptr;
@@ -38,6 +57,7 @@ struct KvCall {
     int H = 0, K = 0, D = 0, gq = 0;
     float scale = 0.f;                  // of the scores
     KvSide prefix, own;                 // rows == 0: absent
+    KvDiv by_gq, by_K;
 };
 
 // Bytes of workspace that any attend within the maxima needs (kv_attend.cu).

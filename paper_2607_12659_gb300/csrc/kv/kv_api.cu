@@ -156,6 +156,8 @@ jpi_status make_call(const jpi_kv_handle* h, const void* q, long long q_stride, 
     c->D = h->D;
     c->gq = h->gq;
     c->scale = h->scale;
+    c->by_gq = KvDiv((uint32_t)h->gq);
+    c->by_K = KvDiv((uint32_t)h->K);
     c->prefix = side_of(prefix, prefix_len);
     c->own = side_of(own, seen);
     return JPI_OK;

@@ -19,7 +19,6 @@
 
 #include "kv_rows.cuh"
 #include "kv_attend.h"
-#include "kv_maps.h"
 
 #include <algorithm>
 
@@ -36,47 +35,44 @@ struct SidePlan {
     int tiles = 0;        // blocks of wr row tiles per cache and KV head
     int splits = 0;       // key ranges
     long long blocks = 0;
+    KvDiv by_splits, by_tiles;
 };
 
 struct AttendArgs {
     KvCall c;
     SidePlan p, o;
     float* po;            // [parts][rows][D] unnormalised outputs
-    float2* pml;          // [parts][rows] (m, l), m unscaled
+    float2* pml;          // [rows][parts] (m, l), m unscaled
+    int parts;
     float c2;             // log2(e) * scale
     long long rows;       // batch * tokens * H
     void* out;            // rows of one part: the result itself, else null
     float* lse;
-    int* err;
 };
 
 // The block's piece of work: side, cache, KV head, row tile and key split.
 struct Piece {
     bool prefix;
-    int cache, split, part;
+    int cache, kvh, part;
+    uint32_t split;
     RowTile t;
-    int wk, nwk;
 };
 __device__ __forceinline__ Piece piece_of(const AttendArgs& a, long long piece, int warp) {
     Piece x;
-    uint32_t i = (uint32_t)piece;
+    uint32_t i = (uint32_t)piece, tile, kvh;
     x.prefix = i < a.p.blocks;
     if (!x.prefix) i -= (uint32_t)a.p.blocks;
     const SidePlan& s = x.prefix ? a.p : a.o;
-    x.split = (int)(i % (uint32_t)s.splits);
-    i /= (uint32_t)s.splits;
-    const int tile = (int)(i % (uint32_t)s.tiles);
-    i /= (uint32_t)s.tiles;
-    const int kvh = (int)(i % (uint32_t)a.c.K);
-    x.cache = (int)(i / (uint32_t)a.c.K);
-    x.part = x.prefix ? x.split : a.p.splits + x.split;
+    i = s.by_splits.div(i, x.split);
+    i = s.by_tiles.div(i, tile);
+    x.cache = (int)a.c.by_K.div(i, kvh);
+    x.part = (x.prefix ? 0 : a.p.splits) + (int)x.split;
     const int toks = x.prefix ? a.c.batch / a.c.groups * a.c.tokens : a.c.tokens;
     x.t.tok0 = (long long)x.cache * toks;
-    x.t.head0 = kvh * a.c.gq;
+    x.kvh = (int)kvh;
+    x.t.head0 = (int)kvh * a.c.gq;
     x.t.R = toks * a.c.gq;
-    x.t.r0 = (tile * s.wr + warp / s.wk) * KR_ROWS;
-    x.wk = warp % s.wk;
-    x.nwk = s.wk;
+    x.t.r0 = ((int)tile * s.wr + warp / s.wk) * KR_ROWS;
     return x;
 }
 
@@ -106,44 +102,42 @@ struct RowAcc {
     }
 };
 
-// Joins parts first, first + step, .. of a row's `parts` to what `r` holds, all relative to the largest maximum
-// of the row (which r.m becomes). The loads of JOIN parts are in flight together: they are made whether the part
-// weighs anything or not (its memory is the workspace's), and a part of no weight, which may never have been
-// written, is replaced by zeros.
+// Joins parts first, first + step, .. of a row (of `parts`) to `r`, which holds nothing yet, relative to their largest
+// maximum. The loads of JOIN parts are in flight together: they are made whether the part weighs anything or not (its
+// memory is the workspace's), and a part of no weight, which may never have been written, is replaced by zeros.
 template <int DP>
-__device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, long long row, int parts, int first, int step,
-                                           int lane) {
+__device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, long long row, int first, int step, int lane) {
     constexpr int NI = RowAcc<DP>::NI, JOIN = 16 / NI;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < parts) ml = __ldcg(&a.pml[lane * a.rows + row]);
-    float M = fmaxf(r.m, ml.x);
-    for (int p = 32 + lane; p < parts; p += 32) M = fmaxf(M, __ldcg(&a.pml[p * a.rows + row]).x);
-#pragma unroll
-    for (int e = 16; e > 0; e >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, e));
-    const float w0 = r.m == -INFINITY ? 0.f : kr_ex2((r.m - M) * a.c2);
-    float l = 0.f;
-#pragma unroll
-    for (int i = 0; i < NI; ++i) r.o[i] = make_float4(r.o[i].x * w0, r.o[i].y * w0, r.o[i].z * w0, r.o[i].w * w0);
+    const float2* pml = a.pml + row * a.parts;
     int d[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i) d[i] = 4 * lane + 128 * i < a.c.D ? 4 * lane + 128 * i : 0;
-    for (int p0 = 0; p0 < parts; p0 += 32) {
-        if (p0 > 0) {
-            ml = make_float2(-INFINITY, 0.f);
-            if (p0 + lane < parts) ml = __ldcg(&a.pml[(p0 + lane) * a.rows + row]);
-        }
+    const int mine = (a.parts - first + step - 1) / step;   // parts of this warp
+    for (int p0 = 0; p0 < mine; p0 += 32) {
+        const int n = min(32, mine - p0);
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (lane < n) ml = __ldcg(pml + first + (p0 + lane) * step);
+        float M = fmaxf(r.m, ml.x);
+#pragma unroll
+        for (int e = 16; e > 0; e >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, e));
+        const float w0 = r.m == -INFINITY ? 0.f : kr_ex2((r.m - M) * a.c2);
         const float w = ml.x == -INFINITY ? 0.f : kr_ex2((ml.x - M) * a.c2);
-        if ((p0 + lane) % step == first) l += w * ml.y;   // (w = 0 past the parts)
-        const int n = min(32, parts - p0);
-        for (int k0 = first; k0 < n; k0 += JOIN * step) {   // step divides 32
+        float l = w * ml.y;
+#pragma unroll
+        for (int e = 16; e > 0; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
+        r.l = r.l * w0 + l;
+        r.m = M;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) r.o[i] = make_float4(r.o[i].x * w0, r.o[i].y * w0, r.o[i].z * w0, r.o[i].w * w0);
+        for (int k0 = 0; k0 < n; k0 += JOIN) {
             float4 v[JOIN][NI];
             float wk[JOIN];
 #pragma unroll
             for (int k = 0; k < JOIN; ++k) {
-                const int q = min(k0 + k * step, n - 1);
-                const float* src = a.po + ((p0 + q) * a.rows + row) * a.c.D;
+                const int q = min(k0 + k, n - 1);
+                const float* src = a.po + ((first + (p0 + q) * step) * a.rows + row) * a.c.D;
                 wk[k] = __shfl_sync(0xffffffffu, w, q);
-                if (k0 + k * step >= n) wk[k] = 0.f;
+                if (k0 + k >= n) wk[k] = 0.f;
 #pragma unroll
                 for (int i = 0; i < NI; ++i) v[k][i] = __ldcg((const float4*)(src + d[i]));
             }
@@ -156,10 +150,6 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, l
             }
         }
     }
-#pragma unroll
-    for (int e = 16; e > 0; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
-    r.l = r.l * w0 + l;
-    r.m = M;
 }
 
 // The row's result from its joined sums.
@@ -182,25 +172,25 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>&
 
 // Joins the key warps of each row tile (their outputs and (m, l) are in shared memory) and writes the part, or, where
 // the block's keys are the last of its rows, the result.
-template <int DP, typename E>
+template <int DP>
 __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece& x, const SidePlan& s, const float* sm, int warp,
                                                 int lane) {
     using M = MergeSmem<DP>;
     constexpr int NI = RowAcc<DP>::NI;
     __syncthreads();
-    // Every warp takes rows (its index among the key warps) + n nwk of its row tile.
+    // Every warp takes rows (its index among the key warps) + n wk of its row tile.
     const float* tile = sm + (warp / s.wk) * s.wk * M::WARP_FLOATS;
-    for (int rr = x.wk; rr < KR_ROWS; rr += x.nwk) {
+    for (int rr = warp % s.wk; rr < KR_ROWS; rr += s.wk) {
         const int r = x.t.r0 + rr;
         if (r >= x.t.R) continue;
-        const long long row = row_index(x.t, a.c.gq, a.c.H, r);
+        const long long row = row_index(a.c, x.t, r);
         RowAcc<DP> acc;
         acc.m = -INFINITY;
         acc.l = 0.f;
-        for (int k = 0; k < x.nwk; ++k) acc.m = fmaxf(acc.m, tile[k * M::WARP_FLOATS + KR_ROWS * M::LD + 2 * rr]);
+        for (int k = 0; k < s.wk; ++k) acc.m = fmaxf(acc.m, tile[k * M::WARP_FLOATS + KR_ROWS * M::LD + 2 * rr]);
 #pragma unroll
         for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < x.nwk; ++k) {
+        for (int k = 0; k < s.wk; ++k) {
             const float* f = tile + k * M::WARP_FLOATS;
             const float mk = f[KR_ROWS * M::LD + 2 * rr];
             if (mk == -INFINITY) continue;
@@ -215,11 +205,11 @@ __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece
             acc.add(w, v);
         }
         if (a.out) {
-            write_row<DP, E>(a, acc, row, lane);
+            write_row<DP, float>(a, acc, row, lane);
             continue;
         }
         const long long at = x.part * a.rows + row;
-        if (lane == 0) a.pml[at] = make_float2(acc.m, acc.l);
+        if (lane == 0) a.pml[row * a.parts + x.part] = make_float2(acc.m, acc.l);
         if (acc.m != -INFINITY) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
@@ -230,216 +220,31 @@ __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece
     }
 }
 
-// bf16, any head dim to DP: one warp = 8 query rows over the 16-key blocks wk, wk + nwk, .. of the split.
-// Probabilities enter the second product as two bf16 terms (the rounded value and what the rounding left), so
-// that its error stays that of fp32 sums: the products are bound by the loads of keys and values, and the
-// second term costs no time there.
-template <int DP>
-__global__ void __launch_bounds__(AT_THREADS, 2) k_kv_attend_mma(const __grid_constant__ AttendArgs a) {
-    extern __shared__ __align__(16) float kv_smem[];
-    constexpr int NC = DP / 32;    // chunk groups of a key
-    constexpr int NV = DP / 64;    // chunk groups of a value row
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int g = lane >> 2, j = lane & 3;
-    ptx::grid_dep_launch();
-    const Piece x = piece_of(a, blockIdx.x, warp);
-    const SidePlan& sp = x.prefix ? a.p : a.o;
-    const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
-    const int D = a.c.D;
-    uint4* qs = reinterpret_cast<uint4*>(kv_smem) + (warp / sp.wk) * (NC * 32);
-    if (x.wk == 0) load_q_frags<DP>(a.c, x.t, qs, lane);
-    // Keys this lane's two rows (columns 2 j, 2 j + 1 of the products) see, and the most any row of the tile sees.
-    const int n0 = row_seen(a.c, x.prefix, x.cache, x.t, x.t.r0 + 2 * j);
-    const int n1 = row_seen(a.c, x.prefix, x.cache, x.t, x.t.r0 + 2 * j + 1);
-    int lim = max(n0, n1), low = 0x7fffffff;
-    if (x.t.r0 + 2 * j < x.t.R) low = n0;
-    if (x.t.r0 + 2 * j + 1 < x.t.R) low = min(low, n1);
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-        lim = max(lim, __shfl_xor_sync(0xffffffffu, lim, o));
-        low = min(low, __shfl_xor_sync(0xffffffffu, low, o));
-    }
-    __syncthreads();
-    const long long nb = (lim + KR_KEYS - 1) / KR_KEYS;
-    const int b0 = (int)(nb * x.split / sp.splits), b1 = (int)(nb * (x.split + 1) / sp.splits);
-    const __nv_bfloat16* kbase = (const __nv_bfloat16*)s.k + x.cache * s.cs + (x.t.head0 / a.c.gq) * s.hs;
-    const __nv_bfloat16* vbase = (const __nv_bfloat16*)s.v + x.cache * s.cs + (x.t.head0 / a.c.gq) * s.hs;
-    float o[NV][4][4];
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][t][e] = 0.f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-    for (int blk = b0 + x.wk; blk < b1; blk += x.nwk) {
-        const int key0 = blk * KR_KEYS;
-        uint4 kf[NC][2], vf[NV][4];
-        {
-            const __nv_bfloat16* kp = kbase + (long long)(key0 + g) * s.rs + 8 * j;
-            const bool ok0 = key0 + g < lim, ok1 = key0 + g + 8 < lim;
-#pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const bool in = 8 * (4 * i + j) < D;
-                kf[i][0] = kr_ld(kp + 32 * i, ok0 && in);
-                kf[i][1] = kr_ld(kp + 8 * s.rs + 32 * i, ok1 && in);
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const int key = key0 + 2 * j + (h & 1) + 8 * (h >> 1);
-            const __nv_bfloat16* vp = vbase + (long long)key * s.rs + 8 * g;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) vf[i][h] = kr_ld(vp + 64 * i, key < lim && 8 * (g + 8 * i) < D);
-        }
-        float sc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const uint4 q = qs[32 * i + lane];
-            kr_mma(sc, kf[i][0].x, kf[i][1].x, kf[i][0].y, kf[i][1].y, q.x, q.y);
-            kr_mma(sc, kf[i][0].z, kf[i][1].z, kf[i][0].w, kf[i][1].w, q.z, q.w);
-        }
-        // Scores of keys g, g + 8 and rows 2 j, 2 j + 1; hidden ones are replaced, whatever they hold.
-        const float s00 = key0 + g < n0 ? sc[0] : -INFINITY;
-        const float s01 = key0 + g < n1 ? sc[1] : -INFINITY;
-        const float s10 = key0 + g + 8 < n0 ? sc[2] : -INFINITY;
-        const float s11 = key0 + g + 8 < n1 ? sc[3] : -INFINITY;
-        float x0 = fmaxf(s00, s10), x1 = fmaxf(s01, s11);
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-            x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, d));
-            x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, d));
-        }
-        if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
-            const float y0 = fmaxf(m0, x0), y1 = fmaxf(m1, x1);
-            const float a0 = m0 == -INFINITY ? 0.f : kr_ex2((m0 - y0) * a.c2), a1 = m1 == -INFINITY ? 0.f : kr_ex2((m1 - y1) * a.c2);
-            m0 = y0;
-            m1 = y1;
-            l0 *= a0;
-            l1 *= a1;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    o[i][t][0] *= a0;
-                    o[i][t][1] *= a1;
-                    o[i][t][2] *= a0;
-                    o[i][t][3] *= a1;
-                }
-        }
-        const float f0 = m0 == -INFINITY ? 0.f : m0, f1 = m1 == -INFINITY ? 0.f : m1;
-        const float p00 = kr_ex2((s00 - f0) * a.c2), p01 = kr_ex2((s01 - f1) * a.c2);
-        const float p10 = kr_ex2((s10 - f0) * a.c2), p11 = kr_ex2((s11 - f1) * a.c2);
-        l0 += p00 + p10;
-        l1 += p01 + p11;
-        const uint32_t h0 = kr_pack(p00, p01), h1 = kr_pack(p10, p11);
-        const uint32_t e0 = kr_pack(p00 - __uint_as_float(h0 << 16), p01 - __uint_as_float(h0 & 0xffff0000u));
-        const uint32_t e1 = kr_pack(p10 - __uint_as_float(h1 << 16), p11 - __uint_as_float(h1 & 0xffff0000u));
-        const uint32_t ph0 = kr_transpose(h0), ph1 = kr_transpose(h1), pe0 = kr_transpose(e0), pe1 = kr_transpose(e1);
-        auto product = [&](uint32_t bh0, uint32_t bh1, uint32_t be0, uint32_t be1) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const uint32_t v0[4] = {vf[i][0].x, vf[i][0].y, vf[i][0].z, vf[i][0].w};
-                const uint32_t v1[4] = {vf[i][1].x, vf[i][1].y, vf[i][1].z, vf[i][1].w};
-                const uint32_t v2[4] = {vf[i][2].x, vf[i][2].y, vf[i][2].z, vf[i][2].w};
-                const uint32_t v3[4] = {vf[i][3].x, vf[i][3].y, vf[i][3].z, vf[i][3].w};
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const uint32_t a0 = __byte_perm(v0[t], v1[t], 0x5410), a1 = __byte_perm(v0[t], v1[t], 0x7632);
-                    const uint32_t a2 = __byte_perm(v2[t], v3[t], 0x5410), a3 = __byte_perm(v2[t], v3[t], 0x7632);
-                    kr_mma(o[i][t], a0, a1, a2, a3, bh0, bh1);
-                    kr_mma(o[i][t], a0, a1, a2, a3, be0, be1);
-                }
-            }
-        };
-        // A block that some rows see only a part of: 0 times an infinity or NaN that one row sees and another does
-        // not would reach the other. Where it holds such a value, row by row over the row's own keys.
-        bool odd = false;
-        if (low < min(key0 + KR_KEYS, lim)) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const uint32_t v[4] = {vf[i][h].x, vf[i][h].y, vf[i][h].z, vf[i][h].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        odd = odd || (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
-                }
-            odd = __any_sync(0xffffffffu, odd);
-        }
-        if (!odd) {
-            product(ph0, ph1, pe0, pe1);
-        } else {
-            for (int r = KR_ROWS - 1; r >= 0; --r) {
-                // Row r's count, from a lane that holds it.
-                const int nr = __shfl_sync(0xffffffffu, (r & 1) ? n1 : n0, r >> 1);
-                uint4 keep_v[NV][4];
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        keep_v[i][h] = vf[i][h];
-                        if (key0 + 2 * j + (h & 1) + 8 * (h >> 1) >= nr) vf[i][h] = make_uint4(0, 0, 0, 0);
-                    }
-                const bool mine = g == r;
-                product(mine ? ph0 : 0u, mine ? ph1 : 0u, mine ? pe0 : 0u, mine ? pe1 : 0u);
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) vf[i][h] = keep_v[i][h];
-            }
-        }
-    }
-    // Sums over the key lanes.
-#pragma unroll
-    for (int d = 4; d < 32; d <<= 1) {
-        l0 += __shfl_xor_sync(0xffffffffu, l0, d);
-        l1 += __shfl_xor_sync(0xffffffffu, l1, d);
-    }
-    __syncthreads();   // the query fragments have been read
-    float* f = kv_smem + warp * MergeSmem<DP>::WARP_FLOATS;
-    constexpr int LD = MergeSmem<DP>::LD;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int d = 8 * (g + 8 * i);
-        *(float4*)(f + (2 * j) * LD + d) = make_float4(o[i][0][0], o[i][0][2], o[i][1][0], o[i][1][2]);
-        *(float4*)(f + (2 * j) * LD + d + 4) = make_float4(o[i][2][0], o[i][2][2], o[i][3][0], o[i][3][2]);
-        *(float4*)(f + (2 * j + 1) * LD + d) = make_float4(o[i][0][1], o[i][0][3], o[i][1][1], o[i][1][3]);
-        *(float4*)(f + (2 * j + 1) * LD + d + 4) = make_float4(o[i][2][1], o[i][2][3], o[i][3][1], o[i][3][3]);
-    }
-    if (g == 0) {
-        float* ml = f + KR_ROWS * LD + 4 * j;
-        ml[0] = m0;
-        ml[1] = l0;
-        ml[2] = m1;
-        ml[3] = l1;
-    }
-    merge_and_write<DP, __nv_bfloat16>(a, x, sp, kv_smem, warp, lane);
-}
-
-// The same work for caches that bulk tensor copies can read (head dims from 64, see kv_maps.h): each warp
-// streams its 16 KB blocks of 16 (D = 256) to 64 (D = 64) keys through shared memory of its own, the next keys on
-// their way while this block's values are used and the other way round, and reads fragments with ldmatrix. Against loads
-// to registers this needs half the registers and no room in L1 for what is in flight, so that a block fits beside
-// the 128-row tiles on their SM. Blocks are persistent: piece blockIdx.x, + gridDim.x, ..
-constexpr int RT_WARPS = 2;
-constexpr int RT_THREADS = 32 * RT_WARPS;
-constexpr int RT_BLOCK = 16384;   // bytes of a warp's keys and values
-constexpr uint64_t RT_WAIT_NS = 200ull * 1000 * 1000;
+// bf16. A warp works alone: it takes pieces (8 query rows over a range of keys) in turn and streams their blocks of 16
+// (D to 256) to 64 (D to 64) keys, 16 KB with their values, through two stages of shared memory of its own by 16-byte
+// asynchronous copies, the next piece's first blocks and query rows behind this one's last. So a piece has no start-up
+// of its own and pieces can be small enough to even out requests of different lengths; what is in flight needs neither
+// registers nor room in L1; and rows that no query of the piece sees arrive as zeros.
+//
+// Keys are the 16 rows of mma.sync m16n8k16 and query rows its 8 columns; the values' product runs over keys with
+// d as its rows, so that the probabilities turn from one's result into the other's operand by 8 x 8 transposes within
+// the warp. Probabilities enter that product as two bf16 terms (the rounded value and what the rounding left), so that
+// its error stays that of fp32 sums: the kernel is bound by memory, not by its products.
+constexpr int RT_STAGE = 16384;
 
 template <int DP>
 struct RtSmem {
-    static constexpr int KEYS = RT_BLOCK / (4 * DP);   // keys of a block
-    static constexpr int HALF = RT_BLOCK / 2;          // its keys, then its values
-    static constexpr int BAR_OFF = RT_WARPS * RT_BLOCK > RT_WARPS * MergeSmem<DP>::WARP_FLOATS * 4
-                                       ? RT_WARPS * RT_BLOCK
-                                       : RT_WARPS * MergeSmem<DP>::WARP_FLOATS * 4;
-    static constexpr int BYTES = BAR_OFF + 8 * 2 * RT_WARPS;
-};
-
-struct RtMaps {
-    CUtensorMap k[2], v[2];   // prefix, own
-    int3 at[2];
+    static constexpr int KEYS = RT_STAGE / (4 * DP);     // keys of a block
+    static constexpr int HALF = RT_STAGE / 2;            // its keys' bytes; its values follow
+    static constexpr int QBYTES = KR_ROWS * DP * 2;      // query rows of a piece: two pieces' worth
+    static constexpr int Q_OFF = 2 * RT_STAGE;
+    static constexpr int SEEN_OFF = Q_OFF + 2 * QBYTES;  // [AHEAD][8] counts of the pieces in hand
+    static constexpr int AHEAD = 4;
+    static constexpr int BYTES = SEEN_OFF + AHEAD * KR_ROWS * 4;
+    static constexpr int BESIDE = DP == 256 ? 2 : DP == 128 ? 3 : 4;   // blocks that fit beside the tiles on an SM
+    static constexpr int ALONE = DP == 256 ? 5 : 6;                    // and without them
+    // A warp beside the tiles has the registers that theirs leave in its quarter of the SM's file.
+    static constexpr int REGS = DP == 256 ? 224 : 152;
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
@@ -456,36 +261,99 @@ __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
 }
 
 template <int DP>
-__global__ void __launch_bounds__(RT_THREADS) k_kv_attend_rows(const __grid_constant__ RtMaps maps,
-                                                               const __grid_constant__ AttendArgs a) {
+__global__ void __maxnreg__(RtSmem<DP>::REGS) k_kv_attend_rows(const __grid_constant__ AttendArgs a) {
     using L = RtSmem<DP>;
-    extern __shared__ __align__(1024) uint8_t rt_smem[];
+    extern __shared__ __align__(128) uint8_t rt_smem[];
     constexpr int MT = L::KEYS / 16;   // 16-key tiles of a block
     constexpr int ND = DP / 16;
-    const int warp = ptx::warp_index(), lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
-    uint8_t* block = rt_smem + warp * RT_BLOCK;
-    const uint32_t ks = ptx::smem_u32(block), vs = ks + L::HALF;
-    uint64_t* bar = (uint64_t*)(rt_smem + L::BAR_OFF) + 2 * warp;   // keys, values
+    constexpr int CH = DP / 8;         // 16-byte chunks of a row; chunk c of row r lies at c ^ (r & 7)
+    constexpr int RPI = 32 / CH > 0 ? 32 / CH : 1;   // rows one instruction of the warp copies
+    const int lane = threadIdx.x, g = lane >> 2, j = lane & 3;
+    const uint32_t sm = ptx::smem_u32(rt_smem);
+    int* const counts = (int*)(rt_smem + L::SEEN_OFF);
     ptx::grid_dep_launch();
-    if (lane == 0) {
-        ptx::mbar_init(&bar[0], 1);
-        ptx::mbar_init(&bar[1], 1);
-        ptx::fence_mbar_init();
-    }
-    __syncwarp();
-    int asked[2] = {0, 0}, done[2] = {0, 0};   // copies asked for and waited for, of keys and of values
-    bool good = true;
-    const long long pieces = a.p.blocks + a.o.blocks;
-    for (long long piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
-        const Piece x = piece_of(a, piece, warp);
+    const uint32_t pieces = (uint32_t)(a.p.blocks + a.o.blocks);
+    const int D = a.c.D, mych = lane % CH, myrow = lane / CH;
+    const bool dlive = 8 * mych < D;
+    const float slack = 8.f / a.c2;
+
+    // ---- what is to be copied: pieces opened in order, block by block
+    uint32_t f_piece = blockIdx.x;   // the next piece to open
+    int f_seq = 0, f_full = 0, f_blk = 0, f_end = 0, f_lim = 0;   // f_full: opened pieces that have blocks
+    const __nv_bfloat16 *f_k = nullptr, *f_v = nullptr;   // this lane's chunk of the open piece's row 0
+    long long f_rs = 0;
+    int ahead = 0;                   // this lane's row's count of the next piece (lanes 0-7), on its way since the last one opened
+    auto peek = [&]() {
+        ahead = 0;
+        if (f_piece < pieces) {
+            const Piece x = piece_of(a, f_piece, 0);
+            if (lane < KR_ROWS) ahead = row_seen(a.c, x.prefix, x.cache, x.t, x.t.r0 + lane);
+        }
+    };
+    int issued = 0, used = 0;        // blocks asked for, and through
+    int seq = 0, full = 0;           // pieces finished, and begun with blocks
+    // Asks for the next block, opening pieces on the way (at most AHEAD in hand); false if there is none.
+    auto produce = [&]() {
+        while (f_blk >= f_end) {
+            if (f_piece >= pieces || f_seq - seq >= L::AHEAD) return false;
+            const Piece x = piece_of(a, f_piece, 0);
+            const SidePlan& sp = x.prefix ? a.p : a.o;
+            const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
+            if (lane < KR_ROWS) counts[(f_seq & (L::AHEAD - 1)) * KR_ROWS + lane] = ahead;
+            f_lim = __reduce_max_sync(0xffffffffu, lane < KR_ROWS ? ahead : 0);
+            const int nb = (f_lim + L::KEYS - 1) / L::KEYS;
+            f_blk = (int)((long long)nb * x.split / sp.splits);
+            f_end = (int)((long long)nb * (x.split + 1) / sp.splits);
+            if (f_blk < f_end) {
+                const long long base = x.cache * s.cs + x.kvh * s.hs + (dlive ? 8 * mych : 0);
+                f_k = static_cast<const __nv_bfloat16*>(s.k) + base;
+                f_v = static_cast<const __nv_bfloat16*>(s.v) + base;
+                f_rs = s.rs;
+                // The query rows travel with the first block. (Two pieces' fit: with two blocks in hand, the piece with
+                // blocks before the last one is through.)
+#pragma unroll
+                for (int i = 0; i < KR_ROWS / RPI; ++i) {
+                    const int rr = i * RPI + myrow, r = x.t.r0 + rr;
+                    const bool in = dlive && r < x.t.R;
+                    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + (in ? row_query(a.c, x.t, r) + 8 * mych : 0);
+                    ptx::cp_async_16(sm + L::Q_OFF + (f_full & 1) * L::QBYTES + rr * (DP * 2) + ((mych ^ (rr & 7)) << 4), q, in);
+                }
+                ++f_full;
+            }
+            ++f_seq;
+            f_piece += gridDim.x;
+            peek();
+        }
+        const uint32_t dst = sm + (issued & 1) * RT_STAGE;
+        const int key0 = f_blk * L::KEYS;
+        const __nv_bfloat16 *k = f_k + (long long)(key0 + myrow) * f_rs, *v = f_v + (long long)(key0 + myrow) * f_rs;
+#pragma unroll
+        for (int i = 0; i < L::KEYS / RPI; ++i) {
+            const int rr = i * RPI + myrow;
+            const bool in = dlive && key0 + rr < f_lim;
+            const uint32_t at = rr * (DP * 2) + ((mych ^ (rr & 7)) << 4);
+            ptx::cp_async_16(dst + at, in ? k : f_k, in);
+            ptx::cp_async_16(dst + L::HALF + at, in ? v : f_v, in);
+            k += RPI * f_rs;
+            v += RPI * f_rs;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        ++issued;
+        ++f_blk;
+        return true;
+    };
+
+    peek();
+    if (produce()) produce();
+    for (uint32_t piece = blockIdx.x; piece < pieces; piece += gridDim.x, ++seq) {
+        const Piece x = piece_of(a, piece, 0);
         const SidePlan& sp = x.prefix ? a.p : a.o;
-        const int side = x.prefix ? 0 : 1;
-        const int kvh = x.t.head0 / a.c.gq;
-        const int n0 = row_seen(a.c, x.prefix, x.cache, x.t, x.t.r0 + 2 * j);
-        const int n1 = row_seen(a.c, x.prefix, x.cache, x.t, x.t.r0 + 2 * j + 1);
-        int lim = max(n0, n1), low = 0x7fffffff;
-        if (x.t.r0 + 2 * j < x.t.R) low = n0;
-        if (x.t.r0 + 2 * j + 1 < x.t.R) low = min(low, n1);
+        if (f_seq <= seq) produce();   // (opens it, if the pieces before had fewer blocks than there are stages)
+        __syncwarp();
+        // What the lane's rows 2 j, 2 j + 1 see, and the most and the least of the tile's rows.
+        const int n0 = counts[(seq & (L::AHEAD - 1)) * KR_ROWS + 2 * j], n1 = counts[(seq & (L::AHEAD - 1)) * KR_ROWS + 2 * j + 1];
+        const int rj = x.t.r0 + 2 * j;
+        int lim = max(n0, n1), low = min(rj < x.t.R ? n0 : 0x7fffffff, rj + 1 < x.t.R ? n1 : 0x7fffffff);
 #pragma unroll
         for (int o = 1; o < 4; o <<= 1) {
             lim = max(lim, __shfl_xor_sync(0xffffffffu, lim, o));
@@ -493,79 +361,88 @@ __global__ void __launch_bounds__(RT_THREADS) k_kv_attend_rows(const __grid_cons
         }
         const int nb = (lim + L::KEYS - 1) / L::KEYS;
         const int b0 = (int)((long long)nb * x.split / sp.splits), b1 = (int)((long long)nb * (x.split + 1) / sp.splits);
-        auto load = [&](int what, int blk) {
-            ++asked[what];
-            if (!ptx::elect_one()) return;
-            ptx::mbar_expect_tx(&bar[what], (uint32_t)L::HALF);
-            for (int db = 0; db < DP / 64; ++db)
-                kv_load_box(block + what * L::HALF + db * (L::KEYS * 128), what ? &maps.v[side] : &maps.k[side], &bar[what],
-                            db * 64, maps.at[side], kvh, blk * L::KEYS, x.cache);
-        };
-        const int first = b0 + x.wk;
-        if (first < b1 && good) {
-            load(0, first);
-            load(1, first);
-        }
-        // Query fragments: row g, elements 16 i + 2 j, + 1 and + 8, + 9.
         uint32_t qf[ND][2];
-        {
-            const int r = x.t.r0 + g;
-            const bool in = r < x.t.R;
-            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + 2 * j;
-            if (in) q += row_token(x.t, a.c.gq, r) * a.c.q_stride + (long long)(x.t.head0 + r % a.c.gq) * a.c.D;
-#pragma unroll
-            for (int i = 0; i < ND; ++i)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    qf[i][e] = in && 16 * i + 8 * e < a.c.D ? __ldg((const uint32_t*)(q + 16 * i + 8 * e)) : 0u;
-        }
         float o[ND][4];
 #pragma unroll
         for (int i = 0; i < ND; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-        for (int blk = first; blk < b1 && good; blk += x.nwk) {
+        for (int blk = b0; blk < b1; ++blk) {
             const int key0 = blk * L::KEYS;
-            good = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&bar[0], done[0] & 1, RT_WAIT_NS));
-            if (!good) break;
-            ++done[0];
-            float sc[MT][4];
+            if (issued == used) produce();
+            // This block's copies have landed; the one after may be on its way.
+            if (issued - used > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            const uint32_t ks = sm + (used & 1) * RT_STAGE, vs = ks + L::HALF;
+            if (blk == b0) {
+                const uint32_t qs = sm + L::Q_OFF + (full++ & 1) * L::QBYTES + (lane & 7) * (DP * 2);
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+                for (int i = 0; i < ND; i += 2) {
+                    uint32_t f[4];
+                    ldsm4(f, qs + (((2 * i + (lane >> 3)) ^ (lane & 7)) << 4));
+                    qf[i][0] = f[0];
+                    qf[i][1] = f[1];
+                    qf[i + 1][0] = f[2];
+                    qf[i + 1][1] = f[3];
+                }
+            }
+            // Four chains of products whatever the shape: one of D / 16 steps would be its latency.
+            constexpr int NCH = MT >= 4 ? 1 : 4 / MT;
+            float part[NCH][MT][4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[t][e] = 0.f;
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) part[c][t][e] = 0.f;
             const int kr = (lane & 7) + (lane & 8);   // key of this lane's matrix row; its chunk is 2 i + lane / 16
 #pragma unroll
             for (int i = 0; i < ND; ++i)
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
-                    const int ch = 2 * i + (lane >> 4);
                     uint32_t f[4];
-                    ldsm4(f, ks + (ch >> 3) * (L::KEYS * 128) + (16 * t + kr) * 128 + (((ch & 7) ^ (kr & 7)) << 4));
-                    kr_mma(sc[t], f[0], f[1], f[2], f[3], qf[i][0], qf[i][1]);
+                    ldsm4(f, ks + (16 * t + kr) * (DP * 2) + (((2 * i + (lane >> 4)) ^ (kr & 7)) << 4));
+                    kr_mma(part[i % NCH][t], f[0], f[1], f[2], f[3], qf[i][0], qf[i][1]);
                 }
-            __syncwarp();
-            if (blk + x.nwk < b1) load(0, blk + x.nwk);
+            float sc[MT][4];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[t][e] = part[0][t][e];
+#pragma unroll
+                    for (int c = 1; c < NCH; ++c) sc[t][e] += part[c][t][e];
+                }
             // Keys g, g + 8 of each tile, rows 2 j, 2 j + 1; hidden scores are replaced, whatever they hold.
+            const bool cut = low < key0 + L::KEYS;   // the same for the warp
+            if (cut) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int key = key0 + 16 * t + g + 8 * e;
+                        if (key >= n0) sc[t][2 * e] = -INFINITY;
+                        if (key >= n1) sc[t][2 * e + 1] = -INFINITY;
+                    }
+            }
             float x0 = -INFINITY, x1 = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int key = key0 + 16 * t + g + 8 * e;
-                    if (key >= n0) sc[t][2 * e] = -INFINITY;
-                    if (key >= n1) sc[t][2 * e + 1] = -INFINITY;
                     x0 = fmaxf(x0, sc[t][2 * e]);
                     x1 = fmaxf(x1, sc[t][2 * e + 1]);
                 }
-            }
+            // The maximum moves only when a score passes it by more than 8 in log2 units (probabilities stay below 2^8):
+            // most blocks do not, and need no maximum over the keys' lanes.
+            if (__any_sync(0xffffffffu, x0 > m0 + slack || x1 > m1 + slack)) {
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) {
-                x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, d));
-                x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, d));
-            }
-            if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
+                for (int d = 4; d < 32; d <<= 1) {
+                    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, d));
+                    x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, d));
+                }
                 const float y0 = fmaxf(m0, x0), y1 = fmaxf(m1, x1);
                 const float a0 = m0 == -INFINITY ? 0.f : kr_ex2((m0 - y0) * a.c2);
                 const float a1 = m1 == -INFINITY ? 0.f : kr_ex2((m1 - y1) * a.c2);
@@ -595,95 +472,100 @@ __global__ void __launch_bounds__(RT_THREADS) k_kv_attend_rows(const __grid_cons
                     ph[t][e] = kr_transpose(h);
                     pe[t][e] = kr_transpose(r);
                 }
-            good = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&bar[1], done[1] & 1, RT_WAIT_NS));
-            if (!good) break;
-            ++done[1];
             const int vr = (lane & 7) + ((lane >> 4) << 3);   // key of this lane's matrix row; its chunk is 2 i + bit 3
             auto values = [&](int t, int i, uint32_t(&f)[4]) {
-                const int ch = 2 * i + ((lane >> 3) & 1);
-                ldsm4_t(f, vs + (ch >> 3) * (L::KEYS * 128) + (16 * t + vr) * 128 + (((ch & 7) ^ (vr & 7)) << 4));
+                ldsm4_t(f, vs + (16 * t + vr) * (DP * 2) + (((2 * i + ((lane >> 3) & 1)) ^ (vr & 7)) << 4));
             };
-            // Values of keys from `n` on become zeros, whatever they hold (0 times a NaN is not 0).
-            auto mask = [&](int t, int n, uint32_t& lo, uint32_t& hi) {
-                const int key = key0 + 16 * t + 2 * j;
-                lo = (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
-                hi = (key + 8 < n ? 0xffffu : 0u) | (key + 9 < n ? 0xffff0000u : 0u);
-            };
-            // A block that some rows see only a part of, with an infinity or NaN among its values: row by row over the
-            // row's own keys (one row's would reach another).
+            // A block that some rows see only a part of, with an infinity or NaN among its values: 0 times one of those
+            // that one row sees would reach another. Then row by row, over the row's own keys.
             bool odd = false;
-            if (low < min(key0 + L::KEYS, lim)) {
+            if (cut && low < lim) {
 #pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    uint32_t lo, hi;
-                    mask(t, lim, lo, hi);
+                for (int t = 0; t < MT; ++t)
                     for (int i = 0; i < ND; ++i) {
                         uint32_t f[4];
                         values(t, i, f);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t v = f[e] & (e < 2 ? lo : hi);
-                            odd = odd || (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+                        for (int e = 0; e < 4; ++e) odd = odd || (f[e] & 0x7f80u) == 0x7f80u || (f[e] & 0x7f800000u) == 0x7f800000u;
+                    }
+                odd = __any_sync(0xffffffffu, odd);
+            }
+            if (!odd) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) {
+                        uint32_t f[4];
+                        values(t, i, f);
+                        kr_mma(o[i], f[0], f[1], f[2], f[3], ph[t][0], ph[t][1]);
+                        kr_mma(o[i], f[0], f[1], f[2], f[3], pe[t][0], pe[t][1]);
+                    }
+            } else {
+#pragma unroll 1
+                for (int r = 0; r < KR_ROWS; ++r) {
+                    const int n = __shfl_sync(0xffffffffu, (r & 1) ? n1 : n0, r >> 1);
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        const int key = key0 + 16 * t + 2 * j;
+                        const uint32_t lo = (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
+                        const uint32_t hi = (key + 8 < n ? 0xffffu : 0u) | (key + 9 < n ? 0xffff0000u : 0u);
+#pragma unroll
+                        for (int i = 0; i < ND; ++i) {
+                            uint32_t f[4];
+                            values(t, i, f);
+                            kr_mma(o[i], f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, g == r ? ph[t][0] : 0u, g == r ? ph[t][1] : 0u);
+                            kr_mma(o[i], f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, g == r ? pe[t][0] : 0u, g == r ? pe[t][1] : 0u);
                         }
                     }
                 }
-                odd = __any_sync(0xffffffffu, odd);
             }
-            auto product = [&](int n, bool cut, int row) {
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    uint32_t lo = ~0u, hi = ~0u;
-                    if (cut) mask(t, n, lo, hi);
-                    const bool mine = row < 0 || g == row;
-                    const uint32_t h0 = mine ? ph[t][0] : 0u, h1 = mine ? ph[t][1] : 0u;
-                    const uint32_t e0 = mine ? pe[t][0] : 0u, e1 = mine ? pe[t][1] : 0u;
-#pragma unroll
-                    for (int i = 0; i < ND; ++i) {
-                        uint32_t f[4];
-                        values(t, i, f);
-                        kr_mma(o[i], f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, h0, h1);
-                        kr_mma(o[i], f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, e0, e1);
-                    }
-                }
-            };
-            if (!odd) {
-                product(lim, key0 + L::KEYS > lim, -1);
-            } else {
-#pragma unroll 1
-                for (int r = 0; r < KR_ROWS; ++r) product(__shfl_sync(0xffffffffu, (r & 1) ? n1 : n0, r >> 1), true, r);
-            }
-            __syncwarp();
-            if (blk + x.nwk < b1) load(1, blk + x.nwk);
+            __syncwarp();   // every lane has read the stage
+            ++used;
+            produce();
         }
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, d);
             l1 += __shfl_xor_sync(0xffffffffu, l1, d);
         }
-        // Copies that are still on their way (a wait gave up) land before their memory is used for anything else.
-        for (int what = 0; what < 2; ++what)
-            for (; done[what] < asked[what]; ++done[what]) (void)ptx::mbar_wait_bounded(&bar[what], done[what] & 1, RT_WAIT_NS);
-        __syncthreads();   // every warp is through with its blocks: their memory holds the merge now
-        float* f = (float*)rt_smem + warp * MergeSmem<DP>::WARP_FLOATS;
-        constexpr int LD = MergeSmem<DP>::LD;
-        if (good) {
+        // Rows 2 j (elements 0 and 2 of each fragment) and 2 j + 1 (1 and 3), d = 16 i + g and + 8.
+        const bool in0 = rj < x.t.R, in1 = rj + 1 < x.t.R;
+        const long long row0 = in0 ? row_index(a.c, x.t, rj) : 0, row1 = in1 ? row_index(a.c, x.t, rj + 1) : 0;
+        if (a.out) {
+            // The only part: the result itself. Lanes g and g + 1 exchange halves, so that the even one has a pair of row
+            // 2 j and the odd one a pair of row 2 j + 1.
+            const bool even = (g & 1) == 0;
+            const float inv0 = l0 > 0.f ? 1.f / l0 : 0.f, inv1 = l1 > 0.f ? 1.f / l1 : 0.f;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (even ? row0 : row1) * D + (g & ~1);
 #pragma unroll
             for (int i = 0; i < ND; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[(2 * j + (e & 1)) * LD + 16 * i + g + 8 * (e >> 1)] = o[i][e];
+                for (int e = 0; e < 2; ++e) {
+                    const float u = o[i][2 * e] * inv0, v = o[i][2 * e + 1] * inv1;
+                    const float w = __shfl_xor_sync(0xffffffffu, even ? v : u, 4);
+                    if ((even ? in0 : in1) && 16 * i + 8 * e < D)
+                        *(uint32_t*)(out + 16 * i + 8 * e) = even ? kr_pack(u, w) : kr_pack(w, v);
+                }
+            if (g == 0 && a.lse) {
+                if (in0) a.lse[row0] = m0 == -INFINITY ? -INFINITY : fmaf(m0, a.c.scale, logf(l0));
+                if (in1) a.lse[row1] = m1 == -INFINITY ? -INFINITY : fmaf(m1, a.c.scale, logf(l1));
+            }
+        } else {
+            const long long at0 = x.part * a.rows + row0, at1 = x.part * a.rows + row1;
+            if (g == 0 && in0) a.pml[row0 * a.parts + x.part] = make_float2(m0, l0);
+            if (g == 0 && in1) a.pml[row1 * a.parts + x.part] = make_float2(m1, l1);
+            float *o0 = a.po + at0 * D + g, *o1 = a.po + at1 * D + g;
+            const bool w0 = in0 && m0 != -INFINITY, w1 = in1 && m1 != -INFINITY;
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (16 * i + 8 * e >= D) continue;
+                    if (w0) o0[16 * i + 8 * e] = o[i][2 * e];
+                    if (w1) o1[16 * i + 8 * e] = o[i][2 * e + 1];
+                }
         }
-        if (g == 0) {
-            float* ml = f + KR_ROWS * LD + 4 * j;
-            ml[0] = m0;
-            ml[1] = l0;
-            ml[2] = m1;
-            ml[3] = l1;
-        }
-        merge_and_write<DP, __nv_bfloat16>(a, x, sp, (const float*)rt_smem, warp, lane);
-        ptx::fence_proxy_async_smem();   // before the next piece's copies land where the merge was
-        __syncthreads();
     }
-    if (!good && lane == 0) atomicCAS(a.err, 0, (int)DEV_TIMEOUT_WEIGHTS);
 }
 
 // fp32 on CUDA cores: one warp = 8 query rows over 32-key blocks. Scores with a key per lane, the
@@ -698,13 +580,14 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
     const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
     const int D = a.c.D;
     float* qs = kv_smem + warp / sp.wk * (KR_ROWS * DP);
-    if (x.wk == 0) {
+    const int wk = warp % sp.wk;
+    if (wk == 0) {
         for (int e = lane; e < KR_ROWS * (DP / 4); e += 32) {
             const int rr = e / (DP / 4), d = 4 * (e % (DP / 4)), r = x.t.r0 + rr;
             const float* q = static_cast<const float*>(a.c.q);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (r < x.t.R && d < D)
-                v = *(const float4*)(q + row_token(x.t, a.c.gq, r) * a.c.q_stride + (long long)(x.t.head0 + r % a.c.gq) * D + d);
+                v = *(const float4*)(q + row_query(a.c, x.t, r) + d);
             *(float4*)(qs + rr * DP + d) = v;
         }
     }
@@ -717,8 +600,8 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
     __syncthreads();
     const long long nb = (lim + 31) / 32;
     const int b0 = (int)(nb * x.split / sp.splits), b1 = (int)(nb * (x.split + 1) / sp.splits);
-    const float* kbase = (const float*)s.k + x.cache * s.cs + (x.t.head0 / a.c.gq) * s.hs;
-    const float* vbase = (const float*)s.v + x.cache * s.cs + (x.t.head0 / a.c.gq) * s.hs;
+    const float* kbase = (const float*)s.k + x.cache * s.cs + (x.kvh) * s.hs;
+    const float* vbase = (const float*)s.v + x.cache * s.cs + (x.kvh) * s.hs;
     constexpr int NI = (DP + 127) / 128;
     float4 o[KR_ROWS][NI];
     float m[KR_ROWS], l[KR_ROWS];
@@ -729,7 +612,7 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
 #pragma unroll
         for (int i = 0; i < NI; ++i) o[r][i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    for (int blk = b0 + x.wk; blk < b1; blk += x.nwk) {
+    for (int blk = b0 + wk; blk < b1; blk += sp.wk) {
         const int key0 = blk * 32, key = key0 + lane;
         float p[KR_ROWS];
 #pragma unroll
@@ -802,36 +685,46 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
             f[KR_ROWS * MergeSmem<DP>::LD + 2 * r + 1] = l[r];
         }
     }
-    merge_and_write<DP, float>(a, x, sp, kv_smem, warp, lane);
+    merge_and_write<DP>(a, x, sp, kv_smem, warp, lane);
 }
 
-// Joins the parts of all rows: `wpr` warps (1, 2 or 4) a row, each with every wpr-th part.
+// Joins the parts of all rows: `wpr` warps (a power of two) a row, each with every wpr-th part, then the warps in order.
+constexpr int CB_WARPS = 16;   // most of a block
 template <int DP, typename E>
-__global__ void __launch_bounds__(AT_THREADS) k_kv_combine(const __grid_constant__ AttendArgs a, int wpr) {
-    __shared__ float4 so[AT_WARPS][RowAcc<DP>::NI][32];
-    __shared__ float sl[AT_WARPS];
+__global__ void __launch_bounds__(32 * CB_WARPS) k_kv_combine(const __grid_constant__ AttendArgs a, int wpr) {
+    __shared__ float4 so[CB_WARPS][RowAcc<DP>::NI][32];
+    __shared__ float2 sml[CB_WARPS];
     constexpr int NI = RowAcc<DP>::NI;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp % wpr;
-    const long long row = ((long long)blockIdx.x * AT_WARPS + warp) / wpr;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp & (wpr - 1);
+    const long long row = ((long long)blockIdx.x * (blockDim.x >> 5) + warp) / wpr;
     ptx::grid_dep_wait();
     RowAcc<DP> acc;
     acc.m = -INFINITY;
     acc.l = 0.f;
 #pragma unroll
     for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row < a.rows) join_parts<DP>(a, acc, row, a.p.splits + a.o.splits, first, wpr, lane);
+    if (row < a.rows) join_parts<DP>(a, acc, row, first, wpr, lane);
     if (wpr > 1) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) so[warp][i][lane] = acc.o[i];
-        if (lane == 0) sl[warp] = acc.l;
+        if (lane == 0) sml[warp] = make_float2(acc.m, acc.l);
         __syncthreads();
         if (first != 0) return;
-        for (int k = 1; k < wpr; ++k) {
+        float M = acc.m;
+        for (int k = 1; k < wpr; ++k) M = fmaxf(M, sml[warp + k].x);
+        const float m = acc.m;
+        acc.m = M;
+        acc.l = 0.f;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < wpr; ++k) {
+            const float2 ml = k == 0 ? make_float2(m, sml[warp].y) : sml[warp + k];
+            const float w = ml.x == -INFINITY ? 0.f : kr_ex2((ml.x - M) * a.c2);
             float4 v[NI];
 #pragma unroll
             for (int i = 0; i < NI; ++i) v[i] = so[warp + k][i][lane];
-            acc.add(1.f, v);
-            acc.l += sl[warp + k];
+            acc.add(w, v);
+            acc.l += w * ml.y;
         }
     }
     if (row < a.rows) write_row<DP, E>(a, acc, row, lane);
@@ -843,9 +736,11 @@ long long ws_rows(const jpi_kv_handle* h) {
     return 2 * rows + 512ll * h->num_sms;
 }
 
-// A side's pieces for blocks of `warps` warps: key splits until there are `want` pieces in all, as long as a warp keeps
-// `least` keys and the parts fit their half of the workspace.
-SidePlan plan_side(const jpi_kv_handle* h, const KvCall& c, bool prefix, int warps, int least, long long want) {
+// A side's pieces for blocks of `warps` warps, whose warps take `step` keys at a time. Key splits: up to `want` pieces
+// in all while a warp keeps `least` keys (below that a part's rows are as many bytes as a good share of its keys); but a
+// call of few pieces is split down to single steps, as far as two blocks an SM go: it is waited for. The parts fit their
+// half of the workspace.
+SidePlan plan_side(const jpi_kv_handle* h, const KvCall& c, bool prefix, int warps, int step, int least, long long want) {
     SidePlan s;
     const KvSide& side = prefix ? c.prefix : c.own;
     if (side.rows == 0) return s;
@@ -857,9 +752,12 @@ SidePlan plan_side(const jpi_kv_handle* h, const KvCall& c, bool prefix, int war
     s.tiles = (int)((rt + s.wr - 1) / s.wr);
     const long long blocks = (long long)caches * c.K * s.tiles, rows = (long long)c.batch * c.tokens * c.H;
     const long long room = std::max(1ll, (ws_rows(h) / 2) / rows);
-    const long long splits = std::min({want / blocks, room, (long long)(side.rows + least * s.wk - 1) / (least * s.wk)});
-    s.splits = (int)std::max(1ll, splits);
+    const long long coarse = std::min(want / blocks, ((long long)side.rows + least * s.wk - 1) / (least * s.wk));
+    const long long fine = std::min(2ll * h->num_sms / blocks, ((long long)side.rows + step * s.wk - 1) / (step * s.wk));
+    s.splits = (int)std::max(1ll, std::min(std::max(coarse, fine), room));
     s.blocks = blocks * s.splits;
+    s.by_splits = KvDiv((uint32_t)s.splits);
+    s.by_tiles = KvDiv((uint32_t)s.tiles);
     return s;
 }
 
@@ -872,23 +770,23 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
     a.po = static_cast<float*>(h->ws);
     a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
     a.lse = lse;
-    a.err = h->dev_err;
     int splits = 0;
     const bool tiles = kv_prefix_splits(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), &splits);
-    // The row kernel: on bulk copies where both sides' strides allow them.
-    KvMapDims md[2];
-    const bool copies = h->bf16 && c.D >= 64 && kv_maps_available() &&
-                        (tiles || c.prefix.rows == 0 || kv_map_dims(c.prefix, c.K, c.D, c.groups, &md[0])) &&
-                        (c.own.rows == 0 || kv_map_dims(c.own, c.K, c.D, c.batch, &md[1]));
-    const int warps = copies ? RT_WARPS : AT_WARPS, least = copies ? RtSmem<DP>::KEYS : h->bf16 ? KR_KEYS : 32;
-    const long long want = 2ll * h->num_sms;
-    a.p = plan_side(h, c, true, warps, least, want);
-    a.o = plan_side(h, c, false, warps, least, want);
+    if (h->bf16) {
+        // Single warps with 64 KB of keys and values or more each.
+        constexpr int KEYS = RtSmem<DP>::KEYS;
+        const long long want = (long long)(tiles ? RtSmem<DP>::BESIDE : RtSmem<DP>::ALONE) * h->num_sms;
+        a.p = plan_side(h, c, true, 1, KEYS, 4 * KEYS, want);
+        a.o = plan_side(h, c, false, 1, KEYS, 4 * KEYS, want);
+    } else {
+        a.p = plan_side(h, c, true, AT_WARPS, 32, 32, 2ll * h->num_sms);
+        a.o = plan_side(h, c, false, AT_WARPS, 32, 32, 2ll * h->num_sms);
+    }
     if (tiles) {
         a.p.blocks = 0;
         a.p.splits = splits;
     }
-    const int parts = a.p.splits + a.o.splits;
+    const int parts = a.parts = a.p.splits + a.o.splits;
     const long long pieces = a.p.blocks + a.o.blocks;
     if (pieces > 0x7fffffffll) {
         set_error("the call needs more than 2^31 blocks");
@@ -897,37 +795,28 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
     if (pieces > 0) {
         AttendArgs r = a;
         if (parts == 1) r.out = out;
-        if (copies) {
-            RtMaps m = {};
-            for (int i = 0; i < 2; ++i) {
-                const KvSide& s = i ? c.own : c.prefix;
-                if (s.rows == 0 || (i == 0 && tiles)) continue;
-                if (!kv_make_map(md[i], s.k, c.D, RtSmem<DP>::KEYS, &m.k[i]) || !kv_make_map(md[i], s.v, c.D, RtSmem<DP>::KEYS, &m.v[i])) {
-                    set_error("cuTensorMapEncodeTiled refused the %s", i ? "own rows" : "prefix");
-                    return JPI_ERR_CUDA;
-                }
-                m.at[i] = make_int3(md[i].at_head, md[i].at_row, md[i].at_cache);
-            }
-            const long long most = (tiles ? 2ll : 6ll) * h->num_sms;
-            JPI_TRY(kv_start(k_kv_attend_rows<DP>, std::min(pieces, most), RT_THREADS, RtSmem<DP>::BYTES, false, st, m, r));
-        } else if (h->bf16) {
-            JPI_TRY(kv_start(k_kv_attend_mma<DP>, pieces, AT_THREADS, MergeSmem<DP>::BYTES, false, st, r));
+        if (h->bf16) {
+            const long long most = (long long)(tiles ? RtSmem<DP>::BESIDE : RtSmem<DP>::ALONE) * h->num_sms;
+            JPI_TRY(kv_start(k_kv_attend_rows<DP>, std::min(pieces, most), 32, RtSmem<DP>::BYTES, false, st, r));
         } else {
             JPI_TRY(kv_start(k_kv_attend_f32<DP>, pieces, AT_THREADS, MergeSmem<DP>::BYTES, false, st, r));
         }
     }
-    if (tiles) JPI_TRY(launch_kv_prefix_t5(h, c, splits, a.po, a.pml, pieces > 0, st));
+    if (tiles) JPI_TRY(launch_kv_prefix_t5(h, c, splits, a.po, a.pml, parts, pieces > 0, st));
     if (parts == 1 && pieces > 0) return JPI_OK;
     a.out = out;
-    const int wpr = parts > 16 ? 4 : parts > 4 ? 2 : 1;
-    const long long grid = (a.rows * wpr + AT_WARPS - 1) / AT_WARPS;
-    return h->bf16 ? kv_start(k_kv_combine<DP, __nv_bfloat16>, grid, AT_THREADS, 0, true, st, a, wpr)
-                   : kv_start(k_kv_combine<DP, float>, grid, AT_THREADS, 0, true, st, a, wpr);
+    // A warp has the loads of 8 parts (16 to D = 128) in flight: warps for as many batches, to four a row, or where the
+    // rows are few to sixteen.
+    int wpr = 1;
+    while (wpr < (a.rows <= 64 ? CB_WARPS : 4) && wpr * 8 < parts) wpr *= 2;
+    const int warps = std::max(wpr, AT_WARPS);
+    const long long grid = (a.rows * wpr + warps - 1) / warps;
+    return h->bf16 ? kv_start(k_kv_combine<DP, __nv_bfloat16>, grid, 32 * warps, 0, true, st, a, wpr)
+                   : kv_start(k_kv_combine<DP, float>, grid, 32 * warps, 0, true, st, a, wpr);
 }
 
 template <int DP>
 jpi_status prepare_dim() {
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_mma<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
     JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
     JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_attend_rows<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, RtSmem<DP>::BYTES));
     // All of its loads go to shared memory, and the 128-row tiles need the SM set up for the most of it.

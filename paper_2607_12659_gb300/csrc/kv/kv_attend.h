@@ -8,10 +8,10 @@ namespace jpi {
 jpi_status kv_prefix_prepare(jpi_kv_handle* h);
 // Whether the call's prefix side takes that kernel, and then its key splits (at most `room`).
 bool kv_prefix_splits(const jpi_kv_handle* h, const KvCall& c, long long room, int* splits);
-// Parts 0 .. splits - 1 of `po` [parts][rows][D] and `pml` [parts][rows] (m unscaled, l). With `early` it starts while
+// Parts 0 .. splits - 1 of the call's: `po` [parts][rows][D] and `pml` [rows][parts] (m unscaled, l). With `early` it starts while
 // the kernel before it runs, and ends after that.
-jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, float* po, float2* pml, bool early,
-                               cudaStream_t st);
+jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, float* po, float2* pml, int parts,
+                               bool early, cudaStream_t st);
 
 // An ordinary launch, or with `early` one that starts while the kernel before it runs.
 template <typename... Params, typename... Args>

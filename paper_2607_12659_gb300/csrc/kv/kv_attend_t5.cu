@@ -50,14 +50,15 @@ struct PrefixArgs {
     int splits, tiles;   // key ranges, row tiles per run and KV head
     int3 at;             // of the maps' outer dimensions: heads, rows, runs
     float* po;           // [parts][rows][D]
-    float2* pml;         // [parts][rows]
+    float2* pml;         // [rows][parts]
     long long rows;
+    int parts;
     int* err;
 };
 
 template <int DP>
 struct KpSmem {
-    static constexpr int NS = DP == 256 ? 2 : 4;
+    static constexpr int NS = DP == 256 ? 2 : DP == 128 ? 3 : 4;
     static constexpr int KVBYTES = KP_KEYS * DP * 2;
     static constexpr int STAGE = 2 * KVBYTES;               // ring slot: K, then V
     static constexpr int OUT_LD = DP * 4 + 16;              // bytes of a staged output row: the pad spreads the banks
@@ -464,8 +465,8 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
             ptx::named_bar_sync(pair_bar, 64);
             ptx::grid_dep_wait();   // the row kernel that started before this one: what waits for this kernel has both
             if (half == 0 && valid) {
-                const long long row_out = split * a.rows + row_index(t, a.c.gq, a.c.H, r);
-                a.pml[row_out] = make_float2(m_used, l);
+                const long long row_at = row_index(a.c, t, r), row_out = split * a.rows + row_at;
+                a.pml[row_at * a.parts + split] = make_float2(m_used, l);
                 if (good && nb > 0) {
                     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.po + row_out * a.c.D),
                                  "r"(ptx::smem_u32(orow)), "r"(a.c.D * 4)
@@ -518,8 +519,8 @@ bool kv_prefix_splits(const jpi_kv_handle* h, const KvCall& c, long long room, i
     return blocks * *splits <= 0x7fffffffll;
 }
 
-jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, float* po, float2* pml, bool early,
-                               cudaStream_t st) {
+jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, float* po, float2* pml, int parts,
+                               bool early, cudaStream_t st) {
     PrefixArgs a;
     a.c = c;
     a.c2 = KR_LOG2E * c.scale;
@@ -528,6 +529,7 @@ jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, fl
     a.tiles = (int)((R + KP_ROWS - 1) / KP_ROWS);
     a.po = po;
     a.pml = pml;
+    a.parts = parts;
     a.rows = (long long)c.batch * c.tokens * c.H;
     a.err = h->dev_err;
     KvMapDims m;

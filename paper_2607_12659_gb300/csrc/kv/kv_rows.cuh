@@ -6,10 +6,7 @@
 // query token r / gq of the run (or request), head kvh * gq + r % gq. A warp takes 8 of them.
 //
 // Keys are the 16 rows of an mma.sync m16n8k16 and query rows its 8 columns, so that 8 query rows (one token of
-// eight heads) waste nothing. Both operands come from global memory without shared memory: the sum over d may run
-// in any order, so lane (g, j) takes 16-byte chunk 4 i + j of its key (and of its query row) as the four element
-// pairs of two k-steps. For the values the sum runs over keys and d is the free dimension: lane (g, j) takes chunk
-// g + 8 i of keys 2 j, 2 j + 1, 2 j + 8, 2 j + 9, and element pairs of neighbouring keys are joined with a byte permute.
+// eight heads) waste nothing.
 
 #pragma once
 
@@ -29,15 +26,23 @@ struct RowTile {
     int r0, R;        // first row of the tile, rows in all
 };
 
-__device__ __forceinline__ long long row_token(const RowTile& t, int gq, int r) { return t.tok0 + r / gq; }
-__device__ __forceinline__ long long row_index(const RowTile& t, int gq, int H, int r) {
-    return row_token(t, gq, r) * H + t.head0 + r % gq;
+__device__ __forceinline__ long long row_token(const KvCall& c, const RowTile& t, int r) { return t.tok0 + c.by_gq.div((uint32_t)r); }
+// Its index in [batch][tokens][H], and its first element in q.
+__device__ __forceinline__ long long row_index(const KvCall& c, const RowTile& t, int r) {
+    uint32_t h;
+    const uint32_t tok = c.by_gq.div((uint32_t)r, h);
+    return (t.tok0 + tok) * c.H + t.head0 + h;
+}
+__device__ __forceinline__ long long row_query(const KvCall& c, const RowTile& t, int r) {
+    uint32_t h;
+    const uint32_t tok = c.by_gq.div((uint32_t)r, h);
+    return (t.tok0 + tok) * c.q_stride + (long long)(t.head0 + h) * c.D;
 }
 // Keys that row r sees on its side.
 __device__ __forceinline__ int row_seen(const KvCall& c, bool prefix, int cache, const RowTile& t, int r) {
     if (r >= t.R) return 0;
     const KvSide& s = prefix ? c.prefix : c.own;
-    const int n = prefix ? s.len[cache] : s.len[row_token(t, c.gq, r)];
+    const int n = prefix ? s.len[cache] : s.len[row_token(c, t, r)];
     return min(max(n, 0), s.rows);
 }
 
@@ -69,20 +74,6 @@ __device__ __forceinline__ uint32_t kr_pack(float lo, float hi) {
 }
 __device__ __forceinline__ uint4 kr_ld(const void* p, bool ok) {
     return ok ? __ldg(static_cast<const uint4*>(p)) : make_uint4(0, 0, 0, 0);
-}
-
-// Query fragments of a tile of 8 rows: entry 32 i + lane is chunk 4 i + j of row g, zero past the rows and
-// past D. `qs` holds DP / 32 * 32 entries.
-template <int DP>
-__device__ __forceinline__ void load_q_frags(const KvCall& c, const RowTile& t, uint4* qs, int lane) {
-    const int r = t.r0 + (lane >> 2);
-    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(c.q);
-    const __nv_bfloat16* p = q + (r < t.R ? row_token(t, c.gq, r) * c.q_stride + (long long)(t.head0 + r % c.gq) * c.D : 0);
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
-        const int ch = 4 * i + (lane & 3);
-        qs[32 * i + lane] = kr_ld(p + 8 * ch, r < t.R && 8 * ch < c.D);
-    }
 }
 
 }  // namespace

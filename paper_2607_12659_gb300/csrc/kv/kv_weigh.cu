@@ -6,7 +6,8 @@
 // global memory.
 //
 // bf16: a warp keeps 16 keys in registers as the rows of mma.sync and streams the query rows past them, 8 at
-// a time; a lane adds up the weights of its two keys, and the four lanes of a key and the warps that share it
+// a time (the sum over d may run in any order, so lane (g, j) takes 16-byte chunk 4 i + j of its key and of its query
+// row as the four element pairs of two k-steps: both come from global memory as they lie); a lane adds up the weights of its two keys, and the four lanes of a key and the warps that share it
 // are joined at the end. fp32 on CUDA cores: a key per lane.
 
 #include "kv_rows.cuh"
@@ -97,7 +98,7 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_mma(const __grid_consta
         for (int rt = wrow * KR_ROWS; rt < x.t.R; rt += x.wr * KR_ROWS) {
             const int rq = rt + g;
             const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + 8 * j;
-            if (rq < x.t.R) q += row_token(x.t, a.c.gq, rq) * a.c.q_stride + (long long)(x.t.head0 + rq % a.c.gq) * a.c.D;
+            if (rq < x.t.R) q += row_query(a.c, x.t, rq);
             float sc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
@@ -109,7 +110,7 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_mma(const __grid_consta
             for (int e = 0; e < 2; ++e) {
                 const int r = rt + 2 * j + e;
                 if (r >= x.t.R) continue;
-                const float ls = a.lse[row_index(x.t, a.c.gq, a.c.H, r)];
+                const float ls = a.lse[row_index(a.c, x.t, r)];
                 const int n = row_seen(a.c, x.prefix, x.cache, x.t, r);
                 if (ls == -INFINITY) continue;
                 if (key0 + g < n) acc0 += kr_ex2(fmaf(sc[e], a.c.scale, -ls) * KR_LOG2E);
@@ -151,7 +152,7 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_f32(const __grid_consta
         for (int r = 0; r < KR_ROWS; ++r) {
             const int rr = min(rt + r, x.t.R - 1);
             p[r] = 0.f;
-            q[r] = static_cast<const float*>(a.c.q) + row_token(x.t, a.c.gq, rr) * a.c.q_stride + (long long)(x.t.head0 + rr % a.c.gq) * a.c.D;
+            q[r] = static_cast<const float*>(a.c.q) + row_query(a.c, x.t, rr);
         }
         if (key < live)
             for (int d = 0; d < a.c.D; d += 4) {
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_f32(const __grid_consta
 #pragma unroll
         for (int r = 0; r < KR_ROWS; ++r) {
             if (rt + r >= x.t.R) break;
-            const float ls = a.lse[row_index(x.t, a.c.gq, a.c.H, rt + r)];
+            const float ls = a.lse[row_index(a.c, x.t, rt + r)];
             const int n = row_seen(a.c, x.prefix, x.cache, x.t, rt + r);
             if (key < n && ls != -INFINITY) acc += expf(fmaf(p[r], a.c.scale, -ls));
         }
