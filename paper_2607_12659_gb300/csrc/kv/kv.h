@@ -74,4 +74,22 @@ jpi_status launch_kv_evict(const jpi_kv_handle* h, const jpi_kv_cache& src, cons
                            int caches, int keep, int sink, int recent, const jpi_kv_cache& dst, float* w_out,
                            int* length_out, int* kept, cudaStream_t st);
 
+// An ordinary launch, or with `early` one that starts while the kernel before it runs.
+template <typename... Params, typename... Args>
+jpi_status kv_start(void (*kernel)(Params...), long long grid, int threads, size_t smem, bool early, cudaStream_t st,
+                    const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = early ? 1 : 0;
+    JPI_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    return JPI_OK;
+}
+
 }  // namespace jpi

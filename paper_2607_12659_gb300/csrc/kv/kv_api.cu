@@ -2,6 +2,7 @@
 // its rotary table. The kernels are in kv_append.cu, kv_attend.cu, kv_weigh.cu and kv_evict.cu.
 
 #include "kv.h"
+#include "kv_weigh.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -213,6 +214,7 @@ JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* ro
         }
         h->ws_bytes = kv_attend_ws_bytes(h);
         JPI_TRY(kv_alloc(h, &h->ws, h->ws_bytes));
+        JPI_TRY(kv_weigh_prepare(h));
         return kv_attend_prepare(h);
     };
     const jpi_status s = setup();

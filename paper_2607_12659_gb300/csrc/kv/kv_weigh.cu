@@ -11,6 +11,7 @@
 // are joined at the end. fp32 on CUDA cores: a key per lane.
 
 #include "kv_rows.cuh"
+#include "kv_weigh.h"
 
 #include <algorithm>
 
@@ -81,6 +82,7 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_mma(const __grid_consta
     __shared__ int top;
     constexpr int NC = DP / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+    ptx::grid_dep_launch();
     const KeyPiece x = key_piece(a);
     const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
     const int live = live_keys(a, x, &top);
@@ -139,6 +141,7 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_f32(const __grid_consta
     __shared__ float part[WG_WARPS][32];
     __shared__ int top;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    ptx::grid_dep_launch();
     const KeyPiece x = key_piece(a);
     const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
     const int live = live_keys(a, x, &top);
@@ -207,17 +210,19 @@ jpi_status launch_kv_weigh(jpi_kv_handle* h, const KvCall& c, const float* lse, 
     const int keys = h->bf16 ? 16 : 32;
     a.wr_p = row_warps(h, c, true, keys, &a.tiles_p);
     a.wr_o = row_warps(h, c, false, keys, &a.tiles_o);
-    a.blocks_p = (long long)c.groups * c.K * a.tiles_p;
+    // Many rows on one prefix go to the tensor-core tiles.
+    const bool tiles = kv_weigh_tiles(h, c);
+    a.blocks_p = tiles ? 0 : (long long)c.groups * c.K * a.tiles_p;
     const long long blocks = a.blocks_p + (long long)c.batch * c.K * a.tiles_o;
     if (blocks > 0x7fffffffll) {
         set_error("the call needs more than 2^31 blocks");
         return JPI_ERR_SHAPE;
     }
-    if (!h->bf16) k_kv_weigh_f32<<<(unsigned)blocks, WG_THREADS, 0, st>>>(a);
-    else if (h->D <= 64) k_kv_weigh_mma<64><<<(unsigned)blocks, WG_THREADS, 0, st>>>(a);
-    else if (h->D <= 128) k_kv_weigh_mma<128><<<(unsigned)blocks, WG_THREADS, 0, st>>>(a);
-    else k_kv_weigh_mma<256><<<(unsigned)blocks, WG_THREADS, 0, st>>>(a);
-    JPI_CUDA_TRY(cudaGetLastError());
+    if (blocks > 0)
+        JPI_TRY(kv_start(!h->bf16 ? k_kv_weigh_f32
+                                  : h->D <= 64 ? k_kv_weigh_mma<64> : h->D <= 128 ? k_kv_weigh_mma<128> : k_kv_weigh_mma<256>,
+                         blocks, WG_THREADS, 0, false, st, a));
+    if (tiles) return launch_kv_weigh_t5(h, c, lse, decay, prefix_in, prefix_out, blocks > 0, st);
     return JPI_OK;
 }
 

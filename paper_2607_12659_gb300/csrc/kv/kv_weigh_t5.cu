@@ -1,0 +1,261 @@
+// The prefix side of jpi_kv_weigh on tcgen05: 128 keys a block, all query rows of the run past them in tiles of
+// 128. Keys are the rows of the products (TMEM lanes) and query rows their columns, so that a key's weights
+// are one lane's: no maximum, no exchange between lanes until the end, nothing to mask (a row past the prefix's end is
+// a lane that is not written), and a sum's order is fixed.
+//   warp 0      one thread: the key tile by bulk tensor copies, once
+//   warp 1      one thread: S = K Q^T (M = 128, N = 128, K = D) into one of two TMEM buffers
+//   warps 2-9   query rows gathered into one of two shared-memory tiles (128-byte swizzle) by asynchronous copies,
+//               with their -lse: four warps fill each tile, so that one's copies fly while the other's are issued
+//   warps 10-17 two threads per key (its TMEM lane), half of a tile's columns each: the sum of exp(scale s - lse)
+// Bound by 2^x and the products alike (128 x R of the one, 4096 cycles of the other at R = 512, D = 256); the keys come
+// from memory once and the query rows from L2 once per 128 keys. Every wait is bounded.
+
+#include "kv_rows.cuh"
+#include "kv_maps.h"
+#include "kv_weigh.h"
+
+namespace jpi {
+namespace {
+
+constexpr int WT_KEYS = 128, WT_ROWS = 128;
+constexpr int WT_LOAD = 128, WT_SUM = 256;          // threads that load a tile, and of the sums
+constexpr int WT_THREADS = 64 + 2 * WT_LOAD + WT_SUM;
+constexpr uint64_t WT_WAIT_NS = 200ull * 1000 * 1000;
+
+struct WeighT5Args {
+    KvCall c;
+    const float* lse;
+    float decay;
+    const float* in;
+    float* out;
+    int tiles;           // key tiles per run and KV head
+    int3 at;             // of the map's outer dimensions: heads, rows, runs
+    int* err;
+    KvDiv by_tiles;
+};
+
+template <int DP>
+struct WtSmem {
+    static constexpr int KBYTES = WT_KEYS * DP * 2, QBYTES = WT_ROWS * DP * 2;
+    static constexpr int Q_OFF = KBYTES;                      // two tiles
+    static constexpr int LSE_OFF = Q_OFF + 2 * QBYTES;        // [2][128] -lse
+    static constexpr int SUM_OFF = LSE_OFF + 2 * WT_ROWS * 4; // [128] the second halves' sums
+    static constexpr int BAR_OFF = SUM_OFF + WT_KEYS * 4;
+    static constexpr int BYTES = BAR_OFF + 9 * 8 + 8;
+    static_assert(BYTES <= 227 * 1024, "fits an SM");
+    static constexpr uint32_t TMEM_COLS = 256;
+};
+
+template <int DP>
+__global__ void __launch_bounds__(WT_THREADS, 1) k_kv_weigh_t5(const __grid_constant__ CUtensorMap kmap,
+                                                               const __grid_constant__ WeighT5Args a) {
+    using L = WtSmem<DP>;
+    constexpr int NDB = DP / 64;
+    constexpr uint32_t IDESC = ptx::idesc_bf16_f32(WT_KEYS, WT_ROWS);
+    extern __shared__ __align__(1024) uint8_t wt_smem[];
+    float* nlse = (float*)(wt_smem + L::LSE_OFF);
+    float* sums = (float*)(wt_smem + L::SUM_OFF);
+    uint64_t* kfull = (uint64_t*)(wt_smem + L::BAR_OFF);
+    uint64_t* qfull = kfull + 1;     // 2: query tile in shared memory
+    uint64_t* qempty = kfull + 3;    // 2: its products are done
+    uint64_t* sfull = kfull + 5;     // 2: scores ready
+    uint64_t* sfree = kfull + 7;     // 2: scores read
+    uint32_t* tmem_slot = (uint32_t*)(kfull + 9);
+    int* flag = (int*)(tmem_slot + 1);
+    const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
+    uint32_t tile, kvh;
+    const int run = (int)a.c.by_K.div(a.by_tiles.div(blockIdx.x, tile), kvh);
+    const int len = min(max(a.c.prefix.len[run], 0), a.c.prefix.rows), key0 = (int)tile * WT_KEYS;
+    if (key0 >= len) {
+        ptx::grid_dep_wait();   // (ends after the kernel that started before it)
+        return;
+    }
+    RowTile t;
+    const int toks = a.c.batch / a.c.groups * a.c.tokens;
+    t.tok0 = (long long)run * toks;
+    t.head0 = (int)kvh * a.c.gq;
+    t.R = toks * a.c.gq;
+    t.r0 = 0;
+    const int nt = (t.R + WT_ROWS - 1) / WT_ROWS;
+
+    if (warp == 0 && ptx::elect_one()) {
+        ptx::prefetch_tmap(&kmap);
+        ptx::mbar_init(kfull, 1);
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(&qfull[b], WT_LOAD);
+            ptx::mbar_init(&qempty[b], 1);
+            ptx::mbar_init(&sfull[b], 1);
+            ptx::mbar_init(&sfree[b], WT_SUM);
+        }
+        ptx::fence_mbar_init();
+        *flag = 0;
+        ptx::mbar_expect_tx(kfull, (uint32_t)L::KBYTES);
+        for (int db = 0; db < NDB; ++db)
+            kv_load_box(wt_smem + db * (WT_KEYS * 128), &kmap, kfull, db * 64, a.at, (int)kvh, key0, run);
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(tmem_slot, L::TMEM_COLS);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        // (the key tile is waited for below, also where a wait gave up: nothing may land after the block)
+        if (lane == 0 && !ptx::mbar_wait_bounded(kfull, 0, WT_WAIT_NS)) *flag = DEV_TIMEOUT_WEIGHTS;
+    } else if (warp == 1) {
+        if (ptx::elect_one()) {
+            const uint32_t kb = ptx::smem_u32(wt_smem), qb = kb + L::Q_OFF;
+            bool good = ptx::mbar_wait_bounded(kfull, 0, WT_WAIT_NS);
+            for (int i = 0; i < nt; ++i) {
+                const int b = i & 1;
+                if (good) good = ptx::mbar_wait_bounded(&qfull[b], (i >> 1) & 1, WT_WAIT_NS);
+                if (i >= 2 && good) good = ptx::mbar_wait_bounded(&sfree[b], ((i >> 1) - 1) & 1, WT_WAIT_NS);
+                ptx::tc_fence_after();
+                if (good) {
+                    const uint64_t kd = ptx::desc_sw128(kb), qd = ptx::desc_sw128(qb + (uint32_t)(b * L::QBYTES));
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            ptx::mma_bf16(tmem + (uint32_t)(WT_ROWS * b), ptx::desc_add(kd, db * (WT_KEYS * 128) + kk * 32),
+                                          ptx::desc_add(qd, db * (WT_ROWS * 128) + kk * 32), IDESC, (db | kk) != 0);
+                }
+                if (i + 2 < nt) ptx::mma_commit(&qempty[b]);
+                ptx::mma_commit(&sfull[b]);
+            }
+            if (!good) *flag = DEV_TIMEOUT_MMA;
+        }
+    } else if (warp < 10) {
+        const int b = (warp - 2) >> 2, lt = (tid - 64) % WT_LOAD;   // fills tile buffer b: tiles b, b + 2, ..
+        bool good = true;
+        constexpr int CH = DP / 8, RPI = WT_LOAD / CH;   // chunks of a row, rows of one pass of the loaders
+        const int ch = lt % CH, rr0 = lt / CH;
+        const bool dlive = 8 * ch < a.c.D;
+        uint32_t hd_step;
+        const uint32_t tok_step = a.c.by_gq.div((uint32_t)RPI, hd_step), gq = (uint32_t)a.c.gq;
+        const __nv_bfloat16* base = static_cast<const __nv_bfloat16*>(a.c.q) + t.tok0 * a.c.q_stride +
+                                    (long long)t.head0 * a.c.D + (dlive ? 8 * ch : 0);
+        const uint32_t dst = ptx::smem_u32(wt_smem) + L::Q_OFF + b * L::QBYTES + (ch >> 3) * (WT_ROWS * 128);
+        for (int i = b; i < nt; i += 2) {
+            const int rl = i * WT_ROWS + lt;
+            const float ls = rl < t.R ? a.lse[row_index(a.c, t, rl)] : -INFINITY;
+            // Rows i WT_ROWS + rr0, + RPI, ..: token and head, stepped without a division. Past the run's rows nothing is read.
+            int r = i * WT_ROWS + rr0;
+            uint32_t hd, tok = a.c.by_gq.div((uint32_t)r, hd);
+            if (i >= 2 && good) good = ptx::mbar_wait_bounded(&qempty[b], ((i >> 1) - 1) & 1, WT_WAIT_NS);
+#pragma unroll 8
+            for (int rr = rr0; rr < WT_ROWS; rr += RPI) {
+                const bool in = dlive && r < t.R;
+                ptx::cp_async_16(dst + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4),
+                                 in ? base + (long long)tok * a.c.q_stride + hd * (uint32_t)a.c.D : base, in);
+                r += RPI;
+                tok += tok_step;
+                hd += hd_step;
+                if (hd >= gq) {
+                    hd -= gq;
+                    ++tok;
+                }
+            }
+            if (i >= 2 && good) good = ptx::mbar_wait_bounded(&sfree[b], ((i >> 1) - 1) & 1, WT_WAIT_NS);   // the sums have read it
+            nlse[b * WT_ROWS + lt] = ls == -INFINITY ? -INFINITY : -ls;   // a row that saw nothing gives nothing
+            ptx::cp_async_wait_all();
+            ptx::fence_proxy_async_smem();
+            ptx::mbar_arrive(&qfull[b]);
+        }
+        if (!good) *flag = DEV_TIMEOUT_MMA;
+    } else {
+        const int key = (warp & 3) * 32 + lane, half = (warp - 10) >> 2;
+        const uint32_t col0 = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * (WT_ROWS / 2));
+        bool good = true;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < nt; ++i) {
+            const int b = i & 1;
+            if (good) good = ptx::mbar_wait_bounded(&sfull[b], (i >> 1) & 1, WT_WAIT_NS);
+            ptx::tc_fence_after();
+            uint32_t s[4][16];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) ptx::tmem_ld_x16(col0 + (uint32_t)(WT_ROWS * b + 16 * k), s[k]);
+            ptx::tmem_ld_wait();
+            const float4* nl = (const float4*)(nlse + b * WT_ROWS + half * (WT_ROWS / 2));
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const float4 n = nl[k];
+                const uint32_t* x = s[k >> 2] + 4 * (k & 3);
+                acc[0] += kr_ex2(fmaf(__uint_as_float(x[0]), a.c.scale, n.x) * KR_LOG2E);
+                acc[1] += kr_ex2(fmaf(__uint_as_float(x[1]), a.c.scale, n.y) * KR_LOG2E);
+                acc[2] += kr_ex2(fmaf(__uint_as_float(x[2]), a.c.scale, n.z) * KR_LOG2E);
+                acc[3] += kr_ex2(fmaf(__uint_as_float(x[3]), a.c.scale, n.w) * KR_LOG2E);
+            }
+            ptx::tc_fence_before();
+            // Scores and -lse of this buffer are read: the next tile but one may take both.
+            if (i + 2 < nt) ptx::mbar_arrive(&sfree[b]);
+        }
+        if (!good) *flag = DEV_TIMEOUT_MMA;
+        const float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+        if (half == 1) sums[key] = sum;
+        ptx::named_bar_sync(1, WT_SUM);
+        ptx::grid_dep_wait();   // the row kernel that started before this one: what follows this kernel has both
+        if (half == 0 && key0 + key < len && good) {
+            const long long at = ((long long)run * a.c.K + kvh) * a.c.prefix.rows + key0 + key;
+            const float w = sum + sums[key];
+            a.out[at] = a.in && a.decay != 0.f ? fmaf(a.decay, a.in[at], w) : w;
+        }
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    if (tid == 0 && *flag != 0) atomicCAS(a.err, 0, *flag);
+    if (warp == 1) ptx::tmem_dealloc(tmem, L::TMEM_COLS);
+}
+
+template <int DP>
+jpi_status launch_dim(const WeighT5Args& a, const CUtensorMap& map, bool early, cudaStream_t st) {
+    return kv_start(k_kv_weigh_t5<DP>, (long long)a.tiles * a.c.K * a.c.groups, WT_THREADS, WtSmem<DP>::BYTES, early, st, map, a);
+}
+
+}  // namespace
+
+jpi_status kv_weigh_prepare(jpi_kv_handle* h) {
+    if (!h->bf16 || h->D < 64) return JPI_OK;
+    if (h->D <= 64)
+        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_weigh_t5<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, WtSmem<64>::BYTES));
+    else if (h->D <= 128)
+        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_weigh_t5<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, WtSmem<128>::BYTES));
+    else
+        JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_weigh_t5<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, WtSmem<256>::BYTES));
+    return JPI_OK;
+}
+
+bool kv_weigh_tiles(const jpi_kv_handle* h, const KvCall& c) {
+    if (!h->bf16 || c.D < 64 || c.prefix.rows == 0) return false;
+    KvMapDims m;
+    const long long R = (long long)(c.batch / c.groups) * c.tokens * c.gq;
+    return R >= 64 && kv_map_dims(c.prefix, c.K, c.D, c.groups, &m) &&
+           (long long)((c.prefix.rows + WT_KEYS - 1) / WT_KEYS) * c.K * c.groups <= 0x7fffffffll;
+}
+
+jpi_status launch_kv_weigh_t5(jpi_kv_handle* h, const KvCall& c, const float* lse, float decay, const float* in, float* out,
+                              bool early, cudaStream_t st) {
+    WeighT5Args a = {};
+    a.c = c;
+    a.lse = lse;
+    a.decay = decay;
+    a.in = in;
+    a.out = out;
+    a.tiles = (c.prefix.rows + WT_KEYS - 1) / WT_KEYS;
+    a.by_tiles = KvDiv((uint32_t)a.tiles);
+    a.err = h->dev_err;
+    KvMapDims m;
+    CUtensorMap map;
+    if (!kv_map_dims(c.prefix, c.K, c.D, c.groups, &m) || !kv_make_map(m, c.prefix.k, c.D, WT_KEYS, &map)) {
+        set_error("cuTensorMapEncodeTiled refused the prefix");
+        return JPI_ERR_CUDA;
+    }
+    a.at = make_int3(m.at_head, m.at_row, m.at_cache);
+    return c.D <= 64 ? launch_dim<64>(a, map, early, st) : c.D <= 128 ? launch_dim<128>(a, map, early, st) : launch_dim<256>(a, map, early, st);
+}
+
+}  // namespace jpi
