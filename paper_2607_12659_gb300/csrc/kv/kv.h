@@ -76,10 +76,10 @@ jpi_status launch_kv_evict(const jpi_kv_handle* h, const jpi_kv_cache& src, cons
 
 // An ordinary launch, or with `early` one that starts while the kernel before it runs.
 template <typename... Params, typename... Args>
-jpi_status kv_start(void (*kernel)(Params...), long long grid, int threads, size_t smem, bool early, cudaStream_t st,
+jpi_status kv_start(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, bool early, cudaStream_t st,
                     const Args&... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

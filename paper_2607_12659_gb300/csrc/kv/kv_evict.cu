@@ -4,16 +4,20 @@
 // The choice (k_kv_select), one block per layer, cache and KV head. The weights, as unsigned keys of
 // the same order (NaN 0, below everything), are searched for the need-th largest by three passes over
 // 11, 11 and 10 bits, a histogram in shared memory each: exact, whatever the distribution. Above the
-// threshold every row stays; of the rows equal to it the lowest, as many as are left. Each thread then
-// counts its run of consecutive rows, one block-wide scan gives every run its place, and the kept rows
+// threshold every row stays; of the rows equal to it the lowest, as many as are left. Each thread has a
+// run of consecutive rows (in registers up to 16), one block-wide scan gives every run its place, and the kept rows
 // come out ascending.
 //
-// The move (k_kv_gather): a block takes 64 bytes of every kept row of one cache, head and matrix, in
-// tiles of ascending rows: a tile is loaded whole, then stored. In place this needs no second buffer:
-// a row never moves up (row i goes to at most i) and what a tile overwrites lies in it or before it,
-// so it has been read. Bound by memory: every kept row is read and written once.
+// The move (k_kv_gather): a block takes a slice (16 to 512 bytes, whole rows where there are blocks enough) of every
+// kept row of one cache, head and matrix, in tiles of ascending rows: a tile is loaded whole, then stored. In place this
+// needs no second buffer: a row never moves up (row i goes to at most i) and what a tile overwrites lies in it or
+// before it, so it has been read. Apart, the tiles are independent and dealt to further blocks. Bound by memory: every
+// kept row is read and written once.
 
 #include "kv.h"
+#include "../ptx.h"
+
+#include <algorithm>
 
 namespace jpi {
 namespace {
@@ -61,6 +65,8 @@ __device__ __forceinline__ uint2 block_scan(uint2 v, uint2* warp_sums, uint2* to
     return make_uint2(before.x + s.x - v.x, before.y + s.y - v.y);
 }
 
+// RUN: rows of a thread, its keys in registers; 0: any number, read again in every pass.
+template <int RUN>
 __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, const int* length, int rows, int caches,
                                                            int K, int keep, int sink, int recent, int dst_rows,
                                                            float* w_out_all, int* kept_all) {
@@ -68,6 +74,7 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
     __shared__ uint2 warp_sums[SEL_THREADS / 32];
     __shared__ uint32_t found[2];   // chosen bin, rows still needed within it
     const int t = threadIdx.x;
+    ptx::grid_dep_launch();
     const long long item = blockIdx.x;   // (layer, cache, head)
     const int c = (int)((item / K) % caches);
     const float* w = w_all + item * rows;
@@ -81,22 +88,57 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
         }
         return;
     }
+    const int run = RUN > 0 ? RUN : (n + SEL_THREADS - 1) / SEL_THREADS;
+    // The thread's rows r0 .. r1 - 1 (in registers from r0 = t RUN on, also past the end: aligned for loads of four).
+    const int r0 = RUN > 0 ? t * RUN : min(n, t * run), r1 = min(n, r0 + run);
+    uint32_t keys[RUN > 0 ? RUN : 1];
+    if constexpr (RUN % 4 == 0 && RUN > 0) {
+        const bool four = (reinterpret_cast<uintptr_t>(w) & 15) == 0;   // with r0 a multiple of 4
+#pragma unroll
+        for (int e = 0; e < RUN; e += 4) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (four && r0 + e + 4 <= n) {
+                v = *(const float4*)(w + r0 + e);
+            } else {
+                if (r0 + e < n) v.x = w[r0 + e];
+                if (r0 + e + 1 < n) v.y = w[r0 + e + 1];
+                if (r0 + e + 2 < n) v.z = w[r0 + e + 2];
+                if (r0 + e + 3 < n) v.w = w[r0 + e + 3];
+            }
+            keys[e] = sort_key(v.x);
+            keys[e + 1] = sort_key(v.y);
+            keys[e + 2] = sort_key(v.z);
+            keys[e + 3] = sort_key(v.w);
+        }
+    } else if constexpr (RUN == 1) {
+        keys[0] = r0 < n ? sort_key(w[r0]) : 0u;
+    }
+    // f(key) for the thread's share of rows lo .. hi - 1 (its run in registers, else strided: order does not matter).
+    auto each = [&](int lo, int hi, auto f) {
+        if constexpr (RUN > 0) {
+#pragma unroll
+            for (int e = 0; e < RUN; ++e)
+                if (r0 + e >= lo && r0 + e < hi) f(keys[e]);
+        } else {
+            for (int i = lo + t; i < hi; i += SEL_THREADS) f(sort_key(w[i]));
+        }
+    };
     // The need-th largest key of rows lo .. hi - 1 (need < hi - lo).
     const int lo = sink, hi = n - recent;
     uint32_t need = (uint32_t)(keep - sink - recent);
     uint32_t prefix = 0, mask = 0;   // keys with (key & mask) == prefix are still candidates
     if (need > 0) {
         const int shifts[3] = {21, 10, 0};
+#pragma unroll
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = shifts[pass];
             const uint32_t bins = pass == 2 ? 1024u : 2048u;
             hist[t] = 0;
             hist[t + SEL_THREADS] = 0;
             __syncthreads();
-            for (int i = lo + t; i < hi; i += SEL_THREADS) {
-                const uint32_t k = sort_key(w[i]);
+            each(lo, hi, [&](uint32_t k) {
                 if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
-            }
+            });
             __syncthreads();
             // Bins from the top, two a thread.
             const uint32_t b1 = SEL_BINS - 1 - 2 * t, n1 = hist[b1], n0 = hist[b1 - 1];
@@ -118,32 +160,43 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
     }
     // Rows that stay: protected or above the threshold (x), and `need` of those equal to it (y).
     const bool some = keep > sink + recent;
-    const int run = (n + SEL_THREADS - 1) / SEL_THREADS, r0 = min(n, t * run), r1 = min(n, r0 + run);
-    auto kind = [&](int i) -> uint2 {
+    auto kind = [&](int i, uint32_t k) -> uint2 {
         if (i < lo || i >= hi) return make_uint2(1, 0);
-        const uint32_t k = sort_key(w[i]);
         return make_uint2(some && k > prefix, some && k == prefix);
     };
-    uint2 mine = make_uint2(0, 0);
-    for (int i = r0; i < r1; ++i) {
-        const uint2 x = kind(i);
+    uint2 mine = make_uint2(0, 0), tot;
+    auto count = [&](int i, uint32_t k) {
+        const uint2 x = kind(i, k);
         mine.x += x.x;
         mine.y += x.y;
+    };
+    if constexpr (RUN > 0) {
+#pragma unroll
+        for (int e = 0; e < RUN; ++e)
+            if (r0 + e < r1) count(r0 + e, keys[e]);
+    } else {
+        for (int i = r0; i < r1; ++i) count(i, sort_key(w[i]));
     }
-    uint2 tot;
     uint2 at = block_scan(mine, warp_sums, &tot);
-    for (int i = r0; i < r1; ++i) {
-        const uint2 x = kind(i);
+    auto place = [&](int i, uint32_t k) {
+        const uint2 x = kind(i, k);
         if (x.x || (x.y && at.y < need)) kept[at.x + min(at.y, need)] = i;
         at.x += x.x;
         at.y += x.y;
+    };
+    if constexpr (RUN > 0) {
+#pragma unroll
+        for (int e = 0; e < RUN; ++e)
+            if (r0 + e < r1) place(r0 + e, keys[e]);
+    } else {
+        for (int i = r0; i < r1; ++i) place(i, sort_key(w[i]));
     }
     __syncthreads();
     // The weights follow, in tiles: in place, a tile's stores come after its loads.
     for (int i0 = 0; i0 < keep; i0 += SEL_THREADS) {
         const int i = i0 + t;
         const float x = i < keep ? w[kept[i]] : 0.f;
-        __syncthreads();
+        if (w_out == w) __syncthreads();
         if (i < keep) w_out[i] = x;
     }
 }
@@ -162,35 +215,39 @@ struct GatherArgs {
 };
 
 constexpr int GA_THREADS = 256;
-constexpr int GA_LANES = 4;                           // 16-byte chunks of a slice
-constexpr int GA_ROWS = GA_THREADS / GA_LANES;        // rows of one load
 constexpr int GA_UNROLL = 8;
 
+// LANES: 16-byte chunks of a slice.
+template <int LANES>
 __global__ void __launch_bounds__(GA_THREADS) k_kv_gather(const __grid_constant__ GatherArgs a) {
+    constexpr int ROWS = GA_THREADS / LANES;   // rows of one load
     const int item = blockIdx.y;   // (layer, cache, head)
     const int h = item % a.K, c = (item / a.K) % a.caches, l = item / (a.K * a.caches);
-    const int slices = (a.chunks + GA_LANES - 1) / GA_LANES;
+    const int slices = (a.chunks + LANES - 1) / LANES;
     const bool is_v = (int)blockIdx.x >= slices;
-    const int ch = (blockIdx.x - (is_v ? slices : 0)) * GA_LANES + (threadIdx.x & (GA_LANES - 1));
-    const int r0 = threadIdx.x / GA_LANES;
+    const int ch = (blockIdx.x - (is_v ? slices : 0)) * LANES + (threadIdx.x & (LANES - 1));
+    const int r0 = threadIdx.x / LANES;
     const uint8_t* src = (is_v ? a.v : a.k) + l * a.ls + c * a.cs + h * a.hs + ch * 16;
     uint8_t* dst = (is_v ? a.ov : a.ok) + l * a.ols + c * a.ocs + h * a.ohs + ch * 16;
     const int* kept = a.kept + (long long)item * a.keep;
     const bool mine = ch < a.chunks;
-    for (int i0 = (int)blockIdx.z * GA_ROWS * GA_UNROLL; i0 < a.keep; i0 += (int)gridDim.z * GA_ROWS * GA_UNROLL) {
+    ptx::grid_dep_wait();   // the choice
+    for (int i0 = (int)blockIdx.z * ROWS * GA_UNROLL; i0 < a.keep; i0 += (int)gridDim.z * ROWS * GA_UNROLL) {
         uint4 x[GA_UNROLL];
-        bool move[GA_UNROLL];
+        int r[GA_UNROLL];
 #pragma unroll
         for (int u = 0; u < GA_UNROLL; ++u) {
-            const int i = i0 + u * GA_ROWS + r0;
-            const int r = i < a.keep && mine ? kept[i] : -1;
-            move[u] = r >= 0 && !(a.in_place && r == i);
-            if (move[u]) x[u] = *(const uint4*)(src + r * a.rs);
+            const int i = i0 + u * ROWS + r0;
+            r[u] = i < a.keep && mine ? kept[i] : -1;
+            if (a.in_place && r[u] == i) r[u] = -1;
         }
+#pragma unroll
+        for (int u = 0; u < GA_UNROLL; ++u)
+            if (r[u] >= 0) x[u] = *(const uint4*)(src + r[u] * a.rs);
         if (a.in_place) __syncthreads();
 #pragma unroll
         for (int u = 0; u < GA_UNROLL; ++u)
-            if (move[u]) *(uint4*)(dst + (long long)(i0 + u * GA_ROWS + r0) * a.ors) = x[u];
+            if (r[u] >= 0) *(uint4*)(dst + (long long)(i0 + u * ROWS + r0) * a.ors) = x[u];
     }
     // The choice has read the lengths: one thread of each cache's first block replaces its length.
     if (blockIdx.x == 0 && blockIdx.z == 0 && l == 0 && h == 0 && threadIdx.x == 0)
@@ -203,8 +260,10 @@ jpi_status launch_kv_evict(const jpi_kv_handle* h, const jpi_kv_cache& src, cons
                            int caches, int keep, int sink, int recent, const jpi_kv_cache& dst, float* w_out,
                            int* length_out, int* kept, cudaStream_t st) {
     const int items = layers * caches * h->K;
-    k_kv_select<<<items, SEL_THREADS, 0, st>>>(w, length, src.rows, caches, h->K, keep, sink, recent, dst.rows, w_out, kept);
-    JPI_CUDA_TRY(cudaGetLastError());
+    JPI_TRY(kv_start(src.rows <= SEL_THREADS ? k_kv_select<1>
+                                             : src.rows <= 4 * SEL_THREADS ? k_kv_select<4>
+                                                                           : src.rows <= 16 * SEL_THREADS ? k_kv_select<16> : k_kv_select<0>,
+                     items, SEL_THREADS, 0, false, st, w, length, src.rows, caches, h->K, keep, sink, recent, dst.rows, w_out, kept));
     const long long e = h->bf16 ? 2 : 4;
     GatherArgs a = {};
     a.k = (const uint8_t*)src.k;
@@ -228,16 +287,23 @@ jpi_status launch_kv_evict(const jpi_kv_handle* h, const jpi_kv_cache& src, cons
     a.length_out = length_out;
     a.rows = src.rows;
     a.in_place = src.k == dst.k;
-    const int gx = 2 * ((a.chunks + GA_LANES - 1) / GA_LANES);
-    // Apart, the tiles of a slice are independent: more blocks where there are few slices.
+    // Whole rows (to 512 bytes) where that still leaves two blocks an SM, else narrower slices: in place a slice's rows are
+    // one block's.
+    int lanes = 32;
+    while (lanes > 1 && lanes / 2 >= a.chunks) lanes /= 2;
+    auto blocks_of = [&](int n) { return 2ll * ((a.chunks + n - 1) / n) * items; };
+    const int tile = GA_THREADS / lanes * GA_UNROLL;
     int gz = 1;
-    if (!a.in_place) {
-        const int tiles = (keep + GA_ROWS * GA_UNROLL - 1) / (GA_ROWS * GA_UNROLL);
-        while (gz < tiles && gz < 64 && (long long)gx * items * gz < 8ll * h->num_sms) ++gz;
+    if (a.in_place) {
+        while (lanes > 2 && blocks_of(lanes) < 2ll * h->num_sms) lanes /= 2;
+    } else {
+        const int tiles = (keep + tile - 1) / tile;
+        gz = (int)std::max(1ll, std::min({(long long)tiles, 8ll * h->num_sms / blocks_of(lanes), 65535ll}));
     }
-    k_kv_gather<<<dim3(gx, items, gz), GA_THREADS, 0, st>>>(a);
-    JPI_CUDA_TRY(cudaGetLastError());
-    return JPI_OK;
+    return kv_start(lanes == 32 ? k_kv_gather<32>
+                                : lanes == 16 ? k_kv_gather<16>
+                                              : lanes == 8 ? k_kv_gather<8> : lanes == 4 ? k_kv_gather<4> : lanes == 2 ? k_kv_gather<2> : k_kv_gather<1>,
+                    dim3((unsigned)(blocks_of(lanes) / items), (unsigned)items, (unsigned)gz), GA_THREADS, 0, true, st, a);
 }
 
 }  // namespace jpi

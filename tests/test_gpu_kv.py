@@ -427,6 +427,14 @@ def test_evict_types_and_layouts(kv, dtype, D):
         check_evict(kv, w, [130, 128, 90], 70, 1, 5, K=4, D=D, dtype=dtype, in_place=in_place, store=head_major)
 
 
+@pytest.mark.parametrize("R", [900, 1024, 2048, 4096, 4100, 16384, 16388])
+def test_evict_caches_far_from_full(kv, R):
+    """Lengths that end anywhere in a cache, odd ones among them: threads of the choice past the end read nothing."""
+    w = np.random.default_rng(R).normal(size=(1, 4, 1, R)).astype(np.float32) ** 2
+    check_evict(kv, w, [R // 2 + 1, R // 3 + 2, 130, 101], 100, 2, 7, D=8)
+    check_evict(kv, w, [R - 1, R // 3, 133, 99], 100, 2, 7, D=8, in_place=True)
+
+
 def test_evict_long_cache(kv):
     w = np.random.default_rng(6).normal(size=(1, 1, 1, 70000)).astype(np.float32) ** 2
     check_evict(kv, w, [70000], 20001, 4, 500, in_place=True)
