@@ -64,6 +64,7 @@ struct KvCall {
 size_t kv_attend_ws_bytes(const jpi_kv_handle* h);
 jpi_status kv_attend_prepare(jpi_kv_handle* h);
 
+jpi_status kv_append_prepare();
 jpi_status launch_kv_append(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
                             const void* v, long long v_stride, const int* position, const int* row, int batch,
                             int tokens, void* q_out, const jpi_kv_cache* cache, cudaStream_t st);

@@ -214,6 +214,7 @@ JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* ro
         }
         h->ws_bytes = kv_attend_ws_bytes(h);
         JPI_TRY(kv_alloc(h, &h->ws, h->ws_bytes));
+        JPI_TRY(kv_append_prepare());
         JPI_TRY(kv_weigh_prepare(h));
         return kv_attend_prepare(h);
     };
