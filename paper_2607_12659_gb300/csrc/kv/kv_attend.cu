@@ -12,8 +12,8 @@
 // products, and the difference is scaled, not the product: log2(e) times a score near the type's largest
 // values would overflow.
 //
-// Kernels: the row kernels here take both sides, 8 query rows a warp; many rows on one prefix (from 32) go to
-// tiles of 128 rows instead (kv_attend_t5.cu), bound by tensor cores and 2^x where the row kernel is bound by
+// Kernels: the row kernels here take both sides, 8 query rows a warp; a side with many query rows on the same keys
+// (from 32) goes to tiles of 128 rows instead (kv_attend_t5.cu), bound by tensor cores and 2^x where the row kernel is bound by
 // memory, so the two share the SMs: the row kernel starts first with two blocks per SM, the tiles start while it
 // runs. k_kv_combine joins the parts, except where a row has only one.
 
@@ -501,21 +501,28 @@ __global__ void __maxnreg__(RtSmem<DP>::REGS) k_kv_attend_rows(const __grid_cons
                         kr_mma(o[i], f[0], f[1], f[2], f[3], pe[t][0], pe[t][1]);
                     }
             } else {
+                // (each row's product in registers of its own: of one with other rows' columns zero, 0 times the NaN would
+                // still be theirs)
 #pragma unroll 1
                 for (int r = 0; r < KR_ROWS; ++r) {
                     const int n = __shfl_sync(0xffffffffu, (r & 1) ? n1 : n0, r >> 1);
+                    const bool mine = g == r;
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) {
-                        const int key = key0 + 16 * t + 2 * j;
-                        const uint32_t lo = (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
-                        const uint32_t hi = (key + 8 < n ? 0xffffu : 0u) | (key + 9 < n ? 0xffff0000u : 0u);
+                    for (int i = 0; i < ND; ++i) {
+                        float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int i = 0; i < ND; ++i) {
+                        for (int t = 0; t < MT; ++t) {
+                            const int key = key0 + 16 * t + 2 * j;
+                            const uint32_t lo = (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
+                            const uint32_t hi = (key + 8 < n ? 0xffffu : 0u) | (key + 9 < n ? 0xffff0000u : 0u);
                             uint32_t f[4];
                             values(t, i, f);
-                            kr_mma(o[i], f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, g == r ? ph[t][0] : 0u, g == r ? ph[t][1] : 0u);
-                            kr_mma(o[i], f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, g == r ? pe[t][0] : 0u, g == r ? pe[t][1] : 0u);
+                            kr_mma(y, f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, mine ? ph[t][0] : 0u, mine ? ph[t][1] : 0u);
+                            kr_mma(y, f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, mine ? pe[t][0] : 0u, mine ? pe[t][1] : 0u);
                         }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (2 * j + (e & 1) == r) o[i][e] += y[e];
                     }
                 }
             }
@@ -770,22 +777,25 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
     a.po = static_cast<float*>(h->ws);
     a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
     a.lse = lse;
-    int splits = 0;
-    const bool tiles = kv_prefix_splits(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), &splits);
+    int tiles[2];   // key splits of the sides that take the 128-row tiles
+    kv_tiles_plan(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), tiles);
+    const bool beside = tiles[0] + tiles[1] > 0;
     if (h->bf16) {
         // Single warps with 64 KB of keys and values or more each.
         constexpr int KEYS = RtSmem<DP>::KEYS;
-        const long long want = (long long)(tiles ? RtSmem<DP>::BESIDE : RtSmem<DP>::ALONE) * h->num_sms;
+        const long long want = (long long)(beside ? RtSmem<DP>::BESIDE : RtSmem<DP>::ALONE) * h->num_sms;
         a.p = plan_side(h, c, true, 1, KEYS, 4 * KEYS, want);
         a.o = plan_side(h, c, false, 1, KEYS, 4 * KEYS, want);
     } else {
         a.p = plan_side(h, c, true, AT_WARPS, 32, 32, 2ll * h->num_sms);
         a.o = plan_side(h, c, false, AT_WARPS, 32, 32, 2ll * h->num_sms);
     }
-    if (tiles) {
-        a.p.blocks = 0;
-        a.p.splits = splits;
-    }
+    for (int i = 0; i < 2; ++i)
+        if (tiles[i] > 0) {
+            SidePlan& s = i ? a.o : a.p;
+            s.blocks = 0;
+            s.splits = tiles[i];
+        }
     const int parts = a.parts = a.p.splits + a.o.splits;
     const long long pieces = a.p.blocks + a.o.blocks;
     if (pieces > 0x7fffffffll) {
@@ -796,13 +806,14 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
         AttendArgs r = a;
         if (parts == 1) r.out = out;
         if (h->bf16) {
-            const long long most = (long long)(tiles ? RtSmem<DP>::BESIDE : RtSmem<DP>::ALONE) * h->num_sms;
+            const long long most = (long long)(beside ? RtSmem<DP>::BESIDE : RtSmem<DP>::ALONE) * h->num_sms;
             JPI_TRY(kv_start(k_kv_attend_rows<DP>, std::min(pieces, most), 32, RtSmem<DP>::BYTES, false, st, r));
         } else {
             JPI_TRY(kv_start(k_kv_attend_f32<DP>, pieces, AT_THREADS, MergeSmem<DP>::BYTES, false, st, r));
         }
     }
-    if (tiles) JPI_TRY(launch_kv_prefix_t5(h, c, splits, a.po, a.pml, parts, pieces > 0, st));
+    const int part0[2] = {0, a.p.splits};
+    if (beside) JPI_TRY(launch_kv_tiles_t5(h, c, tiles, part0, a.po, a.pml, parts, pieces > 0, st));
     if (parts == 1 && pieces > 0) return JPI_OK;
     a.out = out;
     // A warp has the loads of 8 parts (16 to D = 128) in flight: warps for as many batches, to four a row, or where the
@@ -832,7 +843,7 @@ size_t kv_attend_ws_bytes(const jpi_kv_handle* h) {
 }
 
 jpi_status kv_attend_prepare(jpi_kv_handle* h) {
-    JPI_TRY(kv_prefix_prepare(h));
+    JPI_TRY(kv_tiles_prepare(h));
     return h->D <= 64 ? prepare_dim<64>() : h->D <= 128 ? prepare_dim<128>() : prepare_dim<256>();
 }
 

@@ -1,5 +1,5 @@
-// The prefix side of jpi_kv_attend on tcgen05: 128 query rows of a run (tokens x heads of one KV head) per
-// block over a range of the shared keys, in blocks of 64 keys.
+// Sides of jpi_kv_attend with many query rows on tcgen05: 128 query rows (tokens x heads of one KV head, of a run
+// over its prefix or of a request over its own rows) per block over a range of their keys, in blocks of 64 keys.
 //   warp 0  one thread: K blocks by bulk tensor copies into a ring of NS slots (the first ones, of V too, before
 //           the block has set itself up)
 //   warp 1  one thread: V blocks into a ring of their own
@@ -12,16 +12,18 @@
 //           even and the odd blocks, each with a maximum, sum and output of its own, joined at the end. At D = 256 the
 //           products need that long, and tensor memory holds one output. O is rescaled only when a block's maximum passes the running one by
 //           more than 8 in log2 units, so that probabilities stay below 2^8.
-// The query rows are gathered by the softmax threads (a run's tokens may lie at any stride and a row
-// tile may begin and end inside a token's heads) straight into tensor memory, columns 384.., as the A operand of the
-// score products, which leaves all of shared memory to keys and values.
+// The query rows are gathered by the softmax threads (tokens may lie at any stride and a row tile may begin and end
+// inside a token's heads) into tensor memory as the A operand of the score products, which leaves all of shared memory
+// to keys and values.
 //
 // Probabilities are rounded to bf16 once (2^-9 on average of independent signs): with 128 rows a block there is
 // no time for a second term as in the row kernel, and the result's own rounding to bf16 is as large.
 // The sum l takes them unrounded.
 //
-// Rows of the last key block past the prefix's end may hold anything: their scores are replaced, and their
-// values are cleared in shared memory before the product, since 0 times a NaN would reach every row.
+// Rows past the last one that a query row of the tile sees may hold anything: their scores are replaced, and their
+// values are cleared in shared memory before the product, since 0 times a NaN would reach every row. Own rows that
+// only some of the query rows see are searched for infinities and NaN; a block that holds one is added row by row on
+// CUDA cores instead (each row its own keys), and the product adds nothing.
 //
 // Each block leaves a part (unnormalised fp32 rows, (m, l)) for k_kv_combine: rows pass through shared memory
 // (the ring, free by then) and leave by one bulk copy each, contiguous in global memory.
@@ -43,12 +45,22 @@ constexpr int KP_KEYS = 64;
 constexpr int KP_SOFT = 256;   // threads of a softmax group
 constexpr uint64_t KP_WAIT_NS = 200ull * 1000 * 1000;
 constexpr float KP_RESCALE = 8.f;   // log2 units
+constexpr int KP_LEAST = 32;        // query rows from which a side takes the tiles
+constexpr int KP_FIXED = 5;         // start and end of a block, in key blocks
 
-struct PrefixArgs {
+struct TileSide {
+    int splits = 1, tiles = 0, part0 = 0;   // key ranges, row tiles per cache and KV head, first part
+    uint32_t blocks = 0;
+    int3 at = {0, 0, 0};                    // of the maps' outer dimensions: heads, rows, caches
+    KvDiv by_splits, by_tiles;
+};
+struct TileMaps {
+    CUtensorMap k[2], v[2];   // prefix, own
+};
+struct TileArgs {
     KvCall c;
     float c2;            // log2(e) * scale
-    int splits, tiles;   // key ranges, row tiles per run and KV head
-    int3 at;             // of the maps' outer dimensions: heads, rows, runs
+    TileSide side[2];    // prefix, own
     float* po;           // [parts][rows][D]
     float2* pml;         // [rows][parts]
     long long rows;
@@ -65,13 +77,14 @@ struct KpSmem {
     static constexpr int RING = NS * STAGE > KP_ROWS * OUT_LD ? NS * STAGE : KP_ROWS * OUT_LD;
     static constexpr int NG = DP == 256 ? 1 : 2;            // softmax groups
     static constexpr int THREADS = 128 + NG * KP_SOFT;
+    static constexpr int REGS = NG == 1 ? 96 : 72;          // the rest of the SM's is the row kernel's
     // Score buffers: a third where it fits, so that a group's next scores are there when it is through with the last
     // (with two they wait for the product that reads the probabilities lying over them).
     static constexpr int NB = DP == 256 ? 2 : 3;
     static constexpr int XM_OFF = RING;                     // [groups][2 blocks][2 key halves][128 rows]
     static constexpr int ML_OFF = XM_OFF + NG * 4 * KP_ROWS * 4;    // [groups][128 rows] (m, l)
     static constexpr int BAR_OFF = ML_OFF + NG * KP_ROWS * 8;
-    static constexpr int BYTES = BAR_OFF + 8 * (3 * NB + NG + 1 + 4 * NS + 1);
+    static constexpr int BYTES = BAR_OFF + 8 * (3 * NB + NG + 1 + 4 * NS + 2);
     // The query rows' way to a row per thread: 4 KB a warp in the last QS value slots, which are filled after it.
     static constexpr int TURN = KVBYTES / 4096, QS = DP == 256 ? 1 : 2;
     static_assert(QS < NS && TURN * QS >= (DP == 64 ? 4 : 8), "the query rows fit those slots");
@@ -94,10 +107,20 @@ __device__ __forceinline__ uint64_t pair2(float a) {
     return v;
 }
 
+// Whether any of the `n` threads that share named barrier `id` says so.
+__device__ __forceinline__ bool group_any(uint32_t id, uint32_t n, bool mine) {
+    uint32_t r;
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.u32 p, %3, 0;\n bar.red.or.pred q, %1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+        : "=r"(r)
+        : "r"(id), "r"(n), "r"((uint32_t)mine)
+        : "memory");
+    return r != 0;
+}
+
 template <int DP>
-__global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const __grid_constant__ CUtensorMap kmap,
-                                                                const __grid_constant__ CUtensorMap vmap,
-                                                                const __grid_constant__ PrefixArgs a) {
+__global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constant__ TileMaps maps,
+                                                               const __grid_constant__ TileArgs a) {
     using L = KpSmem<DP>;
     constexpr int NS = L::NS, NG = L::NG, NB = L::NB, NDB = DP / 64;
     constexpr uint32_t IDESC_S = ptx::idesc_bf16_f32(KP_ROWS, KP_KEYS);
@@ -118,21 +141,44 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
     uint64_t* vempty = kempty + NS;
     uint32_t* tmem_slot = (uint32_t*)(vempty + NS);
     int* flag = (int*)(tmem_slot + 1);
+    int* begun = flag + 1;             // NG: the group's output holds something before its first product
 
     const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
     ptx::grid_dep_launch();
+    const bool own = blockIdx.x >= a.side[0].blocks;
+    const TileSide& sd = a.side[own];
+    const KvSide& ks = own ? a.c.own : a.c.prefix;
+    const CUtensorMap* const kmap = &maps.k[own];
+    const CUtensorMap* const vmap = &maps.v[own];
     // Row tiles fastest: the blocks that read the same keys run together.
-    uint32_t w = blockIdx.x;
-    const int tile = (int)(w % (uint32_t)a.tiles);
-    w /= (uint32_t)a.tiles;
-    const int split = (int)(w % (uint32_t)a.splits);
-    w /= (uint32_t)a.splits;
-    const int kvh = (int)(w % (uint32_t)a.c.K), run = (int)(w / (uint32_t)a.c.K);
-    const int len = min(max(a.c.prefix.len[run], 0), a.c.prefix.rows);
-    // This block's key blocks; none where the prefix is shorter than its splits: the part then weighs nothing.
+    uint32_t tile, split, kvh;
+    const int cache = (int)a.c.by_K.div(sd.by_splits.div(sd.by_tiles.div(blockIdx.x - (own ? a.side[0].blocks : 0), tile), split), kvh);
+    RowTile t;
+    const int toks = own ? a.c.tokens : a.c.batch / a.c.groups * a.c.tokens;
+    t.tok0 = (long long)cache * toks;
+    t.head0 = (int)kvh * a.c.gq;
+    t.R = toks * a.c.gq;
+    t.r0 = (int)tile * KP_ROWS;
+    // Keys that some row of the tile sees, and that every row sees.
+    int len, low;
+    if (own) {
+        const int last = (int)a.c.by_gq.div((uint32_t)min(t.r0 + KP_ROWS, t.R) - 1);
+        len = 0;
+        low = ks.rows;
+        for (int k = (int)a.c.by_gq.div((uint32_t)t.r0) + lane; k <= last; k += 32) {
+            const int n = min(max(ks.len[t.tok0 + k], 0), ks.rows);
+            len = max(len, n);
+            low = min(low, n);
+        }
+        len = __reduce_max_sync(0xffffffffu, len);
+        low = __reduce_min_sync(0xffffffffu, low);
+    } else {
+        len = low = min(max(ks.len[cache], 0), ks.rows);
+    }
+    // This block's key blocks; none where the keys are fewer than the splits: the part then weighs nothing.
     const int nb_all = (len + KP_KEYS - 1) / KP_KEYS;
-    const int blk0 = (int)((long long)split * nb_all / a.splits);
-    const int nb = (int)((long long)(split + 1) * nb_all / a.splits) - blk0;
+    const int blk0 = (int)((long long)split * nb_all / sd.splits);
+    const int nb = (int)((long long)(split + 1) * nb_all / sd.splits) - blk0;
     // Key (value) block i into its ring slot.
     auto load = [&](bool is_v, int i) {
         const int sl = i % NS, key0 = (blk0 + i) * KP_KEYS;
@@ -140,11 +186,11 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
         uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0);
         ptx::mbar_expect_tx(full, (uint32_t)L::KVBYTES);
         for (int db = 0; db < NDB; ++db)
-            kv_load_box(base + db * (KP_KEYS * 128), is_v ? &vmap : &kmap, full, db * 64, a.at, kvh, key0, run);
+            kv_load_box(base + db * (KP_KEYS * 128), is_v ? vmap : kmap, full, db * 64, sd.at, (int)kvh, key0, cache);
     };
     if (warp == 0 && ptx::elect_one()) {
-        ptx::prefetch_tmap(&kmap);
-        ptx::prefetch_tmap(&vmap);
+        ptx::prefetch_tmap(kmap);
+        ptx::prefetch_tmap(vmap);
         for (int b = 0; b < NB; ++b) {
             ptx::mbar_init(&sfull[b], 1);
             ptx::mbar_init(&pfull[b], KP_SOFT);
@@ -160,6 +206,7 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
         }
         ptx::fence_mbar_init();
         *flag = 0;
+        for (int b = 0; b < NG; ++b) begun[b] = 0;
         // The first use of the ring needs nothing of the other warps.
         for (int i = 0; i < NS && i < nb; ++i) {
             load(false, i);
@@ -170,12 +217,6 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
         ptx::tmem_alloc(tmem_slot, L::TMEM_COLS);
         ptx::tmem_relinquish();
     }
-    RowTile t;
-    const int toks = a.c.batch / a.c.groups * a.c.tokens;
-    t.tok0 = (long long)run * toks;
-    t.head0 = kvh * a.c.gq;
-    t.R = toks * a.c.gq;
-    t.r0 = tile * KP_ROWS;
     // The softmax warps' query rows, on their way while the block sets itself up: 64-element blocks (warp - 4) / 4,
     // + 2, of the rows of the warp's TMEM lanes.
     constexpr int QN = (NDB + 1) / 2;
@@ -270,7 +311,7 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
 #pragma unroll
                     for (int kk = 0; kk < KP_KEYS / 16; ++kk)
                         ptx::mma_bf16_ta(tmem + L::TMEM_O + (uint32_t)(i % NG * DP), tmem + (uint32_t)(KP_KEYS * (i % NB) + 8 * kk),
-                                         ptx::desc_add(vb, kk * 16 * 128), IDESC_PV, i >= NG || kk != 0);
+                                         ptx::desc_add(vb, kk * 16 * 128), IDESC_PV, i >= NG || kk != 0 || begun[i] != 0);
                 }
                 if (i + NS < nb) ptx::mma_commit(&vempty[sl]);
                 if (i + NB < nb) ptx::mma_commit(&odone[i % NB]);
@@ -282,7 +323,7 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
         const int grp = (warp - 4) >> 3, row = (warp & 3) * 32 + lane, half = ((warp - 4) >> 2) & 1;
         const int r = t.r0 + row;
         const bool valid = r < t.R;
-        const int nvis = valid ? len : 0;
+        const int nvis = !valid ? 0 : own ? min(max(ks.len[row_token(a.c, t, r)], 0), ks.rows) : len;
         const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t out = lane_base + L::TMEM_O + (uint32_t)(grp * DP);
         const uint32_t pair_bar = 1 + 4 * grp + (warp & 3);   // the two warps of these 32 rows
@@ -293,17 +334,17 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
         if (grp == 0) {
             const int wi = warp - 4;
             uint4* turn = (uint4*)(stages + (NS - 1 - wi / L::TURN) * L::STAGE + L::KVBYTES + wi % L::TURN * 4096);
-    #pragma unroll
+#pragma unroll
             for (int k = 0; k < QN; ++k) {
                 const int db = half + 2 * k;
                 if (db < NDB) {
-    #pragma unroll
+#pragma unroll
                     for (int i = 0; i < 8; ++i) turn[(4 * i + (lane >> 3)) * 8 + ((lane & 7) ^ ((4 * i + (lane >> 3)) & 7))] = qv[k][i];
                     __syncwarp();
-    #pragma unroll
+#pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {
                         uint32_t rq[16];
-    #pragma unroll
+#pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             const uint4 v = turn[lane * 8 + ((4 * hf + c) ^ (lane & 7))];
                             rq[4 * c] = v.x;
@@ -315,7 +356,7 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
                     }
                     __syncwarp();
                 }
-        }
+            }
             ptx::tmem_st_wait();
             ptx::fence_proxy_async_smem();   // the slots' values land after these accesses
             ptx::tc_fence_before();
@@ -385,11 +426,75 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
                 pk[k / 2] = kr_pack(p0, p1);
             }
             l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+            const int live = len - (blk0 + i) * KP_KEYS;   // keys of the block that some row sees; the same for all threads
+            if (low < min(len, (blk0 + i + 1) * KP_KEYS)) {
+                // Some rows see a part of them only: is there an infinity or NaN among the values?
+                const int sl = i % NS;
+                if (good) good = ptx::mbar_wait_bounded(&vfull[sl], (i / NS) & 1, KP_WAIT_NS);
+                uint8_t* vb = stages + sl * L::STAGE + L::KVBYTES;
+                bool odd = false;
+                for (int e = (tid - 128) % KP_SOFT; e < min(live, KP_KEYS) * NDB * 8; e += KP_SOFT) {
+                    const int key = e / (NDB * 8), p = e % (NDB * 8);
+                    const uint4 v = *(const uint4*)(vb + (p / 8) * (KP_KEYS * 128) + key * 128 + (p % 8) * 16);
+                    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) odd = odd || (x[k] & 0x7f80u) == 0x7f80u || (x[k] & 0x7f800000u) == 0x7f800000u;
+                }
+                if (group_any(11 + grp, KP_SOFT, odd)) {
+                    // Row by row: first one half's keys, then the other's, onto the settled output of the blocks before.
+                    if (i >= NG && good) good = ptx::mbar_wait_bounded(&gdone[grp], (i / NG - 1) & 1, KP_WAIT_NS);
+                    ptx::tc_fence_after();
+                    for (int turn = 0; turn < 2; ++turn) {
+                        if (turn == half) {
+#pragma unroll 1
+                            for (int c0 = 0; c0 < DP; c0 += 16) {
+                                uint32_t ro[16];
+                                if (i < NG && turn == 0) {
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) ro[j] = 0u;
+                                } else {
+                                    ptx::tmem_ld_x16(out + (uint32_t)c0, ro);
+                                    ptx::tmem_ld_wait();
+                                }
+#pragma unroll
+                                for (int k = 0; k < HK; ++k) {
+                                    if (k >= vis) continue;
+                                    const int key = HK * half + k;
+                                    const float pr = __uint_as_float(k & 1 ? pk[k / 2] & 0xffff0000u : pk[k / 2] << 16);
+                                    const uint8_t* vr = vb + (c0 / 64) * (KP_KEYS * 128) + key * 128;
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h) {
+                                        const uint4 v = *(const uint4*)(vr + (((c0 % 64 / 8 + h) ^ (key & 7)) << 4));
+                                        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                        for (int e = 0; e < 4; ++e) {
+                                            uint32_t &y0 = ro[8 * h + 2 * e], &y1 = ro[8 * h + 2 * e + 1];
+                                            y0 = __float_as_uint(fmaf(pr, __uint_as_float(x[e] << 16), __uint_as_float(y0)));
+                                            y1 = __float_as_uint(fmaf(pr, __uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y1)));
+                                        }
+                                    }
+                                }
+                                __syncwarp();
+                                ptx::tmem_st_x16(out + (uint32_t)c0, ro);
+                            }
+                            ptx::tmem_st_wait();
+                            ptx::tc_fence_before();
+                        }
+                        ptx::named_bar_sync(pair_bar, 64);
+                        ptx::tc_fence_after();
+                    }
+#pragma unroll
+                    for (int k = 0; k < HK / 2; ++k) pk[k] = 0u;
+                    ptx::named_bar_sync(11 + grp, KP_SOFT);   // every thread has read the values
+                    for (int e = (tid - 128) % KP_SOFT; good && e < KP_KEYS * NDB * 8; e += KP_SOFT) ((uint4*)vb)[e] = make_uint4(0, 0, 0, 0);
+                    if (i < NG && tid % KP_SOFT == 128) begun[grp] = 1;
+                    ptx::fence_proxy_async_smem();
+                }
+            }
             // Over the scores of both halves: both threads of a row have read theirs (the barrier above). Column 16 half
             // + e holds keys 32 half + 2 e, + 1.
             ptx::tmem_st_x16(lane_base + (uint32_t)(KP_KEYS * (i % NB) + 16 * half), pk);
             ptx::tmem_st_wait();
-            const int live = len - (blk0 + i) * KP_KEYS;   // the same for the whole block
             if (live < KP_KEYS) {
                 // Values of rows past the end, as they landed: cleared (a row's 16-byte pieces stay in the row).
                 const int sl = i % NS;
@@ -465,8 +570,8 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
             ptx::named_bar_sync(pair_bar, 64);
             ptx::grid_dep_wait();   // the row kernel that started before this one: what waits for this kernel has both
             if (half == 0 && valid) {
-                const long long row_at = row_index(a.c, t, r), row_out = split * a.rows + row_at;
-                a.pml[row_at * a.parts + split] = make_float2(m_used, l);
+                const long long row_at = row_index(a.c, t, r), row_out = (sd.part0 + (long long)split) * a.rows + row_at;
+                a.pml[row_at * a.parts + sd.part0 + split] = make_float2(m_used, l);
                 if (good && nb > 0) {
                     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.po + row_out * a.c.D),
                                  "r"(ptx::smem_u32(orow)), "r"(a.c.D * 4)
@@ -485,63 +590,101 @@ __global__ void __launch_bounds__(KpSmem<DP>::THREADS, 1) k_kv_prefix_t5(const _
 }
 
 template <int DP>
-jpi_status launch_dim(const PrefixArgs& a, const CUtensorMap& km, const CUtensorMap& vm, bool early, cudaStream_t st) {
-    const long long blocks = (long long)a.tiles * a.splits * a.c.K * a.c.groups;
-    return kv_start(k_kv_prefix_t5<DP>, blocks, KpSmem<DP>::THREADS, KpSmem<DP>::BYTES, early, st, km, vm, a);
+jpi_status launch_dim(const TileArgs& a, const TileMaps& m, bool early, cudaStream_t st) {
+    return kv_start(k_kv_tiles_t5<DP>, dim3(a.side[0].blocks + a.side[1].blocks), KpSmem<DP>::THREADS, KpSmem<DP>::BYTES, early, st, m, a);
 }
 
 template <int DP>
 jpi_status prepare_dim() {
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<DP>::BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_tiles_t5<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<DP>::BYTES));
     // An SM that runs a block of the row kernel takes one of these beside it only if both want it set up alike.
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_prefix_t5<DP>, cudaFuncAttributePreferredSharedMemoryCarveout,
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_tiles_t5<DP>, cudaFuncAttributePreferredSharedMemoryCarveout,
                                       cudaSharedmemCarveoutMaxShared));
     return JPI_OK;
 }
 
+// What the tiles would make of a side: row tiles over all caches and KV heads, and key blocks of each.
+struct TileWork {
+    bool fit = false;
+    long long tiles = 0, blocks = 0, nb = 0;
+};
+TileWork work_of(const jpi_kv_handle* h, const KvCall& c, bool own) {
+    TileWork w;
+    const KvSide& s = own ? c.own : c.prefix;
+    if (!h->bf16 || c.D < 64 || s.rows == 0) return w;
+    const int caches = own ? c.batch : c.groups;
+    const long long R = (long long)(own ? 1 : c.batch / c.groups) * c.tokens * c.gq;
+    KvMapDims m;
+    if (R < KP_LEAST || !kv_map_dims(s, c.K, c.D, caches, &m)) return w;
+    w.tiles = (R + KP_ROWS - 1) / KP_ROWS;
+    w.blocks = w.tiles * c.K * caches;
+    w.nb = (s.rows + KP_KEYS - 1) / KP_KEYS;
+    w.fit = w.blocks * w.nb < (1ll << 31);
+    return w;
+}
+
 }  // namespace
 
-jpi_status kv_prefix_prepare(jpi_kv_handle* h) {
+jpi_status kv_tiles_prepare(jpi_kv_handle* h) {
     if (!h->bf16 || h->D < 64) return JPI_OK;
     return h->D <= 64 ? prepare_dim<64>() : h->D <= 128 ? prepare_dim<128>() : prepare_dim<256>();
 }
 
-bool kv_prefix_splits(const jpi_kv_handle* h, const KvCall& c, long long room, int* splits) {
-    if (!h->bf16 || c.D < 64 || c.prefix.rows == 0) return false;
-    const long long R = (long long)(c.batch / c.groups) * c.tokens * c.gq;
-    if (R < 32) return false;
-    KvMapDims m;
-    if (!kv_map_dims(c.prefix, c.K, c.D, c.groups, &m)) return false;
-    const long long tiles = (R + KP_ROWS - 1) / KP_ROWS, blocks = tiles * c.K * c.groups;
-    const long long nb = (c.prefix.rows + KP_KEYS - 1) / KP_KEYS;
-    long long s = std::max(1ll, h->num_sms / blocks);
-    *splits = (int)std::max(1ll, std::min({s, room, nb}));
-    return blocks * *splits <= 0x7fffffffll;
+void kv_tiles_plan(const jpi_kv_handle* h, const KvCall& c, long long room, int splits[2]) {
+    const TileWork p = work_of(h, c, false), o = work_of(h, c, true);
+    splits[0] = splits[1] = 0;
+    // The side of more key blocks is split so that the longest block, or the waves of them, end first; a block starts and ends
+    // in about KP_FIXED key blocks' time. The other side is split to blocks no longer than those.
+    const bool own_first = o.fit && (!p.fit || o.blocks * o.nb > p.blocks * p.nb);
+    const TileWork &a = own_first ? o : p, &b = own_first ? p : o;
+    if (!a.fit) return;
+    const long long most = std::min({a.nb, room, std::max(1ll, 2ll * h->num_sms / a.blocks)});
+    long long best = 1, best_time = 0, unit = a.nb + KP_FIXED;
+    for (long long s = 1; s <= most; ++s) {
+        const long long u = (a.nb + s - 1) / s + KP_FIXED;
+        const long long rest = b.fit ? b.blocks * (std::min(b.nb, u - KP_FIXED) + KP_FIXED) * ((b.nb + u - KP_FIXED - 1) / (u - KP_FIXED)) : 0;
+        const long long time = std::max((a.blocks * s + h->num_sms - 1) / h->num_sms * u, (a.blocks * s * u + rest) / h->num_sms);
+        if (s == 1 || time < best_time) {
+            best = s;
+            best_time = time;
+            unit = u;
+        }
+    }
+    splits[own_first] = (int)best;
+    if (b.fit) splits[!own_first] = (int)std::max(1ll, std::min(room, (b.nb + unit - KP_FIXED - 1) / (unit - KP_FIXED)));
 }
 
-jpi_status launch_kv_prefix_t5(jpi_kv_handle* h, const KvCall& c, int splits, float* po, float2* pml, int parts,
-                               bool early, cudaStream_t st) {
-    PrefixArgs a;
+jpi_status launch_kv_tiles_t5(jpi_kv_handle* h, const KvCall& c, const int splits[2], const int part0[2], float* po, float2* pml,
+                              int parts, bool early, cudaStream_t st) {
+    TileArgs a = {};
+    TileMaps maps = {};
     a.c = c;
     a.c2 = KR_LOG2E * c.scale;
-    a.splits = splits;
-    const long long R = (long long)(c.batch / c.groups) * c.tokens * c.gq;
-    a.tiles = (int)((R + KP_ROWS - 1) / KP_ROWS);
     a.po = po;
     a.pml = pml;
     a.parts = parts;
     a.rows = (long long)c.batch * c.tokens * c.H;
     a.err = h->dev_err;
-    KvMapDims m;
-    CUtensorMap km, vm;
-    if (!kv_map_dims(c.prefix, c.K, c.D, c.groups, &m) || !kv_make_map(m, c.prefix.k, c.D, KP_KEYS, &km) ||
-        !kv_make_map(m, c.prefix.v, c.D, KP_KEYS, &vm)) {
-        set_error("cuTensorMapEncodeTiled refused the prefix");
-        return JPI_ERR_CUDA;
+    for (int i = 0; i < 2; ++i) {
+        if (splits[i] == 0) continue;
+        const TileWork w = work_of(h, c, i == 1);
+        const KvSide& s = i ? c.own : c.prefix;
+        TileSide& d = a.side[i];
+        d.splits = splits[i];
+        d.tiles = (int)w.tiles;
+        d.part0 = part0[i];
+        d.blocks = (uint32_t)(w.blocks * splits[i]);
+        d.by_splits = KvDiv((uint32_t)d.splits);
+        d.by_tiles = KvDiv((uint32_t)d.tiles);
+        KvMapDims m;
+        if (!kv_map_dims(s, c.K, c.D, i ? c.batch : c.groups, &m) || !kv_make_map(m, s.k, c.D, KP_KEYS, &maps.k[i]) ||
+            !kv_make_map(m, s.v, c.D, KP_KEYS, &maps.v[i])) {
+            set_error("cuTensorMapEncodeTiled refused the %s", i ? "own rows" : "prefix");
+            return JPI_ERR_CUDA;
+        }
+        d.at = make_int3(m.at_head, m.at_row, m.at_cache);
     }
-    a.at = make_int3(m.at_head, m.at_row, m.at_cache);
-    return c.D <= 64 ? launch_dim<64>(a, km, vm, early, st)
-                     : c.D <= 128 ? launch_dim<128>(a, km, vm, early, st) : launch_dim<256>(a, km, vm, early, st);
+    return c.D <= 64 ? launch_dim<64>(a, maps, early, st) : c.D <= 128 ? launch_dim<128>(a, maps, early, st) : launch_dim<256>(a, maps, early, st);
 }
 
 }  // namespace jpi

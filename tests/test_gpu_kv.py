@@ -243,6 +243,7 @@ def test_attend_batches_and_masks(kv, mask, B, T, G):
 
 
 @pytest.mark.parametrize("H,K,D,B,T,G,P,R", [
+    (8, 1, 256, 2, 100, 1, 130, 300), (16, 2, 128, 3, 64, 3, 70, 1000), (4, 1, 64, 2, 33, 1, 5, 129), (8, 1, 256, 1, 300, 1, 0, 700),
     (8, 1, 256, 16, 1, 1, 816, 40), (8, 1, 256, 40, 1, 1, 333, 9), (8, 1, 256, 4, 51, 2, 200, 51), (8, 1, 128, 32, 1, 1, 700, 5),
     (32, 8, 128, 48, 1, 1, 450, 33), (16, 16, 64, 64, 2, 1, 260, 12), (8, 1, 256, 18, 8, 1, 64, 0), (8, 1, 64, 16, 3, 1, 1, 1)])
 def test_attend_many_rows_on_one_prefix(kv, H, K, D, B, T, G, P, R):
@@ -262,21 +263,36 @@ def test_attend_scale_and_large_scores(kv):
     check_attend(kv, "fp32", 2, 1, 64, 2, 2, 1, 120, 10, seed=3, std=30.0)
 
 
-def test_attend_a_bad_value_reaches_only_the_queries_that_see_it(kv):
-    for dtype in ("bf16", "fp32"):
-        c = make_call(7, dtype, 8, 1, 64, 2, 6, 1, 20, 12, mask="causal")
-        c["seen"] = i32([[0, 1, 5, 6, 7, 12], [3, 3, 3, 4, 4, 4]])
-        for t in (*c["own"],):
-            t.copy_(rand(8, *t.shape, dtype=dtype))
-        for bad in (float("nan"), float("inf")):
-            h = kv.KV(8, 1, 64, max_batch=2, max_tokens=6, precision=dtype)
-            want, _ = h.attend(**c)
+@pytest.mark.parametrize("dtype,H,K,D,T,R", [("fp32", 8, 1, 64, 6, 12), ("bf16", 2, 1, 64, 6, 12), ("bf16", 8, 1, 64, 6, 12),
+                                             ("bf16", 8, 1, 256, 40, 150), ("bf16", 16, 2, 128, 70, 300), ("bf16", 8, 1, 96, 20, 70),
+                                             ("bf16", 4, 4, 64, 50, 200)])
+def test_attend_a_bad_value_reaches_only_the_queries_that_see_it(kv, dtype, H, K, D, T, R):
+    """Infinities and NaN among the values, in the first, a middle and the last rows: the queries that see them get
+    non-finite results in that element, the others what the oracle gives without them."""
+    c = make_call(7, dtype, H, K, D, 2, T, 1, 20, R, mask="any")
+    rng = np.random.default_rng(R)
+    seen = np.sort(rng.integers(0, R + 1, (2, T)), axis=1)
+    seen[0, 0], seen[0, -1] = 0, R
+    seen[1] = rng.permutation(seen[1])
+    c["seen"] = i32(seen)
+    for t in c["own"]:
+        t.copy_(rand(8, *t.shape, dtype=dtype))
+    ref, rlse, dot, mass = attend_ref(c, 1 / math.sqrt(D))
+    tol, ltol = attend_tols(c, dtype, ref, dot, mass, rlse)
+    h = kv.KV(H, K, D, max_batch=2, max_tokens=T, precision=dtype)
+    for bad in (float("nan"), float("inf")):
+        for at in (0, R // 2, R - 1):
             dirty = dict(c, own=(c["own"][0], c["own"][1].clone()))
-            dirty["own"][1][0, 6] = bad     # seen by tokens 4 and 5 of request 0 only
-            dirty["own"][1][1, 3] = bad     # by tokens 3, 4, 5 of request 1
-            got, _ = h.attend(**dirty)
-            assert torch.equal(got[0, :4], want[0, :4]) and torch.equal(got[1, :3], want[1, :3])
-            assert not got[0, 4:].isfinite().all() and not got[1, 3:].isfinite().all()
+            dirty["own"][1][:, at, 0, 3] = bad
+            got, lse = h.attend(**dirty)
+            h.device_status()
+            within(lse, rlse, ltol, "lse")
+            sees = seen > at                                            # [2][T]
+            hit = np.zeros(ref.shape, bool)
+            hit[:, :, :H // K, 3] = sees[:, :, None]
+            assert not np.isfinite(np64(got)[hit]).any()
+            clean = torch.where(torch.tensor(hit, device="cuda"), torch.zeros_like(got), got)
+            within(clean, np.where(hit, 0.0, ref), np.where(hit, 0.0, tol), f"value {bad} in row {at}")
 
 
 def test_attend_lowest_values_and_lengths_out_of_range(kv):
