@@ -777,9 +777,9 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
     a.po = static_cast<float*>(h->ws);
     a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
     a.lse = lse;
-    int tiles[2];   // key splits of the sides that take the 128-row tiles
-    kv_tiles_plan(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), tiles);
-    const bool beside = tiles[0] + tiles[1] > 0;
+    KvTilesPlan tiles;
+    kv_tiles_plan(h, c, std::max(1ll, ws_rows(h) / 2 / a.rows), &tiles);
+    const bool beside = tiles.takes(false) || tiles.takes(true);
     if (h->bf16) {
         // Single warps with 64 KB of keys and values or more each.
         constexpr int KEYS = RtSmem<DP>::KEYS;
@@ -791,10 +791,10 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
         a.o = plan_side(h, c, false, AT_WARPS, 32, 32, 2ll * h->num_sms);
     }
     for (int i = 0; i < 2; ++i)
-        if (tiles[i] > 0) {
+        if (tiles.takes(i)) {
             SidePlan& s = i ? a.o : a.p;
             s.blocks = 0;
-            s.splits = tiles[i];
+            s.splits = tiles.splits[i];
         }
     const int parts = a.parts = a.p.splits + a.o.splits;
     const long long pieces = a.p.blocks + a.o.blocks;
@@ -813,8 +813,8 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
         }
     }
     const int part0[2] = {0, a.p.splits};
-    if (beside) JPI_TRY(launch_kv_tiles_t5(h, c, tiles, part0, a.po, a.pml, parts, pieces > 0, st));
-    if (parts == 1 && pieces > 0) return JPI_OK;
+    if (beside) JPI_TRY(launch_kv_tiles_t5(h, c, tiles, part0, a.po, a.pml, parts, out, lse, pieces > 0, st));
+    if (parts == 1) return JPI_OK;
     a.out = out;
     // A warp has the loads of 8 parts (16 to D = 128) in flight: warps for as many batches, to four a row, or where the
     // rows are few to sixteen.

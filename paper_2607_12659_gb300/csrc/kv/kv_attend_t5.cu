@@ -1,5 +1,8 @@
 // Sides of jpi_kv_attend with many query rows on tcgen05: 128 query rows (tokens x heads of one KV head, of a run
-// over its prefix or of a request over its own rows) per block over a range of their keys, in blocks of 64 keys.
+// over its prefix or of a request over its own rows) per block over a range of their keys, in blocks of 64 keys. Where a
+// request's query rows alone fill tiles, these take the prefix's keys and then the request's own in one pass, and a
+// tile that is not split writes the result itself; else the run's rows share the prefix's tiles, and the parts are
+// joined by k_kv_combine.
 //   warp 0  one thread: K blocks by bulk tensor copies into a ring of NS slots (the first ones, of V too, before
 //           the block has set itself up)
 //   warp 1  one thread: V blocks into a ring of their own
@@ -25,8 +28,8 @@
 // only some of the query rows see are searched for infinities and NaN; a block that holds one is added row by row on
 // CUDA cores instead (each row its own keys), and the product adds nothing.
 //
-// Each block leaves a part (unnormalised fp32 rows, (m, l)) for k_kv_combine: rows pass through shared memory
-// (the ring, free by then) and leave by one bulk copy each, contiguous in global memory.
+// Each block leaves a part (unnormalised fp32 rows, (m, l)) for k_kv_combine, or the result: rows pass through shared
+// memory (the ring, free by then) and leave by bulk copies, contiguous in global memory (about 27 bytes a cycle).
 //
 // Every wait is bounded; a wait that gives up records an error in the handle's word, and its thread waits for
 // nothing more.
@@ -48,10 +51,11 @@ constexpr float KP_RESCALE = 8.f;   // log2 units
 constexpr int KP_LEAST = 32;        // query rows from which a side takes the tiles
 constexpr int KP_FIXED = 5;         // start and end of a block, in key blocks
 
+// Tiles of a run's rows over its prefix (0), or of a request's rows over its own keys (1), with `both` over the prefix's
+// before them.
 struct TileSide {
-    int splits = 1, tiles = 0, part0 = 0;   // key ranges, row tiles per cache and KV head, first part
+    int splits = 1, tiles = 0, part0 = 0;   // key ranges, row tiles per run or request and KV head, first part
     uint32_t blocks = 0;
-    int3 at = {0, 0, 0};                    // of the maps' outer dimensions: heads, rows, caches
     KvDiv by_splits, by_tiles;
 };
 struct TileMaps {
@@ -60,11 +64,16 @@ struct TileMaps {
 struct TileArgs {
     KvCall c;
     float c2;            // log2(e) * scale
-    TileSide side[2];    // prefix, own
+    TileSide side[2];
+    int3 at[2];          // of the maps' outer dimensions: heads, rows, caches
+    bool both;
+    KvDiv by_run;        // requests of a run
     float* po;           // [parts][rows][D]
     float2* pml;         // [rows][parts]
     long long rows;
     int parts;
+    __nv_bfloat16* out;  // of a call of one part: the result, else null
+    float* lse;
     int* err;
 };
 
@@ -118,7 +127,12 @@ __device__ __forceinline__ bool group_any(uint32_t id, uint32_t n, bool mine) {
     return r != 0;
 }
 
-template <int DP>
+// Whether one of two bf16 values is an infinity or NaN.
+__device__ __forceinline__ bool bad_pair(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+
+// OWN: some tiles take own rows (the kernel without them needs fewer registers: prefixes of 30016 keys of 8 KV heads took 43 us
+// with it and 39 without).
+template <int DP, bool OWN>
 __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constant__ TileMaps maps,
                                                                const __grid_constant__ TileArgs a) {
     using L = KpSmem<DP>;
@@ -145,11 +159,8 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
 
     const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
     ptx::grid_dep_launch();
-    const bool own = blockIdx.x >= a.side[0].blocks;
+    const bool own = OWN && blockIdx.x >= a.side[0].blocks;
     const TileSide& sd = a.side[own];
-    const KvSide& ks = own ? a.c.own : a.c.prefix;
-    const CUtensorMap* const kmap = &maps.k[own];
-    const CUtensorMap* const vmap = &maps.v[own];
     // Row tiles fastest: the blocks that read the same keys run together.
     uint32_t tile, split, kvh;
     const int cache = (int)a.c.by_K.div(sd.by_splits.div(sd.by_tiles.div(blockIdx.x - (own ? a.side[0].blocks : 0), tile), split), kvh);
@@ -159,38 +170,40 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
     t.head0 = (int)kvh * a.c.gq;
     t.R = toks * a.c.gq;
     t.r0 = (int)tile * KP_ROWS;
-    // Keys that some row of the tile sees, and that every row sees.
-    int len, low;
+    // The tile's keys: rows of the run's prefix, then of the request's cache. Of the latter, `own_len` that some query row
+    // of the tile sees and `own_low` that every one does.
+    const int run = own ? (int)a.by_run.div((uint32_t)cache) : cache;
+    const int pre_len = own && !a.both ? 0 : min(max(a.c.prefix.len[run], 0), a.c.prefix.rows);
+    int own_len = 0, own_low = 0;
     if (own) {
         const int last = (int)a.c.by_gq.div((uint32_t)min(t.r0 + KP_ROWS, t.R) - 1);
-        len = 0;
-        low = ks.rows;
+        own_low = a.c.own.rows;
         for (int k = (int)a.c.by_gq.div((uint32_t)t.r0) + lane; k <= last; k += 32) {
-            const int n = min(max(ks.len[t.tok0 + k], 0), ks.rows);
-            len = max(len, n);
-            low = min(low, n);
+            const int n = min(max(a.c.own.len[t.tok0 + k], 0), a.c.own.rows);
+            own_len = max(own_len, n);
+            own_low = min(own_low, n);
         }
-        len = __reduce_max_sync(0xffffffffu, len);
-        low = __reduce_min_sync(0xffffffffu, low);
-    } else {
-        len = low = min(max(ks.len[cache], 0), ks.rows);
+        own_len = __reduce_max_sync(0xffffffffu, own_len);
+        own_low = __reduce_min_sync(0xffffffffu, own_low);
     }
-    // This block's key blocks; none where the keys are fewer than the splits: the part then weighs nothing.
-    const int nb_all = (len + KP_KEYS - 1) / KP_KEYS;
+    // This block's key blocks, of the prefix's npre and then the own ones; none where they are fewer than the splits: the
+    // part then weighs nothing.
+    const int npre = (pre_len + KP_KEYS - 1) / KP_KEYS, nb_all = npre + (own_len + KP_KEYS - 1) / KP_KEYS;
     const int blk0 = (int)((long long)split * nb_all / sd.splits);
     const int nb = (int)((long long)(split + 1) * nb_all / sd.splits) - blk0;
     // Key (value) block i into its ring slot.
     auto load = [&](bool is_v, int i) {
-        const int sl = i % NS, key0 = (blk0 + i) * KP_KEYS;
+        const int sl = i % NS, mine = OWN && blk0 + i >= npre, key0 = (blk0 + i - (mine ? npre : 0)) * KP_KEYS;
         uint64_t* full = (is_v ? vfull : kfull) + sl;
         uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0);
         ptx::mbar_expect_tx(full, (uint32_t)L::KVBYTES);
         for (int db = 0; db < NDB; ++db)
-            kv_load_box(base + db * (KP_KEYS * 128), is_v ? vmap : kmap, full, db * 64, sd.at, (int)kvh, key0, cache);
+            kv_load_box(base + db * (KP_KEYS * 128), is_v ? &maps.v[mine] : &maps.k[mine], full, db * 64, a.at[mine], (int)kvh, key0,
+                        mine ? cache : run);
     };
     if (warp == 0 && ptx::elect_one()) {
-        ptx::prefetch_tmap(kmap);
-        ptx::prefetch_tmap(vmap);
+        ptx::prefetch_tmap(&maps.k[OWN && blk0 >= npre]);
+        ptx::prefetch_tmap(&maps.v[OWN && blk0 >= npre]);
         for (int b = 0; b < NB; ++b) {
             ptx::mbar_init(&sfull[b], 1);
             ptx::mbar_init(&pfull[b], KP_SOFT);
@@ -311,7 +324,7 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
 #pragma unroll
                     for (int kk = 0; kk < KP_KEYS / 16; ++kk)
                         ptx::mma_bf16_ta(tmem + L::TMEM_O + (uint32_t)(i % NG * DP), tmem + (uint32_t)(KP_KEYS * (i % NB) + 8 * kk),
-                                         ptx::desc_add(vb, kk * 16 * 128), IDESC_PV, i >= NG || kk != 0 || begun[i] != 0);
+                                         ptx::desc_add(vb, kk * 16 * 128), IDESC_PV, i >= NG || kk != 0 || (OWN && begun[i] != 0));
                 }
                 if (i + NS < nb) ptx::mma_commit(&vempty[sl]);
                 if (i + NB < nb) ptx::mma_commit(&odone[i % NB]);
@@ -323,7 +336,8 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
         const int grp = (warp - 4) >> 3, row = (warp & 3) * 32 + lane, half = ((warp - 4) >> 2) & 1;
         const int r = t.r0 + row;
         const bool valid = r < t.R;
-        const int nvis = !valid ? 0 : own ? min(max(ks.len[row_token(a.c, t, r)], 0), ks.rows) : len;
+        const int pre_vis = valid ? pre_len : 0;
+        const int own_vis = valid && own ? min(max(a.c.own.len[row_token(a.c, t, r)], 0), a.c.own.rows) : 0;
         const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t out = lane_base + L::TMEM_O + (uint32_t)(grp * DP);
         const uint32_t pair_bar = 1 + 4 * grp + (warp & 3);   // the two warps of these 32 rows
@@ -375,7 +389,10 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
                 ptx::tmem_ld_x16(sa + 16u, s[1]);
                 ptx::tmem_ld_wait();
             }
-            const int vis = nvis - (blk0 + i) * KP_KEYS - HK * half;   // keys of this half block the row sees
+            // Keys of the block: its first one, and of this half the ones that the row sees.
+            const bool theirs = OWN && blk0 + i >= npre;   // own rows
+            const int key0 = (blk0 + i - (theirs ? npre : 0)) * KP_KEYS;
+            const int vis = (theirs ? own_vis : pre_vis) - key0 - HK * half;
             const bool full = __all_sync(0xffffffffu, vis >= HK);
             if (!full) {
 #pragma unroll
@@ -426,8 +443,8 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
                 pk[k / 2] = kr_pack(p0, p1);
             }
             l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-            const int live = len - (blk0 + i) * KP_KEYS;   // keys of the block that some row sees; the same for all threads
-            if (low < min(len, (blk0 + i + 1) * KP_KEYS)) {
+            const int live = (theirs ? own_len : pre_len) - key0;   // keys of the block that some row sees; the same for all threads
+            if (OWN && theirs && own_low < min(own_len, key0 + KP_KEYS)) {
                 // Some rows see a part of them only: is there an infinity or NaN among the values?
                 const int sl = i % NS;
                 if (good) good = ptx::mbar_wait_bounded(&vfull[sl], (i / NS) & 1, KP_WAIT_NS);
@@ -436,9 +453,7 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
                 for (int e = (tid - 128) % KP_SOFT; e < min(live, KP_KEYS) * NDB * 8; e += KP_SOFT) {
                     const int key = e / (NDB * 8), p = e % (NDB * 8);
                     const uint4 v = *(const uint4*)(vb + (p / 8) * (KP_KEYS * 128) + key * 128 + (p % 8) * 16);
-                    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) odd = odd || (x[k] & 0x7f80u) == 0x7f80u || (x[k] & 0x7f800000u) == 0x7f800000u;
+                    odd = odd || bad_pair(v.x) || bad_pair(v.y) || bad_pair(v.z) || bad_pair(v.w);
                 }
                 if (group_any(11 + grp, KP_SOFT, odd)) {
                     // Row by row: first one half's keys, then the other's, onto the settled output of the blocks before.
@@ -533,6 +548,8 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
             l = w * l + (other.x == -INFINITY ? 0.f : kr_ex2((other.x - M) * a.c2) * other.y);
             m_used = M;
         }
+        // A result is scaled by 1 / l and rounded on its way; a half row's 16-bit values go where its own 32-bit ones were.
+        const float inv = l > 0.f ? 1.f / l : 0.f;
         uint8_t* orow = kp_smem + row * L::OUT_LD;
 #pragma unroll 1
         for (int turn = 0; turn < NG; ++turn) {
@@ -543,20 +560,31 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
                     ptx::tmem_ld_x16(out + (uint32_t)c0, v[0]);
                     ptx::tmem_ld_x16(out + (uint32_t)(c0 + 16), v[1]);
                     ptx::tmem_ld_wait();
-                    if (good && mine > 0) {   // a wait that gave up may have left copies on their way into the ring
+                    // (a wait that gave up may have left copies on their way into the ring)
+                    if (good && (mine > 0 || (a.out && nb > 0))) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
-                            float4* dst = (float4*)(orow + (c0 + 4 * k) * 4);
-                            float4 x = make_float4(__uint_as_float(v[k >> 2][4 * (k & 3)]), __uint_as_float(v[k >> 2][4 * (k & 3) + 1]),
-                                                   __uint_as_float(v[k >> 2][4 * (k & 3) + 2]), __uint_as_float(v[k >> 2][4 * (k & 3) + 3]));
-                            if (NG > 1) {
-                                x = make_float4(w * x.x, w * x.y, w * x.z, w * x.w);
-                                if (grp > 0) {
-                                    const float4 y = *dst;
-                                    x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-                                }
+                            uint4* dst = (uint4*)(orow + (c0 + 4 * k) * 4);
+                            float x[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                x[e] = __uint_as_float(v[k >> 2][4 * (k & 3) + e]);
+                                if (NG > 1) x[e] = mine > 0 ? w * x[e] : 0.f;
                             }
-                            *dst = x;
+                            if (grp > 0) {
+                                const uint4 y = *dst;
+                                x[0] += __uint_as_float(y.x);
+                                x[1] += __uint_as_float(y.y);
+                                x[2] += __uint_as_float(y.z);
+                                x[3] += __uint_as_float(y.w);
+                            }
+                            if (a.out && grp == NG - 1) {
+                                uint32_t* dst16 = (uint32_t*)(orow + half * (DP * 2) + (c0 + 4 * k - half * (DP / 2)) * 2);
+                                dst16[0] = kr_pack(x[0] * inv, x[1] * inv);
+                                dst16[1] = kr_pack(x[2] * inv, x[3] * inv);
+                            } else {
+                                *dst = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+                            }
                         }
                     }
                 }
@@ -571,14 +599,26 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
             ptx::grid_dep_wait();   // the row kernel that started before this one: what waits for this kernel has both
             if (half == 0 && valid) {
                 const long long row_at = row_index(a.c, t, r), row_out = (sd.part0 + (long long)split) * a.rows + row_at;
-                a.pml[row_at * a.parts + sd.part0 + split] = make_float2(m_used, l);
-                if (good && nb > 0) {
-                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.po + row_out * a.c.D),
-                                 "r"(ptx::smem_u32(orow)), "r"(a.c.D * 4)
+                auto copy = [&](void* dst, const uint8_t* src, int bytes) {
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(ptx::smem_u32(src)),
+                                 "r"(bytes)
                                  : "memory");
-                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                };
+                if (a.out) {
+                    __nv_bfloat16* dst = a.out + row_at * a.c.D;
+                    if (a.lse) a.lse[row_at] = m_used == -INFINITY ? -INFINITY : fmaf(m_used, a.c.scale, logf(l));
+                    if (nb == 0) {
+                        for (int d = 0; d < a.c.D; d += 8) *(uint4*)(dst + d) = make_uint4(0, 0, 0, 0);
+                    } else if (good) {
+                        copy(dst, orow, min(a.c.D, DP / 2) * 2);
+                        if (a.c.D > DP / 2) copy(dst + DP / 2, orow + DP * 2, (a.c.D - DP / 2) * 2);
+                    }
+                } else {
+                    a.pml[row_at * a.parts + sd.part0 + split] = make_float2(m_used, l);
+                    if (good && nb > 0) copy(a.po + row_out * a.c.D, orow, a.c.D * 4);
                 }
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             }
         }
     }
@@ -591,19 +631,21 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
 
 template <int DP>
 jpi_status launch_dim(const TileArgs& a, const TileMaps& m, bool early, cudaStream_t st) {
-    return kv_start(k_kv_tiles_t5<DP>, dim3(a.side[0].blocks + a.side[1].blocks), KpSmem<DP>::THREADS, KpSmem<DP>::BYTES, early, st, m, a);
+    return kv_start(a.side[1].blocks > 0 ? k_kv_tiles_t5<DP, true> : k_kv_tiles_t5<DP, false>,
+                    dim3(a.side[0].blocks + a.side[1].blocks), KpSmem<DP>::THREADS, KpSmem<DP>::BYTES, early, st, m, a);
 }
 
 template <int DP>
 jpi_status prepare_dim() {
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_tiles_t5<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<DP>::BYTES));
-    // An SM that runs a block of the row kernel takes one of these beside it only if both want it set up alike.
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_tiles_t5<DP>, cudaFuncAttributePreferredSharedMemoryCarveout,
-                                      cudaSharedmemCarveoutMaxShared));
+    for (auto* kernel : {k_kv_tiles_t5<DP, false>, k_kv_tiles_t5<DP, true>}) {
+        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, KpSmem<DP>::BYTES));
+        // An SM that runs a block of the row kernel takes one of these beside it only if both want it set up alike.
+        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+    }
     return JPI_OK;
 }
 
-// What the tiles would make of a side: row tiles over all caches and KV heads, and key blocks of each.
+// What the tiles would make of a side: row tiles over all runs or requests and KV heads, and key blocks of each.
 struct TileWork {
     bool fit = false;
     long long tiles = 0, blocks = 0, nb = 0;
@@ -623,6 +665,18 @@ TileWork work_of(const jpi_kv_handle* h, const KvCall& c, bool own) {
     return w;
 }
 
+// Key blocks' time that s splits of each of `blocks` tiles take with `rest` of other work to share the SMs with.
+long long tiles_time(const jpi_kv_handle* h, const TileWork& w, long long s, long long rest) {
+    const long long u = (w.nb + s - 1) / s + KP_FIXED;
+    return std::max((w.blocks * s + h->num_sms - 1) / h->num_sms * u, (w.blocks * s * u + rest) / h->num_sms);
+}
+// What a result in `parts` parts costs beside one written by its tiles, in the same unit: rows of 32 bits to the
+// workspace, the combine's launch, and the rows read back (about 4 MB in a key block's time). One part and two of the 16
+// chunks of 51 tokens over prefixes of 816 keys: 23 and 26 us.
+long long join_time(const KvCall& c, long long parts) {
+    return 7 + parts * ((long long)c.batch * c.tokens * c.H * c.D * 4 >> 10) / 3900;
+}
+
 }  // namespace
 
 jpi_status kv_tiles_prepare(jpi_kv_handle* h) {
@@ -630,59 +684,82 @@ jpi_status kv_tiles_prepare(jpi_kv_handle* h) {
     return h->D <= 64 ? prepare_dim<64>() : h->D <= 128 ? prepare_dim<128>() : prepare_dim<256>();
 }
 
-void kv_tiles_plan(const jpi_kv_handle* h, const KvCall& c, long long room, int splits[2]) {
+void kv_tiles_plan(const jpi_kv_handle* h, const KvCall& c, long long room, KvTilesPlan* plan) {
     const TileWork p = work_of(h, c, false), o = work_of(h, c, true);
-    splits[0] = splits[1] = 0;
-    // The side of more key blocks is split so that the longest block, or the waves of them, end first; a block starts and ends
-    // in about KP_FIXED key blocks' time. The other side is split to blocks no longer than those.
+    *plan = KvTilesPlan();
+    auto splits_most = [&](const TileWork& w) { return std::min({w.nb, room, std::max(1ll, 2ll * h->num_sms / w.blocks)}); };
+    // The side of more work is split so that its blocks, or the waves of them, end first; the other to blocks no longer.
     const bool own_first = o.fit && (!p.fit || o.blocks * o.nb > p.blocks * p.nb);
     const TileWork &a = own_first ? o : p, &b = own_first ? p : o;
     if (!a.fit) return;
-    const long long most = std::min({a.nb, room, std::max(1ll, 2ll * h->num_sms / a.blocks)});
-    long long best = 1, best_time = 0, unit = a.nb + KP_FIXED;
-    for (long long s = 1; s <= most; ++s) {
-        const long long u = (a.nb + s - 1) / s + KP_FIXED;
-        const long long rest = b.fit ? b.blocks * (std::min(b.nb, u - KP_FIXED) + KP_FIXED) * ((b.nb + u - KP_FIXED - 1) / (u - KP_FIXED)) : 0;
-        const long long time = std::max((a.blocks * s + h->num_sms - 1) / h->num_sms * u, (a.blocks * s * u + rest) / h->num_sms);
-        if (s == 1 || time < best_time) {
+    long long best = 1, best_time = -1, best_b = 0;
+    for (long long s = 1; s <= splits_most(a); ++s) {
+        const long long u = (a.nb + s - 1) / s;
+        const long long sb = b.fit ? std::min(room, (b.nb + u - 1) / u) : 0;
+        const long long rest = b.fit ? b.blocks * sb * ((b.nb + sb - 1) / sb + KP_FIXED) : 0;
+        const bool more = c.prefix.rows > 0 && c.own.rows > 0;   // parts of the other side, tiles or not
+        const long long time = tiles_time(h, a, s, rest) + (s + sb + more > 1 ? join_time(c, s + std::max<long long>(sb, more)) : 0);
+        if (best_time < 0 || time < best_time) {
             best = s;
             best_time = time;
-            unit = u;
+            best_b = sb;
         }
     }
-    splits[own_first] = (int)best;
-    if (b.fit) splits[!own_first] = (int)std::max(1ll, std::min(room, (b.nb + unit - KP_FIXED - 1) / (unit - KP_FIXED)));
+    plan->splits[own_first] = (int)best;
+    plan->splits[!own_first] = (int)best_b;
+    // Both sides by the requests' tiles, where that is estimated to end earlier: no tile is shared between requests, but
+    // a single split needs no combine.
+    if (p.fit && o.fit) {
+        TileWork w = o;
+        w.nb += p.nb;
+        for (long long s = 1; s <= splits_most(w); ++s) {
+            const long long time = tiles_time(h, w, s, 0) + (s > 1 ? join_time(c, s) : 0);
+            if (time <= best_time) {
+                best_time = time;
+                plan->both = true;
+                plan->splits[0] = 0;
+                plan->splits[1] = (int)s;
+            }
+        }
+    }
 }
 
-jpi_status launch_kv_tiles_t5(jpi_kv_handle* h, const KvCall& c, const int splits[2], const int part0[2], float* po, float2* pml,
-                              int parts, bool early, cudaStream_t st) {
+jpi_status launch_kv_tiles_t5(jpi_kv_handle* h, const KvCall& c, const KvTilesPlan& plan, const int part0[2], float* po,
+                              float2* pml, int parts, void* out, float* lse, bool early, cudaStream_t st) {
     TileArgs a = {};
     TileMaps maps = {};
     a.c = c;
     a.c2 = KR_LOG2E * c.scale;
+    a.both = plan.both;
+    a.by_run = KvDiv((uint32_t)(c.batch / c.groups));
     a.po = po;
     a.pml = pml;
     a.parts = parts;
     a.rows = (long long)c.batch * c.tokens * c.H;
+    a.out = parts == 1 ? static_cast<__nv_bfloat16*>(out) : nullptr;
+    a.lse = lse;
     a.err = h->dev_err;
     for (int i = 0; i < 2; ++i) {
-        if (splits[i] == 0) continue;
-        const TileWork w = work_of(h, c, i == 1);
+        if (plan.splits[i] > 0) {
+            const TileWork w = work_of(h, c, i == 1);
+            TileSide& d = a.side[i];
+            d.splits = plan.splits[i];
+            d.tiles = (int)w.tiles;
+            d.part0 = part0[i];
+            d.blocks = (uint32_t)(w.blocks * d.splits);
+            d.by_splits = KvDiv((uint32_t)d.splits);
+            d.by_tiles = KvDiv((uint32_t)d.tiles);
+        } else if (!(i == 0 && plan.both)) {
+            continue;
+        }
         const KvSide& s = i ? c.own : c.prefix;
-        TileSide& d = a.side[i];
-        d.splits = splits[i];
-        d.tiles = (int)w.tiles;
-        d.part0 = part0[i];
-        d.blocks = (uint32_t)(w.blocks * splits[i]);
-        d.by_splits = KvDiv((uint32_t)d.splits);
-        d.by_tiles = KvDiv((uint32_t)d.tiles);
         KvMapDims m;
         if (!kv_map_dims(s, c.K, c.D, i ? c.batch : c.groups, &m) || !kv_make_map(m, s.k, c.D, KP_KEYS, &maps.k[i]) ||
             !kv_make_map(m, s.v, c.D, KP_KEYS, &maps.v[i])) {
             set_error("cuTensorMapEncodeTiled refused the %s", i ? "own rows" : "prefix");
             return JPI_ERR_CUDA;
         }
-        d.at = make_int3(m.at_head, m.at_row, m.at_cache);
+        a.at[i] = make_int3(m.at_head, m.at_row, m.at_cache);
     }
     return c.D <= 64 ? launch_dim<64>(a, maps, early, st) : c.D <= 128 ? launch_dim<128>(a, maps, early, st) : launch_dim<256>(a, maps, early, st);
 }
