@@ -115,7 +115,9 @@ typedef struct jpi_weights {
 /*
  * Create a handle: validates `cfg`, allocates every persistent device buffer (sized by the
  * maxima), packs the weights (bf16 rounding, tile layout for the bulk tensor copies) and
- * returns the handle in *out. This is the only call that allocates device memory.
+ * returns the handle in *out. This is the only call that allocates device memory, but for the first of
+ * jpi_share_prefix, jpi_weigh_prefix, jpi_evict_prefix and jpi_append_prefix on a handle, which
+ * allocates what those share.
  * Ownership: the weights are copied; the caller may free its buffers when the call returns.
  * Synchronous. Errors: INVALID_ARG (null pointer, bad dims), UNSUPPORTED (dims the kernels
  * do not tile), OOM, CUDA.
@@ -164,6 +166,41 @@ JPI_API jpi_status jpi_prefix_kv_ptr(jpi_handle* h, int layer, void** k, void** 
 JPI_API jpi_status jpi_commit_prefix(jpi_handle* h, int batch, int prefix_len);
 
 /*
+ * Operations on the stored prefix, over the KV-cache operators of jpi_kv.h (the paper stores, hands over and
+ * reads the cache, App. A; these are no part of it). The calling thread's current device must be the
+ * handle's (else JPI_ERR_INVALID_ARG); not for handles created with JPI_BATCH_INVARIANT=1
+ * (JPI_ERR_UNSUPPORTED: their kernels are split by the whole call).
+ *
+ * jpi_share_prefix: from now on each stored prefix serves `requests` consecutive requests of a call
+ *   (several action chunks drawn from one observation): a call's batch is requests x the prefix's batch,
+ *   at most max_batch, and attention reads each prefix once for all of them. 1: one request a prefix,
+ *   the default. Calls that set or commit a prefix keep it.
+ * jpi_weigh_prefix: one expert evaluation at flow time t (arguments as in jpi_expert_forward; its velocity is
+ *   not returned) that adds up the attention weight each prefix key receives from all suffix tokens and heads of
+ *   the requests that share it: w = decay w + weight, device fp32 [n_layers][prefix batch][prefix_len];
+ *   decay 0 does not read w.
+ * jpi_evict_prefix: keeps `keep` tokens of every stored prefix, layer by layer those with the largest w (as
+ *   jpi_kv_evict: the first `sink`, the last `recent`, the best of the others, in their order), in
+ *   place, and makes the shorter prefix current. The suffix tokens keep their rotary positions (those
+ *   after the whole prefix). w is moved with the keys, [n_layers][batch][keep] at the old strides.
+ *   kept: device int [n_layers][batch][keep], the tokens that stay, or NULL.
+ * jpi_append_prefix: `tokens` further prefix tokens behind the stored ones, prefix_len + tokens <= max_prefix:
+ *   k_layers[l], v_layers[l]: device [batch][tokens][D] in the store's type, keys without position code: they are
+ *   coded for the positions that follow (rope_base as the expert's own tokens), and the suffix tokens' positions
+ *   move on with them.
+ * jpi_commit_prefix_at: jpi_commit_prefix, with the suffix tokens' rotary positions starting at `position`
+ *   (prefix_len .. max_prefix) instead of prefix_len, for a store that was cut outside these calls.
+ */
+JPI_API jpi_status jpi_share_prefix(jpi_handle* h, int requests);
+JPI_API jpi_status jpi_weigh_prefix(jpi_handle* h, const float* state, const float* x_t, float t, int batch,
+                                    int chunk, float decay, float* w, void* stream);
+JPI_API jpi_status jpi_evict_prefix(jpi_handle* h, float* w, int keep, int sink, int recent, int* kept,
+                                    void* stream);
+JPI_API jpi_status jpi_append_prefix(jpi_handle* h, const void* const* k_layers, const void* const* v_layers,
+                                     int tokens, void* stream);
+JPI_API jpi_status jpi_commit_prefix_at(jpi_handle* h, int batch, int prefix_len, int position);
+
+/*
  * Correction items (Sec. 4.1 "Foresight-Aligned Asynchronous Correction", App. B, App. C Alg. 1):
  * the future correction module's prediction of the compressed VLM final-layer state at
  * t + Delta, T' tokens of width d_AE, is given to the action expert as future environment
@@ -190,8 +227,8 @@ JPI_API jpi_status jpi_set_correction(jpi_handle* h, const float* items, int bat
  *   state:       device fp32 [batch][S_d]
  *   noise:       device fp32 [batch][chunk][A]
  *   out_actions: device fp32 [batch][chunk][A] (may alias noise)
- *   batch must equal the batch of the last jpi_set_prefix_kv/jpi_commit_prefix (and of the
- *   last jpi_set_correction while items are set); 1 <= chunk <= max_chunk;
+ *   batch must equal the batch of the last jpi_set_prefix_kv/jpi_commit_prefix (times the
+ *   requests of jpi_share_prefix, and that of the last jpi_set_correction while items are set); 1 <= chunk <= max_chunk;
  *   1 <= num_steps <= max_steps.
  * The first call for a (batch, chunk, num_steps, prefix_len, num_items) shape captures the whole
  * unrolled N-step loop as one CUDA graph (Sec. 4.3: graph reuse and flow unrolling) and every

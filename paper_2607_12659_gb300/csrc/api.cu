@@ -8,6 +8,7 @@
 
 #include "jpi_internal.h"
 #include "tc_path.h"
+#include "kv/kv_expert.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -18,8 +19,25 @@
 
 namespace jpi {
 
+// Graphs of one way to read the prefix (requests that share it, rotary positions that start behind it).
+struct GraphSet {
+    std::map<GraphKey, cudaGraphExec_t> graphs;
+    std::map<GraphKey, int> kernels;
+};
+
+// Every handle is one of these: with what the calls on a stored prefix add to it.
+struct PrefixHandle : jpi_handle {
+    int share = 1;              // requests a prefix serves (jpi_share_prefix)
+    int shift = 0;              // rotary positions of the suffix start at cur_prefix + shift
+    ExpertKv kv;                // allocated by the first of those calls
+    float* weigh = nullptr;     // while jpi_weigh_prefix enqueues its evaluation: where the weights go
+    float decay = 0.f;
+    std::map<std::pair<int, int>, GraphSet> sets;   // graphs by (share, shift)
+};
+
 namespace {
 thread_local char g_err[1024] = "";
+PrefixHandle* ext(jpi_handle* h) { return static_cast<PrefixHandle*>(h); }
 }
 
 void set_error(const char* fmt, ...) {
@@ -280,14 +298,15 @@ void free_handle(jpi_handle* h) {
     if (!h) return;
     cudaSetDevice(h->device);
     cudaDeviceSynchronize();
-    for (auto& kv : h->graphs) cudaGraphExecDestroy(kv.second);
-    h->graphs.clear();
+    for (auto& set : ext(h)->sets)
+        for (auto& kv : set.second.graphs) cudaGraphExecDestroy(kv.second);
+    expert_kv_destroy(&ext(h)->kv);
     if (h->cap_stream) cudaStreamDestroy(h->cap_stream);
     tc_release(h);
     for (void* p : h->allocations) cudaFree(p);
     h->allocations.clear();
     cudaGetLastError();
-    delete h;
+    delete ext(h);
 }
 
 // The whole unrolled denoise: time conditioning for every step time, then N Euler steps.
@@ -301,8 +320,9 @@ jpi_status enqueue_denoise(jpi_handle* h, int B, int C, int N, cudaStream_t st) 
 
 jpi_status get_graph(jpi_handle* h, int B, int C, int N, cudaGraphExec_t* out) {
     const GraphKey key{B, C, N, h->cur_prefix, h->n_corr};
-    auto it = h->graphs.find(key);
-    if (it != h->graphs.end()) {
+    GraphSet& set = ext(h)->sets[{ext(h)->share, ext(h)->shift}];
+    auto it = set.graphs.find(key);
+    if (it != set.graphs.end()) {
         *out = it->second;
         return JPI_OK;
     }
@@ -332,24 +352,37 @@ jpi_status get_graph(jpi_handle* h, int B, int C, int N, cudaGraphExec_t* out) {
             }
     }
     cudaGraphDestroy(g);
-    h->graph_kernels[key] = kernels;
-    h->graphs[key] = ex;
+    set.kernels[key] = kernels;
+    set.graphs[key] = ex;
     *out = ex;
     return JPI_OK;
 }
 
 }  // namespace
 
+// One sub-step of a layer (ops 2..6), the attention over a shared or weighed prefix by the KV-cache operators.
+static jpi_status launch_op(jpi_handle* h, int op, int l, int step, int B, int C, cudaStream_t st) {
+    PrefixHandle* e = ext(h);
+    if (op == 3 && (e->share > 1 || e->weigh))
+        return expert_kv_attention(h, e->kv, l, B, C, e->share,
+                                   e->weigh ? e->weigh + (size_t)l * h->cur_batch * h->cur_prefix : nullptr, e->decay, st);
+    return h->tc ? tc_launch_op(h, op, l, step, B, C, st) : launch_op_simt(h, op, l, step, B, C, st);
+}
+
 // One Euler step (or one forward): token embedding, L layers, final norm + projection.
 jpi_status enqueue_step(jpi_handle* h, int step, int B, int C, float delta, float* v_out,
                         cudaStream_t st) {
+    PrefixHandle* e = ext(h);
+    if (step == 0 && (e->share > 1 || e->weigh)) JPI_TRY(expert_kv_fill(h, e->kv, B, C, e->share, st));
     JPI_TRY(launch_embed(h, step, B, C, h->x, st));
-    for (int l = 0; l < h->L; ++l) {
-        if (h->tc)
-            JPI_TRY(tc_launch_layer(h, l, step, B, C, st));
-        else
-            JPI_TRY(launch_layer_simt(h, l, step, B, C, st));
-    }
+    // The kernels take suffix row i's rotary position as cur_prefix + i: a table that starts `shift` positions further on.
+    float2* const rope = h->rope_tab;
+    if (rope) h->rope_tab = rope + (size_t)e->shift * (h->D / 2);
+    jpi_status s = JPI_OK;
+    for (int l = 0; l < h->L && s == JPI_OK; ++l)
+        for (int op = 2; op <= 6 && s == JPI_OK; ++op) s = launch_op(h, op, l, step, B, C, st);
+    h->rope_tab = rope;
+    JPI_TRY(s);
     return launch_final(h, step, B, C, delta, v_out ? nullptr : h->x, v_out, st);
 }
 
@@ -360,8 +393,9 @@ jpi_status check_call(jpi_handle* h, int B, int C, int N) {
         return fail(JPI_ERR_SHAPE, "batch %d / chunk %d / steps %d exceed the maxima %d / %d / %d",
                     B, C, N, h->maxB, h->maxC, h->maxN);
     if (!h->prefix_ready) return fail(JPI_ERR_NOT_READY, "no prefix KV has been set");
-    if (B != h->cur_batch)
-        return fail(JPI_ERR_SHAPE, "batch %d differs from the prefix KV's batch %d", B, h->cur_batch);
+    if (B != h->cur_batch * ext(h)->share)
+        return fail(JPI_ERR_SHAPE, "batch %d differs from the prefix KV's batch %d%s", B, h->cur_batch * ext(h)->share,
+                    ext(h)->share > 1 ? " (with the requests that share each prefix)" : "");
     if (h->n_corr > 0 && B != h->corr_batch)
         return fail(JPI_ERR_SHAPE, "batch %d differs from the correction items' batch %d", B, h->corr_batch);
     return JPI_OK;
@@ -381,7 +415,7 @@ JPI_API jpi_status jpi_expert_create(const jpi_config* cfg, const jpi_weights* w
     *out = nullptr;
     JPI_TRY(check_config(cfg));
     if (!w) return fail(JPI_ERR_INVALID_ARG, "weights are NULL");
-    jpi_handle* h = new (std::nothrow) jpi_handle();
+    jpi_handle* h = new (std::nothrow) PrefixHandle();
     if (!h) return fail(JPI_ERR_OOM, "host allocation failed");
     h->cfg = *cfg;
     h->bf16 = cfg->precision == JPI_BF16;
@@ -395,7 +429,7 @@ JPI_API jpi_status jpi_expert_create(const jpi_config* cfg, const jpi_weights* w
     jpi_status s = JPI_OK;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e != cudaSuccess) {
-        delete h;
+        delete ext(h);
         return fail(JPI_ERR_CUDA, "no CUDA device: %s", cudaGetErrorString(e));
     }
     h->tc = h->bf16 && tc_supported(h);
@@ -442,6 +476,7 @@ JPI_API jpi_status jpi_set_prefix_kv(jpi_handle* h, const void* const* k_layers,
     JPI_TRY(launch_load_prefix(h, k_layers, v_layers, kv_is_fp32, batch, prefix_len, st));
     h->cur_batch = batch;
     h->cur_prefix = prefix_len;
+    ext(h)->shift = 0;
     h->prefix_ready = true;
     return JPI_OK;
 }
@@ -465,7 +500,86 @@ JPI_API jpi_status jpi_commit_prefix(jpi_handle* h, int batch, int prefix_len) {
     if (batch > h->maxB || prefix_len > h->maxP) return fail(JPI_ERR_SHAPE, "batch/prefix exceed the maxima");
     h->cur_batch = batch;
     h->cur_prefix = prefix_len;
+    ext(h)->shift = 0;
     h->prefix_ready = true;
+    return JPI_OK;
+}
+
+JPI_API jpi_status jpi_commit_prefix_at(jpi_handle* h, int batch, int prefix_len, int position) {
+    clear_error();
+    if (!h) return fail(JPI_ERR_INVALID_ARG, "handle is NULL");
+    if (position < prefix_len || position > h->maxP)
+        return fail(JPI_ERR_SHAPE, "position %d must be in prefix_len..max_prefix (%d..%d)", position, prefix_len, h->maxP);
+    JPI_TRY(jpi_commit_prefix(h, batch, prefix_len));
+    ext(h)->shift = position - prefix_len;
+    return JPI_OK;
+}
+
+// What the calls on a stored prefix share: the right device, a handle whose kernels may be split by the call, and their
+// buffers, allocated by the first.
+static jpi_status prefix_ops(jpi_handle* h) {
+    if (!h) return fail(JPI_ERR_INVALID_ARG, "handle is NULL");
+    int dev = -1;
+    JPI_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev != h->device) return fail(JPI_ERR_INVALID_ARG, "the current device is %d, the handle's %d", dev, h->device);
+    if (h->batch_invariant) return fail(JPI_ERR_UNSUPPORTED, "not for a batch-invariant handle (JPI_BATCH_INVARIANT=1)");
+    return ext(h)->kv.kv ? JPI_OK : expert_kv_create(h, &ext(h)->kv);
+}
+
+JPI_API jpi_status jpi_share_prefix(jpi_handle* h, int requests) {
+    clear_error();
+    if (!h) return fail(JPI_ERR_INVALID_ARG, "handle is NULL");
+    if (requests < 1) return fail(JPI_ERR_INVALID_ARG, "requests must be >= 1");
+    if (requests > h->maxB) return fail(JPI_ERR_SHAPE, "requests %d exceed max_batch %d", requests, h->maxB);
+    if (requests > 1) JPI_TRY(prefix_ops(h));
+    ext(h)->share = requests;
+    return JPI_OK;
+}
+
+JPI_API jpi_status jpi_weigh_prefix(jpi_handle* h, const float* state, const float* x_t, float t, int batch, int chunk,
+                                    float decay, float* w, void* stream) {
+    clear_error();
+    JPI_TRY(check_call(h, batch, chunk, 1));
+    if (!state || !x_t || !w) return fail(JPI_ERR_INVALID_ARG, "NULL input or output");
+    if (!(t >= 0.f)) return fail(JPI_ERR_INVALID_ARG, "t must be >= 0");
+    if (!(decay >= 0.f) || std::isinf(decay)) return fail(JPI_ERR_INVALID_ARG, "decay must be >= 0 and finite");
+    JPI_TRY(prefix_ops(h));
+    ext(h)->weigh = w;
+    ext(h)->decay = decay;
+    const jpi_status s = jpi_expert_forward(h, state, x_t, t, batch, chunk, h->out, nullptr, stream);
+    ext(h)->weigh = nullptr;
+    return s;
+}
+
+JPI_API jpi_status jpi_evict_prefix(jpi_handle* h, float* w, int keep, int sink, int recent, int* kept, void* stream) {
+    clear_error();
+    if (!h || !w) return fail(JPI_ERR_INVALID_ARG, "NULL argument");
+    if (!h->prefix_ready) return fail(JPI_ERR_NOT_READY, "no prefix KV has been set");
+    if (keep < 1 || sink < 0 || recent < 0 || (long long)sink + recent > keep)
+        return fail(JPI_ERR_INVALID_ARG, "keep %d must be >= 1 and hold sink %d and recent %d", keep, sink, recent);
+    if (keep > h->cur_prefix) return fail(JPI_ERR_SHAPE, "keep %d exceeds the prefix's %d tokens", keep, h->cur_prefix);
+    JPI_TRY(prefix_ops(h));
+    JPI_TRY(expert_kv_evict(h, ext(h)->kv, w, keep, sink, recent, kept, (cudaStream_t)stream));
+    ext(h)->shift += h->cur_prefix - keep;
+    h->cur_prefix = keep;
+    return JPI_OK;
+}
+
+JPI_API jpi_status jpi_append_prefix(jpi_handle* h, const void* const* k_layers, const void* const* v_layers, int tokens,
+                                     void* stream) {
+    clear_error();
+    if (!h || !k_layers || !v_layers) return fail(JPI_ERR_INVALID_ARG, "NULL argument");
+    if (!h->prefix_ready) return fail(JPI_ERR_NOT_READY, "no prefix KV has been set");
+    if (tokens < 1) return fail(JPI_ERR_INVALID_ARG, "tokens must be >= 1");
+    if (h->cfg.rope_base > 0.f && h->cfg.rope_base < 1.f) return fail(JPI_ERR_UNSUPPORTED, "rope_base must be 0 or at least 1");
+    if ((long long)h->cur_prefix + ext(h)->shift + tokens > h->maxP)
+        return fail(JPI_ERR_SHAPE, "%d tokens behind position %d exceed max_prefix %d", tokens, h->cur_prefix + ext(h)->shift, h->maxP);
+    for (int l = 0; l < h->L; ++l)
+        if (!k_layers[l] || !v_layers[l] || ((uintptr_t)k_layers[l] & 15) || ((uintptr_t)v_layers[l] & 15))
+            return fail(JPI_ERR_INVALID_ARG, "layer %d K or V is NULL or not 16-byte aligned", l);
+    JPI_TRY(prefix_ops(h));
+    JPI_TRY(expert_kv_append(h, ext(h)->kv, k_layers, v_layers, tokens, h->cur_prefix + ext(h)->shift, (cudaStream_t)stream));
+    h->cur_prefix += tokens;
     return JPI_OK;
 }
 
@@ -563,7 +677,7 @@ JPI_API jpi_status jpi_graph_kernel_count(jpi_handle* h, int batch, int chunk, i
     if (!count) return fail(JPI_ERR_INVALID_ARG, "count is NULL");
     cudaGraphExec_t ex = nullptr;
     JPI_TRY(get_graph(h, batch, chunk, num_steps, &ex));
-    *count = h->graph_kernels[GraphKey{batch, chunk, num_steps, h->cur_prefix, h->n_corr}];
+    *count = ext(h)->sets[{ext(h)->share, ext(h)->shift}].kernels[GraphKey{batch, chunk, num_steps, h->cur_prefix, h->n_corr}];
     return JPI_OK;
 }
 
@@ -585,10 +699,8 @@ JPI_API jpi_status jpi_profile_op(jpi_handle* h, int op, int layer, int batch, i
                 JPI_TRY(launch_final(h, 0, batch, chunk, 0.f, nullptr, h->out, st));
                 break;
             default:
-                if (h->tc)
-                    JPI_TRY(tc_launch_op(h, op, layer, 0, batch, chunk, st));
-                else
-                    JPI_TRY(launch_op_simt(h, op, layer, 0, batch, chunk, st));
+                if (op == 3 && r == 0 && ext(h)->share > 1) JPI_TRY(expert_kv_fill(h, ext(h)->kv, batch, chunk, ext(h)->share, st));
+                JPI_TRY(launch_op(h, op, layer, 0, batch, chunk, st));
         }
     }
     return JPI_OK;

@@ -16,6 +16,7 @@ struct jpi_kv_handle {
     void* ws = nullptr;          // partial outputs and statistics of jpi_kv_attend
     size_t ws_bytes = 0;
     int* dev_err = nullptr;
+    bool pdl = true;             // kernels of one call may start before the one before them has finished
     size_t device_bytes = 0;
     std::vector<void*> allocations;
 };

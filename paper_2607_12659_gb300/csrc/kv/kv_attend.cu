@@ -813,7 +813,7 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
         }
     }
     const int part0[2] = {0, a.p.splits};
-    if (beside) JPI_TRY(launch_kv_tiles_t5(h, c, tiles, part0, a.po, a.pml, parts, out, lse, pieces > 0, st));
+    if (beside) JPI_TRY(launch_kv_tiles_t5(h, c, tiles, part0, a.po, a.pml, parts, out, lse, pieces > 0 && h->pdl, st));
     if (parts == 1) return JPI_OK;
     a.out = out;
     // A warp has the loads of 8 parts (16 to D = 128) in flight: warps for as many batches, to four a row, or where the
@@ -822,8 +822,8 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
     while (wpr < (a.rows <= 64 ? CB_WARPS : 4) && wpr * 8 < parts) wpr *= 2;
     const int warps = std::max(wpr, AT_WARPS);
     const long long grid = (a.rows * wpr + warps - 1) / warps;
-    return h->bf16 ? kv_start(k_kv_combine<DP, __nv_bfloat16>, grid, 32 * warps, 0, true, st, a, wpr)
-                   : kv_start(k_kv_combine<DP, float>, grid, 32 * warps, 0, true, st, a, wpr);
+    return h->bf16 ? kv_start(k_kv_combine<DP, __nv_bfloat16>, grid, 32 * warps, 0, h->pdl, st, a, wpr)
+                   : kv_start(k_kv_combine<DP, float>, grid, 32 * warps, 0, h->pdl, st, a, wpr);
 }
 
 template <int DP>

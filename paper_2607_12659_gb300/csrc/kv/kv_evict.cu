@@ -303,7 +303,7 @@ jpi_status launch_kv_evict(const jpi_kv_handle* h, const jpi_kv_cache& src, cons
     return kv_start(lanes == 32 ? k_kv_gather<32>
                                 : lanes == 16 ? k_kv_gather<16>
                                               : lanes == 8 ? k_kv_gather<8> : lanes == 4 ? k_kv_gather<4> : lanes == 2 ? k_kv_gather<2> : k_kv_gather<1>,
-                    dim3((unsigned)(blocks_of(lanes) / items), (unsigned)items, (unsigned)gz), GA_THREADS, 0, true, st, a);
+                    dim3((unsigned)(blocks_of(lanes) / items), (unsigned)items, (unsigned)gz), GA_THREADS, 0, h->pdl, st, a);
 }
 
 }  // namespace jpi

@@ -222,7 +222,7 @@ jpi_status launch_kv_weigh(jpi_kv_handle* h, const KvCall& c, const float* lse, 
         JPI_TRY(kv_start(!h->bf16 ? k_kv_weigh_f32
                                   : h->D <= 64 ? k_kv_weigh_mma<64> : h->D <= 128 ? k_kv_weigh_mma<128> : k_kv_weigh_mma<256>,
                          blocks, WG_THREADS, 0, false, st, a));
-    if (tiles) return launch_kv_weigh_t5(h, c, lse, decay, prefix_in, prefix_out, blocks > 0, st);
+    if (tiles) return launch_kv_weigh_t5(h, c, lse, decay, prefix_in, prefix_out, blocks > 0 && h->pdl, st);
     return JPI_OK;
 }
 

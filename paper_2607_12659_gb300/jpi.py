@@ -63,6 +63,11 @@ _SIGS = {
     "jpi_set_prefix_kv": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
     "jpi_prefix_kv_ptr": [c_void_p, c_int, POINTER(c_void_p), POINTER(c_void_p), POINTER(c_longlong)],
     "jpi_commit_prefix": [c_void_p, c_int, c_int],
+    "jpi_share_prefix": [c_void_p, c_int],
+    "jpi_weigh_prefix": [c_void_p, c_void_p, c_void_p, c_float, c_int, c_int, c_float, c_void_p, c_void_p],
+    "jpi_evict_prefix": [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p],
+    "jpi_append_prefix": [c_void_p, c_void_p, c_void_p, c_int, c_void_p],
+    "jpi_commit_prefix_at": [c_void_p, c_int, c_int, c_int],
     "jpi_set_correction": [c_void_p, c_void_p, c_int, c_int, c_void_p],
     "jpi_denoise": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p],
     "jpi_denoise_host": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p],
@@ -217,6 +222,30 @@ def jpi_commit_prefix(h, batch, prefix_len):
     _check(load().jpi_commit_prefix(h, batch, prefix_len), "jpi_commit_prefix")
 
 
+def jpi_commit_prefix_at(h, batch, prefix_len, position):
+    _check(load().jpi_commit_prefix_at(h, batch, prefix_len, position), "jpi_commit_prefix_at")
+
+
+def jpi_share_prefix(h, requests):
+    _check(load().jpi_share_prefix(h, requests), "jpi_share_prefix")
+
+
+def jpi_weigh_prefix(h, state, x_t, t, batch, chunk, decay, w, stream=None):
+    _check(load().jpi_weigh_prefix(h, _ptr(state), _ptr(x_t), float(t), batch, chunk, float(decay), _ptr(w),
+                                   _stream(stream)), "jpi_weigh_prefix")
+
+
+def jpi_evict_prefix(h, w, keep, sink, recent, kept=None, stream=None):
+    _check(load().jpi_evict_prefix(h, _ptr(w), keep, sink, recent, _ptr(kept), _stream(stream)), "jpi_evict_prefix")
+
+
+def jpi_append_prefix(h, k_layers, v_layers, tokens, stream=None):
+    L = len(k_layers)
+    ka = (c_void_p * L)(*[_ptr(k) for k in k_layers])
+    va = (c_void_p * L)(*[_ptr(v) for v in v_layers])
+    _check(load().jpi_append_prefix(h, ka, va, tokens, _stream(stream)), "jpi_append_prefix")
+
+
 def jpi_set_correction(h, items, batch, num_items, stream=None):
     _check(load().jpi_set_correction(h, _ptr(items), batch, num_items, _stream(stream)),
            "jpi_set_correction")
@@ -332,6 +361,47 @@ class Expert:
             assert k.dtype == torch.bfloat16
         jpi_set_prefix_kv(self.handle, [k[l] for l in range(L)], [v[l] for l in range(L)], B, P,
                           fp32, stream)
+        self._kv_keepalive = (k, v)
+
+    def share_prefix(self, requests: int):
+        """Each stored prefix serves `requests` consecutive requests of a call (1: one each)."""
+        jpi_share_prefix(self.handle, requests)
+
+    def weigh_prefix(self, state, x_t, t, w, decay=1.0, stream=None):
+        """w [L][prefix batch][prefix length] (CUDA float32) = decay w + the attention weight each prefix key receives in
+        one expert evaluation."""
+        import torch
+        assert w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.shape[0] == self.dims.n_layers
+        B, C, _ = x_t.shape
+        with OnStream(stream, x_t.device) as on:
+            on.reads(state, x_t, w)
+        jpi_weigh_prefix(self.handle, state, x_t, t, B, C, decay, w, stream)
+        return w
+
+    def evict_prefix(self, w, keep, sink=0, recent=0, stream=None):
+        """Cuts every stored prefix to `keep` tokens by the weights w (as weigh_prefix gives them; moved with the keys).
+        Returns the tokens that stay, int32 [L][prefix batch][keep]."""
+        import torch
+        assert w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.dim() == 3 and w.shape[0] == self.dims.n_layers
+        with OnStream(stream, w.device) as on:
+            on.reads(w)
+            kept = torch.empty((*w.shape[:2], max(keep, 0)), dtype=torch.int32, device=w.device)
+            on.returns(kept)
+        jpi_evict_prefix(self.handle, w, keep, sink, recent, kept, stream)
+        return kept
+
+    def append_prefix(self, k, v, stream=None):
+        """Further prefix tokens behind the stored ones: k, v CUDA tensors [L][B][T][D] in the store's type, keys without
+        position code."""
+        import torch
+        want = torch.float32 if self.cfg.precision == JPI_FP32 else torch.bfloat16
+        assert k.is_cuda and v.is_cuda and k.shape == v.shape and k.dtype == want and v.dtype == want
+        assert k.shape[0] == self.dims.n_layers and k.shape[3] == self.dims.head_dim
+        with OnStream(stream, k.device) as on:
+            on.reads(k, v)
+            k = k.contiguous()
+            v = v.contiguous()
+        jpi_append_prefix(self.handle, list(k), list(v), k.shape[2], stream)
         self._kv_keepalive = (k, v)
 
     def set_correction(self, items, stream=None):

@@ -87,6 +87,14 @@ def test_null_handles_are_refused(lib):
     assert lib.jpi_kv_memory_usage(None, ctypes.byref(b)) == -1
 
 
+def test_null_experts_are_refused_by_the_calls_on_a_stored_prefix(lib):
+    assert lib.jpi_share_prefix(None, 2) == -1
+    assert lib.jpi_weigh_prefix(None, None, None, 0.0, 1, 1, 1.0, None, None) == -1
+    assert lib.jpi_evict_prefix(None, None, 1, 0, 0, None, None) == -1
+    assert lib.jpi_append_prefix(None, None, None, 1, None) == -1
+    assert lib.jpi_commit_prefix_at(None, 1, 1, 1) == -1
+
+
 # ------------------------------------------------------------------ pins of the oracle
 
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
