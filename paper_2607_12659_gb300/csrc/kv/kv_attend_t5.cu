@@ -93,7 +93,7 @@ struct KpSmem {
     static constexpr int XM_OFF = RING;                     // [groups][2 blocks][2 key halves][128 rows]
     static constexpr int ML_OFF = XM_OFF + NG * 4 * KP_ROWS * 4;    // [groups][128 rows] (m, l)
     static constexpr int BAR_OFF = ML_OFF + NG * KP_ROWS * 8;
-    static constexpr int BYTES = BAR_OFF + 8 * (3 * NB + NG + 1 + 4 * NS + 2);
+    static constexpr int BYTES = BAR_OFF + 8 * (3 * NB + NG + 2 + 4 * NS + 2);
     // The query rows' way to a row per thread: 4 KB a warp in the last QS value slots, which are filled after it.
     static constexpr int TURN = KVBYTES / 4096, QS = DP == 256 ? 1 : 2;
     static_assert(QS < NS && TURN * QS >= (DP == 64 ? 4 : 8), "the query rows fit those slots");
@@ -147,8 +147,9 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
     uint64_t* sfull = bars;            // NB: score buffer ready
     uint64_t* pfull = sfull + NB;      // NB: probabilities written over the score buffer
     uint64_t* odone = pfull + NB;      // NB: P V of the block in score buffer b done
-    uint64_t* gdone = odone + NB;      // NG: P V of the group's block done
-    uint64_t* qready = gdone + NG;     // the query rows are in TMEM
+    uint64_t* gdone = odone + NB;      // NG: P V of the group's block done, of a block that another one of the group follows
+    uint64_t* alldone = gdone + NG;    // every P V done
+    uint64_t* qready = alldone + 1;    // the query rows are in TMEM
     uint64_t* kfull = qready + 1;      // NS each
     uint64_t* vfull = kfull + NS;
     uint64_t* kempty = vfull + NS;
@@ -210,6 +211,7 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
             ptx::mbar_init(&odone[b], 1);
         }
         for (int b = 0; b < NG; ++b) ptx::mbar_init(&gdone[b], 1);
+        ptx::mbar_init(alldone, 1);
         ptx::mbar_init(qready, 256);
         for (int s = 0; s < NS; ++s) {
             ptx::mbar_init(&kfull[s], 1);
@@ -328,8 +330,9 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
                 }
                 if (i + NS < nb) ptx::mma_commit(&vempty[sl]);
                 if (i + NB < nb) ptx::mma_commit(&odone[i % NB]);
-                ptx::mma_commit(&gdone[i % NG]);
+                if (i + NG < nb) ptx::mma_commit(&gdone[i % NG]);
             }
+            ptx::mma_commit(alldone);
             if (!good) *flag = DEV_TIMEOUT_MMA;
         }
     } else {
@@ -530,11 +533,9 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
         xl[half * KP_ROWS] = l;
         ptx::named_bar_sync(pair_bar, 64);
         l = xl[0] + xl[KP_ROWS];
-        // Every P V of the block is done, and with them every read of the ring.
-        for (int b = 0; b < NG; ++b) {
-            const int of = (nb - b + NG - 1) / NG;   // blocks of group b
-            if (of > 0 && good) good = ptx::mbar_wait_bounded(&gdone[b], (of - 1) & 1, KP_WAIT_NS);
-        }
+        // Every P V of the block is done, and with them every read of the ring. (The groups' own barriers cannot tell: the
+        // last scores came when up to two products of a group were still to run.)
+        if (good) good = ptx::mbar_wait_bounded(alldone, 0, KP_WAIT_NS);
         ptx::tc_fence_after();
         if (!good) *flag = DEV_TIMEOUT_MMA;
         // The groups' outputs are joined on the way: w_g = 2^((m_g - M) c).

@@ -250,6 +250,17 @@ def test_attend_many_rows_on_one_prefix(kv, H, K, D, B, T, G, P, R):
     check_attend(kv, "bf16", H, K, D, B, T, G, P, R, seed=B)
 
 
+@pytest.mark.parametrize("H,K,D,B,T,P,R", [(8, 1, 256, 64, 1, 4096, 300), (8, 1, 256, 64, 1, 16384, 512), (32, 8, 128, 48, 1, 4000, 100),
+                                            (8, 1, 64, 64, 2, 8000, 0), (8, 2, 256, 9, 16, 2100, 700)])
+def test_attend_long_prefix_many_rows(kv, H, K, D, B, T, P, R):
+    """Blocks of many keys: the last products are waited for, however far behind the scores they are."""
+    c, out, lse = check_attend(kv, "bf16", H, K, D, B, T, 1, P, R, seed=P)
+    h = kv.KV(H, K, D, max_batch=B, max_tokens=T)
+    for _ in range(10):
+        again, lse2 = h.attend(**c)
+        assert torch.equal(out, again) and torch.equal(lse, lse2), "two runs differ"
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("store", [head_major, padded])
 def test_attend_cache_layouts(kv, dtype, store):
