@@ -1,9 +1,13 @@
-"""Builds the libraries in-tree for sm_103a with nvcc (no cmake, no torch build).
+"""Builds the libraries in-tree for sm_103a with nvcc (no cmake; one small Python module uses torch's headers).
 
 ``libjpi.so``: the action expert, the future correction module (every .cu directly under csrc/)
 and the KV-cache operators (csrc/kv/). Each translation unit compiles in parallel; the objects link into one shared library
 with the CUDA runtime linked statically, so the library needs no libcuda at load time (the
 driver entry points are resolved at run time).
+
+``_kv.so``: a Python module of g++ alone (csrc/kv/kv_calls.cpp), the checks of torch tensors in front of the KV-cache
+operators. It uses the headers and libraries of the torch that is installed, and is rebuilt for another one. A failure to
+build it leaves only kv.py's KV unbuilt (reported on stderr and by ``KV_CALLS_BUILD_ERROR``).
 
 ``libjpi_prefill.so``: the LLM prefill (csrc/prefill/), its own tensor-core kernels, linked the
 same way. A failure to build it leaves only the prefill unbuilt (reported on stderr and by
@@ -27,6 +31,9 @@ KV_SRC = os.path.join(CSRC, "kv")
 PREFILL_SRC = os.path.join(CSRC, "prefill")
 PREFILL_LIB = os.path.join(PKG, "libjpi_prefill.so")
 PREFILL_BUILD_ERROR = None
+KV_CALLS_SRC = os.path.join(KV_SRC, "kv_calls.cpp")
+KV_CALLS_LIB = os.path.join(PKG, "_kv.so")
+KV_CALLS_BUILD_ERROR = None
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + [
@@ -88,6 +95,36 @@ def build_prefill(verbose: bool = False, force: bool = False) -> str:
     return PREFILL_LIB
 
 
+def build_kv_calls(verbose: bool = False, force: bool = False) -> str:
+    """Compile csrc/kv/kv_calls.cpp against this Python and its torch into _kv.so."""
+    import sysconfig
+
+    import torch
+    os.makedirs(BUILD, exist_ok=True)
+    t = os.path.dirname(torch.__file__)
+    paths = sysconfig.get_paths()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-I", os.path.join(ROOT, "include"),
+           "-isystem", os.path.join(t, "include"), "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"),
+           "-I", paths["include"], f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", KV_CALLS_SRC,
+           "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", f"-Wl,-rpath,{os.path.join(t, 'lib')}"]
+    # Built for one torch and one Python: the command and their versions are kept beside the object files.
+    stamp, made = os.path.join(BUILD, "kv_calls.txt"), " ".join([torch.__version__, sys.version.split()[0], *cmd])
+    deps = [KV_CALLS_SRC] + [os.path.join(ROOT, "include", f) for f in ("jpi.h", "jpi_kv.h")]
+    if not force and os.path.exists(KV_CALLS_LIB) and os.path.exists(stamp) and open(stamp).read() == made and all(
+            os.path.getmtime(d) <= os.path.getmtime(KV_CALLS_LIB) for d in deps):
+        return KV_CALLS_LIB
+    tmp = KV_CALLS_LIB + ".tmp"
+    r = subprocess.run(cmd + ["-o", tmp], capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for kv_calls.cpp:\n{r.stderr}")
+    if verbose and r.stderr:
+        print(r.stderr, file=sys.stderr)
+    os.replace(tmp, KV_CALLS_LIB)
+    with open(stamp, "w") as f:
+        f.write(made)
+    return KV_CALLS_LIB
+
+
 PROBE_SRC = os.path.join(CSRC, "probe", "primitives.cu")
 PROBE_BIN = os.path.join(BUILD, "primitives")
 
@@ -106,8 +143,9 @@ def build_probe(force: bool = False) -> str:
 
 
 def build(verbose: bool = False, force: bool = False) -> str:
-    """Compile every .cu directly under csrc/ and in csrc/kv/ and link libjpi.so, then the prefill library;
-    returns libjpi.so's path."""
+    """Compile every .cu directly under csrc/ and in csrc/kv/ and link libjpi.so, the module _kv.so, then the
+    prefill library; returns libjpi.so's path."""
+    global KV_CALLS_BUILD_ERROR
     os.makedirs(BUILD, exist_ok=True)
     cc = nvcc()
     srcs = sources()
@@ -123,10 +161,17 @@ def build(verbose: bool = False, force: bool = False) -> str:
             raise RuntimeError(f"nvcc failed for {os.path.basename(src)}:\n{r.stderr}")
         return r.stderr if verbose else None
 
-    with cf.ThreadPoolExecutor(max_workers=max(1, min(len(srcs), os.cpu_count() or 4))) as ex:
+    with cf.ThreadPoolExecutor(max_workers=max(1, min(len(srcs) + 1, os.cpu_count() or 4))) as ex:
+        module = ex.submit(build_kv_calls, verbose, force)
         for msg in ex.map(compile_one, zip(srcs, objs)):
             if msg:
                 print(msg, file=sys.stderr)
+        try:
+            module.result()
+            KV_CALLS_BUILD_ERROR = None
+        except (RuntimeError, OSError, ImportError) as e:
+            KV_CALLS_BUILD_ERROR = str(e)
+            print(f"warning: _kv.so not built: {e}", file=sys.stderr)
     relink = force or not os.path.exists(LIB) or any(
         os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs)
     if relink:

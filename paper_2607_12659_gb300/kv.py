@@ -120,6 +120,16 @@ def cache_of(k, v=None, layers=False) -> jpi_kv_cache:
                         k.shape[-3])
 
 
+def _checked_calls(*geometry):
+    """The module _kv and its view of a handle's geometry, with the entry points of the library that is loaded."""
+    try:
+        from . import _kv
+    except ImportError as e:
+        raise RuntimeError(f"the module _kv is not built ({e}): run `python -m paper_2607_12659_gb300.build`") from e
+    lib = load()
+    return _kv, _kv.calls(*geometry, *(ctypes.cast(getattr(lib, f"jpi_kv_{n}"), c_void_p).value for n in ("append", "attend", "weigh", "evict")))
+
+
 class KV:
     """A created handle of the KV-cache operators (jpi_kv_handle)."""
 
@@ -135,7 +145,8 @@ class KV:
         self.handle = jpi_kv_create(self.cfg, rope.c() if rope is not None else None)
         self.index = torch.cuda.current_device()
         self.device = torch.device("cuda", self.index)
-        self._torch, self._int, self._float, self._lib = torch, torch.int32, torch.float32, load()
+        self._torch, self._int, self._float = torch, torch.int32, torch.float32
+        self._kv, self._calls = _checked_calls(n_heads, n_kv_heads, head_dim, precision == "bf16", self.index)
 
     def close(self):
         if self.handle:
@@ -148,143 +159,51 @@ class KV:
         except Exception:
             pass
 
-    # The C-ABI sees addresses only: what they point to is checked here. A call for one token lasts a few
-    # microseconds on the GPU, so the checks read each property of a tensor once.
-    def _data(self, name, t, dtype):
-        if t.get_device() != self.index:
-            raise ValueError(f"{name} is on {t.device}, the handle on {self.device}")
-        if t.dtype is not dtype:
-            raise ValueError(f"{name} is {t.dtype}, not {dtype}")
-
-    def _whole(self, name, t, shape, dtype):
-        """The address of a tensor that is taken (and written) as one contiguous block."""
-        self._data(name, t, dtype)
-        if t.shape != shape:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        return t.data_ptr()
-
-    def _cache(self, name, k, v, n, layers=None):
-        self._data(name, k, self.dtype)
-        if v is not None:
-            self._data(name, v, self.dtype)
-        c = cache_of(k, v, layers is not None)      # v has k's shape
-        shape = k.shape
-        if shape[-1] != self.head_dim or shape[-2] != self.kv_heads or shape[-4] != n or (layers is not None and shape[0] != layers):
-            raise ValueError(f"{name} has shape {tuple(shape)}, not {'' if layers is None else f'[{layers}]'}[{n}][rows]"
-                             f"[{self.kv_heads}][{self.head_dim}]")
-        return c
-
-    def _tokens(self, name, t, heads):
-        """(tensor, address, token stride): new tokens [batch][tokens][heads][D], one row of `stride` elements each."""
-        self._data(name, t, self.dtype)
-        shape, s, at = t.shape, t.stride(), t.data_ptr()
-        if len(shape) != 4 or shape[2] != heads or shape[3] != self.head_dim:
-            raise ValueError(f"{name} has shape {tuple(shape)}, not [batch][tokens][{heads}][{self.head_dim}]")
-        B, T, _, D = shape
-        stride = s[1] if T > 1 else s[0] if B > 1 else heads * D
-        if s[3] != 1 or (s[2] != D and heads > 1) or (B > 1 and T > 1 and s[0] != T * s[1]) or stride < heads * D \
-                or (stride * t.element_size()) % 16 or at % 16:
-            t = t.contiguous()
-            at, stride = t.data_ptr(), heads * D
-        return t, at, stride
-
+    # The C-ABI sees addresses only: what the tensors are is checked by the module _kv (csrc/kv/kv_calls.cpp), with
+    # ValueError, before each call.
     def _on(self, stream):
         """Torch's side of a call on another stream than the current one (None: this one)."""
         return _HERE if stream is None else OnStream(stream, self.device)
 
-    def _run(self, fn, stream, args, on, reads, returns):
-        """The C call, with what it reads and returns kept by the stream that it runs on."""
+    def _call(self, fn, on, stream, args, reads, returns):
+        """The checked call; on a stream of its own, with what it reads and returns kept by it."""
+        raw = self._torch._C._cuda_getCurrentRawStream(self.index) if on is None else _stream(stream)
+        status = getattr(self._kv, fn)(self._calls, self.handle, raw, *args)
+        if status:
+            _check(status, "jpi_kv_" + fn)
         if on is not None:
             on.reads(*(t for t in reads if t is not None))
             on.returns(*returns)
-            raw = _stream(stream)
-        else:
-            raw = self._torch._C._cuda_getCurrentRawStream(self.index)
-        status = getattr(self._lib, fn)(self.handle, *args, raw)
-        if status:
-            _check(status, fn)
 
     def append(self, q, k, v, positions, rows, cache_k=None, cache_v=None, q_out=None, stream=None):
         """Codes q [B][T][H][D] and k [B][T][Hk][D] for `positions` (int32 [B][T]) and writes k and v into `rows`
         (int32 [B][T]; a row outside the cache marks padding) of the caches. Returns the coded queries. q, v, or k
         with v and the caches may be None."""
-        if q is None and k is None:
-            raise ValueError("neither q nor k is given")
         with self._on(stream) as on:
-            lead = (q if q is not None else k).shape[:2]
-            B, T = lead
-            args, fresh = [], []
-            reads = [q, k, v, positions, rows]
-            for name, t, heads in (("q", q, self.heads), ("k", k, self.kv_heads), ("v", v, self.kv_heads)):
-                if t is None:
-                    args += (None, 0)
-                    continue
-                if t.shape[:2] != lead:
-                    raise ValueError(f"{name} has shape {tuple(t.shape)}, not [{B}][{T}]..")
-                t, at, stride = self._tokens(name, t, heads)
-                fresh.append(t)     # lives until the call is enqueued
-                args += (at, stride)
-            args += (self._whole("positions", positions, lead, self._int), self._whole("rows", rows, lead, self._int), B, T)
-            returns = []
+            returns = ()
             if q is None:
                 q_out = None
-                args.append(None)
-            else:
-                shape = (B, T, self.heads, self.head_dim)
-                if q_out is None:
-                    q_out = self._torch.zeros(shape, dtype=self.dtype, device=self.device)
-                    returns.append(q_out)
-                else:
-                    reads.append(q_out)
-                args.append(self._whole("q_out", q_out, shape, self.dtype))
-            if k is None:
-                args.append(None)
-            else:
-                if cache_k is None or (v is not None and cache_v is None):
-                    raise ValueError("k and v need the caches they go to")
-                args.append(byref(self._cache("cache", cache_k, cache_v if v is not None else None, B)))
-                reads += (cache_k, cache_v)
-            self._run("jpi_kv_append", stream, args, on, reads, returns)
+            elif q_out is None:
+                q_out = self._torch.zeros((*q.shape[:2], self.heads, self.head_dim), dtype=self.dtype, device=self.device)
+                returns = (q_out,)
+            self._call("append", on, stream, (q, k, v, positions, rows, cache_k, cache_v, q_out),
+                       (q, k, v, positions, rows, cache_k, cache_v, None if returns else q_out), returns)
         return q_out
-
-    def _sides(self, q, prefix, prefix_len, own, seen):
-        """(q, address, stride, B, T, [prefix, groups, prefix_len, own, seen] as arguments, prefix, own caches)."""
-        q, at, stride = self._tokens("q", q, self.heads)
-        B, T = q.shape[:2]
-        if (prefix is None) != (prefix_len is None) or (own is None) != (seen is None):
-            raise ValueError("prefix goes with prefix_len, own with seen")
-        p = o = None
-        args = [None, 1, None, None, None]
-        if prefix is not None:
-            groups = prefix[0].shape[0]
-            p = self._cache("prefix", *prefix, groups)
-            args[:3] = byref(p), groups, self._whole("prefix_len", prefix_len, (groups,), self._int)
-        if own is not None:
-            o = self._cache("own", *own, B)
-            args[3:] = byref(o), self._whole("seen", seen, (B, T), self._int)
-        return q, at, stride, B, T, args, p, o
 
     def attend(self, q, prefix=None, prefix_len=None, own=None, seen=None, out=None, lse=None, stream=None):
         """Attention of q [B][T][H][D] over the first prefix_len[g] rows of prefix (k, v) [G][P][Hk][D], shared by each
         run of B / G requests, and the first seen[b][t] rows of own (k, v) [B][R][Hk][D]. Returns (out, lse)."""
         with self._on(stream) as on:
-            x, at, stride, B, T, sides, _, _ = self._sides(q, prefix, prefix_len, own, seen)
-            reads, returns = [q, prefix_len, seen, *(prefix or ()), *(own or ())], []
-            shape = (B, T, self.heads, self.head_dim)
+            reads, returns = (out, lse), []
             if out is None:
-                out = self._torch.empty(shape, dtype=self.dtype, device=self.device)
+                out = self._torch.empty((*q.shape[:2], self.heads, self.head_dim), dtype=self.dtype, device=self.device)
                 returns.append(out)
-            else:
-                reads.append(out)
             if lse is None:
-                lse = self._torch.empty(shape[:3], dtype=self._float, device=self.device)
+                lse = self._torch.empty((*q.shape[:2], self.heads), dtype=self._float, device=self.device)
                 returns.append(lse)
-            else:
-                reads.append(lse)
-            self._run("jpi_kv_attend", stream, (at, stride, B, T, *sides, self._whole("out", out, shape, self.dtype),
-                                                self._whole("lse", lse, shape[:3], self._float)), on, reads, returns)
+            if on is not None:
+                reads += (q, prefix_len, seen, *(prefix or ()), *(own or ()))
+            self._call("attend", on, stream, (q, prefix, prefix_len, own, seen, out, lse), reads, returns)
         return out, lse
 
     def weigh(self, q, lse, prefix=None, prefix_len=None, own=None, seen=None, w_prefix=None, w_own=None, decay=1.0,
@@ -293,29 +212,14 @@ class KV:
         `own` (keys [B][R][Hk][D]) to decay times w_prefix [G][Hk][P] and w_own [B][Hk][R] (None: zeros). Returns
         the sums, in out_prefix and out_own (None: new ones, zero where a row holds no key)."""
         with self._on(stream) as on:
-            x, at, stride, B, T, sides, p, o = self._sides(q, None if prefix is None else (prefix, None), prefix_len,
-                                                           None if own is None else (own, None), seen)
-            reads, returns = [q, lse, prefix, prefix_len, own, seen], []
-            args, outs = [], []
-            for name, cache, n, w, out in (("prefix", p, sides[1], w_prefix, out_prefix), ("own", o, B, w_own, out_own)):
-                if cache is None:
-                    if w is not None or out is not None:
-                        raise ValueError(f"weights of {name} without {name}")
-                    args += (None, None)
-                    outs.append(None)
-                    continue
-                shape = (n, self.kv_heads, cache.rows)
-                if out is None:
-                    out = self._torch.zeros(shape, dtype=self._float, device=self.device)
-                    returns.append(out)
-                else:
-                    reads.append(out)
-                reads.append(w)
-                args += (None if w is None else self._whole(f"w_{name}", w, shape, self._float),
-                         self._whole(f"out_{name}", out, shape, self._float))
-                outs.append(out)
-            self._run("jpi_kv_weigh", stream, (at, stride, self._whole("lse", lse, (B, T, self.heads), self._float), B, T,
-                                               *sides, decay, *args), on, reads, returns)
+            reads, returns = (q, lse, prefix, prefix_len, own, seen, w_prefix, w_own, out_prefix, out_own), []
+            outs = [out_prefix, out_own]
+            for i, keys in enumerate((prefix, own)):
+                if keys is not None and outs[i] is None:
+                    outs[i] = self._torch.zeros((keys.shape[0], self.kv_heads, keys.shape[1]), dtype=self._float, device=self.device)
+                    returns.append(outs[i])
+            self._call("weigh", on, stream, (q, lse, prefix, prefix_len, own, seen, decay, w_prefix, outs[0], w_own, outs[1]),
+                       reads, returns)
         return outs[0], outs[1]
 
     def evict(self, k, v, w, length, keep, sink=0, recent=0, out_k=None, out_v=None, out_w=None, out_length=None,
@@ -332,15 +236,10 @@ class KV:
         if out_length is None:
             out_length = length
         with self._on(stream) as on:
-            L, N, R = k.shape[:3]
-            src = self._cache("k, v", k, v, N, L)
-            dst = self._cache("out", out_k, out_v, N, L)
-            kept = self._torch.empty((L, N, self.kv_heads, max(keep, 0)), dtype=self._int, device=self.device)
-            args = (byref(src), self._whole("w", w, (L, N, self.kv_heads, R), self._float),
-                    self._whole("length", length, (N,), self._int), L, N, keep, sink, recent, byref(dst),
-                    self._whole("out_w", out_w, (L, N, self.kv_heads, dst.rows), self._float),
-                    self._whole("out_length", out_length, (N,), self._int), kept.data_ptr())
-            self._run("jpi_kv_evict", stream, args, on, (k, v, w, length, out_k, out_v, out_w, out_length), (kept,))
+            rows = min(max(keep, 0), max(k.shape[2], out_k.shape[2]))      # (more are refused)
+            kept = self._torch.empty((*k.shape[:2], self.kv_heads, rows), dtype=self._int, device=self.device)
+            self._call("evict", on, stream, (k, v, w, length, keep, sink, recent, out_k, out_v, out_w, out_length, kept),
+                       (k, v, w, length, out_k, out_v, out_w, out_length), (kept,))
         return kept
 
     def device_status(self):

@@ -647,3 +647,36 @@ def test_the_binding_checks_what_the_c_abi_cannot_see(kv):
     from paper_2607_12659_gb300.jpi import JpiError
     with pytest.raises(JpiError):
         h.attend(rand(1, 5, 1, 8, 64), own=(rand(1, 5, 3, 2, 64),) * 2, seen=i32([[1]] * 5))
+
+
+def test_the_binding_takes_rows_of_any_stride_and_refuses_what_is_no_cache(kv):
+    h = kv.KV(8, 2, 64, max_batch=4, max_tokens=4)
+    q, k = rand(1, 4, 4, 8, 64), rand(2, 4, 10, 2, 64)
+    seen = i32([[10] * 4] * 4)
+    want, lse = h.attend(q, own=(k, k), seen=seen)
+    flat = rand(3, 4 * 4 * 8 * 64 + 1)
+    off = flat[1:].view(4, 4, 8, 64)      # contiguous, two bytes past a 16-byte boundary
+    off.copy_(q)
+    rows = rand(4, 4, 4, 11, 64)[:, :, 2:10]
+    rows.copy_(q)
+    cols = rand(5, 4, 4, 8, 65)[..., :64]
+    cols.copy_(q)
+    for x in (off, rows, cols, q.transpose(0, 1).contiguous().transpose(0, 1), q.transpose(1, 2).contiguous().transpose(1, 2)):
+        got, lse2 = h.attend(x, own=[k, k], seen=seen)      # a list is a pair too
+        assert torch.equal(got, want) and torch.equal(lse2, lse)
+    for kw in [dict(own=k), dict(own=(k,)), dict(own=(k, None)), dict(own=(k, 3)), dict(q=None, out=q, lse=lse), dict(seen=[[10] * 4] * 4)]:
+        with pytest.raises((TypeError, ValueError)):
+            h.attend(**{**dict(q=q, own=(k, k), seen=seen), **kw})
+    w, n = torch.zeros((1, 4, 2, 10), device="cuda"), i32([10] * 4)
+    for keep in (2 ** 40, 1.5):
+        with pytest.raises((TypeError, ValueError, RuntimeError)):
+            h.evict(k[None], k[None], w, n, keep)
+    with pytest.raises(ValueError):
+        h.evict(k, k, w, n, 5)
+    sparse = torch.sparse_coo_tensor(torch.zeros((4, 1), dtype=torch.int64, device="cuda"), torch.ones(1, device="cuda").bfloat16(), q.shape)
+    with pytest.raises(ValueError):
+        h.attend(sparse, own=(k, k), seen=seen)
+    h.close()
+    from paper_2607_12659_gb300.jpi import JpiError
+    with pytest.raises(JpiError):
+        h.attend(q, own=(k, k), seen=seen)

@@ -158,3 +158,46 @@ def test_evict_keeps_the_protected_rows_and_the_heaviest():
     assert okv.evict(w, 8, 2, 1, 1) == [0, 7]
     assert okv.evict(w, 8, 8, 1, 1) == list(range(8)) and okv.evict(w, 3, 5, 1, 1) == [0, 1, 2]
     assert okv.evict([math.nan, math.nan, -math.inf], 3, 2, 0, 0) == [0, 2]
+
+
+def test_the_module_of_checks_refuses_before_any_call(lib):
+    """The checked calls' own refusals: nothing here reaches the entry points (their addresses are zero)."""
+    torch = pytest.importorskip("torch")
+    from paper_2607_12659_gb300 import _kv
+    c = _kv.calls(8, 2, 64, True, 0, 0, 0, 0, 0)
+    q, k = torch.zeros((2, 3, 8, 64), dtype=torch.bfloat16), torch.zeros((2, 5, 2, 64), dtype=torch.bfloat16)
+    i, f = torch.zeros((2, 3), dtype=torch.int32), torch.zeros((2, 3, 8))
+    with pytest.raises(ValueError, match="q is a Strided tensor on cpu, the handle on cuda:0"):
+        _kv.attend(c, 1, 0, q, (k, k), i, None, None, q, f)
+    with pytest.raises(ValueError, match="cpu"):
+        _kv.weigh(c, 1, 0, q, f, k, i, None, None, 1.0, None, None, None, None)
+    with pytest.raises(ValueError, match="cpu"):
+        _kv.append(c, 1, 0, q, k, k, i, i, k, k, q)
+    with pytest.raises(ValueError, match="cpu"):
+        _kv.evict(c, 1, 0, k[None], k[None], f, i, 1, 0, 0, k[None], k[None], f, i, i)
+    with pytest.raises(ValueError, match="neither q nor k"):
+        _kv.append(c, 1, 0, None, None, k, i, i, k, k, q)
+    with pytest.raises(ValueError, match="layers"):
+        _kv.evict(c, 1, 0, k, k, f, i, 1, 0, 0, k, k, f, i, i)
+    for bad in (None, 3, [1.0]):
+        with pytest.raises(TypeError, match="q must be a tensor"):
+            _kv.attend(c, 1, 0, bad, (k, k), i, None, None, q, f)
+    with pytest.raises(TypeError, match="10 arguments"):
+        _kv.attend(c, 1, 0, q)
+    with pytest.raises(TypeError):
+        _kv.calls(8, 2, 64)
+    for capsule, handle in ((None, 1), (c, "x")):
+        with pytest.raises((TypeError, ValueError)):
+            _kv.attend(capsule, handle, 0, q, (k, k), i, None, None, q, f)
+    sparse = torch.sparse_coo_tensor(torch.zeros((4, 1), dtype=torch.int64), torch.ones(1, dtype=torch.bfloat16), (2, 3, 8, 64))
+    for odd in (sparse, torch.empty((2, 3, 8, 64), dtype=torch.bfloat16, device="meta")):
+        with pytest.raises(ValueError):
+            _kv.attend(c, 1, 0, odd, (k, k), i, None, None, q, f)
+
+
+def test_a_missing_module_of_checks_is_an_error(lib, monkeypatch):
+    import sys
+    monkeypatch.setitem(sys.modules, "paper_2607_12659_gb300._kv", None)
+    monkeypatch.delattr("paper_2607_12659_gb300._kv", raising=False)
+    with pytest.raises(RuntimeError, match="not built"):
+        kv._checked_calls(8, 2, 64, True, 0)
