@@ -7,6 +7,7 @@
 // Nothing here links against libjpi.so: kv.py passes the entry points of the library that it has loaded.
 
 #include <Python.h>
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
@@ -161,13 +162,14 @@ Side side(const Calls& c, const char* name, PyObject* o, const char* len_name, P
     return r;
 }
 
+// The call itself runs without the interpreter's lock. Its status, or where that is JPI_OK and `result` is given, the result.
 template <typename F>
-PyObject* status_of(F&& call) {
+PyObject* status_of(F&& call, const at::Tensor* result = nullptr) {
     jpi_status s;
     Py_BEGIN_ALLOW_THREADS;
     s = call();
     Py_END_ALLOW_THREADS;
-    return PyLong_FromLong(s);
+    return s == JPI_OK && result ? THPVariable_Wrap(*result) : PyLong_FromLong(s);
 }
 
 // Arguments are counted, and no C++ exception leaves an entry.
@@ -266,9 +268,9 @@ PyObject* weigh(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// (calls, handle, stream, k, v, w, length, keep, sink, recent, out_k, out_v, out_w, out_length, kept)
+// (calls, handle, stream, k, v, w, length, keep, sink, recent, out_k, out_v, out_w, out_length); returns the rows kept
 PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return entry(a, n, 15, [&](const Calls& c, jpi_kv_handle* h, void* st) {
+    return entry(a, n, 14, [&](const Calls& c, jpi_kv_handle* h, void* st) {
         const at::Tensor& k = tensor(a[3], "k");
         if (k.dim() != 5) throw Refused("k has shape " + str(k.sizes()) + ", not [layers][caches][rows][KV heads][head dim]");
         const int64_t L = k.size(0), N = k.size(1);
@@ -278,12 +280,15 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const float* w = whole<float>(c, "w", a[5], w_shape, at::kFloat);
         const int* length = whole<int>(c, "length", a[6], {N}, at::kInt);
         const int keep = int_of(a[7], "keep"), sink = int_of(a[8], "sink"), recent = int_of(a[9], "recent");
-        if (keep > src.rows && keep > dst.rows) throw Refused("keep is " + std::to_string(keep) + " of " + std::to_string(src.rows) + " rows");
+        if (keep < 0 || (keep > src.rows && keep > dst.rows)) throw Refused("keep is " + std::to_string(keep) + " of " + std::to_string(src.rows) + " rows");
         float* w_out = whole<float>(c, "out_w", a[12], o_shape, at::kFloat);
         int* len_out = whole<int>(c, "out_length", a[13], {N}, at::kInt);
-        const int64_t k_shape[4] = {L, N, c.K, keep > 0 ? keep : 0};
-        int* kept = whole<int>(c, "kept", a[14], k_shape, at::kInt);
-        return status_of([&] { return c.evict(h, &src, w, length, layers, caches, keep, sink, recent, &dst, w_out, len_out, kept, st); });
+        const at::Tensor kept = at::empty({L, N, c.K, keep}, k.options().dtype(at::kInt));
+        return status_of(
+            [&] {
+                return c.evict(h, &src, w, length, layers, caches, keep, sink, recent, &dst, w_out, len_out, static_cast<int*>(kept.data_ptr()), st);
+            },
+            &kept);
     });
 }
 

@@ -145,7 +145,7 @@ class KV:
         self.handle = jpi_kv_create(self.cfg, rope.c() if rope is not None else None)
         self.index = torch.cuda.current_device()
         self.device = torch.device("cuda", self.index)
-        self._torch, self._int, self._float = torch, torch.int32, torch.float32
+        self._torch, self._float = torch, torch.float32
         self._kv, self._calls = _checked_calls(n_heads, n_kv_heads, head_dim, precision == "bf16", self.index)
 
     def close(self):
@@ -166,14 +166,16 @@ class KV:
         return _HERE if stream is None else OnStream(stream, self.device)
 
     def _call(self, fn, on, stream, args, reads, returns):
-        """The checked call; on a stream of its own, with what it reads and returns kept by it."""
+        """The checked call, and its result if it makes one; on a stream of its own, what it reads and returns is kept."""
         raw = self._torch._C._cuda_getCurrentRawStream(self.index) if on is None else _stream(stream)
-        status = getattr(self._kv, fn)(self._calls, self.handle, raw, *args)
-        if status:
-            _check(status, "jpi_kv_" + fn)
+        result = getattr(self._kv, fn)(self._calls, self.handle, raw, *args)
+        made = type(result) is not int      # else a status
+        if not made and result:
+            _check(result, "jpi_kv_" + fn)
         if on is not None:
             on.reads(*(t for t in reads if t is not None))
-            on.returns(*returns)
+            on.returns(*returns, *((result,) if made else ()))
+        return result
 
     def append(self, q, k, v, positions, rows, cache_k=None, cache_v=None, q_out=None, stream=None):
         """Codes q [B][T][H][D] and k [B][T][Hk][D] for `positions` (int32 [B][T]) and writes k and v into `rows`
@@ -236,11 +238,8 @@ class KV:
         if out_length is None:
             out_length = length
         with self._on(stream) as on:
-            rows = min(max(keep, 0), max(k.shape[2], out_k.shape[2]))      # (more are refused)
-            kept = self._torch.empty((*k.shape[:2], self.kv_heads, rows), dtype=self._int, device=self.device)
-            self._call("evict", on, stream, (k, v, w, length, keep, sink, recent, out_k, out_v, out_w, out_length, kept),
-                       (k, v, w, length, out_k, out_v, out_w, out_length), (kept,))
-        return kept
+            return self._call("evict", on, stream, (k, v, w, length, keep, sink, recent, out_k, out_v, out_w, out_length),
+                              (k, v, w, length, out_k, out_v, out_w, out_length), ())
 
     def device_status(self):
         jpi_kv_device_status(self.handle)

@@ -174,11 +174,11 @@ def test_the_module_of_checks_refuses_before_any_call(lib):
     with pytest.raises(ValueError, match="cpu"):
         _kv.append(c, 1, 0, q, k, k, i, i, k, k, q)
     with pytest.raises(ValueError, match="cpu"):
-        _kv.evict(c, 1, 0, k[None], k[None], f, i, 1, 0, 0, k[None], k[None], f, i, i)
+        _kv.evict(c, 1, 0, k[None], k[None], f, i, 1, 0, 0, k[None], k[None], f, i)
     with pytest.raises(ValueError, match="neither q nor k"):
         _kv.append(c, 1, 0, None, None, k, i, i, k, k, q)
     with pytest.raises(ValueError, match="layers"):
-        _kv.evict(c, 1, 0, k, k, f, i, 1, 0, 0, k, k, f, i, i)
+        _kv.evict(c, 1, 0, k, k, f, i, 1, 0, 0, k, k, f, i)
     for bad in (None, 3, [1.0]):
         with pytest.raises(TypeError, match="q must be a tensor"):
             _kv.attend(c, 1, 0, bad, (k, k), i, None, None, q, f)
