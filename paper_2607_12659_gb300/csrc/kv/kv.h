@@ -76,22 +76,34 @@ jpi_status launch_kv_evict(const jpi_kv_handle* h, const jpi_kv_cache& src, cons
                            int caches, int keep, int sink, int recent, const jpi_kv_cache& dst, float* w_out,
                            int* length_out, int* kept, cudaStream_t st);
 
-// An ordinary launch, or with `early` one that starts while the kernel before it runs.
+// An ordinary launch, or with `early` one that starts while the kernel before it runs; in clusters of `ranks` blocks.
 template <typename... Params, typename... Args>
-jpi_status kv_start(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, bool early, cudaStream_t st,
-                    const Args&... args) {
+jpi_status kv_start_clusters(void (*kernel)(Params...), dim3 grid, unsigned ranks, int threads, size_t smem, bool early,
+                             cudaStream_t st, const Args&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = early ? 1 : 0;
+    cudaLaunchAttribute at[2];
+    cfg.attrs = at;
+    if (early) {
+        at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (ranks > 1) {
+        at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        at[cfg.numAttrs].val.clusterDim.x = ranks;
+        at[cfg.numAttrs].val.clusterDim.y = 1;
+        at[cfg.numAttrs++].val.clusterDim.z = 1;
+    }
     JPI_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     return JPI_OK;
+}
+template <typename... Params, typename... Args>
+jpi_status kv_start(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, bool early, cudaStream_t st,
+                    const Args&... args) {
+    return kv_start_clusters(kernel, grid, 1, threads, smem, early, st, args...);
 }
 
 }  // namespace jpi

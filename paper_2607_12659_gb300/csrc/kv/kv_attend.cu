@@ -575,10 +575,14 @@ __global__ void __maxnreg__(RtSmem<DP>::REGS) k_kv_attend_rows(const __grid_cons
     }
 }
 
-// fp32 on CUDA cores: one warp = 8 query rows over 32-key blocks. Scores with a key per lane, the
-// values with a lane per four elements of d.
+// fp32 on CUDA cores: one warp = 8 query rows over 32-key blocks. Scores with a key per lane, the values with a lane per four
+// elements of d. What bounds it is latency: a block's loads, its products (5 instructions for 4 of them) and 2^x follow one
+// another in a warp, and a small call has a block or two per warp. So the loads of 8 pieces of a key and of 8 values are on
+// their way together, in as many registers as leave an SM three blocks: 16 us for 4 requests of 9 tokens over 342 keys where
+// loads one by one took 20; a call of 294 tokens over 103 keys took 47 with 16 loads of a key and two blocks per SM, 39 with
+// four blocks, 36 with three.
 template <int DP>
-__global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32(const __grid_constant__ AttendArgs a) {
     extern __shared__ __align__(16) float kv_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     ptx::grid_dep_launch();
@@ -610,6 +614,7 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
     const float* kbase = (const float*)s.k + x.cache * s.cs + (x.kvh) * s.hs;
     const float* vbase = (const float*)s.v + x.cache * s.cs + (x.kvh) * s.hs;
     constexpr int NI = (DP + 127) / 128;
+    constexpr int KL = 8 / NI, VL = 8 / NI;   // 16-byte loads of a key, values, that are on their way at a time
     float4 o[KR_ROWS][NI];
     float m[KR_ROWS], l[KR_ROWS];
 #pragma unroll
@@ -625,13 +630,18 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
 #pragma unroll
         for (int r = 0; r < KR_ROWS; ++r) p[r] = 0.f;
         const float* kp = kbase + (long long)key * s.rs;
-        if (key < lim) {
-            for (int d = 0; d < D; d += 4) {
-                const float4 k = __ldg((const float4*)(kp + d));
+        for (int d0 = 0; d0 < D; d0 += 4 * KL) {
+            float4 k[KL];
+#pragma unroll
+            for (int i = 0; i < KL; ++i)
+                k[i] = key < lim && d0 + 4 * i < D ? __ldg((const float4*)(kp + d0 + 4 * i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < KL; ++i) {
+                if (d0 + 4 * i >= D) break;
 #pragma unroll
                 for (int r = 0; r < KR_ROWS; ++r) {
-                    const float4 q = *(const float4*)(qs + r * DP + d);
-                    p[r] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, p[r]))));
+                    const float4 q = *(const float4*)(qs + r * DP + d0 + 4 * i);
+                    p[r] = fmaf(q.x, k[i].x, fmaf(q.y, k[i].y, fmaf(q.z, k[i].z, fmaf(q.w, k[i].w, p[r]))));
                 }
             }
         }
@@ -651,27 +661,31 @@ __global__ void __launch_bounds__(AT_THREADS) k_kv_attend_f32(const __grid_const
             p[r] = m[r] == -INFINITY ? 0.f : exp2f((sc - m[r]) * a.c2);
             l[r] += p[r];
         }
-        for (int t = 0; t < 32 && key0 + t < lim; ++t) {
-            const float* vp = vbase + (long long)(key0 + t) * s.rs;
-            float4 v[NI];
+        for (int t0 = 0; t0 < 32 && key0 + t0 < lim; t0 += VL) {
+            float4 v[VL][NI];
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int d = 4 * lane + 128 * i;
-                v[i] = d < D ? __ldg((const float4*)(vp + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
+            for (int t = 0; t < VL; ++t)
 #pragma unroll
-            for (int r = 0; r < KR_ROWS; ++r) {
-                const float w = __shfl_sync(0xffffffffu, p[r], t);
-                if (key0 + t < n[r]) {   // a hidden value is not even multiplied by zero
+                for (int i = 0; i < NI; ++i) {
+                    const int d = 4 * lane + 128 * i;
+                    v[t][i] = d < D && key0 + t0 + t < lim ? __ldg((const float4*)(vbase + (long long)(key0 + t0 + t) * s.rs + d))
+                                                           : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
 #pragma unroll
-                    for (int i = 0; i < NI; ++i) {
-                        o[r][i].x = fmaf(w, v[i].x, o[r][i].x);
-                        o[r][i].y = fmaf(w, v[i].y, o[r][i].y);
-                        o[r][i].z = fmaf(w, v[i].z, o[r][i].z);
-                        o[r][i].w = fmaf(w, v[i].w, o[r][i].w);
+            for (int t = 0; t < VL; ++t)
+#pragma unroll
+                for (int r = 0; r < KR_ROWS; ++r) {
+                    const float w = __shfl_sync(0xffffffffu, p[r], t0 + t);
+                    if (key0 + t0 + t < n[r]) {   // a hidden value is not even multiplied by zero
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) {
+                            o[r][i].x = fmaf(w, v[t][i].x, o[r][i].x);
+                            o[r][i].y = fmaf(w, v[t][i].y, o[r][i].y);
+                            o[r][i].z = fmaf(w, v[t][i].z, o[r][i].z);
+                            o[r][i].w = fmaf(w, v[t][i].w, o[r][i].w);
+                        }
                     }
                 }
-            }
         }
     }
 #pragma unroll

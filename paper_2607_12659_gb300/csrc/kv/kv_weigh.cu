@@ -97,26 +97,41 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_mma(const __grid_consta
             kf[i][0] = kr_ld(kp + 32 * i, in && key0 + g < live);
             kf[i][1] = kr_ld(kp + 8 * s.rs + 32 * i, in && key0 + g + 8 < live);
         }
-        for (int rt = wrow * KR_ROWS; rt < x.t.R; rt += x.wr * KR_ROWS) {
+        // A row tile's loads: its query rows, and of rows 2 j and 2 j + 1 the lse and what they see.
+        struct Rows {
+            uint4 q[NC];
+            float ls[2];
+            int n[2];
+        };
+        auto load = [&](int rt) {
+            Rows y;
             const int rq = rt + g;
             const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + 8 * j;
             if (rq < x.t.R) q += row_query(a.c, x.t, rq);
-            float sc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const uint4 v = kr_ld(q + 32 * i, rq < x.t.R && 8 * (4 * i + j) < a.c.D);
-                kr_mma(sc, kf[i][0].x, kf[i][1].x, kf[i][0].y, kf[i][1].y, v.x, v.y);
-                kr_mma(sc, kf[i][0].z, kf[i][1].z, kf[i][0].w, kf[i][1].w, v.z, v.w);
-            }
+            for (int i = 0; i < NC; ++i) y.q[i] = kr_ld(q + 32 * i, rq < x.t.R && 8 * (4 * i + j) < a.c.D);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int r = rt + 2 * j + e;
-                if (r >= x.t.R) continue;
-                const float ls = a.lse[row_index(a.c, x.t, r)];
-                const int n = row_seen(a.c, x.prefix, x.cache, x.t, r);
-                if (ls == -INFINITY) continue;
-                if (key0 + g < n) acc0 += kr_ex2(fmaf(sc[e], a.c.scale, -ls) * KR_LOG2E);
-                if (key0 + g + 8 < n) acc1 += kr_ex2(fmaf(sc[2 + e], a.c.scale, -ls) * KR_LOG2E);
+                y.ls[e] = r < x.t.R ? a.lse[row_index(a.c, x.t, r)] : -INFINITY;
+                y.n[e] = row_seen(a.c, x.prefix, x.cache, x.t, r);
+            }
+            return y;
+        };
+        const int step = x.wr * KR_ROWS;
+        for (int rt = wrow * KR_ROWS; rt < x.t.R; rt += step) {
+            const Rows y = load(rt);
+            float sc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                kr_mma(sc, kf[i][0].x, kf[i][1].x, kf[i][0].y, kf[i][1].y, y.q[i].x, y.q[i].y);
+                kr_mma(sc, kf[i][0].z, kf[i][1].z, kf[i][0].w, kf[i][1].w, y.q[i].z, y.q[i].w);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (y.ls[e] == -INFINITY) continue;
+                if (key0 + g < y.n[e]) acc0 += kr_ex2(fmaf(sc[e], a.c.scale, -y.ls[e]) * KR_LOG2E);
+                if (key0 + g + 8 < y.n[e]) acc1 += kr_ex2(fmaf(sc[2 + e], a.c.scale, -y.ls[e]) * KR_LOG2E);
             }
         }
     }
@@ -149,12 +164,15 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_f32(const __grid_consta
     float acc = 0.f;
     const float* kp = (const float*)s.k + x.cache * s.cs + x.kvh * s.hs + (long long)(key < live ? key : 0) * s.rs;
     for (int rt = wrow * KR_ROWS; rt < x.t.R; rt += x.wr * KR_ROWS) {
-        float p[KR_ROWS];
+        float p[KR_ROWS], ls[KR_ROWS];
+        int n[KR_ROWS];
         const float* q[KR_ROWS];
 #pragma unroll
         for (int r = 0; r < KR_ROWS; ++r) {
             const int rr = min(rt + r, x.t.R - 1);
             p[r] = 0.f;
+            ls[r] = a.lse[row_index(a.c, x.t, rr)];
+            n[r] = row_seen(a.c, x.prefix, x.cache, x.t, rt + r);
             q[r] = static_cast<const float*>(a.c.q) + row_query(a.c, x.t, rr);
         }
         if (key < live)
@@ -167,12 +185,8 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_f32(const __grid_consta
                 }
             }
 #pragma unroll
-        for (int r = 0; r < KR_ROWS; ++r) {
-            if (rt + r >= x.t.R) break;
-            const float ls = a.lse[row_index(a.c, x.t, rt + r)];
-            const int n = row_seen(a.c, x.prefix, x.cache, x.t, rt + r);
-            if (key < n && ls != -INFINITY) acc += expf(fmaf(p[r], a.c.scale, -ls));
-        }
+        for (int r = 0; r < KR_ROWS; ++r)
+            if (key < n[r] && ls[r] != -INFINITY) acc += expf(fmaf(p[r], a.c.scale, -ls[r]));
     }
     part[warp][lane] = acc;
     __syncthreads();

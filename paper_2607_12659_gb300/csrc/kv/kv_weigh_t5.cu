@@ -31,7 +31,8 @@ struct WeighT5Args {
     int tiles;           // key tiles per run and KV head
     int3 at;             // of the map's outer dimensions: heads, rows, runs
     int* err;
-    KvDiv by_tiles;
+    KvDiv by_tiles, by_ranks;
+    int ranks;           // blocks (a cluster) that share a key tile, each with every ranks-th row tile
 };
 
 template <int DP>
@@ -63,8 +64,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) k_kv_weigh_t5(const __grid_cons
     uint32_t* tmem_slot = (uint32_t*)(kfull + 9);
     int* flag = (int*)(tmem_slot + 1);
     const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
-    uint32_t tile, kvh;
-    const int run = (int)a.c.by_K.div(a.by_tiles.div(blockIdx.x, tile), kvh);
+    uint32_t tile, kvh, rank;
+    const int run = (int)a.c.by_K.div(a.by_tiles.div(a.by_ranks.div(blockIdx.x, rank), tile), kvh);
     const int len = min(max(a.c.prefix.len[run], 0), a.c.prefix.rows), key0 = (int)tile * WT_KEYS;
     if (key0 >= len) {
         ptx::grid_dep_wait();   // (ends after the kernel that started before it)
@@ -76,7 +77,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) k_kv_weigh_t5(const __grid_cons
     t.head0 = (int)kvh * a.c.gq;
     t.R = toks * a.c.gq;
     t.r0 = 0;
-    const int nt = (t.R + WT_ROWS - 1) / WT_ROWS;
+    // Row tiles of this block: rank, rank + ranks, ..
+    const int nt = ((t.R + WT_ROWS - 1) / WT_ROWS - (int)rank + a.ranks - 1) / a.ranks;
 
     if (warp == 0 && ptx::elect_one()) {
         ptx::prefetch_tmap(&kmap);
@@ -140,10 +142,10 @@ __global__ void __launch_bounds__(WT_THREADS, 1) k_kv_weigh_t5(const __grid_cons
                                     (long long)t.head0 * a.c.D + (dlive ? 8 * ch : 0);
         const uint32_t dst = ptx::smem_u32(wt_smem) + L::Q_OFF + b * L::QBYTES + (ch >> 3) * (WT_ROWS * 128);
         for (int i = b; i < nt; i += 2) {
-            const int rl = i * WT_ROWS + lt;
+            const int rt = ((int)rank + i * a.ranks) * WT_ROWS, rl = rt + lt;
             const float ls = rl < t.R ? a.lse[row_index(a.c, t, rl)] : -INFINITY;
-            // Rows i WT_ROWS + rr0, + RPI, ..: token and head, stepped without a division. Past the run's rows nothing is read.
-            int r = i * WT_ROWS + rr0;
+            // Rows rt + rr0, + RPI, ..: token and head, stepped without a division. Past the run's rows nothing is read.
+            int r = rt + rr0;
             uint32_t hd, tok = a.c.by_gq.div((uint32_t)r, hd);
             if (i >= 2 && good) good = ptx::mbar_wait_bounded(&qempty[b], ((i >> 1) - 1) & 1, WT_WAIT_NS);
 #pragma unroll 8
@@ -197,23 +199,33 @@ __global__ void __launch_bounds__(WT_THREADS, 1) k_kv_weigh_t5(const __grid_cons
         const float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
         if (half == 1) sums[key] = sum;
         ptx::named_bar_sync(1, WT_SUM);
-        ptx::grid_dep_wait();   // the row kernel that started before this one: what follows this kernel has both
-        if (half == 0 && key0 + key < len && good) {
-            const long long at = ((long long)run * a.c.K + kvh) * a.c.prefix.rows + key0 + key;
-            const float w = sum + sums[key];
-            a.out[at] = a.in && a.decay != 0.f ? fmaf(a.decay, a.in[at], w) : w;
-        }
+        if (half == 0) sums[key] += sum;
     }
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
+    // The sums of the blocks that share the keys, in their order.
+    if (a.ranks > 1) ptx::cluster_sync_all();
+    const int key = tid - (WT_THREADS - WT_SUM);
+    if (rank == 0 && key >= 0 && key < WT_KEYS) {
+        float w = sums[key];
+        for (int k = 1; k < a.ranks; ++k) w += ptx::dsmem_ld_f32(ptx::dsmem_map(ptx::smem_u32(sums + key), (uint32_t)k));
+        ptx::grid_dep_wait();   // the row kernel that started before this one: what follows this kernel has both
+        if (key0 + key < len && *flag == 0) {
+            const long long at = ((long long)run * a.c.K + kvh) * a.c.prefix.rows + key0 + key;
+            a.out[at] = a.in && a.decay != 0.f ? fmaf(a.decay, a.in[at], w) : w;
+        }
+    }
+    __syncwarp();
+    if (a.ranks > 1) ptx::cluster_sync_all();   // (a block's shared memory lasts until its sums have been read)
     if (tid == 0 && *flag != 0) atomicCAS(a.err, 0, *flag);
     if (warp == 1) ptx::tmem_dealloc(tmem, L::TMEM_COLS);
 }
 
 template <int DP>
 jpi_status launch_dim(const WeighT5Args& a, const CUtensorMap& map, bool early, cudaStream_t st) {
-    return kv_start(k_kv_weigh_t5<DP>, (long long)a.tiles * a.c.K * a.c.groups, WT_THREADS, WtSmem<DP>::BYTES, early, st, map, a);
+    return kv_start_clusters(k_kv_weigh_t5<DP>, (long long)a.tiles * a.c.K * a.c.groups * a.ranks, (unsigned)a.ranks, WT_THREADS,
+                             WtSmem<DP>::BYTES, early, st, map, a);
 }
 
 }  // namespace
@@ -234,7 +246,7 @@ bool kv_weigh_tiles(const jpi_kv_handle* h, const KvCall& c) {
     KvMapDims m;
     const long long R = (long long)(c.batch / c.groups) * c.tokens * c.gq;
     return R >= 64 && kv_map_dims(c.prefix, c.K, c.D, c.groups, &m) &&
-           (long long)((c.prefix.rows + WT_KEYS - 1) / WT_KEYS) * c.K * c.groups <= 0x7fffffffll;
+           (long long)((c.prefix.rows + WT_KEYS - 1) / WT_KEYS) * c.K * c.groups <= 0x7fffffffll / 8;
 }
 
 jpi_status launch_kv_weigh_t5(jpi_kv_handle* h, const KvCall& c, const float* lse, float decay, const float* in, float* out,
@@ -248,6 +260,12 @@ jpi_status launch_kv_weigh_t5(jpi_kv_handle* h, const KvCall& c, const float* ls
     a.tiles = (c.prefix.rows + WT_KEYS - 1) / WT_KEYS;
     a.by_tiles = KvDiv((uint32_t)a.tiles);
     a.err = h->dev_err;
+    // Few keys and many rows: a row tile is 1.5 us of a block, one after the other.
+    const long long blocks = (long long)a.tiles * c.K * c.groups;
+    const long long nt = ((long long)(c.batch / c.groups) * c.tokens * c.gq + WT_ROWS - 1) / WT_ROWS;
+    a.ranks = 1;
+    while (a.ranks < 8 && 2 * a.ranks <= nt && blocks * a.ranks * 2 <= h->num_sms) a.ranks *= 2;
+    a.by_ranks = KvDiv((uint32_t)a.ranks);
     KvMapDims m;
     CUtensorMap map;
     if (!kv_map_dims(c.prefix, c.K, c.D, c.groups, &m) || !kv_make_map(m, c.prefix.k, c.D, WT_KEYS, &map)) {

@@ -368,6 +368,14 @@ def test_weigh_many_rows(kv, H, K, D, B, T, G, P, R):
     check_weigh(kv, "bf16", H, K, D, B, T, G, P, R, seed=B, decay=1.0)
 
 
+@pytest.mark.parametrize("H,K,D,B,T,G,P,R", [(8, 1, 256, 5, 36, 1, 8, 40), (8, 1, 256, 4, 80, 2, 700, 0), (16, 2, 128, 9, 31, 1, 130, 3),
+                                             (8, 1, 64, 130, 1, 1, 129, 1), (4, 1, 80, 3, 100, 3, 1, 5), (8, 2, 256, 48, 17, 3, 300, 7)])
+def test_weigh_few_keys_many_rows(kv, H, K, D, B, T, G, P, R):
+    """Row tiles of one key tile dealt to several blocks, in equal and unequal numbers."""
+    check_weigh(kv, "bf16", H, K, D, B, T, G, P, R, seed=P)
+
+
+
 def test_weigh_in_place_no_input_and_decay_zero(kv):
     check_weigh(kv, "bf16", 8, 2, 64, 2, 3, 1, 40, 9, with_in=False)
     h, c, lse, got = check_weigh(kv, "bf16", 8, 2, 64, 2, 3, 1, 40, 9, decay=0.5)
