@@ -92,6 +92,8 @@ typedef struct jpi_kv_cache {
 /* Checks the shapes, allocates the workspace for the maxima and tabulates the rotary coding (NULL:
  * none; append then copies). Synchronous; the only call that allocates. On failure *out is NULL. */
 JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* rope, jpi_kv_handle** out);
+/* The environment read here: JPI_KV_TILES=0 / 1 keeps jpi_kv_attend and jpi_kv_weigh on the kernels for few query rows,
+ * or on the tensor-core tiles wherever those fit, for the handle's lifetime (results agree to rounding). */
 JPI_API jpi_status jpi_kv_destroy(jpi_kv_handle* h);   /* NULL is a no-op */
 
 /*

@@ -17,6 +17,7 @@ struct jpi_kv_handle {
     size_t ws_bytes = 0;
     int* dev_err = nullptr;
     bool pdl = true;             // kernels of one call may start before the one before them has finished
+    int tiles = -1;              // attend, weigh: the tensor-core tiles never, (1) wherever they fit, (-1) by size
     size_t device_bytes = 0;
     std::vector<void*> allocations;
 };

@@ -4,6 +4,7 @@
 #include "kv.h"
 #include "kv_weigh.h"
 
+#include <cstdlib>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -198,6 +199,9 @@ JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* ro
     h->K = cfg->n_kv_heads;
     h->D = cfg->head_dim;
     h->gq = h->H / h->K;
+    // JPI_KV_TILES=0 / 1 fixes which kernels take the sides that both could.
+    const char* tiles_env = std::getenv("JPI_KV_TILES");
+    if (tiles_env && (tiles_env[0] == '0' || tiles_env[0] == '1')) h->tiles = tiles_env[0] - '0';
     h->scale = cfg->scale > 0.f ? cfg->scale : 1.f / sqrtf((float)h->D);
     auto setup = [&]() -> jpi_status {
         JPI_CUDA_TRY(cudaGetDevice(&h->device));

@@ -49,6 +49,13 @@ constexpr int KP_SOFT = 256;   // threads of a softmax group
 constexpr uint64_t KP_WAIT_NS = 200ull * 1000 * 1000;
 constexpr float KP_RESCALE = 8.f;   // log2 units
 constexpr int KP_LEAST = 32;        // query rows from which a side takes the tiles
+// Elements of keys up to which a call stays with the row kernel, which reads a key once for every 8 query rows but has
+// neither the tiles' long start nor their query rows to turn. Microseconds of row kernel and tiles where 16 own rows come with it:
+// 1 KV head at D = 256, 256 rows over 64, 512, 1024 and 2048 keys (0.5, 4, 8 and 17 M elements): 8.2 11.3 11.8 17.4 and
+// 11.8 12.5 12.6 14.0; 1024 rows over 256 and 512 keys (8 and 17 M): 11.6 17.9 and 13.5 13.4; 8 KV heads at D = 128, 128
+// rows each over 512 and 1024 keys: 10.9 14.7 and 12.5 13.0; 512 rows at D = 64 over 2048 and 4096 keys: 10.7 15.2
+// and 11.7 12.4.
+constexpr long long KP_ROW_ELEMENTS = 10ll << 20;
 constexpr int KP_FIXED = 5;         // start and end of a block, in key blocks
 
 // Tiles of a run's rows over its prefix (0), or of a request's rows over its own keys (1), with `both` over the prefix's
@@ -650,6 +657,7 @@ jpi_status prepare_dim() {
 struct TileWork {
     bool fit = false;
     long long tiles = 0, blocks = 0, nb = 0;
+    long long elements = 0;   // of keys that the row kernel would read: each row of 8 query rows' tile by itself
 };
 TileWork work_of(const jpi_kv_handle* h, const KvCall& c, bool own) {
     TileWork w;
@@ -658,11 +666,12 @@ TileWork work_of(const jpi_kv_handle* h, const KvCall& c, bool own) {
     const int caches = own ? c.batch : c.groups;
     const long long R = (long long)(own ? 1 : c.batch / c.groups) * c.tokens * c.gq;
     KvMapDims m;
-    if (R < KP_LEAST || !kv_map_dims(s, c.K, c.D, caches, &m)) return w;
+    if (h->tiles == 0 || (h->tiles < 0 && R < KP_LEAST) || !kv_map_dims(s, c.K, c.D, caches, &m)) return w;
     w.tiles = (R + KP_ROWS - 1) / KP_ROWS;
     w.blocks = w.tiles * c.K * caches;
     w.nb = (s.rows + KP_KEYS - 1) / KP_KEYS;
     w.fit = w.blocks * w.nb < (1ll << 31);
+    w.elements = (R + 7) / 8 * c.K * caches * s.rows * c.D;
     return w;
 }
 
@@ -686,8 +695,9 @@ jpi_status kv_tiles_prepare(jpi_kv_handle* h) {
 }
 
 void kv_tiles_plan(const jpi_kv_handle* h, const KvCall& c, long long room, KvTilesPlan* plan) {
-    const TileWork p = work_of(h, c, false), o = work_of(h, c, true);
+    TileWork p = work_of(h, c, false), o = work_of(h, c, true);
     *plan = KvTilesPlan();
+    if (h->tiles < 0 && (p.fit ? p.elements : 0) + (o.fit ? o.elements : 0) <= KP_ROW_ELEMENTS) return;
     auto splits_most = [&](const TileWork& w) { return std::min({w.nb, room, std::max(1ll, 2ll * h->num_sms / w.blocks)}); };
     // The side of more work is split so that its blocks, or the waves of them, end first; the other to blocks no longer.
     const bool own_first = o.fit && (!p.fit || o.blocks * o.nb > p.blocks * p.nb);

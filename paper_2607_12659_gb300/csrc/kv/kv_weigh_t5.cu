@@ -241,11 +241,18 @@ jpi_status kv_weigh_prepare(jpi_kv_handle* h) {
     return JPI_OK;
 }
 
+// The row kernel reads a key once for every 8 query rows, and its warps take those one after the other. Up to 16 M elements
+// of keys read so it ends earlier, as long as the rows are not many: with 1 KV head at D = 256 and 16 own rows each,
+// 128 rows over 1024, 4096 and 8192 keys take 5.3, 6.3 and 8.5 us there and 5.9, 6.0 and 6.1 here; 256 over 512 and 4096
+// keys 6.8 and 8.7, here 7.1 and 7.2; 512 over 16 keys 9.5 and 7.0. Of fewer than 64 rows a tile is mostly empty: 32 rows over
+// 16384 keys of 8 KV heads at D = 128 take 21 us there and 27 here.
 bool kv_weigh_tiles(const jpi_kv_handle* h, const KvCall& c) {
     if (!h->bf16 || c.D < 64 || c.prefix.rows == 0) return false;
     KvMapDims m;
     const long long R = (long long)(c.batch / c.groups) * c.tokens * c.gq;
-    return R >= 64 && kv_map_dims(c.prefix, c.K, c.D, c.groups, &m) &&
+    const long long elements = (R + 7) / 8 * c.K * c.groups * c.prefix.rows * c.D;
+    const bool take = h->tiles < 0 ? R >= 64 && (R >= 512 || elements > 16ll << 20) : h->tiles == 1;
+    return take && kv_map_dims(c.prefix, c.K, c.D, c.groups, &m) &&
            (long long)((c.prefix.rows + WT_KEYS - 1) / WT_KEYS) * c.K * c.groups <= 0x7fffffffll / 8;
 }
 
@@ -260,7 +267,8 @@ jpi_status launch_kv_weigh_t5(jpi_kv_handle* h, const KvCall& c, const float* ls
     a.tiles = (c.prefix.rows + WT_KEYS - 1) / WT_KEYS;
     a.by_tiles = KvDiv((uint32_t)a.tiles);
     a.err = h->dev_err;
-    // Few keys and many rows: a row tile is 1.5 us of a block, one after the other.
+    // Few keys and many rows: a row tile is 1.5 us of a block, one after the other, unless a cluster shares them. 1440
+    // rows over 8 keys: 21 us by one block, 9 us by eight.
     const long long blocks = (long long)a.tiles * c.K * c.groups;
     const long long nt = ((long long)(c.batch / c.groups) * c.tokens * c.gq + WT_ROWS - 1) / WT_ROWS;
     a.ranks = 1;

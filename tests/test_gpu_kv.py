@@ -26,6 +26,13 @@ def kv():
     return kv
 
 
+@pytest.fixture(params=["by size", "1"])
+def tiles(request, monkeypatch):
+    """Kernels chosen by size, and the tensor-core tiles also where a call is too small for them."""
+    if request.param == "1":
+        monkeypatch.setenv("JPI_KV_TILES", "1")
+
+
 DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
 HALF_EPS = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}
 
@@ -222,6 +229,7 @@ SHAPES = [(8, 1, 256), (4, 1, 64), (8, 8, 128), (32, 8, 128), (6, 2, 80), (14, 2
           (16, 1, 256), (3, 1, 160)]
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("H,K,D", SHAPES)
 def test_attend_head_shapes(kv, dtype, H, K, D):
@@ -229,6 +237,7 @@ def test_attend_head_shapes(kv, dtype, H, K, D):
     check_attend(kv, dtype, H, K, D, 4, 5, 2, 33, 18, seed=H + 1, mask="any")
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("P,R", [(1, 0), (0, 1), (1, 1), (15, 17), (16, 16), (63, 0), (64, 3), (65, 1), (129, 0), (816, 51),
                                  (1000, 0), (0, 300), (2049, 5)])
@@ -236,12 +245,14 @@ def test_attend_lengths(kv, dtype, P, R):
     check_attend(kv, dtype, 8, 1, 128, 2, 3, 1, P, R, seed=P + R)
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("mask", ["causal", "context", "any"])
 @pytest.mark.parametrize("B,T,G", [(1, 1, 1), (2, 51, 1), (6, 7, 3), (8, 16, 4), (5, 40, 5), (33, 2, 1), (64, 4, 2)])
 def test_attend_batches_and_masks(kv, mask, B, T, G):
     check_attend(kv, "bf16", 8, 1, 64, B, T, G, 100, 60, seed=B + T, mask=mask)
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("H,K,D,B,T,G,P,R", [
     (8, 1, 256, 2, 100, 1, 130, 300), (16, 2, 128, 3, 64, 3, 70, 1000), (4, 1, 64, 2, 33, 1, 5, 129), (8, 1, 256, 1, 300, 1, 0, 700),
     (8, 1, 256, 16, 1, 1, 816, 40), (8, 1, 256, 40, 1, 1, 333, 9), (8, 1, 256, 4, 51, 2, 200, 51), (8, 1, 128, 32, 1, 1, 700, 5),
@@ -250,6 +261,7 @@ def test_attend_many_rows_on_one_prefix(kv, H, K, D, B, T, G, P, R):
     check_attend(kv, "bf16", H, K, D, B, T, G, P, R, seed=B)
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("H,K,D,B,T,P,R", [(8, 1, 256, 64, 1, 4096, 300), (8, 1, 256, 64, 1, 16384, 512), (32, 8, 128, 48, 1, 4000, 100),
                                             (8, 1, 64, 64, 2, 8000, 0), (8, 2, 256, 9, 16, 2100, 700)])
 def test_attend_long_prefix_many_rows(kv, H, K, D, B, T, P, R):
@@ -261,6 +273,7 @@ def test_attend_long_prefix_many_rows(kv, H, K, D, B, T, P, R):
         assert torch.equal(out, again) and torch.equal(lse, lse2), "two runs differ"
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("store", [head_major, padded])
 def test_attend_cache_layouts(kv, dtype, store):
@@ -268,12 +281,14 @@ def test_attend_cache_layouts(kv, dtype, store):
     check_attend(kv, dtype, 8, 2, 256, 40, 2, 1, 190, 30, seed=4, store=store)
 
 
+@pytest.mark.usefixtures("tiles")
 def test_attend_scale_and_large_scores(kv):
     check_attend(kv, "bf16", 8, 1, 64, 2, 2, 1, 120, 10, seed=1, scale=0.02)
     check_attend(kv, "bf16", 8, 1, 128, 20, 1, 1, 300, 10, seed=2, std=30.0)
     check_attend(kv, "fp32", 2, 1, 64, 2, 2, 1, 120, 10, seed=3, std=30.0)
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("dtype,H,K,D,T,R", [("fp32", 8, 1, 64, 6, 12), ("bf16", 2, 1, 64, 6, 12), ("bf16", 8, 1, 64, 6, 12),
                                              ("bf16", 8, 1, 256, 40, 150), ("bf16", 16, 2, 128, 70, 300), ("bf16", 8, 1, 96, 20, 70),
                                              ("bf16", 4, 4, 64, 50, 200)])
@@ -306,6 +321,7 @@ def test_attend_a_bad_value_reaches_only_the_queries_that_see_it(kv, dtype, H, K
             within(clean, np.where(hit, 0.0, ref), np.where(hit, 0.0, tol), f"value {bad} in row {at}")
 
 
+@pytest.mark.usefixtures("tiles")
 def test_attend_lowest_values_and_lengths_out_of_range(kv):
     # Scores of the type's lowest value are values; lengths outside a cache are taken as its ends.
     q = torch.full((1, 1, 1, 8), torch.finfo(torch.bfloat16).max, dtype=torch.bfloat16, device="cuda")
@@ -351,23 +367,27 @@ def check_weigh(kv, dtype, H, K, D, B, T, G, P, R, seed=0, decay=0.75, with_in=T
     return h, c, lse, got
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("H,K,D", SHAPES)
 def test_weigh_head_shapes(kv, dtype, H, K, D):
     check_weigh(kv, dtype, H, K, D, 4, 3, 2, 45, 18, seed=H, mask="any")
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("P,R", [(1, 0), (0, 1), (15, 17), (64, 3), (127, 0), (129, 4), (816, 51), (0, 300)])
 def test_weigh_lengths(kv, P, R):
     check_weigh(kv, "bf16", 8, 1, 128, 2, 3, 1, P, R, seed=P)
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("H,K,D,B,T,G,P,R", [(8, 1, 256, 40, 1, 1, 333, 9), (8, 1, 256, 1, 32, 1, 500, 32), (32, 8, 128, 48, 1, 1, 450, 33),
                                              (16, 16, 64, 64, 2, 1, 260, 12), (8, 1, 64, 33, 4, 3, 130, 7), (8, 1, 256, 24, 3, 2, 90, 0)])
 def test_weigh_many_rows(kv, H, K, D, B, T, G, P, R):
     check_weigh(kv, "bf16", H, K, D, B, T, G, P, R, seed=B, decay=1.0)
 
 
+@pytest.mark.usefixtures("tiles")
 @pytest.mark.parametrize("H,K,D,B,T,G,P,R", [(8, 1, 256, 5, 36, 1, 8, 40), (8, 1, 256, 4, 80, 2, 700, 0), (16, 2, 128, 9, 31, 1, 130, 3),
                                              (8, 1, 64, 130, 1, 1, 129, 1), (4, 1, 80, 3, 100, 3, 1, 5), (8, 2, 256, 48, 17, 3, 300, 7)])
 def test_weigh_few_keys_many_rows(kv, H, K, D, B, T, G, P, R):
@@ -376,6 +396,7 @@ def test_weigh_few_keys_many_rows(kv, H, K, D, B, T, G, P, R):
 
 
 
+@pytest.mark.usefixtures("tiles")
 def test_weigh_in_place_no_input_and_decay_zero(kv):
     check_weigh(kv, "bf16", 8, 2, 64, 2, 3, 1, 40, 9, with_in=False)
     h, c, lse, got = check_weigh(kv, "bf16", 8, 2, 64, 2, 3, 1, 40, 9, decay=0.5)
@@ -516,6 +537,7 @@ def test_a_decode_loop_with_eviction(kv):
     h.device_status()
 
 
+@pytest.mark.usefixtures("tiles")
 def test_calls_on_another_stream_and_in_a_graph(kv):
     H, K, D, B = 8, 1, 128, 12
     h = kv.KV(H, K, D, max_batch=B, rope=kv.Rope(dim=D))
