@@ -186,10 +186,12 @@ __global__ void __launch_bounds__(WT_THREADS, 1) k_kv_weigh_t5(const __grid_cons
             for (int k = 0; k < 16; ++k) {
                 const float4 n = nl[k];
                 const uint32_t* x = s[k >> 2] + 4 * (k & 3);
-                acc[0] += kr_ex2(fmaf(__uint_as_float(x[0]), a.c.scale, n.x) * KR_LOG2E);
-                acc[1] += kr_ex2(fmaf(__uint_as_float(x[1]), a.c.scale, n.y) * KR_LOG2E);
-                acc[2] += kr_ex2(fmaf(__uint_as_float(x[2]), a.c.scale, n.z) * KR_LOG2E);
-                acc[3] += kr_ex2(fmaf(__uint_as_float(x[3]), a.c.scale, n.w) * KR_LOG2E);
+                const float m[4] = {n.x, n.y, n.z, n.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float w = kr_ex2(fmaf(__uint_as_float(x[e]), a.c.scale, m[e]) * KR_LOG2E);
+                    acc[e] += m[e] == -INFINITY ? 0.f : w;   // (whatever such a row's query holds)
+                }
             }
             ptx::tc_fence_before();
             // Scores and -lse of this buffer are read: the next tile but one may take both.

@@ -397,6 +397,24 @@ def test_weigh_few_keys_many_rows(kv, H, K, D, B, T, G, P, R):
 
 
 @pytest.mark.usefixtures("tiles")
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_weigh_leaves_out_rows_without_a_sum(kv, dtype):
+    """An lse of -infinity marks a row that saw nothing: it weighs nothing, whatever its query holds."""
+    B, T, H, D = 3, 50, 8, 64
+    c = make_call(3, dtype, H, 1, D, B, T, 1, 200, 60, mask="any")
+    out, lse = kv.KV(H, 1, D, max_batch=B, max_tokens=T, precision=dtype).attend(**c)
+    h = kv.KV(H, 1, D, max_batch=B, max_tokens=T, precision=dtype)
+    c["prefix"], c["own"] = c["prefix"][0], c["own"][0]
+    gone = torch.rand((B, T, 1), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda") < 0.4
+    lse = torch.where(gone, torch.full_like(lse, -math.inf), lse)
+    want = h.weigh(lse=lse, **dict(c, q=torch.where(gone[..., None], torch.zeros_like(c["q"]), c["q"])))
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        got = h.weigh(lse=lse, **dict(c, q=torch.where(gone[..., None], torch.full_like(c["q"], bad), c["q"])))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert want[0].isfinite().all() and want[0].sum() > 0
+
+
+@pytest.mark.usefixtures("tiles")
 def test_weigh_in_place_no_input_and_decay_zero(kv):
     check_weigh(kv, "bf16", 8, 2, 64, 2, 3, 1, 40, 9, with_in=False)
     h, c, lse, got = check_weigh(kv, "bf16", 8, 2, 64, 2, 3, 1, 40, 9, decay=0.5)
