@@ -192,6 +192,8 @@ JPI_API jpi_status jpi_commit_prefix(jpi_handle* h, int batch, int prefix_len);
  *   (prefix_len .. max_prefix) instead of prefix_len, for a store that was cut outside these calls.
  */
 JPI_API jpi_status jpi_share_prefix(jpi_handle* h, int requests);
+/* The stored prefix: how many, tokens of each, the rotary position that follows them. */
+JPI_API jpi_status jpi_prefix_shape(const jpi_handle* h, int* batch, int* prefix_len, int* position);
 JPI_API jpi_status jpi_weigh_prefix(jpi_handle* h, const float* state, const float* x_t, float t, int batch,
                                     int chunk, float decay, float* w, void* stream);
 JPI_API jpi_status jpi_evict_prefix(jpi_handle* h, float* w, int keep, int sink, int recent, int* kept,

@@ -536,6 +536,16 @@ JPI_API jpi_status jpi_share_prefix(jpi_handle* h, int requests) {
     return JPI_OK;
 }
 
+JPI_API jpi_status jpi_prefix_shape(const jpi_handle* h, int* batch, int* prefix_len, int* position) {
+    clear_error();
+    if (!h || !batch || !prefix_len || !position) return fail(JPI_ERR_INVALID_ARG, "NULL argument");
+    if (!h->prefix_ready) return fail(JPI_ERR_NOT_READY, "no prefix KV has been set");
+    *batch = h->cur_batch;
+    *prefix_len = h->cur_prefix;
+    *position = h->cur_prefix + static_cast<const PrefixHandle*>(h)->shift;
+    return JPI_OK;
+}
+
 JPI_API jpi_status jpi_weigh_prefix(jpi_handle* h, const float* state, const float* x_t, float t, int batch, int chunk,
                                     float decay, float* w, void* stream) {
     clear_error();

@@ -71,6 +71,7 @@ jpi_status expert_kv_create(jpi_handle* h, ExpertKv* e) {
     rope.mscale = 1.f;
     JPI_TRY(jpi_kv_create(&cfg, h->cfg.rope_base >= 1.f ? &rope : nullptr, &e->kv));
     e->kv->pdl = h->pdl;
+    e->kv->dev_err = h->dev_err;   // what its kernels report is the expert's status
     const size_t ints = (size_t)h->maxB * h->maxS + h->maxB + 2 * (size_t)h->maxB * h->maxP + (size_t)h->L * h->maxB * h->maxP;
     const size_t bytes = ints * sizeof(int) + (size_t)h->maxMt * h->H * sizeof(float);
     void* p = nullptr;

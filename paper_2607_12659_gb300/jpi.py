@@ -64,6 +64,7 @@ _SIGS = {
     "jpi_prefix_kv_ptr": [c_void_p, c_int, POINTER(c_void_p), POINTER(c_void_p), POINTER(c_longlong)],
     "jpi_commit_prefix": [c_void_p, c_int, c_int],
     "jpi_share_prefix": [c_void_p, c_int],
+    "jpi_prefix_shape": [c_void_p, POINTER(c_int), POINTER(c_int), POINTER(c_int)],
     "jpi_weigh_prefix": [c_void_p, c_void_p, c_void_p, c_float, c_int, c_int, c_float, c_void_p, c_void_p],
     "jpi_evict_prefix": [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p],
     "jpi_append_prefix": [c_void_p, c_void_p, c_void_p, c_int, c_void_p],
@@ -230,6 +231,12 @@ def jpi_share_prefix(h, requests):
     _check(load().jpi_share_prefix(h, requests), "jpi_share_prefix")
 
 
+def jpi_prefix_shape(h) -> tuple[int, int, int]:
+    b, p, at = c_int(), c_int(), c_int()
+    _check(load().jpi_prefix_shape(h, byref(b), byref(p), byref(at)), "jpi_prefix_shape")
+    return b.value, p.value, at.value
+
+
 def jpi_weigh_prefix(h, state, x_t, t, batch, chunk, decay, w, stream=None):
     _check(load().jpi_weigh_prefix(h, _ptr(state), _ptr(x_t), float(t), batch, chunk, float(decay), _ptr(w),
                                    _stream(stream)), "jpi_weigh_prefix")
@@ -367,11 +374,21 @@ class Expert:
         """Each stored prefix serves `requests` consecutive requests of a call (1: one each)."""
         jpi_share_prefix(self.handle, requests)
 
+    def prefix_shape(self) -> tuple[int, int, int]:
+        """(batch, tokens, rotary position that follows them) of the stored prefix."""
+        return jpi_prefix_shape(self.handle)
+
+    def _weights(self, w):
+        """`w` as weights of the stored prefix's keys: what the C-ABI cannot see."""
+        import torch
+        want = (self.dims.n_layers, *self.prefix_shape()[:2])
+        if not (w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.shape == want):
+            raise ValueError(f"w must be a contiguous CUDA float32 tensor {list(want)}, not {w.dtype} {list(w.shape)} on {w.device}")
+
     def weigh_prefix(self, state, x_t, t, w, decay=1.0, stream=None):
         """w [L][prefix batch][prefix length] (CUDA float32) = decay w + the attention weight each prefix key receives in
         one expert evaluation."""
-        import torch
-        assert w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.shape[0] == self.dims.n_layers
+        self._weights(w)
         B, C, _ = x_t.shape
         with OnStream(stream, x_t.device) as on:
             on.reads(state, x_t, w)
@@ -382,10 +399,10 @@ class Expert:
         """Cuts every stored prefix to `keep` tokens by the weights w (as weigh_prefix gives them; moved with the keys).
         Returns the tokens that stay, int32 [L][prefix batch][keep]."""
         import torch
-        assert w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.dim() == 3 and w.shape[0] == self.dims.n_layers
+        self._weights(w)
         with OnStream(stream, w.device) as on:
             on.reads(w)
-            kept = torch.empty((*w.shape[:2], max(keep, 0)), dtype=torch.int32, device=w.device)
+            kept = torch.empty((*w.shape[:2], min(max(keep, 0), w.shape[2])), dtype=torch.int32, device=w.device)
             on.returns(kept)
         jpi_evict_prefix(self.handle, w, keep, sink, recent, kept, stream)
         return kept
@@ -395,8 +412,11 @@ class Expert:
         position code."""
         import torch
         want = torch.float32 if self.cfg.precision == JPI_FP32 else torch.bfloat16
-        assert k.is_cuda and v.is_cuda and k.shape == v.shape and k.dtype == want and v.dtype == want
-        assert k.shape[0] == self.dims.n_layers and k.shape[3] == self.dims.head_dim
+        for t in (k, v):
+            if not (t.is_cuda and t.dtype == want and t.dim() == 4 and t.shape == k.shape and t.shape[0] == self.dims.n_layers
+                    and t.shape[1] == self.prefix_shape()[0] and t.shape[3] == self.dims.head_dim):
+                raise ValueError(f"k and v must be CUDA {want} tensors [{self.dims.n_layers}][{self.prefix_shape()[0]}][tokens]"
+                                 f"[{self.dims.head_dim}], not {t.dtype} {list(t.shape)} on {t.device}")
         with OnStream(stream, k.device) as on:
             on.reads(k, v)
             k = k.contiguous()

@@ -229,6 +229,15 @@ def test_refusals(monkeypatch):
         with pytest.raises(jpi.JpiError):
             ex.denoise(state, noise, 1)                    # two prefixes, two requests each: four are wanted
         ex.share_prefix(1)
+        assert ex.prefix_shape() == (2, 30, 30)
+        for bad in (weights[:, :1], weights[..., :29].contiguous(), weights[:1], weights.double(), weights.cpu(), weights.transpose(0, 1)):
+            with pytest.raises(ValueError):                # too small for the stored prefix, or no block of fp32
+                ex.weigh_prefix(state, noise, 0.0, bad)
+            with pytest.raises(ValueError):
+                ex.evict_prefix(bad, 5)
+        for bad in (k[:, :1, :1], k[:1, :, :1], k[:, :, :1, :-8], k[:, :, :1].double(), k[:, :, :1].cpu()):
+            with pytest.raises(ValueError):
+                ex.append_prefix(bad, bad)
         assert_close(gpu_denoise(ex, TINY, r, 2), oracle_denoise(TINY, w, r, 2), TINY, "after the refusals")
     finally:
         ex.close()
