@@ -24,6 +24,7 @@ jpi_status fail(jpi_status s, const char* fmt, ...) {
 }
 
 jpi_status kv_alloc(jpi_kv_handle* h, void** p, size_t bytes) {
+    h->allocations.reserve(h->allocations.size() + 1);   // (may throw, so before there is something to lose)
     cudaError_t e = cudaMalloc(p, bytes ? bytes : 16);
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -222,7 +223,12 @@ JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* ro
         JPI_TRY(kv_weigh_prepare(h));
         return kv_attend_prepare(h);
     };
-    const jpi_status s = setup();
+    jpi_status s;
+    try {
+        s = setup();
+    } catch (const std::bad_alloc&) {
+        s = fail(JPI_ERR_OOM, "host allocation failed");
+    }
     if (s != JPI_OK) {
         free_kv(h);
         return s;

@@ -25,8 +25,6 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
 
 }  // namespace
 
-bool kv_maps_available() { return encode_fn() != nullptr; }
-
 bool kv_map_dims(const KvSide& s, int K, int D, int n, KvMapDims* m) {
     struct Dim {
         long long stride;

@@ -11,8 +11,6 @@ struct KvMapDims {
     int at_head = 0, at_row = 0, at_cache = 0;   // which outer dimension is which
 };
 
-// Whether tensor maps can be built in this process.
-bool kv_maps_available();
 // The dimensions of `n` caches of this side, K heads of D bf16 elements. False where the strides are not those that
 // maps are documented for (each a multiple of the one before, below 2^40 bytes).
 bool kv_map_dims(const KvSide& s, int K, int D, int n, KvMapDims* m);

@@ -17,7 +17,6 @@ namespace jpi {
 namespace {
 
 constexpr int KR_ROWS = 8;    // query rows of a warp
-constexpr int KR_KEYS = 16;   // keys of a warp's step (bf16)
 
 // Where a warp's query rows live.
 struct RowTile {
