@@ -13,8 +13,8 @@
 // values would overflow.
 //
 // Kernels: the row kernels here take both sides, 8 query rows a warp; a side with many query rows on the same keys
-// (from 32) goes to tiles of 128 rows instead (kv_attend_t5.cu), bound by tensor cores and 2^x where the row kernel is bound by
-// memory, so the two share the SMs: the row kernel starts first with two blocks per SM, the tiles start while it
+// goes to tiles of 128 rows instead (kv_attend_t5.cu) where the call is large, bound by tensor cores and 2^x where the row kernel is
+// bound by memory, so the two share the SMs: the row kernel starts first with two blocks per SM, the tiles start while it
 // runs. k_kv_combine joins the parts, except where a row has only one.
 
 #include "kv_rows.cuh"
@@ -102,16 +102,17 @@ struct RowAcc {
     }
 };
 
-// Joins parts first, first + step, .. of a row (of `parts`) to `r`, which holds nothing yet, relative to their largest
-// maximum. The loads of JOIN parts are in flight together: they are made whether the part weighs anything or not (its
-// memory is the workspace's), and a part of no weight, which may never have been written, is replaced by zeros.
+// Joins elements d0 .. d0 + DP - 1 of parts first, first + step, .. of a row (of `parts`) to `r`, which holds nothing yet,
+// relative to their largest maximum. The loads of JOIN parts are in flight together: they are made whether the part weighs
+// anything or not (its memory is the workspace's), and a part of no weight, which may never have been written, is replaced
+// by zeros.
 template <int DP>
-__device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, long long row, int first, int step, int lane) {
+__device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, long long row, int d0, int first, int step, int lane) {
     constexpr int NI = RowAcc<DP>::NI, JOIN = 16 / NI;
     const float2* pml = a.pml + row * a.parts;
     int d[NI];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) d[i] = 4 * lane + 128 * i < a.c.D ? 4 * lane + 128 * i : 0;
+    for (int i = 0; i < NI; ++i) d[i] = d0 + 4 * lane + 128 * i < a.c.D ? d0 + 4 * lane + 128 * i : 0;
     const int mine = (a.parts - first + step - 1) / step;   // parts of this warp
     for (int p0 = 0; p0 < mine; p0 += 32) {
         const int n = min(32, mine - p0);
@@ -152,14 +153,14 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, l
     }
 }
 
-// The row's result from its joined sums.
+// The row's result from its joined sums, elements from d0 on.
 template <int DP, typename E>
-__device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>& r, long long row, int lane) {
+__device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>& r, long long row, int d0, int lane) {
     const float inv = r.l > 0.f ? 1.f / r.l : 0.f;   // (a NaN sum comes with NaN outputs)
     E* out = static_cast<E*>(a.out) + row * a.c.D;
 #pragma unroll
     for (int i = 0; i < RowAcc<DP>::NI; ++i) {
-        const int d = 4 * lane + 128 * i;
+        const int d = d0 + 4 * lane + 128 * i;
         if (d >= a.c.D) continue;
         const float4 v = make_float4(r.o[i].x * inv, r.o[i].y * inv, r.o[i].z * inv, r.o[i].w * inv);
         if constexpr (sizeof(E) == 2)
@@ -167,7 +168,7 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>&
         else
             *(float4*)(out + d) = v;
     }
-    if (lane == 0 && a.lse) a.lse[row] = r.m == -INFINITY ? -INFINITY : fmaf(r.m, a.c.scale, logf(r.l));
+    if (d0 == 0 && lane == 0 && a.lse) a.lse[row] = r.m == -INFINITY ? -INFINITY : fmaf(r.m, a.c.scale, logf(r.l));
 }
 
 // Joins the key warps of each row tile (their outputs and (m, l) are in shared memory) and writes the part, or, where
@@ -205,7 +206,7 @@ __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece
             acc.add(w, v);
         }
         if (a.out) {
-            write_row<DP, float>(a, acc, row, lane);
+            write_row<DP, float>(a, acc, row, 0, lane);
             continue;
         }
         const long long at = x.part * a.rows + row;
@@ -709,14 +710,18 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
     merge_and_write<DP>(a, x, sp, kv_smem, warp, lane);
 }
 
-// Joins the parts of all rows: `wpr` warps (a power of two) a row, each with every wpr-th part, then the warps in order.
+// Joins the parts of all rows, DP elements of one (from DP blockIdx.y on) by `wpr` warps (a power of two), each with every
+// wpr-th part, then the warps in order. Latency bounds it: 16 loads of a lane are on their way together, and where the rows are few
+// a row of more than 128 elements is two blocks'. (One request over 65536 keys, 760 parts of 256 elements, took 28 us with
+// both halves in one warp and 25 so; 48 requests of 32 heads with 30011 shared keys 58 with up to four warps a row and 55
+// with as many as are resident together; 16 x 10 tokens of 8 heads in 2 parts 11.1 with the halves apart, 9.6 together.)
 constexpr int CB_WARPS = 16;   // most of a block
 template <int DP, typename E>
 __global__ void __launch_bounds__(32 * CB_WARPS) k_kv_combine(const __grid_constant__ AttendArgs a, int wpr) {
     __shared__ float4 so[CB_WARPS][RowAcc<DP>::NI][32];
     __shared__ float2 sml[CB_WARPS];
     constexpr int NI = RowAcc<DP>::NI;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp & (wpr - 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp & (wpr - 1), d0 = DP * blockIdx.y;
     const long long row = ((long long)blockIdx.x * (blockDim.x >> 5) + warp) / wpr;
     ptx::grid_dep_wait();
     RowAcc<DP> acc;
@@ -724,7 +729,7 @@ __global__ void __launch_bounds__(32 * CB_WARPS) k_kv_combine(const __grid_const
     acc.l = 0.f;
 #pragma unroll
     for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row < a.rows) join_parts<DP>(a, acc, row, first, wpr, lane);
+    if (row < a.rows) join_parts<DP>(a, acc, row, d0, first, wpr, lane);
     if (wpr > 1) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) so[warp][i][lane] = acc.o[i];
@@ -733,13 +738,12 @@ __global__ void __launch_bounds__(32 * CB_WARPS) k_kv_combine(const __grid_const
         if (first != 0) return;
         float M = acc.m;
         for (int k = 1; k < wpr; ++k) M = fmaxf(M, sml[warp + k].x);
-        const float m = acc.m;
         acc.m = M;
         acc.l = 0.f;
 #pragma unroll
         for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k = 0; k < wpr; ++k) {
-            const float2 ml = k == 0 ? make_float2(m, sml[warp].y) : sml[warp + k];
+            const float2 ml = sml[warp + k];
             const float w = ml.x == -INFINITY ? 0.f : kr_ex2((ml.x - M) * a.c2);
             float4 v[NI];
 #pragma unroll
@@ -748,7 +752,7 @@ __global__ void __launch_bounds__(32 * CB_WARPS) k_kv_combine(const __grid_const
             acc.l += w * ml.y;
         }
     }
-    if (row < a.rows) write_row<DP, E>(a, acc, row, lane);
+    if (row < a.rows) write_row<DP, E>(a, acc, row, d0, lane);
 }
 
 // Rows of partial outputs the workspace holds.
@@ -830,14 +834,15 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
     if (beside) JPI_TRY(launch_kv_tiles_t5(h, c, tiles, part0, a.po, a.pml, parts, out, lse, pieces > 0 && h->pdl, st));
     if (parts == 1) return JPI_OK;
     a.out = out;
-    // A warp has the loads of 8 parts (16 to D = 128) in flight: warps for as many batches, to four a row, or where the
-    // rows are few to sixteen.
+    // Warps for 8 to 16 parts each, to sixteen, as long as all are resident together (16 an SM).
+    const int slices = c.D > 128 && a.rows * 2 <= 16ll * h->num_sms ? 2 : 1;
     int wpr = 1;
-    while (wpr < (a.rows <= 64 ? CB_WARPS : 4) && wpr * 8 < parts) wpr *= 2;
+    while (wpr < CB_WARPS && wpr * 8 < parts && a.rows * slices * wpr * 2 <= 16ll * h->num_sms) wpr *= 2;
     const int warps = std::max(wpr, AT_WARPS);
-    const long long grid = (a.rows * wpr + warps - 1) / warps;
-    return h->bf16 ? kv_start(k_kv_combine<DP, __nv_bfloat16>, grid, 32 * warps, 0, h->pdl, st, a, wpr)
-                   : kv_start(k_kv_combine<DP, float>, grid, 32 * warps, 0, h->pdl, st, a, wpr);
+    const dim3 grid((unsigned)((a.rows * wpr + warps - 1) / warps), (unsigned)slices);
+    const bool wide = DP == 256 && slices == 1;
+    return kv_start(h->bf16 ? (wide ? k_kv_combine<256, __nv_bfloat16> : k_kv_combine<128, __nv_bfloat16>)
+                            : (wide ? k_kv_combine<256, float> : k_kv_combine<128, float>), grid, 32 * warps, 0, h->pdl, st, a, wpr);
 }
 
 template <int DP>

@@ -48,7 +48,12 @@ constexpr int KP_KEYS = 64;
 constexpr int KP_SOFT = 256;   // threads of a softmax group
 constexpr uint64_t KP_WAIT_NS = 200ull * 1000 * 1000;
 constexpr float KP_RESCALE = 8.f;   // log2 units
-constexpr int KP_LEAST = 32;        // query rows from which a side takes the tiles
+// Query rows from which a side takes the tiles: 32, and of a prefix at D > 128, where a step of the row kernel is 16 keys
+// only, as soon as that reads the keys twice. Microseconds of row kernel and tiles: 24 rows over 16384 and 65536 keys of
+// 8 KV heads at D = 128 25.1 65.9 and 25.5 53.4, 32 rows 30.2 85.6 and 23.2 54.0; 16 rows over 32768 keys of one KV
+// head at D = 256 19.4 and 14.0, 8 rows 14.9 and 14.1; 64 requests' own 2048 and 8192 rows at 8 query rows each 29.4
+// 86.5 and 29.0 83.1.
+constexpr int kp_least(bool own, int D) { return !own && D > 128 ? 9 : 32; }
 // Elements of keys up to which a call stays with the row kernel, which reads a key once for every 8 query rows but has
 // neither the tiles' long start nor their query rows to turn. Microseconds of row kernel and tiles where 16 own rows come with it:
 // 1 KV head at D = 256, 256 rows over 64, 512, 1024 and 2048 keys (0.5, 4, 8 and 17 M elements): 8.2 11.3 11.8 17.4 and
@@ -666,7 +671,7 @@ TileWork work_of(const jpi_kv_handle* h, const KvCall& c, bool own) {
     const int caches = own ? c.batch : c.groups;
     const long long R = (long long)(own ? 1 : c.batch / c.groups) * c.tokens * c.gq;
     KvMapDims m;
-    if (h->tiles == 0 || (h->tiles < 0 && R < KP_LEAST) || !kv_map_dims(s, c.K, c.D, caches, &m)) return w;
+    if (h->tiles == 0 || (h->tiles < 0 && R < kp_least(own, c.D)) || !kv_map_dims(s, c.K, c.D, caches, &m)) return w;
     w.tiles = (R + KP_ROWS - 1) / KP_ROWS;
     w.blocks = w.tiles * c.K * caches;
     w.nb = (s.rows + KP_KEYS - 1) / KP_KEYS;
