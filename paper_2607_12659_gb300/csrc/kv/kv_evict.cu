@@ -6,7 +6,9 @@
 // 11, 11 and 10 bits, a histogram in shared memory each: exact, whatever the distribution. Above the
 // threshold every row stays; of the rows equal to it the lowest, as many as are left. Each thread has a
 // run of consecutive rows (in registers up to 16), one block-wide scan gives every run its place, and the kept rows
-// come out ascending.
+// come out ascending. Its time is that of barriers and latencies, so every warp finds the bin, and its place, from sums that
+// all of them read: 8 barriers where a block-wide scan in each pass took 25 (18 layers of 816 rows 8.8 us a call, then
+// 9.7).
 //
 // The move (k_kv_gather): a block takes a slice (16 to 512 bytes, whole rows where there are blocks enough) of every
 // kept row of one cache, head and matrix, in tiles of ascending rows: a tile is loaded whole, then stored. In place this
@@ -32,48 +34,35 @@ __device__ __forceinline__ uint32_t sort_key(float w) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Exclusive sums of (x, y) over the block's threads in order; `tot` gets the whole sums.
-__device__ __forceinline__ uint2 block_scan(uint2 v, uint2* warp_sums, uint2* tot) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint2 s = v;
+// Inclusive sums over the warp's lanes.
+__device__ __forceinline__ uint32_t warp_scan(uint32_t x) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, s.x, o), y = __shfl_up_sync(0xffffffffu, s.y, o);
-        if (lane >= o) {
-            s.x += x;
-            s.y += y;
-        }
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
     }
+    return x;
+}
+// Exclusive sums of (x, y) over the block's threads in order; each warp adds up the warps before it by itself.
+__device__ __forceinline__ uint2 block_scan(uint2 v, uint2* warp_sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint2 s = make_uint2(warp_scan(v.x), warp_scan(v.y));
     if (lane == 31) warp_sums[warp] = s;
     __syncthreads();
-    if (warp == 0) {
-        uint2 t = warp_sums[lane];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t x = __shfl_up_sync(0xffffffffu, t.x, o), y = __shfl_up_sync(0xffffffffu, t.y, o);
-            if (lane >= o) {
-                t.x += x;
-                t.y += y;
-            }
-        }
-        warp_sums[lane] = t;
-    }
-    __syncthreads();
-    const uint2 before = warp ? warp_sums[warp - 1] : make_uint2(0, 0);
-    *tot = warp_sums[SEL_THREADS / 32 - 1];
-    __syncthreads();   // warp_sums may be used again
-    return make_uint2(before.x + s.x - v.x, before.y + s.y - v.y);
+    const uint2 w = lane < warp ? warp_sums[lane] : make_uint2(0, 0);
+    return make_uint2(__reduce_add_sync(0xffffffffu, w.x) + s.x - v.x, __reduce_add_sync(0xffffffffu, w.y) + s.y - v.y);
 }
 
-// RUN: rows of a thread, its keys in registers; 0: any number, read again in every pass.
+// RUN: rows of a thread, their weights in registers; 0: any number, read again in every pass.
 template <int RUN>
 __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, const int* length, int rows, int caches,
                                                            int K, int keep, int sink, int recent, int dst_rows,
                                                            float* w_out_all, int* kept_all) {
-    __shared__ uint32_t hist[SEL_BINS];
+    __shared__ __align__(8) uint32_t hist[3][SEL_BINS];      // of each pass, the largest digit first
+    __shared__ uint32_t bin_sums[3][SEL_THREADS / 32];       // of 64 bins each
     __shared__ uint2 warp_sums[SEL_THREADS / 32];
-    __shared__ uint32_t found[2];   // chosen bin, rows still needed within it
-    const int t = threadIdx.x;
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     ptx::grid_dep_launch();
     const long long item = blockIdx.x;   // (layer, cache, head)
     const int c = (int)((item / K) % caches);
@@ -91,7 +80,7 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
     const int run = RUN > 0 ? RUN : (n + SEL_THREADS - 1) / SEL_THREADS;
     // The thread's rows r0 .. r1 - 1 (in registers from r0 = t RUN on, also past the end: aligned for loads of four).
     const int r0 = RUN > 0 ? t * RUN : min(n, t * run), r1 = min(n, r0 + run);
-    uint32_t keys[RUN > 0 ? RUN : 1];
+    float ws[RUN > 0 ? RUN : 1];
     if constexpr (RUN % 4 == 0 && RUN > 0) {
         const bool four = (reinterpret_cast<uintptr_t>(w) & 15) == 0;   // with r0 a multiple of 4
 #pragma unroll
@@ -105,20 +94,20 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
                 if (r0 + e + 2 < n) v.z = w[r0 + e + 2];
                 if (r0 + e + 3 < n) v.w = w[r0 + e + 3];
             }
-            keys[e] = sort_key(v.x);
-            keys[e + 1] = sort_key(v.y);
-            keys[e + 2] = sort_key(v.z);
-            keys[e + 3] = sort_key(v.w);
+            ws[e] = v.x;
+            ws[e + 1] = v.y;
+            ws[e + 2] = v.z;
+            ws[e + 3] = v.w;
         }
     } else if constexpr (RUN == 1) {
-        keys[0] = r0 < n ? sort_key(w[r0]) : 0u;
+        ws[0] = r0 < n ? w[r0] : 0.f;
     }
     // f(key) for the thread's share of rows lo .. hi - 1 (its run in registers, else strided: order does not matter).
     auto each = [&](int lo, int hi, auto f) {
         if constexpr (RUN > 0) {
 #pragma unroll
             for (int e = 0; e < RUN; ++e)
-                if (r0 + e >= lo && r0 + e < hi) f(keys[e]);
+                if (r0 + e >= lo && r0 + e < hi) f(sort_key(ws[e]));
         } else {
             for (int i = lo + t; i < hi; i += SEL_THREADS) f(sort_key(w[i]));
         }
@@ -129,33 +118,32 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
     uint32_t prefix = 0, mask = 0;   // keys with (key & mask) == prefix are still candidates
     if (need > 0) {
         const int shifts[3] = {21, 10, 0};
+        for (int i = t; i < 3 * SEL_BINS; i += SEL_THREADS) hist[0][i] = 0;
+        __syncthreads();
 #pragma unroll
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = shifts[pass];
-            const uint32_t bins = pass == 2 ? 1024u : 2048u;
-            hist[t] = 0;
-            hist[t + SEL_THREADS] = 0;
-            __syncthreads();
+            const uint32_t last = pass == 2 ? 1023u : 2047u;   // the largest digit
             each(lo, hi, [&](uint32_t k) {
-                if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+                if ((k & mask) == prefix) atomicAdd(&hist[pass][last - ((k >> shift) & last)], 1u);
             });
             __syncthreads();
-            // Bins from the top, two a thread.
-            const uint32_t b1 = SEL_BINS - 1 - 2 * t, n1 = hist[b1], n0 = hist[b1 - 1];
-            uint2 tot;
-            const uint32_t above = block_scan(make_uint2(n1 + n0, 0), warp_sums, &tot).x;
-            if (above < need && need <= above + n1) {
-                found[0] = b1;
-                found[1] = need - above;
-            } else if (above + n1 < need && need <= above + n1 + n0) {
-                found[0] = b1 - 1;
-                found[1] = need - above - n1;
-            }
+            // The bin that holds the need-th: each warp adds up 64 bins, then every warp finds the 64 and the bin by itself.
+            const uint2 own = *(const uint2*)&hist[pass][64 * warp + 2 * lane];
+            const uint32_t sum = __reduce_add_sync(0xffffffffu, own.x + own.y);
+            if (lane == 0) bin_sums[pass][warp] = sum;
             __syncthreads();
-            prefix |= found[0] << shift;
-            mask |= (bins - 1) << shift;
-            need = found[1];
-            __syncthreads();
+            const uint32_t part = bin_sums[pass][lane], upto = warp_scan(part);
+            const int seg = (__ffs(__ballot_sync(0xffffffffu, upto >= need)) - 1) & 31;   // (there is one)
+            const uint32_t before = __shfl_sync(0xffffffffu, upto - part, seg);
+            const uint2 two = *(const uint2*)&hist[pass][64 * seg + 2 * lane];
+            const uint32_t in = before + warp_scan(two.x + two.y);
+            const int at = (__ffs(__ballot_sync(0xffffffffu, in >= need)) - 1) & 31;
+            const uint32_t above = __shfl_sync(0xffffffffu, in - two.x - two.y, at), first = __shfl_sync(0xffffffffu, two.x, at);
+            const bool second = need > above + first;
+            prefix |= (last - (uint32_t)(64 * seg + 2 * at + second)) << shift;
+            mask |= last << shift;
+            need -= second ? above + first : above;
         }
     }
     // Rows that stay: protected or above the threshold (x), and `need` of those equal to it (y).
@@ -164,7 +152,7 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
         if (i < lo || i >= hi) return make_uint2(1, 0);
         return make_uint2(some && k > prefix, some && k == prefix);
     };
-    uint2 mine = make_uint2(0, 0), tot;
+    uint2 mine = make_uint2(0, 0);
     auto count = [&](int i, uint32_t k) {
         const uint2 x = kind(i, k);
         mine.x += x.x;
@@ -173,31 +161,38 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
     if constexpr (RUN > 0) {
 #pragma unroll
         for (int e = 0; e < RUN; ++e)
-            if (r0 + e < r1) count(r0 + e, keys[e]);
+            if (r0 + e < r1) count(r0 + e, sort_key(ws[e]));
     } else {
         for (int i = r0; i < r1; ++i) count(i, sort_key(w[i]));
     }
-    uint2 at = block_scan(mine, warp_sums, &tot);
+    uint2 at = block_scan(mine, warp_sums);
+    // Place of row i among the kept, or -1.
     auto place = [&](int i, uint32_t k) {
         const uint2 x = kind(i, k);
-        if (x.x || (x.y && at.y < need)) kept[at.x + min(at.y, need)] = i;
+        const int p = x.x || (x.y && at.y < need) ? (int)(at.x + min(at.y, need)) : -1;
         at.x += x.x;
         at.y += x.y;
+        if (p >= 0) kept[p] = i;
+        return p;
     };
     if constexpr (RUN > 0) {
+        // The weights go along from the registers: every one was read before the first barrier, so in place too.
 #pragma unroll
         for (int e = 0; e < RUN; ++e)
-            if (r0 + e < r1) place(r0 + e, keys[e]);
+            if (r0 + e < r1) {
+                const int p = place(r0 + e, sort_key(ws[e]));
+                if (p >= 0) w_out[p] = ws[e];
+            }
     } else {
         for (int i = r0; i < r1; ++i) place(i, sort_key(w[i]));
-    }
-    __syncthreads();
-    // The weights follow, in tiles: in place, a tile's stores come after its loads.
-    for (int i0 = 0; i0 < keep; i0 += SEL_THREADS) {
-        const int i = i0 + t;
-        const float x = i < keep ? w[kept[i]] : 0.f;
-        if (w_out == w) __syncthreads();
-        if (i < keep) w_out[i] = x;
+        __syncthreads();
+        // The weights follow in tiles: in place, a tile's stores come after its loads.
+        for (int i0 = 0; i0 < keep; i0 += SEL_THREADS) {
+            const int i = i0 + t;
+            const float x = i < keep ? w[kept[i]] : 0.f;
+            if (w_out == w) __syncthreads();
+            if (i < keep) w_out[i] = x;
+        }
     }
 }
 
