@@ -4,11 +4,12 @@
 // The choice (k_kv_select), one block per layer, cache and KV head. The weights, as unsigned keys of
 // the same order (NaN 0, below everything), are searched for the need-th largest by three passes over
 // 11, 11 and 10 bits, a histogram in shared memory each: exact, whatever the distribution. Above the
-// threshold every row stays; of the rows equal to it the lowest, as many as are left. Each thread has a
-// run of consecutive rows (in registers up to 16), one block-wide scan gives every run its place, and the kept rows
-// come out ascending. Its time is that of barriers and latencies, so every warp finds the bin, and its place, from sums that
-// all of them read: 8 barriers where a block-wide scan in each pass took 25 (18 layers of 816 rows 8.8 us a call, then
-// 9.7).
+// threshold every row stays; of the rows equal to it the lowest, as many as are left. Each warp has a
+// run of consecutive rows (in registers up to 512), so that ballots and one sum over the warps give every row its place, the kept
+// rows come out ascending and what a warp stores lies side by side (12 caches of 2513 rows: 10.6 us a call with a run per thread,
+// 9.6 so). Its time is that of barriers and latencies, so every warp finds the bin by itself, from sums that all of them
+// read: 8 barriers where a block-wide scan in each pass took 25 (18 caches of 816 rows 8.5 us a call, then 9.7). Of 16384
+// rows half of its 17 us is the first read of the weights.
 //
 // The move (k_kv_gather): a block takes a slice (16 to 512 bytes, whole rows where there are blocks enough) of every
 // kept row of one cache, head and matrix, in tiles of ascending rows: a tile is loaded whole, then stored. In place this
@@ -44,16 +45,6 @@ __device__ __forceinline__ uint32_t warp_scan(uint32_t x) {
     }
     return x;
 }
-// Exclusive sums of (x, y) over the block's threads in order; each warp adds up the warps before it by itself.
-__device__ __forceinline__ uint2 block_scan(uint2 v, uint2* warp_sums) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint2 s = make_uint2(warp_scan(v.x), warp_scan(v.y));
-    if (lane == 31) warp_sums[warp] = s;
-    __syncthreads();
-    const uint2 w = lane < warp ? warp_sums[lane] : make_uint2(0, 0);
-    return make_uint2(__reduce_add_sync(0xffffffffu, w.x) + s.x - v.x, __reduce_add_sync(0xffffffffu, w.y) + s.y - v.y);
-}
-
 // RUN: rows of a thread, their weights in registers; 0: any number, read again in every pass.
 template <int RUN>
 __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, const int* length, int rows, int caches,
@@ -77,39 +68,20 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
         }
         return;
     }
-    const int run = RUN > 0 ? RUN : (n + SEL_THREADS - 1) / SEL_THREADS;
-    // The thread's rows r0 .. r1 - 1 (in registers from r0 = t RUN on, also past the end: aligned for loads of four).
-    const int r0 = RUN > 0 ? t * RUN : min(n, t * run), r1 = min(n, r0 + run);
+    // A warp has 32 run consecutive rows, a lane every 32nd of them from `base` on.
+    const int run = RUN > 0 ? RUN : (n + SEL_THREADS - 1) / SEL_THREADS, base = warp * 32 * run + lane;
     float ws[RUN > 0 ? RUN : 1];
-    if constexpr (RUN % 4 == 0 && RUN > 0) {
-        const bool four = (reinterpret_cast<uintptr_t>(w) & 15) == 0;   // with r0 a multiple of 4
+    if constexpr (RUN > 0) {
 #pragma unroll
-        for (int e = 0; e < RUN; e += 4) {
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (four && r0 + e + 4 <= n) {
-                v = *(const float4*)(w + r0 + e);
-            } else {
-                if (r0 + e < n) v.x = w[r0 + e];
-                if (r0 + e + 1 < n) v.y = w[r0 + e + 1];
-                if (r0 + e + 2 < n) v.z = w[r0 + e + 2];
-                if (r0 + e + 3 < n) v.w = w[r0 + e + 3];
-            }
-            ws[e] = v.x;
-            ws[e + 1] = v.y;
-            ws[e + 2] = v.z;
-            ws[e + 3] = v.w;
-        }
-    } else if constexpr (RUN == 1) {
-        ws[0] = r0 < n ? w[r0] : 0.f;
+        for (int e = 0; e < RUN; ++e) ws[e] = base + 32 * e < n ? w[base + 32 * e] : 0.f;
     }
-    // f(key) for the thread's share of rows lo .. hi - 1 (its run in registers, else strided: order does not matter).
-    auto each = [&](int lo, int hi, auto f) {
+    // f(row, key) for the thread's rows, and some past the end, by whole warps.
+    auto each = [&](auto f) {
         if constexpr (RUN > 0) {
 #pragma unroll
-            for (int e = 0; e < RUN; ++e)
-                if (r0 + e >= lo && r0 + e < hi) f(sort_key(ws[e]));
+            for (int e = 0; e < RUN; ++e) f(base + 32 * e, sort_key(ws[e]));
         } else {
-            for (int i = lo + t; i < hi; i += SEL_THREADS) f(sort_key(w[i]));
+            for (int e = 0; e < run; ++e) f(base + 32 * e, base + 32 * e < n ? sort_key(w[base + 32 * e]) : 0u);
         }
     };
     // The need-th largest key of rows lo .. hi - 1 (need < hi - lo).
@@ -124,8 +96,8 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = shifts[pass];
             const uint32_t last = pass == 2 ? 1023u : 2047u;   // the largest digit
-            each(lo, hi, [&](uint32_t k) {
-                if ((k & mask) == prefix) atomicAdd(&hist[pass][last - ((k >> shift) & last)], 1u);
+            each([&](int i, uint32_t k) {
+                if (i >= lo && i < hi && (k & mask) == prefix) atomicAdd(&hist[pass][last - ((k >> shift) & last)], 1u);
             });
             __syncthreads();
             // The bin that holds the need-th: each warp adds up 64 bins, then every warp finds the 64 and the bin by itself.
@@ -146,45 +118,57 @@ __global__ void __launch_bounds__(SEL_THREADS) k_kv_select(const float* w_all, c
             need -= second ? above + first : above;
         }
     }
-    // Rows that stay: protected or above the threshold (x), and `need` of those equal to it (y).
+    // Rows that stay: protected or above the threshold, and `need` of those equal to it.
     const bool some = keep > sink + recent;
-    auto kind = [&](int i, uint32_t k) -> uint2 {
-        if (i < lo || i >= hi) return make_uint2(1, 0);
-        return make_uint2(some && k > prefix, some && k == prefix);
+    auto above = [&](int i, uint32_t k) { return i < n && (i < lo || i >= hi || (some && k > prefix)); };
+    auto equal = [&](int i, uint32_t k) { return i >= lo && i < hi && some && k == prefix; };
+    // A warp's rows by ballots, `at` the rows of each kind before them; put(place, row, e) for those that stay.
+    uint2 at;
+    const uint32_t below = (1u << lane) - 1;
+    auto place = [&](int e, bool is_above, bool is_equal, auto put) {
+        const uint32_t a = __ballot_sync(0xffffffffu, is_above), q = __ballot_sync(0xffffffffu, is_equal);
+        if (q == 0) {
+            if (is_above) put(at.x + __popc(a & below) + min(at.y, need), e);
+        } else {
+            const uint32_t y = at.y + __popc(q & below);
+            if (is_above || (is_equal && y < need)) put(at.x + __popc(a & below) + min(y, need), e);
+            at.y += __popc(q);
+        }
+        at.x += __popc(a);
     };
-    uint2 mine = make_uint2(0, 0);
-    auto count = [&](int i, uint32_t k) {
-        const uint2 x = kind(i, k);
-        mine.x += x.x;
-        mine.y += x.y;
-    };
-    if constexpr (RUN > 0) {
-#pragma unroll
-        for (int e = 0; e < RUN; ++e)
-            if (r0 + e < r1) count(r0 + e, sort_key(ws[e]));
-    } else {
-        for (int i = r0; i < r1; ++i) count(i, sort_key(w[i]));
-    }
-    uint2 at = block_scan(mine, warp_sums);
-    // Place of row i among the kept, or -1.
-    auto place = [&](int i, uint32_t k) {
-        const uint2 x = kind(i, k);
-        const int p = x.x || (x.y && at.y < need) ? (int)(at.x + min(at.y, need)) : -1;
-        at.x += x.x;
-        at.y += x.y;
-        if (p >= 0) kept[p] = i;
-        return p;
+    // Kept rows of each kind in the warps before.
+    auto before = [&](uint32_t x, uint32_t y) {
+        x = __reduce_add_sync(0xffffffffu, x);
+        y = __reduce_add_sync(0xffffffffu, y);
+        if (lane == 0) warp_sums[warp] = make_uint2(x, y);
+        __syncthreads();
+        const uint2 o = lane < warp ? warp_sums[lane] : make_uint2(0, 0);
+        return make_uint2(__reduce_add_sync(0xffffffffu, o.x), __reduce_add_sync(0xffffffffu, o.y));
     };
     if constexpr (RUN > 0) {
-        // The weights go along from the registers: every one was read before the first barrier, so in place too.
+        uint32_t as = 0, es = 0;   // bit e: the thread's e-th row
+#pragma unroll
+        for (int e = 0; e < RUN; ++e) {
+            const uint32_t k = sort_key(ws[e]);
+            as |= (uint32_t)above(base + 32 * e, k) << e;
+            es |= (uint32_t)equal(base + 32 * e, k) << e;
+        }
+        // The weights go along: they were read before the barrier and are stored after it, so in place too.
+        at = before(__popc(as), __popc(es));
 #pragma unroll
         for (int e = 0; e < RUN; ++e)
-            if (r0 + e < r1) {
-                const int p = place(r0 + e, sort_key(ws[e]));
-                if (p >= 0) w_out[p] = ws[e];
-            }
+            place(e, as >> e & 1, es >> e & 1, [&](uint32_t p, int) {
+                kept[p] = base + 32 * e;
+                w_out[p] = ws[e];
+            });
     } else {
-        for (int i = r0; i < r1; ++i) place(i, sort_key(w[i]));
+        uint32_t x = 0, y = 0;
+        each([&](int i, uint32_t k) {
+            x += above(i, k);
+            y += equal(i, k);
+        });
+        at = before(x, y);
+        each([&](int i, uint32_t k) { place(i, above(i, k), equal(i, k), [&](uint32_t p, int row) { kept[p] = row; }); });
         __syncthreads();
         // The weights follow in tiles: in place, a tile's stores come after its loads.
         for (int i0 = 0; i0 < keep; i0 += SEL_THREADS) {
