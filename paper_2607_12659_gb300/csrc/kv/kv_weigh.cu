@@ -152,41 +152,73 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_mma(const __grid_consta
     }
 }
 
+// A warp takes 32 keys, one a lane, and 8 query rows at a time; 32 elements of both pass through its shared memory, loaded in
+// whole lines a step ahead. (Bound by the reads of shared memory, 9 for 32 fused products, and latency: 2 requests of 34 tokens of 8
+// heads of 256 over 62 keys took
+// 68 us with each lane reading its key from memory, 32 sectors a load, and 44 so; 12 requests of 7 tokens of 8 heads of
+// 128 over 26 keys 18.5, with the rows read from memory too, and 11.)
 __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_f32(const __grid_constant__ WeighArgs a) {
+    constexpr int CH = 8;   // 16-byte pieces of a row in a step
+    __shared__ float4 rows[WG_WARPS][KR_ROWS][CH];
+    __shared__ float4 kbuf[WG_WARPS][32][CH + 1];   // (the pad spreads the lanes' rows over the banks)
     __shared__ float part[WG_WARPS][32];
     __shared__ int top;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.c.D;
     ptx::grid_dep_launch();
     const KeyPiece x = key_piece(a);
     const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
     const int live = live_keys(a, x, &top);
-    const int kt = WG_WARPS / x.wr, key = (x.tile * kt + warp / x.wr) * 32 + lane, wrow = warp % x.wr;
+    const int kt = WG_WARPS / x.wr, key0 = (x.tile * kt + warp / x.wr) * 32, key = key0 + lane, wrow = warp % x.wr;
     float acc = 0.f;
-    const float* kp = (const float*)s.k + x.cache * s.cs + x.kvh * s.hs + (long long)(key < live ? key : 0) * s.rs;
-    for (int rt = wrow * KR_ROWS; rt < x.t.R; rt += x.wr * KR_ROWS) {
-        float p[KR_ROWS], ls[KR_ROWS];
-        int n[KR_ROWS];
-        const float* q[KR_ROWS];
+    if (key0 < live) {
+        const int c = lane & 7, sub = lane >> 3;   // this lane's piece of a step, of every fourth row
+        const float* kp = (const float*)s.k + x.cache * s.cs + x.kvh * s.hs + (long long)(key0 + sub) * s.rs + 4 * c;
+        for (int rt = wrow * KR_ROWS; rt < x.t.R; rt += x.wr * KR_ROWS) {
+            float p[KR_ROWS], ls[KR_ROWS];
+            int n[KR_ROWS];
+            const float* q[2];
+            float4 k[8], v[2];
 #pragma unroll
-        for (int r = 0; r < KR_ROWS; ++r) {
-            const int rr = min(rt + r, x.t.R - 1);
-            p[r] = 0.f;
-            ls[r] = a.lse[row_index(a.c, x.t, rr)];
-            n[r] = row_seen(a.c, x.prefix, x.cache, x.t, rt + r);
-            q[r] = static_cast<const float*>(a.c.q) + row_query(a.c, x.t, rr);
-        }
-        if (key < live)
-            for (int d = 0; d < a.c.D; d += 4) {
-                const float4 k = __ldg((const float4*)(kp + d));
+            for (int j = 0; j < 2; ++j)
+                q[j] = static_cast<const float*>(a.c.q) + row_query(a.c, x.t, min(rt + sub + 4 * j, x.t.R - 1)) + 4 * c;
+            auto load = [&](int d0) {
+                const bool in = d0 + 4 * c < D;
 #pragma unroll
-                for (int r = 0; r < KR_ROWS; ++r) {
-                    const float4 v = __ldg((const float4*)(q[r] + d));
-                    p[r] = fmaf(v.x, k.x, fmaf(v.y, k.y, fmaf(v.z, k.z, fmaf(v.w, k.w, p[r]))));
+                for (int j = 0; j < 8; ++j)
+                    k[j] = in && key0 + sub + 4 * j < live ? __ldg((const float4*)(kp + 4 * j * s.rs + d0)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) v[j] = in ? __ldg((const float4*)(q[j] + d0)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            };
+            load(0);
+#pragma unroll
+            for (int r = 0; r < KR_ROWS; ++r) {
+                p[r] = 0.f;
+                ls[r] = a.lse[row_index(a.c, x.t, min(rt + r, x.t.R - 1))];
+                n[r] = row_seen(a.c, x.prefix, x.cache, x.t, rt + r);
+            }
+#pragma unroll 1
+            for (int d0 = 0; d0 < D; d0 += 4 * CH) {
+                __syncwarp();   // the step before has been read
+#pragma unroll
+                for (int j = 0; j < 8; ++j) kbuf[warp][sub + 4 * j][c] = k[j];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) rows[warp][sub + 4 * j][c] = v[j];
+                __syncwarp();
+                if (d0 + 4 * CH < D) load(d0 + 4 * CH);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const float4 z = kbuf[warp][lane][i];
+#pragma unroll
+                    for (int r = 0; r < KR_ROWS; ++r) {
+                        const float4 y = rows[warp][r][i];
+                        p[r] = fmaf(y.x, z.x, fmaf(y.y, z.y, fmaf(y.z, z.z, fmaf(y.w, z.w, p[r]))));
+                    }
                 }
             }
 #pragma unroll
-        for (int r = 0; r < KR_ROWS; ++r)
-            if (key < n[r] && ls[r] != -INFINITY) acc += expf(fmaf(p[r], a.c.scale, -ls[r]));
+            for (int r = 0; r < KR_ROWS; ++r)
+                if (key < n[r] && ls[r] != -INFINITY) acc += expf(fmaf(p[r], a.c.scale, -ls[r]));
+        }
     }
     part[warp][lane] = acc;
     __syncthreads();
