@@ -7,8 +7,10 @@
 //
 // bf16: a warp keeps 16 keys in registers as the rows of mma.sync and streams the query rows past them, 8 at
 // a time (the sum over d may run in any order, so lane (g, j) takes 16-byte chunk 4 i + j of its key and of its query
-// row as the four element pairs of two k-steps: both come from global memory as they lie); a lane adds up the weights of its two keys, and the four lanes of a key and the warps that share it
-// are joined at the end. fp32 on CUDA cores: a key per lane.
+// row as the four element pairs of two k-steps: both come from global memory as they lie); a lane adds up the weights of
+// its two keys, and the four lanes of a key and the warps that share it are joined at the end. Small calls are latency:
+// 6 to 8 us a call, two of them the launch; larger ones go to the tensor-core tiles (kv_weigh_t5.cu). fp32 on CUDA
+// cores: a key per lane.
 
 #include "kv_rows.cuh"
 #include "kv_weigh.h"
@@ -154,9 +156,8 @@ __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_mma(const __grid_consta
 
 // A warp takes 32 keys, one a lane, and 8 query rows at a time; 32 elements of both pass through its shared memory, loaded in
 // whole lines a step ahead. (Bound by the reads of shared memory, 9 for 32 fused products, and latency: 2 requests of 34 tokens of 8
-// heads of 256 over 62 keys took
-// 68 us with each lane reading its key from memory, 32 sectors a load, and 44 so; 12 requests of 7 tokens of 8 heads of
-// 128 over 26 keys 18.5, with the rows read from memory too, and 11.)
+// heads of 256 over 62 keys took 68 us with each lane reading its key from memory, 32 sectors a load, and 44 so; 12 requests
+// of 7 tokens of 8 heads of 128 over 26 keys 18.5, with the rows read from memory too, and 11.)
 __global__ void __launch_bounds__(WG_THREADS) k_kv_weigh_f32(const __grid_constant__ WeighArgs a) {
     constexpr int CH = 8;   // 16-byte pieces of a row in a step
     __shared__ float4 rows[WG_WARPS][KR_ROWS][CH];
