@@ -763,7 +763,8 @@ long long ws_rows(const jpi_kv_handle* h) {
 
 // A side's pieces for blocks of `warps` warps, whose warps take `step` keys at a time. Key splits: up to `want` pieces
 // in all while a warp keeps `least` keys (below that a part's rows are as many bytes as a good share of its keys); but a
-// call of few pieces is split down to single steps, as far as two blocks an SM go: it is waited for. The parts fit their
+// call of few pieces is split down to single steps, as far as two blocks an SM go: it is waited for (one request over 816
+// and 40 keys: 8.5 us by single steps, 8.6 by two, 9.5 by three). The parts fit their
 // half of the workspace.
 SidePlan plan_side(const jpi_kv_handle* h, const KvCall& c, bool prefix, int warps, int step, int least, long long want) {
     SidePlan s;
