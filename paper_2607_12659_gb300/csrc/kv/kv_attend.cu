@@ -578,10 +578,10 @@ __global__ void __maxnreg__(RtSmem<DP>::REGS) k_kv_attend_rows(const __grid_cons
 
 // fp32 on CUDA cores: one warp = 8 query rows over 32-key blocks. Scores with a key per lane, the values with a lane per four
 // elements of d. What bounds it is latency: a block's loads, its products (5 instructions for 4 of them) and 2^x follow one
-// another in a warp, and a small call has a block or two per warp. So the loads of 8 pieces of a key and of 8 values are on
-// their way together, in as many registers as leave an SM three blocks: 16 us for 4 requests of 9 tokens over 342 keys where
-// loads one by one took 20; a call of 294 tokens over 103 keys took 47 with 16 loads of a key and two blocks per SM, 39 with
-// four blocks, 36 with three.
+// another in a warp, and a small call has a block or two per warp. So the loads of several pieces of a key are on their way
+// together, those of the next values while these are used, in as many registers as leave an SM three blocks, and a warp with
+// its keys to itself writes its rows from registers: 4 requests of 9 tokens over 342 keys took 20 us with loads one by one, 16
+// with 8 at a time, 14 so; a call of 294 tokens over 103 keys 54, 36 and 37 (44 with two blocks an SM).
 template <int DP>
 __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32(const __grid_constant__ AttendArgs a) {
     extern __shared__ __align__(16) float kv_smem[];
@@ -594,13 +594,16 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
     float* qs = kv_smem + warp / sp.wk * (KR_ROWS * DP);
     const int wk = warp % sp.wk;
     if (wk == 0) {
-        for (int e = lane; e < KR_ROWS * (DP / 4); e += 32) {
-            const int rr = e / (DP / 4), d = 4 * (e % (DP / 4)), r = x.t.r0 + rr;
-            const float* q = static_cast<const float*>(a.c.q);
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < x.t.R && d < D)
-                v = *(const float4*)(q + row_query(a.c, x.t, r) + d);
-            *(float4*)(qs + rr * DP + d) = v;
+        for (int e0 = lane; e0 < KR_ROWS * (DP / 4); e0 += 4 * 32) {
+            float4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = e0 + 32 * i, r = x.t.r0 + e / (DP / 4), d = 4 * (e % (DP / 4));
+                v[i] = r < x.t.R && d < D ? *(const float4*)(static_cast<const float*>(a.c.q) + row_query(a.c, x.t, r) + d)
+                                          : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *(float4*)(qs + 4 * (e0 + 32 * i)) = v[i];
         }
     }
     int n[KR_ROWS], lim = 0;
@@ -615,7 +618,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
     const float* kbase = (const float*)s.k + x.cache * s.cs + (x.kvh) * s.hs;
     const float* vbase = (const float*)s.v + x.cache * s.cs + (x.kvh) * s.hs;
     constexpr int NI = (DP + 127) / 128;
-    constexpr int KL = 8 / NI, VL = 8 / NI;   // 16-byte loads of a key, values, that are on their way at a time
+    constexpr int KL = 4 / NI, VL = 4 / NI;   // 16-byte loads of a key, values, that are on their way at a time
     float4 o[KR_ROWS][NI];
     float m[KR_ROWS], l[KR_ROWS];
 #pragma unroll
@@ -631,6 +634,19 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
 #pragma unroll
         for (int r = 0; r < KR_ROWS; ++r) p[r] = 0.f;
         const float* kp = kbase + (long long)key * s.rs;
+        // Values of VL keys, those of the next ones on their way while these are used, the first ones during the scores.
+        float4 next[VL][NI];
+        auto load = [&](int t0) {
+#pragma unroll
+            for (int t = 0; t < VL; ++t)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int d = 4 * lane + 128 * i;
+                    next[t][i] = d < D && key0 + t0 + t < lim ? __ldg((const float4*)(vbase + (long long)(key0 + t0 + t) * s.rs + d))
+                                                              : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+        };
+        load(0);
         for (int d0 = 0; d0 < D; d0 += 4 * KL) {
             float4 k[KL];
 #pragma unroll
@@ -667,11 +683,8 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
 #pragma unroll
             for (int t = 0; t < VL; ++t)
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const int d = 4 * lane + 128 * i;
-                    v[t][i] = d < D && key0 + t0 + t < lim ? __ldg((const float4*)(vbase + (long long)(key0 + t0 + t) * s.rs + d))
-                                                           : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
+                for (int i = 0; i < NI; ++i) v[t][i] = next[t][i];
+            if (t0 + VL < 32) load(t0 + VL);
 #pragma unroll
             for (int t = 0; t < VL; ++t)
 #pragma unroll
@@ -693,6 +706,28 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
     for (int r = 0; r < KR_ROWS; ++r)
 #pragma unroll
         for (int e = 16; e > 0; e >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], e);
+    if (sp.wk == 1) {   // (of the whole block) nothing to merge
+#pragma unroll
+        for (int r = 0; r < KR_ROWS; ++r) {
+            if (x.t.r0 + r >= x.t.R) break;
+            const long long row = row_index(a.c, x.t, x.t.r0 + r);
+            if (a.out) {
+                RowAcc<DP> acc;
+                acc.m = m[r];
+                acc.l = l[r];
+#pragma unroll
+                for (int i = 0; i < NI; ++i) acc.o[i] = o[r][i];
+                write_row<DP, float>(a, acc, row, 0, lane);
+                continue;
+            }
+            if (lane == 0) a.pml[row * a.parts + x.part] = make_float2(m[r], l[r]);
+            if (m[r] == -INFINITY) continue;
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+                if (4 * lane + 128 * i < D) *(float4*)(a.po + (x.part * a.rows + row) * D + 4 * lane + 128 * i) = o[r][i];
+        }
+        return;
+    }
     __syncthreads();   // the queries have been read
     float* f = kv_smem + warp * MergeSmem<DP>::WARP_FLOATS;
 #pragma unroll
