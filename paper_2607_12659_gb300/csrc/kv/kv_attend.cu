@@ -8,7 +8,9 @@
 // sum l per row and an unnormalised output, all fp32, and they are joined as
 //   o = sum_s w_s O_s / sum_s w_s l_s,  w_s = exp(scale (m_s - M)),
 // in part order, so that a result does not depend on which block finished first. A part that saw no key
-// has m = -inf and weighs nothing; a row of only such parts is zero. Maxima are those of the unscaled
+// has l = 0 and weighs nothing; a row of only such parts is zero, its lse -inf. (m = -inf is no sign of it: maxima skip
+// NaN, and a part whose scores are all NaN has m = -inf and l = NaN. l alone says which, and a NaN l makes the whole row
+// NaN, its lse too, whatever the other parts hold.) Maxima are those of the unscaled
 // products, and the difference is scaled, not the product: log2(e) times a score near the type's largest
 // values would overflow.
 //
@@ -103,9 +105,8 @@ struct RowAcc {
 };
 
 // Joins elements d0 .. d0 + DP - 1 of parts first, first + step, .. of a row (of `parts`) to `r`, which holds nothing yet,
-// relative to their largest maximum. The loads of JOIN parts are in flight together: they are made whether the part weighs
-// anything or not (its memory is the workspace's), and a part of no weight, which may never have been written, is replaced
-// by zeros.
+// relative to their largest maximum. The loads of JOIN parts are in flight together: they are made whether the part holds
+// anything or not (its memory is the workspace's), and a part of no keys, which was never written, is replaced by zeros.
 template <int DP>
 __device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, long long row, int d0, int first, int step, int lane) {
     constexpr int NI = RowAcc<DP>::NI, JOIN = 16 / NI;
@@ -123,6 +124,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, l
         for (int e = 16; e > 0; e >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, e));
         const float w0 = r.m == -INFINITY ? 0.f : kr_ex2((r.m - M) * a.c2);
         const float w = ml.x == -INFINITY ? 0.f : kr_ex2((ml.x - M) * a.c2);
+        const uint32_t written = __ballot_sync(0xffffffffu, lane < n && ml.y != 0.f);
         float l = w * ml.y;
 #pragma unroll
         for (int e = 16; e > 0; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
@@ -146,17 +148,21 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, l
             for (int k = 0; k < JOIN; ++k) {
 #pragma unroll
                 for (int i = 0; i < NI; ++i)
-                    if (wk[k] == 0.f) v[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (k0 + k >= n || !(written >> (k0 + k) & 1)) v[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
                 r.add(wk[k], v[k]);
             }
         }
     }
 }
 
+// What a row's outputs are multiplied by: 0 without a key, NaN with a NaN score.
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float log_sum(float m, float l, float scale) { return l == 0.f ? -INFINITY : fmaf(m, scale, logf(l)); }
+
 // The row's result from its joined sums, elements from d0 on.
 template <int DP, typename E>
 __device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>& r, long long row, int d0, int lane) {
-    const float inv = r.l > 0.f ? 1.f / r.l : 0.f;   // (a NaN sum comes with NaN outputs)
+    const float inv = inverse_sum(r.l);
     E* out = static_cast<E*>(a.out) + row * a.c.D;
 #pragma unroll
     for (int i = 0; i < RowAcc<DP>::NI; ++i) {
@@ -168,7 +174,7 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>&
         else
             *(float4*)(out + d) = v;
     }
-    if (d0 == 0 && lane == 0 && a.lse) a.lse[row] = r.m == -INFINITY ? -INFINITY : fmaf(r.m, a.c.scale, logf(r.l));
+    if (d0 == 0 && lane == 0 && a.lse) a.lse[row] = log_sum(r.m, r.l, a.c.scale);
 }
 
 // Joins the key warps of each row tile (their outputs and (m, l) are in shared memory) and writes the part, or, where
@@ -193,10 +199,10 @@ __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece
         for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k = 0; k < s.wk; ++k) {
             const float* f = tile + k * M::WARP_FLOATS;
-            const float mk = f[KR_ROWS * M::LD + 2 * rr];
-            if (mk == -INFINITY) continue;
-            const float w = kr_ex2((mk - acc.m) * a.c2);
-            acc.l += w * f[KR_ROWS * M::LD + 2 * rr + 1];
+            const float mk = f[KR_ROWS * M::LD + 2 * rr], lk = f[KR_ROWS * M::LD + 2 * rr + 1];
+            if (lk == 0.f) continue;
+            const float w = mk == -INFINITY ? 0.f : kr_ex2((mk - acc.m) * a.c2);
+            acc.l += w * lk;
             float4 v[NI];
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
@@ -211,7 +217,7 @@ __device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece
         }
         const long long at = x.part * a.rows + row;
         if (lane == 0) a.pml[row * a.parts + x.part] = make_float2(acc.m, acc.l);
-        if (acc.m != -INFINITY) {
+        if (acc.l != 0.f) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const int d = 4 * lane + 128 * i;
@@ -543,7 +549,7 @@ __global__ void __maxnreg__(RtSmem<DP>::REGS) k_kv_attend_rows(const __grid_cons
             // The only part: the result itself. Lanes g and g + 1 exchange halves, so that the even one has a pair of row
             // 2 j and the odd one a pair of row 2 j + 1.
             const bool even = (g & 1) == 0;
-            const float inv0 = l0 > 0.f ? 1.f / l0 : 0.f, inv1 = l1 > 0.f ? 1.f / l1 : 0.f;
+            const float inv0 = inverse_sum(l0), inv1 = inverse_sum(l1);
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (even ? row0 : row1) * D + (g & ~1);
 #pragma unroll
             for (int i = 0; i < ND; ++i)
@@ -555,15 +561,15 @@ __global__ void __maxnreg__(RtSmem<DP>::REGS) k_kv_attend_rows(const __grid_cons
                         *(uint32_t*)(out + 16 * i + 8 * e) = even ? kr_pack(u, w) : kr_pack(w, v);
                 }
             if (g == 0 && a.lse) {
-                if (in0) a.lse[row0] = m0 == -INFINITY ? -INFINITY : fmaf(m0, a.c.scale, logf(l0));
-                if (in1) a.lse[row1] = m1 == -INFINITY ? -INFINITY : fmaf(m1, a.c.scale, logf(l1));
+                if (in0) a.lse[row0] = log_sum(m0, l0, a.c.scale);
+                if (in1) a.lse[row1] = log_sum(m1, l1, a.c.scale);
             }
         } else {
             const long long at0 = x.part * a.rows + row0, at1 = x.part * a.rows + row1;
             if (g == 0 && in0) a.pml[row0 * a.parts + x.part] = make_float2(m0, l0);
             if (g == 0 && in1) a.pml[row1 * a.parts + x.part] = make_float2(m1, l1);
             float *o0 = a.po + at0 * D + g, *o1 = a.po + at1 * D + g;
-            const bool w0 = in0 && m0 != -INFINITY, w1 = in1 && m1 != -INFINITY;
+            const bool w0 = in0 && l0 != 0.f, w1 = in1 && l1 != 0.f;
 #pragma unroll
             for (int i = 0; i < ND; ++i)
 #pragma unroll
@@ -675,7 +681,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
 #pragma unroll
                 for (int i = 0; i < NI; ++i) o[r][i] = make_float4(o[r][i].x * al, o[r][i].y * al, o[r][i].z * al, o[r][i].w * al);
             }
-            p[r] = m[r] == -INFINITY ? 0.f : exp2f((sc - m[r]) * a.c2);
+            p[r] = exp2f((sc - (m[r] == -INFINITY ? 0.f : m[r])) * a.c2);   // (of -inf 0, of NaN NaN)
             l[r] += p[r];
         }
         for (int t0 = 0; t0 < 32 && key0 + t0 < lim; t0 += VL) {
@@ -721,7 +727,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
                 continue;
             }
             if (lane == 0) a.pml[row * a.parts + x.part] = make_float2(m[r], l[r]);
-            if (m[r] == -INFINITY) continue;
+            if (l[r] == 0.f) continue;
 #pragma unroll
             for (int i = 0; i < NI; ++i)
                 if (4 * lane + 128 * i < D) *(float4*)(a.po + (x.part * a.rows + row) * D + 4 * lane + 128 * i) = o[r][i];

@@ -558,11 +558,11 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
             const float2 other = ml[(1 - grp) * KP_ROWS + row];
             const float M = fmaxf(m_used, other.x);
             w = m_used == -INFINITY ? 0.f : kr_ex2((m_used - M) * a.c2);
-            l = w * l + (other.x == -INFINITY ? 0.f : kr_ex2((other.x - M) * a.c2) * other.y);
+            l = w * l + (other.x == -INFINITY ? 0.f : kr_ex2((other.x - M) * a.c2)) * other.y;   // (0 times a NaN sum is NaN)
             m_used = M;
         }
         // A result is scaled by 1 / l and rounded on its way; a half row's 16-bit values go where its own 32-bit ones were.
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l == 0.f ? 0.f : 1.f / l;   // (0: the row saw no key; a NaN score makes l, and so the row, NaN)
         uint8_t* orow = kp_smem + row * L::OUT_LD;
 #pragma unroll 1
         for (int turn = 0; turn < NG; ++turn) {
@@ -619,7 +619,7 @@ __global__ void __maxnreg__(KpSmem<DP>::REGS) k_kv_tiles_t5(const __grid_constan
                 };
                 if (a.out) {
                     __nv_bfloat16* dst = a.out + row_at * a.c.D;
-                    if (a.lse) a.lse[row_at] = m_used == -INFINITY ? -INFINITY : fmaf(m_used, a.c.scale, logf(l));
+                    if (a.lse) a.lse[row_at] = l == 0.f ? -INFINITY : fmaf(m_used, a.c.scale, logf(l));
                     if (nb == 0) {
                         for (int d = 0; d < a.c.D; d += 8) *(uint4*)(dst + d) = make_uint4(0, 0, 0, 0);
                     } else if (good) {

@@ -728,3 +728,77 @@ def test_the_binding_takes_rows_of_any_stride_and_refuses_what_is_no_cache(kv):
     from paper_2607_12659_gb300.jpi import JpiError
     with pytest.raises(JpiError):
         h.attend(q, own=(k, k), seen=seen)
+
+
+# ------------------------------------------------------------------ NaN and infinities that a query sees
+
+def clean_call(seed, dtype, H, K, D, B, T, G, P, R, std=2.0):
+    """Inputs of finite numbers; the last query of the first and of the last request sees every row, and rows that no query
+    sees hold NaN."""
+    c = make_call(seed, dtype, H, K, D, B, T, G, P, R, mask="any", std=std)
+    if P:
+        c["prefix_len"].fill_(P - 1)
+        c["prefix"] = tuple(rand(seed + i, G, P, K, D, dtype=dtype) for i in (11, 12))
+        for t in c["prefix"]:
+            t[:, P - 1] = float("nan")
+    if R:
+        c["seen"][0, -1] = c["seen"][-1, -1] = R
+        c["own"] = tuple(rand(seed + i, B, R, K, D, dtype=dtype) for i in (13, 14))
+        for b in range(B):
+            for t in c["own"]:
+                t[b, int(c["seen"][b].max()):] = float("nan")
+    return c
+
+
+def check_attend_special(kv, dtype, c, what):
+    """Attention over infinities and NaN: what the formula gives, NaN where it gives NaN."""
+    B, T, H, D = c["q"].shape
+    K = (c["prefix"] or c["own"])[0].shape[2]
+    h = kv.KV(H, K, D, max_batch=B, max_tokens=T, precision=dtype)
+    out, lse = h.attend(**c)
+    h.device_status()
+    with np.errstate(invalid="ignore"):
+        ref, rlse, dot, mass = attend_ref(c, 1 / math.sqrt(D))
+    assert not np.isfinite(ref).all(), "the case has nothing special"
+    tol, ltol = attend_tols(c, dtype, *(np.where(np.isfinite(a), a, 0.0) for a in (ref, dot, mass)), rlse)
+    for name, got, want, bound in (("out", out, ref, tol), ("lse", lse, rlse, ltol)):
+        assert np.array_equal(np.isnan(np64(got)), np.isnan(want)), f"{what}: NaN of {name}"
+        # (an infinite element has to be equal)
+        within(got.nan_to_num(0.0, math.inf, -math.inf), np.where(np.isnan(want), 0.0, want), np.where(np.isfinite(want), bound, 0.0), f"{what}: {name}")
+    return lse
+
+
+# One part and several, few query rows and many, each side alone and both.
+SPECIAL = [("fp32", 4, 2, 64, 3, 2, 1, 70, 20), ("fp32", 2, 1, 64, 1, 1, 1, 30, 0), ("fp32", 8, 1, 256, 2, 9, 1, 333, 40),
+           ("fp32", 8, 2, 128, 2, 40, 1, 0, 64), ("bf16", 4, 2, 64, 3, 2, 1, 70, 20), ("bf16", 2, 1, 64, 1, 1, 1, 9, 0),
+           ("bf16", 8, 1, 256, 2, 3, 1, 900, 40), ("bf16", 8, 2, 96, 2, 40, 1, 0, 150), ("bf16", 16, 2, 128, 8, 4, 2, 300, 130),
+           ("bf16", 8, 1, 256, 4, 51, 2, 200, 51)]
+NAN_KINDS = ["a query", "a key", "a key of the last rows", "the first keys", "all keys of a side"]
+
+
+@pytest.mark.usefixtures("tiles")
+@pytest.mark.parametrize("kind", NAN_KINDS)
+@pytest.mark.parametrize("dtype,H,K,D,B,T,G,P,R", SPECIAL)
+def test_attend_a_nan_query_or_key_gives_nan(kv, dtype, H, K, D, B, T, G, P, R, kind):
+    """A NaN score is no missing key: the rows that have one are NaN and so is their lse, however the call is split, and the
+    weights that come of them."""
+    c = clean_call(H + D, dtype, H, K, D, B, T, G, P, R)
+    k = (c["prefix"] or c["own"])[0]
+    if kind == "a query":
+        c["q"][-1, -1, -1, 3] = float("nan")
+    elif kind == "a key":
+        k[0, 1, 0, 2] = float("nan")
+    elif kind == "a key of the last rows":
+        (c["own"] or c["prefix"])[0][-1, (R or P - 1) - 1, -1, 5] = float("nan")
+    elif kind == "the first keys":
+        k[0, :35] = float("nan")
+    else:
+        k[:] = float("nan")
+    lse = check_attend_special(kv, dtype, c, kind)
+    keys = dict(prefix=(c["prefix"] or [None])[0], prefix_len=c["prefix_len"], own=(c["own"] or [None])[0], seen=c["seen"])
+    got = kv.KV(H, K, D, max_batch=B, max_tokens=T, precision=dtype).weigh(c["q"], lse, **keys)
+    host = [None if t is None else t.cpu().numpy() if t.dtype is torch.int32 else np64(t) for t in keys.values()]
+    with np.errstate(invalid="ignore"):
+        ref = okv.weigh(np64(c["q"]), np64(lse), *host, 1 / math.sqrt(D), 1.0, None, None, *(None if g is None else np.zeros(g.shape) for g in got))
+    for g, (y, _) in zip(got, ref):
+        assert g is None or np.array_equal(np.isnan(np64(g)), np.isnan(y)), "NaN of the weights"
