@@ -130,8 +130,9 @@ JPI_API jpi_status jpi_kv_append(jpi_kv_handle* h, const void* q, long long q_st
  *   lse:         device fp32 [batch][tokens][H], log of the sum of exp(score), or NULL
  * A query that sees no key gets zeros and -infinity (as one all of whose scores are -infinity). A NaN score,
  * of a NaN in the query or in a key that it sees, makes out and lse NaN, and so the weights that jpi_kv_weigh
- * forms with them. Nothing in rows that a query does not see reaches it, infinities and NaN included. Scores,
- * softmax and sums in fp32; results do not depend on the run.
+ * forms with them. An infinite value that a query sees makes the element infinite, NaN where both signs meet or where
+ * its weight is below the least that fp32 holds. Nothing in rows that a query does not see reaches it, infinities and
+ * NaN included. Scores, softmax and sums in fp32; results do not depend on the run.
  */
 JPI_API jpi_status jpi_kv_attend(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
                                  const jpi_kv_cache* prefix, int groups, const int* prefix_len,

@@ -480,59 +480,15 @@ __global__ void __maxnreg__(RtSmem<DP>::REGS) k_kv_attend_rows(const __grid_cons
                     pe[t][e] = kr_transpose(r);
                 }
             const int vr = (lane & 7) + ((lane >> 4) << 3);   // key of this lane's matrix row; its chunk is 2 i + bit 3
-            auto values = [&](int t, int i, uint32_t(&f)[4]) {
-                ldsm4_t(f, vs + (16 * t + vr) * (DP * 2) + (((2 * i + ((lane >> 3) & 1)) ^ (vr & 7)) << 4));
-            };
-            // A block that some rows see only a part of, with an infinity or NaN among its values: 0 times one of those
-            // that one row sees would reach another. Then row by row, over the row's own keys.
-            bool odd = false;
-            if (cut && low < lim) {
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    for (int i = 0; i < ND; ++i) {
-                        uint32_t f[4];
-                        values(t, i, f);
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) odd = odd || (f[e] & 0x7f80u) == 0x7f80u || (f[e] & 0x7f800000u) == 0x7f800000u;
-                    }
-                odd = __any_sync(0xffffffffu, odd);
-            }
-            if (!odd) {
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int i = 0; i < ND; ++i) {
-                        uint32_t f[4];
-                        values(t, i, f);
-                        kr_mma(o[i], f[0], f[1], f[2], f[3], ph[t][0], ph[t][1]);
-                        kr_mma(o[i], f[0], f[1], f[2], f[3], pe[t][0], pe[t][1]);
-                    }
-            } else {
-                // (each row's product in registers of its own: of one with other rows' columns zero, 0 times the NaN would
-                // still be theirs)
-#pragma unroll 1
-                for (int r = 0; r < KR_ROWS; ++r) {
-                    const int n = __shfl_sync(0xffffffffu, (r & 1) ? n1 : n0, r >> 1);
-                    const bool mine = g == r;
-#pragma unroll
-                    for (int i = 0; i < ND; ++i) {
-                        float y[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int t = 0; t < MT; ++t) {
-                            const int key = key0 + 16 * t + 2 * j;
-                            const uint32_t lo = (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
-                            const uint32_t hi = (key + 8 < n ? 0xffffu : 0u) | (key + 9 < n ? 0xffff0000u : 0u);
-                            uint32_t f[4];
-                            values(t, i, f);
-                            kr_mma(y, f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, mine ? ph[t][0] : 0u, mine ? ph[t][1] : 0u);
-                            kr_mma(y, f[0] & lo, f[1] & lo, f[2] & hi, f[3] & hi, mine ? pe[t][0] : 0u, mine ? pe[t][1] : 0u);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (2 * j + (e & 1) == r) o[i][e] += y[e];
-                    }
+                for (int i = 0; i < ND; ++i) {
+                    uint32_t f[4];
+                    ldsm4_t(f, vs + (16 * t + vr) * (DP * 2) + (((2 * i + ((lane >> 3) & 1)) ^ (vr & 7)) << 4));
+                    kr_mma(o[i], f[0], f[1], f[2], f[3], ph[t][0], ph[t][1]);
+                    kr_mma(o[i], f[0], f[1], f[2], f[3], pe[t][0], pe[t][1]);
                 }
-            }
             __syncwarp();   // every lane has read the stage
             ++used;
             produce();
@@ -541,6 +497,56 @@ __global__ void __maxnreg__(RtSmem<DP>::REGS) k_kv_attend_rows(const __grid_cons
         for (int d = 4; d < 32; d <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, d);
             l1 += __shfl_xor_sync(0xffffffffu, l1, d);
+        }
+        // An infinite value times what the rounding left of its probability (0, or of the other sign) is NaN, and so is 0 times an
+        // infinity or NaN that only another row of the tile sees. Rows whose sum is finite and outputs are not are formed
+        // again, key by key in fp32, each over its own keys. (One check a piece, where a search of every block that some rows see a
+        // part of would read its values twice.)
+        float z0 = 0.f, z1 = 0.f;   // 0 as long as all are finite
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            z0 = fmaf(o[i][0], 0.f, fmaf(o[i][2], 0.f, z0));
+            z1 = fmaf(o[i][1], 0.f, fmaf(o[i][3], 0.f, z1));
+        }
+        uint32_t again = __reduce_or_sync(0xffffffffu, (rj < x.t.R && l0 < INFINITY && !(z0 == 0.f) ? 1u << (2 * j) : 0u) |
+                                                           (rj + 1 < x.t.R && l1 < INFINITY && !(z1 == 0.f) ? 2u << (2 * j) : 0u));
+        for (; again; again &= again - 1) {
+            const int r = __ffs(again) - 1;
+            const KvSide& s = x.prefix ? a.c.prefix : a.c.own;
+            const int n = min(b1 * L::KEYS, __shfl_sync(0xffffffffu, (r & 1) ? n1 : n0, r >> 1));
+            float m = __shfl_sync(0xffffffffu, (r & 1) ? m1 : m0, r >> 1);
+            if (m == -INFINITY) m = 0.f;
+            constexpr int NL = DP / 32;   // lane's elements of a row: lane + 32 i
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + row_query(a.c, x.t, x.t.r0 + r);
+            const long long base = x.cache * s.cs + x.kvh * s.hs;
+            float qr[NL], sum[NL];
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                qr[i] = lane + 32 * i < D ? __bfloat162float(q[lane + 32 * i]) : 0.f;
+                sum[i] = 0.f;
+            }
+#pragma unroll 1
+            for (int key = b0 * L::KEYS; key < n; ++key) {
+                const __nv_bfloat16 *k = static_cast<const __nv_bfloat16*>(s.k) + base + key * s.rs,
+                                    *v = static_cast<const __nv_bfloat16*>(s.v) + base + key * s.rs;
+                float dot = 0.f;
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    if (lane + 32 * i < D) dot = fmaf(qr[i], __bfloat162float(k[lane + 32 * i]), dot);
+#pragma unroll
+                for (int e = 16; e > 0; e >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, e);
+                const float pr = kr_ex2((dot - m) * a.c2);
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    if (lane + 32 * i < D) sum[i] = fmaf(pr, __bfloat162float(v[lane + 32 * i]), sum[i]);
+            }
+            // Back to the fragments: elements 16 i + g, + 8 of the row to the lanes of its column.
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {
+                const float y0 = __shfl_sync(0xffffffffu, sum[i >> 1], 16 * (i & 1) + g), y1 = __shfl_sync(0xffffffffu, sum[i >> 1], 16 * (i & 1) + g + 8);
+                if (r == 2 * j) o[i][0] = y0, o[i][2] = y1;
+                if (r == 2 * j + 1) o[i][1] = y0, o[i][3] = y1;
+            }
         }
         // Rows 2 j (elements 0 and 2 of each fragment) and 2 j + 1 (1 and 3), d = 16 i + g and + 8.
         const bool in0 = rj < x.t.R, in1 = rj + 1 < x.t.R;

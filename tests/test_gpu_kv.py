@@ -802,3 +802,19 @@ def test_attend_a_nan_query_or_key_gives_nan(kv, dtype, H, K, D, B, T, G, P, R, 
         ref = okv.weigh(np64(c["q"]), np64(lse), *host, 1 / math.sqrt(D), 1.0, None, None, *(None if g is None else np.zeros(g.shape) for g in got))
     for g, (y, _) in zip(got, ref):
         assert g is None or np.array_equal(np.isnan(np64(g)), np.isnan(y)), "NaN of the weights"
+
+
+@pytest.mark.usefixtures("tiles")
+@pytest.mark.parametrize("dtype,H,K,D,B,T,G,P,R", SPECIAL)
+def test_attend_an_infinite_value_that_a_query_sees_stays_infinite(kv, dtype, H, K, D, B, T, G, P, R):
+    """An infinite value of positive weight makes its element that infinity, NaN only where both signs meet; queries that do
+    not see it keep what they have."""
+    n = R or P - 1
+    for at in (0, n // 2, n - 1):
+        c = clean_call(D + at, dtype, H, K, D, B, T, G, P, R, std=1.0)
+        v = (c["own"] or c["prefix"])[1]
+        v[0, at, 0, 3], v[0, at, 0, 4] = float("inf"), -float("inf")
+        v[0, 0, 0, 6], v[0, n - 1, 0, 6] = float("inf"), -float("inf")
+        if P and R:
+            c["prefix"][1][0, 1, -1, 7], v[0, at, -1, 7] = float("inf"), -float("inf")
+        check_attend_special(kv, dtype, c, f"row {at}")
