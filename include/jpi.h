@@ -184,10 +184,11 @@ JPI_API jpi_status jpi_commit_prefix(jpi_handle* h, int batch, int prefix_len);
  *   place, and makes the shorter prefix current. The suffix tokens keep their rotary positions (those
  *   after the whole prefix). w is moved with the keys, [n_layers][batch][keep] at the old strides.
  *   kept: device int [n_layers][batch][keep], the tokens that stay, or NULL.
- * jpi_append_prefix: `tokens` further prefix tokens behind the stored ones, prefix_len + tokens <= max_prefix:
+ * jpi_append_prefix: `tokens` further prefix tokens behind the stored ones, prefix_len + tokens <= max_prefix (of
+ *   the prefix as it is now: rows that jpi_evict_prefix freed take new tokens):
  *   k_layers[l], v_layers[l]: device [batch][tokens][D] in the store's type, keys without position code: they are
  *   coded for the positions that follow (rope_base as the expert's own tokens), and the suffix tokens' positions
- *   move on with them.
+ *   move on with them, past max_prefix too, to 2^30.
  * jpi_commit_prefix_at: jpi_commit_prefix, with the suffix tokens' rotary positions starting at `position`
  *   (prefix_len .. max_prefix) instead of prefix_len, for a store that was cut outside these calls.
  */

@@ -29,10 +29,13 @@ struct GraphSet {
 struct PrefixHandle : jpi_handle {
     int share = 1;              // requests a prefix serves (jpi_share_prefix)
     int shift = 0;              // rotary positions of the suffix start at cur_prefix + shift
+    bool far() const { return cur_prefix + shift > maxP; }   // past those of the table (jpi_append_prefix alone goes there)
     ExpertKv kv;                // allocated by the first of those calls
     float* weigh = nullptr;     // while jpi_weigh_prefix enqueues its evaluation: where the weights go
     float decay = 0.f;
-    std::map<std::pair<int, int>, GraphSet> sets;   // graphs by (share, shift)
+    // Graphs by share and shift; past the table the positions are read on the device (ExpertKv::start), and one set serves all.
+    std::map<std::pair<int, int>, GraphSet> sets;
+    GraphSet& set() { return sets[{share, far() ? -1 : shift}]; }
 };
 
 namespace {
@@ -320,7 +323,7 @@ jpi_status enqueue_denoise(jpi_handle* h, int B, int C, int N, cudaStream_t st) 
 
 jpi_status get_graph(jpi_handle* h, int B, int C, int N, cudaGraphExec_t* out) {
     const GraphKey key{B, C, N, h->cur_prefix, h->n_corr};
-    GraphSet& set = ext(h)->sets[{ext(h)->share, ext(h)->shift}];
+    GraphSet& set = ext(h)->set();
     auto it = set.graphs.find(key);
     if (it != set.graphs.end()) {
         *out = it->second;
@@ -375,9 +378,15 @@ jpi_status enqueue_step(jpi_handle* h, int step, int B, int C, float delta, floa
     PrefixHandle* e = ext(h);
     if (step == 0 && (e->share > 1 || e->weigh)) JPI_TRY(expert_kv_fill(h, e->kv, B, C, e->share, st));
     JPI_TRY(launch_embed(h, step, B, C, h->x, st));
-    // The kernels take suffix row i's rotary position as cur_prefix + i: a table that starts `shift` positions further on.
+    // The kernels take suffix row i's rotary position as cur_prefix + i: a table that starts `shift` positions further on, or
+    // one of the suffix's positions alone, as if it began cur_prefix rows before.
     float2* const rope = h->rope_tab;
-    if (rope) h->rope_tab = rope + (size_t)e->shift * (h->D / 2);
+    if (rope && e->far()) {
+        if (step == 0) JPI_TRY(expert_kv_rope(h, e->kv, C, st));
+        h->rope_tab = reinterpret_cast<float2*>(reinterpret_cast<uintptr_t>(e->kv.rope) - (size_t)h->cur_prefix * (h->D / 2) * sizeof(float2));
+    } else if (rope) {
+        h->rope_tab = rope + (size_t)e->shift * (h->D / 2);
+    }
     jpi_status s = JPI_OK;
     for (int l = 0; l < h->L && s == JPI_OK; ++l)
         for (int op = 2; op <= 6 && s == JPI_OK; ++op) s = launch_op(h, op, l, step, B, C, st);
@@ -582,8 +591,10 @@ JPI_API jpi_status jpi_append_prefix(jpi_handle* h, const void* const* k_layers,
     if (!h->prefix_ready) return fail(JPI_ERR_NOT_READY, "no prefix KV has been set");
     if (tokens < 1) return fail(JPI_ERR_INVALID_ARG, "tokens must be >= 1");
     if (h->cfg.rope_base > 0.f && h->cfg.rope_base < 1.f) return fail(JPI_ERR_UNSUPPORTED, "rope_base must be 0 or at least 1");
-    if ((long long)h->cur_prefix + ext(h)->shift + tokens > h->maxP)
-        return fail(JPI_ERR_SHAPE, "%d tokens behind position %d exceed max_prefix %d", tokens, h->cur_prefix + ext(h)->shift, h->maxP);
+    if ((long long)h->cur_prefix + tokens > h->maxP)
+        return fail(JPI_ERR_SHAPE, "%d tokens behind %d exceed max_prefix %d", tokens, h->cur_prefix, h->maxP);
+    if ((long long)h->cur_prefix + ext(h)->shift + tokens > (1 << 30))
+        return fail(JPI_ERR_SHAPE, "%d tokens behind position %d exceed 2^30", tokens, h->cur_prefix + ext(h)->shift);
     for (int l = 0; l < h->L; ++l)
         if (!k_layers[l] || !v_layers[l] || ((uintptr_t)k_layers[l] & 15) || ((uintptr_t)v_layers[l] & 15))
             return fail(JPI_ERR_INVALID_ARG, "layer %d K or V is NULL or not 16-byte aligned", l);
@@ -687,7 +698,7 @@ JPI_API jpi_status jpi_graph_kernel_count(jpi_handle* h, int batch, int chunk, i
     if (!count) return fail(JPI_ERR_INVALID_ARG, "count is NULL");
     cudaGraphExec_t ex = nullptr;
     JPI_TRY(get_graph(h, batch, chunk, num_steps, &ex));
-    *count = ext(h)->sets[{ext(h)->share, ext(h)->shift}].kernels[GraphKey{batch, chunk, num_steps, h->cur_prefix, h->n_corr}];
+    *count = ext(h)->set().kernels[GraphKey{batch, chunk, num_steps, h->cur_prefix, h->n_corr}];
     return JPI_OK;
 }
 

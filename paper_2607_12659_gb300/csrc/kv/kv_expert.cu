@@ -19,8 +19,18 @@ __global__ void k_fill_seen(int* seen, int* len, int B, int S, int nctx, int G, 
 __global__ void k_fill_len(int* len, int n, int P) {
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) len[i] = P;
 }
-// Appended tokens [B][T]: positions p0 + t, rows r0 + t.
-__global__ void k_fill_tokens(int* position, int* row, int n, int T, int p0, int r0) {
+// As the expert's own table is made: the angle in 64 bits, its cosine and sine rounded.
+__global__ void k_fill_rope(float2* rope, const int* start, int S, int half, double base) {
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < S * half; i += gridDim.x * blockDim.x) {
+        const int d = i % half;
+        double s, c;
+        sincos((double)(*start + i / half) * pow(base, -1.0 * d / half), &s, &c);
+        rope[i] = make_float2((float)c, (float)s);
+    }
+}
+// Appended tokens [B][T]: positions p0 + t, rows r0 + t; the suffix follows at p0 + T.
+__global__ void k_fill_tokens(int* position, int* row, int* start, int n, int T, int p0, int r0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *start = p0 + T;
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
         position[i] = p0 + i % T;
         row[i] = r0 + i % T;
@@ -72,8 +82,8 @@ jpi_status expert_kv_create(jpi_handle* h, ExpertKv* e) {
     JPI_TRY(jpi_kv_create(&cfg, h->cfg.rope_base >= 1.f ? &rope : nullptr, &e->kv));
     e->kv->pdl = h->pdl;
     e->kv->dev_err = h->dev_err;   // what its kernels report is the expert's status
-    const size_t ints = (size_t)h->maxB * h->maxS + h->maxB + 2 * (size_t)h->maxB * h->maxP + (size_t)h->L * h->maxB * h->maxP;
-    const size_t bytes = ints * sizeof(int) + (size_t)h->maxMt * h->H * sizeof(float);
+    const size_t ints = (size_t)h->maxB * h->maxS + h->maxB + 2 * (size_t)h->maxB * h->maxP + (size_t)h->L * h->maxB * h->maxP + 1;
+    const size_t bytes = (size_t)h->maxS * (h->D / 2) * sizeof(float2) + ints * sizeof(int) + (size_t)h->maxMt * h->H * sizeof(float);
     void* p = nullptr;
     if (cudaMalloc(&p, bytes) != cudaSuccess) {
         cudaGetLastError();
@@ -83,12 +93,14 @@ jpi_status expert_kv_create(jpi_handle* h, ExpertKv* e) {
     }
     h->allocations.push_back(p);
     h->device_bytes += bytes + e->kv->device_bytes;
-    e->lse = static_cast<float*>(p);
+    e->rope = static_cast<float2*>(p);
+    e->lse = reinterpret_cast<float*>(e->rope + (size_t)h->maxS * (h->D / 2));
     e->seen = reinterpret_cast<int*>(e->lse + (size_t)h->maxMt * h->H);
     e->len = e->seen + (size_t)h->maxB * h->maxS;
     e->position = e->len + h->maxB;
     e->row = e->position + (size_t)h->maxB * h->maxP;
     e->kept = e->row + (size_t)h->maxB * h->maxP;
+    e->start = e->kept + (size_t)h->L * h->maxB * h->maxP;
     return JPI_OK;
 }
 
@@ -134,10 +146,17 @@ jpi_status expert_kv_evict(jpi_handle* h, const ExpertKv& e, float* w, int keep,
     return launch_kv_evict(e.kv, c, w, e.len, h->L, h->cur_batch, keep, sink, recent, c, w, e.len, kept ? kept : e.kept, st);
 }
 
+jpi_status expert_kv_rope(jpi_handle* h, const ExpertKv& e, int C, cudaStream_t st) {
+    const int S = C + h->n_ctx();
+    k_fill_rope<<<grid_of((long long)S * (h->D / 2)), 256, 0, st>>>(e.rope, e.start, S, h->D / 2, h->cfg.rope_base);
+    JPI_CUDA_TRY(cudaGetLastError());
+    return JPI_OK;
+}
+
 jpi_status expert_kv_append(jpi_handle* h, const ExpertKv& e, const void* const* k_layers, const void* const* v_layers, int tokens,
                             int position, cudaStream_t st) {
     const int n = h->cur_batch * tokens;
-    k_fill_tokens<<<grid_of(n), 256, 0, st>>>(e.position, e.row, n, tokens, position, h->cur_prefix);
+    k_fill_tokens<<<grid_of(n), 256, 0, st>>>(e.position, e.row, e.start, n, tokens, position, h->cur_prefix);
     JPI_CUDA_TRY(cudaGetLastError());
     for (int l = 0; l < h->L; ++l) {
         const jpi_kv_cache c = store_of(h, l, 0, h->kv_rows);

@@ -14,6 +14,9 @@ struct ExpertKv {
     int* row = nullptr;
     int* kept = nullptr;       // [L][maxB][maxP]
     float* lse = nullptr;      // [maxMt][H]
+    // Rotary positions past the expert's table: [maxS][D / 2] (cos, sin) of those that follow the prefix, and the first of them.
+    float2* rope = nullptr;
+    int* start = nullptr;
 };
 
 jpi_status expert_kv_create(jpi_handle* h, ExpertKv* e);
@@ -24,7 +27,9 @@ jpi_status expert_kv_fill(jpi_handle* h, const ExpertKv& e, int B, int C, int sh
 jpi_status expert_kv_attention(jpi_handle* h, const ExpertKv& e, int l, int B, int C, int share, float* w, float decay,
                                cudaStream_t st);
 jpi_status expert_kv_evict(jpi_handle* h, const ExpertKv& e, float* w, int keep, int sink, int recent, int* kept, cudaStream_t st);
-// `tokens` rows behind the cur_prefix ones of every layer, keys coded for positions from `position` on.
+// Fills `rope` from `start` for the suffix of C actions.
+jpi_status expert_kv_rope(jpi_handle* h, const ExpertKv& e, int C, cudaStream_t st);
+// `tokens` rows behind the cur_prefix ones of every layer, keys coded for positions from `position` on; `start` follows them.
 jpi_status expert_kv_append(jpi_handle* h, const ExpertKv& e, const void* const* k_layers, const void* const* v_layers, int tokens,
                             int position, cudaStream_t st);
 

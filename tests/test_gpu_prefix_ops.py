@@ -249,3 +249,56 @@ def test_refusals(monkeypatch):
             ex.share_prefix(2)
     finally:
         ex.close()
+
+
+@pytest.mark.parametrize("cfg,share", [(TINY, 1), (TINY, 3), (SMALL_BF16, 1), (SMALL_BF16, 2)])
+def test_tokens_appended_to_what_eviction_left(cfg, share, monkeypatch):
+    """The rows that eviction frees take new tokens, at the positions that follow, past max_prefix too."""
+    w = make_weights(cfg, 0)
+    P, T, C, G = 40, 17, 6, 2
+    B, L = G * share, cfg.n_layers
+    r, slots = shared(cfg, 6, G, share, P, C)
+    ex = make_expert(cfg, w, max_batch=B, max_prefix=P, max_chunk=C, max_steps=2)
+    rng = np.random.default_rng(share)
+    state, noise = dev(r["state"]), dev(r["noise"])
+    real = oe.rope
+    try:
+        k, v = to_dev_kv(r, cfg)
+        ex.share_prefix(share)
+        ex.set_prefix_kv(k[:, slots], v[:, slots])
+        keys, values = (a[:, slots].astype(np.float64) for a in (r["prefix_k"], r["prefix_v"]))
+        end = P
+        for turn in range(3):
+            weights = dev(rng.random((L, G, keys.shape[2]), np.float32))
+            before, keep = weights.clone(), 20 + (turn > 0)      # (the last turn: the same shapes at later positions)
+            kept = ex.evict_prefix(weights, keep, sink=1, recent=3)
+            assert ex.prefix_shape() == (G, keep, end)
+            moved = torch.gather(before, 2, kept.long())
+            assert torch.equal(weights[..., :keep], moved) and torch.equal(weights[..., keep:], before[..., keep:])
+            idx = kept.cpu().numpy()[..., None]
+            keys, values = (np.take_along_axis(a, idx, axis=2) for a in (keys, values))
+            new_k, new_v = (dev(rng.standard_normal((L, G, T, cfg.head_dim)).astype(np.float32)).to(k.dtype) for _ in range(2))
+            with pytest.raises(lib().JpiError):
+                ex.append_prefix(*(torch.cat([t, t], dim=2) for t in (new_k, new_v)))      # more rows than are free
+            ex.append_prefix(new_k, new_v)
+            coded = real(new_k.double().cpu().numpy().transpose(2, 0, 1, 3), np.arange(end, end + T), cfg.rope_base).transpose(1, 2, 0, 3)
+            if cfg.precision == "bf16":     # as the store holds them
+                coded = torch.from_numpy(coded).bfloat16().double().numpy()
+            keys, values = np.concatenate([keys, coded], axis=2), np.concatenate([values, new_v.double().cpu().numpy()], axis=2)
+            end += T
+            assert ex.prefix_shape() == (G, keep + T, end) and end > P
+            run = np.repeat(np.arange(G), share)
+            now = {**r, "prefix_k": keys[:, run], "prefix_v": values[:, run]}
+            for steps in (2, 1):
+                got = ex.denoise(state, noise, steps)
+                ex.device_status()
+                monkeypatch.setattr(oe, "rope", lambda x, pos, base: real(x, pos + (end - keep - T), base))
+                ref = oracle_denoise(cfg, w, now, steps)
+                monkeypatch.undo()
+                assert_close(got.cpu().numpy(), ref, cfg, f"turn {turn}, {steps} steps")
+        # The next observation starts afresh.
+        ex.set_prefix_kv(k[:, slots], v[:, slots])
+        assert ex.prefix_shape() == (G, P, P)
+        assert_close(ex.denoise(state, noise, 2).cpu().numpy(), oracle_denoise(cfg, w, r, 2), cfg, "a new prefix")
+    finally:
+        ex.close()
