@@ -8,7 +8,8 @@
 //               with their -lse: four warps fill each tile, so that one's copies fly while the other's are issued
 //   warps 10-17 two threads per key (its TMEM lane), half of a tile's columns each: the sum of exp(scale s - lse)
 // Bound by 2^x and the products alike (128 x R of the one, 4096 cycles of the other at R = 512, D = 256); the keys come
-// from memory once and the query rows from L2 once per 128 keys. Every wait is bounded.
+// from memory once and the query rows from L2 once per 128 keys. Every wait is bounded; where one gave up, in any block that shares the
+// keys, their weights stay as they were.
 
 #include "kv_rows.cuh"
 #include "kv_maps.h"
@@ -211,9 +212,13 @@ __global__ void __launch_bounds__(WT_THREADS, 1) k_kv_weigh_t5(const __grid_cons
     const int key = tid - (WT_THREADS - WT_SUM);
     if (rank == 0 && key >= 0 && key < WT_KEYS) {
         float w = sums[key];
-        for (int k = 1; k < a.ranks; ++k) w += ptx::dsmem_ld_f32(ptx::dsmem_map(ptx::smem_u32(sums + key), (uint32_t)k));
+        bool whole = *flag == 0;   // no block's rows are missing
+        for (int k = 1; k < a.ranks; ++k) {
+            w += ptx::dsmem_ld_f32(ptx::dsmem_map(ptx::smem_u32(sums + key), (uint32_t)k));
+            whole = whole && __float_as_int(ptx::dsmem_ld_f32(ptx::dsmem_map(ptx::smem_u32(flag), (uint32_t)k))) == 0;
+        }
         ptx::grid_dep_wait();   // the row kernel that started before this one: what follows this kernel has both
-        if (key0 + key < len && *flag == 0) {
+        if (key0 + key < len && whole) {
             const long long at = ((long long)run * a.c.K + kvh) * a.c.prefix.rows + key0 + key;
             a.out[at] = a.in && a.decay != 0.f ? fmaf(a.decay, a.in[at], w) : w;
         }

@@ -66,3 +66,17 @@ def test_clusters_meet_twice_around_the_sums_of_their_blocks():
     reads = body.index("dsmem_ld_f32(")
     meets = [m.start() for m in re.finditer(r"if \(a\.ranks > 1\) ptx::cluster_sync_all\(\);", body)]
     assert len(meets) == 2 and meets[0] < reads < meets[1]
+
+
+def test_a_wait_that_gave_up_in_any_block_of_a_cluster_keeps_its_keys_weights():
+    # The block that writes reads the others' flags too, between the cluster's two meetings, and writes only if all are clear:
+    # a sum that lacks a block's rows must not reach weights that are kept from call to call.
+    body = kernel("kv_weigh_t5.cu")
+    meets = [m.start() for m in re.finditer(r"if \(a\.ranks > 1\) ptx::cluster_sync_all\(\);", body)]
+    part = body[meets[0]:meets[1]]
+    own = re.search(r"bool whole = \*flag == 0;", part)
+    loop = re.search(r"for \(int k = 1; k < a\.ranks; \+\+k\) \{(.*?)\n        \}", part, re.S)
+    assert own and loop and own.start() < loop.start()
+    assert re.search(r"whole = whole && __float_as_int\(ptx::dsmem_ld_f32\(ptx::dsmem_map\(ptx::smem_u32\(flag\), \(uint32_t\)k\)\)\) == 0;", loop[1])
+    write = re.search(r"if \(([^{]*)\) \{[^}]*a\.out\[at\] =", part)
+    assert write and "whole" in write[1] and write.start() > loop.end()
