@@ -104,7 +104,8 @@ JPI_API jpi_status jpi_kv_destroy(jpi_kv_handle* h);   /* NULL is a no-op */
  *   position:  device int [batch][tokens], any value (negative: the rotation backwards).
  *   row:       device int [batch][tokens], the row of cache b that takes the token. A row outside
  *              0 .. cache->rows - 1 marks padding: nothing is written for that token, its q_out
- *              included. Two tokens of one request with the same row leave either of them there.
+ *              included. A row that several tokens of one request name is left with elements of any of
+ *              them, mixed and not the same from call to call; no other row is touched by them.
  *   q_out:     device E [batch][tokens][H][D], the coded queries (may alias q where q is contiguous).
  *   cache:     `batch` caches; its k (and v) may be where k (and v) point to, the same rows at the
  *              same addresses.

@@ -179,8 +179,8 @@ class KV:
 
     def append(self, q, k, v, positions, rows, cache_k=None, cache_v=None, q_out=None, stream=None):
         """Codes q [B][T][H][D] and k [B][T][Hk][D] for `positions` (int32 [B][T]) and writes k and v into `rows`
-        (int32 [B][T]; a row outside the cache marks padding) of the caches. Returns the coded queries. q, v, or k
-        with v and the caches may be None."""
+        (int32 [B][T]; a row outside the cache marks padding, one that a request names twice holds a mixture) of the caches.
+        Returns the coded queries. q, v, or k with v and the caches may be None."""
         with self._on(stream) as on:
             returns = ()
             if q is None:

@@ -162,6 +162,29 @@ def test_append_passes_32_bit_offsets(kv):
     del cache
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_append_two_tokens_of_one_row(kv, dtype):
+    """What the row holds then is either token's, element by element; every other row is as without them."""
+    H, K, D, B, T, R = 4, 2, 64, 2, 40, 50
+    h = kv.KV(H, K, D, max_batch=B, max_tokens=T, precision=dtype, rope=kv.Rope(dim=D))
+    q, k, v = rand(1, B, T, H, D, dtype=dtype), rand(2, B, T, K, D, dtype=dtype), rand(3, B, T, K, D, dtype=dtype)
+    pos = i32([list(range(T))] * B)
+    rows = np.stack([np.random.default_rng(b).permutation(R)[:T] for b in range(B)])
+    alone = [torch.zeros((B, R, K, D), dtype=DT[dtype], device="cuda") for _ in range(2)]
+    want_q = h.append(q, k, v, pos, i32(rows), *alone)
+    twice = rows.copy()
+    twice[:, 7] = rows[:, 30]
+    got = [torch.zeros((B, R, K, D), dtype=DT[dtype], device="cuda") for _ in range(2)]
+    assert torch.equal(h.append(q, k, v, pos, i32(twice), *got), want_q)
+    for a, b in zip(got, alone):
+        for n in range(B):
+            one, other = b[n, rows[n, 7]], b[n, rows[n, 30]]
+            assert ((a[n, rows[n, 30]] == one) | (a[n, rows[n, 30]] == other)).all()
+            want = b[n].clone()
+            want[rows[n, 7]], want[rows[n, 30]] = 0, a[n, rows[n, 30]]
+            assert torch.equal(a[n], want)
+
+
 # ------------------------------------------------------------------ attend
 
 def make_call(seed, dtype, H, K, D, B, T, G, P, R, mask="causal", store=lambda t: t, std=2.0):
