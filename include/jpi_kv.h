@@ -109,7 +109,8 @@ JPI_API jpi_status jpi_kv_destroy(jpi_kv_handle* h);   /* NULL is a no-op */
  *   q_out:     device E [batch][tokens][H][D], the coded queries (may alias q where q is contiguous).
  *   cache:     `batch` caches; its k (and v) may be where k (and v) point to, the same rows at the
  *              same addresses.
- * Angles are exact to 2^-32 turns at any position. Sums in fp32, one rounding to E.
+ * Angles are within 2^-26 + |position| 2^-53 turns (2^-26: the phase as an fp32 number; 2^-53: the table, whose
+ * entries are computed in 64-bit floating point). Sums in fp32, one rounding to E.
  */
 JPI_API jpi_status jpi_kv_append(jpi_kv_handle* h, const void* q, long long q_stride, const void* k,
                                  long long k_stride, const void* v, long long v_stride, const int* position,

@@ -3,9 +3,11 @@
 // Pair i of a head, (x1, x2), turns by the angle a = position theta_i:
 //   y1 = m (x1 cos a - x2 sin a),  y2 = m (x2 cos a + x1 sin a).
 // The table holds theta_i / 2 pi, turns per position, as a fraction of 2^64, so that the phase
-// position * turns is an integer product whose wrap-around is the reduction modulo a whole turn:
-// exact to 2^-32 turns for any 32-bit position (2^31 * 2^-65 = 2^-34 from the table, 2^-33 from the
-// 32 leading bits kept), where a 32-bit angle would be off by a whole turn. sincospif takes it from there.
+// position * turns is an integer product whose wrap-around is the reduction modulo a whole turn,
+// without error of its own. The phase is off by the table's error times the position, less than |position| 2^-53 turns (an entry, at
+// most 1 / 2 pi, comes of a power, a quotient or two and a division by 2 pi in 64-bit floating point: a few times 2^-53 of itself), and
+// by 2^-26 where its 32 leading bits become an fp32 number of half turns in [-1, 1): a 32-bit angle would be off by
+// whole turns far out. sincospif takes it from there. At position 131071 that is 2^-26 turns, at 2^31 up to 2^-22.
 //
 // Bound by memory: every element is read and written once. A block takes tokens in turn; a thread has the same
 // units (a 16-byte chunk, or the two chunks of a half-layout pair) of each and copies them asynchronously into shared

@@ -7,6 +7,7 @@ them in fp32 (D + 2 steps of 2^-23 of the sum of |q_d k_d|, doubled for sums tha
 """
 
 import math
+from decimal import Decimal, localcontext
 
 import numpy as np
 import pytest
@@ -160,6 +161,32 @@ def test_append_passes_32_bit_offsets(kv):
     got, _ = kv.KV(1, 1, D).attend(x, prefix=(cache, cache), prefix_len=i32([R]))
     assert got.float().abs().max() > 1e-2      # the last row's weight: e^(|x|^2 / 16) of 2^23 zeros'
     del cache
+
+
+def turns_exact(dim, i, base):
+    """Turns per position of pair i of a plain coding, in 60 digits."""
+    with localcontext() as ctx:
+        ctx.prec = 60
+        two_pi = Decimal("6.28318530717958647692528676655900576839433879875021164194989")
+        return (-(Decimal(base).ln() * 2 * i / dim)).exp() / two_pi
+
+
+def test_append_angles_at_any_position(kv):
+    """Angles within 2^-26 + |position| 2^-53 turns, against 60 digits: pairs (1, 0) become (cos, sin)."""
+    dim, base = 64, 10000.0
+    pos = [0, 1, 7, 816, 4095, 131071, 10 ** 6, 2 ** 24 + 1, 2 ** 28 - 3, 2 ** 30 + 12345, 2 ** 31 - 1, -1, -131071, -(2 ** 31)]
+    T = len(pos)
+    h = kv.KV(1, 1, dim, max_tokens=T, precision="fp32", rope=kv.Rope(dim=dim, base=base))
+    x = torch.zeros((1, T, 1, dim), device="cuda")
+    x[..., :dim // 2] = 1.0
+    got = np64(h.append(x, None, None, i32([pos]), i32([list(range(T))])))[0, :, 0]
+    turns = [turns_exact(dim, i, base) for i in range(dim // 2)]
+    for t, p in enumerate(pos):
+        frac = np.array([float((p * x) % 1) for x in turns])
+        # sines and cosines to 2^-22 beside the angle's bound
+        tol = 2 * math.pi * (2.0 ** -26 + abs(p) * 2.0 ** -53) + 2.0 ** -22
+        for part, want in ((got[t, :dim // 2], np.cos(2 * math.pi * frac)), (got[t, dim // 2:], np.sin(2 * math.pi * frac))):
+            assert np.abs(part - want).max() <= tol, (p, np.abs(part - want).max(), tol)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
