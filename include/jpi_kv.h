@@ -93,7 +93,9 @@ typedef struct jpi_kv_cache {
  * none; append then copies). Synchronous; the only call that allocates. On failure *out is NULL. */
 JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* rope, jpi_kv_handle** out);
 /* The environment read here: JPI_KV_TILES=0 / 1 keeps jpi_kv_attend and jpi_kv_weigh on the kernels for few query rows,
- * or on the tensor-core tiles wherever those fit, for the handle's lifetime (results agree to rounding). */
+ * or on the tensor-core tiles wherever those fit, for the handle's lifetime (results agree to rounding: see
+ * jpi_kv_attend for that of the probabilities). The workspace is attention's and has the same size whichever calls are made:
+ * (2 max_batch max_tokens H + 512 SMs) rows of head_dim + 2 fp32 numbers, 80 MB at least for heads of 256 on 152 SMs. */
 JPI_API jpi_status jpi_kv_destroy(jpi_kv_handle* h);   /* NULL is a no-op */
 
 /*
@@ -134,7 +136,11 @@ JPI_API jpi_status jpi_kv_append(jpi_kv_handle* h, const void* q, long long q_st
  * of a NaN in the query or in a key that it sees, makes out and lse NaN, and so the weights that jpi_kv_weigh
  * forms with them. An infinite value that a query sees makes the element infinite, NaN where both signs meet or where
  * its weight is below the least that fp32 holds. Nothing in rows that a query does not see reaches it, infinities and
- * NaN included. Scores, softmax and sums in fp32; results do not depend on the run.
+ * NaN included. Scores, softmax and sums in fp32; results do not depend on the run. In JPI_BF16 mode the
+ * probabilities enter the second product as bf16: calls of many query rows on the same keys, which take the 128-row
+ * tensor-core tiles, round each once (off by at most 2^-8 of itself, so an element by at most 2^-8 of the sum of
+ * p |v|); the others carry what the rounding left as a second term (2^-16). A handle made with JPI_KV_TILES=0 always has both
+ * terms, at the row kernels' speed.
  */
 JPI_API jpi_status jpi_kv_attend(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
                                  const jpi_kv_cache* prefix, int groups, const int* prefix_len,

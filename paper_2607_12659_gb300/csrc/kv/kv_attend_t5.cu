@@ -19,9 +19,9 @@
 // inside a token's heads) into tensor memory as the A operand of the score products, which leaves all of shared memory
 // to keys and values.
 //
-// Probabilities are rounded to bf16 once (2^-9 on average of independent signs): with 128 rows a block there is
-// no time for a second term as in the row kernel, and the result's own rounding to bf16 is as large.
-// The sum l takes them unrounded.
+// Probabilities are rounded to bf16 once, each off by at most 2^-8 of itself, of either sign: with 128 rows a block there is
+// no time for a second term as in the row kernel, which would be half as many products again, and the result's own rounding to
+// bf16 is as large. The sum l takes them unrounded. A handle made with JPI_KV_TILES=0 does not come here.
 //
 // Rows past the last one that a query row of the tile sees may hold anything: their scores are replaced, and their
 // values are cleared in shared memory before the product, since 0 times a NaN would reach every row. Own rows that

@@ -386,6 +386,18 @@ def test_attend_lowest_values_and_lengths_out_of_range(kv):
     assert torch.equal(out[0, 0, 0], v[0, 0, 0])     # the only key, however low its score
 
 
+@pytest.mark.parametrize("tiles,prob", [("0", 2.0 ** -16), ("1", 2.0 ** -8)])
+@pytest.mark.parametrize("H,K,D,B,T,G,P,R", [(8, 1, 256, 8, 20, 2, 300, 30), (16, 2, 128, 40, 1, 1, 700, 20), (8, 1, 64, 2, 64, 1, 40, 300)])
+def test_attend_rounding_of_the_probabilities(kv, monkeypatch, tiles, prob, H, K, D, B, T, G, P, R):
+    """Two bf16 terms in the row kernels (each half an eps of what it holds: 2^-8 of 2^-8), one on the tiles."""
+    monkeypatch.setenv("JPI_KV_TILES", tiles)
+    c = make_call(D, "bf16", H, K, D, B, T, G, P, R)
+    out, lse = kv.KV(H, K, D, max_batch=B, max_tokens=T).attend(**c)
+    ref, rlse, dot, mass = attend_ref(c, 1 / math.sqrt(D))
+    tol, _ = attend_tols(c, "fp32", ref, dot, mass, rlse)      # scores, 2^x and sums
+    within(out, ref, tol - HALF_EPS["fp32"] * np.abs(ref) + HALF_EPS["bf16"] * np.abs(ref) + prob * (1 + 2.0 ** -7) * mass, "out")
+
+
 # ------------------------------------------------------------------ weigh
 
 def check_weigh(kv, dtype, H, K, D, B, T, G, P, R, seed=0, decay=0.75, with_in=True, **kw):
