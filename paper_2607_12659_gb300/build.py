@@ -113,6 +113,8 @@ def build_kv_calls(verbose: bool = False, force: bool = False) -> str:
     if not force and os.path.exists(KV_CALLS_LIB) and os.path.exists(stamp) and open(stamp).read() == made and all(
             os.path.getmtime(d) <= os.path.getmtime(KV_CALLS_LIB) for d in deps):
         return KV_CALLS_LIB
+    if os.path.exists(KV_CALLS_LIB):   # (of another source, torch or Python: not to be imported should this build fail)
+        os.remove(KV_CALLS_LIB)
     tmp = KV_CALLS_LIB + ".tmp"
     r = subprocess.run(cmd + ["-o", tmp], capture_output=True, text=True)
     if r.returncode != 0:

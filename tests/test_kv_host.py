@@ -201,3 +201,16 @@ def test_a_missing_module_of_checks_is_an_error(lib, monkeypatch):
     monkeypatch.delattr("paper_2607_12659_gb300._kv", raising=False)
     with pytest.raises(RuntimeError, match="not built"):
         kv._checked_calls(8, 2, 64, True, 0)
+
+
+def test_a_module_that_does_not_build_leaves_no_older_one(tmp_path, monkeypatch):
+    """One built for another torch or Python would be imported in its place."""
+    for name, file in (("BUILD", "."), ("KV_CALLS_LIB", "_kv.so")):
+        monkeypatch.setattr(build, name, str(tmp_path / file))
+    (tmp_path / "_kv.so").write_bytes(b"older")
+    (tmp_path / "kv_calls.txt").write_text("older")
+    for compiler in ("false", "no-such-compiler"):
+        monkeypatch.setenv("CXX", compiler)
+        with pytest.raises((RuntimeError, OSError)):
+            build.build_kv_calls()
+        assert not (tmp_path / "_kv.so").exists()
