@@ -192,8 +192,6 @@ struct jpi_handle {
     int n_corr = 0, corr_batch = 0;
     int n_ctx() const { return 1 + n_corr; }
     cudaStream_t cap_stream = nullptr;
-    std::map<jpi::GraphKey, cudaGraphExec_t> graphs;
-    std::map<jpi::GraphKey, int> graph_kernels;
 };
 
 namespace jpi {
@@ -205,8 +203,6 @@ jpi_status launch_time_conditioning(jpi_handle* h, int nsteps, cudaStream_t st);
 jpi_status launch_time_conditioning_into(jpi_handle* h, double t, float* temb, float* c1,
                                          float* cond, cudaStream_t st);
 jpi_status launch_embed(jpi_handle* h, int step, int batch, int chunk, const float* x, cudaStream_t st);
-jpi_status launch_layer_simt(jpi_handle* h, int layer, int step, int batch, int chunk,
-                             cudaStream_t st);
 // One sub-step of a layer (ops 2..6 of jpi_profile_op).
 jpi_status launch_op_simt(jpi_handle* h, int op, int layer, int step, int batch, int chunk,
                           cudaStream_t st);

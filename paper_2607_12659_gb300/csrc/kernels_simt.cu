@@ -1509,11 +1509,6 @@ jpi_status launch_op_simt(jpi_handle* h, int op, int layer, int step, int B, int
                    : op_simt<float>(h, op, layer, step, B, C, st);
 }
 
-jpi_status launch_layer_simt(jpi_handle* h, int layer, int step, int B, int C, cudaStream_t st) {
-    for (int op = 2; op <= 6; ++op) JPI_TRY(launch_op_simt(h, op, layer, step, B, C, st));
-    return JPI_OK;
-}
-
 jpi_status launch_final(jpi_handle* h, int step, int B, int C, float delta, float* x_inout, float* v_out,
                         cudaStream_t st) {
     const int W = h->W, rows = B * C;

@@ -747,11 +747,6 @@ jpi_status tc_launch_op(jpi_handle* h, int op, int l, int step, int B, int C, cu
     }
 }
 
-jpi_status tc_launch_layer(jpi_handle* h, int l, int step, int B, int C, cudaStream_t st) {
-    for (int op = 2; op <= 6; ++op) JPI_TRY(tc_launch_op(h, op, l, step, B, C, st));
-    return JPI_OK;
-}
-
 void tc_release(jpi_handle*) {}
 
 }  // namespace jpi

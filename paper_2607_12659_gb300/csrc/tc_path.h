@@ -10,10 +10,7 @@ bool tc_supported(const jpi_handle* h);
 jpi_status tc_pack_layers(jpi_handle* h, const jpi_weights* w, float* tmp, bool on_device);
 // Builds tensor maps, workspaces and kernel attributes once the buffers exist.
 jpi_status tc_prepare(jpi_handle* h);
-// Enqueues one expert layer (norm + QKV + rotary, attention, O-proj, norm + GeGLU, down).
-jpi_status tc_launch_layer(jpi_handle* h, int layer, int step, int batch, int chunk,
-                           cudaStream_t st);
-// One sub-step of a layer (ops 2..6 of jpi_profile_op).
+// One sub-step of an expert layer (ops 2..6 of jpi_profile_op: norm + QKV + rotary, attention, O-proj, norm + GeGLU, down).
 jpi_status tc_launch_op(jpi_handle* h, int op, int layer, int step, int batch, int chunk,
                         cudaStream_t st);
 // Tensor-core attention (attn_tc.cu).
