@@ -182,7 +182,8 @@ JPI_API jpi_status jpi_commit_prefix(jpi_handle* h, int batch, int prefix_len);
  * jpi_evict_prefix: keeps `keep` tokens of every stored prefix, layer by layer those with the largest w (as
  *   jpi_kv_evict: the first `sink`, the last `recent`, the best of the others, in their order), in
  *   place, and makes the shorter prefix current. The suffix tokens keep their rotary positions (those
- *   after the whole prefix). w is moved with the keys, [n_layers][batch][keep] at the old strides.
+ *   after the whole prefix). w is moved with the keys, [n_layers][batch][keep] at the old strides: the calls on the
+ *   shorter prefix take [n_layers][batch][keep] without gaps, so the caller copies it to that.
  *   kept: device int [n_layers][batch][keep], the tokens that stay, or NULL.
  * jpi_append_prefix: `tokens` further prefix tokens behind the stored ones, prefix_len + tokens <= max_prefix (of
  *   the prefix as it is now: rows that jpi_evict_prefix freed take new tokens):

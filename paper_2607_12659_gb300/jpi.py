@@ -396,8 +396,9 @@ class Expert:
         return w
 
     def evict_prefix(self, w, keep, sink=0, recent=0, stream=None):
-        """Cuts every stored prefix to `keep` tokens by the weights w (as weigh_prefix gives them; moved with the keys).
-        Returns the tokens that stay, int32 [L][prefix batch][keep]."""
+        """Cuts every stored prefix to `keep` tokens by the weights w (as weigh_prefix gives them). Their weights move with
+        them to w[..., :keep]; for the next weigh_prefix or evict_prefix, which take the cut prefix's, that is to be copied:
+        w[..., :keep].contiguous(). Returns the tokens that stay, int32 [L][prefix batch][keep]."""
         import torch
         self._weights(w)
         with OnStream(stream, w.device) as on:

@@ -302,3 +302,28 @@ def test_tokens_appended_to_what_eviction_left(cfg, share, monkeypatch):
         assert_close(ex.denoise(state, noise, 2).cpu().numpy(), oracle_denoise(cfg, w, r, 2), cfg, "a new prefix")
     finally:
         ex.close()
+
+
+def test_weights_go_on_after_an_eviction():
+    """The moved weights are the first `keep` of each row: a contiguous copy of them is the cut prefix's."""
+    cfg, P, B, C, keep = SMALL_BF16, 50, 2, 6, 30
+    r = make_requests(cfg, 9, B, P, C)
+    ex = make_expert(cfg, make_weights(cfg, 0), max_batch=B, max_prefix=P, max_chunk=C, max_steps=1)
+    try:
+        ex.set_prefix_kv(*to_dev_kv(r, cfg))
+        state, noise = dev(r["state"]), dev(r["noise"])
+        w = torch.zeros((cfg.n_layers, B, P), device="cuda")
+        ex.weigh_prefix(state, noise, 0.5, w)
+        ex.evict_prefix(w, keep, sink=1, recent=2)
+        with pytest.raises(ValueError):
+            ex.weigh_prefix(state, noise, 0.5, w)
+        moved = w[..., :keep].contiguous()
+        once = ex.weigh_prefix(state, noise, 0.5, torch.zeros_like(moved))
+        both = ex.weigh_prefix(state, noise, 0.5, moved.clone())
+        # one product and one sum, rounded once or twice: an eps of the sum
+        assert ((both - (moved + once)).abs() <= 2.0 ** -23 * both).all() and once.sum() > 0
+        kept = ex.evict_prefix(both, keep - 7)
+        assert torch.equal(kept, torch.topk(moved + once, keep - 7).indices.sort(-1).values.int())
+        ex.device_status()
+    finally:
+        ex.close()
