@@ -327,3 +327,50 @@ def test_weights_go_on_after_an_eviction():
         ex.device_status()
     finally:
         ex.close()
+
+
+def test_the_c_entry_points_on_the_stored_prefix():
+    """The operators on the expert's own store, by its addresses (jpi_prefix_kv_ptr): what they give on copies of it."""
+    from paper_2607_12659_gb300 import jpi, kv
+    cfg, P, B, T, layer = SMALL_BF16, 40, 2, 5, 1
+    H, D = cfg.n_heads, cfg.head_dim
+    r = make_requests(cfg, 10, B, P, 4)
+    ex = make_expert(cfg, make_weights(cfg, 0), max_batch=B, max_prefix=P, max_chunk=4, max_steps=1)
+    h = kv.KV(H, 1, D, max_batch=B, max_tokens=T, rope=kv.Rope(dim=D))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    try:
+        k, v = to_dev_kv(r, cfg)
+        ex.set_prefix_kv(k, v)
+        ck, cv = (t[layer][:, :, None].clone() for t in (k, v))      # [B][P][1][D]
+        pk, pv, stride = jpi.jpi_prefix_kv_ptr(ex.handle, layer)
+        store = kv.jpi_kv_cache(pk, pv, stride, D, D, 0, P)
+        q, nk, nv = new(B, T, H, D), new(B, T, 1, D), new(B, T, 1, D)
+        pos, rows = i32([[7 + t for t in range(T)]] * B), i32([[P - T + t for t in range(T)]] * B)
+        coded = torch.empty_like(q)
+        kv.jpi_kv_append(h.handle, q, H * D, nk, D, nv, D, pos, rows, B, T, coded, store)
+        assert torch.equal(coded, h.append(q, nk, nv, pos, rows, ck, cv))
+        length, seen = i32([P] * B), i32([[P - T + 1 + t for t in range(T)]] * B)
+        for side in (dict(prefix=store, groups=B, prefix_len=length, own=None, seen=None), dict(prefix=None, groups=1, prefix_len=None, own=store, seen=seen)):
+            out, lse = torch.empty_like(q), torch.empty((B, T, H), device="cuda")
+            kv.jpi_kv_attend(h.handle, coded, H * D, B, T, out=out, lse=lse, **side)
+            name = "prefix" if side["prefix"] else "own"
+            lens = dict(prefix_len=length) if side["prefix"] else dict(seen=seen)
+            want = h.attend(coded, **{name: (ck, cv)}, **lens)
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+            w = torch.zeros((B, 1, P), device="cuda")
+            into = dict(prefix_in=None, prefix_out=None, own_in=None, own_out=None)
+            into[name + "_out"] = w
+            kv.jpi_kv_weigh(h.handle, coded, H * D, lse, B, T, decay=1.0, **side, **into)
+            assert torch.equal(w, [x for x in h.weigh(coded, lse, **{name: ck}, **lens) if x is not None][0])
+        kept, cut, n = torch.empty((1, B, 1, 25), dtype=torch.int32, device="cuda"), w.clone(), length.clone()
+        kv.jpi_kv_evict(h.handle, store, cut, n, 1, B, 25, 2, 3, store, cut, n, kept)
+        assert torch.equal(kept, h.evict(ck[None], cv[None], w[None], length, 25, 2, 3))
+        assert torch.equal(cut, w) and torch.equal(n, length) and n.tolist() == [25] * B
+        out, lse = torch.empty_like(q), torch.empty((B, T, H), device="cuda")
+        kv.jpi_kv_attend(h.handle, coded, H * D, B, T, store, B, n, None, None, out, lse)
+        assert torch.equal(out, h.attend(coded, prefix=(ck, cv), prefix_len=n)[0])
+        h.device_status()
+    finally:
+        ex.close()
