@@ -174,7 +174,10 @@ JPI_API jpi_status jpi_commit_prefix(jpi_handle* h, int batch, int prefix_len);
  * jpi_share_prefix: from now on each stored prefix serves `requests` consecutive requests of a call
  *   (several action chunks drawn from one observation): a call's batch is requests x the prefix's batch,
  *   at most max_batch, and attention reads each prefix once for all of them. 1: one request a prefix,
- *   the default. Calls that set or commit a prefix keep it.
+ *   the default. Calls that set or commit a prefix keep it. It saves the copies and the time to make them; an evaluation
+ *   takes longer than over a copy for every request while prefixes are short (8 requests of 50 actions, pi0.5:
+ *   18% over 816 tokens, 7% over 4096, 5% less over 16384) and less where they are long or the actions few (16 requests
+ *   of 8: 8% longer over 816, 7% less over 4096, 36% less over 16384).
  * jpi_weigh_prefix: one expert evaluation at flow time t (arguments as in jpi_expert_forward; its velocity is
  *   not returned) that adds up the attention weight each prefix key receives from all suffix tokens and heads of
  *   the requests that share it: w = decay w + weight, device fp32 [n_layers][prefix batch][prefix_len];
