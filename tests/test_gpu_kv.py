@@ -672,6 +672,30 @@ def test_calls_on_another_stream_and_in_a_graph(kv):
         assert torch.equal(a, b)
 
 
+def test_several_handles_at_once(kv):
+    """Three handles on three streams share the SMs (tensor memory among them) and nothing else: what they give alone, bit for bit."""
+    shapes = [(8, 1, 256, 48, 2, 1, 4000, 300), (32, 8, 128, 24, 1, 1, 9000, 200), (8, 1, 64, 40, 4, 2, 3000, 100)]
+    runs = []
+    for i, (H, K, D, B, T, G, P, R) in enumerate(shapes):
+        c = clean_call(i, "bf16", H, K, D, B, T, G, P, R)
+        h = kv.KV(H, K, D, max_batch=B, max_tokens=T)
+        keys = dict(prefix=c["prefix"][0], prefix_len=c["prefix_len"], own=c["own"][0], seen=c["seen"])
+        out, lse = h.attend(**c)
+        runs.append((h, c, keys, out, lse, h.weigh(c["q"], lse, **keys), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(8):
+        for h, c, keys, _, _, _, stream in runs:
+            out, lse = h.attend(**c, stream=stream)
+            got.append((out, lse, *h.weigh(c["q"], lse, **keys, stream=stream)))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        h, _, _, out, lse, w, _ = runs[i % len(runs)]
+        h.device_status()
+        for a, b in zip(g, (out, lse, *w)):
+            assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------ refusals
 
 def test_refusals_of_the_entry_points(kv):
