@@ -2,6 +2,8 @@
 jpi_commit_prefix_at) against the fp64 oracle: several requests over one prefix, the weights its keys receive,
 denoises over what eviction leaves and over appended tokens. Tolerances of the denoise are the expert's own."""
 
+import contextlib
+
 import numpy as np
 import pytest
 
@@ -372,5 +374,33 @@ def test_the_c_entry_points_on_the_stored_prefix():
         kv.jpi_kv_attend(h.handle, coded, H * D, B, T, store, B, n, None, None, out, lse)
         assert torch.equal(out, h.attend(coded, prefix=(ck, cv), prefix_len=n)[0])
         h.device_status()
+    finally:
+        ex.close()
+
+
+@pytest.mark.parametrize("cfg,groups,share,P,C", [(TINY, 1, 3, 40, 6), (SMALL_BF16, 2, 2, 50, 7), (SMALL_BF16, 1, 12, 300, 33)])
+def test_a_broken_request_shows_and_stays_alone(cfg, groups, share, P, C):
+    """NaN in one request's state: its actions are NaN (its own state token is a key that they see), the other requests of the
+    prefix get what they get without it, and the weights of that prefix's keys are NaN."""
+    B = groups * share
+    r, slots = shared(cfg, 11, groups, share, P, C)
+    ex = make_expert(cfg, make_weights(cfg, 0), max_batch=B, max_prefix=P, max_chunk=C, max_steps=2)
+    try:
+        k, v = to_dev_kv(r, cfg)
+        ex.share_prefix(share)
+        ex.set_prefix_kv(k[:, slots], v[:, slots])
+        state, noise = dev(r["state"]), dev(r["noise"])
+        want = ex.denoise(state, noise, 2).clone()
+        broken = state.clone()
+        broken[-1, 0] = float("nan")
+        got = ex.denoise(broken, noise, 2)
+        assert want.isfinite().all() and got[-1].isnan().all() and torch.equal(got[:-1], want[:-1])
+        w = ex.weigh_prefix(broken, noise, 0.5, torch.zeros((cfg.n_layers, groups, P), device="cuda"))
+        assert w[:, -1].isnan().all() and w[:, :-1].isfinite().all()
+        # The bf16 projections exchange partial sums as fp16 and report that these did not fit (code 4; no wait gave up).
+        with pytest.raises(lib().JpiError, match="code 4") if cfg.precision == "bf16" else contextlib.nullcontext():
+            ex.device_status()
+        assert torch.equal(ex.denoise(state, noise, 2), want)
+        ex.device_status()
     finally:
         ex.close()
