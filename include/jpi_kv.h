@@ -8,13 +8,17 @@
  *   - Sec. 4.3 ("System Design"): intermediate buffers stay on the GPU, and nothing a call does
  *     depends on a host copy: lengths and rows are read from device memory, so that one captured
  *     graph serves a growing cache.
- * The operators themselves (rotary coding of parts and scalings of long contexts, one prefix for
- * many requests, eviction by accumulated attention weight) are no part of the paper.
+ * The operators themselves (rotary coding of parts and scalings of long contexts, norms of heads, one prefix for
+ * many requests, windows, caches in 8 bits, eviction by accumulated attention weight) are no part of the paper.
  *
- *   jpi_kv_append   rotary coding of new queries and keys, keys and values written into the cache
- *   jpi_kv_attend   attention of a batch over shared prefixes and each request's own rows
- *   jpi_kv_weigh    the attention weight each cached key received, accumulated
- *   jpi_kv_evict    the rows with the most of it kept, in order, the others dropped
+ *   jpi_kv_append         rotary coding of new queries and keys, keys and values written into the cache
+ *   jpi_kv_append_normed  the same after a norm of each head's queries and keys
+ *   jpi_kv_attend         attention of a batch over shared prefixes and each request's own rows
+ *   jpi_kv_attend_window  attention over the newest rows before each token and a few first ones
+ *   jpi_kv_weigh          the attention weight each cached key received, accumulated
+ *   jpi_kv_evict          the rows with the most of it kept, in order, the others dropped
+ *   jpi_kv8_append        new tokens into a cache held in 8 bits, with a scale for each block of rows and head
+ *   jpi_kv8_attend        attention over such a cache, its window included
  *
  * A jpi_kv_handle fixes the attention's geometry, its rotary coding and the maxima of a call, and
  * owns the workspace. Caches belong to the caller: the expert's store (jpi_prefix_kv_ptr), the
@@ -181,6 +185,86 @@ JPI_API jpi_status jpi_kv_weigh(jpi_kv_handle* h, const void* q, long long q_str
 JPI_API jpi_status jpi_kv_evict(jpi_kv_handle* h, const jpi_kv_cache* src, const float* w, const int* length,
                                 int layers, int caches, int keep, int sink, int recent, const jpi_kv_cache* dst,
                                 float* w_out, int* length_out, int* kept, void* stream);
+
+/* Norms of a head's queries and keys before their rotary coding: x / sqrt(mean(x^2) + eps) * weight, over the D
+ * elements of each head. */
+typedef struct jpi_kv_norm {
+    const float *q_weight, *k_weight;   /* device fp32 [D], 4-byte aligned; NULL: ones                */
+    float eps;                          /* 2^-126 or more, finite                                    */
+} jpi_kv_norm;
+
+/*
+ * jpi_kv_append after a norm of each head of q and k, in one pass; v is copied. Arguments and what is written as there.
+ * Squares are summed in fp32 (a head whose squares pass fp32's range is summed again at 2^-70 of its values, so that finite
+ * values give finite norms); everything up to the one rounding to E is fp32.
+ */
+JPI_API jpi_status jpi_kv_append_normed(jpi_kv_handle* h, const void* q, long long q_stride, const void* k,
+                                        long long k_stride, const void* v, long long v_stride, const jpi_kv_norm* norm,
+                                        const int* position, const int* row, int batch, int tokens, void* q_out,
+                                        const jpi_kv_cache* cache, void* stream);
+
+/*
+ * Attention over a window: query token (b, t) sees of cache b's rows before seen[b][t] the first `sink` ones and the
+ * last `window` ones, rows r < seen with r < sink or r >= seen - window.
+ *   cache:   `batch` caches
+ *   seen:    device int [batch][tokens]; taken as 0 .. cache->rows (0: padding, which sees nothing)
+ *   window:  >= 1;  sink: >= 0
+ * q, out, lse, empty rows, NaN and infinities as in jpi_kv_attend; rows outside a token's window are rows that it does not
+ * see, and rows that no token of a call sees are not read. The work follows the windows, not the cache's length. In
+ * JPI_BF16 mode the probabilities enter the second product as there: calls of many query rows on the 128-row
+ * tiles round each to bf16 once, the others carry what the rounding left. JPI_KV_TILES holds here too.
+ */
+JPI_API jpi_status jpi_kv_attend_window(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
+                                        const jpi_kv_cache* cache, const int* seen, int window, int sink, void* out,
+                                        float* lse, void* stream);
+
+/*
+ * `n` caches of `rows` rows in 8 bits: element d of KV head h in row r of cache c is an e4m3 number at
+ * base + c cache_stride + r row_stride + h head_stride + d (bytes; strides multiples of 16 as the base is), times
+ * 2^(s - 127) with s the byte (e8m0) of its block of `block` rows and head, scale[c][h][r / block], contiguous
+ * [n][Hk][ceil(rows / block)]. A scale of 255 is NaN and makes the block's elements NaN. head_dim is a multiple of 16
+ * (else JPI_ERR_UNSUPPORTED).
+ */
+typedef struct jpi_kv8_cache {
+    void *k, *v;
+    unsigned char *k_scale, *v_scale;
+    long long cache_stride, row_stride, head_stride;
+    int rows;
+    int block;        /* 16, 32 or 64 rows                                                           */
+} jpi_kv8_cache;
+
+/*
+ * Rotary coding, with `norm` (may be NULL: none) after norms as in jpi_kv_append_normed, and the write into 8-bit caches:
+ * token t < count[b] of request b goes to row start[b] + t of cache b.
+ *   start:  device int [batch], the rows that cache b holds before the call; what later rows hold is taken as nothing. A
+ *           start outside 0 .. cache->rows - 1 marks a request of padding only.
+ *   count:  device int [batch], taken as 0 .. tokens; NULL: tokens. Later tokens, and those that would pass the last row, are
+ *           padding: nothing is written for them, their q_out included.
+ * A block that holds no row before `start` gets the least scale 2^k, -126 <= k, at which its new elements' magnitudes are at
+ * most 448 (in the block, of one head; keys and values by themselves). One that does keeps its scale or has it raised to
+ * that, and its rows before `start` are rounded again to the new scale: a step of a power of two, exact but for
+ * elements below 2^-6 of the new scale, which move by at most 2^-10 of it. Each new element is rounded once, from fp32 to the nearest code
+ * (off by at most 2^-4 of itself, or 2^-10 of the scale). Infinities and NaN do not count for the scale and are held
+ * as NaN. Rows of a block behind the new ones are left as they are; a scale of 255 under rows before `start` stays.
+ * k and v go together. Everything else as in jpi_kv_append.
+ */
+JPI_API jpi_status jpi_kv8_append(jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
+                                  const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position,
+                                  const int* start, const int* count, int batch, int tokens, void* q_out,
+                                  const jpi_kv8_cache* cache, void* stream);
+
+/*
+ * Attention over 8-bit caches: query token (b, t) sees rows 0 .. seen[b][t] - 1 of cache b, with window >= 1 as in
+ * jpi_kv_attend_window (0: all of them, and `sink` is not used). q, out and lse are as in jpi_kv_attend, of the handle's type; so
+ * are empty rows, and NaN in what a query sees.
+ * Scores, softmax and sums in fp32, codes and scales taken as they are. JPI_BF16 mode: queries enter the first product scaled by a
+ * power of two as fp16 (bf16's eight bits whole; an element below 2^-14 of its head's largest is off by at most 2^-25 of that)
+ * or as bf16, the probabilities the second as two fp16 terms (2^-22 of each, or 2^-31 of what the largest value of the blocks
+ * seen would weigh) or, on the 128-row tiles, as bf16 once (2^-8).
+ */
+JPI_API jpi_status jpi_kv8_attend(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
+                                  const jpi_kv8_cache* cache, const int* seen, int window, int sink, void* out,
+                                  float* lse, void* stream);
 
 /* Synchronises the device and reports device-side errors of earlier calls, as jpi_device_status. */
 JPI_API jpi_status jpi_kv_device_status(jpi_kv_handle* h);

@@ -148,3 +148,96 @@ def evict(w, n, keep, sink, recent) -> list:
     # Python's sort is stable: ties keep the lowest row first; NaN below everything.
     rest.sort(key=lambda i: (1, 0.0) if math.isnan(w[i]) else (0, -float(w[i])))
     return sorted(first + rest[:keep - len(first)])
+
+
+# ------------------------------------------------------------------ norms, windows, 8 bits
+
+def norm(x, weight, eps) -> np.ndarray:
+    """Heads x [..][D] divided by the root of their mean square, times the weight (None: ones)."""
+    x = x.astype(F64)
+    y = x / np.sqrt((x * x).mean(-1, keepdims=True) + float(np.float32(eps)))
+    return y if weight is None else y * weight.astype(F64)
+
+
+def append_normed(q, k, v, positions, rows, cache_k, cache_v, r, q_weight, k_weight, eps):
+    return append(norm(q, q_weight, eps), norm(k, k_weight, eps), v, positions, rows, cache_k, cache_v, r)
+
+
+def visible(n, rows, window, sink) -> np.ndarray:
+    """Rows that a token of count n sees of a cache of `rows` rows (window 0: all before n)."""
+    n = min(max(int(n), 0), rows)
+    r = np.arange(n)
+    return r if window == 0 else r[(r < sink) | (r >= n - window)]
+
+
+def attend_window(q, k, v, seen, window, sink, scale):
+    """(out, lse, dot, mass) as attend's, over the rows that `visible` says."""
+    B, T, H, D = q.shape
+    K = k.shape[2]
+    out, lse = np.zeros(q.shape, F64), np.full((B, T, H), -np.inf)
+    dot, mass = np.zeros((B, T, H)), np.zeros(q.shape, F64)
+    for b in range(B):
+        for t in range(T):
+            at = visible(seen[b, t], k.shape[1], window, sink)
+            if len(at) == 0:
+                continue
+            x = q[b, t].astype(F64).reshape(K, H // K, D)
+            kk, vv = k[b, at].astype(F64), v[b, at].astype(F64)
+            s = scale * np.einsum("kgd,jkd->kgj", x, kk)
+            m = s.max(-1, keepdims=True)
+            p = np.exp(s - m)
+            tot = p.sum(-1, keepdims=True)
+            lse[b, t] = (m + np.log(tot)).reshape(H)
+            p /= tot
+            out[b, t] = np.einsum("kgj,jkd->kgd", p, vv).reshape(H, D)
+            dot[b, t] = scale * np.einsum("kgd,jkd->kgj", np.abs(x), np.abs(kk)).max(-1).reshape(H)
+            mass[b, t] = np.einsum("kgj,jkd->kgd", p, np.abs(vv)).reshape(H, D)
+    return out, lse, dot, mass
+
+
+def e4m3(x) -> np.ndarray:
+    """The e4m3 number nearest to each x of magnitude up to 448 (ties to the even one); what is not finite becomes NaN."""
+    x = np.asarray(x, F64)
+    _, p = np.frexp(np.maximum(np.abs(np.where(np.isfinite(x), x, 0.0)), 2.0 ** -6))
+    step = np.ldexp(1.0, p - 4)
+    return np.where(np.isfinite(x), np.rint(np.where(np.isfinite(x), x, 0.0) / step) * step, np.nan)
+
+
+def scale8(x) -> int:
+    """The byte of the least power of two 2^(byte - 127), byte >= 1, at which the finite x are at most 448 of it."""
+    x = np.abs(np.asarray(x, F64))
+    top = float(x[np.isfinite(x)].max(initial=0.0))
+    m, p = math.frexp(top / 448.0)
+    return max(1, (p if m > 0.5 else p - 1) + 127) if top > 0 else 1
+
+
+def append8(x, start, count, codes, scales, block):
+    """(codes, scales) of 8-bit caches after rows x [B][T][K][D] (coded already, fp64) went to rows start .. : codes are e4m3
+    numbers [B][R][K][D], scales bytes [B][K][blocks]."""
+    codes, scales = codes.astype(F64).copy(), scales.astype(np.int64).copy()
+    B, T, K, _ = x.shape
+    R = codes.shape[1]
+    for b in range(B):
+        s = int(start[b])
+        if not 0 <= s < R:
+            continue
+        end = min(R, s + min(max(int(count[b]), 0), T))
+        for i in range(s // block, (end - 1) // block + 1 if end > s else 0):
+            lo, hi = max(s, i * block), min(end, (i + 1) * block)
+            for h in range(K):
+                part = x[b, lo - s:hi - s, h]
+                e = scale8(part)
+                if i * block < s:
+                    old = int(scales[b, h, i])
+                    e = max(e, old)
+                    if e > old:
+                        codes[b, i * block:s, h] = e4m3(codes[b, i * block:s, h] * 2.0 ** (old - e))
+                scales[b, h, i] = e
+                codes[b, lo:hi, h] = e4m3(part * 2.0 ** (127 - e)) if e < 255 else np.nan
+    return codes, scales
+
+
+def values8(codes, scales, block) -> np.ndarray:
+    """The numbers that 8-bit caches hold."""
+    s = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(F64) - 127))
+    return codes.astype(F64) * np.repeat(s, block, axis=2)[:, :, :codes.shape[1]].transpose(0, 2, 1)[..., None]

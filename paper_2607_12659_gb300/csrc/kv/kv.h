@@ -70,6 +70,12 @@ jpi_status kv_append_prepare();
 jpi_status launch_kv_append(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
                             const void* v, long long v_stride, const int* position, const int* row, int batch,
                             int tokens, void* q_out, const jpi_kv_cache* cache, cudaStream_t st);
+jpi_status launch_kv_append_normed(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
+                                   const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position, const int* row,
+                                   int batch, int tokens, void* q_out, const jpi_kv_cache* cache, cudaStream_t st);
+jpi_status launch_kv8_append(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
+                             const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position, const int* start,
+                             const int* count, int batch, int tokens, void* q_out, const jpi_kv8_cache* cache, cudaStream_t st);
 jpi_status launch_kv_attend(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, cudaStream_t st);
 jpi_status launch_kv_weigh(jpi_kv_handle* h, const KvCall& c, const float* lse, float decay, const float* prefix_in,
                            float* prefix_out, const float* own_in, float* own_out, cudaStream_t st);

@@ -1,0 +1,220 @@
+// New tokens into a cache held in 8 bits (jpi_kv8_append).
+//
+// An element x of a block of rows and head is held as the e4m3 code of x / s, s = 2^(e - 127) the least power of two with
+// max |x| <= 448 s over the block's elements: division by s is exact, so a code is one rounding of fp32 x, and a scale that
+// grows as rows come moves the codes before by a power of two, which e4m3 holds exactly but for its subnormals. (A scale that is
+// the maximum itself would round every code of the block again at each step.)
+//
+// Bound by memory. A block of threads has one KV head's keys or values in one block of rows: the new rows' loads are on
+// their way together, held by groups of lanes (kv_heads.cuh), which normalise and turn them in registers; the maximum is
+// joined over the block, and the codes are written from the same registers. A (row, pair) has one user here, so its sine
+// and cosine need no table. The queries' tokens are blocks of the same launch.
+
+#include "kv8.cuh"
+#include "kv_heads.cuh"
+
+namespace jpi {
+namespace {
+
+struct Append8Args {
+    HeadArgs h;               // (its H queries; K of them are none of its tokens' blocks')
+    CodeTokens ct;            // of the queries
+    int K;
+    const int *start, *count;
+    uint8_t *ck, *cv, *ks, *vs;
+    long long cs, rs, hs;
+    int rows, n_log2, nblk;   // rows of a cache, of a block (log2), blocks of a cache
+    int touch;                // blocks that a request's tokens can touch
+    uint32_t units;           // blocks of threads of keys and values; the queries' follow
+    KvDiv by_touch, by_K;
+};
+
+// Rows [first, end) of cache b that the call writes.
+__device__ __forceinline__ int2 new_rows(const Append8Args& a, int b) {
+    const int s = a.start[b], c = a.count ? min(max(a.count[b], 0), a.h.tokens) : a.h.tokens;
+    if (s < 0 || s >= a.rows) return make_int2(0, 0);
+    return make_int2(s, min(s + c, a.rows));
+}
+
+template <typename E, int MODE>
+__device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit) {
+    constexpr int V = Chunk<E>::V;
+    constexpr int PASSES = V == 8 ? 4 : 8;   // rows of a group of lanes: 64 rows at 16 (bf16) or 8 groups
+    __shared__ float most[CT_THREADS / 32];
+    uint32_t j, kvh;
+    const bool value = unit & 1;
+    const int b = (int)a.by_K.div(a.by_touch.div(unit >> 1, j), kvh);
+    const int2 span = new_rows(a, b);
+    const int first = ((span.x >> a.n_log2) + (int)j) << a.n_log2, lo = max(first, span.x), hi = min(first + (1 << a.n_log2), span.y);
+    if (lo >= hi) return;
+    const int t = threadIdx.x, groups = blockDim.x >> a.h.lanes_log2, grp = t >> a.h.lanes_log2;
+    const HeadLane<E, MODE> ln(t & ((1 << a.h.lanes_log2) - 1), a.h.D, a.h.dim);
+    uint8_t* scale = (value ? a.vs : a.ks) + ((long long)b * a.K + kvh) * a.nblk + (first >> a.n_log2);
+    uint8_t* codes = (value ? a.cv : a.ck) + b * a.cs + kvh * a.hs;
+    const int e_old = first < span.x ? *scale : 0;
+    const long long tok0 = (long long)b * a.h.tokens + (lo - span.x);
+    const long long stride = value ? a.h.v_stride : a.h.k_stride;
+    const E* src = static_cast<const E*>(value ? a.h.v : a.h.k) + tok0 * stride + kvh * a.h.D;
+    uint4 raw[PASSES][2];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int r = p * groups + grp;
+        ln.load(src + r * stride, lo + r < hi, raw[p]);
+    }
+    float x[PASSES][2 * V];
+    float top = 0.f;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        if (lo + p * groups >= hi) break;   // (the same for the block)
+        const int r = p * groups + grp;
+        const bool in = lo + r < hi;
+        if (value) {
+            float z[2][V];
+            Chunk<E>::unpack(raw[p][0], z[0]);
+            Chunk<E>::unpack(raw[p][1], z[1]);
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) x[p][i] = z[i / V][i % V];
+        } else {
+            const int position = MODE != RM_NONE && in ? a.h.position[tok0 + r] : 0;
+            auto rot = [&](int pr) { return phase(position, a.h.turns[pr], a.h.m); };
+            code_head<E, MODE>(ln, a.h, src + r * stride, in, raw[p], a.h.norm, a.h.k_weight, rot, x[p]);
+        }
+        if (in) {
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) {
+                const float y = fabsf(x[p][i]);
+                if (ln.live[i / V] && y < INFINITY) top = fmaxf(top, y);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if ((t & 31) == 0) most[t >> 5] = top;
+    __syncthreads();   // (and every thread has the old scale)
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) top = fmaxf(top, most[w]);
+    const int e = max(kv8_exponent(top), e_old);
+    const float inv = kv8_pow2(254 - e);
+    if (t == 0) *scale = (uint8_t)e;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int r = lo + p * groups + grp;
+        if (r >= hi) break;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            if (!ln.live[c]) continue;
+            uint32_t w[V / 4];
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) {
+                const float* y = &x[p][c * V + 4 * i];
+                w[i] = kv8_codes(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+            }
+            uint8_t* dst = codes + r * a.rs + ln.c[c] * V;
+            if constexpr (V == 8)
+                *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+            else
+                *reinterpret_cast<uint32_t*>(dst) = w[0];
+        }
+    }
+    if (first < span.x && e > e_old) {   // (a scale of 255 is above every other)
+        const float f = kv8_pow2(127 + e_old - e);
+        const int per = a.h.D / 16, n = (span.x - first) * per;
+        for (int i = t; i < n; i += blockDim.x) {
+            uint4* at = reinterpret_cast<uint4*>(codes + (first + i / per) * a.rs + i % per * 16);
+            uint4 u = *at;
+            uint32_t* w = &u.x;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float z[4];
+                kv8_values(w[k], z);
+                w[k] = kv8_codes(z[0] * f, z[1] * f, z[2] * f, z[3] * f);
+            }
+            *at = u;
+        }
+    }
+}
+
+template <typename E, int MODE>
+__global__ void __launch_bounds__(CT_THREADS) k_kv8_append(const __grid_constant__ Append8Args a) {
+    __shared__ CodeSmem sm;
+    if (blockIdx.x < a.units) {
+        store8<E, MODE>(a, blockIdx.x);
+        return;
+    }
+    auto place = [&](int tok) {
+        uint32_t t;
+        const int2 span = new_rows(a, (int)a.h.by_tokens.div((uint32_t)tok, t));
+        return (int)t < span.y - span.x ? 0 : -1;
+    };
+    auto at = [](long long, int) { return 0ll; };
+    code_tokens<E, MODE>(a.h, a.ct, sm, blockIdx.x - a.units, static_cast<E*>(nullptr), static_cast<E*>(nullptr), 0, place, at);
+}
+
+template <typename E>
+jpi_status launch(const Append8Args& a, int mode, unsigned blocks, int threads, cudaStream_t st) {
+    return kv_start(mode == RM_NONE ? k_kv8_append<E, RM_NONE>
+                                    : mode == RM_HALF ? k_kv8_append<E, RM_HALF>
+                                                      : mode == RM_INTER ? k_kv8_append<E, RM_INTER> : k_kv8_append<E, RM_SCALAR>,
+                    dim3(blocks), threads, 0, false, st, a);
+}
+
+}  // namespace
+
+jpi_status launch_kv8_append(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
+                             const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position, const int* start,
+                             const int* count, int batch, int tokens, void* q_out, const jpi_kv8_cache* cache, cudaStream_t st) {
+    Append8Args a = {};
+    a.h.q = q;
+    a.h.k = k;
+    a.h.v = v;
+    a.h.q_stride = q_stride;
+    a.h.k_stride = k_stride;
+    a.h.v_stride = v_stride;
+    a.h.position = position;
+    a.h.q_out = q_out;
+    a.h.H = q ? h->H : 0;
+    a.h.batch = batch;
+    a.h.tokens = tokens;
+    a.h.norm = norm != nullptr;
+    if (norm) {
+        a.h.q_weight = norm->q_weight;
+        a.h.k_weight = norm->k_weight;
+        a.h.eps = norm->eps;
+    }
+    int threads;
+    const int mode = plan_code_tokens(h, a.h, a.ct, 0, &threads);
+    a.K = h->K;
+    a.start = start;
+    a.count = count;
+    a.rows = cache->rows;
+    a.n_log2 = cache->block == 16 ? 4 : cache->block == 32 ? 5 : 6;
+    a.nblk = (cache->rows + cache->block - 1) / cache->block;
+    a.touch = 1;
+    long long units = 0;
+    if (k) {
+        a.ck = static_cast<uint8_t*>(cache->k);
+        a.cv = static_cast<uint8_t*>(cache->v);
+        a.ks = cache->k_scale;
+        a.vs = cache->v_scale;
+        a.cs = cache->cache_stride;
+        a.rs = cache->row_stride;
+        a.hs = cache->head_stride;
+        a.touch = (int)std::min<long long>(a.nblk, ((long long)tokens + 2 * cache->block - 2) / cache->block);
+        units = 2ll * batch * h->K * a.touch;
+        // Groups of lanes for the rows of a block, four (bf16) or eight of them each.
+        const int passes = h->bf16 ? 4 : 8, rows = std::min(tokens, cache->block);
+        const int most = std::min(CT_THREADS, ((rows << a.h.lanes_log2) + 31) / 32 * 32);
+        if (!q || threads < most) threads = std::max(64, most);
+        if ((threads >> a.h.lanes_log2) * passes < rows) threads = CT_THREADS;
+    }
+    a.by_touch = KvDiv((uint32_t)a.touch);
+    a.by_K = KvDiv((uint32_t)h->K);
+    const long long n = (long long)batch * tokens, blocks = units + (q ? (n + a.ct.tt - 1) / a.ct.tt : 0);
+    if (blocks > 0x7fffffffll) {
+        set_error("the call needs more than 2^31 blocks");
+        return JPI_ERR_SHAPE;
+    }
+    a.units = (uint32_t)units;
+    return h->bf16 ? launch<__nv_bfloat16>(a, mode, (unsigned)blocks, threads, st) : launch<float>(a, mode, (unsigned)blocks, threads, st);
+}
+
+}  // namespace jpi

@@ -1,7 +1,9 @@
 // C-ABI entry points of the KV-cache operators (include/jpi_kv.h): argument checks, the handle and
-// its rotary table. The kernels are in kv_append.cu, kv_attend.cu, kv_weigh.cu and kv_evict.cu.
+// its rotary table. The kernels are in kv_append.cu, kv_append_normed.cu, kv8_append.cu, kv_attend.cu, kv_span.cu, kv_weigh.cu and
+// kv_evict.cu.
 
 #include "kv.h"
+#include "kv_span.h"
 #include "kv_weigh.h"
 
 #include <cstdlib>
@@ -134,6 +136,58 @@ KvSide side_of(const jpi_kv_cache* c, const int* len) {
     return s;
 }
 
+// The new tokens of the appends.
+jpi_status check_tokens(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
+                        const void* v, long long v_stride, const void* q_out, bool cache) {
+    if (!q && !k) return fail(JPI_ERR_INVALID_ARG, "q and k are both NULL");
+    if ((q != nullptr) != (q_out != nullptr)) return fail(JPI_ERR_INVALID_ARG, "q goes with q_out");
+    if ((k != nullptr) != cache) return fail(JPI_ERR_INVALID_ARG, "k goes with cache");
+    if (v && !k) return fail(JPI_ERR_INVALID_ARG, "v without k");
+    if (q) {
+        JPI_TRY(check_stride(h, "q", q, q_stride, h->H));
+        if (!aligned(q_out)) return fail(JPI_ERR_INVALID_ARG, "q_out is not 16-byte aligned");
+    }
+    if (k) JPI_TRY(check_stride(h, "k", k, k_stride, h->K));
+    if (v) JPI_TRY(check_stride(h, "v", v, v_stride, h->K));
+    return JPI_OK;
+}
+
+jpi_status check_norm(const jpi_kv_norm* n) {
+    if (!(n->eps >= 0x1p-126f) || std::isinf(n->eps)) return fail(JPI_ERR_INVALID_ARG, "the norm's eps must be 2^-126 or more and finite");
+    if (((uintptr_t)n->q_weight | (uintptr_t)n->k_weight) & 3) return fail(JPI_ERR_INVALID_ARG, "a norm's weight is not 4-byte aligned");
+    return JPI_OK;
+}
+
+jpi_status check_cache8(const jpi_kv_handle* h, const jpi_kv8_cache* c, int n) {
+    if (h->D % 16) return fail(JPI_ERR_UNSUPPORTED, "head_dim %d must be a multiple of 16 for a cache in 8 bits", h->D);
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(JPI_ERR_INVALID_ARG, "cache: k, v or a scale is NULL");
+    if (!aligned(c->k) || !aligned(c->v)) return fail(JPI_ERR_INVALID_ARG, "cache: k or v is not 16-byte aligned");
+    if (c->rows < 1 || c->rows > (1 << 30)) return fail(JPI_ERR_INVALID_ARG, "cache: rows %d must be in 1..2^30", c->rows);
+    if (c->block != 16 && c->block != 32 && c->block != 64)
+        return fail(JPI_ERR_INVALID_ARG, "cache: block %d must be 16, 32 or 64 rows", c->block);
+    const struct { const char* name; long long stride, size; } s[3] = {{"cache_stride", c->cache_stride, n},
+        {"row_stride", c->row_stride, c->rows}, {"head_stride", c->head_stride, h->K}};
+    for (const auto& d : s)
+        if (d.size > 1 && (d.stride < h->D || d.stride > (1ll << 60) / d.size || d.stride % 16))
+            return fail(JPI_ERR_INVALID_ARG, "cache: %s %lld must be at least head_dim and a multiple of 16 bytes", d.name, d.stride);
+    return JPI_OK;
+}
+
+void fill_call(const jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens, int groups, KvCall* c) {
+    c->q = q;
+    c->q_stride = q_stride;
+    c->batch = batch;
+    c->tokens = tokens;
+    c->groups = groups;
+    c->H = h->H;
+    c->K = h->K;
+    c->D = h->D;
+    c->gq = h->gq;
+    c->scale = h->scale;
+    c->by_gq = KvDiv((uint32_t)h->gq);
+    c->by_K = KvDiv((uint32_t)h->K);
+}
+
 // The arguments that attend and weigh share.
 jpi_status make_call(const jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
                      const jpi_kv_cache* prefix, int groups, const int* prefix_len, const jpi_kv_cache* own,
@@ -149,18 +203,7 @@ jpi_status make_call(const jpi_kv_handle* h, const void* q, long long q_stride, 
     JPI_TRY(check_stride(h, "q", q, q_stride, h->H));
     if (prefix) JPI_TRY(check_cache(h, "prefix", prefix, groups, 1, need_v));
     if (own) JPI_TRY(check_cache(h, "own", own, batch, 1, need_v));
-    c->q = q;
-    c->q_stride = q_stride;
-    c->batch = batch;
-    c->tokens = tokens;
-    c->groups = groups;
-    c->H = h->H;
-    c->K = h->K;
-    c->D = h->D;
-    c->gq = h->gq;
-    c->scale = h->scale;
-    c->by_gq = KvDiv((uint32_t)h->gq);
-    c->by_K = KvDiv((uint32_t)h->K);
+    fill_call(h, q, q_stride, batch, tokens, groups, c);
     c->prefix = side_of(prefix, prefix_len);
     c->own = side_of(own, seen);
     return JPI_OK;
@@ -221,6 +264,7 @@ JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* ro
         JPI_TRY(kv_alloc(h, &h->ws, h->ws_bytes));
         JPI_TRY(kv_append_prepare());
         JPI_TRY(kv_weigh_prepare(h));
+        JPI_TRY(kv_span_prepare(h));
         return kv_attend_prepare(h);
     };
     jpi_status s;
@@ -249,20 +293,9 @@ JPI_API jpi_status jpi_kv_append(jpi_kv_handle* h, const void* q, long long q_st
     clear_error();
     JPI_TRY(check_handle(h));
     JPI_TRY(check_count(h, batch, tokens));
-    if (!q && !k) return fail(JPI_ERR_INVALID_ARG, "q and k are both NULL");
-    if ((q != nullptr) != (q_out != nullptr)) return fail(JPI_ERR_INVALID_ARG, "q goes with q_out");
-    if ((k != nullptr) != (cache != nullptr)) return fail(JPI_ERR_INVALID_ARG, "k goes with cache");
-    if (v && !k) return fail(JPI_ERR_INVALID_ARG, "v without k");
+    JPI_TRY(check_tokens(h, q, q_stride, k, k_stride, v, v_stride, q_out, cache != nullptr));
     if (!position || !row) return fail(JPI_ERR_INVALID_ARG, "position or row is NULL");
-    if (q) {
-        JPI_TRY(check_stride(h, "q", q, q_stride, h->H));
-        if (!aligned(q_out)) return fail(JPI_ERR_INVALID_ARG, "q_out is not 16-byte aligned");
-    }
-    if (k) {
-        JPI_TRY(check_stride(h, "k", k, k_stride, h->K));
-        if (v) JPI_TRY(check_stride(h, "v", v, v_stride, h->K));
-        JPI_TRY(check_cache(h, "cache", cache, batch, 1, v != nullptr));
-    }
+    if (k) JPI_TRY(check_cache(h, "cache", cache, batch, 1, v != nullptr));
     return launch_kv_append(h, q, q_stride, k, k_stride, v, v_stride, position, row, batch, tokens, q_out, cache,
                             (cudaStream_t)stream);
 }
@@ -275,6 +308,86 @@ JPI_API jpi_status jpi_kv_attend(jpi_kv_handle* h, const void* q, long long q_st
     JPI_TRY(make_call(h, q, q_stride, batch, tokens, prefix, groups, prefix_len, own, seen, true, &c));
     if (!out || !aligned(out)) return fail(JPI_ERR_INVALID_ARG, "out is NULL or not 16-byte aligned");
     return launch_kv_attend(h, c, out, lse, (cudaStream_t)stream);
+}
+
+JPI_API jpi_status jpi_kv_append_normed(jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
+                                        const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position,
+                                        const int* row, int batch, int tokens, void* q_out, const jpi_kv_cache* cache,
+                                        void* stream) {
+    clear_error();
+    JPI_TRY(check_handle(h));
+    JPI_TRY(check_count(h, batch, tokens));
+    if (!norm) return fail(JPI_ERR_INVALID_ARG, "norm is NULL");
+    JPI_TRY(check_tokens(h, q, q_stride, k, k_stride, v, v_stride, q_out, cache != nullptr));
+    JPI_TRY(check_norm(norm));
+    if (!position || !row) return fail(JPI_ERR_INVALID_ARG, "position or row is NULL");
+    if (k) JPI_TRY(check_cache(h, "cache", cache, batch, 1, v != nullptr));
+    return launch_kv_append_normed(h, q, q_stride, k, k_stride, v, v_stride, norm, position, row, batch, tokens, q_out, cache,
+                                   (cudaStream_t)stream);
+}
+
+JPI_API jpi_status jpi_kv_attend_window(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
+                                        const jpi_kv_cache* cache, const int* seen, int window, int sink, void* out, float* lse,
+                                        void* stream) {
+    clear_error();
+    KvCall c;
+    if (!cache || !seen) return fail(JPI_ERR_INVALID_ARG, "cache or seen is NULL");
+    JPI_TRY(make_call(h, q, q_stride, batch, tokens, nullptr, 1, nullptr, cache, seen, true, &c));
+    if (!out || !aligned(out)) return fail(JPI_ERR_INVALID_ARG, "out is NULL or not 16-byte aligned");
+    if (window < 1 || sink < 0) return fail(JPI_ERR_INVALID_ARG, "window %d must be >= 1 and sink %d >= 0", window, sink);
+    KvSpan s;
+    s.window = window;
+    s.sink = sink;
+    return launch_kv_span(h, c, s, out, lse, (cudaStream_t)stream);
+}
+
+JPI_API jpi_status jpi_kv8_append(jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
+                                  const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position,
+                                  const int* start, const int* count, int batch, int tokens, void* q_out,
+                                  const jpi_kv8_cache* cache, void* stream) {
+    clear_error();
+    JPI_TRY(check_handle(h));
+    JPI_TRY(check_count(h, batch, tokens));
+    if (!cache) return fail(JPI_ERR_INVALID_ARG, "cache is NULL");
+    JPI_TRY(check_tokens(h, q, q_stride, k, k_stride, v, v_stride, q_out, k != nullptr));
+    if ((k != nullptr) != (v != nullptr)) return fail(JPI_ERR_INVALID_ARG, "k goes with v");
+    if (norm) JPI_TRY(check_norm(norm));
+    if (!position || !start) return fail(JPI_ERR_INVALID_ARG, "position or start is NULL");
+    JPI_TRY(check_cache8(h, cache, batch));
+    return launch_kv8_append(h, q, q_stride, k, k_stride, v, v_stride, norm, position, start, count, batch, tokens, q_out, cache,
+                             (cudaStream_t)stream);
+}
+
+JPI_API jpi_status jpi_kv8_attend(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
+                                  const jpi_kv8_cache* cache, const int* seen, int window, int sink, void* out, float* lse,
+                                  void* stream) {
+    clear_error();
+    JPI_TRY(check_handle(h));
+    JPI_TRY(check_count(h, batch, tokens));
+    if (!q || !cache || !seen) return fail(JPI_ERR_INVALID_ARG, "q, cache or seen is NULL");
+    JPI_TRY(check_stride(h, "q", q, q_stride, h->H));
+    JPI_TRY(check_cache8(h, cache, batch));
+    if (!out || !aligned(out)) return fail(JPI_ERR_INVALID_ARG, "out is NULL or not 16-byte aligned");
+    if (window < 0 || sink < 0) return fail(JPI_ERR_INVALID_ARG, "window %d and sink %d must be >= 0", window, sink);
+    KvCall c;
+    fill_call(h, q, q_stride, batch, tokens, 1, &c);
+    c.own.k = cache->k;
+    c.own.v = cache->v;
+    c.own.cs = cache->cache_stride;
+    c.own.rs = cache->row_stride;
+    c.own.hs = cache->head_stride;
+    c.own.rows = cache->rows;
+    c.own.len = seen;
+    KvSpan s;
+    if (window > 0) {
+        s.window = window;
+        s.sink = sink;
+    }
+    s.ks = cache->k_scale;
+    s.vs = cache->v_scale;
+    s.n_log2 = cache->block == 16 ? 4 : cache->block == 32 ? 5 : 6;
+    s.nblk = (cache->rows + cache->block - 1) / cache->block;
+    return launch_kv_span(h, c, s, out, lse, (cudaStream_t)stream);
 }
 
 JPI_API jpi_status jpi_kv_weigh(jpi_kv_handle* h, const void* q, long long q_stride, const float* lse, int batch,

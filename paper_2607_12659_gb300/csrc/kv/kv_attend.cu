@@ -19,90 +19,13 @@
 // bound by memory, so the two share the SMs: the row kernel starts first with two blocks per SM, the tiles start while it
 // runs. k_kv_combine joins the parts, except where a row has only one.
 
-#include "kv_rows.cuh"
+#include "kv_parts.cuh"
 #include "kv_attend.h"
 
 #include <algorithm>
 
 namespace jpi {
 namespace {
-
-constexpr int AT_WARPS = 4;
-constexpr int AT_THREADS = 32 * AT_WARPS;
-
-// How one side is dealt to blocks: `wr` warps of a block take different row tiles, and each of those `wk` warps
-// different keys.
-struct SidePlan {
-    int wr = 1, wk = 1;
-    int tiles = 0;        // blocks of wr row tiles per cache and KV head
-    int splits = 0;       // key ranges
-    long long blocks = 0;
-    KvDiv by_splits, by_tiles;
-};
-
-struct AttendArgs {
-    KvCall c;
-    SidePlan p, o;
-    float* po;            // [parts][rows][D] unnormalised outputs
-    float2* pml;          // [rows][parts] (m, l), m unscaled
-    int parts;
-    float c2;             // log2(e) * scale
-    long long rows;       // batch * tokens * H
-    void* out;            // rows of one part: the result itself, else null
-    float* lse;
-};
-
-// The block's piece of work: side, cache, KV head, row tile and key split.
-struct Piece {
-    bool prefix;
-    int cache, kvh, part;
-    uint32_t split;
-    RowTile t;
-};
-__device__ __forceinline__ Piece piece_of(const AttendArgs& a, long long piece, int warp) {
-    Piece x;
-    uint32_t i = (uint32_t)piece, tile, kvh;
-    x.prefix = i < a.p.blocks;
-    if (!x.prefix) i -= (uint32_t)a.p.blocks;
-    const SidePlan& s = x.prefix ? a.p : a.o;
-    i = s.by_splits.div(i, x.split);
-    i = s.by_tiles.div(i, tile);
-    x.cache = (int)a.c.by_K.div(i, kvh);
-    x.part = (x.prefix ? 0 : a.p.splits) + (int)x.split;
-    const int toks = x.prefix ? a.c.batch / a.c.groups * a.c.tokens : a.c.tokens;
-    x.t.tok0 = (long long)x.cache * toks;
-    x.kvh = (int)kvh;
-    x.t.head0 = (int)kvh * a.c.gq;
-    x.t.R = toks * a.c.gq;
-    x.t.r0 = ((int)tile * s.wr + warp / s.wk) * KR_ROWS;
-    return x;
-}
-
-// Shared memory of one warp's share of the merge: 8 rows of DP outputs, then (m, l) per row. BYTES: of a block of
-// AT_WARPS warps, which holds the query fragments in it before.
-template <int DP>
-struct MergeSmem {
-    static constexpr int LD = DP + 4;   // the row pad spreads the rows over the banks
-    static constexpr int WARP_FLOATS = KR_ROWS * LD + 2 * KR_ROWS;
-    static constexpr int BYTES = AT_WARPS * WARP_FLOATS * 4;
-};
-
-// One row's elements as a warp holds them: lane's float4 i is d = 4 lane + 128 i.
-template <int DP>
-struct RowAcc {
-    static constexpr int NI = (DP + 127) / 128;
-    float4 o[NI];
-    float m, l;
-    __device__ __forceinline__ void add(float w, const float4 (&v)[NI]) {
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            o[i].x = fmaf(w, v[i].x, o[i].x);
-            o[i].y = fmaf(w, v[i].y, o[i].y);
-            o[i].z = fmaf(w, v[i].z, o[i].z);
-            o[i].w = fmaf(w, v[i].w, o[i].w);
-        }
-    }
-};
 
 // Joins elements d0 .. d0 + DP - 1 of parts first, first + step, .. of a row (of `parts`) to `r`, which holds nothing yet,
 // relative to their largest maximum. The loads of JOIN parts are in flight together: they are made whether the part holds
@@ -150,78 +73,6 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, RowAcc<DP>& r, l
                 for (int i = 0; i < NI; ++i)
                     if (k0 + k >= n || !(written >> (k0 + k) & 1)) v[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
                 r.add(wk[k], v[k]);
-            }
-        }
-    }
-}
-
-// What a row's outputs are multiplied by: 0 without a key, NaN with a NaN score.
-__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
-__device__ __forceinline__ float log_sum(float m, float l, float scale) { return l == 0.f ? -INFINITY : fmaf(m, scale, logf(l)); }
-
-// The row's result from its joined sums, elements from d0 on.
-template <int DP, typename E>
-__device__ __forceinline__ void write_row(const AttendArgs& a, const RowAcc<DP>& r, long long row, int d0, int lane) {
-    const float inv = inverse_sum(r.l);
-    E* out = static_cast<E*>(a.out) + row * a.c.D;
-#pragma unroll
-    for (int i = 0; i < RowAcc<DP>::NI; ++i) {
-        const int d = d0 + 4 * lane + 128 * i;
-        if (d >= a.c.D) continue;
-        const float4 v = make_float4(r.o[i].x * inv, r.o[i].y * inv, r.o[i].z * inv, r.o[i].w * inv);
-        if constexpr (sizeof(E) == 2)
-            *(uint2*)(out + d) = make_uint2(kr_pack(v.x, v.y), kr_pack(v.z, v.w));
-        else
-            *(float4*)(out + d) = v;
-    }
-    if (d0 == 0 && lane == 0 && a.lse) a.lse[row] = log_sum(r.m, r.l, a.c.scale);
-}
-
-// Joins the key warps of each row tile (their outputs and (m, l) are in shared memory) and writes the part, or, where
-// the block's keys are the last of its rows, the result.
-template <int DP>
-__device__ __forceinline__ void merge_and_write(const AttendArgs& a, const Piece& x, const SidePlan& s, const float* sm, int warp,
-                                                int lane) {
-    using M = MergeSmem<DP>;
-    constexpr int NI = RowAcc<DP>::NI;
-    __syncthreads();
-    // Every warp takes rows (its index among the key warps) + n wk of its row tile.
-    const float* tile = sm + (warp / s.wk) * s.wk * M::WARP_FLOATS;
-    for (int rr = warp % s.wk; rr < KR_ROWS; rr += s.wk) {
-        const int r = x.t.r0 + rr;
-        if (r >= x.t.R) continue;
-        const long long row = row_index(a.c, x.t, r);
-        RowAcc<DP> acc;
-        acc.m = -INFINITY;
-        acc.l = 0.f;
-        for (int k = 0; k < s.wk; ++k) acc.m = fmaxf(acc.m, tile[k * M::WARP_FLOATS + KR_ROWS * M::LD + 2 * rr]);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) acc.o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < s.wk; ++k) {
-            const float* f = tile + k * M::WARP_FLOATS;
-            const float mk = f[KR_ROWS * M::LD + 2 * rr], lk = f[KR_ROWS * M::LD + 2 * rr + 1];
-            if (lk == 0.f) continue;
-            const float w = mk == -INFINITY ? 0.f : kr_ex2((mk - acc.m) * a.c2);
-            acc.l += w * lk;
-            float4 v[NI];
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int d = 4 * lane + 128 * i;
-                v[i] = d < DP ? *(const float4*)(f + rr * M::LD + d) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-            acc.add(w, v);
-        }
-        if (a.out) {
-            write_row<DP, float>(a, acc, row, 0, lane);
-            continue;
-        }
-        const long long at = x.part * a.rows + row;
-        if (lane == 0) a.pml[row * a.parts + x.part] = make_float2(acc.m, acc.l);
-        if (acc.l != 0.f) {
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int d = 4 * lane + 128 * i;
-                if (d < a.c.D) *(float4*)(a.po + at * a.c.D + d) = acc.o[i];
             }
         }
     }
@@ -754,7 +605,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_attend_f32
             f[KR_ROWS * MergeSmem<DP>::LD + 2 * r + 1] = l[r];
         }
     }
-    merge_and_write<DP>(a, x, sp, kv_smem, warp, lane);
+    merge_and_write<DP, float>(a, x, sp, kv_smem, warp, lane);
 }
 
 // Joins the parts of all rows, DP elements of one (from DP blockIdx.y on) by `wpr` warps (a power of two), each with every
@@ -800,12 +651,6 @@ __global__ void __launch_bounds__(32 * CB_WARPS) k_kv_combine(const __grid_const
         }
     }
     if (row < a.rows) write_row<DP, E>(a, acc, row, d0, lane);
-}
-
-// Rows of partial outputs the workspace holds.
-long long ws_rows(const jpi_kv_handle* h) {
-    const long long rows = (long long)h->cfg.max_batch * h->cfg.max_tokens * h->H;
-    return 2 * rows + 512ll * h->num_sms;
 }
 
 // A side's pieces for blocks of `warps` warps, whose warps take `step` keys at a time. Key splits: up to `want` pieces
@@ -880,17 +725,7 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, 
     }
     const int part0[2] = {0, a.p.splits};
     if (beside) JPI_TRY(launch_kv_tiles_t5(h, c, tiles, part0, a.po, a.pml, parts, out, lse, pieces > 0 && h->pdl, st));
-    if (parts == 1) return JPI_OK;
-    a.out = out;
-    // Warps for 8 to 16 parts each, to sixteen, as long as all are resident together (16 an SM).
-    const int slices = c.D > 128 && a.rows * 2 <= 16ll * h->num_sms ? 2 : 1;
-    int wpr = 1;
-    while (wpr < CB_WARPS && wpr * 8 < parts && a.rows * slices * wpr * 2 <= 16ll * h->num_sms) wpr *= 2;
-    const int warps = std::max(wpr, AT_WARPS);
-    const dim3 grid((unsigned)((a.rows * wpr + warps - 1) / warps), (unsigned)slices);
-    const bool wide = DP == 256 && slices == 1;
-    return kv_start(h->bf16 ? (wide ? k_kv_combine<256, __nv_bfloat16> : k_kv_combine<128, __nv_bfloat16>)
-                            : (wide ? k_kv_combine<256, float> : k_kv_combine<128, float>), grid, 32 * warps, 0, h->pdl, st, a, wpr);
+    return parts == 1 ? JPI_OK : launch_kv_combine(h, c, parts, out, lse, st);
 }
 
 template <int DP>
@@ -912,6 +747,27 @@ size_t kv_attend_ws_bytes(const jpi_kv_handle* h) {
 jpi_status kv_attend_prepare(jpi_kv_handle* h) {
     JPI_TRY(kv_tiles_prepare(h));
     return h->D <= 64 ? prepare_dim<64>() : h->D <= 128 ? prepare_dim<128>() : prepare_dim<256>();
+}
+
+jpi_status launch_kv_combine(const jpi_kv_handle* h, const KvCall& c, int parts, void* out, float* lse, cudaStream_t st) {
+    AttendArgs a = {};
+    a.c = c;
+    a.c2 = KR_LOG2E * c.scale;
+    a.rows = (long long)c.batch * c.tokens * c.H;
+    a.po = static_cast<float*>(h->ws);
+    a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
+    a.parts = parts;
+    a.out = out;
+    a.lse = lse;
+    // Warps for 8 to 16 parts each, to sixteen, as long as all are resident together (16 an SM).
+    const int slices = c.D > 128 && a.rows * 2 <= 16ll * h->num_sms ? 2 : 1;
+    int wpr = 1;
+    while (wpr < CB_WARPS && wpr * 8 < parts && a.rows * slices * wpr * 2 <= 16ll * h->num_sms) wpr *= 2;
+    const int warps = std::max(wpr, AT_WARPS);
+    const dim3 grid((unsigned)((a.rows * wpr + warps - 1) / warps), (unsigned)slices);
+    const bool wide = c.D > 128 && slices == 1;
+    return kv_start(h->bf16 ? (wide ? k_kv_combine<256, __nv_bfloat16> : k_kv_combine<128, __nv_bfloat16>)
+                            : (wide ? k_kv_combine<256, float> : k_kv_combine<128, float>), grid, 32 * warps, 0, h->pdl, st, a, wpr);
 }
 
 jpi_status launch_kv_attend(jpi_kv_handle* h, const KvCall& c, void* out, float* lse, cudaStream_t st) {

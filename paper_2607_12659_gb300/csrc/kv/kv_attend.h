@@ -21,4 +21,7 @@ void kv_tiles_plan(const jpi_kv_handle* h, const KvCall& c, long long room, KvTi
 jpi_status launch_kv_tiles_t5(jpi_kv_handle* h, const KvCall& c, const KvTilesPlan& plan, const int part0[2], float* po,
                               float2* pml, int parts, void* out, float* lse, bool early, cudaStream_t st);
 
+// Joins the parts 0 .. parts - 1 that a call's kernels left in the handle's workspace.
+jpi_status launch_kv_combine(const jpi_kv_handle* h, const KvCall& c, int parts, void* out, float* lse, cudaStream_t st);
+
 }  // namespace jpi

@@ -26,6 +26,10 @@ struct Calls {
     decltype(&jpi_kv_attend) attend;
     decltype(&jpi_kv_weigh) weigh;
     decltype(&jpi_kv_evict) evict;
+    decltype(&jpi_kv_append_normed) append_normed;
+    decltype(&jpi_kv_attend_window) attend_window;
+    decltype(&jpi_kv8_append) append8;
+    decltype(&jpi_kv8_attend) attend8;
 };
 
 // A refused argument: a Python ValueError or TypeError.
@@ -195,35 +199,149 @@ PyObject* entry(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F&& body) {
     return nullptr;
 }
 
+// The new tokens of an append: q, k and v (each may be None) and their common batch and tokens.
+struct News {
+    Tokens t[3];
+    int64_t B = -1, T = -1;
+};
+News news(const Calls& c, PyObject* const* a) {
+    News r;
+    if (a[0] == Py_None && a[1] == Py_None) throw Refused("neither q nor k is given");
+    const char* const names[3] = {"q", "k", "v"};
+    for (int i = 0; i < 3; ++i) {
+        if (a[i] == Py_None) continue;
+        r.t[i] = tokens(c, names[i], a[i], i == 0 ? c.H : c.K);
+        if (r.B < 0) r.B = r.t[i].B, r.T = r.t[i].T;
+        if (r.t[i].B != r.B || r.t[i].T != r.T)
+            throw Refused(std::string(names[i]) + " holds " + std::to_string(r.t[i].B) + " x " + std::to_string(r.t[i].T) + " tokens, not " +
+                          std::to_string(r.B) + " x " + std::to_string(r.T));
+    }
+    return r;
+}
+
+// A norm: (q_weight, k_weight, eps), weights None or fp32 [D].
+jpi_kv_norm norm_of(const Calls& c, PyObject* q_weight, PyObject* k_weight, PyObject* eps) {
+    jpi_kv_norm r = {};
+    if (q_weight != Py_None) r.q_weight = whole<float>(c, "the norm's q_weight", q_weight, {c.D}, at::kFloat);
+    if (k_weight != Py_None) r.k_weight = whole<float>(c, "the norm's k_weight", k_weight, {c.D}, at::kFloat);
+    const double e = PyFloat_AsDouble(eps);
+    if (e == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Mistyped("the norm's eps must be a number");
+    }
+    r.eps = (float)e;
+    return r;
+}
+
+// Of an append into caches of the handle's type: a[0 ..] = q, k, v, positions, rows, cache_k, cache_v, q_out.
+template <typename F>
+PyObject* append_to(const Calls& c, PyObject* const* a, F&& call) {
+    const News n = news(c, a);
+    const int64_t lead[2] = {n.B, n.T}, heads[4] = {n.B, n.T, c.H, c.D};
+    const int* pos = whole<int>(c, "positions", a[3], lead, at::kInt);
+    const int* row = whole<int>(c, "rows", a[4], lead, at::kInt);
+    void* out = a[0] == Py_None ? nullptr : whole<void>(c, "q_out", a[7], heads, c.dtype);
+    jpi_kv_cache ca = {};
+    const bool k = a[1] != Py_None, v = a[2] != Py_None;
+    if (k) {
+        if (a[5] == Py_None || (v && a[6] == Py_None)) throw Refused("k and v need the caches they go to");
+        ca = cache(c, "the cache", a[5], v ? a[6] : nullptr, n.B);
+    }
+    return status_of([&] { return call(n, pos, row, out, k ? &ca : nullptr); });
+}
+
 // (calls, handle, stream, q, k, v, positions, rows, cache_k, cache_v, q_out)
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return entry(a, n, 11, [&](const Calls& c, jpi_kv_handle* h, void* st) {
-        if (a[3] == Py_None && a[4] == Py_None) throw Refused("neither q nor k is given");
-        Tokens t[3];
-        const char* const names[3] = {"q", "k", "v"};
-        int64_t B = -1, T = -1;
-        for (int i = 0; i < 3; ++i) {
-            if (a[3 + i] == Py_None) continue;
-            t[i] = tokens(c, names[i], a[3 + i], i == 0 ? c.H : c.K);
-            if (B < 0) B = t[i].B, T = t[i].T;
-            if (t[i].B != B || t[i].T != T)
-                throw Refused(std::string(names[i]) + " holds " + std::to_string(t[i].B) + " x " + std::to_string(t[i].T) + " tokens, not " +
-                              std::to_string(B) + " x " + std::to_string(T));
-        }
-        const int64_t lead[2] = {B, T}, heads[4] = {B, T, c.H, c.D};
-        const int* pos = whole<int>(c, "positions", a[6], lead, at::kInt);
-        const int* row = whole<int>(c, "rows", a[7], lead, at::kInt);
-        void* out = a[3] == Py_None ? nullptr : whole<void>(c, "q_out", a[10], heads, c.dtype);
-        jpi_kv_cache ca = {};
-        const bool k = a[4] != Py_None, v = a[5] != Py_None;
-        if (k) {
-            if (a[8] == Py_None || (v && a[9] == Py_None)) throw Refused("k and v need the caches they go to");
-            ca = cache(c, "the cache", a[8], v ? a[9] : nullptr, B);
-        }
-        return status_of([&] {
-            return c.append(h, t[0].at, t[0].stride, t[1].at, t[1].stride, t[2].at, t[2].stride, pos, row, (int)B, (int)T, out,
-                            k ? &ca : nullptr, st);
+        return append_to(c, a + 3, [&](const News& x, const int* pos, const int* row, void* out, const jpi_kv_cache* ca) {
+            return c.append(h, x.t[0].at, x.t[0].stride, x.t[1].at, x.t[1].stride, x.t[2].at, x.t[2].stride, pos, row, (int)x.B, (int)x.T,
+                            out, ca, st);
         });
+    });
+}
+
+// (calls, handle, stream, q, k, v, positions, rows, cache_k, cache_v, q_out, q_weight, k_weight, eps)
+PyObject* append_normed(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(a, n, 14, [&](const Calls& c, jpi_kv_handle* h, void* st) {
+        const jpi_kv_norm nm = norm_of(c, a[11], a[12], a[13]);
+        return append_to(c, a + 3, [&](const News& x, const int* pos, const int* row, void* out, const jpi_kv_cache* ca) {
+            return c.append_normed(h, x.t[0].at, x.t[0].stride, x.t[1].at, x.t[1].stride, x.t[2].at, x.t[2].stride, &nm, pos, row,
+                                   (int)x.B, (int)x.T, out, ca, st);
+        });
+    });
+}
+
+// An 8-bit cache of n requests: codes [n][rows][KV heads][D] of k and v, e8m0 scales [n][KV heads][ceil(rows / block)].
+jpi_kv8_cache cache8(const Calls& c, PyObject* ok, PyObject* ov, PyObject* ks, PyObject* vs, PyObject* block, int64_t n) {
+    const at::Tensor &k = tensor(ok, "the cache's k"), &v = tensor(ov, "the cache's v");
+    check_data(c, "the cache's k", k, at::kFloat8_e4m3fn);
+    check_data(c, "the cache's v", v, at::kFloat8_e4m3fn);
+    const at::IntArrayRef s = k.strides(), z = k.sizes();
+    if (v.sizes() != z || v.strides() != s) throw Refused("the cache: k and v must be caches of one shape, type and strides");
+    if (z.size() != 4 || z[0] != n || z[2] != c.K || z[3] != c.D)
+        throw Refused("the cache has shape " + str(z) + ", not [" + std::to_string(n) + "][rows][" + std::to_string(c.K) + "][" +
+                      std::to_string(c.D) + "]");
+    if (s[3] != 1) throw Refused("the cache: a head's elements must be contiguous");
+    jpi_kv8_cache r = {};
+    r.block = int_of(block, "the cache's block");
+    if (r.block < 1) throw Refused("the cache's block is " + std::to_string(r.block));
+    r.k = k.data_ptr();
+    r.v = v.data_ptr();
+    r.cache_stride = s[0];
+    r.row_stride = s[1];
+    r.head_stride = s[2];
+    r.rows = to_int(z[1], "the number of rows");
+    const int64_t shape[3] = {n, c.K, (z[1] + r.block - 1) / r.block};
+    r.k_scale = whole<unsigned char>(c, "the cache's k_scale", ks, shape, at::kFloat8_e8m0fnu);
+    r.v_scale = whole<unsigned char>(c, "the cache's v_scale", vs, shape, at::kFloat8_e8m0fnu);
+    return r;
+}
+
+// (calls, handle, stream, q, k, v, positions, start, count, cache: k, v, k_scale, v_scale, block, q_out, normed, q_weight, k_weight, eps)
+PyObject* append8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(a, n, 19, [&](const Calls& c, jpi_kv_handle* h, void* st) {
+        const News x = news(c, a + 3);
+        if ((a[4] == Py_None) != (a[5] == Py_None)) throw Refused("k goes with v");
+        const int64_t lead[2] = {x.B, x.T}, heads[4] = {x.B, x.T, c.H, c.D};
+        const int* pos = whole<int>(c, "positions", a[6], lead, at::kInt);
+        const int* start = whole<int>(c, "start", a[7], {x.B}, at::kInt);
+        const int* count = a[8] == Py_None ? nullptr : whole<int>(c, "count", a[8], {x.B}, at::kInt);
+        const jpi_kv8_cache ca = cache8(c, a[9], a[10], a[11], a[12], a[13], x.B);
+        void* out = a[3] == Py_None ? nullptr : whole<void>(c, "q_out", a[14], heads, c.dtype);
+        const bool normed = a[15] != Py_None;
+        const jpi_kv_norm nm = normed ? norm_of(c, a[16], a[17], a[18]) : jpi_kv_norm{};
+        return status_of([&] {
+            return c.append8(h, x.t[0].at, x.t[0].stride, x.t[1].at, x.t[1].stride, x.t[2].at, x.t[2].stride, normed ? &nm : nullptr, pos,
+                             start, count, (int)x.B, (int)x.T, out, &ca, st);
+        });
+    });
+}
+
+// (calls, handle, stream, q, cache: (k, v), seen, window, sink, out, lse)
+PyObject* attend_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(a, n, 10, [&](const Calls& c, jpi_kv_handle* h, void* st) {
+        const Tokens q = tokens(c, "q", a[3], c.H);
+        if (a[4] == Py_None) throw Refused("the cache is None");
+        const Side s = side(c, "the cache", a[4], "seen", a[5], true, q.B, q.T);
+        const int window = int_of(a[6], "window"), sink = int_of(a[7], "sink");
+        const int64_t heads[4] = {q.B, q.T, c.H, c.D};
+        void* out = whole<void>(c, "out", a[8], heads, c.dtype);
+        float* lse = whole<float>(c, "lse", a[9], at::IntArrayRef(heads, 3), at::kFloat);
+        return status_of([&] { return c.attend_window(h, q.at, q.stride, (int)q.B, (int)q.T, s.p, s.len, window, sink, out, lse, st); });
+    });
+}
+
+// (calls, handle, stream, q, cache: k, v, k_scale, v_scale, block, seen, window, sink, out, lse)
+PyObject* attend8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return entry(a, n, 14, [&](const Calls& c, jpi_kv_handle* h, void* st) {
+        const Tokens q = tokens(c, "q", a[3], c.H);
+        const jpi_kv8_cache ca = cache8(c, a[4], a[5], a[6], a[7], a[8], q.B);
+        const int64_t lead[2] = {q.B, q.T}, heads[4] = {q.B, q.T, c.H, c.D};
+        const int* seen = whole<int>(c, "seen", a[9], lead, at::kInt);
+        const int window = int_of(a[10], "window"), sink = int_of(a[11], "sink");
+        void* out = whole<void>(c, "out", a[12], heads, c.dtype);
+        float* lse = whole<float>(c, "lse", a[13], at::IntArrayRef(heads, 3), at::kFloat);
+        return status_of([&] { return c.attend8(h, q.at, q.stride, (int)q.B, (int)q.T, &ca, seen, window, sink, out, lse, st); });
     });
 }
 
@@ -292,17 +410,23 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// The geometry that calls are checked against: (heads, KV heads, head dim, bf16, device, the four entry points)
+// The geometry that calls are checked against: (heads, KV heads, head dim, bf16, device, the entry points append, attend, weigh,
+// evict and, where they are called, append_normed, attend_window, append8, attend8)
 PyObject* calls(PyObject*, PyObject* args) {
     int bf16;
-    unsigned long long f[4];
+    unsigned long long f[8] = {};
     Calls c = {};
-    if (!PyArg_ParseTuple(args, "iiipiKKKK", &c.H, &c.K, &c.D, &bf16, &c.device, &f[0], &f[1], &f[2], &f[3])) return nullptr;
+    if (!PyArg_ParseTuple(args, "iiipiKKKK|KKKK", &c.H, &c.K, &c.D, &bf16, &c.device, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6],
+                          &f[7])) return nullptr;
     c.dtype = bf16 ? at::kBFloat16 : at::kFloat;
     c.append = reinterpret_cast<decltype(c.append)>(f[0]);
     c.attend = reinterpret_cast<decltype(c.attend)>(f[1]);
     c.weigh = reinterpret_cast<decltype(c.weigh)>(f[2]);
     c.evict = reinterpret_cast<decltype(c.evict)>(f[3]);
+    c.append_normed = reinterpret_cast<decltype(c.append_normed)>(f[4]);
+    c.attend_window = reinterpret_cast<decltype(c.attend_window)>(f[5]);
+    c.append8 = reinterpret_cast<decltype(c.append8)>(f[6]);
+    c.attend8 = reinterpret_cast<decltype(c.attend8)>(f[7]);
     return PyCapsule_New(new Calls(c), "jpi.kv", [](PyObject* o) { delete static_cast<Calls*>(PyCapsule_GetPointer(o, "jpi.kv")); });
 }
 
@@ -315,6 +439,10 @@ PyMethodDef methods[] = {{"calls", calls, METH_VARARGS, nullptr},
                          {"attend", fast(attend), METH_FASTCALL, nullptr},
                          {"weigh", fast(weigh), METH_FASTCALL, nullptr},
                          {"evict", fast(evict), METH_FASTCALL, nullptr},
+                         {"append_normed", fast(append_normed), METH_FASTCALL, nullptr},
+                         {"attend_window", fast(attend_window), METH_FASTCALL, nullptr},
+                         {"append8", fast(append8), METH_FASTCALL, nullptr},
+                         {"attend8", fast(attend8), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv", nullptr, -1, methods};
 

@@ -1,0 +1,18 @@
+// Attention over windows of a cache, in the handle's type or in 8 bits (jpi_kv_attend_window, jpi_kv8_attend): kv_span.cu.
+#pragma once
+#include "kv.h"
+
+namespace jpi {
+
+// What a query token sees of the rows before its count n, and how the cache is held: rows r < n with r < sink or r >= n - window.
+// The cache itself is the call's `own` side; codes of 8 bits have one byte an element, so that strides are bytes there.
+struct KvSpan {
+    int window = 0x7fffffff, sink = 0;
+    const uint8_t *ks = nullptr, *vs = nullptr;   // scales [caches][K][nblk], or NULL: not in 8 bits
+    int n_log2 = 0, nblk = 0;                     // rows of a block (log2), blocks of a cache
+};
+
+jpi_status kv_span_prepare(jpi_kv_handle* h);
+jpi_status launch_kv_span(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, void* out, float* lse, cudaStream_t st);
+
+}  // namespace jpi

@@ -91,6 +91,14 @@ _SIGS = {
                      c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p],
     "jpi_kv_evict": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p,
                      c_void_p, c_void_p, c_void_p],
+    "jpi_kv_append_normed": [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_void_p,
+                             c_void_p, c_int, c_int, c_void_p, c_void_p, c_void_p],
+    "jpi_kv_attend_window": [c_void_p, c_void_p, c_longlong, c_int, c_int, c_void_p, c_void_p, c_int, c_int, c_void_p, c_void_p,
+                             c_void_p],
+    "jpi_kv8_append": [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_void_p, c_void_p,
+                       c_void_p, c_int, c_int, c_void_p, c_void_p, c_void_p],
+    "jpi_kv8_attend": [c_void_p, c_void_p, c_longlong, c_int, c_int, c_void_p, c_void_p, c_int, c_int, c_void_p, c_void_p,
+                       c_void_p],
     "jpi_kv_device_status": [c_void_p],
     "jpi_kv_memory_usage": [c_void_p, POINTER(c_longlong)],
 }

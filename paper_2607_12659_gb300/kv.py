@@ -9,6 +9,10 @@ head-major cache is ``stored.transpose(1, 2)``):
 ``attend``  attention of a batch over shared prefixes and each request's own rows
 ``weigh``   accumulates the attention weight each cached key received
 ``evict``   keeps the rows with the most of it
+``attend_window``  attention over the newest rows before each token and a few first ones
+
+``append`` takes a ``Norm`` of each head's queries and keys before their coding. ``append8`` and ``attend8`` are the same on a
+``Cache8``, a cache held in 8 bits with a scale for each block of rows and head (``KV.cache8`` makes one).
 """
 
 from __future__ import annotations
@@ -33,6 +37,15 @@ class jpi_kv_config(ctypes.Structure):
 class jpi_kv_cache(ctypes.Structure):
     _fields_ = [("k", c_void_p), ("v", c_void_p)] + [
         (n, c_longlong) for n in ("cache_stride", "row_stride", "head_stride", "layer_stride")] + [("rows", c_int)]
+
+
+class jpi_kv_norm(ctypes.Structure):
+    _fields_ = [("q_weight", c_void_p), ("k_weight", c_void_p), ("eps", c_float)]
+
+
+class jpi_kv8_cache(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [
+        (n, c_longlong) for n in ("cache_stride", "row_stride", "head_stride")] + [("rows", c_int), ("block", c_int)]
 
 
 LAYOUTS = {"half": 0, "interleaved": 1}
@@ -76,6 +89,31 @@ def jpi_kv_evict(h, src, w, length, layers, caches, keep, sink, recent, dst, w_o
                                _ptr(w_out), _ptr(length_out), _ptr(kept), _stream(stream)), "jpi_kv_evict")
 
 
+def jpi_kv_append_normed(h, q, q_stride, k, k_stride, v, v_stride, norm, position, row, batch, tokens, q_out, cache, stream=None):
+    _check(load().jpi_kv_append_normed(h, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride,
+                                       byref(norm) if norm is not None else None, _ptr(position), _ptr(row), batch, tokens,
+                                       _ptr(q_out), byref(cache) if cache is not None else None, _stream(stream)),
+           "jpi_kv_append_normed")
+
+
+def jpi_kv_attend_window(h, q, q_stride, batch, tokens, cache, seen, window, sink, out, lse, stream=None):
+    _check(load().jpi_kv_attend_window(h, _ptr(q), q_stride, batch, tokens, byref(cache) if cache is not None else None,
+                                       _ptr(seen), window, sink, _ptr(out), _ptr(lse), _stream(stream)), "jpi_kv_attend_window")
+
+
+def jpi_kv8_append(h, q, q_stride, k, k_stride, v, v_stride, norm, position, start, count, batch, tokens, q_out, cache,
+                   stream=None):
+    _check(load().jpi_kv8_append(h, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride,
+                                 byref(norm) if norm is not None else None, _ptr(position), _ptr(start), _ptr(count), batch,
+                                 tokens, _ptr(q_out), byref(cache) if cache is not None else None, _stream(stream)),
+           "jpi_kv8_append")
+
+
+def jpi_kv8_attend(h, q, q_stride, batch, tokens, cache, seen, window, sink, out, lse, stream=None):
+    _check(load().jpi_kv8_attend(h, _ptr(q), q_stride, batch, tokens, byref(cache) if cache is not None else None, _ptr(seen),
+                                 window, sink, _ptr(out), _ptr(lse), _stream(stream)), "jpi_kv8_attend")
+
+
 def jpi_kv_device_status(h):
     _check(load().jpi_kv_device_status(h), "jpi_kv_device_status")
 
@@ -107,6 +145,34 @@ class Rope:
                            mscale=self.mscale)
 
 
+@dataclass(frozen=True)
+class Norm:
+    """Norm of each head's queries and keys before their rotary coding (jpi_kv_norm): x / sqrt(mean(x^2) + eps) * weight, weights
+    fp32 [head dim] or None (ones)."""
+    q_weight: object = None
+    k_weight: object = None
+    eps: float = 1e-6
+
+
+@dataclass(frozen=True)
+class Cache8:
+    """Caches held in 8 bits (jpi_kv8_cache): codes k, v float8_e4m3fn [caches][rows][KV heads][head dim], of any strides that are
+    multiples of 16 with contiguous heads, and the powers of two that blocks of `block` (16, 32 or 64) rows of a head are multiplied by, k_scale,
+    v_scale float8_e8m0fnu [caches][KV heads][ceil(rows / block)], contiguous."""
+    k: object
+    v: object
+    k_scale: object
+    v_scale: object
+    block: int = 32
+
+    def values(self):
+        """(k, v) as the fp32 numbers that they stand for."""
+        def of(codes, scale):
+            by = scale.float().transpose(1, 2).repeat_interleave(self.block, 1)[:, :codes.shape[1], :, None]
+            return codes.float() * by
+        return of(self.k, self.k_scale), of(self.v, self.v_scale)
+
+
 def cache_of(k, v=None, layers=False) -> jpi_kv_cache:
     """The jpi_kv_cache of tensors [caches][rows][KV heads][head dim], or with `layers` another dimension before them."""
     s = k.stride()
@@ -127,7 +193,9 @@ def _checked_calls(*geometry):
     except ImportError as e:
         raise RuntimeError(f"the module _kv is not built ({e}): run `python -m paper_2607_12659_gb300.build`") from e
     lib = load()
-    return _kv, _kv.calls(*geometry, *(ctypes.cast(getattr(lib, f"jpi_kv_{n}"), c_void_p).value for n in ("append", "attend", "weigh", "evict")))
+    return _kv, _kv.calls(*geometry, *(ctypes.cast(getattr(lib, n), c_void_p).value for n in (
+        "jpi_kv_append", "jpi_kv_attend", "jpi_kv_weigh", "jpi_kv_evict", "jpi_kv_append_normed", "jpi_kv_attend_window",
+        "jpi_kv8_append", "jpi_kv8_attend")))
 
 
 class KV:
@@ -171,16 +239,17 @@ class KV:
         result = getattr(self._kv, fn)(self._calls, self.handle, raw, *args)
         made = type(result) is not int      # else a status
         if not made and result:
-            _check(result, "jpi_kv_" + fn)
+            _check(result, "jpi_kv8_" + fn[:-1] if fn[-1] == "8" else "jpi_kv_" + fn)
         if on is not None:
             on.reads(*(t for t in reads if t is not None))
             on.returns(*returns, *((result,) if made else ()))
         return result
 
-    def append(self, q, k, v, positions, rows, cache_k=None, cache_v=None, q_out=None, stream=None):
+    def append(self, q, k, v, positions, rows, cache_k=None, cache_v=None, q_out=None, stream=None, norm=None):
         """Codes q [B][T][H][D] and k [B][T][Hk][D] for `positions` (int32 [B][T]) and writes k and v into `rows`
         (int32 [B][T]; a row outside the cache marks padding, one that a request names twice holds a mixture) of the caches.
-        Returns the coded queries. q, v, or k with v and the caches may be None."""
+        Returns the coded queries. q, v, or k with v and the caches may be None. With a `norm` (Norm) each head's queries and
+        keys are normalised first."""
         with self._on(stream) as on:
             returns = ()
             if q is None:
@@ -188,9 +257,70 @@ class KV:
             elif q_out is None:
                 q_out = self._torch.zeros((*q.shape[:2], self.heads, self.head_dim), dtype=self.dtype, device=self.device)
                 returns = (q_out,)
-            self._call("append", on, stream, (q, k, v, positions, rows, cache_k, cache_v, q_out),
-                       (q, k, v, positions, rows, cache_k, cache_v, None if returns else q_out), returns)
+            args = reads = (q, k, v, positions, rows, cache_k, cache_v)
+            args += (q_out,)
+            if norm is not None:
+                args += (norm.q_weight, norm.k_weight, norm.eps)
+                reads += (norm.q_weight, norm.k_weight)
+            self._call("append" if norm is None else "append_normed", on, stream, args,
+                       reads + (None if returns else q_out,), returns)
         return q_out
+
+    def cache8(self, caches: int, rows: int, block: int = 32) -> Cache8:
+        """New 8-bit caches of this geometry, all zeros."""
+        t = self._torch
+        codes = [t.zeros((caches, rows, self.kv_heads, self.head_dim), dtype=t.uint8, device=self.device) for _ in range(2)]
+        scales = [t.full((caches, self.kv_heads, -(-rows // block)), 127, dtype=t.uint8, device=self.device) for _ in range(2)]
+        return Cache8(*(c.view(t.float8_e4m3fn) for c in codes), *(s.view(t.float8_e8m0fnu) for s in scales), block)
+
+    def append8(self, q, k, v, positions, start, cache, count=None, norm=None, q_out=None, stream=None):
+        """Codes q [B][T][H][D] and k [B][T][Hk][D] for `positions` (int32 [B][T]), after a `norm` (Norm) if one is given, and
+        writes k and v of request b's first count[b] tokens (int32 [B]; None: all) into the rows from start[b] (int32 [B]) on
+        of the Cache8 `cache`. What the cache holds from those rows on is given up; a block with rows before them keeps its
+        scale or has it raised. Returns the coded queries. q, or k with v, may be None."""
+        with self._on(stream) as on:
+            returns = ()
+            if q is None:
+                q_out = None
+            elif q_out is None:
+                q_out = self._torch.zeros((*q.shape[:2], self.heads, self.head_dim), dtype=self.dtype, device=self.device)
+                returns = (q_out,)
+            reads = (q, k, v, positions, start, count, cache.k, cache.v, cache.k_scale, cache.v_scale)
+            args = reads + (cache.block, q_out)
+            args += (None, None, None, None) if norm is None else (True, norm.q_weight, norm.k_weight, norm.eps)
+            if norm is not None:
+                reads += (norm.q_weight, norm.k_weight)
+            self._call("append8", on, stream, args, reads + (None if returns else q_out,), returns)
+        return q_out
+
+    def _results(self, q, out, lse):
+        """(out, lse) of an attention over q, those that were made, and those that were given."""
+        made, given = [], [t for t in (out, lse) if t is not None]
+        if out is None:
+            out = self._torch.empty((*q.shape[:2], self.heads, self.head_dim), dtype=self.dtype, device=self.device)
+            made.append(out)
+        if lse is None:
+            lse = self._torch.empty((*q.shape[:2], self.heads), dtype=self._float, device=self.device)
+            made.append(lse)
+        return out, lse, made, given
+
+    def attend_window(self, q, cache, seen, window, sink=0, out=None, lse=None, stream=None):
+        """Attention of q [B][T][H][D] over the cache (k, v) [B][R][Hk][D]: token (b, t) sees of its rows before seen[b][t] (int32
+        [B][T]) the last `window` and the first `sink`. Returns (out, lse)."""
+        with self._on(stream) as on:
+            out, lse, made, given = self._results(q, out, lse)
+            self._call("attend_window", on, stream, (q, cache, seen, window, sink, out, lse),
+                       (q, seen, *(cache if isinstance(cache, (tuple, list)) else ()), *given), made)
+        return out, lse
+
+    def attend8(self, q, cache, seen, window=0, sink=0, out=None, lse=None, stream=None):
+        """Attention of q [B][T][H][D] over the Cache8 `cache`: token (b, t) sees its rows before seen[b][t] (int32 [B][T]), with a
+        window as in attend_window (0: all of them). Returns (out, lse)."""
+        with self._on(stream) as on:
+            out, lse, made, given = self._results(q, out, lse)
+            parts = (cache.k, cache.v, cache.k_scale, cache.v_scale)
+            self._call("attend8", on, stream, (q, *parts, cache.block, seen, window, sink, out, lse), (q, seen, *parts, *given), made)
+        return out, lse
 
     def attend(self, q, prefix=None, prefix_len=None, own=None, seen=None, out=None, lse=None, stream=None):
         """Attention of q [B][T][H][D] over the first prefix_len[g] rows of prefix (k, v) [G][P][Hk][D], shared by each
@@ -248,5 +378,6 @@ class KV:
         return jpi_kv_memory_usage(self.handle)
 
 
-__all__ = ["KV", "Rope", "cache_of", "jpi_kv_create", "jpi_kv_destroy", "jpi_kv_append", "jpi_kv_attend", "jpi_kv_weigh",
-           "jpi_kv_evict", "jpi_kv_device_status", "jpi_kv_memory_usage"]
+__all__ = ["KV", "Rope", "Norm", "Cache8", "cache_of", "jpi_kv_create", "jpi_kv_destroy", "jpi_kv_append", "jpi_kv_attend", "jpi_kv_weigh",
+           "jpi_kv_evict", "jpi_kv_append_normed", "jpi_kv_attend_window", "jpi_kv8_append", "jpi_kv8_attend",
+           "jpi_kv_device_status", "jpi_kv_memory_usage"]
