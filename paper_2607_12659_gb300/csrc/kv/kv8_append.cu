@@ -76,7 +76,7 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit) {
             for (int i = 0; i < 2 * V; ++i) x[p][i] = z[i / V][i % V];
         } else {
             const int position = MODE != RM_NONE && in ? a.h.position[tok0 + r] : 0;
-            auto rot = [&](int pr) { return phase(position, a.h.turns[pr], a.h.m); };
+            auto rot = [&](int pr) { return phase_near(position, a.h.turns[pr], a.h.m); };
             code_head<E, MODE>(ln, a.h, src + r * stride, in, raw[p], a.h.norm, a.h.k_weight, rot, x[p]);
         }
         if (in) {

@@ -57,6 +57,19 @@ __device__ __forceinline__ float2 phase(int position, uint64_t turns, float m) {
     return make_float2(c * m, s * m);
 }
 
+// The same with the angle reduced to an eighth of a turn before it becomes an fp32 number: off by 2^-28 turns in place of 2^-26, for
+// codes of 8 bits, where each value beside a border that falls to the other side is a step of its own.
+__device__ __forceinline__ float2 phase_near(int position, uint64_t turns, float m) {
+    const uint64_t ph = (uint64_t)(int64_t)position * turns;
+    const uint32_t quarter = (uint32_t)((ph + (1ull << 61)) >> 62);
+    const int32_t rest = (int32_t)((int64_t)(ph - ((uint64_t)quarter << 62)) >> 32);   // in units of 2^-32 turns
+    float s, c;
+    sincospif((float)rest * 4.656612873077393e-10f, &s, &c);
+    const float x = quarter & 1 ? s : c, y = quarter & 1 ? c : s;
+    // (c, s), (-s, c), (-c, -s), (s, -c)
+    return make_float2((quarter == 1 || quarter == 2 ? -x : x) * m, (quarter >= 2 ? -y : y) * m);
+}
+
 constexpr int AP_MAX_PAIRS = 128;   // dim / 2
 
 }  // namespace

@@ -71,13 +71,13 @@ __device__ __forceinline__ float2 head_norm(const float (&x)[N], int D, float ep
 #pragma unroll
     for (int i = 0; i < N; ++i) s = fmaf(x[i], x[i], s);
     s = group_sum(s, lanes_log2);
-    float2 r = make_float2(1.f, rsqrtf(s / (float)D + eps));
+    float2 r = make_float2(1.f, 1.f / sqrtf(s / (float)D + eps));
     if (__any_sync(0xffffffffu, s > 1e38f)) {
         float z = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) z = fmaf(x[i] * 0x1p-70f, x[i] * 0x1p-70f, z);
         z = group_sum(z, lanes_log2);
-        if (s > 1e38f) r = make_float2(0x1p-70f, rsqrtf(z / (float)D));   // (eps is less than a rounding here)
+        if (s > 1e38f) r = make_float2(0x1p-70f, 1.f / sqrtf(z / (float)D));   // (eps is less than a rounding here)
     }
     return r;
 }
@@ -200,7 +200,7 @@ __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens&
             if (MODE != RM_NONE)
                 for (int e = t; e < nt * half; e += nth) {
                     const int i = e / half, p = e - i * half;
-                    sm.table[i][entry(p)] = phase(a.position[tok0 + i], a.turns[p], a.m);
+                    sm.table[i][entry(p)] = phase_near(a.position[tok0 + i], a.turns[p], a.m);
                 }
             __syncthreads();
         }

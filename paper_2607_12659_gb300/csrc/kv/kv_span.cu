@@ -13,6 +13,7 @@
 #include "kv_span.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace jpi {
 namespace {
@@ -41,7 +42,7 @@ __device__ __forceinline__ float4 four<Code8>(const Code8* p) {
     return make_float4(z[0], z[1], z[2], z[3]);
 }
 
-// On CUDA cores: a warp takes 8 query rows over blocks of 32 keys, scores with a key per lane, values with a lane per four
+// fp32, on CUDA cores: a warp takes 8 query rows over blocks of 32 keys, scores with a key per lane, values with a lane per four
 // elements of d; the warps of a block take different row tiles or different keys of one.
 template <int DP, typename E, typename T>
 __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(const __grid_constant__ SpanArgs g) {
@@ -164,27 +165,572 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
     merge_and_write<DP, E>(a, x, sp, kv_smem, warp, lane);
 }
 
-// Pieces for blocks of `warps` warps that take blocks of `step` keys: splits of the rows that a tile can see, while each
-// warp keeps one and the parts fit the workspace, to `want` blocks in all.
-SidePlan plan_span(const jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, int warps, int step, long long want) {
+// bf16 queries. A warp works alone: it takes pieces (8 query rows over a range of the blocks that they see) in turn and streams
+// their blocks of keys, 16 KB with their values, through two stages of shared memory of its own by 16-byte asynchronous
+// copies, the next piece's first blocks and query rows behind this one's last; rows that no token of the piece sees arrive as zeros and
+// are not read. Keys are the 16 rows of mma.sync m16n8k16 and query rows its 8 columns; the values' product runs over keys
+// with d as its rows, the probabilities turned from one's result into the other's operand by 8 x 8 transposes.
+//
+// In 8 bits the codes become fp16 numbers on their way from shared memory into the fragments, two by one instruction: e4m3 is a
+// subset of fp16. What a lane reads as 32 bits of a key are four elements of d, taken as the fragment's two pairs (the
+// queries' are taken alike); of the values, by a transposing load, two elements of d of two keys, whose bytes one
+// permutation brings together by keys, so that the fragment's rows g and g + 8 are elements 2 g and 2 g + 1. A block's scale
+// multiplies its scores, and its probabilities before the second product: relative to the largest scale 2^e that the row
+// has seen, p 2^(e_j - e) 2^7 is at most 2^15, and as two fp16 terms is off by 2^-22 of itself or 2^-32 of 2^(e + 7).
+constexpr int SR_STAGE = 16384;
+
+template <int DP, bool Q8>
+struct SrSmem {
+    static constexpr int ROW = Q8 ? DP : 2 * DP;         // bytes of a key
+    static constexpr int KEYS = SR_STAGE / 2 / ROW;      // keys of a block
+    static constexpr int HALF = SR_STAGE / 2;
+    static constexpr int QBYTES = KR_ROWS * DP * 2;
+    static constexpr int Q_OFF = 2 * SR_STAGE;
+    static constexpr int SEEN_OFF = Q_OFF + 2 * QBYTES;  // [AHEAD][8] counts of the pieces in hand
+    static constexpr int AHEAD = 4;
+    static constexpr int BYTES = SEEN_OFF + AHEAD * KR_ROWS * 4;
+    static constexpr int ALONE = DP == 256 ? 5 : 6;      // blocks of an SM
+};
+
+__device__ __forceinline__ void sr_ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void sr_ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+// D += A B as kr_mma, fp16 operands.
+__device__ __forceinline__ void sr_mma_half(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                            uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t sr_half2(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+constexpr int SR_NONE = -4096;   // no scale seen yet
+
+template <int DP, bool Q8>
+__global__ void __launch_bounds__(32) k_kv_span_rows(const __grid_constant__ SpanArgs g_) {
+    using L = SrSmem<DP, Q8>;
+    using T = typename std::conditional<Q8, uint8_t, __nv_bfloat16>::type;
+    extern __shared__ __align__(128) uint8_t sr_smem[];
+    const AttendArgs& a = g_.a;
+    const KvSpan& sn = g_.s;
+    constexpr int MT = L::KEYS / 16;   // 16-key tiles of a block
+    constexpr int ND = DP / 16;
+    constexpr int EPC = Q8 ? 16 : 8;   // elements of a 16-byte chunk
+    constexpr int CH = DP / EPC;       // chunks of a row; chunk c of row r lies at c ^ turn(r)
+    constexpr int RPI = 32 / CH;       // rows one instruction of the warp copies
+    constexpr int QCH = DP / 8, QRPI = 32 / QCH;
+    const int lane = threadIdx.x, g = lane >> 2, j = lane & 3;
+    const uint32_t sm = ptx::smem_u32(sr_smem);
+    int* const counts = (int*)(sr_smem + L::SEEN_OFF);
+    ptx::grid_dep_launch();
+    const uint32_t pieces = (uint32_t)a.o.blocks;
+    const KvSide& s = a.c.own;
+    const int D = a.c.D, mych = lane % CH, myrow = lane / CH;
+    const bool dlive = EPC * mych < D;
+    const float slack = 8.f / a.c2;
+    auto turn = [](int r) { return CH == 4 ? (r >> 1) & 3 : r & 7; };
+
+    // ---- what is to be copied: pieces opened in order, block by block
+    uint32_t f_piece = blockIdx.x;
+    int f_seq = 0, f_full = 0, f_blk = 0, f_end = 0, f_lim = 0, f_first = 0;
+    SpanBlocks<L::KEYS> f_blocks(sn, 0, 0);
+    const T *f_k = nullptr, *f_v = nullptr;   // this lane's chunk of the open piece's row 0
+    const uint8_t* f_s = nullptr;             // scales of the open piece's keys (lanes below 16) or values
+    int s_new = 0, s_old = 0;                 // scales of the last block asked for, and the one before: tile lane % 16
+    int ahead = 0;                            // this lane's row's count of the next piece (lanes 0-7)
+    auto peek = [&]() {
+        ahead = 0;
+        if (f_piece < pieces) {
+            const Piece x = piece_of(a, f_piece, 0);
+            if (lane < KR_ROWS) ahead = row_seen(a.c, false, x.cache, x.t, x.t.r0 + lane);
+        }
+    };
+    int issued = 0, used = 0;
+    int seq = 0, full = 0;
+    auto produce = [&]() {
+        while (f_blk >= f_end) {
+            if (f_piece >= pieces || f_seq - seq >= L::AHEAD) return false;
+            const Piece x = piece_of(a, f_piece, 0);
+            if (lane < KR_ROWS) counts[(f_seq & (L::AHEAD - 1)) * KR_ROWS + lane] = ahead;
+            f_lim = __reduce_max_sync(0xffffffffu, lane < KR_ROWS ? ahead : 0);
+            f_first = __reduce_min_sync(0xffffffffu, lane < KR_ROWS && ahead > 0 ? span_first(sn, ahead) : 0x7fffffff);
+            f_blocks = SpanBlocks<L::KEYS>(sn, f_lim, f_first);
+            f_blk = (int)((long long)f_blocks.count * x.split / a.o.splits);
+            f_end = (int)((long long)f_blocks.count * (x.split + 1) / a.o.splits);
+            if (f_blk < f_end) {
+                const long long base = x.cache * s.cs + x.kvh * s.hs + (dlive ? EPC * mych : 0);
+                f_k = static_cast<const T*>(s.k) + base;
+                f_v = static_cast<const T*>(s.v) + base;
+                if (Q8) f_s = (lane < 16 ? sn.ks : sn.vs) + ((long long)x.cache * a.c.K + x.kvh) * sn.nblk;
+                // The query rows travel with the first block. (Two pieces' fit: with two blocks in hand, the piece with
+                // blocks before the last one is through.)
+#pragma unroll
+                for (int i = 0; i < KR_ROWS / QRPI; ++i) {
+                    const int rr = i * QRPI + lane / QCH, r = x.t.r0 + rr, ch = lane % QCH;
+                    const bool in = 8 * ch < D && r < x.t.R;
+                    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + (in ? row_query(a.c, x.t, r) + 8 * ch : 0);
+                    ptx::cp_async_16(sm + L::Q_OFF + (f_full & 1) * L::QBYTES + rr * (DP * 2) + ((ch ^ (rr & 7)) << 4), q, in);
+                }
+                ++f_full;
+            }
+            ++f_seq;
+            f_piece += gridDim.x;
+            peek();
+        }
+        const uint32_t dst = sm + (issued & 1) * SR_STAGE;
+        const int key0 = f_blocks.row(f_blk);
+        const T *k = f_k + (long long)(key0 + myrow) * s.rs, *v = f_v + (long long)(key0 + myrow) * s.rs;
+#pragma unroll
+        for (int i = 0; i < L::KEYS / RPI; ++i) {
+            const int rr = i * RPI + myrow;
+            const bool in = dlive && span_sees(sn, key0 + rr, f_lim, f_first);
+            const uint32_t at = rr * L::ROW + ((mych ^ turn(rr)) << 4);
+            ptx::cp_async_16(dst + at, in ? k : f_k, in);
+            ptx::cp_async_16(dst + L::HALF + at, in ? v : f_v, in);
+            k += RPI * s.rs;
+            v += RPI * s.rs;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (Q8) {
+            s_old = s_new;
+            const int tile = key0 + 16 * (lane & 15);
+            // (a tile that no row sees has no scale)
+            const bool in = (lane & 15) < MT && tile < f_lim && (tile < sn.sink || tile + 16 > f_first);
+            s_new = in ? (int)f_s[tile >> sn.n_log2] : -1;
+        }
+        ++issued;
+        ++f_blk;
+        return true;
+    };
+
+    peek();
+    if (produce()) produce();
+    for (uint32_t piece = blockIdx.x; piece < pieces; piece += gridDim.x, ++seq) {
+        const Piece x = piece_of(a, piece, 0);
+        if (f_seq <= seq) produce();
+        __syncwarp();
+        // What the lane's rows 2 j, 2 j + 1 see, and the tile's rows together.
+        const int n0 = counts[(seq & (L::AHEAD - 1)) * KR_ROWS + 2 * j], n1 = counts[(seq & (L::AHEAD - 1)) * KR_ROWS + 2 * j + 1];
+        const int w0 = span_first(sn, n0), w1 = span_first(sn, n1);
+        const int rj = x.t.r0 + 2 * j;
+        const bool in0 = rj < x.t.R, in1 = rj + 1 < x.t.R;
+        int lim = max(n0, n1), low = min(in0 ? n0 : 0x7fffffff, in1 ? n1 : 0x7fffffff);     // counts: most, least
+        int first = min(n0 > 0 ? w0 : 0x7fffffff, n1 > 0 ? w1 : 0x7fffffff), late = max(w0, w1);   // first rows: least, most
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            lim = max(lim, __shfl_xor_sync(0xffffffffu, lim, o));
+            low = min(low, __shfl_xor_sync(0xffffffffu, low, o));
+            first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
+            late = max(late, __shfl_xor_sync(0xffffffffu, late, o));
+        }
+        const SpanBlocks<L::KEYS> blocks(sn, lim, first);
+        const int b0 = (int)((long long)blocks.count * x.split / a.o.splits), b1 = (int)((long long)blocks.count * (x.split + 1) / a.o.splits);
+        uint32_t qf[ND][2];
+        float qs0 = 1.f, qs1 = 1.f;    // Q8: what the rows' queries were divided by
+        float o[ND][4];
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+        int v0 = SR_NONE, v1 = SR_NONE;   // Q8: the largest scale of values that the rows have seen
+        for (int blk = b0; blk < b1; ++blk) {
+            const int key0 = blocks.row(blk);
+            if (issued == used) produce();
+            int scale = 0;
+            if (issued - used > 1) {
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                if (Q8) scale = s_old;
+            } else {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                if (Q8) scale = s_new;
+            }
+            __syncwarp();
+            const uint32_t ks = sm + (used & 1) * SR_STAGE, vs = ks + L::HALF;
+            if (blk == b0) {
+                const uint32_t qb = L::Q_OFF + (full++ & 1) * L::QBYTES;
+                if constexpr (Q8) {
+                    const uint8_t* row = sr_smem + qb + g * (DP * 2) + (j & 1) * 8;
+                    auto at = [&](int i) { return *(const uint2*)(row + (((2 * i + (j >> 1)) ^ g) << 4)); };
+                    float top = 0.f;
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) {
+                        const uint2 u = at(i);
+                        const uint32_t w[2] = {u.x & 0x7fff7fffu, u.y & 0x7fff7fffu};
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xffff0000u);
+                            top = fmaxf(top, lo < INFINITY ? lo : 0.f);
+                            top = fmaxf(top, hi < INFINITY ? hi : 0.f);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 1; e < 4; e <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, e));
+                    // The largest to 2 .. 4: elements keep bf16's bits down to 2^-14 of it.
+                    const int E = max((int)(__float_as_uint(top) >> 23), 2);
+                    const float f = kv8_pow2(255 - E), q = kv8_pow2(E - 1);
+                    qs0 = __shfl_sync(0xffffffffu, q, 8 * j);
+                    qs1 = __shfl_sync(0xffffffffu, q, 8 * j + 4);
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) {
+                        const uint2 u = at(i);
+                        qf[i][0] = sr_half2(__uint_as_float(u.x << 16) * f, __uint_as_float(u.x & 0xffff0000u) * f);
+                        qf[i][1] = sr_half2(__uint_as_float(u.y << 16) * f, __uint_as_float(u.y & 0xffff0000u) * f);
+                    }
+                } else {
+                    const uint32_t qa = sm + qb + (lane & 7) * (DP * 2);
+#pragma unroll
+                    for (int i = 0; i < ND; i += 2) {
+                        uint32_t f[4];
+                        sr_ldsm4(f, qa + (((2 * i + (lane >> 3)) ^ (lane & 7)) << 4));
+                        qf[i][0] = f[0];
+                        qf[i][1] = f[1];
+                        qf[i + 1][0] = f[2];
+                        qf[i + 1][1] = f[3];
+                    }
+                }
+            }
+            // Four chains of products whatever the shape: one of D / 16 steps would be its latency.
+            constexpr int NCH = MT >= 4 ? 1 : 4 / MT;
+            float part[NCH][MT][4];
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) part[c][t][e] = 0.f;
+            const int kr = (lane & 7) + (lane & 8);   // key of this lane's matrix row; its chunk is 2 i + lane / 16
+            if constexpr (Q8) {
+#pragma unroll
+                for (int i = 0; i < ND; i += 2)
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        uint32_t f[4];
+                        sr_ldsm4(f, ks + (16 * t + kr) * L::ROW + (((i + (lane >> 4)) ^ turn(kr)) << 4));
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            sr_mma_half(part[(i + c) % NCH][t], kv8_half2(f[2 * c]), kv8_half2(f[2 * c + 1]), kv8_half2(f[2 * c] >> 16),
+                                        kv8_half2(f[2 * c + 1] >> 16), qf[i + c][0], qf[i + c][1]);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < ND; ++i)
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        uint32_t f[4];
+                        sr_ldsm4(f, ks + (16 * t + kr) * L::ROW + (((2 * i + (lane >> 4)) ^ turn(kr)) << 4));
+                        kr_mma(part[i % NCH][t], f[0], f[1], f[2], f[3], qf[i][0], qf[i][1]);
+                    }
+            }
+            float sc[MT][4];
+            const float mine = Q8 ? kv8_scale((uint32_t)max(scale, 0)) : 1.f;   // of tile lane % 16: keys below lane 16, values from there
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const float by = Q8 ? __shfl_sync(0xffffffffu, mine, t) : 1.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[t][e] = part[0][t][e];
+#pragma unroll
+                    for (int c = 1; c < NCH; ++c) sc[t][e] += part[c][t][e];
+                    if (Q8) sc[t][e] = sc[t][e] * by * (e & 1 ? qs1 : qs0);
+                }
+            }
+            // Keys g, g + 8 of each tile, rows 2 j, 2 j + 1; hidden scores are replaced, whatever they hold.
+            const bool cut = low < key0 + L::KEYS || (key0 < late && key0 + L::KEYS > sn.sink);   // the same for the warp
+            if (cut) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int key = key0 + 16 * t + g + 8 * e;
+                        if (!span_sees(sn, key, n0, w0)) sc[t][2 * e] = -INFINITY;
+                        if (!span_sees(sn, key, n1, w1)) sc[t][2 * e + 1] = -INFINITY;
+                    }
+            }
+            float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    x0 = fmaxf(x0, sc[t][2 * e]);
+                    x1 = fmaxf(x1, sc[t][2 * e + 1]);
+                }
+            float a0 = 1.f, a1 = 1.f;      // what the outputs so far are multiplied by
+            bool moved = false;            // (of the warp)
+            // The maximum moves only when a score passes it by more than 8 in log2 units (probabilities stay below 2^8):
+            // most blocks do not, and need no maximum over the keys' lanes.
+            if (__any_sync(0xffffffffu, x0 > m0 + slack || x1 > m1 + slack)) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, d));
+                    x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, d));
+                }
+                const float y0 = fmaxf(m0, x0), y1 = fmaxf(m1, x1);
+                a0 = m0 == -INFINITY ? 0.f : kr_ex2((m0 - y0) * a.c2);
+                a1 = m1 == -INFINITY ? 0.f : kr_ex2((m1 - y1) * a.c2);
+                m0 = y0;
+                m1 = y1;
+                l0 *= a0;
+                l1 *= a1;
+                moved = true;
+            }
+            // Likewise the largest scale of the values: outputs are in units of it.
+            if constexpr (Q8) {
+                const int top = __reduce_max_sync(0xffffffffu, lane >= 16 && scale < 255 ? scale : -1);
+                if (__any_sync(0xffffffffu, top > v0 || top > v1)) {
+                    int t0 = v0, t1 = v1;
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        const int e = __shfl_sync(0xffffffffu, scale, 16 + t), tile = key0 + 16 * t;
+                        if (e >= 0 && e < 255) {
+                            if (tile < n0 && (tile < sn.sink || tile + 16 > w0)) t0 = max(t0, max(e, 1));
+                            if (tile < n1 && (tile < sn.sink || tile + 16 > w1)) t1 = max(t1, max(e, 1));
+                        }
+                    }
+                    a0 *= kv8_pow2(127 + v0 - t0);
+                    a1 *= kv8_pow2(127 + v1 - t1);
+                    v0 = t0;
+                    v1 = t1;
+                    moved = true;
+                }
+            }
+            if (moved) {
+#pragma unroll
+                for (int i = 0; i < ND; ++i) {
+                    o[i][0] *= a0;
+                    o[i][1] *= a1;
+                    o[i][2] *= a0;
+                    o[i][3] *= a1;
+                }
+            }
+            const float f0 = m0 == -INFINITY ? 0.f : m0, f1 = m1 == -INFINITY ? 0.f : m1;
+            uint32_t ph[MT][2], pe[MT][2];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                float by0 = 1.f, by1 = 1.f;
+                if (Q8) {
+                    const int e = __shfl_sync(0xffffffffu, scale, 16 + t);
+                    by0 = e == 255 ? NAN : kv8_pow2(min(134 + e - v0, 254));
+                    by1 = e == 255 ? NAN : kv8_pow2(min(134 + e - v1, 254));
+                    if (e < 0) by0 = by1 = 1.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float p0 = kr_ex2((sc[t][2 * e] - f0) * a.c2), p1 = kr_ex2((sc[t][2 * e + 1] - f1) * a.c2);
+                    l0 += p0;
+                    l1 += p1;
+                    uint32_t h, r;
+                    if constexpr (Q8) {
+                        p0 *= by0;
+                        p1 *= by1;
+                        h = sr_half2(p0, p1);
+                        const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                        r = sr_half2(p0 - b.x, p1 - b.y);
+                    } else {
+                        h = kr_pack(p0, p1);
+                        r = kr_pack(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+                    }
+                    ph[t][e] = kr_transpose(h);
+                    pe[t][e] = kr_transpose(r);
+                }
+            }
+            if constexpr (Q8) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int i = 0; i < ND; i += 2) {
+                        uint32_t f[4];
+                        sr_ldsm4_t(f, vs + (16 * t + kr) * L::ROW + (((i + (lane >> 4)) ^ turn(kr)) << 4));
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const uint32_t lo = __byte_perm(f[2 * c], 0, 0x3120), hi = __byte_perm(f[2 * c + 1], 0, 0x3120);
+                            const uint32_t u0 = kv8_half2(lo), u1 = kv8_half2(lo >> 16), u2 = kv8_half2(hi), u3 = kv8_half2(hi >> 16);
+                            sr_mma_half(o[i + c], u0, u1, u2, u3, ph[t][0], ph[t][1]);
+                            sr_mma_half(o[i + c], u0, u1, u2, u3, pe[t][0], pe[t][1]);
+                        }
+                    }
+            } else {
+                const int vr = (lane & 7) + ((lane >> 4) << 3);   // key of this lane's matrix row; its chunk is 2 i + bit 3
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) {
+                        uint32_t f[4];
+                        sr_ldsm4_t(f, vs + (16 * t + vr) * L::ROW + (((2 * i + ((lane >> 3) & 1)) ^ turn(vr)) << 4));
+                        kr_mma(o[i], f[0], f[1], f[2], f[3], ph[t][0], ph[t][1]);
+                        kr_mma(o[i], f[0], f[1], f[2], f[3], pe[t][0], pe[t][1]);
+                    }
+            }
+            __syncwarp();   // every lane has read the stage
+            ++used;
+            produce();
+        }
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, d);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, d);
+        }
+        if (Q8) {
+            const float u0 = v0 == SR_NONE ? 0.f : kv8_scale((uint32_t)v0), u1 = v1 == SR_NONE ? 0.f : kv8_scale((uint32_t)v1);
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {
+                o[i][0] = o[i][0] * 0x1p-7f * u0;
+                o[i][1] = o[i][1] * 0x1p-7f * u1;
+                o[i][2] = o[i][2] * 0x1p-7f * u0;
+                o[i][3] = o[i][3] * 0x1p-7f * u1;
+            }
+        }
+        // Element e (0, 1: rows 2 j and 2 j + 1; 2, 3 likewise) of fragment i.
+        auto elem = [&](int i, int half) { return Q8 ? 16 * i + 2 * g + half : 16 * i + g + 8 * half; };
+        // An infinite value times what the rounding left of its probability (0, or of the other sign) is NaN, and so is 0 times an
+        // infinity or NaN that only another row of the tile sees. Rows whose sum is finite and outputs are not are formed
+        // again, key by key in fp32, each over its own keys.
+        float z0 = 0.f, z1 = 0.f;   // 0 as long as all are finite
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            z0 = fmaf(o[i][0], 0.f, fmaf(o[i][2], 0.f, z0));
+            z1 = fmaf(o[i][1], 0.f, fmaf(o[i][3], 0.f, z1));
+        }
+        uint32_t again = __reduce_or_sync(0xffffffffu, (in0 && l0 < INFINITY && !(z0 == 0.f) ? 1u << (2 * j) : 0u) |
+                                                           (in1 && l1 < INFINITY && !(z1 == 0.f) ? 2u << (2 * j) : 0u));
+        for (; again; again &= again - 1) {
+            const int r = __ffs(again) - 1;
+            const int n = __shfl_sync(0xffffffffu, (r & 1) ? n1 : n0, r >> 1);
+            float m = __shfl_sync(0xffffffffu, (r & 1) ? m1 : m0, r >> 1);
+            if (m == -INFINITY) m = 0.f;
+            constexpr int NL = DP / 32;   // lane's elements of a row: lane + 32 i
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q) + row_query(a.c, x.t, x.t.r0 + r);
+            const long long base = x.cache * s.cs + x.kvh * s.hs;
+            const long long sb = ((long long)x.cache * a.c.K + x.kvh) * sn.nblk;
+            auto value = [](T u) {
+                if constexpr (Q8) return __half2float(__ushort_as_half((unsigned short)kv8_half2(u)));
+                else return __bfloat162float(u);
+            };
+            float qr[NL], sum[NL];
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                qr[i] = lane + 32 * i < D ? __bfloat162float(q[lane + 32 * i]) : 0.f;
+                sum[i] = 0.f;
+            }
+#pragma unroll 1
+            for (int e = b0 * L::KEYS; e < b1 * L::KEYS; ++e) {
+                const int key = blocks.row(e / L::KEYS) + e % L::KEYS;
+                if (!span_sees(sn, key, n, span_first(sn, n))) continue;
+                const T *k = static_cast<const T*>(s.k) + base + key * s.rs, *v = static_cast<const T*>(s.v) + base + key * s.rs;
+                float dot = 0.f;
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    if (lane + 32 * i < D) dot = fmaf(qr[i], value(k[lane + 32 * i]), dot);
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
+                float vsc = 1.f;
+                if (Q8) {
+                    dot *= kv8_scale(sn.ks[sb + (key >> sn.n_log2)]);
+                    vsc = kv8_scale(sn.vs[sb + (key >> sn.n_log2)]);
+                }
+                const float pr = kr_ex2((dot - m) * a.c2);
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    if (lane + 32 * i < D) sum[i] = fmaf(pr, value(v[lane + 32 * i]) * vsc, sum[i]);
+            }
+            // Back to the fragments, through the lanes that hold the elements.
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {
+                const float y0 = __shfl_sync(0xffffffffu, sum[i >> 1], elem(i, 0) & 31), y1 = __shfl_sync(0xffffffffu, sum[i >> 1], elem(i, 1) & 31);
+                if (r == 2 * j) o[i][0] = y0, o[i][2] = y1;
+                if (r == 2 * j + 1) o[i][1] = y0, o[i][3] = y1;
+            }
+        }
+        const long long row0 = in0 ? row_index(a.c, x.t, rj) : 0, row1 = in1 ? row_index(a.c, x.t, rj + 1) : 0;
+        if (a.out) {
+            const float inv0 = inverse_sum(l0), inv1 = inverse_sum(l1);
+            __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(a.out);
+            if constexpr (Q8) {
+#pragma unroll
+                for (int i = 0; i < ND; ++i) {
+                    if (16 * i >= D) continue;
+                    if (in0) *(uint32_t*)(out + row0 * D + elem(i, 0)) = kr_pack(o[i][0] * inv0, o[i][2] * inv0);
+                    if (in1) *(uint32_t*)(out + row1 * D + elem(i, 0)) = kr_pack(o[i][1] * inv1, o[i][3] * inv1);
+                }
+            } else {
+                // Lanes g and g + 1 exchange halves, so that the even one has a pair of row 2 j and the odd one of row 2 j + 1.
+                const bool even = (g & 1) == 0;
+                __nv_bfloat16* dst = out + (even ? row0 : row1) * D + (g & ~1);
+#pragma unroll
+                for (int i = 0; i < ND; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float u = o[i][2 * e] * inv0, v = o[i][2 * e + 1] * inv1;
+                        const float w = __shfl_xor_sync(0xffffffffu, even ? v : u, 4);
+                        if ((even ? in0 : in1) && 16 * i + 8 * e < D)
+                            *(uint32_t*)(dst + 16 * i + 8 * e) = even ? kr_pack(u, w) : kr_pack(w, v);
+                    }
+            }
+            if (g == 0 && a.lse) {
+                if (in0) a.lse[row0] = log_sum(m0, l0, a.c.scale);
+                if (in1) a.lse[row1] = log_sum(m1, l1, a.c.scale);
+            }
+        } else {
+            const long long at0 = x.part * a.rows + row0, at1 = x.part * a.rows + row1;
+            if (g == 0 && in0) a.pml[row0 * a.parts + x.part] = make_float2(m0, l0);
+            if (g == 0 && in1) a.pml[row1 * a.parts + x.part] = make_float2(m1, l1);
+            const bool u0 = in0 && l0 != 0.f, u1 = in1 && l1 != 0.f;
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {
+                if constexpr (Q8) {
+                    if (16 * i >= D) continue;
+                    if (u0) *(float2*)(a.po + at0 * D + elem(i, 0)) = make_float2(o[i][0], o[i][2]);
+                    if (u1) *(float2*)(a.po + at1 * D + elem(i, 0)) = make_float2(o[i][1], o[i][3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (16 * i + 8 * e >= D) continue;
+                        if (u0) a.po[at0 * D + elem(i, e)] = o[i][2 * e];
+                        if (u1) a.po[at1 * D + elem(i, e)] = o[i][2 * e + 1];
+                    }
+                }
+            }
+        }
+    }
+}
+
+// How a call is dealt to blocks of `warps` warps, whose warps take `step` keys at a time: splits of the rows that a tile can see,
+// up to `want` blocks in all while a warp keeps `least` keys; a call of few pieces, which is waited for, down to single steps as
+// far as two blocks an SM go. The parts fit the workspace.
+SidePlan plan_span(const jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, int warps, int step, int least, long long want) {
     SidePlan s;
     const long long R = (long long)c.tokens * c.gq, rt = (R + KR_ROWS - 1) / KR_ROWS;
     while (s.wr < warps && s.wr < rt) s.wr *= 2;
     s.wk = warps / s.wr;
     s.tiles = (int)((rt + s.wr - 1) / s.wr);
-    // Rows of the cache that a tile's tokens see, and the ends of their blocks.
+    // Rows of the cache that the tokens of a tile see, with the ends of their blocks.
     const long long toks = std::min<long long>(c.tokens, (KR_ROWS + c.gq - 1) / c.gq + 1);
     const long long rows = std::min<long long>(c.own.rows, (long long)sn.window + toks + std::min(sn.sink, c.own.rows) + 2 * step);
     const long long blocks = (long long)c.batch * c.K * s.tiles, all = (long long)c.batch * c.tokens * c.H;
     const long long room = std::max(1ll, ws_rows(h) / all);
-    s.splits = (int)std::max(1ll, std::min({want / blocks, (rows + step * s.wk - 1) / (step * s.wk), room}));
+    const long long coarse = std::min(want / blocks, (rows + least * s.wk - 1) / (least * s.wk));
+    const long long fine = std::min(2ll * h->num_sms / blocks, (rows + step * s.wk - 1) / (step * s.wk));
+    s.splits = (int)std::max(1ll, std::min(std::max(coarse, fine), room));
     s.blocks = blocks * s.splits;
     s.by_splits = KvDiv((uint32_t)s.splits);
     s.by_tiles = KvDiv((uint32_t)s.tiles);
     return s;
 }
 
-template <int DP, typename E>
+template <int DP>
 jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void* out, float* lse, cudaStream_t st) {
     SpanArgs g = {};
     AttendArgs& a = g.a;
@@ -195,7 +741,13 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
     a.po = static_cast<float*>(h->ws);
     a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
     a.lse = lse;
-    a.o = plan_span(h, c, sn, AT_WARPS, 32, 2ll * h->num_sms);
+    const long long most = (long long)(DP == 256 ? 5 : 6) * h->num_sms;   // resident warps of the row kernels
+    if (h->bf16) {
+        const int keys = sn.ks ? SrSmem<DP, true>::KEYS : SrSmem<DP, false>::KEYS;
+        a.o = plan_span(h, c, sn, 1, keys, 4 * keys, most);
+    } else {
+        a.o = plan_span(h, c, sn, AT_WARPS, 32, 32, 2ll * h->num_sms);
+    }
     a.p.splits = 0;
     a.parts = a.o.splits;
     if (a.o.blocks > 0x7fffffffll) {
@@ -203,34 +755,39 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
         return JPI_ERR_SHAPE;
     }
     if (a.parts == 1) a.out = out;
-    JPI_TRY(kv_start(sn.ks ? k_kv_span_cc<DP, E, Code8> : k_kv_span_cc<DP, E, E>, dim3((unsigned)a.o.blocks), AT_THREADS,
-                     MergeSmem<DP>::BYTES, false, st, g));
+    if (h->bf16)
+        JPI_TRY(kv_start(sn.ks ? k_kv_span_rows<DP, true> : k_kv_span_rows<DP, false>, dim3((unsigned)std::min(a.o.blocks, most)), 32,
+                         SrSmem<DP, true>::BYTES, false, st, g));
+    else
+        JPI_TRY(kv_start(sn.ks ? k_kv_span_cc<DP, float, Code8> : k_kv_span_cc<DP, float, float>, dim3((unsigned)a.o.blocks), AT_THREADS,
+                         MergeSmem<DP>::BYTES, false, st, g));
     return a.parts == 1 ? JPI_OK : launch_kv_combine(h, c, a.parts, out, lse, st);
 }
 
-template <int DP, typename E>
-jpi_status prepare_dim() {
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_cc<DP, E, E>, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_cc<DP, E, Code8>, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
+template <int DP>
+jpi_status prepare_dim(const jpi_kv_handle* h) {
+    if (!h->bf16) {
+        for (auto* kernel : {k_kv_span_cc<DP, float, float>, k_kv_span_cc<DP, float, Code8>})
+            JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
+        return JPI_OK;
+    }
+    for (auto* kernel : {k_kv_span_rows<DP, false>, k_kv_span_rows<DP, true>}) {
+        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, true>::BYTES));
+        // All of its loads go to shared memory.
+        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+    }
     return JPI_OK;
-}
-
-template <typename E>
-jpi_status launch_type(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, void* out, float* lse, cudaStream_t st) {
-    return h->D <= 64 ? launch_dim<64, E>(h, c, s, out, lse, st)
-                      : h->D <= 128 ? launch_dim<128, E>(h, c, s, out, lse, st) : launch_dim<256, E>(h, c, s, out, lse, st);
-}
-template <typename E>
-jpi_status prepare_type(const jpi_kv_handle* h) {
-    return h->D <= 64 ? prepare_dim<64, E>() : h->D <= 128 ? prepare_dim<128, E>() : prepare_dim<256, E>();
 }
 
 }  // namespace
 
-jpi_status kv_span_prepare(jpi_kv_handle* h) { return h->bf16 ? prepare_type<__nv_bfloat16>(h) : prepare_type<float>(h); }
+jpi_status kv_span_prepare(jpi_kv_handle* h) {
+    return h->D <= 64 ? prepare_dim<64>(h) : h->D <= 128 ? prepare_dim<128>(h) : prepare_dim<256>(h);
+}
 
 jpi_status launch_kv_span(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, void* out, float* lse, cudaStream_t st) {
-    return h->bf16 ? launch_type<__nv_bfloat16>(h, c, s, out, lse, st) : launch_type<float>(h, c, s, out, lse, st);
+    return h->D <= 64 ? launch_dim<64>(h, c, s, out, lse, st)
+                      : h->D <= 128 ? launch_dim<128>(h, c, s, out, lse, st) : launch_dim<256>(h, c, s, out, lse, st);
 }
 
 }  // namespace jpi
