@@ -5,9 +5,9 @@
 // grows as rows come moves the codes before by a power of two, which e4m3 holds exactly but for its subnormals. (A scale that is
 // the maximum itself would round every code of the block again at each step.)
 //
-// Bound by memory. A block of threads has one KV head's keys or values in one block of rows: the new rows' loads are on
+// Bound by memory. A team of warps has one KV head's keys or values in one block of rows: the new rows' loads are on
 // their way together, held by groups of lanes (kv_heads.cuh), which normalise and turn them in registers; the maximum is
-// joined over the block, and the codes are written from the same registers. A (row, pair) has one user here, so its sine
+// joined over the team, and the codes are written from the same registers. A (row, pair) has one user here, so its sine
 // and cosine need no table. The queries' tokens are blocks of the same launch.
 
 #include "kv8.cuh"
@@ -25,7 +25,8 @@ struct Append8Args {
     long long cs, rs, hs;
     int rows, n_log2, nblk;   // rows of a cache, of a block (log2), blocks of a cache
     int touch;                // blocks that a request's tokens can touch
-    uint32_t units;           // blocks of threads of keys and values; the queries' follow
+    int team, teams;          // warps of a unit, units of a block
+    uint32_t units, blocks;   // of keys and values; the queries' blocks follow
     KvDiv by_touch, by_K;
 };
 
@@ -36,18 +37,19 @@ __device__ __forceinline__ int2 new_rows(const Append8Args& a, int b) {
     return make_int2(s, min(s + c, a.rows));
 }
 
+// One team of warps' unit: the keys or the values of one KV head in one block of rows. The team's threads meet at barrier
+// `bar` (a single warp: nowhere).
 template <typename E, int MODE>
-__device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit) {
+__device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit, int team, float* most) {
     constexpr int V = Chunk<E>::V;
-    constexpr int PASSES = V == 8 ? 4 : 8;   // rows of a group of lanes: 64 rows at 16 (bf16) or 8 groups
-    __shared__ float most[CT_THREADS / 32];
+    constexpr int PASSES = V == 8 ? 4 : 8;   // rows of a group of lanes
     uint32_t j, kvh;
     const bool value = unit & 1;
     const int b = (int)a.by_K.div(a.by_touch.div(unit >> 1, j), kvh);
     const int2 span = new_rows(a, b);
     const int first = ((span.x >> a.n_log2) + (int)j) << a.n_log2, lo = max(first, span.x), hi = min(first + (1 << a.n_log2), span.y);
     if (lo >= hi) return;
-    const int t = threadIdx.x, groups = blockDim.x >> a.h.lanes_log2, grp = t >> a.h.lanes_log2;
+    const int size = a.team * 32, t = threadIdx.x - team * size, groups = size >> a.h.lanes_log2, grp = t >> a.h.lanes_log2;
     const HeadLane<E, MODE> ln(t & ((1 << a.h.lanes_log2) - 1), a.h.D, a.h.dim);
     uint8_t* scale = (value ? a.vs : a.ks) + ((long long)b * a.K + kvh) * a.nblk + (first >> a.n_log2);
     uint8_t* codes = (value ? a.cv : a.ck) + b * a.cs + kvh * a.hs;
@@ -77,7 +79,13 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit) {
         } else {
             const int position = MODE != RM_NONE && in ? a.h.position[tok0 + r] : 0;
             auto rot = [&](int pr) { return phase_near(position, a.h.turns[pr], a.h.m); };
-            code_head<E, MODE>(ln, a.h, src + r * stride, in, raw[p], a.h.norm, a.h.k_weight, rot, x[p]);
+            const float* w = a.h.k_weight;
+            auto weight = [&](int i) {
+                const int c = 4 * i / V, d = ln.c[c] * V + 4 * i % V;
+                return w && ln.live[c] ? make_float4(w[d], w[d + 1], w[d + 2], w[d + 3]) : make_float4(1.f, 1.f, 1.f, 1.f);
+            };
+            auto other = [&](int d) { return w ? w[d] : 1.f; };
+            code_head<E, MODE>(ln, a.h, src + r * stride, in, raw[p], weight, other, rot, x[p]);
         }
         if (in) {
 #pragma unroll
@@ -89,9 +97,14 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit) {
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if ((t & 31) == 0) most[t >> 5] = top;
-    __syncthreads();   // (and every thread has the old scale)
-    for (int w = 0; w < (int)blockDim.x / 32; ++w) top = fmaxf(top, most[w]);
+    if (a.team > 1) {
+        most += team * a.team;
+        if ((t & 31) == 0) most[t >> 5] = top;
+        ptx::named_bar_sync(1 + team, size);   // (and every thread has the old scale)
+        for (int w = 0; w < a.team; ++w) top = fmaxf(top, most[w]);
+    } else {
+        __syncwarp();
+    }
     const int e = max(kv8_exponent(top), e_old);
     const float inv = kv8_pow2(254 - e);
     if (t == 0) *scale = (uint8_t)e;
@@ -118,7 +131,7 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit) {
     if (first < span.x && e > e_old) {   // (a scale of 255 is above every other)
         const float f = kv8_pow2(127 + e_old - e);
         const int per = a.h.D / 16, n = (span.x - first) * per;
-        for (int i = t; i < n; i += blockDim.x) {
+        for (int i = t; i < n; i += size) {
             uint4* at = reinterpret_cast<uint4*>(codes + (first + i / per) * a.rs + i % per * 16);
             uint4 u = *at;
             uint32_t* w = &u.x;
@@ -136,8 +149,12 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit) {
 template <typename E, int MODE>
 __global__ void __launch_bounds__(CT_THREADS) k_kv8_append(const __grid_constant__ Append8Args a) {
     __shared__ CodeSmem sm;
-    if (blockIdx.x < a.units) {
-        store8<E, MODE>(a, blockIdx.x);
+    __shared__ float most[CT_THREADS / 32];
+    extern __shared__ __align__(16) uint4 stage[];
+    if (blockIdx.x < a.blocks) {
+        const int team = threadIdx.x / (32 * a.team);
+        const uint32_t unit = blockIdx.x * a.teams + team;
+        if (team < a.teams && unit < a.units) store8<E, MODE>(a, unit, team, most);
         return;
     }
     auto place = [&](int tok) {
@@ -146,18 +163,28 @@ __global__ void __launch_bounds__(CT_THREADS) k_kv8_append(const __grid_constant
         return (int)t < span.y - span.x ? 0 : -1;
     };
     auto at = [](long long, int) { return 0ll; };
-    code_tokens<E, MODE>(a.h, a.ct, sm, blockIdx.x - a.units, static_cast<E*>(nullptr), static_cast<E*>(nullptr), 0, place, at);
+    code_tokens<E, MODE>(a.h, a.ct, sm, stage, blockIdx.x - a.blocks, gridDim.x - a.blocks, static_cast<E*>(nullptr), static_cast<E*>(nullptr), 0, place, at);
 }
 
 template <typename E>
-jpi_status launch(const Append8Args& a, int mode, unsigned blocks, int threads, cudaStream_t st) {
+jpi_status launch(const Append8Args& a, int mode, unsigned blocks, int threads, size_t smem, cudaStream_t st) {
     return kv_start(mode == RM_NONE ? k_kv8_append<E, RM_NONE>
                                     : mode == RM_HALF ? k_kv8_append<E, RM_HALF>
                                                       : mode == RM_INTER ? k_kv8_append<E, RM_INTER> : k_kv8_append<E, RM_SCALAR>,
-                    dim3(blocks), threads, 0, false, st, a);
+                    dim3(blocks), threads, smem, false, st, a);
+}
+
+template <typename E>
+jpi_status prepare_type() {
+    const int most = CT_STAGES * CT_PASSES * 2 * CT_THREADS * 16;
+    for (auto* kernel : {k_kv8_append<E, RM_NONE>, k_kv8_append<E, RM_HALF>, k_kv8_append<E, RM_INTER>, k_kv8_append<E, RM_SCALAR>})
+        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    return JPI_OK;
 }
 
 }  // namespace
+
+jpi_status kv8_append_prepare(const jpi_kv_handle* h) { return h->bf16 ? prepare_type<__nv_bfloat16>() : prepare_type<float>(); }
 
 jpi_status launch_kv8_append(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
                              const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position, const int* start,
@@ -200,21 +227,25 @@ jpi_status launch_kv8_append(const jpi_kv_handle* h, const void* q, long long q_
         a.hs = cache->head_stride;
         a.touch = (int)std::min<long long>(a.nblk, ((long long)tokens + 2 * cache->block - 2) / cache->block);
         units = 2ll * batch * h->K * a.touch;
-        // Groups of lanes for the rows of a block, four (bf16) or eight of them each.
-        const int passes = h->bf16 ? 4 : 8, rows = std::min(tokens, cache->block);
-        const int most = std::min(CT_THREADS, ((rows << a.h.lanes_log2) + 31) / 32 * 32);
-        if (!q || threads < most) threads = std::max(64, most);
-        if ((threads >> a.h.lanes_log2) * passes < rows) threads = CT_THREADS;
+        // Warps of a unit: two rows of its block for each group of lanes, as many more as that needs to fit its passes.
+        const int rows = std::min(tokens, cache->block);
+        a.team = 1;
+        while (a.team < CT_THREADS / 32 && (a.team * 32 >> a.h.lanes_log2) * 2 < rows) a.team *= 2;
+        if (!q) threads = std::max(64, a.team * 32);
+        threads = std::max(threads, a.team * 32);
+        a.teams = threads / 32 / a.team;
+        a.blocks = (uint32_t)((units + a.teams - 1) / a.teams);
     }
     a.by_touch = KvDiv((uint32_t)a.touch);
     a.by_K = KvDiv((uint32_t)h->K);
-    const long long n = (long long)batch * tokens, blocks = units + (q ? (n + a.ct.tt - 1) / a.ct.tt : 0);
-    if (blocks > 0x7fffffffll) {
+    if (units > 0x7fffffffll) {
         set_error("the call needs more than 2^31 blocks");
         return JPI_ERR_SHAPE;
     }
     a.units = (uint32_t)units;
-    return h->bf16 ? launch<__nv_bfloat16>(a, mode, (unsigned)blocks, threads, st) : launch<float>(a, mode, (unsigned)blocks, threads, st);
+    const size_t smem = q ? code_smem(a.ct, threads) : 0;
+    const unsigned blocks = a.blocks + (q ? (unsigned)std::min<long long>(a.ct.tasks, code_blocks(h, smem, threads)) : 0);
+    return h->bf16 ? launch<__nv_bfloat16>(a, mode, blocks, threads, smem, st) : launch<float>(a, mode, blocks, threads, smem, st);
 }
 
 }  // namespace jpi

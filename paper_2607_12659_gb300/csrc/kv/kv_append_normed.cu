@@ -2,8 +2,8 @@
 //
 //   y = rope(x / sqrt(mean(x^2) + eps) * w)
 //
-// Bound by memory: every element is read and written once. A block takes a few tokens; its heads are held by groups
-// of lanes (kv_heads.cuh), whose loads are all on their way before the tokens' rows, positions, sines and cosines are.
+// Bound by memory: every element is read and written once. Blocks stay and take tasks of a few tokens in turn, whose heads are
+// held by groups of lanes (kv_heads.cuh).
 
 #include "kv_heads.cuh"
 
@@ -22,24 +22,35 @@ struct NormedArgs {
 template <typename E, int MODE>
 __global__ void __launch_bounds__(CT_THREADS) k_kv_append_normed(const __grid_constant__ NormedArgs a) {
     __shared__ CodeSmem sm;
+    extern __shared__ __align__(16) uint4 stage[];
     auto place = [&](int tok) {
         const int r = a.row[tok];
         return r < a.rows ? r : -1;
     };
     auto at = [&](long long tok, int row) { return (long long)a.h.by_tokens.div((uint32_t)tok) * a.cs + row * a.rs; };
-    code_tokens<E, MODE>(a.h, a.ct, sm, blockIdx.x, static_cast<E*>(a.ck), static_cast<E*>(a.cv), a.hs, place, at);
+    code_tokens<E, MODE>(a.h, a.ct, sm, stage, blockIdx.x, gridDim.x, static_cast<E*>(a.ck), static_cast<E*>(a.cv), a.hs, place, at);
 }
 
 template <typename E>
-jpi_status launch(const NormedArgs& a, int mode, int threads, cudaStream_t st) {
-    const long long n = (long long)a.h.batch * a.h.tokens, blocks = (n + a.ct.tt - 1) / a.ct.tt;
-    return kv_start(mode == RM_NONE ? k_kv_append_normed<E, RM_NONE>
-                                    : mode == RM_HALF ? k_kv_append_normed<E, RM_HALF>
-                                                      : mode == RM_INTER ? k_kv_append_normed<E, RM_INTER> : k_kv_append_normed<E, RM_SCALAR>,
-                    dim3((unsigned)blocks), threads, 0, false, st, a);
+jpi_status launch(const jpi_kv_handle* h, const NormedArgs& a, int mode, int threads, cudaStream_t st) {
+    auto* const kernel = mode == RM_NONE ? k_kv_append_normed<E, RM_NONE>
+                                         : mode == RM_HALF ? k_kv_append_normed<E, RM_HALF>
+                                                           : mode == RM_INTER ? k_kv_append_normed<E, RM_INTER> : k_kv_append_normed<E, RM_SCALAR>;
+    const size_t smem = code_smem(a.ct, threads);
+    return kv_start(kernel, dim3((unsigned)std::min<long long>(a.ct.tasks, code_blocks(h, smem, threads))), threads, smem, false, st, a);
+}
+
+template <typename E>
+jpi_status prepare_type() {
+    const int most = CT_STAGES * CT_PASSES * 2 * CT_THREADS * 16;
+    for (auto* kernel : {k_kv_append_normed<E, RM_NONE>, k_kv_append_normed<E, RM_HALF>, k_kv_append_normed<E, RM_INTER>, k_kv_append_normed<E, RM_SCALAR>})
+        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    return JPI_OK;
 }
 
 }  // namespace
+
+jpi_status kv_append_normed_prepare(const jpi_kv_handle* h) { return h->bf16 ? prepare_type<__nv_bfloat16>() : prepare_type<float>(); }
 
 jpi_status launch_kv_append_normed(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
                                    const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position, const int* row,
@@ -73,7 +84,7 @@ jpi_status launch_kv_append_normed(const jpi_kv_handle* h, const void* q, long l
     }
     int threads;
     const int mode = plan_code_tokens(h, a.h, a.ct, v ? h->K : 0, &threads);
-    return h->bf16 ? launch<__nv_bfloat16>(a, mode, threads, st) : launch<float>(a, mode, threads, st);
+    return h->bf16 ? launch<__nv_bfloat16>(h, a, mode, threads, st) : launch<float>(h, a, mode, threads, st);
 }
 
 }  // namespace jpi

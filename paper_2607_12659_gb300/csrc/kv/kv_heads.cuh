@@ -6,6 +6,9 @@
 #pragma once
 
 #include "kv_code.cuh"
+#include "../ptx.h"
+
+#include <algorithm>
 
 namespace jpi {
 namespace {
@@ -82,12 +85,14 @@ __device__ __forceinline__ float2 head_norm(const float (&x)[N], int D, float ep
     return r;
 }
 
-// One lane's part of a head, normalised (with `weight`, in memory that every lane can read, or NULL) and coded. `head` is
-// where it was loaded from, unwritten so far; rot(pair) gives (cos, sin) times m. Every lane of the warp calls.
-template <typename E, int MODE, typename Rot>
+// One lane's part of a head, normalised if the call asks for it and coded. weight(i) gives the norm's weights of the lane's elements
+// 4 i .., other(d) that of element d; `head` is where it was loaded from, unwritten so far; rot(pair) gives (cos, sin)
+// times m. Every lane of the warp calls.
+template <typename E, int MODE, typename Weight, typename Other, typename Rot>
 __device__ __forceinline__ void code_head(const HeadLane<E, MODE>& ln, const HeadArgs& a, const E* head, bool in,
-                                          const uint4 (&raw)[2], bool norm, const float* weight, const Rot& rot,
+                                          const uint4 (&raw)[2], const Weight& weight, const Other& other, const Rot& rot,
                                           float (&y)[2 * Chunk<E>::V]) {
+    const bool norm = a.norm;
     constexpr int V = Chunk<E>::V;
     float x[2 * V];
     {
@@ -101,9 +106,12 @@ __device__ __forceinline__ void code_head(const HeadLane<E, MODE>& ln, const Hea
     if (norm) {
         r = head_norm(x, a.D, a.eps, a.lanes_log2);
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) {
-            x[i] = x[i] * r.x * r.y;
-            if (weight && ln.live[i / V]) x[i] *= weight[ln.c[i / V] * V + i % V];
+        for (int i = 0; i < 2 * V; i += 4) {
+            const float4 w = weight(i / 4);
+            x[i] = x[i] * r.x * r.y * w.x;
+            x[i + 1] = x[i + 1] * r.x * r.y * w.y;
+            x[i + 2] = x[i + 2] * r.x * r.y * w.z;
+            x[i + 3] = x[i + 3] * r.x * r.y * w.w;
         }
     }
     const int half = a.dim / 2;
@@ -133,10 +141,7 @@ __device__ __forceinline__ void code_head(const HeadLane<E, MODE>& ln, const Hea
             if (turn) {
                 const int o = d < half ? d + half : d - half;
                 float z = to_f(head[o]);
-                if (norm) {
-                    z = z * r.x * r.y;
-                    if (weight) z *= weight[o];
-                }
+                if (norm) z = z * r.x * r.y * other(o);
                 const float2 c = rot(d < half ? d : o);
                 y[i] = d < half ? x[i] * c.x - z * c.y : x[i] * c.x + z * c.y;
             }
@@ -148,91 +153,148 @@ __device__ __forceinline__ void code_head(const HeadLane<E, MODE>& ln, const Hea
     }
 }
 
-constexpr int CT_TOKENS = 8;    // most tokens of a block
-constexpr int CT_PASSES = 4;    // heads of a group of lanes that are on their way together
+constexpr int CT_TOKENS = 4;    // most tokens of a task
+constexpr int CT_PASSES = 4;    // most heads of a group of lanes in a task
+constexpr int CT_STAGES = 3;    // tasks in hand
+constexpr int CT_RUN = 16;      // tasks whose rows and positions are read together
 constexpr int CT_THREADS = 256;
 
+// A call's tokens as tasks: `tt` tokens, or, of more heads than the groups of lanes hold in their passes, a part of one token's.
 struct CodeTokens {
-    int tt;               // tokens of a block
-    KvDiv by_heads;       // rows of a token: H queries, K keys, K values
-    int heads;
+    int tt, heads, passes;   // heads of a token: H queries, K keys, K values
+    int parts, tasks;        // tasks of a token, of the call
+    KvDiv by_heads, by_parts;
 };
 
 struct CodeSmem {
-    float2 table[CT_TOKENS][AP_MAX_PAIRS + 8];
-    float weight[2][256];
-    int2 token[CT_TOKENS];   // (row, position)
+    float2 table[2][CT_TOKENS][AP_MAX_PAIRS + 8];
+    float4 weight[2][4][32];          // of queries and keys: elements 4 i .. of each lane's of a group
+    int2 token[CT_RUN][CT_TOKENS];    // (row, position)
 };
 
-// The tokens tt * block, .. of a call: rotary tables of all of them, then their heads in turn. place(token) is the row that
-// takes it, negative: padding; at(token, row) its place in the cache (element offset). A table is laid out so that the
-// lanes of a group, which read the same pair of consecutive chunks, read side by side.
+// Takes tasks first, first + step, .. of a call. Their heads are copied asynchronously into shared memory, each thread's chunks
+// into places of its own, two tasks ahead of the one whose sines, cosines and norms are computed; a table of those of a task's tokens
+// serves all its heads. place(token) is the row that takes it, negative: padding; at(token, row) its place in the cache (element
+// offset). A table is laid out so that the lanes of a group, which read the same pair of consecutive chunks, read side by side.
 template <typename E, int MODE, typename Place, typename At>
-__device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens& ct, CodeSmem& sm, int block, E* ck, E* cv,
-                                            long long hs, const Place& place, const At& at) {
+__device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens& ct, CodeSmem& sm, uint4* stage, int first, int step,
+                                            E* ck, E* cv, long long hs, const Place& place, const At& at) {
     constexpr int V = Chunk<E>::V, PC = MODE == RM_HALF ? V : MODE == RM_INTER ? V / 2 : 1;
     const int t = threadIdx.x, nth = blockDim.x, half = a.dim / 2, chunks = (half + PC - 1) / PC;
-    const int tok0 = block * ct.tt, nt = min(ct.tt, a.batch * a.tokens - tok0), rows = nt * ct.heads;
-    const int groups = nth >> a.lanes_log2, grp = t >> a.lanes_log2;
-    const HeadLane<E, MODE> ln(t & ((1 << a.lanes_log2) - 1), a.D, a.dim);
+    const int groups = nth >> a.lanes_log2, grp = t >> a.lanes_log2, u = t & ((1 << a.lanes_log2) - 1), n = a.batch * a.tokens;
+    const HeadLane<E, MODE> ln(u, a.D, a.dim);
     auto entry = [&](int p) { return p % PC * chunks + p / PC; };
-    for (int r0 = 0; r0 < rows; r0 += CT_PASSES * groups) {
-        uint4 raw[CT_PASSES][2];
-        const E* src[CT_PASSES];
+    auto slot = [&](int k, int p, int c) { return ((k % CT_STAGES * ct.passes + p) * 2 + c) * nth + t; };
+    struct Task {
+        int tok0, nt, r0, rows;   // tokens; rows r0 .. rows - 1 of (token, head)
+    };
+    auto task_of = [&](int k) {   // the run's k-th
+        uint32_t part;
+        Task x;
+        x.tok0 = (int)ct.by_parts.div((uint32_t)(first + k * step), part) * ct.tt;
+        x.nt = min(ct.tt, n - x.tok0);
+        x.r0 = (int)part * ct.passes * groups;
+        x.rows = min(x.nt * ct.heads, x.r0 + ct.passes * groups);
+        return x;
+    };
+    // A row's token of the task and head.
+    auto head_of = [&](int r, int& i) {
+        uint32_t h;
+        i = (int)ct.by_heads.div((uint32_t)r, h);
+        return (int)h;
+    };
+    auto source = [&](long long tok, int hd) {
+        return hd < a.H ? static_cast<const E*>(a.q) + tok * a.q_stride + hd * a.D
+                        : hd < a.H + a.K ? static_cast<const E*>(a.k) + tok * a.k_stride + (hd - a.H) * a.D
+                                         : static_cast<const E*>(a.v) + tok * a.v_stride + (hd - a.H - a.K) * a.D;
+    };
+    auto fetch = [&](int k, int count, bool known) {
+        if (k < count) {
+            const Task x = task_of(k);
+            for (int p = 0; p < ct.passes; ++p) {
+                const int r = x.r0 + p * groups + grp;
+                if (r >= x.rows) break;
+                int i;
+                const int hd = head_of(r, i);
+                if (known && sm.token[k][i].x < 0) continue;
+                const E* src = source(x.tok0 + i, hd);
 #pragma unroll
-        for (int p = 0; p < CT_PASSES; ++p) {
-            const int r = r0 + p * groups + grp;
-            uint32_t h;
-            const long long tok = tok0 + ct.by_heads.div((uint32_t)r, h);
-            const int hd = (int)h;
-            src[p] = hd < a.H ? static_cast<const E*>(a.q) + tok * a.q_stride + hd * a.D
-                              : hd < a.H + a.K ? static_cast<const E*>(a.k) + tok * a.k_stride + (hd - a.H) * a.D
-                                               : static_cast<const E*>(a.v) + tok * a.v_stride + (hd - a.H - a.K) * a.D;
-            ln.load(src[p], r < rows, raw[p]);
-        }
-        if (r0 == 0) {   // beside the first loads
-            if (t < nt) sm.token[t] = make_int2(place(tok0 + t), a.position[tok0 + t]);
-            if (a.norm)
-                for (int d = t; d < a.D; d += nth) {
-                    sm.weight[0][d] = a.q_weight ? a.q_weight[d] : 1.f;
-                    sm.weight[1][d] = a.k_weight ? a.k_weight[d] : 1.f;
-                }
-            if (MODE != RM_NONE)
-                for (int e = t; e < nt * half; e += nth) {
-                    const int i = e / half, p = e - i * half;
-                    sm.table[i][entry(p)] = phase_near(a.position[tok0 + i], a.turns[p], a.m);
-                }
-            __syncthreads();
-        }
-#pragma unroll
-        for (int p = 0; p < CT_PASSES; ++p) {
-            if (r0 + p * groups >= rows) break;   // (the same for the block)
-            const int r = r0 + p * groups + grp;
-            const bool in = r < rows;
-            uint32_t h;
-            const int i = in ? (int)ct.by_heads.div((uint32_t)r, h) : 0, hd = in ? (int)h : 0;
-            const bool value = hd >= a.H + a.K, key = !value && hd >= a.H;
-            float y[2 * V];
-            auto rot = [&](int pr) { return sm.table[i][entry(pr)]; };
-            code_head<E, MODE>(ln, a, src[p], in && !value, raw[p], a.norm, sm.weight[key], rot, y);
-            const int row = sm.token[i].x;
-            if (!in || row < 0) continue;
-            const long long tok = tok0 + i;
-            E* dst = hd < a.H ? static_cast<E*>(a.q_out) + (tok * a.H + hd) * a.D
-                              : (value ? cv + (hd - a.H - a.K) * hs : ck + (hd - a.H) * hs) + at(tok, row);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (!ln.live[c]) continue;
-                float z[V];
-#pragma unroll
-                for (int e = 0; e < V; ++e) z[e] = y[c * V + e];
-                *reinterpret_cast<uint4*>(dst + ln.c[c] * V) = value ? raw[p][c] : Chunk<E>::pack(z);
+                for (int c = 0; c < 2; ++c)
+                    if (ln.live[c]) ptx::cp_async_16(ptx::smem_u32(stage + slot(k, p, c)), src + ln.c[c] * V, true);
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int turn = 0;
+    for (bool begin = true; first < ct.tasks; first += CT_RUN * step, begin = false) {
+        const int count = min(CT_RUN, (ct.tasks - first + step - 1) / step);
+        if (begin) fetch(0, count, false);   // the first task's heads on their way beside its rows
+        __syncthreads();                     // the last run's tokens have been read
+        for (int e = t; e < count * ct.tt; e += nth) {
+            const int k = e / ct.tt, i = e - k * ct.tt;
+            const Task x = task_of(k);
+            if (i < x.nt) sm.token[k][i] = make_int2(place(x.tok0 + i), a.position[x.tok0 + i]);
+        }
+        if (begin && a.norm)
+            for (int e = t; e < 2 * (V / 2) << a.lanes_log2; e += nth) {
+                const int lane = e & ((1 << a.lanes_log2) - 1), i = (e >> a.lanes_log2) % (V / 2), k = (e >> a.lanes_log2) / (V / 2);
+                const HeadLane<E, MODE> x(lane, a.D, a.dim);
+                const float* w = k ? a.k_weight : a.q_weight;
+                const int c = 4 * i / V, d = x.c[c] * V + 4 * i % V;
+                sm.weight[k][i][lane] = w && x.live[c] ? make_float4(w[d], w[d + 1], w[d + 2], w[d + 3]) : make_float4(1.f, 1.f, 1.f, 1.f);
+            }
+        __syncthreads();
+        if (!begin) fetch(0, count, true);
+        fetch(1, count, true);
+        for (int k = 0; k < count; ++k) {
+            fetch(k + 2, count, true);
+            const Task x = task_of(k);
+            turn ^= 1;   // the other table may still be read; this one's readers are past the last barrier
+            if (MODE != RM_NONE) {
+                for (int e = t; e < x.nt * half; e += nth) {
+                    const int i = e / half, p = e - i * half;
+                    if (sm.token[k][i].x >= 0) sm.table[turn][i][entry(p)] = phase_near(sm.token[k][i].y, a.turns[p], a.m);
+                }
+                __syncthreads();
+            }
+            asm volatile("cp.async.wait_group 2;" ::: "memory");
+            for (int p = 0; p < ct.passes; ++p) {
+                if (x.r0 + p * groups >= x.rows) break;   // (the same for the block)
+                const int r = x.r0 + p * groups + grp;
+                int i;
+                int hd = head_of(min(r, x.rows - 1), i);
+                const bool live = r < x.rows && sm.token[k][i].x >= 0;
+                if (!__any_sync(0xffffffffu, live)) continue;
+                const bool value = hd >= a.H + a.K, key = !value && hd >= a.H;
+                uint4 raw[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) raw[c] = live && ln.live[c] ? stage[slot(k, p, c)] : make_uint4(0, 0, 0, 0);
+                float y[2 * V];
+                auto rot = [&](int pr) { return sm.table[turn][i][entry(pr)]; };
+                auto weight = [&](int e4) { return sm.weight[key][e4][u]; };
+                auto other = [&](int d) { return (key ? a.k_weight : a.q_weight) ? (key ? a.k_weight : a.q_weight)[d] : 1.f; };
+                const E* src = source(x.tok0 + i, hd);
+                code_head<E, MODE>(ln, a, src, live && !value, raw, weight, other, rot, y);
+                if (!live) continue;
+                const int row = sm.token[k][i].x;
+                const long long tok = x.tok0 + i;
+                E* dst = hd < a.H ? static_cast<E*>(a.q_out) + (tok * a.H + hd) * a.D
+                                  : (value ? cv + (hd - a.H - a.K) * hs : ck + (hd - a.H) * hs) + at(tok, row);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (!ln.live[c]) continue;
+                    float z[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) z[e] = y[c * V + e];
+                    *reinterpret_cast<uint4*>(dst + ln.c[c] * V) = value ? raw[c] : Chunk<E>::pack(z);
+                }
+            }
+        }
+        ptx::cp_async_wait_all();   // (empty groups)
     }
 }
 
-// Fills in how a call is coded; a.q .. a.norm are the caller's.
+// Fills in how a call is coded; a.q .. a.norm are the caller's. Returns the rotary mode.
 inline int plan_code_tokens(const jpi_kv_handle* h, HeadArgs& a, CodeTokens& ct, int values, int* threads) {
     const int V = h->bf16 ? 8 : 4;
     int mode = RM_NONE;
@@ -245,16 +307,24 @@ inline int plan_code_tokens(const jpi_kv_handle* h, HeadArgs& a, CodeTokens& ct,
     }
     a.by_tokens = KvDiv((uint32_t)a.tokens);
     a.lanes_log2 = head_lanes_log2(a.D, V, a.dim, mode);
-    ct.heads = a.H + a.K + values;
-    ct.by_heads = KvDiv((uint32_t)(ct.heads > 0 ? ct.heads : 1));
+    ct.heads = std::max(1, a.H + a.K + values);
+    ct.by_heads = KvDiv((uint32_t)ct.heads);
     const long long n = (long long)a.batch * a.tokens;
-    // As many tokens as a block's loads in flight hold, while there are two blocks an SM.
+    // Tokens of a task: as many as its passes hold, while there are two tasks an SM.
     const int groups = CT_THREADS >> a.lanes_log2;
     ct.tt = 1;
     while (ct.tt < CT_TOKENS && 2 * ct.tt * ct.heads <= CT_PASSES * groups && n >= 4ll * ct.tt * h->num_sms) ct.tt *= 2;
-    const int want = ((ct.tt * ct.heads) << a.lanes_log2) + 31;
-    *threads = want >= CT_THREADS ? CT_THREADS : want < 64 ? 64 : want / 32 * 32;
+    ct.passes = std::min(CT_PASSES, (ct.tt * ct.heads + groups - 1) / groups);
+    ct.parts = (ct.tt * ct.heads + ct.passes * groups - 1) / (ct.passes * groups);
+    ct.by_parts = KvDiv((uint32_t)ct.parts);
+    ct.tasks = (int)((n + ct.tt - 1) / ct.tt * ct.parts);
+    *threads = ct.parts > 1 || ct.passes > 1 ? CT_THREADS : std::max(64, ((ct.tt * ct.heads << a.lanes_log2) + 31) / 32 * 32);
     return mode;
+}
+inline size_t code_smem(const CodeTokens& ct, int threads) { return (size_t)CT_STAGES * ct.passes * 2 * threads * 16; }
+// Blocks that are resident together, by shared memory (to 190 KB of an SM) and threads.
+inline long long code_blocks(const jpi_kv_handle* h, size_t smem, int threads) {
+    return (long long)h->num_sms * std::max<long long>(1, std::min<long long>(1536 / threads, (190 << 10) / (long long)(smem + sizeof(CodeSmem) + 2048)));
 }
 
 }  // namespace
