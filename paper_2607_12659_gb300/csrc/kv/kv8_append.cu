@@ -63,22 +63,33 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit, int 
         const int r = p * groups + grp;
         ln.load(src + r * stride, lo + r < hi, raw[p]);
     }
-    float x[PASSES][2 * V];
+    float2 x[PASSES][V];
     float top = 0.f;
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-        if (lo + p * groups >= hi) break;   // (the same for the block)
+        if (lo + p * groups >= hi) break;   // (the same for the team)
         const int r = p * groups + grp;
         const bool in = lo + r < hi;
         if (value) {
-            float z[2][V];
-            Chunk<E>::unpack(raw[p][0], z[0]);
-            Chunk<E>::unpack(raw[p][1], z[1]);
 #pragma unroll
-            for (int i = 0; i < 2 * V; ++i) x[p][i] = z[i / V][i % V];
+            for (int c = 0; c < 2; ++c) {
+                float z[V];
+                Chunk<E>::unpack(raw[p][c], z);
+#pragma unroll
+                for (int i = 0; i < V / 2; ++i) x[p][c * (V / 2) + i] = make_float2(z[2 * i], z[2 * i + 1]);
+            }
         } else {
             const int position = MODE != RM_NONE && in ? a.h.position[tok0 + r] : 0;
-            auto rot = [&](int pr) { return phase_near(position, a.h.turns[pr], a.h.m); };
+            constexpr int PC = pairs_of_chunk<E, MODE>();
+            auto rot = [&](int q, float (&c)[PC], float (&s)[PC]) {
+#pragma unroll
+                for (int i = 0; i < PC; ++i) {
+                    const int pr = q * PC + i;
+                    const float2 z = phase_near(position, pr < a.h.dim / 2 ? a.h.turns[pr] : 0, a.h.m);
+                    c[i] = z.x;
+                    s[i] = z.y;
+                }
+            };
             const float* w = a.h.k_weight;
             auto weight = [&](int i) {
                 const int c = 4 * i / V, d = ln.c[c] * V + 4 * i % V;
@@ -89,9 +100,10 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit, int 
         }
         if (in) {
 #pragma unroll
-            for (int i = 0; i < 2 * V; ++i) {
-                const float y = fabsf(x[p][i]);
-                if (ln.live[i / V] && y < INFINITY) top = fmaxf(top, y);
+            for (int i = 0; i < V; ++i) {
+                const float y = fabsf(x[p][i].x), z = fabsf(x[p][i].y);
+                if (ln.live[i / (V / 2)] && y < INFINITY) top = fmaxf(top, y);
+                if (ln.live[i / (V / 2)] && z < INFINITY) top = fmaxf(top, z);
             }
         }
     }
@@ -118,8 +130,8 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit, int 
             uint32_t w[V / 4];
 #pragma unroll
             for (int i = 0; i < V / 4; ++i) {
-                const float* y = &x[p][c * V + 4 * i];
-                w[i] = kv8_codes(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+                const float2 y = x[p][c * (V / 2) + 2 * i], z = x[p][c * (V / 2) + 2 * i + 1];
+                w[i] = kv8_codes(y.x * inv, y.y * inv, z.x * inv, z.y * inv);
             }
             uint8_t* dst = codes + r * a.rs + ln.c[c] * V;
             if constexpr (V == 8)

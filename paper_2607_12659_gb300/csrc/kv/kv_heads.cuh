@@ -61,96 +61,130 @@ struct HeadLane {
     }
 };
 
+// Two fp32 numbers by one instruction.
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+    uint64_t r, a = *reinterpret_cast<uint64_t*>(&x), b = *reinterpret_cast<uint64_t*>(&y);
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+    uint64_t r, a = *reinterpret_cast<uint64_t*>(&x), b = *reinterpret_cast<uint64_t*>(&y), c = *reinterpret_cast<uint64_t*>(&z);
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return *reinterpret_cast<float2*>(&r);
+}
+
 __device__ __forceinline__ float group_sum(float x, int lanes_log2) {
     for (int i = 0; i < lanes_log2; ++i) x += __shfl_xor_sync(0xffffffffu, x, 1 << i);
     return x;
 }
 
-// The factors (first, second) that make a head's elements x (those of one lane) x / sqrt(mean(x^2) + eps). Of heads whose squares
-// pass fp32's range the first is 2^-70, else it is 1. Every lane of the warp calls.
+// Makes a head's elements x (those of one lane) x / sqrt(mean(x^2) + eps); returns the factors that did it, one after the other. Of heads
+// whose squares pass fp32's range the first is 2^-70, else it is 1. Every lane of the warp calls.
 template <int N>
-__device__ __forceinline__ float2 head_norm(const float (&x)[N], int D, float eps, int lanes_log2) {
-    float s = 0.f;
+__device__ __forceinline__ float2 head_norm(float2 (&x)[N], int D, float eps, int lanes_log2) {
+    float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) s = fmaf(x[i], x[i], s);
-    s = group_sum(s, lanes_log2);
+    for (int i = 0; i < N; ++i) s2 = fma2(x[i], x[i], s2);
+    const float s = group_sum(s2.x + s2.y, lanes_log2);
     float2 r = make_float2(1.f, 1.f / sqrtf(s / (float)D + eps));
     if (__any_sync(0xffffffffu, s > 1e38f)) {
         float z = 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) z = fmaf(x[i] * 0x1p-70f, x[i] * 0x1p-70f, z);
+        for (int i = 0; i < N; ++i) {
+            const float2 y = make_float2(x[i].x * 0x1p-70f, x[i].y * 0x1p-70f);
+            z = fmaf(y.x, y.x, fmaf(y.y, y.y, z));
+            if (s > 1e38f) x[i] = y;
+        }
         z = group_sum(z, lanes_log2);
         if (s > 1e38f) r = make_float2(0x1p-70f, 1.f / sqrtf(z / (float)D));   // (eps is less than a rounding here)
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = mul2(x[i], make_float2(r.y, r.y));
     return r;
 }
 
+// Pairs of a chunk (half layout: of two).
+template <typename E, int MODE>
+constexpr int pairs_of_chunk() { return MODE == RM_HALF ? Chunk<E>::V : MODE == RM_INTER ? Chunk<E>::V / 2 : 1; }
+
 // One lane's part of a head, normalised if the call asks for it and coded. weight(i) gives the norm's weights of the lane's elements
-// 4 i .., other(d) that of element d; `head` is where it was loaded from, unwritten so far; rot(pair) gives (cos, sin)
-// times m. Every lane of the warp calls.
+// 4 i .., other(d) that of element d; `head` is where it was loaded from, unwritten so far; rot(q, c, s) gives cosines and sines
+// times m of the pairs of chunk q. Every lane of the warp calls.
 template <typename E, int MODE, typename Weight, typename Other, typename Rot>
 __device__ __forceinline__ void code_head(const HeadLane<E, MODE>& ln, const HeadArgs& a, const E* head, bool in,
                                           const uint4 (&raw)[2], const Weight& weight, const Other& other, const Rot& rot,
-                                          float (&y)[2 * Chunk<E>::V]) {
-    const bool norm = a.norm;
-    constexpr int V = Chunk<E>::V;
-    float x[2 * V];
-    {
-        float p[2][V];
-        Chunk<E>::unpack(raw[0], p[0]);
-        Chunk<E>::unpack(raw[1], p[1]);
+                                          float2 (&x)[Chunk<E>::V]) {
+    constexpr int V = Chunk<E>::V, PC = pairs_of_chunk<E, MODE>();
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) x[i] = p[i / V][i % V];
+    for (int c = 0; c < 2; ++c) {
+        float p[V];
+        Chunk<E>::unpack(raw[c], p);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) x[c * (V / 2) + i] = make_float2(p[2 * i], p[2 * i + 1]);
     }
     float2 r = make_float2(1.f, 1.f);
-    if (norm) {
+    if (a.norm) {
         r = head_norm(x, a.D, a.eps, a.lanes_log2);
 #pragma unroll
-        for (int i = 0; i < 2 * V; i += 4) {
-            const float4 w = weight(i / 4);
-            x[i] = x[i] * r.x * r.y * w.x;
-            x[i + 1] = x[i + 1] * r.x * r.y * w.y;
-            x[i + 2] = x[i + 2] * r.x * r.y * w.z;
-            x[i + 3] = x[i + 3] * r.x * r.y * w.w;
+        for (int i = 0; i < V; i += 2) {
+            const float4 w = weight(i / 2);
+            x[i] = mul2(x[i], make_float2(w.x, w.y));
+            x[i + 1] = mul2(x[i + 1], make_float2(w.z, w.w));
         }
     }
     const int half = a.dim / 2;
-    if (MODE == RM_HALF && ln.pair) {
+    if constexpr (MODE == RM_HALF) {
+        if (ln.pair) {
+            float c[PC], s[PC];
+            rot(ln.c[0], c, s);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float2 c = rot(ln.c[0] * V + i);
-            y[i] = x[i] * c.x - x[V + i] * c.y;
-            y[V + i] = x[V + i] * c.x + x[i] * c.y;
+            for (int i = 0; i < V / 2; ++i) {
+                const float2 c2 = make_float2(c[2 * i], c[2 * i + 1]), s2 = make_float2(s[2 * i], s[2 * i + 1]);
+                const float2 n2 = make_float2(-s2.x, -s2.y), x1 = x[i], x2 = x[V / 2 + i];
+                x[i] = fma2(x1, c2, mul2(x2, n2));
+                x[V / 2 + i] = fma2(x2, c2, mul2(x1, s2));
+            }
         }
-    } else if (MODE == RM_INTER) {
+    } else if constexpr (MODE == RM_INTER) {
 #pragma unroll
-        for (int i = 0; i < 2 * V; i += 2) {
-            const int p = (ln.c[i / V] * V + i % V) / 2;
-            const bool turn = p < half && ln.live[i / V];
-            const float2 c = turn ? rot(p) : make_float2(1.f, 0.f);
-            y[i] = turn ? x[i] * c.x - x[i + 1] * c.y : x[i];
-            y[i + 1] = turn ? x[i + 1] * c.x + x[i] * c.y : x[i + 1];
+        for (int k = 0; k < 2; ++k) {
+            if (!ln.live[k] || ln.c[k] * PC >= half) continue;
+            float c[PC], s[PC];
+            rot(ln.c[k], c, s);
+#pragma unroll
+            for (int i = 0; i < PC; ++i) {
+                float2& z = x[k * PC + i];
+                const float2 y = fma2(z, make_float2(c[i], c[i]), mul2(make_float2(z.y, z.x), make_float2(-s[i], s[i])));
+                if (ln.c[k] * PC + i < half) z = y;   // (the last chunk may be coded in part)
+            }
         }
-    } else if (MODE == RM_SCALAR) {
+    } else if constexpr (MODE == RM_SCALAR) {
         // A pair's other element is another lane's: read again, before any lane writes.
 #pragma unroll
         for (int i = 0; i < 2 * V; ++i) {
             const int d = ln.c[i / V] * V + i % V;
-            const bool turn = d < a.dim && ln.live[i / V] && in;
-            y[i] = x[i];
-            if (turn) {
+            float& y = i & 1 ? x[i / 2].y : x[i / 2].x;
+            if (d < a.dim && ln.live[i / V] && in) {
                 const int o = d < half ? d + half : d - half;
                 float z = to_f(head[o]);
-                if (norm) z = z * r.x * r.y * other(o);
-                const float2 c = rot(d < half ? d : o);
-                y[i] = d < half ? x[i] * c.x - z * c.y : x[i] * c.x + z * c.y;
+                if (a.norm) z = z * r.x * r.y * other(o);
+                float c[1], s[1];
+                rot(min(d, o), c, s);
+                y = d < half ? y * c[0] - z * s[0] : y * c[0] + z * s[0];
             }
         }
         __syncwarp();
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2 * V; ++i) y[i] = x[i];
     }
+}
+
+// Elements of a lane's chunk c, rounded to E.
+template <typename E>
+__device__ __forceinline__ uint4 pack_chunk(const float2 (&x)[Chunk<E>::V], int c) {
+    constexpr int V = Chunk<E>::V;
+    float z[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = i & 1 ? x[c * (V / 2) + i / 2].y : x[c * (V / 2) + i / 2].x;
+    return Chunk<E>::pack(z);
 }
 
 constexpr int CT_TOKENS = 4;    // most tokens of a task
@@ -167,7 +201,7 @@ struct CodeTokens {
 };
 
 struct CodeSmem {
-    float2 table[2][CT_TOKENS][AP_MAX_PAIRS + 8];
+    float table[2][CT_TOKENS][2][AP_MAX_PAIRS + 8];   // cosines and sines of the tokens of this task and the last
     float4 weight[2][4][32];          // of queries and keys: elements 4 i .. of each lane's of a group
     int2 token[CT_RUN][CT_TOKENS];    // (row, position)
 };
@@ -175,52 +209,60 @@ struct CodeSmem {
 // Takes tasks first, first + step, .. of a call. Their heads are copied asynchronously into shared memory, each thread's chunks
 // into places of its own, two tasks ahead of the one whose sines, cosines and norms are computed; a table of those of a task's tokens
 // serves all its heads. place(token) is the row that takes it, negative: padding; at(token, row) its place in the cache (element
-// offset). A table is laid out so that the lanes of a group, which read the same pair of consecutive chunks, read side by side.
+// offset). In a table, up to four pairs of a chunk lie together, and those of the next chunk, which the next lane reads, behind them.
 template <typename E, int MODE, typename Place, typename At>
 __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens& ct, CodeSmem& sm, uint4* stage, int first, int step,
                                             E* ck, E* cv, long long hs, const Place& place, const At& at) {
-    constexpr int V = Chunk<E>::V, PC = MODE == RM_HALF ? V : MODE == RM_INTER ? V / 2 : 1;
+    constexpr int V = Chunk<E>::V, PC = pairs_of_chunk<E, MODE>(), PV = PC < 4 ? PC : 4;
     const int t = threadIdx.x, nth = blockDim.x, half = a.dim / 2, chunks = (half + PC - 1) / PC;
     const int groups = nth >> a.lanes_log2, grp = t >> a.lanes_log2, u = t & ((1 << a.lanes_log2) - 1), n = a.batch * a.tokens;
     const HeadLane<E, MODE> ln(u, a.D, a.dim);
-    auto entry = [&](int p) { return p % PC * chunks + p / PC; };
-    auto slot = [&](int k, int p, int c) { return ((k % CT_STAGES * ct.passes + p) * 2 + c) * nth + t; };
-    struct Task {
-        int tok0, nt, r0, rows;   // tokens; rows r0 .. rows - 1 of (token, head)
+    auto entry = [&](int p) { return (p % PC / PV * chunks + p / PC) * PV + p % PV; };
+    const uint32_t mine = ptx::smem_u32(stage) + 16 * t;
+    auto slot = [&](int k, int p, int c) { return ((k % CT_STAGES * ct.passes + p) * 2 + c) * nth; };
+    // The group's heads of a task, pass by pass: the same of every task where a task has whole tokens.
+    struct Unit {
+        int kind;          // 0 query, 1 key, 2 value, -1 none
+        int i;             // token of the task
+        const E* src;      // of a task that begins with token 0
+        long long stride;
+        E* dst;            // without the token of a query, or the row of a key or value
+    } un[CT_PASSES];
+    auto set_units = [&](int part) {
+#pragma unroll
+        for (int p = 0; p < CT_PASSES; ++p) {
+            const int r = (part * ct.passes + p) * groups + grp;
+            uint32_t h;
+            Unit& x = un[p];
+            x.i = (int)ct.by_heads.div((uint32_t)r, h);
+            int hd = (int)h;
+            x.kind = p >= ct.passes || x.i >= ct.tt ? -1 : hd < a.H ? 0 : hd < a.H + a.K ? 1 : 2;
+            hd -= x.kind == 1 ? a.H : x.kind == 2 ? a.H + a.K : 0;
+            x.stride = x.kind == 1 ? a.k_stride : x.kind == 2 ? a.v_stride : a.q_stride;
+            x.src = static_cast<const E*>(x.kind == 1 ? a.k : x.kind == 2 ? a.v : a.q) + x.i * x.stride + hd * a.D;
+            x.dst = x.kind == 0 ? static_cast<E*>(a.q_out) + ((long long)x.i * a.H + hd) * a.D : (x.kind == 1 ? ck : cv) + hd * hs;
+        }
     };
-    auto task_of = [&](int k) {   // the run's k-th
+    set_units(0);
+    // Of the run's k-th task: its first token and tokens, and its units.
+    auto open = [&](int k, int& tok0) {
         uint32_t part;
-        Task x;
-        x.tok0 = (int)ct.by_parts.div((uint32_t)(first + k * step), part) * ct.tt;
-        x.nt = min(ct.tt, n - x.tok0);
-        x.r0 = (int)part * ct.passes * groups;
-        x.rows = min(x.nt * ct.heads, x.r0 + ct.passes * groups);
-        return x;
-    };
-    // A row's token of the task and head.
-    auto head_of = [&](int r, int& i) {
-        uint32_t h;
-        i = (int)ct.by_heads.div((uint32_t)r, h);
-        return (int)h;
-    };
-    auto source = [&](long long tok, int hd) {
-        return hd < a.H ? static_cast<const E*>(a.q) + tok * a.q_stride + hd * a.D
-                        : hd < a.H + a.K ? static_cast<const E*>(a.k) + tok * a.k_stride + (hd - a.H) * a.D
-                                         : static_cast<const E*>(a.v) + tok * a.v_stride + (hd - a.H - a.K) * a.D;
+        tok0 = (int)ct.by_parts.div((uint32_t)(first + k * step), part) * ct.tt;
+        if (ct.parts > 1) set_units((int)part);
+        return min(ct.tt, n - tok0);
     };
     auto fetch = [&](int k, int count, bool known) {
         if (k < count) {
-            const Task x = task_of(k);
-            for (int p = 0; p < ct.passes; ++p) {
-                const int r = x.r0 + p * groups + grp;
-                if (r >= x.rows) break;
-                int i;
-                const int hd = head_of(r, i);
-                if (known && sm.token[k][i].x < 0) continue;
-                const E* src = source(x.tok0 + i, hd);
+            int tok0;
+            const int nt = open(k, tok0);
+#pragma unroll
+            for (int p = 0; p < CT_PASSES; ++p) {
+                const Unit& x = un[p];
+                if (x.kind < 0 || x.i >= nt || (known && sm.token[k][x.i].x < 0)) continue;
+                const E* src = x.src + tok0 * x.stride;
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
-                    if (ln.live[c]) ptx::cp_async_16(ptx::smem_u32(stage + slot(k, p, c)), src + ln.c[c] * V, true);
+                    if (ln.live[c]) ptx::cp_async_16(mine + 16 * slot(k, p, c), src + ln.c[c] * V, true);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -231,9 +273,8 @@ __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens&
         if (begin) fetch(0, count, false);   // the first task's heads on their way beside its rows
         __syncthreads();                     // the last run's tokens have been read
         for (int e = t; e < count * ct.tt; e += nth) {
-            const int k = e / ct.tt, i = e - k * ct.tt;
-            const Task x = task_of(k);
-            if (i < x.nt) sm.token[k][i] = make_int2(place(x.tok0 + i), a.position[x.tok0 + i]);
+            const int k = e / ct.tt, tok = (int)ct.by_parts.div((uint32_t)(first + k * step)) * ct.tt + e - k * ct.tt;
+            if (tok < n) sm.token[k][e - k * ct.tt] = make_int2(place(tok), a.position[tok]);
         }
         if (begin && a.norm)
             for (int e = t; e < 2 * (V / 2) << a.lanes_log2; e += nth) {
@@ -248,46 +289,66 @@ __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens&
         fetch(1, count, true);
         for (int k = 0; k < count; ++k) {
             fetch(k + 2, count, true);
-            const Task x = task_of(k);
+            int tok0;
+            const int nt = open(k, tok0);
             turn ^= 1;   // the other table may still be read; this one's readers are past the last barrier
             if (MODE != RM_NONE) {
-                for (int e = t; e < x.nt * half; e += nth) {
+                for (int e = t; e < nt * half; e += nth) {
                     const int i = e / half, p = e - i * half;
-                    if (sm.token[k][i].x >= 0) sm.table[turn][i][entry(p)] = phase_near(sm.token[k][i].y, a.turns[p], a.m);
+                    if (sm.token[k][i].x < 0) continue;
+                    const float2 c = phase_near(sm.token[k][i].y, a.turns[p], a.m);
+                    sm.table[turn][i][0][entry(p)] = c.x;
+                    sm.table[turn][i][1][entry(p)] = c.y;
                 }
                 __syncthreads();
             }
             asm volatile("cp.async.wait_group 2;" ::: "memory");
-            for (int p = 0; p < ct.passes; ++p) {
-                if (x.r0 + p * groups >= x.rows) break;   // (the same for the block)
-                const int r = x.r0 + p * groups + grp;
-                int i;
-                int hd = head_of(min(r, x.rows - 1), i);
-                const bool live = r < x.rows && sm.token[k][i].x >= 0;
-                if (!__any_sync(0xffffffffu, live)) continue;
-                const bool value = hd >= a.H + a.K, key = !value && hd >= a.H;
+#pragma unroll
+            for (int p = 0; p < CT_PASSES; ++p) {
+                if (p >= ct.passes) break;
+                const Unit& x = un[p];
+                const int2 token = x.kind >= 0 && x.i < nt ? sm.token[k][x.i] : make_int2(-1, 0);
+                const bool live = token.x >= 0, coded = live && x.kind != 2;
                 uint4 raw[2];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) raw[c] = live && ln.live[c] ? stage[slot(k, p, c)] : make_uint4(0, 0, 0, 0);
-                float y[2 * V];
-                auto rot = [&](int pr) { return sm.table[turn][i][entry(pr)]; };
-                auto weight = [&](int e4) { return sm.weight[key][e4][u]; };
-                auto other = [&](int d) { return (key ? a.k_weight : a.q_weight) ? (key ? a.k_weight : a.q_weight)[d] : 1.f; };
-                const E* src = source(x.tok0 + i, hd);
-                code_head<E, MODE>(ln, a, src, live && !value, raw, weight, other, rot, y);
-                if (!live) continue;
-                const int row = sm.token[k][i].x;
-                const long long tok = x.tok0 + i;
-                E* dst = hd < a.H ? static_cast<E*>(a.q_out) + (tok * a.H + hd) * a.D
-                                  : (value ? cv + (hd - a.H - a.K) * hs : ck + (hd - a.H) * hs) + at(tok, row);
+                for (int c = 0; c < 2; ++c) raw[c] = live && ln.live[c] ? stage[slot(k, p, c) + t] : make_uint4(0, 0, 0, 0);
+                if (__any_sync(0xffffffffu, coded)) {
+                    const int i = live ? x.i : 0;
+                    float2 y[V];
+                    auto rot = [&](int q, float (&c)[PC], float (&s)[PC]) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if (!ln.live[c]) continue;
-                    float z[V];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) z[e] = y[c * V + e];
-                    *reinterpret_cast<uint4*>(dst + ln.c[c] * V) = value ? raw[c] : Chunk<E>::pack(z);
+                        for (int e = 0; e < PC; e += PV) {
+                            const float *fc = &sm.table[turn][i][0][(e / PV * chunks + q) * PV], *fs = &sm.table[turn][i][1][(e / PV * chunks + q) * PV];
+                            if constexpr (PV == 4) {
+                                const float4 c4 = *reinterpret_cast<const float4*>(fc), s4 = *reinterpret_cast<const float4*>(fs);
+                                c[e] = c4.x, c[e + 1] = c4.y, c[e + 2] = c4.z, c[e + 3] = c4.w;
+                                s[e] = s4.x, s[e + 1] = s4.y, s[e + 2] = s4.z, s[e + 3] = s4.w;
+                            } else if constexpr (PV == 2) {
+                                const float2 c2 = *reinterpret_cast<const float2*>(fc), s2 = *reinterpret_cast<const float2*>(fs);
+                                c[e] = c2.x, c[e + 1] = c2.y;
+                                s[e] = s2.x, s[e + 1] = s2.y;
+                            } else {
+                                c[e] = *fc;
+                                s[e] = *fs;
+                            }
+                        }
+                    };
+                    auto weight = [&](int e4) { return sm.weight[x.kind == 1][e4][u]; };
+                    auto other = [&](int d) {
+                        const float* w = x.kind == 1 ? a.k_weight : a.q_weight;
+                        return w ? w[d] : 1.f;
+                    };
+                    code_head<E, MODE>(ln, a, x.src + tok0 * x.stride, coded, raw, weight, other, rot, y);
+                    if (coded) {
+                        raw[0] = pack_chunk<E>(y, 0);
+                        raw[1] = pack_chunk<E>(y, 1);
+                    }
                 }
+                if (!live) continue;
+                E* dst = x.dst + (x.kind == 0 ? (long long)tok0 * a.H * a.D : at(tok0 + x.i, token.x));
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (ln.live[c]) *reinterpret_cast<uint4*>(dst + ln.c[c] * V) = raw[c];
             }
         }
         ptx::cp_async_wait_all();   // (empty groups)
