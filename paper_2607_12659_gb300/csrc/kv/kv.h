@@ -70,8 +70,6 @@ jpi_status kv_append_prepare();
 jpi_status launch_kv_append(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
                             const void* v, long long v_stride, const int* position, const int* row, int batch,
                             int tokens, void* q_out, const jpi_kv_cache* cache, cudaStream_t st);
-jpi_status kv_append_normed_prepare(const jpi_kv_handle* h);
-jpi_status kv8_append_prepare(const jpi_kv_handle* h);
 jpi_status launch_kv_append_normed(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
                                    const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position, const int* row,
                                    int batch, int tokens, void* q_out, const jpi_kv_cache* cache, cudaStream_t st);

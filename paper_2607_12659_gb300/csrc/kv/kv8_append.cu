@@ -160,9 +160,9 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit, int 
 
 template <typename E, int MODE>
 __global__ void __launch_bounds__(CT_THREADS) k_kv8_append(const __grid_constant__ Append8Args a) {
-    __shared__ CodeSmem sm;
+    __shared__ CodeWeights weights;
     __shared__ float most[CT_THREADS / 32];
-    extern __shared__ __align__(16) uint4 stage[];
+    __shared__ __align__(16) CodeTable table[CT_THREADS / 32];
     if (blockIdx.x < a.blocks) {
         const int team = threadIdx.x / (32 * a.team);
         const uint32_t unit = blockIdx.x * a.teams + team;
@@ -175,28 +175,21 @@ __global__ void __launch_bounds__(CT_THREADS) k_kv8_append(const __grid_constant
         return (int)t < span.y - span.x ? 0 : -1;
     };
     auto at = [](long long, int) { return 0ll; };
-    code_tokens<E, MODE>(a.h, a.ct, sm, stage, blockIdx.x - a.blocks, gridDim.x - a.blocks, static_cast<E*>(nullptr), static_cast<E*>(nullptr), 0, place, at);
+    load_weights<E, MODE>(a.h, weights);
+    __syncthreads();
+    code_tokens<E, MODE>(a.h, a.ct, weights, table[threadIdx.x >> 5], (blockIdx.x - a.blocks) * (blockDim.x >> 5) + (threadIdx.x >> 5),
+                         (gridDim.x - a.blocks) * (blockDim.x >> 5), static_cast<E*>(nullptr), static_cast<E*>(nullptr), 0, place, at);
 }
 
 template <typename E>
-jpi_status launch(const Append8Args& a, int mode, unsigned blocks, int threads, size_t smem, cudaStream_t st) {
+jpi_status launch(const Append8Args& a, int mode, unsigned blocks, int threads, cudaStream_t st) {
     return kv_start(mode == RM_NONE ? k_kv8_append<E, RM_NONE>
                                     : mode == RM_HALF ? k_kv8_append<E, RM_HALF>
                                                       : mode == RM_INTER ? k_kv8_append<E, RM_INTER> : k_kv8_append<E, RM_SCALAR>,
-                    dim3(blocks), threads, smem, false, st, a);
-}
-
-template <typename E>
-jpi_status prepare_type() {
-    const int most = CT_STAGES * CT_PASSES * 2 * CT_THREADS * 16;
-    for (auto* kernel : {k_kv8_append<E, RM_NONE>, k_kv8_append<E, RM_HALF>, k_kv8_append<E, RM_INTER>, k_kv8_append<E, RM_SCALAR>})
-        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
-    return JPI_OK;
+                    dim3(blocks), threads, 0, false, st, a);
 }
 
 }  // namespace
-
-jpi_status kv8_append_prepare(const jpi_kv_handle* h) { return h->bf16 ? prepare_type<__nv_bfloat16>() : prepare_type<float>(); }
 
 jpi_status launch_kv8_append(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
                              const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position, const int* start,
@@ -219,8 +212,8 @@ jpi_status launch_kv8_append(const jpi_kv_handle* h, const void* q, long long q_
         a.h.k_weight = norm->k_weight;
         a.h.eps = norm->eps;
     }
-    int threads;
-    const int mode = plan_code_tokens(h, a.h, a.ct, 0, &threads);
+    int threads = 128;
+    const int mode = plan_code_tokens(h, a.h, a.ct, 0);
     a.K = h->K;
     a.start = start;
     a.count = count;
@@ -243,7 +236,6 @@ jpi_status launch_kv8_append(const jpi_kv_handle* h, const void* q, long long q_
         const int rows = std::min(tokens, cache->block);
         a.team = 1;
         while (a.team < CT_THREADS / 32 && (a.team * 32 >> a.h.lanes_log2) * 2 < rows) a.team *= 2;
-        if (!q) threads = std::max(64, a.team * 32);
         threads = std::max(threads, a.team * 32);
         a.teams = threads / 32 / a.team;
         a.blocks = (uint32_t)((units + a.teams - 1) / a.teams);
@@ -255,9 +247,8 @@ jpi_status launch_kv8_append(const jpi_kv_handle* h, const void* q, long long q_
         return JPI_ERR_SHAPE;
     }
     a.units = (uint32_t)units;
-    const size_t smem = q ? code_smem(a.ct, threads) : 0;
-    const unsigned blocks = a.blocks + (q ? (unsigned)std::min<long long>(a.ct.tasks, code_blocks(h, smem, threads)) : 0);
-    return h->bf16 ? launch<__nv_bfloat16>(a, mode, blocks, threads, smem, st) : launch<float>(a, mode, blocks, threads, smem, st);
+    const unsigned blocks = a.blocks + (q ? code_blocks(h, a.ct, threads, 512 / threads) : 0);
+    return h->bf16 ? launch<__nv_bfloat16>(a, mode, blocks, threads, st) : launch<float>(a, mode, blocks, threads, st);
 }
 
 }  // namespace jpi

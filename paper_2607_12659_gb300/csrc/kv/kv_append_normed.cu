@@ -2,7 +2,7 @@
 //
 //   y = rope(x / sqrt(mean(x^2) + eps) * w)
 //
-// Bound by memory: every element is read and written once. Blocks stay and take tasks of a few tokens in turn, whose heads are
+// Bound by memory: every element is read and written once. Warps stay and take tokens in turn, whose heads are
 // held by groups of lanes (kv_heads.cuh).
 
 #include "kv_heads.cuh"
@@ -19,38 +19,32 @@ struct NormedArgs {
     int rows;
 };
 
+constexpr int AN_THREADS = 128, AN_BLOCKS = 8;   // of a block; blocks of an SM
+
 template <typename E, int MODE>
-__global__ void __launch_bounds__(CT_THREADS) k_kv_append_normed(const __grid_constant__ NormedArgs a) {
-    __shared__ CodeSmem sm;
-    extern __shared__ __align__(16) uint4 stage[];
+__global__ void __launch_bounds__(AN_THREADS, AN_BLOCKS) k_kv_append_normed(const __grid_constant__ NormedArgs a) {
+    __shared__ CodeWeights weights;
+    __shared__ __align__(16) CodeTable table[AN_THREADS / 32];
     auto place = [&](int tok) {
         const int r = a.row[tok];
         return r < a.rows ? r : -1;
     };
     auto at = [&](long long tok, int row) { return (long long)a.h.by_tokens.div((uint32_t)tok) * a.cs + row * a.rs; };
-    code_tokens<E, MODE>(a.h, a.ct, sm, stage, blockIdx.x, gridDim.x, static_cast<E*>(a.ck), static_cast<E*>(a.cv), a.hs, place, at);
+    load_weights<E, MODE>(a.h, weights);
+    __syncthreads();
+    code_tokens<E, MODE>(a.h, a.ct, weights, table[threadIdx.x >> 5], blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5),
+                         gridDim.x * (blockDim.x >> 5), static_cast<E*>(a.ck), static_cast<E*>(a.cv), a.hs, place, at);
 }
 
 template <typename E>
-jpi_status launch(const jpi_kv_handle* h, const NormedArgs& a, int mode, int threads, cudaStream_t st) {
+jpi_status launch(const jpi_kv_handle* h, const NormedArgs& a, int mode, cudaStream_t st) {
     auto* const kernel = mode == RM_NONE ? k_kv_append_normed<E, RM_NONE>
                                          : mode == RM_HALF ? k_kv_append_normed<E, RM_HALF>
                                                            : mode == RM_INTER ? k_kv_append_normed<E, RM_INTER> : k_kv_append_normed<E, RM_SCALAR>;
-    const size_t smem = code_smem(a.ct, threads);
-    return kv_start(kernel, dim3((unsigned)std::min<long long>(a.ct.tasks, code_blocks(h, smem, threads))), threads, smem, false, st, a);
-}
-
-template <typename E>
-jpi_status prepare_type() {
-    const int most = CT_STAGES * CT_PASSES * 2 * CT_THREADS * 16;
-    for (auto* kernel : {k_kv_append_normed<E, RM_NONE>, k_kv_append_normed<E, RM_HALF>, k_kv_append_normed<E, RM_INTER>, k_kv_append_normed<E, RM_SCALAR>})
-        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
-    return JPI_OK;
+    return kv_start(kernel, dim3(code_blocks(h, a.ct, AN_THREADS, AN_BLOCKS)), AN_THREADS, 0, false, st, a);
 }
 
 }  // namespace
-
-jpi_status kv_append_normed_prepare(const jpi_kv_handle* h) { return h->bf16 ? prepare_type<__nv_bfloat16>() : prepare_type<float>(); }
 
 jpi_status launch_kv_append_normed(const jpi_kv_handle* h, const void* q, long long q_stride, const void* k, long long k_stride,
                                    const void* v, long long v_stride, const jpi_kv_norm* norm, const int* position, const int* row,
@@ -82,9 +76,8 @@ jpi_status launch_kv_append_normed(const jpi_kv_handle* h, const void* q, long l
         a.hs = cache->head_stride;
         a.rows = cache->rows;
     }
-    int threads;
-    const int mode = plan_code_tokens(h, a.h, a.ct, v ? h->K : 0, &threads);
-    return h->bf16 ? launch<__nv_bfloat16>(h, a, mode, threads, st) : launch<float>(h, a, mode, threads, st);
+    const int mode = plan_code_tokens(h, a.h, a.ct, v ? h->K : 0);
+    return h->bf16 ? launch<__nv_bfloat16>(h, a, mode, st) : launch<float>(h, a, mode, st);
 }
 
 }  // namespace jpi

@@ -27,7 +27,7 @@ struct HeadArgs {
     float m;
     bool norm;
     const float *q_weight, *k_weight;   // NULL: ones
-    float eps;
+    float eps, inv_d;            // 1 / D
     int lanes_log2;              // G
 };
 
@@ -78,15 +78,21 @@ __device__ __forceinline__ float group_sum(float x, int lanes_log2) {
     return x;
 }
 
+// 1 / sqrt(v): the hardware's approximation (2^-22) and one step of Newton's for the equation 1 / r^2 = v.
+__device__ __forceinline__ float inverse_root(float v) {
+    const float r = rsqrtf(v);
+    return v < INFINITY ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
+}
+
 // Makes a head's elements x (those of one lane) x / sqrt(mean(x^2) + eps); returns the factors that did it, one after the other. Of heads
 // whose squares pass fp32's range the first is 2^-70, else it is 1. Every lane of the warp calls.
 template <int N>
-__device__ __forceinline__ float2 head_norm(float2 (&x)[N], int D, float eps, int lanes_log2) {
+__device__ __forceinline__ float2 head_norm(float2 (&x)[N], float inv_d, float eps, int lanes_log2) {
     float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < N; ++i) s2 = fma2(x[i], x[i], s2);
     const float s = group_sum(s2.x + s2.y, lanes_log2);
-    float2 r = make_float2(1.f, 1.f / sqrtf(s / (float)D + eps));
+    float2 r = make_float2(1.f, inverse_root(fmaf(s, inv_d, eps)));
     if (__any_sync(0xffffffffu, s > 1e38f)) {
         float z = 0.f;
 #pragma unroll
@@ -96,7 +102,7 @@ __device__ __forceinline__ float2 head_norm(float2 (&x)[N], int D, float eps, in
             if (s > 1e38f) x[i] = y;
         }
         z = group_sum(z, lanes_log2);
-        if (s > 1e38f) r = make_float2(0x1p-70f, 1.f / sqrtf(z / (float)D));   // (eps is less than a rounding here)
+        if (s > 1e38f) r = make_float2(0x1p-70f, inverse_root(z * inv_d));   // (eps is less than a rounding here)
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = mul2(x[i], make_float2(r.y, r.y));
@@ -124,7 +130,7 @@ __device__ __forceinline__ void code_head(const HeadLane<E, MODE>& ln, const Hea
     }
     float2 r = make_float2(1.f, 1.f);
     if (a.norm) {
-        r = head_norm(x, a.D, a.eps, a.lanes_log2);
+        r = head_norm(x, a.inv_d, a.eps, a.lanes_log2);
 #pragma unroll
         for (int i = 0; i < V; i += 2) {
             const float4 w = weight(i / 2);
@@ -187,138 +193,107 @@ __device__ __forceinline__ uint4 pack_chunk(const float2 (&x)[Chunk<E>::V], int 
     return Chunk<E>::pack(z);
 }
 
-constexpr int CT_TOKENS = 4;    // most tokens of a task
-constexpr int CT_PASSES = 4;    // most heads of a group of lanes in a task
-constexpr int CT_STAGES = 3;    // tasks in hand
-constexpr int CT_RUN = 16;      // tasks whose rows and positions are read together
-constexpr int CT_THREADS = 256;
+constexpr int CT_PASSES = 8;     // most heads of a group of lanes in a task
+constexpr int CT_THREADS = 256;  // most of a block
 
-// A call's tokens as tasks: `tt` tokens, or, of more heads than the groups of lanes hold in their passes, a part of one token's.
+// A call's tokens as tasks of single warps: a token, or, of more heads than a warp's groups of lanes take in their passes or in a call
+// that is waited for, a part of one.
 struct CodeTokens {
-    int tt, heads, passes;   // heads of a token: H queries, K keys, K values
+    int heads, passes;       // of a token: H queries, K keys, K values; of a group of lanes in a task
     int parts, tasks;        // tasks of a token, of the call
-    KvDiv by_heads, by_parts;
+    KvDiv by_parts;
 };
 
-struct CodeSmem {
-    float table[2][CT_TOKENS][2][AP_MAX_PAIRS + 8];   // cosines and sines of the tokens of this task and the last
-    float4 weight[2][4][32];          // of queries and keys: elements 4 i .. of each lane's of a group
-    int2 token[CT_RUN][CT_TOKENS];    // (row, position)
+// A warp's sines and cosines of its token, and a block's weights.
+struct CodeTable {
+    float v[2][AP_MAX_PAIRS + 8];
+};
+struct CodeWeights {
+    float4 v[2][4][32];      // of queries and keys: elements 4 i .. of each lane's of a group
 };
 
-// Takes tasks first, first + step, .. of a call. Their heads are copied asynchronously into shared memory, each thread's chunks
-// into places of its own, two tasks ahead of the one whose sines, cosines and norms are computed; a table of those of a task's tokens
-// serves all its heads. place(token) is the row that takes it, negative: padding; at(token, row) its place in the cache (element
-// offset). In a table, up to four pairs of a chunk lie together, and those of the next chunk, which the next lane reads, behind them.
+template <typename E, int MODE>
+__device__ __forceinline__ void load_weights(const HeadArgs& a, CodeWeights& w) {
+    constexpr int V = Chunk<E>::V;
+    if (a.norm)
+        for (int e = threadIdx.x; e < 2 * (V / 2) << a.lanes_log2; e += blockDim.x) {
+            const int lane = e & ((1 << a.lanes_log2) - 1), i = (e >> a.lanes_log2) % (V / 2), k = (e >> a.lanes_log2) / (V / 2);
+            const HeadLane<E, MODE> x(lane, a.D, a.dim);
+            const float* f = k ? a.k_weight : a.q_weight;
+            const int c = 4 * i / V, d = x.c[c] * V + 4 * i % V;
+            w.v[k][i][lane] = f && x.live[c] ? make_float4(f[d], f[d + 1], f[d + 2], f[d + 3]) : make_float4(1.f, 1.f, 1.f, 1.f);
+        }
+}
+
+// A warp's tasks first, first + step, .. of a call: a table of the token's sines and cosines serves all its heads; the next pass's
+// heads are on their way while one is coded. What bounds this on an SM is instructions, not bytes in flight, so that it wants many
+// warps that wait for nothing but themselves. (A block to four tokens with a table for all of them, its heads copied ahead through
+// shared memory: 4 prompts of 2048 tokens took 24 us, 46 thousand cycles an SM for 21 thousand instructions a scheduler.)
+// place(token) is the row that takes it, negative: padding; at(token, row) its place in the cache (element offset). In the table, up
+// to four pairs of a chunk lie together, and those of the next chunk, which the next lane reads, behind them.
 template <typename E, int MODE, typename Place, typename At>
-__device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens& ct, CodeSmem& sm, uint4* stage, int first, int step,
-                                            E* ck, E* cv, long long hs, const Place& place, const At& at) {
+__device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens& ct, const CodeWeights& weights, CodeTable& table,
+                                            int first, int step, E* ck, E* cv, long long hs, const Place& place, const At& at) {
     constexpr int V = Chunk<E>::V, PC = pairs_of_chunk<E, MODE>(), PV = PC < 4 ? PC : 4;
-    const int t = threadIdx.x, nth = blockDim.x, half = a.dim / 2, chunks = (half + PC - 1) / PC;
-    const int groups = nth >> a.lanes_log2, grp = t >> a.lanes_log2, u = t & ((1 << a.lanes_log2) - 1), n = a.batch * a.tokens;
+    const int lane = threadIdx.x & 31, half = a.dim / 2, chunks = (half + PC - 1) / PC;
+    const int per = 32 >> a.lanes_log2, u = lane & ((1 << a.lanes_log2) - 1);   // heads of a pass, lane of its head
     const HeadLane<E, MODE> ln(u, a.D, a.dim);
-    auto entry = [&](int p) { return (p % PC / PV * chunks + p / PC) * PV + p % PV; };
-    const uint32_t mine = ptx::smem_u32(stage) + 16 * t;
-    auto slot = [&](int k, int p, int c) { return ((k % CT_STAGES * ct.passes + p) * 2 + c) * nth; };
-    // The group's heads of a task, pass by pass: the same of every task where a task has whole tokens.
-    struct Unit {
-        int kind;          // 0 query, 1 key, 2 value, -1 none
-        int i;             // token of the task
-        const E* src;      // of a task that begins with token 0
-        long long stride;
-        E* dst;            // without the token of a query, or the row of a key or value
-    } un[CT_PASSES];
-    auto set_units = [&](int part) {
-#pragma unroll
-        for (int p = 0; p < CT_PASSES; ++p) {
-            const int r = (part * ct.passes + p) * groups + grp;
-            uint32_t h;
-            Unit& x = un[p];
-            x.i = (int)ct.by_heads.div((uint32_t)r, h);
-            int hd = (int)h;
-            x.kind = p >= ct.passes || x.i >= ct.tt ? -1 : hd < a.H ? 0 : hd < a.H + a.K ? 1 : 2;
-            hd -= x.kind == 1 ? a.H : x.kind == 2 ? a.H + a.K : 0;
-            x.stride = x.kind == 1 ? a.k_stride : x.kind == 2 ? a.v_stride : a.q_stride;
-            x.src = static_cast<const E*>(x.kind == 1 ? a.k : x.kind == 2 ? a.v : a.q) + x.i * x.stride + hd * a.D;
-            x.dst = x.kind == 0 ? static_cast<E*>(a.q_out) + ((long long)x.i * a.H + hd) * a.D : (x.kind == 1 ? ck : cv) + hd * hs;
-        }
+    const int mine = lane >> a.lanes_log2;
+    auto source = [&](long long tok, int hd) {
+        return hd < a.H ? static_cast<const E*>(a.q) + tok * a.q_stride + hd * a.D
+                        : hd < a.H + a.K ? static_cast<const E*>(a.k) + tok * a.k_stride + (hd - a.H) * a.D
+                                         : static_cast<const E*>(a.v) + tok * a.v_stride + (hd - a.H - a.K) * a.D;
     };
-    set_units(0);
-    // Of the run's k-th task: its first token and tokens, and its units.
-    auto open = [&](int k, int& tok0) {
+    uint4 next[2];
+    // Asks for the heads of the run's k-th task's pass p.
+    auto fetch = [&](int k, int p) {
         uint32_t part;
-        tok0 = (int)ct.by_parts.div((uint32_t)(first + k * step), part) * ct.tt;
-        if (ct.parts > 1) set_units((int)part);
-        return min(ct.tt, n - tok0);
+        const long long tok = ct.by_parts.div((uint32_t)(first + k * step), part);
+        const int hd = ((int)part * ct.passes + p) * per + mine;
+        ln.load(source(tok, hd), hd < ct.heads, next);
     };
-    auto fetch = [&](int k, int count, bool known) {
-        if (k < count) {
-            int tok0;
-            const int nt = open(k, tok0);
-#pragma unroll
-            for (int p = 0; p < CT_PASSES; ++p) {
-                const Unit& x = un[p];
-                if (x.kind < 0 || x.i >= nt || (known && sm.token[k][x.i].x < 0)) continue;
-                const E* src = x.src + tok0 * x.stride;
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (ln.live[c]) ptx::cp_async_16(mine + 16 * slot(k, p, c), src + ln.c[c] * V, true);
-            }
+    for (bool begin = true; first < ct.tasks; first += 32 * step, begin = false) {   // runs of 32 tasks
+        const int count = min(32, (ct.tasks - first + step - 1) / step);
+        if (begin) fetch(0, 0);   // beside the rows
+        int row = -1, position = 0;   // of the run's task `lane`
+        if (lane < count) {
+            const int tok = (int)ct.by_parts.div((uint32_t)(first + lane * step));
+            row = place(tok);
+            position = a.position[tok];
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    int turn = 0;
-    for (bool begin = true; first < ct.tasks; first += CT_RUN * step, begin = false) {
-        const int count = min(CT_RUN, (ct.tasks - first + step - 1) / step);
-        if (begin) fetch(0, count, false);   // the first task's heads on their way beside its rows
-        __syncthreads();                     // the last run's tokens have been read
-        for (int e = t; e < count * ct.tt; e += nth) {
-            const int k = e / ct.tt, tok = (int)ct.by_parts.div((uint32_t)(first + k * step)) * ct.tt + e - k * ct.tt;
-            if (tok < n) sm.token[k][e - k * ct.tt] = make_int2(place(tok), a.position[tok]);
-        }
-        if (begin && a.norm)
-            for (int e = t; e < 2 * (V / 2) << a.lanes_log2; e += nth) {
-                const int lane = e & ((1 << a.lanes_log2) - 1), i = (e >> a.lanes_log2) % (V / 2), k = (e >> a.lanes_log2) / (V / 2);
-                const HeadLane<E, MODE> x(lane, a.D, a.dim);
-                const float* w = k ? a.k_weight : a.q_weight;
-                const int c = 4 * i / V, d = x.c[c] * V + 4 * i % V;
-                sm.weight[k][i][lane] = w && x.live[c] ? make_float4(w[d], w[d + 1], w[d + 2], w[d + 3]) : make_float4(1.f, 1.f, 1.f, 1.f);
-            }
-        __syncthreads();
-        if (!begin) fetch(0, count, true);
-        fetch(1, count, true);
-        for (int k = 0; k < count; ++k) {
-            fetch(k + 2, count, true);
-            int tok0;
-            const int nt = open(k, tok0);
-            turn ^= 1;   // the other table may still be read; this one's readers are past the last barrier
+        uint32_t todo = __ballot_sync(0xffffffffu, row >= 0);   // without the padding
+        if (todo && !(begin && (todo & 1))) fetch(__ffs(todo) - 1, 0);
+        while (todo) {
+            const int k = __ffs(todo) - 1;
+            todo &= todo - 1;
+            const int r = __shfl_sync(0xffffffffu, row, k), pos = __shfl_sync(0xffffffffu, position, k);
+            uint32_t part;
+            const long long tok = ct.by_parts.div((uint32_t)(first + k * step), part);
             if (MODE != RM_NONE) {
-                for (int e = t; e < nt * half; e += nth) {
-                    const int i = e / half, p = e - i * half;
-                    if (sm.token[k][i].x < 0) continue;
-                    const float2 c = phase_near(sm.token[k][i].y, a.turns[p], a.m);
-                    sm.table[turn][i][0][entry(p)] = c.x;
-                    sm.table[turn][i][1][entry(p)] = c.y;
+                __syncwarp();   // the last task's table has been read
+                for (int p = lane; p < half; p += 32) {
+                    const float2 c = phase_near(pos, a.turns[p], a.m);
+                    const int e = (p % PC / PV * chunks + p / PC) * PV + p % PV;
+                    table.v[0][e] = c.x;
+                    table.v[1][e] = c.y;
                 }
-                __syncthreads();
+                __syncwarp();
             }
-            asm volatile("cp.async.wait_group 2;" ::: "memory");
-#pragma unroll
-            for (int p = 0; p < CT_PASSES; ++p) {
-                if (p >= ct.passes) break;
-                const Unit& x = un[p];
-                const int2 token = x.kind >= 0 && x.i < nt ? sm.token[k][x.i] : make_int2(-1, 0);
-                const bool live = token.x >= 0, coded = live && x.kind != 2;
-                uint4 raw[2];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) raw[c] = live && ln.live[c] ? stage[slot(k, p, c) + t] : make_uint4(0, 0, 0, 0);
+            const long long cache = at(tok, r);
+            const int hd0 = (int)part * ct.passes * per, passes = min(ct.passes, (ct.heads - hd0 + per - 1) / per);
+#pragma unroll 1
+            for (int p = 0; p < passes; ++p) {
+                const int hd = hd0 + p * per + mine;
+                const bool live = hd < ct.heads, value = hd >= a.H + a.K, key = !value && hd >= a.H, coded = live && !value;
+                uint4 raw[2] = {next[0], next[1]};
+                if (p + 1 < passes) fetch(k, p + 1);
+                else if (todo) fetch(__ffs(todo) - 1, 0);
                 if (__any_sync(0xffffffffu, coded)) {
-                    const int i = live ? x.i : 0;
                     float2 y[V];
                     auto rot = [&](int q, float (&c)[PC], float (&s)[PC]) {
 #pragma unroll
                         for (int e = 0; e < PC; e += PV) {
-                            const float *fc = &sm.table[turn][i][0][(e / PV * chunks + q) * PV], *fs = &sm.table[turn][i][1][(e / PV * chunks + q) * PV];
+                            const float *fc = &table.v[0][(e / PV * chunks + q) * PV], *fs = &table.v[1][(e / PV * chunks + q) * PV];
                             if constexpr (PV == 4) {
                                 const float4 c4 = *reinterpret_cast<const float4*>(fc), s4 = *reinterpret_cast<const float4*>(fs);
                                 c[e] = c4.x, c[e + 1] = c4.y, c[e + 2] = c4.z, c[e + 3] = c4.w;
@@ -333,30 +308,30 @@ __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens&
                             }
                         }
                     };
-                    auto weight = [&](int e4) { return sm.weight[x.kind == 1][e4][u]; };
+                    auto weight = [&](int e4) { return weights.v[key][e4][u]; };
                     auto other = [&](int d) {
-                        const float* w = x.kind == 1 ? a.k_weight : a.q_weight;
+                        const float* w = key ? a.k_weight : a.q_weight;
                         return w ? w[d] : 1.f;
                     };
-                    code_head<E, MODE>(ln, a, x.src + tok0 * x.stride, coded, raw, weight, other, rot, y);
+                    code_head<E, MODE>(ln, a, MODE == RM_SCALAR && coded ? source(tok, hd) : nullptr, coded, raw, weight, other, rot, y);
                     if (coded) {
                         raw[0] = pack_chunk<E>(y, 0);
                         raw[1] = pack_chunk<E>(y, 1);
                     }
                 }
                 if (!live) continue;
-                E* dst = x.dst + (x.kind == 0 ? (long long)tok0 * a.H * a.D : at(tok0 + x.i, token.x));
+                E* dst = hd < a.H ? static_cast<E*>(a.q_out) + (tok * a.H + hd) * a.D
+                                  : (value ? cv + (hd - a.H - a.K) * hs : ck + (hd - a.H) * hs) + cache;
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
                     if (ln.live[c]) *reinterpret_cast<uint4*>(dst + ln.c[c] * V) = raw[c];
             }
         }
-        ptx::cp_async_wait_all();   // (empty groups)
     }
 }
 
 // Fills in how a call is coded; a.q .. a.norm are the caller's. Returns the rotary mode.
-inline int plan_code_tokens(const jpi_kv_handle* h, HeadArgs& a, CodeTokens& ct, int values, int* threads) {
+inline int plan_code_tokens(const jpi_kv_handle* h, HeadArgs& a, CodeTokens& ct, int values) {
     const int V = h->bf16 ? 8 : 4;
     int mode = RM_NONE;
     a.D = h->D;
@@ -368,24 +343,22 @@ inline int plan_code_tokens(const jpi_kv_handle* h, HeadArgs& a, CodeTokens& ct,
     }
     a.by_tokens = KvDiv((uint32_t)a.tokens);
     a.lanes_log2 = head_lanes_log2(a.D, V, a.dim, mode);
+    a.inv_d = 1.f / (float)a.D;
     ct.heads = std::max(1, a.H + a.K + values);
-    ct.by_heads = KvDiv((uint32_t)ct.heads);
     const long long n = (long long)a.batch * a.tokens;
-    // Tokens of a task: as many as its passes hold, while there are two tasks an SM.
-    const int groups = CT_THREADS >> a.lanes_log2;
-    ct.tt = 1;
-    while (ct.tt < CT_TOKENS && 2 * ct.tt * ct.heads <= CT_PASSES * groups && n >= 4ll * ct.tt * h->num_sms) ct.tt *= 2;
-    ct.passes = std::min(CT_PASSES, (ct.tt * ct.heads + groups - 1) / groups);
-    ct.parts = (ct.tt * ct.heads + ct.passes * groups - 1) / (ct.passes * groups);
+    // A token's passes as evenly over tasks as their limit needs, or while there are not two tasks for each of an SM's schedulers.
+    const int per = 32 >> a.lanes_log2, all = (ct.heads + per - 1) / per;
+    ct.parts = (all + CT_PASSES - 1) / CT_PASSES;
+    while (ct.parts < all && n * ct.parts < 8ll * h->num_sms) ++ct.parts;
+    ct.passes = (all + ct.parts - 1) / ct.parts;
+    ct.parts = (all + ct.passes - 1) / ct.passes;
     ct.by_parts = KvDiv((uint32_t)ct.parts);
-    ct.tasks = (int)((n + ct.tt - 1) / ct.tt * ct.parts);
-    *threads = ct.parts > 1 || ct.passes > 1 ? CT_THREADS : std::max(64, ((ct.tt * ct.heads << a.lanes_log2) + 31) / 32 * 32);
+    ct.tasks = (int)(n * ct.parts);
     return mode;
 }
-inline size_t code_smem(const CodeTokens& ct, int threads) { return (size_t)CT_STAGES * ct.passes * 2 * threads * 16; }
-// Blocks that are resident together, by shared memory (to 190 KB of an SM) and threads.
-inline long long code_blocks(const jpi_kv_handle* h, size_t smem, int threads) {
-    return (long long)h->num_sms * std::max<long long>(1, std::min<long long>(1536 / threads, (190 << 10) / (long long)(smem + sizeof(CodeSmem) + 2048)));
+// Blocks for the tasks, of those that are resident together (`per_sm`).
+inline unsigned code_blocks(const jpi_kv_handle* h, const CodeTokens& ct, int threads, int per_sm) {
+    return (unsigned)std::min<long long>((ct.tasks + threads / 32 - 1) / (threads / 32), (long long)h->num_sms * per_sm);
 }
 
 }  // namespace
