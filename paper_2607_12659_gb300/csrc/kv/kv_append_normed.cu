@@ -19,7 +19,7 @@ struct NormedArgs {
     int rows;
 };
 
-constexpr int AN_THREADS = 128, AN_BLOCKS = 8;   // of a block; blocks of an SM
+constexpr int AN_THREADS = 128, AN_BLOCKS = 7;   // of a block; blocks of an SM
 
 template <typename E, int MODE>
 __global__ void __launch_bounds__(AN_THREADS, AN_BLOCKS) k_kv_append_normed(const __grid_constant__ NormedArgs a) {

@@ -58,16 +58,17 @@ __device__ __forceinline__ float2 phase(int position, uint64_t turns, float m) {
 }
 
 // The same with the angle reduced to an eighth of a turn before it becomes an fp32 number: off by 2^-28 turns in place of 2^-26, for
-// codes of 8 bits, where each value beside a border that falls to the other side is a step of its own.
+// codes of 8 bits, where each value beside a border that falls to the other side is a step of its own. On |x| <= 1/4 half turns the
+// series of sin(pi x) and cos(pi x) to x^9 and x^10 leave 2^-29 and 2^-33, in a third of sincospif's instructions.
 __device__ __forceinline__ float2 phase_near(int position, uint64_t turns, float m) {
     const uint64_t ph = (uint64_t)(int64_t)position * turns;
-    const uint32_t quarter = (uint32_t)((ph + (1ull << 61)) >> 62);
-    const int32_t rest = (int32_t)((int64_t)(ph - ((uint64_t)quarter << 62)) >> 32);   // in units of 2^-32 turns
-    float s, c;
-    sincospif((float)rest * 4.656612873077393e-10f, &s, &c);
-    const float x = quarter & 1 ? s : c, y = quarter & 1 ? c : s;
+    const uint32_t hi = (uint32_t)(ph >> 32), quarter = (hi + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(hi - (quarter << 30)) * 4.656612873077393e-10f, z = x * x;
+    const float s = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 0.0821458866f, -0.599264529f), 2.55016404f), -5.16771278f), 3.14159265f);
+    const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -0.0258068914f, 0.23533063f), -1.33526277f), 4.05871213f), -4.9348022f), 1.f);
+    const float u = quarter & 1 ? s : c, v = quarter & 1 ? c : s;
     // (c, s), (-s, c), (-c, -s), (s, -c)
-    return make_float2((quarter == 1 || quarter == 2 ? -x : x) * m, (quarter >= 2 ? -y : y) * m);
+    return make_float2((quarter + 1) & 2 ? -u * m : u * m, quarter & 2 ? -v * m : v * m);
 }
 
 constexpr int AP_MAX_PAIRS = 128;   // dim / 2

@@ -239,22 +239,31 @@ __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens&
     const int per = 32 >> a.lanes_log2, u = lane & ((1 << a.lanes_log2) - 1);   // heads of a pass, lane of its head
     const HeadLane<E, MODE> ln(u, a.D, a.dim);
     const int mine = lane >> a.lanes_log2;
-    auto source = [&](long long tok, int hd) {
-        return hd < a.H ? static_cast<const E*>(a.q) + tok * a.q_stride + hd * a.D
-                        : hd < a.H + a.K ? static_cast<const E*>(a.k) + tok * a.k_stride + (hd - a.H) * a.D
-                                         : static_cast<const E*>(a.v) + tok * a.v_stride + (hd - a.H - a.K) * a.D;
+    // A task's heads: head hd of its token is at the base of its kind + hd D. (Pointers, which may lie before their buffers.)
+    struct Source {
+        const E *q, *k, *v;
+        int hd0;   // of the warp's first pass
     };
-    uint4 next[2];
-    // Asks for the heads of the run's k-th task's pass p.
-    auto fetch = [&](int k, int p) {
+    auto open = [&](int k) {
         uint32_t part;
         const long long tok = ct.by_parts.div((uint32_t)(first + k * step), part);
-        const int hd = ((int)part * ct.passes + p) * per + mine;
-        ln.load(source(tok, hd), hd < ct.heads, next);
+        Source x;
+        x.q = static_cast<const E*>(a.q) + tok * a.q_stride;
+        x.k = static_cast<const E*>(a.k) + tok * a.k_stride - a.H * a.D;
+        x.v = static_cast<const E*>(a.v) + tok * a.v_stride - (a.H + a.K) * a.D;
+        x.hd0 = (int)part * ct.passes * per;
+        return x;
+    };
+    auto source = [&](const Source& x, int hd) { return (hd < a.H ? x.q : hd < a.H + a.K ? x.k : x.v) + hd * a.D; };
+    uint4 next[2];
+    auto fetch = [&](const Source& x, int p) {
+        const int hd = x.hd0 + p * per + mine;
+        ln.load(source(x, hd), hd < ct.heads, next);
     };
     for (bool begin = true; first < ct.tasks; first += 32 * step, begin = false) {   // runs of 32 tasks
         const int count = min(32, (ct.tasks - first + step - 1) / step);
-        if (begin) fetch(0, 0);   // beside the rows
+        Source src = open(0);
+        if (begin) fetch(src, 0);   // beside the rows
         int row = -1, position = 0;   // of the run's task `lane`
         if (lane < count) {
             const int tok = (int)ct.by_parts.div((uint32_t)(first + lane * step));
@@ -262,13 +271,17 @@ __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens&
             position = a.position[tok];
         }
         uint32_t todo = __ballot_sync(0xffffffffu, row >= 0);   // without the padding
-        if (todo && !(begin && (todo & 1))) fetch(__ffs(todo) - 1, 0);
+        if (todo && !(begin && (todo & 1))) {
+            src = open(__ffs(todo) - 1);
+            fetch(src, 0);
+        }
         while (todo) {
             const int k = __ffs(todo) - 1;
             todo &= todo - 1;
             const int r = __shfl_sync(0xffffffffu, row, k), pos = __shfl_sync(0xffffffffu, position, k);
-            uint32_t part;
-            const long long tok = ct.by_parts.div((uint32_t)(first + k * step), part);
+            const Source x = src;
+            if (todo) src = open(__ffs(todo) - 1);
+            const long long tok = ct.by_parts.div((uint32_t)(first + k * step));
             if (MODE != RM_NONE) {
                 __syncwarp();   // the last task's table has been read
                 for (int p = lane; p < half; p += 32) {
@@ -279,15 +292,16 @@ __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens&
                 }
                 __syncwarp();
             }
-            const long long cache = at(tok, r);
-            const int hd0 = (int)part * ct.passes * per, passes = min(ct.passes, (ct.heads - hd0 + per - 1) / per);
+            // Likewise where its heads go.
+            E *const dq = static_cast<E*>(a.q_out) + tok * a.H * a.D, *const dk = ck + at(tok, r) - a.H * hs, *const dv = cv + at(tok, r) - (a.H + a.K) * hs;
+            const int passes = min(ct.passes, (ct.heads - x.hd0 + per - 1) / per);
 #pragma unroll 1
             for (int p = 0; p < passes; ++p) {
-                const int hd = hd0 + p * per + mine;
+                const int hd = x.hd0 + p * per + mine;
                 const bool live = hd < ct.heads, value = hd >= a.H + a.K, key = !value && hd >= a.H, coded = live && !value;
                 uint4 raw[2] = {next[0], next[1]};
-                if (p + 1 < passes) fetch(k, p + 1);
-                else if (todo) fetch(__ffs(todo) - 1, 0);
+                if (p + 1 < passes) fetch(x, p + 1);
+                else if (todo) fetch(src, 0);
                 if (__any_sync(0xffffffffu, coded)) {
                     float2 y[V];
                     auto rot = [&](int q, float (&c)[PC], float (&s)[PC]) {
@@ -313,15 +327,14 @@ __device__ __forceinline__ void code_tokens(const HeadArgs& a, const CodeTokens&
                         const float* w = key ? a.k_weight : a.q_weight;
                         return w ? w[d] : 1.f;
                     };
-                    code_head<E, MODE>(ln, a, MODE == RM_SCALAR && coded ? source(tok, hd) : nullptr, coded, raw, weight, other, rot, y);
+                    code_head<E, MODE>(ln, a, MODE == RM_SCALAR && coded ? source(x, hd) : nullptr, coded, raw, weight, other, rot, y);
                     if (coded) {
                         raw[0] = pack_chunk<E>(y, 0);
                         raw[1] = pack_chunk<E>(y, 1);
                     }
                 }
                 if (!live) continue;
-                E* dst = hd < a.H ? static_cast<E*>(a.q_out) + (tok * a.H + hd) * a.D
-                                  : (value ? cv + (hd - a.H - a.K) * hs : ck + (hd - a.H) * hs) + cache;
+                E* const dst = hd < a.H ? dq + hd * a.D : (value ? dv : dk) + hd * hs;
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
                     if (ln.live[c]) *reinterpret_cast<uint4*>(dst + ln.c[c] * V) = raw[c];
@@ -356,9 +369,11 @@ inline int plan_code_tokens(const jpi_kv_handle* h, HeadArgs& a, CodeTokens& ct,
     ct.tasks = (int)(n * ct.parts);
     return mode;
 }
-// Blocks for the tasks, of those that are resident together (`per_sm`).
+// Blocks for the tasks: as many tasks for each warp of those that are resident together (`per_sm` blocks).
 inline unsigned code_blocks(const jpi_kv_handle* h, const CodeTokens& ct, int threads, int per_sm) {
-    return (unsigned)std::min<long long>((ct.tasks + threads / 32 - 1) / (threads / 32), (long long)h->num_sms * per_sm);
+    const long long warps = threads / 32, all = ((long long)ct.tasks + warps - 1) / warps, most = (long long)h->num_sms * per_sm;
+    const long long turns = (all + most - 1) / most;
+    return (unsigned)((all + turns - 1) / turns);
 }
 
 }  // namespace
