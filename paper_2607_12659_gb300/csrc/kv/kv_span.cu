@@ -741,6 +741,10 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
     a.po = static_cast<float*>(h->ws);
     a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
     a.lse = lse;
+    if (const int splits = kv_span_tiles_plan(h, c, sn, std::max(1ll, ws_rows(h) / a.rows))) {
+        JPI_TRY(launch_kv_span_tiles(h, c, sn, splits, a.po, a.pml, out, lse, st));
+        return splits == 1 ? JPI_OK : launch_kv_combine(h, c, splits, out, lse, st);
+    }
     const long long most = (long long)(DP == 256 ? 5 : 6) * h->num_sms;   // resident warps of the row kernels
     if (h->bf16) {
         const int keys = sn.ks ? SrSmem<DP, true>::KEYS : SrSmem<DP, false>::KEYS;
@@ -782,6 +786,7 @@ jpi_status prepare_dim(const jpi_kv_handle* h) {
 }  // namespace
 
 jpi_status kv_span_prepare(jpi_kv_handle* h) {
+    JPI_TRY(kv_span_tiles_prepare(h));
     return h->D <= 64 ? prepare_dim<64>(h) : h->D <= 128 ? prepare_dim<128>(h) : prepare_dim<256>(h);
 }
 

@@ -1,0 +1,833 @@
+// Attention over windows with many query rows on tcgen05 (kv_span.h): 128 query rows (tokens x heads of one KV head of a
+// request) per block over a range of the key blocks of 64 that its tokens see.
+//   warp 0  bf16 caches, one thread: K blocks by bulk tensor copies into a ring of NS slots
+//   warp 1  the same for V
+//   warp 2  one thread: S_i = Q K_i^T (M = 128, N = 64, K = D) into one of NB TMEM score buffers
+//   warp 3  one thread: O += P_i V_i (M = 128, N = D, K = 64), V read as an MN-major operand
+//   warps 4-  groups of eight: two threads per query row, half of a block's keys each: maximum, 2^x, probabilities back to
+//           tensor memory, over the scores they come from. To D = 128 two groups take the even and the odd blocks, each with a
+//           maximum, sum and output of its own, joined at the end. O is rescaled only when a block's maximum passes the running
+//           one by more than 8 in log2 units.
+//   8-bit caches: eight more warps read codes ahead into registers and write them to the ring's slots as fp16 numbers, which
+//           e4m3 is a subset of: one instruction for two, half a tile's shared-memory writes a thread. Then both products take fp16: the
+//           queries at a power of two of each row's own (that its maximum and scale know of), the probabilities times
+//           the scale of their block's values relative to the largest 2^e that the row has seen, p 2^(e_j - e) 2^7 <= 2^15. (As bf16
+//           numbers with the scales in them the codes would take five instructions more a pair, which the softmax needs.)
+// The query rows are gathered by the softmax threads into tensor memory as the A operand of the score products.
+//
+// Probabilities are rounded to the operands' type once: each off by at most 2^-8 of itself, fp16 2^-11 or 2^-32 of 2^(e + 7).
+//
+// Rows of the cache that no query row of the tile sees may hold anything: their scores are replaced, and their values are
+// cleared in shared memory before the product, since 0 times a NaN would reach every row. Blocks that only some of the query
+// rows see whole are searched for infinities and NaN; one that holds any is added row by row on CUDA cores instead (each row
+// its own keys), and the product adds nothing. A row that sees nothing has l = 0, and what its outputs hold is not used.
+//
+// Each block leaves a part (unnormalised fp32 rows, (m, l)) for the combine, or the result: rows pass through shared
+// memory (the ring, free by then) and leave by bulk copies.
+//
+// Every wait is bounded; a wait that gives up records an error in the handle's word, and its thread waits for
+// nothing more.
+
+#include "kv_tiles.cuh"
+#include "kv8.cuh"
+#include "kv_maps.h"
+#include "kv_span.cuh"
+
+#include <algorithm>
+
+namespace jpi {
+namespace {
+
+constexpr int ST_ROWS = 128;
+constexpr int ST_KEYS = 64;
+constexpr int ST_SOFT = 256;    // threads of a softmax group
+constexpr int ST_CONV = 256;    // threads that write codes to the ring: half of them keys, half values
+constexpr uint64_t ST_WAIT_NS = 200ull * 1000 * 1000;
+constexpr float ST_RESCALE = 8.f;   // log2 units
+constexpr int ST_NONE = -4096;      // no scale seen yet
+// Query rows of a request and KV head from which a call takes the tiles, and the elements of keys up to which it stays with the row
+// kernel all the same, which reads a key once for every 8 query rows.
+constexpr int ST_LEAST = 32;
+constexpr long long ST_ROW_ELEMENTS = 10ll << 20;
+constexpr int ST_FIXED = 5;         // start and end of a block, in key blocks
+
+struct SpanMaps {
+    CUtensorMap k, v;
+};
+struct SpanTileArgs {
+    KvCall c;
+    KvSpan s;
+    float c2;              // log2(e) * scale
+    int splits, tiles;     // key ranges, row tiles of a request and KV head
+    KvDiv by_splits, by_tiles;
+    int3 at;               // of the maps' outer dimensions: heads, rows, caches
+    float* po;             // [parts][rows][D]
+    float2* pml;           // [rows][parts]
+    long long rows;
+    __nv_bfloat16* out;    // of a call of one part: the result, else null
+    float* lse;
+    int* err;
+};
+
+template <int DP, bool Q8>
+struct StSmem {
+    static constexpr int NS = DP == 256 ? 2 : DP == 128 ? 3 : 4;
+    static constexpr int KVBYTES = ST_KEYS * DP * 2;
+    static constexpr int STAGE = 2 * KVBYTES;               // ring slot: K, then V
+    static constexpr int OUT_LD = DP * 4 + 16;              // bytes of a staged output row: the pad spreads the banks
+    static constexpr int RING = NS * STAGE > ST_ROWS * OUT_LD ? NS * STAGE : ST_ROWS * OUT_LD;
+    static constexpr int NG = DP == 256 ? 1 : 2;            // softmax groups
+    static constexpr int CONV = 128 + NG * ST_SOFT;         // first thread of those that convert
+    static constexpr int THREADS = CONV + (Q8 ? ST_CONV : 0);
+    static constexpr int REGS = NG == 1 ? 96 : 72;
+    static constexpr int NB = DP == 256 ? 2 : 3;            // score buffers
+    static constexpr int XM_OFF = RING;                     // [groups][2 blocks][2 key halves][128 rows]
+    static constexpr int ML_OFF = XM_OFF + NG * 4 * ST_ROWS * 4;    // [groups][128 rows] (m, l)
+    static constexpr int QM_OFF = ML_OFF + NG * ST_ROWS * 8;        // [2 halves of d][128 rows] largest |q|
+    static constexpr int BAR_OFF = QM_OFF + 2 * ST_ROWS * 4;
+    static constexpr int BYTES = BAR_OFF + 8 * (3 * NB + NG + 2 + 4 * NS + 2);
+    // The query rows' way to a row per thread: 4 KB a warp in the last QS value slots, which are filled after it.
+    static constexpr int TURN = KVBYTES / 4096, QS = DP == 256 ? 1 : 2;
+    static_assert(QS < NS && TURN * QS >= (DP == 64 ? 4 : 8), "the query rows fit those slots");
+    static_assert(BYTES <= 227 * 1024 && THREADS * REGS <= 65536, "fits an SM");
+    static constexpr uint32_t TMEM_O = NB * ST_KEYS, TMEM_Q = TMEM_O + NG * DP, TMEM_COLS = 512;
+    static_assert(TMEM_Q + DP / 2 <= TMEM_COLS, "scores, outputs and queries fit");
+};
+
+// Whether one of two fp16 values is an infinity or NaN.
+__device__ __forceinline__ bool bad_half_pair(uint32_t x) { return (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u; }
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <int DP, bool Q8>
+__global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_constant__ SpanMaps maps,
+                                                               const __grid_constant__ SpanTileArgs a) {
+    using L = StSmem<DP, Q8>;
+    constexpr int NS = L::NS, NG = L::NG, NB = L::NB, NDB = DP / 64;
+    // (fp16 operands are type 0 of both fields)
+    constexpr uint32_t TYPES = Q8 ? ~((1u << 7) | (1u << 10)) : ~0u;
+    constexpr uint32_t IDESC_S = ptx::idesc_bf16_f32(ST_ROWS, ST_KEYS) & TYPES;
+    constexpr uint32_t IDESC_PV = (ptx::idesc_bf16_f32(ST_ROWS, DP) | (1u << 16)) & TYPES;   // B MN-major
+    extern __shared__ __align__(1024) uint8_t st_smem[];
+    uint8_t* stages = st_smem;
+    float* xmax = (float*)(st_smem + L::XM_OFF);
+    float2* ml = (float2*)(st_smem + L::ML_OFF);
+    float* qmax = (float*)(st_smem + L::QM_OFF);
+    uint64_t* bars = (uint64_t*)(st_smem + L::BAR_OFF);
+    uint64_t* sfull = bars;            // NB: score buffer ready
+    uint64_t* pfull = sfull + NB;      // NB: probabilities written over the score buffer
+    uint64_t* odone = pfull + NB;      // NB: P V of the block in score buffer b done
+    uint64_t* gdone = odone + NB;      // NG: P V of the group's block done, of a block that another one of the group follows
+    uint64_t* alldone = gdone + NG;    // every P V done
+    uint64_t* qready = alldone + 1;    // the query rows are in TMEM
+    uint64_t* kfull = qready + 1;      // NS each
+    uint64_t* vfull = kfull + NS;
+    uint64_t* kempty = vfull + NS;
+    uint64_t* vempty = kempty + NS;
+    uint32_t* tmem_slot = (uint32_t*)(vempty + NS);
+    int* flag = (int*)(tmem_slot + 1);
+    int* begun = flag + 1;             // NG: the group's output holds something before its first product
+
+    const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
+    ptx::grid_dep_launch();
+    // Row tiles fastest: the blocks that read the same keys run together.
+    uint32_t tile, split, kvh;
+    const int cache = (int)a.c.by_K.div(a.by_splits.div(a.by_tiles.div(blockIdx.x, tile), split), kvh);
+    RowTile t;
+    t.tok0 = (long long)cache * a.c.tokens;
+    t.head0 = (int)kvh * a.c.gq;
+    t.R = a.c.tokens * a.c.gq;
+    t.r0 = (int)tile * ST_ROWS;
+    const KvSpan& sn = a.s;
+    // Of the tile's tokens that see anything: the largest and the least count, the first and the last first row.
+    int most = 0, low = 0x7fffffff, first = 0x7fffffff, late = 0;
+    {
+        const int last = (int)a.c.by_gq.div((uint32_t)min(t.r0 + ST_ROWS, t.R) - 1);
+        for (int k = (int)a.c.by_gq.div((uint32_t)t.r0) + lane; k <= last; k += 32) {
+            const int n = min(a.c.own.len[t.tok0 + k], a.c.own.rows);
+            if (n <= 0) continue;
+            const int w = span_first(sn, n);
+            most = max(most, n);
+            low = min(low, n);
+            first = min(first, w);
+            late = max(late, w);
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        low = __reduce_min_sync(0xffffffffu, low);
+        first = __reduce_min_sync(0xffffffffu, first);
+        late = __reduce_max_sync(0xffffffffu, late);
+    }
+    const SpanBlocks<ST_KEYS> blocks(sn, most, first);
+    // This block's key blocks; none where they are fewer than the splits: the part then weighs nothing.
+    const int blk0 = (int)((long long)split * blocks.count / a.splits);
+    const int nb = (int)((long long)(split + 1) * blocks.count / a.splits) - blk0;
+    // Key (value) block i into its ring slot (bf16).
+    auto load = [&](bool is_v, int i) {
+        const int sl = i % NS;
+        uint64_t* full = (is_v ? vfull : kfull) + sl;
+        uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0);
+        ptx::mbar_expect_tx(full, (uint32_t)L::KVBYTES);
+        for (int db = 0; db < NDB; ++db)
+            kv_load_box(base + db * (ST_KEYS * 128), is_v ? &maps.v : &maps.k, full, db * 64, a.at, (int)kvh, blocks.row(blk0 + i), cache);
+    };
+    if (warp == 0 && ptx::elect_one()) {
+        if (!Q8) {
+            ptx::prefetch_tmap(&maps.k);
+            ptx::prefetch_tmap(&maps.v);
+        }
+        for (int b = 0; b < NB; ++b) {
+            ptx::mbar_init(&sfull[b], 1);
+            ptx::mbar_init(&pfull[b], ST_SOFT);
+            ptx::mbar_init(&odone[b], 1);
+        }
+        for (int b = 0; b < NG; ++b) ptx::mbar_init(&gdone[b], 1);
+        ptx::mbar_init(alldone, 1);
+        ptx::mbar_init(qready, 256);
+        for (int s = 0; s < NS; ++s) {
+            ptx::mbar_init(&kfull[s], Q8 ? ST_CONV / 2 : 1);
+            ptx::mbar_init(&vfull[s], Q8 ? ST_CONV / 2 : 1);
+            ptx::mbar_init(&kempty[s], 1);
+            ptx::mbar_init(&vempty[s], 1);
+        }
+        ptx::fence_mbar_init();
+        *flag = 0;
+        for (int b = 0; b < NG; ++b) begun[b] = 0;
+        // The first use of the ring needs nothing of the other warps.
+        for (int i = 0; !Q8 && i < NS && i < nb; ++i) {
+            load(false, i);
+            if (i < NS - L::QS) load(true, i);
+        }
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(tmem_slot, L::TMEM_COLS);
+        ptx::tmem_relinquish();
+    }
+    // The softmax warps' query rows, on their way while the block sets itself up: 64-element blocks (warp - 4) / 4,
+    // + 2, of the rows of the warp's TMEM lanes.
+    constexpr int QN = (NDB + 1) / 2;
+    uint4 qv[QN][8];
+    if (warp >= 4 && warp < 12) {
+        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q);
+        // Row 4 i + (lane / 8): its token and head, stepped by 4 rows.
+        int r = t.r0 + (warp & 3) * 32 + (lane >> 3);
+        int tok = r / a.c.gq, hd = r - tok * a.c.gq;
+        const int tok4 = 4 / a.c.gq, hd4 = 4 - tok4 * a.c.gq;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool in = r < t.R;
+            const __nv_bfloat16* row = q + (in ? (t.tok0 + tok) * a.c.q_stride + (long long)(t.head0 + hd) * a.c.D : 0);
+#pragma unroll
+            for (int k = 0; k < QN; ++k) {
+                const int d = 64 * (((warp - 4) >> 2) + 2 * k) + 8 * (lane & 7);
+                qv[k][i] = kr_ld(row + d, in && d < a.c.D);
+            }
+            r += 4;
+            tok += tok4;
+            hd += hd4;
+            if (hd >= a.c.gq) {
+                hd -= a.c.gq;
+                ++tok;
+            }
+        }
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp <= 1) {
+        if (!Q8 && ptx::elect_one()) {
+            const bool is_v = warp == 1;
+            uint64_t* fullb = is_v ? vfull : kfull;
+            uint64_t* emptyb = is_v ? vempty : kempty;
+            int issued = min(NS, nb);
+            bool good = true;
+            if (is_v) {
+                good = ptx::mbar_wait_bounded(qready, 0, ST_WAIT_NS);
+                if (!good) *flag = DEV_TIMEOUT_MMA;
+                if (!good) issued = min(NS - L::QS, nb);
+                for (int i = NS - L::QS; good && i < NS && i < nb; ++i) load(true, i);
+            }
+            for (int i = NS; good && i < nb; ++i) {
+                if (!ptx::mbar_wait_bounded(&emptyb[i % NS], (i / NS - 1) & 1, ST_WAIT_NS)) {
+                    *flag = DEV_TIMEOUT_WEIGHTS;
+                    break;
+                }
+                load(is_v, i);
+                issued = i + 1;
+            }
+            if (!ptx::ring_drain(fullb, NS, issued, ST_WAIT_NS)) *flag = DEV_TIMEOUT_WEIGHTS;
+        }
+    } else if (warp == 2) {
+        if (ptx::elect_one()) {
+            const uint32_t sb = ptx::smem_u32(stages);
+            bool good = ptx::mbar_wait_bounded(qready, 0, ST_WAIT_NS);
+            for (int i = 0; i < nb; ++i) {
+                const int sl = i % NS;
+                // (its score buffer holds P_{i-NB} until that product is done)
+                if (i >= NB && good) good = ptx::mbar_wait_bounded(&odone[i % NB], (i / NB - 1) & 1, ST_WAIT_NS);
+                if (good) good = ptx::mbar_wait_bounded(&kfull[sl], (i / NS) & 1, ST_WAIT_NS);
+                ptx::tc_fence_after();
+                if (good) {
+                    const uint64_t kb = ptx::desc_sw128(sb + sl * L::STAGE);
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            ptx::mma_bf16_ta(tmem + (uint32_t)(ST_KEYS * (i % NB)), tmem + L::TMEM_Q + (uint32_t)(8 * (4 * db + kk)),
+                                             ptx::desc_add(kb, db * (ST_KEYS * 128) + kk * 32), IDESC_S, (db | kk) != 0);
+                }
+                ptx::mma_commit(&sfull[i % NB]);
+                if (i + NS < nb) ptx::mma_commit(&kempty[sl]);
+            }
+            if (!good) *flag = DEV_TIMEOUT_MMA;
+        }
+    } else if (warp == 3) {
+        if (ptx::elect_one()) {
+            const uint32_t sb = ptx::smem_u32(stages);
+            bool good = true;
+            for (int i = 0; i < nb; ++i) {
+                const int sl = i % NS;
+                if (good) good = ptx::mbar_wait_bounded(&pfull[i % NB], (i / NB) & 1, ST_WAIT_NS);
+                if (good) good = ptx::mbar_wait_bounded(&vfull[sl], (i / NS) & 1, ST_WAIT_NS);
+                ptx::tc_fence_after();
+                if (good) {
+                    const uint64_t vb = ptx::desc_sw128_mn(sb + sl * L::STAGE + L::KVBYTES, ST_KEYS * 128, 1024);
+#pragma unroll
+                    for (int kk = 0; kk < ST_KEYS / 16; ++kk)
+                        ptx::mma_bf16_ta(tmem + L::TMEM_O + (uint32_t)(i % NG * DP), tmem + (uint32_t)(ST_KEYS * (i % NB) + 8 * kk),
+                                         ptx::desc_add(vb, kk * 16 * 128), IDESC_PV, i >= NG || kk != 0 || begun[i % NG] != 0);
+                }
+                if (i + NS < nb) ptx::mma_commit(&vempty[sl]);
+                if (i + NB < nb) ptx::mma_commit(&odone[i % NB]);
+                if (i + NG < nb) ptx::mma_commit(&gdone[i % NG]);
+            }
+            ptx::mma_commit(alldone);
+            if (!good) *flag = DEV_TIMEOUT_MMA;
+        }
+    } else if (Q8 && tid >= L::CONV) {
+        // Codes to fp16 numbers in the layout of the copies: 16 codes of a row are two 16-byte chunks of a 128-byte line.
+        constexpr int PIECES = DP / 16, MINE = ST_KEYS * PIECES / (ST_CONV / 2), SWEEP = ST_CONV / 2 / PIECES;   // rows of a sweep
+        const bool is_v = tid >= L::CONV + ST_CONV / 2;
+        const int x = (tid - L::CONV) % (ST_CONV / 2), piece = x % PIECES, row0 = x / PIECES;
+        uint64_t* fullb = is_v ? vfull : kfull;
+        uint64_t* emptyb = is_v ? vempty : kempty;
+        const bool in = 16 * piece < a.c.D;
+        const uint8_t* src = static_cast<const uint8_t*>(is_v ? a.c.own.v : a.c.own.k) + cache * a.c.own.cs + kvh * a.c.own.hs + 16 * piece;
+        const uint8_t* scale = (is_v ? sn.vs : sn.ks) + ((long long)cache * a.c.K + kvh) * sn.nblk;
+        uint4 code[MINE];
+        // (a row that no query row sees arrives as zeros, one under a scale that is NaN as NaN)
+        auto fetch = [&](int i) {
+            const int key0 = blocks.row(blk0 + i) + row0;
+#pragma unroll
+            for (int m = 0; m < MINE; ++m) {
+                const int key = key0 + m * SWEEP;
+                const bool live = in && span_sees(sn, key, most, first);
+                code[m] = live ? __ldg(reinterpret_cast<const uint4*>(src + key * a.c.own.rs)) : make_uint4(0, 0, 0, 0);
+                if (live && scale[key >> sn.n_log2] == 255) code[m] = make_uint4(0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f);
+            }
+        };
+        bool good = true;
+        if (nb > 0) fetch(0);
+        for (int i = 0; i < nb; ++i) {
+            const int sl = i % NS;
+            if (good && i >= NS) good = ptx::mbar_wait_bounded(&emptyb[sl], (i / NS - 1) & 1, ST_WAIT_NS);
+            // (the query rows pass through the last value slots)
+            if (good && is_v && i >= NS - L::QS && i < NS) good = ptx::mbar_wait_bounded(qready, 0, ST_WAIT_NS);
+            if (!good) break;
+            uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0) + piece / 4 * (ST_KEYS * 128);
+#pragma unroll
+            for (int m = 0; m < MINE; ++m) {
+                const int r = row0 + m * SWEEP;
+                const uint32_t c[4] = {code[m].x, code[m].y, code[m].z, code[m].w};
+                uint4 h[2];
+                h[0] = make_uint4(kv8_half2(c[0]), kv8_half2(c[0] >> 16), kv8_half2(c[1]), kv8_half2(c[1] >> 16));
+                h[1] = make_uint4(kv8_half2(c[2]), kv8_half2(c[2] >> 16), kv8_half2(c[3]), kv8_half2(c[3] >> 16));
+                // Neighbouring 128-byte lines begin with the other chunk: eight lanes, eight places in the banks.
+                const int odd = piece >> 2 & 1;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    *reinterpret_cast<uint4*>(base + r * 128 + (((2 * (piece & 3) + (e ^ odd)) ^ (r & 7)) << 4)) = (e ^ odd) ? h[1] : h[0];
+            }
+            if (i + 1 < nb) fetch(i + 1);
+            ptx::fence_proxy_async_smem();
+            ptx::mbar_arrive(&fullb[sl]);
+        }
+        if (!good) *flag = DEV_TIMEOUT_WEIGHTS;
+    } else {
+        const int grp = (warp - 4) >> 3, row = (warp & 3) * 32 + lane, half = ((warp - 4) >> 2) & 1;
+        const int r = t.r0 + row;
+        const bool valid = r < t.R;
+        const int vis = valid ? min(max(a.c.own.len[row_token(a.c, t, r)], 0), a.c.own.rows) : 0;   // the row's count
+        const int begins = span_first(sn, vis);
+        const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t out = lane_base + L::TMEM_O + (uint32_t)(grp * DP);
+        const uint32_t pair_bar = 1 + 4 * grp + (warp & 3);   // the two warps of these 32 rows
+        float m_used = -INFINITY, l = 0.f;          // m_used is the same in both threads of a row
+        int v_used = ST_NONE;                       // 8 bits: the largest scale of values that the row has seen; likewise
+        bool good = true;
+        // The query rows were loaded 128 bytes of four rows an instruction: through 4 KB of shared memory of the warp
+        // to a row per thread, then to TMEM (column 32 db + 4 c + e holds elements 64 db + 8 c + 2 e, + 1).
+        if (grp == 0) {
+            const int wi = warp - 4;
+            float qf[8];   // 8 bits: what row 4 i + lane / 8 is multiplied by
+            if constexpr (Q8) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float top = 0.f;
+#pragma unroll
+                    for (int k = 0; k < QN; ++k) {
+                        const uint32_t w[4] = {qv[k][i].x, qv[k][i].y, qv[k][i].z, qv[k][i].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float lo = fabsf(__uint_as_float(w[e] << 16)), hi = fabsf(__uint_as_float(w[e] & 0xffff0000u));
+                            top = fmaxf(top, lo < INFINITY ? lo : 0.f);
+                            top = fmaxf(top, hi < INFINITY ? hi : 0.f);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 1; e < 8; e <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, e));
+                    if ((lane & 7) == 0) qmax[half * ST_ROWS + (warp & 3) * 32 + 4 * i + (lane >> 3)] = top;
+                }
+                ptx::named_bar_sync(pair_bar, 64);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int rr = (warp & 3) * 32 + 4 * i + (lane >> 3);
+                    const float top = fmaxf(qmax[rr], qmax[ST_ROWS + rr]);
+                    qf[i] = kv8_pow2(255 - max((int)(__float_as_uint(top) >> 23), 2));   // the largest to 2 .. 4
+                }
+            }
+            uint4* turn = (uint4*)(stages + (NS - 1 - wi / L::TURN) * L::STAGE + L::KVBYTES + wi % L::TURN * 4096);
+#pragma unroll
+            for (int k = 0; k < QN; ++k) {
+                const int db = half + 2 * k;
+                if (db < NDB) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint4 v = qv[k][i];
+                        if constexpr (Q8) {
+                            uint32_t* w = &v.x;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                w[e] = half_pair(__uint_as_float(w[e] << 16) * qf[i], __uint_as_float(w[e] & 0xffff0000u) * qf[i]);
+                        }
+                        turn[(4 * i + (lane >> 3)) * 8 + ((lane & 7) ^ ((4 * i + (lane >> 3)) & 7))] = v;
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        uint32_t rq[16];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const uint4 v = turn[lane * 8 + ((4 * hf + c) ^ (lane & 7))];
+                            rq[4 * c] = v.x;
+                            rq[4 * c + 1] = v.y;
+                            rq[4 * c + 2] = v.z;
+                            rq[4 * c + 3] = v.w;
+                        }
+                        ptx::tmem_st_x16(lane_base + L::TMEM_Q + (uint32_t)(32 * db + 16 * hf), rq);
+                    }
+                    __syncwarp();
+                }
+            }
+            ptx::tmem_st_wait();
+            ptx::fence_proxy_async_smem();   // the slots' values land after these accesses
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(qready);
+        }
+        constexpr int HK = ST_KEYS / 2;   // keys per thread
+        // In 8 bits scores and maxima are those of the scaled query, qs of the true ones.
+        float qs = 1.f;
+        if constexpr (Q8) {
+            if (grp > 0) good = ptx::mbar_wait_bounded(qready, 0, ST_WAIT_NS);
+            qs = kv8_pow2(max((int)(__float_as_uint(fmaxf(qmax[row], qmax[ST_ROWS + row])) >> 23), 2) - 1);
+        }
+        const float c2s = fminf(a.c2 * qs, 3e38f);
+        const uint64_t c2 = pair2(c2s);
+        const float rescale = fminf(ST_RESCALE / c2s, 3e38f);
+        // Scales of block i: of its four tiles' values, of the half's two tiles' keys (a tile that no row sees has none: 127).
+        const uint8_t* const ksc = Q8 ? sn.ks + ((long long)cache * a.c.K + kvh) * sn.nblk : nullptr;
+        const uint8_t* const vsc = Q8 ? sn.vs + ((long long)cache * a.c.K + kvh) * sn.nblk : nullptr;
+        uint32_t ve[4] = {127, 127, 127, 127}, ke[2] = {127, 127};
+        auto scales = [&](int i) {
+            const int key0 = blocks.row(blk0 + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = key0 + 16 * e;
+                const bool live = at < most && (at < sn.sink || at + 16 > first);
+                ve[e] = live ? vsc[at >> sn.n_log2] : 127;
+                if (e >> 1 == half) ke[e & 1] = live ? ksc[at >> sn.n_log2] : 127;
+            }
+        };
+        if (Q8 && grp < nb) scales(grp);
+        for (int i = grp; i < nb; i += NG) {
+            if (good) good = ptx::mbar_wait_bounded(&sfull[i % NB], (i / NB) & 1, ST_WAIT_NS);
+            ptx::tc_fence_after();
+            uint32_t s[2][16];
+            {
+                const uint32_t sa = lane_base + (uint32_t)(ST_KEYS * (i % NB) + HK * half);
+                ptx::tmem_ld_x16(sa, s[0]);
+                ptx::tmem_ld_x16(sa + 16u, s[1]);
+                ptx::tmem_ld_wait();
+            }
+            const int key0 = blocks.row(blk0 + i), mine = key0 + HK * half;
+            if constexpr (Q8) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint64_t by = pair2(ke[e] == 255 ? 1.f : kv8_scale(ke[e]));   // (the slot's numbers are NaN then)
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) {
+                        uint64_t v;
+                        asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(s[e][j]), "r"(s[e][j + 1]));
+                        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(by));
+                        asm("mov.b64 {%0, %1}, %2;" : "=r"(s[e][j]), "=r"(s[e][j + 1]) : "l"(v));
+                    }
+                }
+            }
+            // Of this half's keys the ones that the row sees: all, or those below `end`, from `from` on or below `sunk`.
+            const int end = vis - mine, from = begins - mine, sunk = sn.sink - mine;
+            const bool full = __all_sync(0xffffffffu, end >= HK && (from <= 0 || sunk >= HK));
+            auto sees = [&](int j) { return j < end && (j >= from || j < sunk); };
+            if (!full) {
+#pragma unroll
+                for (int j = 0; j < HK; ++j)
+                    if (!sees(j)) s[j >> 4][j & 15] = __float_as_uint(-INFINITY);
+            }
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int j = 0; j < HK; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j >> 4][j & 15]));
+            float mb = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            float* xm = xmax + (2 * grp + (i / NG & 1)) * 2 * ST_ROWS + row;
+            xm[half * ST_ROWS] = mb;
+            ptx::named_bar_sync(pair_bar, 64);
+            mb = fmaxf(mb, xm[(1 - half) * ST_ROWS]);
+            const bool move = mb > m_used + rescale;
+            const float alpha = !move ? 1.f : m_used == -INFINITY ? 0.f : kr_ex2((m_used - mb) * c2s);
+            float beta = alpha;               // what the outputs are multiplied by: in units of the largest scale, too
+            bool grown = false;
+            float pv[2] = {1.f, 1.f};         // what the probabilities of the half's tiles are
+            if constexpr (Q8) {
+                int v_now = v_used;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at = key0 + 16 * e;
+                    if (ve[e] != 255 && at < vis && (at < sn.sink || at + 16 > begins)) v_now = max(v_now, max((int)ve[e], 1));
+                }
+                grown = v_now != v_used;
+                if (grown) beta *= kv8_pow2(127 + v_used - v_now);
+                v_used = v_now;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int at = half ? (int)ve[2 + e] : (int)ve[e];
+                    pv[e] = at == 255 || v_now == ST_NONE ? 0x1p7f : kv8_pow2(min(134 + at - v_now, 254));
+                }
+                if (i + NG < nb) scales(i + NG);
+            }
+            // TMEM accesses are warp-collective: the warp rescales together (its half of the columns), lanes whose
+            // maximum stays put multiply by 1. O is settled once P V of the group's previous block is done.
+            if (__any_sync(0xffffffffu, i >= NG && ((move && m_used != -INFINITY) || grown))) {
+                if (good) good = ptx::mbar_wait_bounded(&gdone[grp], (i / NG - 1) & 1, ST_WAIT_NS);
+                ptx::tc_fence_after();
+#pragma unroll 1
+                for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 16) {
+                    uint32_t ro[16];
+                    ptx::tmem_ld_x16(out + (uint32_t)c0, ro);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) ro[j] = __float_as_uint(__uint_as_float(ro[j]) * beta);
+                    ptx::tmem_st_x16(out + (uint32_t)c0, ro);
+                }
+                ptx::tmem_st_wait();
+            }
+            if (move) {
+                l *= alpha;
+                m_used = mb;
+            }
+            // 2^((s - m) c): a hidden key's -inf gives 0, also while the row has seen none at all (m taken as 0).
+            const uint64_t neg_m = pair2(m_used == -INFINITY ? 0.f : -m_used);
+            float l4[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t pk[HK / 2];
+#pragma unroll
+            for (int k = 0; k < HK; k += 2) {
+                float p0, p1;
+                sub_scale2(__uint_as_float(s[k >> 4][k & 15]), __uint_as_float(s[k >> 4][(k + 1) & 15]), neg_m, c2, p0, p1);
+                p0 = kr_ex2(p0);
+                p1 = kr_ex2(p1);
+                l4[(k >> 1) & 3] += p0 + p1;
+                pk[k / 2] = Q8 ? half_pair(p0 * pv[k >> 4], p1 * pv[k >> 4]) : kr_pack(p0, p1);
+            }
+            l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+            // Keys of the block that some row sees and some does not; rows that none sees. The same for all threads.
+            const bool cut = low < min(most, key0 + ST_KEYS) || (key0 < late && key0 + ST_KEYS > sn.sink);
+            const bool dead = most < key0 + ST_KEYS || (key0 < first && key0 + ST_KEYS > sn.sink);
+            uint8_t* vb = stages + i % NS * L::STAGE + L::KVBYTES;
+            if (cut) {
+                // Is there an infinity or NaN among the values?
+                if (good) good = ptx::mbar_wait_bounded(&vfull[i % NS], (i / NS) & 1, ST_WAIT_NS);
+                bool odd = false;
+                for (int e = (tid - 128) % ST_SOFT; e < ST_KEYS * NDB * 8; e += ST_SOFT) {
+                    const int key = e / (NDB * 8), p = e % (NDB * 8);
+                    if (!span_sees(sn, key0 + key, most, first)) continue;
+                    const uint4 v = *(const uint4*)(vb + (p / 8) * (ST_KEYS * 128) + key * 128 + (p % 8) * 16);
+                    if (Q8) odd = odd || bad_half_pair(v.x) || bad_half_pair(v.y) || bad_half_pair(v.z) || bad_half_pair(v.w);
+                    else odd = odd || bad_pair(v.x) || bad_pair(v.y) || bad_pair(v.z) || bad_pair(v.w);
+                }
+                if (group_any(11 + grp, ST_SOFT, odd)) {
+                    // Row by row: first one half's keys, then the other's, onto the settled output of the blocks before.
+                    if (i >= NG && good) good = ptx::mbar_wait_bounded(&gdone[grp], (i / NG - 1) & 1, ST_WAIT_NS);
+                    ptx::tc_fence_after();
+                    for (int turn = 0; turn < 2; ++turn) {
+                        if (turn == half) {
+#pragma unroll 1
+                            for (int c0 = 0; c0 < DP; c0 += 16) {
+                                uint32_t ro[16];
+                                if (i < NG && turn == 0) {
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) ro[j] = 0u;
+                                } else {
+                                    ptx::tmem_ld_x16(out + (uint32_t)c0, ro);
+                                    ptx::tmem_ld_wait();
+                                }
+#pragma unroll
+                                for (int k = 0; k < HK; ++k) {
+                                    if (!sees(k)) continue;
+                                    const int key = HK * half + k;
+                                    float pr;
+                                    if (Q8) pr = __half2float(__ushort_as_half((unsigned short)(k & 1 ? pk[k / 2] >> 16 : pk[k / 2])));
+                                    else pr = __uint_as_float(k & 1 ? pk[k / 2] & 0xffff0000u : pk[k / 2] << 16);
+                                    const uint8_t* vr = vb + (c0 / 64) * (ST_KEYS * 128) + key * 128;
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h) {
+                                        const uint4 v = *(const uint4*)(vr + (((c0 % 64 / 8 + h) ^ (key & 7)) << 4));
+                                        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                        for (int e = 0; e < 4; ++e) {
+                                            uint32_t &y0 = ro[8 * h + 2 * e], &y1 = ro[8 * h + 2 * e + 1];
+                                            float2 z = make_float2(__uint_as_float(x[e] << 16), __uint_as_float(x[e] & 0xffff0000u));
+                                            if (Q8) z = __half22float2(*reinterpret_cast<const __half2*>(&x[e]));
+                                            y0 = __float_as_uint(fmaf(pr, z.x, __uint_as_float(y0)));
+                                            y1 = __float_as_uint(fmaf(pr, z.y, __uint_as_float(y1)));
+                                        }
+                                    }
+                                }
+                                __syncwarp();
+                                ptx::tmem_st_x16(out + (uint32_t)c0, ro);
+                            }
+                            ptx::tmem_st_wait();
+                            ptx::tc_fence_before();
+                        }
+                        ptx::named_bar_sync(pair_bar, 64);
+                        ptx::tc_fence_after();
+                    }
+#pragma unroll
+                    for (int k = 0; k < HK / 2; ++k) pk[k] = 0u;
+                    ptx::named_bar_sync(11 + grp, ST_SOFT);   // every thread has read the values
+                    for (int e = (tid - 128) % ST_SOFT; good && e < ST_KEYS * NDB * 8; e += ST_SOFT) ((uint4*)vb)[e] = make_uint4(0, 0, 0, 0);
+                    if (i < NG && tid % ST_SOFT == 128) begun[grp] = 1;
+                    ptx::fence_proxy_async_smem();
+                }
+            }
+            // Over the scores of both halves: both threads of a row have read theirs (the barrier above). Column 16 half
+            // + e holds keys 32 half + 2 e, + 1.
+            ptx::tmem_st_x16(lane_base + (uint32_t)(ST_KEYS * (i % NB) + 16 * half), pk);
+            ptx::tmem_st_wait();
+            if (!Q8 && dead) {
+                // Values of rows that no row sees, as they landed: cleared (a row's 16-byte pieces stay in the row).
+                if (good) good = ptx::mbar_wait_bounded(&vfull[i % NS], (i / NS) & 1, ST_WAIT_NS);
+                for (int e = (tid - 128) % ST_SOFT; good && e < ST_KEYS * NDB * 8; e += ST_SOFT) {
+                    const int key = e / (NDB * 8), p = e % (NDB * 8);
+                    if (!span_sees(sn, key0 + key, most, first))
+                        *(uint4*)(vb + (p / 8) * (ST_KEYS * 128) + key * 128 + (p % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                ptx::fence_proxy_async_smem();
+            }
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(&pfull[i % NB]);
+        }
+        // The row's sum: both halves, in order, through the buffer that the last block's maxima are not in.
+        const int mine = (nb - grp + NG - 1) / NG;   // blocks of this group
+        float* xl = xmax + (2 * grp + (mine & 1)) * 2 * ST_ROWS + row;
+        xl[half * ST_ROWS] = l;
+        ptx::named_bar_sync(pair_bar, 64);
+        l = xl[0] + xl[ST_ROWS];
+        // Every P V of the block is done, and with them every read of the ring.
+        if (good) good = ptx::mbar_wait_bounded(alldone, 0, ST_WAIT_NS);
+        ptx::tc_fence_after();
+        if (!good) *flag = DEV_TIMEOUT_MMA;
+        // The groups' outputs are joined on the way: w_g = 2^((m_g - M) c), nothing of a group in which the row saw no key.
+        float w = 1.f;
+        bool some = l != 0.f;
+        if (NG > 1) {
+            if (half == 0) ml[grp * ST_ROWS + row] = make_float2(m_used, l);
+            ptx::named_bar_sync(9, NG * ST_SOFT);
+            const float2 other = ml[(1 - grp) * ST_ROWS + row];
+            const float M = fmaxf(m_used, other.x);
+            w = m_used == -INFINITY ? 0.f : kr_ex2((m_used - M) * c2s);
+            l = w * l + (other.x == -INFINITY ? 0.f : kr_ex2((other.x - M) * c2s)) * other.y;   // (0 times a NaN sum is NaN)
+            m_used = M;
+        }
+        if constexpr (Q8) {
+            m_used *= qs;
+            w = v_used == ST_NONE ? w : w * 0x1p-7f;
+        }
+        const float vscale = Q8 && v_used != ST_NONE ? kv8_scale((uint32_t)v_used) : 1.f;
+        // A result is scaled by 1 / l and rounded on its way; a half row's 16-bit values go where its own 32-bit ones were.
+        const float inv = l == 0.f ? 0.f : 1.f / l;   // (0: the row saw no key; a NaN score makes l, and so the row, NaN)
+        uint8_t* orow = st_smem + row * L::OUT_LD;
+#pragma unroll 1
+        for (int turn = 0; turn < NG; ++turn) {
+            if (turn == grp) {
+#pragma unroll 1
+                for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 32) {
+                    uint32_t v[2][16];
+                    ptx::tmem_ld_x16(out + (uint32_t)c0, v[0]);
+                    ptx::tmem_ld_x16(out + (uint32_t)(c0 + 16), v[1]);
+                    ptx::tmem_ld_wait();
+                    // (a wait that gave up may have left copies on their way into the ring)
+                    if (good && (mine > 0 || (a.out && nb > 0))) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            uint4* dst = (uint4*)(orow + (c0 + 4 * k) * 4);
+                            float x[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                x[e] = __uint_as_float(v[k >> 2][4 * (k & 3) + e]);
+                                x[e] = some ? w * x[e] : 0.f;
+                                if (Q8) x[e] *= vscale;
+                            }
+                            if (grp > 0) {
+                                const uint4 y = *dst;
+                                x[0] += __uint_as_float(y.x);
+                                x[1] += __uint_as_float(y.y);
+                                x[2] += __uint_as_float(y.z);
+                                x[3] += __uint_as_float(y.w);
+                            }
+                            if (a.out && grp == NG - 1) {
+                                uint32_t* dst16 = (uint32_t*)(orow + half * (DP * 2) + (c0 + 4 * k - half * (DP / 2)) * 2);
+                                dst16[0] = kr_pack(x[0] * inv, x[1] * inv);
+                                dst16[1] = kr_pack(x[2] * inv, x[3] * inv);
+                            } else {
+                                *dst = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+                            }
+                        }
+                    }
+                }
+            }
+            if (turn + 1 < NG) ptx::named_bar_sync(10, NG * ST_SOFT);
+        }
+        if (grp == NG - 1) {
+            ptx::fence_proxy_async_smem();
+            ptx::named_bar_sync(pair_bar, 64);
+            if (half == 0 && valid) {
+                const long long row_at = row_index(a.c, t, r), row_out = (long long)split * a.rows + row_at;
+                auto copy = [&](void* dst, const uint8_t* src, int bytes) {
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(ptx::smem_u32(src)),
+                                 "r"(bytes)
+                                 : "memory");
+                };
+                if (a.out) {
+                    __nv_bfloat16* dst = a.out + row_at * a.c.D;
+                    if (a.lse) a.lse[row_at] = l == 0.f ? -INFINITY : fmaf(m_used, a.c.scale, logf(l));
+                    if (nb == 0) {
+                        for (int d = 0; d < a.c.D; d += 8) *(uint4*)(dst + d) = make_uint4(0, 0, 0, 0);
+                    } else if (good) {
+                        copy(dst, orow, min(a.c.D, DP / 2) * 2);
+                        if (a.c.D > DP / 2) copy(dst + DP / 2, orow + DP * 2, (a.c.D - DP / 2) * 2);
+                    }
+                } else {
+                    a.pml[row_at * a.splits + split] = make_float2(m_used, l);
+                    if (good && nb > 0) copy(a.po + row_out * a.c.D, orow, a.c.D * 4);
+                }
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            }
+        }
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    if (tid == 0 && *flag != 0) atomicCAS(a.err, 0, *flag);
+    if (warp == 1) ptx::tmem_dealloc(tmem, L::TMEM_COLS);
+}
+
+template <int DP>
+jpi_status launch_dim(const SpanTileArgs& a, const SpanMaps& m, unsigned blocks, cudaStream_t st) {
+    return a.s.ks ? kv_start(k_kv_span_t5<DP, true>, dim3(blocks), StSmem<DP, true>::THREADS, StSmem<DP, true>::BYTES, false, st, m, a)
+                  : kv_start(k_kv_span_t5<DP, false>, dim3(blocks), StSmem<DP, false>::THREADS, StSmem<DP, false>::BYTES, false, st, m, a);
+}
+
+template <int DP>
+jpi_status prepare_dim() {
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_t5<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, StSmem<DP, false>::BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_t5<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, StSmem<DP, true>::BYTES));
+    return JPI_OK;
+}
+
+// Rows of the cache that the tokens of a tile see at most.
+long long tile_span(const KvCall& c, const KvSpan& s) {
+    const long long toks = std::min<long long>(c.tokens, (ST_ROWS + c.gq - 1) / c.gq + 1);
+    return std::min<long long>(c.own.rows, (long long)s.window + toks + std::min(s.sink, c.own.rows) + ST_KEYS);
+}
+
+}  // namespace
+
+jpi_status kv_span_tiles_prepare(const jpi_kv_handle* h) {
+    if (!h->bf16 || h->D < 64) return JPI_OK;
+    return h->D <= 64 ? prepare_dim<64>() : h->D <= 128 ? prepare_dim<128>() : prepare_dim<256>();
+}
+
+int kv_span_tiles_plan(const jpi_kv_handle* h, const KvCall& c, const KvSpan& s, long long room) {
+    if (!h->bf16 || c.D < 64 || h->tiles == 0) return 0;
+    const long long R = (long long)c.tokens * c.gq, tiles = (R + ST_ROWS - 1) / ST_ROWS, blocks = tiles * c.K * c.batch;
+    const long long span = tile_span(c, s), nb = (span + ST_KEYS - 1) / ST_KEYS;
+    KvMapDims m;
+    if (!s.ks && !kv_map_dims(c.own, c.K, c.D, c.batch, &m)) return 0;
+    if (blocks * nb >= 1ll << 31) return 0;
+    if (h->tiles < 0 && (R < ST_LEAST || (R + KR_ROWS - 1) / KR_ROWS * c.K * c.batch * span * c.D <= ST_ROW_ELEMENTS)) return 0;
+    // Splits by which the waves of blocks end first, in key blocks' time: a block has its start and end beside its keys, a result in
+    // parts its combine and its rows to and from the workspace.
+    long long best = 1, best_time = -1;
+    for (long long n = 1; n <= std::min({nb, room, std::max(1ll, 2ll * h->num_sms / blocks)}); ++n) {
+        const long long time = (blocks * n + h->num_sms - 1) / h->num_sms * ((nb + n - 1) / n + ST_FIXED) +
+                               (n > 1 ? 7 + n * ((long long)c.batch * c.tokens * c.H * c.D * 4 >> 10) / 3900 : 0);
+        if (best_time < 0 || time < best_time) {
+            best_time = time;
+            best = n;
+        }
+    }
+    return (int)best;
+}
+
+jpi_status launch_kv_span_tiles(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, int splits, float* po, float2* pml, void* out, float* lse,
+                                cudaStream_t st) {
+    SpanTileArgs a = {};
+    SpanMaps maps = {};
+    a.c = c;
+    a.s = s;
+    a.c2 = KR_LOG2E * c.scale;
+    a.splits = splits;
+    a.tiles = (int)(((long long)c.tokens * c.gq + ST_ROWS - 1) / ST_ROWS);
+    a.by_splits = KvDiv((uint32_t)a.splits);
+    a.by_tiles = KvDiv((uint32_t)a.tiles);
+    a.po = po;
+    a.pml = pml;
+    a.rows = (long long)c.batch * c.tokens * c.H;
+    a.out = splits == 1 ? static_cast<__nv_bfloat16*>(out) : nullptr;
+    a.lse = lse;
+    a.err = h->dev_err;
+    if (!s.ks) {
+        KvMapDims m;
+        if (!kv_map_dims(c.own, c.K, c.D, c.batch, &m) || !kv_make_map(m, c.own.k, c.D, ST_KEYS, &maps.k) ||
+            !kv_make_map(m, c.own.v, c.D, ST_KEYS, &maps.v)) {
+            set_error("cuTensorMapEncodeTiled refused the cache");
+            return JPI_ERR_CUDA;
+        }
+        a.at = make_int3(m.at_head, m.at_row, m.at_cache);
+    }
+    const unsigned blocks = (unsigned)((long long)a.tiles * splits * c.K * c.batch);
+    return c.D <= 64 ? launch_dim<64>(a, maps, blocks, st) : c.D <= 128 ? launch_dim<128>(a, maps, blocks, st) : launch_dim<256>(a, maps, blocks, st);
+}
+
+}  // namespace jpi
