@@ -258,9 +258,8 @@ JPI_API jpi_status jpi_kv8_append(jpi_kv_handle* h, const void* q, long long q_s
  * jpi_kv_attend_window (0: all of them, and `sink` is not used). q, out and lse are as in jpi_kv_attend, of the handle's type; so
  * are empty rows, and NaN in what a query sees.
  * Scores, softmax and sums in fp32, codes and scales taken as they are. JPI_BF16 mode: queries enter the first product scaled by a
- * power of two as fp16 (bf16's eight bits whole; an element below 2^-14 of its head's largest is off by at most 2^-25 of that)
- * or as bf16, the probabilities the second as two fp16 terms (2^-22 of each, or 2^-31 of what the largest value of the blocks
- * seen would weigh) or, on the 128-row tiles, as bf16 once (2^-8).
+ * power of two as fp16 (bf16's eight bits whole; an element below 2^-14 of its head's largest is off by at most 2^-25 of that), the probabilities the second as fp16, on the 128-row tiles once (off by at most 2^-11 of each, or 2^-28 of what
+ * the largest value of the blocks seen would weigh), else in two terms (2^-22 and 2^-31).
  */
 JPI_API jpi_status jpi_kv8_attend(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
                                   const jpi_kv8_cache* cache, const int* seen, int window, int sink, void* out,

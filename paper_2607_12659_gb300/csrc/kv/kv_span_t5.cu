@@ -6,16 +6,17 @@
 //   warp 3  one thread: O += P_i V_i (M = 128, N = D, K = 64), V read as an MN-major operand
 //   warps 4-  groups of eight: two threads per query row, half of a block's keys each: maximum, 2^x, probabilities back to
 //           tensor memory, over the scores they come from. To D = 128 two groups take the even and the odd blocks, each with a
-//           maximum, sum and output of its own, joined at the end. O is rescaled only when a block's maximum passes the running
-//           one by more than 8 in log2 units.
-//   8-bit caches: eight more warps read codes ahead into registers and write them to the ring's slots as fp16 numbers, which
+//           maximum, sum and output of its own, joined at the end. At D = 256 tensor memory holds one output and two score buffers,
+//           which a block keeps for twice the time of a softmax, so that a second group would wait. O is rescaled only when a block's maximum passes the running one by more
+//           than ST_RESCALE.
+//   8-bit caches: four more warps read codes ahead into registers and write them to the ring's slots as fp16 numbers, which
 //           e4m3 is a subset of: one instruction for two, half a tile's shared-memory writes a thread. Then both products take fp16: the
 //           queries at a power of two of each row's own (that its maximum and scale know of), the probabilities times
-//           the scale of their block's values relative to the largest 2^e that the row has seen, p 2^(e_j - e) 2^7 <= 2^15. (As bf16
+//           the scale of their block's values relative to the largest 2^e that the row has seen, p 2^(e_j - e) 2^4 <= 2^15. (As bf16
 //           numbers with the scales in them the codes would take five instructions more a pair, which the softmax needs.)
 // The query rows are gathered by the softmax threads into tensor memory as the A operand of the score products.
 //
-// Probabilities are rounded to the operands' type once: each off by at most 2^-8 of itself, fp16 2^-11 or 2^-32 of 2^(e + 7).
+// Probabilities are rounded to the operands' type once: each off by at most 2^-8 of itself; in fp16 2^-11, or 2^-29 times 2^(e - e_j).
 //
 // Rows of the cache that no query row of the tile sees may hold anything: their scores are replaced, and their values are
 // cleared in shared memory before the product, since 0 times a NaN would reach every row. Blocks that only some of the query
@@ -41,9 +42,13 @@ namespace {
 constexpr int ST_ROWS = 128;
 constexpr int ST_KEYS = 64;
 constexpr int ST_SOFT = 256;    // threads of a softmax group
-constexpr int ST_CONV = 256;    // threads that write codes to the ring: half of them keys, half values
+constexpr int ST_CONV = 128;    // threads that write codes to the ring: half of them keys, half values
 constexpr uint64_t ST_WAIT_NS = 200ull * 1000 * 1000;
-constexpr float ST_RESCALE = 8.f;   // log2 units
+// How far a block's maximum passes the running one, in log2 units, before the outputs are rescaled, which takes longer than a block's
+// softmax: a probability of bf16 has fp32's range, and the sums have room for 2^24 times what they would be. One of fp16 is at most
+// 2^ST_RESCALE8 ST_BOOST.
+constexpr float ST_RESCALE = 24.f, ST_RESCALE8 = 11.f;
+constexpr int ST_BOOST = 4;         // log2 of what probabilities of fp16 are multiplied by
 constexpr int ST_NONE = -4096;      // no scale seen yet
 // Query rows of a request and KV head from which a call takes the tiles, and the elements of keys up to which it stays with the row
 // kernel all the same, which reads a key once for every 8 query rows.
@@ -79,7 +84,7 @@ struct StSmem {
     static constexpr int NG = DP == 256 ? 1 : 2;            // softmax groups
     static constexpr int CONV = 128 + NG * ST_SOFT;         // first thread of those that convert
     static constexpr int THREADS = CONV + (Q8 ? ST_CONV : 0);
-    static constexpr int REGS = NG == 1 ? 96 : 72;
+    static constexpr int REGS = 65536 / THREADS / 8 * 8;
     static constexpr int NB = DP == 256 ? 2 : 3;            // score buffers
     static constexpr int XM_OFF = RING;                     // [groups][2 blocks][2 key halves][128 rows]
     static constexpr int ML_OFF = XM_OFF + NG * 4 * ST_ROWS * 4;    // [groups][128 rows] (m, l)
@@ -94,8 +99,6 @@ struct StSmem {
     static_assert(TMEM_Q + DP / 2 <= TMEM_COLS, "scores, outputs and queries fit");
 };
 
-// Whether one of two fp16 values is an infinity or NaN.
-__device__ __forceinline__ bool bad_half_pair(uint32_t x) { return (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u; }
 __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -132,9 +135,9 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
 
     const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
     ptx::grid_dep_launch();
-    // Row tiles fastest: the blocks that read the same keys run together.
+    // Row tiles fastest: the blocks that read the same keys run together; the last ones first, whose tokens see most.
     uint32_t tile, split, kvh;
-    const int cache = (int)a.c.by_K.div(a.by_splits.div(a.by_tiles.div(blockIdx.x, tile), split), kvh);
+    const int cache = (int)a.c.by_K.div(a.by_splits.div(a.by_tiles.div(gridDim.x - 1 - blockIdx.x, tile), split), kvh);
     RowTile t;
     t.tok0 = (long long)cache * a.c.tokens;
     t.head0 = (int)kvh * a.c.gq;
@@ -446,7 +449,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         }
         const float c2s = fminf(a.c2 * qs, 3e38f);
         const uint64_t c2 = pair2(c2s);
-        const float rescale = fminf(ST_RESCALE / c2s, 3e38f);
+        const float rescale = fminf((Q8 ? ST_RESCALE8 : ST_RESCALE) / c2s, 3e38f);
         // Scales of block i: of its four tiles' values, of the half's two tiles' keys (a tile that no row sees has none: 127).
         const uint8_t* const ksc = Q8 ? sn.ks + ((long long)cache * a.c.K + kvh) * sn.nblk : nullptr;
         const uint8_t* const vsc = Q8 ? sn.vs + ((long long)cache * a.c.K + kvh) * sn.nblk : nullptr;
@@ -521,7 +524,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int at = half ? (int)ve[2 + e] : (int)ve[e];
-                    pv[e] = at == 255 || v_now == ST_NONE ? 0x1p7f : kv8_pow2(min(134 + at - v_now, 254));
+                    pv[e] = at == 255 || v_now == ST_NONE ? (float)(1 << ST_BOOST) : kv8_pow2(min(127 + ST_BOOST + at - v_now, 254));
                 }
                 if (i + NG < nb) scales(i + NG);
             }
@@ -531,13 +534,15 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                 if (good) good = ptx::mbar_wait_bounded(&gdone[grp], (i / NG - 1) & 1, ST_WAIT_NS);
                 ptx::tc_fence_after();
 #pragma unroll 1
-                for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 16) {
-                    uint32_t ro[16];
-                    ptx::tmem_ld_x16(out + (uint32_t)c0, ro);
+                for (int c0 = half * (DP / 2); c0 < (half + 1) * (DP / 2); c0 += 32) {
+                    uint32_t ro[2][16];
+                    ptx::tmem_ld_x16(out + (uint32_t)c0, ro[0]);
+                    ptx::tmem_ld_x16(out + (uint32_t)(c0 + 16), ro[1]);
                     ptx::tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) ro[j] = __float_as_uint(__uint_as_float(ro[j]) * beta);
-                    ptx::tmem_st_x16(out + (uint32_t)c0, ro);
+                    for (int j = 0; j < 32; ++j) ro[j >> 4][j & 15] = __float_as_uint(__uint_as_float(ro[j >> 4][j & 15]) * beta);
+                    ptx::tmem_st_x16(out + (uint32_t)c0, ro[0]);
+                    ptx::tmem_st_x16(out + (uint32_t)(c0 + 16), ro[1]);
                 }
                 ptx::tmem_st_wait();
             }
@@ -560,21 +565,23 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             }
             l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
             // Keys of the block that some row sees and some does not; rows that none sees. The same for all threads.
-            const bool cut = low < min(most, key0 + ST_KEYS) || (key0 < late && key0 + ST_KEYS > sn.sink);
+            const bool cut = max(key0, low) < min(key0 + ST_KEYS, most) || max(max(key0, sn.sink), first) < min(key0 + ST_KEYS, late);
             const bool dead = most < key0 + ST_KEYS || (key0 < first && key0 + ST_KEYS > sn.sink);
             uint8_t* vb = stages + i % NS * L::STAGE + L::KVBYTES;
             if (cut) {
                 // Is there an infinity or NaN among the values?
                 if (good) good = ptx::mbar_wait_bounded(&vfull[i % NS], (i / NS) & 1, ST_WAIT_NS);
-                bool odd = false;
-                for (int e = (tid - 128) % ST_SOFT; e < ST_KEYS * NDB * 8; e += ST_SOFT) {
-                    const int key = e / (NDB * 8), p = e % (NDB * 8);
-                    if (!span_sees(sn, key0 + key, most, first)) continue;
-                    const uint4 v = *(const uint4*)(vb + (p / 8) * (ST_KEYS * 128) + key * 128 + (p % 8) * 16);
-                    if (Q8) odd = odd || bad_half_pair(v.x) || bad_half_pair(v.y) || bad_half_pair(v.z) || bad_half_pair(v.w);
-                    else odd = odd || bad_pair(v.x) || bad_pair(v.y) || bad_pair(v.z) || bad_pair(v.w);
+                uint32_t top = 0;   // the largest magnitudes, 16 bits each
+#pragma unroll
+                for (int e0 = 0; e0 < ST_KEYS * NDB * 8; e0 += ST_SOFT) {
+                    const int e = e0 + (tid - 128) % ST_SOFT, key = e / (NDB * 8), p = e % (NDB * 8);
+                    uint4 v = *(const uint4*)(vb + (p / 8) * (ST_KEYS * 128) + key * 128 + (p % 8) * 16);
+                    if (!span_sees(sn, key0 + key, most, first)) v = make_uint4(0, 0, 0, 0);
+                    top = __vmaxu2(__vmaxu2(top, v.x & 0x7fff7fffu), v.y & 0x7fff7fffu);
+                    top = __vmaxu2(__vmaxu2(top, v.z & 0x7fff7fffu), v.w & 0x7fff7fffu);
                 }
-                if (group_any(11 + grp, ST_SOFT, odd)) {
+                constexpr uint32_t INF = Q8 ? 0x7c00u : 0x7f80u;
+                if (group_any(11 + grp, ST_SOFT, (top & 0xffffu) >= INF || top >> 16 >= INF)) {
                     // Row by row: first one half's keys, then the other's, onto the settled output of the blocks before.
                     if (i >= NG && good) good = ptx::mbar_wait_bounded(&gdone[grp], (i / NG - 1) & 1, ST_WAIT_NS);
                     ptx::tc_fence_after();
@@ -656,9 +663,10 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         if (good) good = ptx::mbar_wait_bounded(alldone, 0, ST_WAIT_NS);
         ptx::tc_fence_after();
         if (!good) *flag = DEV_TIMEOUT_MMA;
-        // The groups' outputs are joined on the way: w_g = 2^((m_g - M) c), nothing of a group in which the row saw no key.
+        // The groups' sums are joined, and their outputs on the way: w_g = 2^((m_g - M) c), nothing of a group in which the row saw no
+        // key.
         float w = 1.f;
-        bool some = l != 0.f;
+        const bool some = l != 0.f;
         if (NG > 1) {
             if (half == 0) ml[grp * ST_ROWS + row] = make_float2(m_used, l);
             ptx::named_bar_sync(9, NG * ST_SOFT);
@@ -668,14 +676,16 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             l = w * l + (other.x == -INFINITY ? 0.f : kr_ex2((other.x - M) * c2s)) * other.y;   // (0 times a NaN sum is NaN)
             m_used = M;
         }
+        float vscale = 1.f;
         if constexpr (Q8) {
             m_used *= qs;
-            w = v_used == ST_NONE ? w : w * 0x1p-7f;
+            w *= 1.f / (1 << ST_BOOST);
+            vscale = v_used == ST_NONE ? 1.f : kv8_scale((uint32_t)v_used);
         }
-        const float vscale = Q8 && v_used != ST_NONE ? kv8_scale((uint32_t)v_used) : 1.f;
-        // A result is scaled by 1 / l and rounded on its way; a half row's 16-bit values go where its own 32-bit ones were.
+        // A result is scaled by 1 / l and rounded on its way.
         const float inv = l == 0.f ? 0.f : 1.f / l;   // (0: the row saw no key; a NaN score makes l, and so the row, NaN)
         uint8_t* orow = st_smem + row * L::OUT_LD;
+        // A half row's 16-bit values go where its own 32-bit ones were.
 #pragma unroll 1
         for (int turn = 0; turn < NG; ++turn) {
             if (turn == grp) {
@@ -686,7 +696,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                     ptx::tmem_ld_x16(out + (uint32_t)(c0 + 16), v[1]);
                     ptx::tmem_ld_wait();
                     // (a wait that gave up may have left copies on their way into the ring)
-                    if (good && (mine > 0 || (a.out && nb > 0))) {
+                    if (good && (mine > 0 || nb > 0)) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             uint4* dst = (uint4*)(orow + (c0 + 4 * k) * 4);

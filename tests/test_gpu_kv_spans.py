@@ -2,7 +2,8 @@
 
 Tolerances are those of the other attention tests (test_gpu_kv.py): worst-case bounds from the formats and the lengths of the sums.
 Over an 8-bit cache a query may enter the first product as fp16 at a power of two of its own (an element off by at most 2^-25 of
-its head's largest), and a probability as two fp16 terms (off by at most 2^-31 of what the largest value would weigh).
+its head's largest), and a probability the second as fp16: off by half of fp16's least step 2^-24, in units of 2^-4 of a
+probability times the largest scale seen, under which a value is at most 448 and the largest at least half of that: 2^-28 of the largest.
 """
 
 import math
@@ -44,7 +45,7 @@ def tols(q, k, v, n, dtype, ref, dot, mass, lse, scale):
     rel = (D + 2) * 2.0 ** -22 * dot + 2.0 ** -20 + n * 2.0 ** -23 + 2.0 ** -22 * np.where(np.isinf(lse), 0, np.abs(lse))
     rel = rel + scale * 2.0 ** -24 * np.abs(q).max(-1) * np.nanmax(np.abs(np.where(np.isfinite(k), k, 0)).sum(-1))
     big = np.abs(np.where(np.isfinite(v), v, 0)).max()
-    out = HALF_EPS[dtype] * np.abs(ref) + (2 * rel[..., None] + (2.0 ** -8 if dtype == "bf16" else 0)) * mass + n * 2.0 ** -30 * big + 1e-37
+    out = HALF_EPS[dtype] * np.abs(ref) + (2 * rel[..., None] + (2.0 ** -8 if dtype == "bf16" else 0)) * mass + n * 2.0 ** -28 * big + 1e-37
     return out, rel + 1e-6
 
 
