@@ -24,7 +24,7 @@
 // its own keys), and the product adds nothing. A row that sees nothing has l = 0, and what its outputs hold is not used.
 //
 // Each block leaves a part (unnormalised fp32 rows, (m, l)) for the combine, or the result: rows pass through shared
-// memory (the ring, free by then) and leave by bulk copies.
+// memory (the ring, free by then).
 //
 // Every wait is bounded; a wait that gives up records an error in the handle's word, and its thread waits for
 // nothing more.
@@ -76,7 +76,7 @@ struct SpanTileArgs {
 
 template <int DP, bool Q8>
 struct StSmem {
-    static constexpr int NS = DP == 256 ? 2 : DP == 128 ? 3 : 4;
+    static constexpr int NS = Q8 ? (DP == 256 ? 2 : 3) : DP == 256 ? 3 : 5;
     static constexpr int KVBYTES = ST_KEYS * DP * 2;
     static constexpr int STAGE = 2 * KVBYTES;               // ring slot: K, then V
     static constexpr int OUT_LD = DP * 4 + 16;              // bytes of a staged output row: the pad spreads the banks
@@ -86,7 +86,9 @@ struct StSmem {
     static constexpr int THREADS = CONV + (Q8 ? ST_CONV : 0);
     static constexpr int REGS = 65536 / THREADS / 8 * 8;
     static constexpr int NB = DP == 256 ? 2 : 3;            // score buffers
-    static constexpr int XM_OFF = RING;                     // [groups][2 blocks][2 key halves][128 rows]
+    static constexpr int RAW = DP == 256 ? 2 : 4;           // 8 bits: blocks of codes on their way
+    static constexpr int RAWBYTES = ST_KEYS * DP * 2;       // of a block's keys and values
+    static constexpr int XM_OFF = RING + (Q8 ? RAW * RAWBYTES : 0);   // [groups][2 blocks][2 key halves][128 rows]
     static constexpr int ML_OFF = XM_OFF + NG * 4 * ST_ROWS * 4;    // [groups][128 rows] (m, l)
     static constexpr int QM_OFF = ML_OFF + NG * ST_ROWS * 8;        // [2 halves of d][128 rows] largest |q|
     static constexpr int BAR_OFF = QM_OFF + 2 * ST_ROWS * 4;
@@ -143,6 +145,34 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
     t.head0 = (int)kvh * a.c.gq;
     t.R = a.c.tokens * a.c.gq;
     t.r0 = (int)tile * ST_ROWS;
+    // The softmax warps' query rows, on their way while the block sets itself up: 64-element blocks (warp - 4) / 4,
+    // + 2, of the rows of the warp's TMEM lanes.
+    constexpr int QN = (NDB + 1) / 2;
+    uint4 qv[QN][8];
+    if (warp >= 4 && warp < 12) {
+        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q);
+        // Row 4 i + (lane / 8): its token and head, stepped by 4 rows.
+        int r = t.r0 + (warp & 3) * 32 + (lane >> 3);
+        int tok = r / a.c.gq, hd = r - tok * a.c.gq;
+        const int tok4 = 4 / a.c.gq, hd4 = 4 - tok4 * a.c.gq;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool in = r < t.R;
+            const __nv_bfloat16* row = q + (in ? (t.tok0 + tok) * a.c.q_stride + (long long)(t.head0 + hd) * a.c.D : 0);
+#pragma unroll
+            for (int k = 0; k < QN; ++k) {
+                const int d = 64 * (((warp - 4) >> 2) + 2 * k) + 8 * (lane & 7);
+                qv[k][i] = kr_ld(row + d, in && d < a.c.D);
+            }
+            r += 4;
+            tok += tok4;
+            hd += hd4;
+            if (hd >= a.c.gq) {
+                hd -= a.c.gq;
+                ++tok;
+            }
+        }
+    }
     const KvSpan& sn = a.s;
     // Of the tile's tokens that see anything: the largest and the least count, the first and the last first row.
     int most = 0, low = 0x7fffffff, first = 0x7fffffff, late = 0;
@@ -206,34 +236,6 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
     if (warp == 1) {
         ptx::tmem_alloc(tmem_slot, L::TMEM_COLS);
         ptx::tmem_relinquish();
-    }
-    // The softmax warps' query rows, on their way while the block sets itself up: 64-element blocks (warp - 4) / 4,
-    // + 2, of the rows of the warp's TMEM lanes.
-    constexpr int QN = (NDB + 1) / 2;
-    uint4 qv[QN][8];
-    if (warp >= 4 && warp < 12) {
-        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.c.q);
-        // Row 4 i + (lane / 8): its token and head, stepped by 4 rows.
-        int r = t.r0 + (warp & 3) * 32 + (lane >> 3);
-        int tok = r / a.c.gq, hd = r - tok * a.c.gq;
-        const int tok4 = 4 / a.c.gq, hd4 = 4 - tok4 * a.c.gq;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool in = r < t.R;
-            const __nv_bfloat16* row = q + (in ? (t.tok0 + tok) * a.c.q_stride + (long long)(t.head0 + hd) * a.c.D : 0);
-#pragma unroll
-            for (int k = 0; k < QN; ++k) {
-                const int d = 64 * (((warp - 4) >> 2) + 2 * k) + 8 * (lane & 7);
-                qv[k][i] = kr_ld(row + d, in && d < a.c.D);
-            }
-            r += 4;
-            tok += tok4;
-            hd += hd4;
-            if (hd >= a.c.gq) {
-                hd -= a.c.gq;
-                ++tok;
-            }
-        }
     }
     ptx::tc_fence_before();
     __syncthreads();
@@ -311,53 +313,57 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             if (!good) *flag = DEV_TIMEOUT_MMA;
         }
     } else if (Q8 && tid >= L::CONV) {
-        // Codes to fp16 numbers in the layout of the copies: 16 codes of a row are two 16-byte chunks of a 128-byte line.
-        constexpr int PIECES = DP / 16, MINE = ST_KEYS * PIECES / (ST_CONV / 2), SWEEP = ST_CONV / 2 / PIECES;   // rows of a sweep
-        const bool is_v = tid >= L::CONV + ST_CONV / 2;
-        const int x = (tid - L::CONV) % (ST_CONV / 2), piece = x % PIECES, row0 = x / PIECES;
+        // Codes to fp16 numbers in the layout of the copies: 16 codes of a row are two 16-byte chunks of a 128-byte line. Each thread
+        // copies pieces of its own ahead, and waits for no other's. Rows that no query row sees arrive as zeros.
+        constexpr int PIECES = DP / 16, HALFT = ST_CONV / 2, MINE = ST_KEYS * PIECES / HALFT, SWEEP = HALFT / PIECES;   // rows of a sweep
+        const bool is_v = tid >= L::CONV + HALFT;
+        // Eight lanes are four pieces of a 128-byte line in two rows, whose chunks lie in eight places of the banks.
+        const int x = (tid - L::CONV) % HALFT, piece = (x & 3) | (x >> 3) % (PIECES / 4) << 2, row0 = (x >> 2 & 1) + 2 * ((x >> 3) / (PIECES / 4));
         uint64_t* fullb = is_v ? vfull : kfull;
         uint64_t* emptyb = is_v ? vempty : kempty;
         const bool in = 16 * piece < a.c.D;
-        const uint8_t* src = static_cast<const uint8_t*>(is_v ? a.c.own.v : a.c.own.k) + cache * a.c.own.cs + kvh * a.c.own.hs + 16 * piece;
-        const uint8_t* scale = (is_v ? sn.vs : sn.ks) + ((long long)cache * a.c.K + kvh) * sn.nblk;
-        uint4 code[MINE];
-        // (a row that no query row sees arrives as zeros, one under a scale that is NaN as NaN)
+        const uint8_t* src = static_cast<const uint8_t*>(is_v ? a.c.own.v : a.c.own.k) + cache * a.c.own.cs + kvh * a.c.own.hs + (in ? 16 * piece : 0);
+        uint8_t* const raw = st_smem + L::RING + is_v * (L::RAWBYTES / 2) + x * 16;
         auto fetch = [&](int i) {
-            const int key0 = blocks.row(blk0 + i) + row0;
+            if (i < nb) {
+                const int key0 = blocks.row(blk0 + i) + row0;
+                const uint32_t to = ptx::smem_u32(raw + i % L::RAW * L::RAWBYTES);
 #pragma unroll
-            for (int m = 0; m < MINE; ++m) {
-                const int key = key0 + m * SWEEP;
-                const bool live = in && span_sees(sn, key, most, first);
-                code[m] = live ? __ldg(reinterpret_cast<const uint4*>(src + key * a.c.own.rs)) : make_uint4(0, 0, 0, 0);
-                if (live && scale[key >> sn.n_log2] == 255) code[m] = make_uint4(0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f);
+                for (int m = 0; m < MINE; ++m) {
+                    const int key = key0 + m * SWEEP;
+                    const bool live = in && span_sees(sn, key, most, first);
+                    ptx::cp_async_16(to + m * (HALFT * 16), live ? src + key * a.c.own.rs : src, live);
+                }
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
         bool good = true;
-        if (nb > 0) fetch(0);
+#pragma unroll
+        for (int i = 0; i < L::RAW - 1; ++i) fetch(i);
         for (int i = 0; i < nb; ++i) {
             const int sl = i % NS;
+            fetch(i + L::RAW - 1);
             if (good && i >= NS) good = ptx::mbar_wait_bounded(&emptyb[sl], (i / NS - 1) & 1, ST_WAIT_NS);
             // (the query rows pass through the last value slots)
             if (good && is_v && i >= NS - L::QS && i < NS) good = ptx::mbar_wait_bounded(qready, 0, ST_WAIT_NS);
             if (!good) break;
-            uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0) + piece / 4 * (ST_KEYS * 128);
+            asm volatile("cp.async.wait_group %0;" ::"n"(L::RAW - 1) : "memory");
+            // Chunk c of row r lies at c ^ (r & 7) of its line; a sweep is four rows, or a multiple of eight.
+            static_assert(SWEEP == 4 || SWEEP % 8 == 0, "rows of a sweep");
+            uint8_t* base = stages + sl * L::STAGE + (is_v ? L::KVBYTES : 0) + piece / 4 * (ST_KEYS * 128) + row0 * 128;
+            const uint32_t place = (uint32_t)((2 * (piece & 3)) ^ (row0 & 7)) << 4;
 #pragma unroll
             for (int m = 0; m < MINE; ++m) {
-                const int r = row0 + m * SWEEP;
-                const uint32_t c[4] = {code[m].x, code[m].y, code[m].z, code[m].w};
-                uint4 h[2];
-                h[0] = make_uint4(kv8_half2(c[0]), kv8_half2(c[0] >> 16), kv8_half2(c[1]), kv8_half2(c[1] >> 16));
-                h[1] = make_uint4(kv8_half2(c[2]), kv8_half2(c[2] >> 16), kv8_half2(c[3]), kv8_half2(c[3] >> 16));
-                // Neighbouring 128-byte lines begin with the other chunk: eight lanes, eight places in the banks.
-                const int odd = piece >> 2 & 1;
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    *reinterpret_cast<uint4*>(base + r * 128 + (((2 * (piece & 3) + (e ^ odd)) ^ (r & 7)) << 4)) = (e ^ odd) ? h[1] : h[0];
+                const uint4 c = *reinterpret_cast<const uint4*>(raw + i % L::RAW * L::RAWBYTES + m * (HALFT * 16));
+                uint8_t* line = base + m * (SWEEP * 128);
+                const uint32_t at = place ^ (uint32_t)((m * SWEEP & 7) << 4);
+                *reinterpret_cast<uint4*>(line + at) = make_uint4(kv8_half2(c.x), kv8_half2(c.x >> 16), kv8_half2(c.y), kv8_half2(c.y >> 16));
+                *reinterpret_cast<uint4*>(line + (at ^ 16)) = make_uint4(kv8_half2(c.z), kv8_half2(c.z >> 16), kv8_half2(c.w), kv8_half2(c.w >> 16));
             }
-            if (i + 1 < nb) fetch(i + 1);
             ptx::fence_proxy_async_smem();
             ptx::mbar_arrive(&fullb[sl]);
         }
+        ptx::cp_async_wait_all();   // (nothing may land once the block has left)
         if (!good) *flag = DEV_TIMEOUT_WEIGHTS;
     } else {
         const int grp = (warp - 4) >> 3, row = (warp & 3) * 32 + lane, half = ((warp - 4) >> 2) & 1;
@@ -479,7 +485,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             if constexpr (Q8) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint64_t by = pair2(ke[e] == 255 ? 1.f : kv8_scale(ke[e]));   // (the slot's numbers are NaN then)
+                    const uint64_t by = pair2(kv8_scale(ke[e]));
 #pragma unroll
                     for (int j = 0; j < 16; j += 2) {
                         uint64_t v;
@@ -510,13 +516,16 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             const float alpha = !move ? 1.f : m_used == -INFINITY ? 0.f : kr_ex2((m_used - mb) * c2s);
             float beta = alpha;               // what the outputs are multiplied by: in units of the largest scale, too
             bool grown = false;
-            float pv[2] = {1.f, 1.f};         // what the probabilities of the half's tiles are
+            float pv[2] = {1.f, 1.f};         // what the probabilities of the half's tiles are multiplied by
+            uint32_t nan = 0;                 // tiles of the half whose values are NaN
             if constexpr (Q8) {
                 int v_now = v_used;
+                if (__any_sync(0xffffffffu, (int)max(max(ve[0], ve[1]), max(ve[2], ve[3])) > v_used)) {   // (else no row has to look)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int at = key0 + 16 * e;
-                    if (ve[e] != 255 && at < vis && (at < sn.sink || at + 16 > begins)) v_now = max(v_now, max((int)ve[e], 1));
+                    for (int e = 0; e < 4; ++e) {
+                        const int at = key0 + 16 * e;
+                        if (ve[e] != 255 && at < vis && (at < sn.sink || at + 16 > begins)) v_now = max(v_now, max((int)ve[e], 1));
+                    }
                 }
                 grown = v_now != v_used;
                 if (grown) beta *= kv8_pow2(127 + v_used - v_now);
@@ -524,6 +533,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int at = half ? (int)ve[2 + e] : (int)ve[e];
+                    if (at == 255) nan |= 1u << e;
                     pv[e] = at == 255 || v_now == ST_NONE ? (float)(1 << ST_BOOST) : kv8_pow2(min(127 + ST_BOOST + at - v_now, 254));
                 }
                 if (i + NG < nb) scales(i + NG);
@@ -562,6 +572,12 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                 p1 = kr_ex2(p1);
                 l4[(k >> 1) & 3] += p0 + p1;
                 pk[k / 2] = Q8 ? half_pair(p0 * pv[k >> 4], p1 * pv[k >> 4]) : kr_pack(p0, p1);
+            }
+            // Values under a scale that is NaN are NaN to the rows that see them, by way of their probabilities.
+            if (Q8 && nan) {
+#pragma unroll
+                for (int k = 0; k < HK; ++k)
+                    if ((nan >> (k >> 4) & 1) && sees(k)) pk[k / 2] |= k & 1 ? 0x7fff0000u : 0x7fffu;
             }
             l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
             // Keys of the block that some row sees and some does not; rows that none sees. The same for all threads.
@@ -696,7 +712,8 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                     ptx::tmem_ld_x16(out + (uint32_t)(c0 + 16), v[1]);
                     ptx::tmem_ld_wait();
                     // (a wait that gave up may have left copies on their way into the ring)
-                    if (good && (mine > 0 || nb > 0)) {
+                    if (good && nb > 0) {
+                        uint4 packed;
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             uint4* dst = (uint4*)(orow + (c0 + 4 * k) * 4);
@@ -714,10 +731,11 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                                 x[2] += __uint_as_float(y.z);
                                 x[3] += __uint_as_float(y.w);
                             }
-                            if (a.out && grp == NG - 1) {
-                                uint32_t* dst16 = (uint32_t*)(orow + half * (DP * 2) + (c0 + 4 * k - half * (DP / 2)) * 2);
-                                dst16[0] = kr_pack(x[0] * inv, x[1] * inv);
-                                dst16[1] = kr_pack(x[2] * inv, x[3] * inv);
+                            if (a.out && grp == NG - 1) {   // 16 bytes for every two of these
+                                uint32_t* p = (k & 1) ? &packed.z : &packed.x;
+                                p[0] = kr_pack(x[0] * inv, x[1] * inv);
+                                p[1] = kr_pack(x[2] * inv, x[3] * inv);
+                                if (k & 1) *(uint4*)(orow + half * (DP * 2) + (c0 + 4 * (k - 1) - half * (DP / 2)) * 2) = packed;
                             } else {
                                 *dst = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
                             }
@@ -727,31 +745,23 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             }
             if (turn + 1 < NG) ptx::named_bar_sync(10, NG * ST_SOFT);
         }
-        if (grp == NG - 1) {
-            ptx::fence_proxy_async_smem();
-            ptx::named_bar_sync(pair_bar, 64);
-            if (half == 0 && valid) {
-                const long long row_at = row_index(a.c, t, r), row_out = (long long)split * a.rows + row_at;
-                auto copy = [&](void* dst, const uint8_t* src, int bytes) {
-                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(ptx::smem_u32(src)),
-                                 "r"(bytes)
-                                 : "memory");
-                };
-                if (a.out) {
-                    __nv_bfloat16* dst = a.out + row_at * a.c.D;
-                    if (a.lse) a.lse[row_at] = l == 0.f ? -INFINITY : fmaf(m_used, a.c.scale, logf(l));
-                    if (nb == 0) {
-                        for (int d = 0; d < a.c.D; d += 8) *(uint4*)(dst + d) = make_uint4(0, 0, 0, 0);
-                    } else if (good) {
-                        copy(dst, orow, min(a.c.D, DP / 2) * 2);
-                        if (a.c.D > DP / 2) copy(dst + DP / 2, orow + DP * 2, (a.c.D - DP / 2) * 2);
-                    }
-                } else {
-                    a.pml[row_at * a.splits + split] = make_float2(m_used, l);
-                    if (good && nb > 0) copy(a.po + row_out * a.c.D, orow, a.c.D * 4);
-                }
-                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        if (grp == NG - 1 && half == 0 && valid) {
+            const long long row_at = row_index(a.c, t, r);
+            if (!a.out) a.pml[row_at * a.splits + split] = make_float2(m_used, l);
+            else if (a.lse) a.lse[row_at] = l == 0.f ? -INFINITY : fmaf(m_used, a.c.scale, logf(l));
+        }
+        // Rows leave by whole warps. (A bulk copy a row, 128 of them, took 3 thousand cycles longer.)
+        ptx::named_bar_sync(9, NG * ST_SOFT);
+        for (int rr = warp - 4; good && rr < ST_ROWS && t.r0 + rr < t.R; rr += 8 * NG) {
+            const long long row_at = row_index(a.c, t, t.r0 + rr);
+            const uint8_t* from = st_smem + rr * L::OUT_LD;
+            if (a.out) {
+                const int d = 8 * lane, h = d >= DP / 2;
+                if (d < a.c.D)
+                    *(uint4*)(a.out + row_at * a.c.D + d) = nb == 0 ? make_uint4(0, 0, 0, 0) : *(const uint4*)(from + h * (DP * 2) + (d - h * (DP / 2)) * 2);
+            } else if (nb > 0) {
+                for (int d = 4 * lane; d < a.c.D; d += 128)
+                    *(uint4*)(a.po + ((long long)split * a.rows + row_at) * a.c.D + d) = *(const uint4*)(from + 4 * d);
             }
         }
     }
