@@ -50,6 +50,7 @@ constexpr uint64_t ST_WAIT_NS = 200ull * 1000 * 1000;
 constexpr float ST_RESCALE = 24.f, ST_RESCALE8 = 11.f;
 constexpr int ST_BOOST = 4;         // log2 of what probabilities of fp16 are multiplied by
 constexpr int ST_NONE = -4096;      // no scale seen yet
+constexpr int ST_RUN = 32;          // blocks of a group whose scales are read together
 // Query rows of a request and KV head from which a call takes the tiles, and the elements of keys up to which it stays with the row
 // kernel all the same, which reads a key once for every 8 query rows.
 constexpr int ST_LEAST = 32;
@@ -64,7 +65,8 @@ struct SpanTileArgs {
     KvSpan s;
     float c2;              // log2(e) * scale
     int splits, tiles;     // key ranges, row tiles of a request and KV head
-    KvDiv by_splits, by_tiles;
+    KvDiv by_splits, by_tiles, by_rest;   // (rest: splits of all caches and KV heads)
+    bool tiles_outer;
     int3 at;               // of the maps' outer dimensions: heads, rows, caches
     float* po;             // [parts][rows][D]
     float2* pml;           // [rows][parts]
@@ -91,7 +93,8 @@ struct StSmem {
     static constexpr int XM_OFF = RING + (Q8 ? RAW * RAWBYTES : 0);   // [groups][2 blocks][2 key halves][128 rows]
     static constexpr int ML_OFF = XM_OFF + NG * 4 * ST_ROWS * 4;    // [groups][128 rows] (m, l)
     static constexpr int QM_OFF = ML_OFF + NG * ST_ROWS * 8;        // [2 halves of d][128 rows] largest |q|
-    static constexpr int BAR_OFF = QM_OFF + 2 * ST_ROWS * 4;
+    static constexpr int SC_OFF = QM_OFF + 2 * ST_ROWS * 4;         // [groups][ST_RUN blocks] scales of a block's four tiles: keys, values
+    static constexpr int BAR_OFF = SC_OFF + NG * ST_RUN * 8;
     static constexpr int BYTES = BAR_OFF + 8 * (3 * NB + NG + 2 + 4 * NS + 2);
     // The query rows' way to a row per thread: 4 KB a warp in the last QS value slots, which are filled after it.
     static constexpr int TURN = KVBYTES / 4096, QS = DP == 256 ? 1 : 2;
@@ -137,9 +140,13 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
 
     const int tid = threadIdx.x, warp = ptx::warp_index(), lane = tid & 31;
     ptx::grid_dep_launch();
-    // Row tiles fastest: the blocks that read the same keys run together; the last ones first, whose tokens see most.
-    uint32_t tile, split, kvh;
-    const int cache = (int)a.c.by_K.div(a.by_splits.div(a.by_tiles.div(gridDim.x - 1 - blockIdx.x, tile), split), kvh);
+    // The last row tiles first, whose tokens see most: of all caches together where their keys stay in L2, else of one after the other, so
+    // that the blocks that read the same keys run together.
+    uint32_t tile, split, kvh, rest;
+    if (a.tiles_outer) tile = a.by_rest.div(blockIdx.x, rest);
+    else rest = a.by_tiles.div(blockIdx.x, tile);
+    tile = (uint32_t)a.tiles - 1 - tile;
+    const int cache = (int)a.c.by_K.div(a.by_splits.div(rest, split), kvh);
     RowTile t;
     t.tok0 = (long long)cache * a.c.tokens;
     t.head0 = (int)kvh * a.c.gq;
@@ -456,22 +463,28 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         const float c2s = fminf(a.c2 * qs, 3e38f);
         const uint64_t c2 = pair2(c2s);
         const float rescale = fminf((Q8 ? ST_RESCALE8 : ST_RESCALE) / c2s, 3e38f);
-        // Scales of block i: of its four tiles' values, of the half's two tiles' keys (a tile that no row sees has none: 127).
-        const uint8_t* const ksc = Q8 ? sn.ks + ((long long)cache * a.c.K + kvh) * sn.nblk : nullptr;
-        const uint8_t* const vsc = Q8 ? sn.vs + ((long long)cache * a.c.K + kvh) * sn.nblk : nullptr;
-        uint32_t ve[4] = {127, 127, 127, 127}, ke[2] = {127, 127};
-        auto scales = [&](int i) {
-            const int key0 = blocks.row(blk0 + i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int at = key0 + 16 * e;
-                const bool live = at < most && (at < sn.sink || at + 16 > first);
-                ve[e] = live ? vsc[at >> sn.n_log2] : 127;
-                if (e >> 1 == half) ke[e & 1] = live ? ksc[at >> sn.n_log2] : 127;
+        // Scales of the group's next blocks, a byte a thread (of a tile that no row sees: 127).
+        uint8_t* const sc = st_smem + L::SC_OFF + grp * ST_RUN * 8;
+        auto scales = [&](int i0) {
+            const int e = (tid - 128) % ST_SOFT, i = i0 + e / 8 * NG;
+            static_assert(ST_RUN * 8 == ST_SOFT, "one byte a thread");
+            uint8_t byte = 127;
+            if (i < nb) {
+                const int at = blocks.row(blk0 + i) + 16 * (e & 3);
+                if (at < most && (at < sn.sink || at + 16 > first))
+                    byte = (e & 4 ? sn.vs : sn.ks)[((long long)cache * a.c.K + kvh) * sn.nblk + (at >> sn.n_log2)];
             }
+            ptx::named_bar_sync(11 + grp, ST_SOFT);   // the last ones have been read
+            sc[e] = byte;
+            ptx::named_bar_sync(11 + grp, ST_SOFT);
         };
-        if (Q8 && grp < nb) scales(grp);
         for (int i = grp; i < nb; i += NG) {
+            uint2 by = make_uint2(0, 0);   // 8 bits: scales of the block's tiles, keys' and values'
+            if constexpr (Q8) {
+                const int k = i / NG % ST_RUN;
+                if (k == 0) scales(i);
+                by = *(const uint2*)(sc + 8 * k);
+            }
             if (good) good = ptx::mbar_wait_bounded(&sfull[i % NB], (i / NB) & 1, ST_WAIT_NS);
             ptx::tc_fence_after();
             uint32_t s[2][16];
@@ -482,19 +495,6 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                 ptx::tmem_ld_wait();
             }
             const int key0 = blocks.row(blk0 + i), mine = key0 + HK * half;
-            if constexpr (Q8) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint64_t by = pair2(kv8_scale(ke[e]));
-#pragma unroll
-                    for (int j = 0; j < 16; j += 2) {
-                        uint64_t v;
-                        asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(s[e][j]), "r"(s[e][j + 1]));
-                        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(by));
-                        asm("mov.b64 {%0, %1}, %2;" : "=r"(s[e][j]), "=r"(s[e][j + 1]) : "l"(v));
-                    }
-                }
-            }
             // Of this half's keys the ones that the row sees: all, or those below `end`, from `from` on or below `sunk`.
             const int end = vis - mine, from = begins - mine, sunk = sn.sink - mine;
             const bool full = __all_sync(0xffffffffu, end >= HK && (from <= 0 || sunk >= HK));
@@ -504,10 +504,32 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                 for (int j = 0; j < HK; ++j)
                     if (!sees(j)) s[j >> 4][j & 15] = __float_as_uint(-INFINITY);
             }
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            float mt[2] = {-INFINITY, -INFINITY};   // of the half's tiles
 #pragma unroll
-            for (int j = 0; j < HK; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j >> 4][j & 15]));
-            float mb = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            for (int e = 0; e < 2; ++e) {
+                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int j = 0; j < 16; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[e][j]));
+                mt[e] = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            }
+            // 8 bits: scores are the products times the scale of their tile's keys, which multiplies the maximum, and what the scores are
+            // multiplied by.
+            float kc[2] = {c2s, c2s};
+            if constexpr (Q8) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t k = by.x >> (16 * half + 8 * e) & 255u;
+                    if (k == 255) {   // NaN: so are the scores of those that see them
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) s[e][j] = sees(16 * e + j) ? 0x7fffffffu : __float_as_uint(-INFINITY);
+                        mt[e] = -INFINITY;
+                    } else {
+                        mt[e] *= kv8_scale(k);
+                        kc[e] = fmaxf(c2s * kv8_scale(k), 0x1p-126f);   // (0 times a hidden score would be NaN)
+                    }
+                }
+            }
+            float mb = fmaxf(mt[0], mt[1]);
             float* xm = xmax + (2 * grp + (i / NG & 1)) * 2 * ST_ROWS + row;
             xm[half * ST_ROWS] = mb;
             ptx::named_bar_sync(pair_bar, 64);
@@ -520,11 +542,13 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             uint32_t nan = 0;                 // tiles of the half whose values are NaN
             if constexpr (Q8) {
                 int v_now = v_used;
-                if (__any_sync(0xffffffffu, (int)max(max(ve[0], ve[1]), max(ve[2], ve[3])) > v_used)) {   // (else no row has to look)
+                uint32_t top = __vmaxu4(by.y & 0xffff, by.y >> 16);
+                top = max(top & 255, top >> 8);
+                if (__any_sync(0xffffffffu, (int)top > v_used)) {   // (else no row has to look)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int at = key0 + 16 * e;
-                        if (ve[e] != 255 && at < vis && (at < sn.sink || at + 16 > begins)) v_now = max(v_now, max((int)ve[e], 1));
+                        const int at = key0 + 16 * e, v = by.y >> (8 * e) & 255;
+                        if (v != 255 && at < vis && (at < sn.sink || at + 16 > begins)) v_now = max(v_now, max(v, 1));
                     }
                 }
                 grown = v_now != v_used;
@@ -532,11 +556,10 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                 v_used = v_now;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int at = half ? (int)ve[2 + e] : (int)ve[e];
+                    const int at = by.y >> (16 * half + 8 * e) & 255;
                     if (at == 255) nan |= 1u << e;
                     pv[e] = at == 255 || v_now == ST_NONE ? (float)(1 << ST_BOOST) : kv8_pow2(min(127 + ST_BOOST + at - v_now, 254));
                 }
-                if (i + NG < nb) scales(i + NG);
             }
             // TMEM accesses are warp-collective: the warp rescales together (its half of the columns), lanes whose
             // maximum stays put multiply by 1. O is settled once P V of the group's previous block is done.
@@ -562,12 +585,18 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             }
             // 2^((s - m) c): a hidden key's -inf gives 0, also while the row has seen none at all (m taken as 0).
             const uint64_t neg_m = pair2(m_used == -INFINITY ? 0.f : -m_used);
+            const float neg_mc = m_used == -INFINITY ? 0.f : -m_used * c2s;
             float l4[4] = {0.f, 0.f, 0.f, 0.f};
             uint32_t pk[HK / 2];
 #pragma unroll
             for (int k = 0; k < HK; k += 2) {
                 float p0, p1;
-                sub_scale2(__uint_as_float(s[k >> 4][k & 15]), __uint_as_float(s[k >> 4][(k + 1) & 15]), neg_m, c2, p0, p1);
+                if constexpr (Q8) {
+                    p0 = fmaf(__uint_as_float(s[k >> 4][k & 15]), kc[k >> 4], neg_mc);
+                    p1 = fmaf(__uint_as_float(s[k >> 4][(k + 1) & 15]), kc[k >> 4], neg_mc);
+                } else {
+                    sub_scale2(__uint_as_float(s[k >> 4][k & 15]), __uint_as_float(s[k >> 4][(k + 1) & 15]), neg_m, c2, p0, p1);
+                }
                 p0 = kr_ex2(p0);
                 p1 = kr_ex2(p1);
                 l4[(k >> 1) & 3] += p0 + p1;
@@ -659,9 +688,10 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             if (!Q8 && dead) {
                 // Values of rows that no row sees, as they landed: cleared (a row's 16-byte pieces stay in the row).
                 if (good) good = ptx::mbar_wait_bounded(&vfull[i % NS], (i / NS) & 1, ST_WAIT_NS);
-                for (int e = (tid - 128) % ST_SOFT; good && e < ST_KEYS * NDB * 8; e += ST_SOFT) {
-                    const int key = e / (NDB * 8), p = e % (NDB * 8);
-                    if (!span_sees(sn, key0 + key, most, first))
+#pragma unroll
+                for (int e0 = 0; e0 < ST_KEYS * NDB * 8; e0 += ST_SOFT) {
+                    const int e = e0 + (tid - 128) % ST_SOFT, key = e / (NDB * 8), p = e % (NDB * 8);
+                    if (good && !span_sees(sn, key0 + key, most, first))
                         *(uint4*)(vb + (p / 8) * (ST_KEYS * 128) + key * 128 + (p % 8) * 16) = make_uint4(0, 0, 0, 0);
                 }
                 ptx::fence_proxy_async_smem();
@@ -831,6 +861,8 @@ jpi_status launch_kv_span_tiles(jpi_kv_handle* h, const KvCall& c, const KvSpan&
     a.tiles = (int)(((long long)c.tokens * c.gq + ST_ROWS - 1) / ST_ROWS);
     a.by_splits = KvDiv((uint32_t)a.splits);
     a.by_tiles = KvDiv((uint32_t)a.tiles);
+    a.by_rest = KvDiv((uint32_t)((long long)splits * c.K * c.batch));
+    a.tiles_outer = (long long)c.batch * c.K * c.own.rows * c.D * (s.ks ? 2 : 4) <= 64ll << 20;
     a.po = po;
     a.pml = pml;
     a.rows = (long long)c.batch * c.tokens * c.H;
