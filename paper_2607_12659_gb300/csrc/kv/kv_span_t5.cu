@@ -52,10 +52,17 @@ constexpr int ST_BOOST = 4;         // log2 of what probabilities of fp16 are mu
 constexpr int ST_NONE = -4096;      // no scale seen yet
 constexpr int ST_RUN = 32;          // blocks of a group whose scales are read together
 // Query rows of a request and KV head from which a call takes the tiles, and the elements of keys up to which it stays with the row
-// kernel all the same, which reads a key once for every 8 query rows.
+// kernel all the same, which reads a key once for every 8 query rows. Microseconds of row kernel and tiles, bf16: 1 KV head at D = 256,
+// 128 rows over 1024 keys (4 M elements) 13.6 and 13.3, over 4096 18.0 and 14.8; 8 KV heads at D = 128, 128 rows over 256 keys
+// (4.5 M) 11.4 and 12.3, over 1024 (16 M) 15.8 and 13.7. 8 bits: 128 rows at D = 256 over 1024 (4 M) 12.9 and 15.6, 4 times 64
+// rows over 1024 (8 M) 17.8 and 15.1; 8 KV heads at D = 128, 128 rows over 1024 (16 M) 17.7 and 16.0; where a tile's rows are a
+// quarter of it, 32 rows of 32 KV heads at D = 128 over 1024 (16 M) 17.2 and 17.5, over 4096 (64 M) 33.9 and 31.5, of 64 KV heads at
+// D = 64 over 4096 (64 M) 45.1 and 48.7.
 constexpr int ST_LEAST = 32;
-constexpr long long ST_ROW_ELEMENTS = 10ll << 20;
-constexpr int ST_FIXED = 5;         // start and end of a block, in key blocks
+constexpr long long st_row_elements(bool held8, long long R, int D) { return (held8 ? (R < 64 && D <= 128 ? 60ll : 12ll) : 4ll) << 20; }
+// Cycles of a key block of D elements, of a block's start and end, of the combine's launch, and bytes a cycle to and from the workspace.
+constexpr long long st_block(bool held8, int D) { return held8 ? 1000 + 8 * D : 500 + 4 * D; }
+constexpr long long ST_ENDS = 10000, ST_JOIN = 8000, ST_BYTES = 2600;
 
 struct SpanMaps {
     CUtensorMap k, v;
@@ -333,13 +340,15 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         uint8_t* const raw = st_smem + L::RING + is_v * (L::RAWBYTES / 2) + x * 16;
         auto fetch = [&](int i) {
             if (i < nb) {
-                const int key0 = blocks.row(blk0 + i) + row0;
+                const int key0 = blocks.row(blk0 + i);
                 const uint32_t to = ptx::smem_u32(raw + i % L::RAW * L::RAWBYTES);
+                const bool all = key0 + ST_KEYS <= most && (key0 >= first || key0 + ST_KEYS <= sn.sink);
+                const uint8_t* p = src + (key0 + row0) * a.c.own.rs;
 #pragma unroll
                 for (int m = 0; m < MINE; ++m) {
-                    const int key = key0 + m * SWEEP;
-                    const bool live = in && span_sees(sn, key, most, first);
-                    ptx::cp_async_16(to + m * (HALFT * 16), live ? src + key * a.c.own.rs : src, live);
+                    const bool live = in && (all || span_sees(sn, key0 + row0 + m * SWEEP, most, first));
+                    ptx::cp_async_16(to + m * (HALFT * 16), live ? p : src, live);
+                    p += SWEEP * a.c.own.rs;
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -835,13 +844,12 @@ int kv_span_tiles_plan(const jpi_kv_handle* h, const KvCall& c, const KvSpan& s,
     KvMapDims m;
     if (!s.ks && !kv_map_dims(c.own, c.K, c.D, c.batch, &m)) return 0;
     if (blocks * nb >= 1ll << 31) return 0;
-    if (h->tiles < 0 && (R < ST_LEAST || (R + KR_ROWS - 1) / KR_ROWS * c.K * c.batch * span * c.D <= ST_ROW_ELEMENTS)) return 0;
-    // Splits by which the waves of blocks end first, in key blocks' time: a block has its start and end beside its keys, a result in
-    // parts its combine and its rows to and from the workspace.
+    if (h->tiles < 0 && (R < ST_LEAST || (R + KR_ROWS - 1) / KR_ROWS * c.K * c.batch * span * c.D <= st_row_elements(s.ks, R, c.D))) return 0;
+    // Splits by which the waves of blocks end first; a result in parts has its combine, and its rows to and from the workspace.
     long long best = 1, best_time = -1;
     for (long long n = 1; n <= std::min({nb, room, std::max(1ll, 2ll * h->num_sms / blocks)}); ++n) {
-        const long long time = (blocks * n + h->num_sms - 1) / h->num_sms * ((nb + n - 1) / n + ST_FIXED) +
-                               (n > 1 ? 7 + n * ((long long)c.batch * c.tokens * c.H * c.D * 4 >> 10) / 3900 : 0);
+        const long long time = (blocks * n + h->num_sms - 1) / h->num_sms * ((nb + n - 1) / n * st_block(s.ks, c.D) + ST_ENDS) +
+                               (n > 1 ? ST_JOIN + 2 * n * c.batch * c.tokens * c.H * c.D * 4 / ST_BYTES : 0);
         if (best_time < 0 || time < best_time) {
             best_time = time;
             best = n;
