@@ -257,9 +257,10 @@ JPI_API jpi_status jpi_kv8_append(jpi_kv_handle* h, const void* q, long long q_s
  * Attention over 8-bit caches: query token (b, t) sees rows 0 .. seen[b][t] - 1 of cache b, with window >= 1 as in
  * jpi_kv_attend_window (0: all of them, and `sink` is not used). q, out and lse are as in jpi_kv_attend, of the handle's type; so
  * are empty rows, and NaN in what a query sees.
- * Scores, softmax and sums in fp32, codes and scales taken as they are. JPI_BF16 mode: queries enter the first product scaled by a
- * power of two as fp16 (bf16's eight bits whole; an element below 2^-14 of its head's largest is off by at most 2^-25 of that), the probabilities the second as fp16, on the 128-row tiles once (off by at most 2^-11 of each, or 2^-28 of what
- * the largest value of the blocks seen would weigh), else in two terms (2^-22 and 2^-31).
+ * Scores, softmax and sums in fp32, codes and scales taken as they are. JPI_BF16 mode: queries enter the first product as fp16,
+ * scaled by a power of two (bf16's eight bits whole; an element below 2^-14 of its head's largest is off by at most 2^-25 of
+ * that), the probabilities the second as fp16 (each off by at most 2^-11 of itself, or 2^-28 of what the largest value of the
+ * blocks seen would weigh).
  */
 JPI_API jpi_status jpi_kv8_attend(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
                                   const jpi_kv8_cache* cache, const int* seen, int window, int sink, void* out,

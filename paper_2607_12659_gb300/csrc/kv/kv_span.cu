@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
 }
 
 // bf16 queries. A warp works alone: it takes pieces (8 query rows over a range of the blocks that they see) in turn and streams
-// their blocks of keys, 16 KB with their values, through two stages of shared memory of its own by 16-byte asynchronous
+// their blocks of keys, 16 KB with their values (8 of codes), through two stages of shared memory of its own by 16-byte asynchronous
 // copies, the next piece's first blocks and query rows behind this one's last; rows that no token of the piece sees arrive as zeros and
 // are not read. Keys are the 16 rows of mma.sync m16n8k16 and query rows its 8 columns; the values' product runs over keys
 // with d as its rows, the probabilities turned from one's result into the other's operand by 8 x 8 transposes.
@@ -176,20 +176,23 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
 // queries' are taken alike); of the values, by a transposing load, two elements of d of two keys, whose bytes one
 // permutation brings together by keys, so that the fragment's rows g and g + 8 are elements 2 g and 2 g + 1. A block's scale
 // multiplies its scores, and its probabilities before the second product: relative to the largest scale 2^e that the row
-// has seen, p 2^(e_j - e) 2^7 is at most 2^15, and as two fp16 terms is off by 2^-22 of itself or 2^-32 of 2^(e + 7).
-constexpr int SR_STAGE = 16384;
-
+// has seen, p 2^(e_j - e) 2^7 is at most 2^15, and as an fp16 number is off by 2^-11 of itself or 2^-32 times 2^(e - e_j) (fp16's least
+// step, 2^-24). Probabilities of bf16 caches enter as two bf16 terms (the rounded value and what the rounding left).
 template <int DP, bool Q8>
 struct SrSmem {
+    // A block's keys and values. Codes take twice the instructions a byte, and what bounds them is a warp's latency: smaller blocks, more
+    // warps. (64 requests over 16384 rows of one KV head of 256: 129 us with five warps an SM, 16 KB each twice.)
+    static constexpr int STAGE = Q8 ? 8192 : 16384;
     static constexpr int ROW = Q8 ? DP : 2 * DP;         // bytes of a key
-    static constexpr int KEYS = SR_STAGE / 2 / ROW;      // keys of a block
-    static constexpr int HALF = SR_STAGE / 2;
+    static constexpr int KEYS = STAGE / 2 / ROW;         // keys of a block
+    static constexpr int HALF = STAGE / 2;
     static constexpr int QBYTES = KR_ROWS * DP * 2;
-    static constexpr int Q_OFF = 2 * SR_STAGE;
+    static constexpr int Q_OFF = 2 * STAGE;
     static constexpr int SEEN_OFF = Q_OFF + 2 * QBYTES;  // [AHEAD][8] counts of the pieces in hand
     static constexpr int AHEAD = 4;
     static constexpr int BYTES = SEEN_OFF + AHEAD * KR_ROWS * 4;
-    static constexpr int ALONE = DP == 256 ? 5 : 6;      // blocks of an SM
+    static constexpr int ALONE = Q8 ? (DP == 256 ? 8 : DP == 128 ? 10 : 11) : DP == 256 ? 5 : 6;   // blocks of an SM
+    static constexpr int REGS = 65536 / 32 / ALONE / 8 * 8 < 255 ? 65536 / 32 / ALONE / 8 * 8 : 255;
 };
 
 __device__ __forceinline__ void sr_ldsm4(uint32_t (&r)[4], uint32_t addr) {
@@ -220,7 +223,7 @@ __device__ __forceinline__ uint32_t sr_half2(float lo, float hi) {
 constexpr int SR_NONE = -4096;   // no scale seen yet
 
 template <int DP, bool Q8>
-__global__ void __launch_bounds__(32) k_kv_span_rows(const __grid_constant__ SpanArgs g_) {
+__global__ void __maxnreg__((SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_constant__ SpanArgs g_) {
     using L = SrSmem<DP, Q8>;
     using T = typename std::conditional<Q8, uint8_t, __nv_bfloat16>::type;
     extern __shared__ __align__(128) uint8_t sr_smem[];
@@ -290,18 +293,30 @@ __global__ void __launch_bounds__(32) k_kv_span_rows(const __grid_constant__ Spa
             f_piece += gridDim.x;
             peek();
         }
-        const uint32_t dst = sm + (issued & 1) * SR_STAGE;
+        const uint32_t dst = sm + (issued & 1) * L::STAGE;
         const int key0 = f_blocks.row(f_blk);
         const T *k = f_k + (long long)(key0 + myrow) * s.rs, *v = f_v + (long long)(key0 + myrow) * s.rs;
+        if (key0 + L::KEYS <= f_lim && (key0 >= f_first || key0 + L::KEYS <= sn.sink)) {   // all seen, as most are
 #pragma unroll
-        for (int i = 0; i < L::KEYS / RPI; ++i) {
-            const int rr = i * RPI + myrow;
-            const bool in = dlive && span_sees(sn, key0 + rr, f_lim, f_first);
-            const uint32_t at = rr * L::ROW + ((mych ^ turn(rr)) << 4);
-            ptx::cp_async_16(dst + at, in ? k : f_k, in);
-            ptx::cp_async_16(dst + L::HALF + at, in ? v : f_v, in);
-            k += RPI * s.rs;
-            v += RPI * s.rs;
+            for (int i = 0; i < L::KEYS / RPI; ++i) {
+                const int rr = i * RPI + myrow;
+                const uint32_t at = rr * L::ROW + ((mych ^ turn(rr)) << 4);
+                ptx::cp_async_16(dst + at, k, dlive);
+                ptx::cp_async_16(dst + L::HALF + at, v, dlive);
+                k += RPI * s.rs;
+                v += RPI * s.rs;
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < L::KEYS / RPI; ++i) {
+                const int rr = i * RPI + myrow;
+                const bool in = dlive && span_sees(sn, key0 + rr, f_lim, f_first);
+                const uint32_t at = rr * L::ROW + ((mych ^ turn(rr)) << 4);
+                ptx::cp_async_16(dst + at, in ? k : f_k, in);
+                ptx::cp_async_16(dst + L::HALF + at, in ? v : f_v, in);
+                k += RPI * s.rs;
+                v += RPI * s.rs;
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (Q8) {
@@ -359,7 +374,7 @@ __global__ void __launch_bounds__(32) k_kv_span_rows(const __grid_constant__ Spa
                 if (Q8) scale = s_new;
             }
             __syncwarp();
-            const uint32_t ks = sm + (used & 1) * SR_STAGE, vs = ks + L::HALF;
+            const uint32_t ks = sm + (used & 1) * L::STAGE, vs = ks + L::HALF;
             if (blk == b0) {
                 const uint32_t qb = L::Q_OFF + (full++ & 1) * L::QBYTES;
                 if constexpr (Q8) {
@@ -532,19 +547,14 @@ __global__ void __launch_bounds__(32) k_kv_span_rows(const __grid_constant__ Spa
                     float p0 = kr_ex2((sc[t][2 * e] - f0) * a.c2), p1 = kr_ex2((sc[t][2 * e + 1] - f1) * a.c2);
                     l0 += p0;
                     l1 += p1;
-                    uint32_t h, r;
                     if constexpr (Q8) {
-                        p0 *= by0;
-                        p1 *= by1;
-                        h = sr_half2(p0, p1);
-                        const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                        r = sr_half2(p0 - b.x, p1 - b.y);
+                        ph[t][e] = kr_transpose(sr_half2(p0 * by0, p1 * by1));
                     } else {
-                        h = kr_pack(p0, p1);
-                        r = kr_pack(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+                        const uint32_t h = kr_pack(p0, p1);
+                        const uint32_t r = kr_pack(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+                        ph[t][e] = kr_transpose(h);
+                        pe[t][e] = kr_transpose(r);
                     }
-                    ph[t][e] = kr_transpose(h);
-                    pe[t][e] = kr_transpose(r);
                 }
             }
             if constexpr (Q8) {
@@ -559,7 +569,6 @@ __global__ void __launch_bounds__(32) k_kv_span_rows(const __grid_constant__ Spa
                             const uint32_t lo = __byte_perm(f[2 * c], 0, 0x3120), hi = __byte_perm(f[2 * c + 1], 0, 0x3120);
                             const uint32_t u0 = kv8_half2(lo), u1 = kv8_half2(lo >> 16), u2 = kv8_half2(hi), u3 = kv8_half2(hi >> 16);
                             sr_mma_half(o[i + c], u0, u1, u2, u3, ph[t][0], ph[t][1]);
-                            sr_mma_half(o[i + c], u0, u1, u2, u3, pe[t][0], pe[t][1]);
                         }
                     }
             } else {
@@ -745,7 +754,7 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
         JPI_TRY(launch_kv_span_tiles(h, c, sn, splits, a.po, a.pml, out, lse, st));
         return splits == 1 ? JPI_OK : launch_kv_combine(h, c, splits, out, lse, st);
     }
-    const long long most = (long long)(DP == 256 ? 5 : 6) * h->num_sms;   // resident warps of the row kernels
+    const long long most = (long long)(sn.ks ? SrSmem<DP, true>::ALONE : SrSmem<DP, false>::ALONE) * h->num_sms;   // resident warps of the row kernel
     if (h->bf16) {
         const int keys = sn.ks ? SrSmem<DP, true>::KEYS : SrSmem<DP, false>::KEYS;
         a.o = plan_span(h, c, sn, 1, keys, 4 * keys, most);
@@ -761,7 +770,7 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
     if (a.parts == 1) a.out = out;
     if (h->bf16)
         JPI_TRY(kv_start(sn.ks ? k_kv_span_rows<DP, true> : k_kv_span_rows<DP, false>, dim3((unsigned)std::min(a.o.blocks, most)), 32,
-                         SrSmem<DP, true>::BYTES, false, st, g));
+                         sn.ks ? SrSmem<DP, true>::BYTES : SrSmem<DP, false>::BYTES, false, st, g));
     else
         JPI_TRY(kv_start(sn.ks ? k_kv_span_cc<DP, float, Code8> : k_kv_span_cc<DP, float, float>, dim3((unsigned)a.o.blocks), AT_THREADS,
                          MergeSmem<DP>::BYTES, false, st, g));
@@ -775,11 +784,10 @@ jpi_status prepare_dim(const jpi_kv_handle* h) {
             JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
         return JPI_OK;
     }
-    for (auto* kernel : {k_kv_span_rows<DP, false>, k_kv_span_rows<DP, true>}) {
-        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, true>::BYTES));
-        // All of its loads go to shared memory.
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, false>::BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, true>::BYTES));
+    for (auto* kernel : {k_kv_span_rows<DP, false>, k_kv_span_rows<DP, true>})   // all of its loads go to shared memory
         JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
-    }
     return JPI_OK;
 }
 
