@@ -23,32 +23,52 @@ struct SpanArgs {
     KvSpan s;
 };
 
-// Four elements of a cache's row as fp32.
+// A cache's elements as they are loaded and as fp32: four of the values, a run of a key.
 struct Code8 { uint8_t code; };
 template <typename T>
-__device__ __forceinline__ float4 four(const T* p);
+struct Held;
 template <>
-__device__ __forceinline__ float4 four<float>(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
+struct Held<float> {
+    using Four = float4;
+    __device__ static __forceinline__ Four four(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
+    __device__ static __forceinline__ Four none() { return make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ static __forceinline__ float4 value(Four x) { return x; }
+    // Elements of a key that are on their way together, and how they are used.
+    static constexpr int RUN = 16;
+    struct Run { float4 x[4]; };
+    __device__ static __forceinline__ void load(Run& r, const float* p, int n) {   // n: left of the row
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.x[i] = 4 * i < n ? four(p + 4 * i) : none();
+    }
+    __device__ static __forceinline__ float4 part(const Run& r, int i) { return r.x[i]; }
+};
 template <>
-__device__ __forceinline__ float4 four<__nv_bfloat16>(const __nv_bfloat16* p) {
-    const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
-    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                       __uint_as_float(u.y & 0xffff0000u));
-}
-template <>
-__device__ __forceinline__ float4 four<Code8>(const Code8* p) {
-    float z[4];
-    kv8_values(__ldg(reinterpret_cast<const uint32_t*>(p)), z);
-    return make_float4(z[0], z[1], z[2], z[3]);
-}
+struct Held<Code8> {
+    using Four = uint32_t;
+    __device__ static __forceinline__ Four four(const Code8* p) { return __ldg(reinterpret_cast<const uint32_t*>(p)); }
+    __device__ static __forceinline__ Four none() { return 0; }
+    __device__ static __forceinline__ float4 value(Four x) {
+        float z[4];
+        kv8_values(x, z);
+        return make_float4(z[0], z[1], z[2], z[3]);
+    }
+    static constexpr int RUN = 16;
+    struct Run { uint4 x; };
+    __device__ static __forceinline__ void load(Run& r, const Code8* p, int) { r.x = __ldg(reinterpret_cast<const uint4*>(p)); }
+    __device__ static __forceinline__ float4 part(const Run& r, int i) { return value(i == 0 ? r.x.x : i == 1 ? r.x.y : i == 2 ? r.x.z : r.x.w); }
+};
 
 // fp32, on CUDA cores: a warp takes 8 query rows over blocks of 32 keys, scores with a key per lane, values with a lane per four
-// elements of d; the warps of a block take different row tiles or different keys of one.
-template <int DP, typename E, typename T>
+// elements of d; the warps of a block take different row tiles or different keys of one. What bounds it is latency: a block's
+// loads, its products and 2^x follow one another. So a key's next elements, and the next values, are on their way while these
+// are used: 4 requests of 9 tokens with windows of 300 keys took 22 us with loads one by one.
+template <int DP, typename T>
 __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(const __grid_constant__ SpanArgs g) {
     extern __shared__ __align__(16) float kv_smem[];
+    using Hd = Held<T>;
     const AttendArgs& a = g.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    ptx::grid_dep_launch();
     const Piece x = piece_of(a, blockIdx.x, warp);
     const SidePlan& sp = a.o;
     const KvSide& s = a.c.own;
@@ -56,10 +76,16 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
     float* qs = kv_smem + warp / sp.wk * (KR_ROWS * DP);
     const int wk = warp % sp.wk;
     if (wk == 0) {
-        for (int e = lane; e < KR_ROWS * (DP / 4); e += 32) {
-            const int r = x.t.r0 + e / (DP / 4), d = 4 * (e % (DP / 4));
-            *(float4*)(qs + 4 * e) = r < x.t.R && d < D ? four<E>(static_cast<const E*>(a.c.q) + row_query(a.c, x.t, r) + d)
-                                                        : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int e0 = lane; e0 < KR_ROWS * (DP / 4); e0 += 4 * 32) {
+            float4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = e0 + 32 * i, r = x.t.r0 + e / (DP / 4), d = 4 * (e % (DP / 4));
+                v[i] = r < x.t.R && d < D ? *(const float4*)(static_cast<const float*>(a.c.q) + row_query(a.c, x.t, r) + d)
+                                          : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *(float4*)(qs + 4 * (e0 + 32 * i)) = v[i];
         }
     }
     int n[KR_ROWS], lim = 0, first = 0x7fffffff;
@@ -76,7 +102,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
     const T* vbase = (const T*)s.v + x.cache * s.cs + x.kvh * s.hs;
     const long long scales = ((long long)x.cache * a.c.K + x.kvh) * g.s.nblk;
     constexpr bool HELD8 = sizeof(T) == 1;
-    constexpr int NI = (DP + 127) / 128;
+    constexpr int NI = (DP + 127) / 128, VL = 4 / NI;   // values on their way
     float4 o[KR_ROWS][NI];
     float m[KR_ROWS], l[KR_ROWS];
 #pragma unroll
@@ -92,20 +118,43 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
 #pragma unroll
         for (int r = 0; r < KR_ROWS; ++r) p[r] = 0.f;
         const bool live = span_sees(g.s, key, lim, first);   // by some row of the tile
-        const T* kp = kbase + (long long)key * s.rs;
-        for (int d = 0; d < D; d += 4) {
-            const float4 k = live ? four<T>(kp + d) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int r = 0; r < KR_ROWS; ++r) {
-                const float4 q = *(const float4*)(qs + r * DP + d);
-                p[r] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, p[r]))));
-            }
-        }
+        const T* kp = kbase + (live ? key * s.rs : 0);
         float ks = 1.f, vs = 1.f;
         if (HELD8 && live) {
             ks = kv8_scale(g.s.ks[scales + (key >> g.s.n_log2)]);
             vs = kv8_scale(g.s.vs[scales + (key >> g.s.n_log2)]);
         }
+        // Values of VL keys, those of the next ones on their way while these are used, the first ones during the scores.
+        typename Hd::Four next[VL][NI];
+        auto load = [&](int t0) {
+#pragma unroll
+            for (int t = 0; t < VL; ++t)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int d = 4 * lane + 128 * i;
+                    next[t][i] = d < D && span_sees(g.s, key0 + t0 + t, lim, first) ? Hd::four(vbase + (key0 + t0 + t) * s.rs + d) : Hd::none();
+                }
+        };
+        load(0);
+        if (live) {
+            typename Hd::Run k, k2;
+            Hd::load(k, kp, D);
+            for (int d0 = 0; d0 < D; d0 += Hd::RUN) {
+                if (d0 + Hd::RUN < D) Hd::load(k2, kp + d0 + Hd::RUN, D - d0 - Hd::RUN);
+#pragma unroll
+                for (int i = 0; i < Hd::RUN / 4; ++i) {
+                    if (d0 + 4 * i >= D) break;
+                    const float4 y = Hd::part(k, i);
+#pragma unroll
+                    for (int r = 0; r < KR_ROWS; ++r) {
+                        const float4 q = *(const float4*)(qs + r * DP + d0 + 4 * i);
+                        p[r] = fmaf(q.x, y.x, fmaf(q.y, y.y, fmaf(q.z, y.z, fmaf(q.w, y.w, p[r]))));
+                    }
+                }
+                k = k2;
+            }
+        }
+        __syncwarp();
 #pragma unroll
         for (int r = 0; r < KR_ROWS; ++r) {
             const float sc = span_sees(g.s, key, n[r], span_first(g.s, n[r])) ? p[r] * ks : -INFINITY;
@@ -122,26 +171,31 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
             p[r] = exp2f((sc - (m[r] == -INFINITY ? 0.f : m[r])) * a.c2);   // (of -inf 0, of NaN NaN)
             l[r] += p[r];
         }
-        for (int t = 0; t < 32 && key0 + t < lim; ++t) {
-            if (!span_sees(g.s, key0 + t, lim, first)) continue;   // (the same for the warp)
-            const float by = HELD8 ? __shfl_sync(0xffffffffu, vs, t) : 1.f;
-            float4 v[NI];
+        for (int t0 = 0; t0 < 32 && key0 + t0 < lim; t0 += VL) {
+            float4 v[VL][NI];
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int d = 4 * lane + 128 * i;
-                v[i] = d < D ? four<T>(vbase + (long long)(key0 + t) * s.rs + d) : make_float4(0.f, 0.f, 0.f, 0.f);
-                if (HELD8) v[i] = make_float4(v[i].x * by, v[i].y * by, v[i].z * by, v[i].w * by);
-            }
+            for (int t = 0; t < VL; ++t)
 #pragma unroll
-            for (int r = 0; r < KR_ROWS; ++r) {
-                const float w = __shfl_sync(0xffffffffu, p[r], t);
-                if (!span_sees(g.s, key0 + t, n[r], span_first(g.s, n[r]))) continue;   // a hidden value is not even multiplied by zero
+                for (int i = 0; i < NI; ++i) v[t][i] = Hd::value(next[t][i]);
+            if (t0 + VL < 32) load(t0 + VL);
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    o[r][i].x = fmaf(w, v[i].x, o[r][i].x);
-                    o[r][i].y = fmaf(w, v[i].y, o[r][i].y);
-                    o[r][i].z = fmaf(w, v[i].z, o[r][i].z);
-                    o[r][i].w = fmaf(w, v[i].w, o[r][i].w);
+            for (int t = 0; t < VL; ++t) {
+                if (HELD8) {
+                    const float by = __shfl_sync(0xffffffffu, vs, t0 + t);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) v[t][i] = make_float4(v[t][i].x * by, v[t][i].y * by, v[t][i].z * by, v[t][i].w * by);
+                }
+#pragma unroll
+                for (int r = 0; r < KR_ROWS; ++r) {
+                    const float w = __shfl_sync(0xffffffffu, p[r], t0 + t);
+                    if (!span_sees(g.s, key0 + t0 + t, n[r], span_first(g.s, n[r]))) continue;   // a hidden value is not even multiplied by zero
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) {
+                        o[r][i].x = fmaf(w, v[t][i].x, o[r][i].x);
+                        o[r][i].y = fmaf(w, v[t][i].y, o[r][i].y);
+                        o[r][i].z = fmaf(w, v[t][i].z, o[r][i].z);
+                        o[r][i].w = fmaf(w, v[t][i].w, o[r][i].w);
+                    }
                 }
             }
         }
@@ -162,7 +216,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
             f[KR_ROWS * MergeSmem<DP>::LD + 2 * r + 1] = l[r];
         }
     }
-    merge_and_write<DP, E>(a, x, sp, kv_smem, warp, lane);
+    merge_and_write<DP, float>(a, x, sp, kv_smem, warp, lane);
 }
 
 // bf16 queries. A warp works alone: it takes pieces (8 query rows over a range of the blocks that they see) in turn and streams
@@ -772,7 +826,7 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
         JPI_TRY(kv_start(sn.ks ? k_kv_span_rows<DP, true> : k_kv_span_rows<DP, false>, dim3((unsigned)std::min(a.o.blocks, most)), 32,
                          sn.ks ? SrSmem<DP, true>::BYTES : SrSmem<DP, false>::BYTES, false, st, g));
     else
-        JPI_TRY(kv_start(sn.ks ? k_kv_span_cc<DP, float, Code8> : k_kv_span_cc<DP, float, float>, dim3((unsigned)a.o.blocks), AT_THREADS,
+        JPI_TRY(kv_start(sn.ks ? k_kv_span_cc<DP, Code8> : k_kv_span_cc<DP, float>, dim3((unsigned)a.o.blocks), AT_THREADS,
                          MergeSmem<DP>::BYTES, false, st, g));
     return a.parts == 1 ? JPI_OK : launch_kv_combine(h, c, a.parts, out, lse, st);
 }
@@ -780,7 +834,7 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
 template <int DP>
 jpi_status prepare_dim(const jpi_kv_handle* h) {
     if (!h->bf16) {
-        for (auto* kernel : {k_kv_span_cc<DP, float, float>, k_kv_span_cc<DP, float, Code8>})
+        for (auto* kernel : {k_kv_span_cc<DP, float>, k_kv_span_cc<DP, Code8>})
             JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
         return JPI_OK;
     }
