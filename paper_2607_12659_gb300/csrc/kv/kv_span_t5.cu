@@ -241,11 +241,6 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         ptx::fence_mbar_init();
         *flag = 0;
         for (int b = 0; b < NG; ++b) begun[b] = 0;
-        // The first use of the ring needs nothing of the other warps.
-        for (int i = 0; !Q8 && i < NS && i < nb; ++i) {
-            load(false, i);
-            if (i < NS - L::QS) load(true, i);
-        }
     }
     if (warp == 1) {
         ptx::tmem_alloc(tmem_slot, L::TMEM_COLS);
@@ -261,22 +256,17 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             const bool is_v = warp == 1;
             uint64_t* fullb = is_v ? vfull : kfull;
             uint64_t* emptyb = is_v ? vempty : kempty;
-            int issued = min(NS, nb);
+            int issued = 0;
             bool good = true;
-            if (is_v) {
-                good = ptx::mbar_wait_bounded(qready, 0, ST_WAIT_NS);
-                if (!good) *flag = DEV_TIMEOUT_MMA;
-                if (!good) issued = min(NS - L::QS, nb);
-                for (int i = NS - L::QS; good && i < NS && i < nb; ++i) load(true, i);
-            }
-            for (int i = NS; good && i < nb; ++i) {
-                if (!ptx::mbar_wait_bounded(&emptyb[i % NS], (i / NS - 1) & 1, ST_WAIT_NS)) {
-                    *flag = DEV_TIMEOUT_WEIGHTS;
-                    break;
-                }
+            for (int i = 0; i < nb; ++i) {
+                if (i >= NS) good = ptx::mbar_wait_bounded(&emptyb[i % NS], (i / NS - 1) & 1, ST_WAIT_NS);
+                // (the query rows pass through the last value slots)
+                else if (is_v && i >= NS - L::QS) good = ptx::mbar_wait_bounded(qready, 0, ST_WAIT_NS);
+                if (!good) break;
                 load(is_v, i);
                 issued = i + 1;
             }
+            if (!good) *flag = DEV_TIMEOUT_WEIGHTS;
             if (!ptx::ring_drain(fullb, NS, issued, ST_WAIT_NS)) *flag = DEV_TIMEOUT_WEIGHTS;
         }
     } else if (warp == 2) {
@@ -791,7 +781,9 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         }
         // Rows leave by whole warps. (A bulk copy a row, 128 of them, took 3 thousand cycles longer.)
         ptx::named_bar_sync(9, NG * ST_SOFT);
-        for (int rr = warp - 4; good && rr < ST_ROWS && t.r0 + rr < t.R; rr += 8 * NG) {
+#pragma unroll 4
+        for (int rr = warp - 4; rr < ST_ROWS; rr += 8 * NG) {
+            if (!good || t.r0 + rr >= t.R) continue;
             const long long row_at = row_index(a.c, t, t.r0 + rr);
             const uint8_t* from = st_smem + rr * L::OUT_LD;
             if (a.out) {
