@@ -18,6 +18,7 @@ struct jpi_kv_handle {
     int* dev_err = nullptr;
     bool pdl = true;             // kernels of one call may start before the one before them has finished
     int tiles = -1;              // attend, weigh: the tensor-core tiles never, (1) wherever they fit, (-1) by size
+    int span_clusters[2][4] = {};   // attend_window, kv8_attend: clusters of 1, 2, 4 and 8 joining blocks that are resident together
     size_t device_bytes = 0;
     std::vector<void*> allocations;
 };

@@ -232,6 +232,9 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
 // multiplies its scores, and its probabilities before the second product: relative to the largest scale 2^e that the row
 // has seen, p 2^(e_j - e) 2^7 is at most 2^15, and as an fp16 number is off by 2^-11 of itself or 2^-32 times 2^(e - e_j) (fp16's least
 // step, 2^-24). Probabilities of bf16 caches enter as two bf16 terms (the rounded value and what the rounding left).
+//
+// A call of few tiles, which is waited for, takes one launch (JOIN): a cluster of blocks has a tile, each of its warps a part, and
+// the parts are joined through the blocks' shared memories in place of the workspace and a second kernel.
 template <int DP, bool Q8>
 struct SrSmem {
     // A block's keys and values. Codes take twice the instructions a byte, and what bounds them is a warp's latency: smaller blocks, more
@@ -247,7 +250,19 @@ struct SrSmem {
     static constexpr int BYTES = SEEN_OFF + AHEAD * KR_ROWS * 4;
     static constexpr int ALONE = Q8 ? (DP == 256 ? 8 : DP == 128 ? 10 : 11) : DP == 256 ? 5 : 6;   // blocks of an SM
     static constexpr int REGS = 65536 / 32 / ALONE / 8 * 8 < 255 ? 65536 / 32 / ALONE / 8 * 8 : 255;
+    // Joined in a cluster: warps of a block, each with what is above for itself, and then the block's joined rows and their (m, l).
+    static constexpr int TEAM = Q8 ? 8 : 4;
+    static constexpr int JOIN_OFF = TEAM * BYTES, JOIN_ML = JOIN_OFF + KR_ROWS * DP * 4;
+    static constexpr int JOIN_BYTES = JOIN_ML + KR_ROWS * 8;
+    static_assert(BYTES % 128 == 0 && JOIN_BYTES <= 227 * 1024, "fits an SM");
+    static_assert(KR_ROWS * (DP + 4) * 4 + KR_ROWS * 8 <= 2 * STAGE, "a warp's rows fit its stages");
 };
+constexpr int SR_RANKS = 8;   // most blocks of a cluster, as in the handle's table
+// Most blocks of keys for a warp of a cluster. Microseconds of one launch and of two, bf16 and 8 bits, single tokens over one KV head
+// of 256: 300 keys 6.7 and 8.4, 8.0 and 8.9 for one request, 8.4 and 8.9, 8.7 and 10.0 for 16; 867 keys 7.8 and 8.3, 8.5 and 9.3 for one; 2000
+// keys (four blocks, two) 9.3 and 9.1, 9.6 and 10.6 for one, 9.6 and 11.1, 9.9 and 12.2 for eight; 4000 keys (eight, four) 12.0 and 9.6, 11.8 and
+// 11.0 for one, 12.1 and 11.7, 11.9 and 13.1 for four. (On the host a launch less is 2 us less.)
+constexpr int SR_JOIN_BLOCKS = 4;
 
 __device__ __forceinline__ void sr_ldsm4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -276,11 +291,103 @@ __device__ __forceinline__ uint32_t sr_half2(float lo, float hi) {
 
 constexpr int SR_NONE = -4096;   // no scale seen yet
 
+// Joins the parts of a tile of 8 query rows that the warps of a cluster's blocks hold in shared memory, and writes the result: each
+// block its own warps' first, then every block some of the rows over all blocks.
 template <int DP, bool Q8>
-__global__ void __maxnreg__((SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_constant__ SpanArgs g_) {
+__device__ __forceinline__ void join_cluster(const AttendArgs& a, const Piece& x, uint8_t* block, int warp, int lane) {
+    using L = SrSmem<DP, Q8>;
+    constexpr int LD = DP + 4, NI = (DP + 127) / 128;
+    float* const joined = reinterpret_cast<float*>(block + L::JOIN_OFF);
+    float2* const ml = reinterpret_cast<float2*>(block + L::JOIN_ML);
+    auto part = [&](int k) { return reinterpret_cast<const float*>(block + k * L::BYTES); };
+    const int ranks = a.o.splits / L::TEAM;
+    auto weight = [&](float m, float most) { return m == -INFINITY ? 0.f : kr_ex2((m - most) * a.c2); };
+    for (int r = warp; r < KR_ROWS; r += L::TEAM) {
+        float2 p[L::TEAM];
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int k = 0; k < L::TEAM; ++k) {
+            p[k] = *(const float2*)(part(k) + KR_ROWS * LD + 2 * r);
+            m = fmaxf(m, p[k].x);
+        }
+        float4 o[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < L::TEAM; ++k) {
+            if (p[k].y == 0.f) continue;
+            const float w = weight(p[k].x, m);
+            l = fmaf(w, p[k].y, l);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int d = 4 * lane + 128 * i;
+                if (d >= DP) continue;
+                const float4 v = *(const float4*)(part(k) + r * LD + d);
+                o[i] = make_float4(fmaf(w, v.x, o[i].x), fmaf(w, v.y, o[i].y), fmaf(w, v.z, o[i].z), fmaf(w, v.w, o[i].w));
+            }
+        }
+        if (ranks == 1) {
+            if (x.t.r0 + r < x.t.R) {
+                RowAcc<DP> row;
+#pragma unroll
+                for (int i = 0; i < NI; ++i) row.o[i] = o[i];
+                row.m = m;
+                row.l = l;
+                write_row<DP, __nv_bfloat16>(a, row, row_index(a.c, x.t, x.t.r0 + r), 0, lane);
+            }
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int d = 4 * lane + 128 * i;
+            if (d < DP) *(float4*)(joined + r * DP + d) = o[i];
+        }
+        if (lane == 0) ml[r] = make_float2(m, l);
+    }
+    if (ranks == 1) return;
+    __syncwarp();
+    ptx::cluster_sync_all();
+    for (int r = (int)ptx::cluster_rank(); r < KR_ROWS; r += ranks) {
+        if (x.t.r0 + r >= x.t.R) continue;
+        const long long row = row_index(a.c, x.t, x.t.r0 + r);
+        for (int d = 2 * (int)threadIdx.x; d < a.c.D; d += 64 * L::TEAM) {
+            float2 p[SR_RANKS], v[SR_RANKS];
+            float m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int k = 0; k < SR_RANKS; ++k) {
+                p[k] = make_float2(-INFINITY, 0.f);
+                v[k] = make_float2(0.f, 0.f);
+                if (k < ranks) {
+                    p[k] = ptx::dsmem_ld_f2(ptx::dsmem_map(ptx::smem_u32(ml + r), (uint32_t)k));
+                    v[k] = ptx::dsmem_ld_f2(ptx::dsmem_map(ptx::smem_u32(joined + r * DP + d), (uint32_t)k));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < SR_RANKS; ++k) m = fmaxf(m, p[k].x);
+            float2 o = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < SR_RANKS; ++k) {
+                if (p[k].y == 0.f) continue;
+                const float w = weight(p[k].x, m);
+                l = fmaf(w, p[k].y, l);
+                o = make_float2(fmaf(w, v[k].x, o.x), fmaf(w, v[k].y, o.y));
+            }
+            const float inv = inverse_sum(l);
+            *(uint32_t*)(static_cast<__nv_bfloat16*>(a.out) + row * a.c.D + d) = kr_pack(o.x * inv, o.y * inv);
+            if (d == 0 && a.lse) a.lse[row] = log_sum(m, l, a.c.scale);
+        }
+    }
+    __syncwarp();
+    ptx::cluster_sync_all();   // every block's rows have been read
+}
+
+template <int DP, bool Q8, bool JOIN>
+__global__ void __maxnreg__((JOIN ? 248 : SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_constant__ SpanArgs g_) {
     using L = SrSmem<DP, Q8>;
     using T = typename std::conditional<Q8, uint8_t, __nv_bfloat16>::type;
-    extern __shared__ __align__(128) uint8_t sr_smem[];
+    extern __shared__ __align__(128) uint8_t sr_block[];
+    const int warp = JOIN ? (int)threadIdx.x >> 5 : 0, lane = JOIN ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    uint8_t* const sr_smem = sr_block + warp * L::BYTES;   // this warp's own
     const AttendArgs& a = g_.a;
     const KvSpan& sn = g_.s;
     constexpr int MT = L::KEYS / 16;   // 16-key tiles of a block
@@ -289,11 +396,12 @@ __global__ void __maxnreg__((SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_
     constexpr int CH = DP / EPC;       // chunks of a row; chunk c of row r lies at c ^ turn(r)
     constexpr int RPI = 32 / CH;       // rows one instruction of the warp copies
     constexpr int QCH = DP / 8, QRPI = 32 / QCH;
-    const int lane = threadIdx.x, g = lane >> 2, j = lane & 3;
+    const int g = lane >> 2, j = lane & 3;
     const uint32_t sm = ptx::smem_u32(sr_smem);
     int* const counts = (int*)(sr_smem + L::SEEN_OFF);
     ptx::grid_dep_launch();
     const uint32_t pieces = (uint32_t)a.o.blocks;
+    const uint32_t mine0 = JOIN ? blockIdx.x * L::TEAM + warp : blockIdx.x, step = JOIN ? pieces : gridDim.x;   // its first piece; to the next
     const KvSide& s = a.c.own;
     const int D = a.c.D, mych = lane % CH, myrow = lane / CH;
     const bool dlive = EPC * mych < D;
@@ -301,7 +409,7 @@ __global__ void __maxnreg__((SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_
     auto turn = [](int r) { return CH == 4 ? (r >> 1) & 3 : r & 7; };
 
     // ---- what is to be copied: pieces opened in order, block by block
-    uint32_t f_piece = blockIdx.x;
+    uint32_t f_piece = mine0;
     int f_seq = 0, f_full = 0, f_blk = 0, f_end = 0, f_lim = 0, f_first = 0;
     SpanBlocks<L::KEYS> f_blocks(sn, 0, 0);
     const T *f_k = nullptr, *f_v = nullptr;   // this lane's chunk of the open piece's row 0
@@ -344,7 +452,7 @@ __global__ void __maxnreg__((SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_
                 ++f_full;
             }
             ++f_seq;
-            f_piece += gridDim.x;
+            f_piece += step;
             peek();
         }
         const uint32_t dst = sm + (issued & 1) * L::STAGE;
@@ -387,7 +495,7 @@ __global__ void __maxnreg__((SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_
 
     peek();
     if (produce()) produce();
-    for (uint32_t piece = blockIdx.x; piece < pieces; piece += gridDim.x, ++seq) {
+    for (uint32_t piece = mine0; piece < pieces; piece += step, ++seq) {
         const Piece x = piece_of(a, piece, 0);
         if (f_seq <= seq) produce();
         __syncwarp();
@@ -717,6 +825,26 @@ __global__ void __maxnreg__((SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_
                 if (r == 2 * j + 1) o[i][1] = y0, o[i][3] = y1;
             }
         }
+        if constexpr (JOIN) {
+            // The warp's rows go where its stages were, whose copies have all been read.
+            constexpr int LD = DP + 4;
+            float* f = reinterpret_cast<float*>(sr_smem);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    f[2 * j * LD + elem(i, e)] = o[i][2 * e];
+                    f[(2 * j + 1) * LD + elem(i, e)] = o[i][2 * e + 1];
+                }
+            if (g == 0) {
+                *(float2*)(f + KR_ROWS * LD + 4 * j) = make_float2(m0, l0);
+                *(float2*)(f + KR_ROWS * LD + 4 * j + 2) = make_float2(m1, l1);
+            }
+            __syncthreads();
+            join_cluster<DP, Q8>(a, x, sr_block, warp, lane);
+            return;
+        }
         const long long row0 = in0 ? row_index(a.c, x.t, rj) : 0, row1 = in1 ? row_index(a.c, x.t, rj + 1) : 0;
         if (a.out) {
             const float inv0 = inverse_sum(l0), inv1 = inverse_sum(l1);
@@ -770,6 +898,12 @@ __global__ void __maxnreg__((SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_
     }
 }
 
+// Rows of the cache that the tokens of a tile of 8 query rows see, with the ends of their blocks.
+long long rows_span(const KvCall& c, const KvSpan& sn, int step) {
+    const long long toks = std::min<long long>(c.tokens, (KR_ROWS + c.gq - 1) / c.gq + 1);
+    return std::min<long long>(c.own.rows, (long long)sn.window + toks + std::min(sn.sink, c.own.rows) + 2 * step);
+}
+
 // How a call is dealt to blocks of `warps` warps, whose warps take `step` keys at a time: splits of the rows that a tile can see,
 // up to `want` blocks in all while a warp keeps `least` keys; a call of few pieces, which is waited for, down to single steps as
 // far as two blocks an SM go. The parts fit the workspace.
@@ -779,9 +913,7 @@ SidePlan plan_span(const jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, in
     while (s.wr < warps && s.wr < rt) s.wr *= 2;
     s.wk = warps / s.wr;
     s.tiles = (int)((rt + s.wr - 1) / s.wr);
-    // Rows of the cache that the tokens of a tile see, with the ends of their blocks.
-    const long long toks = std::min<long long>(c.tokens, (KR_ROWS + c.gq - 1) / c.gq + 1);
-    const long long rows = std::min<long long>(c.own.rows, (long long)sn.window + toks + std::min(sn.sink, c.own.rows) + 2 * step);
+    const long long rows = rows_span(c, sn, step);
     const long long blocks = (long long)c.batch * c.K * s.tiles, all = (long long)c.batch * c.tokens * c.H;
     const long long room = std::max(1ll, ws_rows(h) / all);
     const long long coarse = std::min(want / blocks, (rows + least * s.wk - 1) / (least * s.wk));
@@ -791,6 +923,19 @@ SidePlan plan_span(const jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, in
     s.by_splits = KvDiv((uint32_t)s.splits);
     s.by_tiles = KvDiv((uint32_t)s.tiles);
     return s;
+}
+
+// Blocks of the cluster that a small call's tile of query rows is dealt to: the most with which all clusters are resident together;
+// 0: more tiles than fit one block each, or more blocks of keys for a warp than a second launch takes.
+template <int DP>
+int join_ranks(const jpi_kv_handle* h, const KvCall& c, const KvSpan& sn) {
+    if (!h->bf16) return 0;
+    const int keys = sn.ks ? SrSmem<DP, true>::KEYS : SrSmem<DP, false>::KEYS, team = sn.ks ? SrSmem<DP, true>::TEAM : SrSmem<DP, false>::TEAM;
+    const long long tiles = (long long)c.batch * c.K * (((long long)c.tokens * c.gq + KR_ROWS - 1) / KR_ROWS);
+    const long long nb = (rows_span(c, sn, keys) + keys - 1) / keys;
+    int n = 3;
+    while (n >= 0 && tiles > h->span_clusters[sn.ks != nullptr][n]) --n;
+    return n >= 0 && nb <= (long long)SR_JOIN_BLOCKS * team << n ? 1 << n : 0;
 }
 
 template <int DP>
@@ -808,6 +953,17 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
         JPI_TRY(launch_kv_span_tiles(h, c, sn, splits, a.po, a.pml, out, lse, st));
         return splits == 1 ? JPI_OK : launch_kv_combine(h, c, splits, out, lse, st);
     }
+    if (const int ranks = join_ranks<DP>(h, c, sn)) {
+        const int team = sn.ks ? SrSmem<DP, true>::TEAM : SrSmem<DP, false>::TEAM;
+        a.o.tiles = (int)(((long long)c.tokens * c.gq + KR_ROWS - 1) / KR_ROWS);
+        a.o.splits = ranks * team;
+        a.o.blocks = (long long)c.batch * c.K * a.o.tiles * a.o.splits;
+        a.o.by_splits = KvDiv((uint32_t)a.o.splits);
+        a.o.by_tiles = KvDiv((uint32_t)a.o.tiles);
+        a.out = out;
+        return kv_start_clusters(sn.ks ? k_kv_span_rows<DP, true, true> : k_kv_span_rows<DP, false, true>, dim3((unsigned)(a.o.blocks / team)),
+                                 (unsigned)ranks, 32 * team, sn.ks ? SrSmem<DP, true>::JOIN_BYTES : SrSmem<DP, false>::JOIN_BYTES, false, st, g);
+    }
     const long long most = (long long)(sn.ks ? SrSmem<DP, true>::ALONE : SrSmem<DP, false>::ALONE) * h->num_sms;   // resident warps of the row kernel
     if (h->bf16) {
         const int keys = sn.ks ? SrSmem<DP, true>::KEYS : SrSmem<DP, false>::KEYS;
@@ -823,7 +979,7 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
     }
     if (a.parts == 1) a.out = out;
     if (h->bf16)
-        JPI_TRY(kv_start(sn.ks ? k_kv_span_rows<DP, true> : k_kv_span_rows<DP, false>, dim3((unsigned)std::min(a.o.blocks, most)), 32,
+        JPI_TRY(kv_start(sn.ks ? k_kv_span_rows<DP, true, false> : k_kv_span_rows<DP, false, false>, dim3((unsigned)std::min(a.o.blocks, most)), 32,
                          sn.ks ? SrSmem<DP, true>::BYTES : SrSmem<DP, false>::BYTES, false, st, g));
     else
         JPI_TRY(kv_start(sn.ks ? k_kv_span_cc<DP, Code8> : k_kv_span_cc<DP, float>, dim3((unsigned)a.o.blocks), AT_THREADS,
@@ -832,16 +988,31 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
 }
 
 template <int DP>
-jpi_status prepare_dim(const jpi_kv_handle* h) {
+jpi_status prepare_dim(jpi_kv_handle* h) {
     if (!h->bf16) {
         for (auto* kernel : {k_kv_span_cc<DP, float>, k_kv_span_cc<DP, Code8>})
             JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
         return JPI_OK;
     }
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, false>::BYTES));
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, true>::BYTES));
-    for (auto* kernel : {k_kv_span_rows<DP, false>, k_kv_span_rows<DP, true>})   // all of its loads go to shared memory
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, false>::BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, true>::BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, false>::JOIN_BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, true>::JOIN_BYTES));
+    for (auto* kernel : {k_kv_span_rows<DP, false, false>, k_kv_span_rows<DP, true, false>})   // all of its loads go to shared memory
         JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+    for (int held8 = 0; held8 < 2; ++held8)
+        for (int n = 0; n < 4; ++n) {
+            cudaLaunchAttribute at = {};
+            at.id = cudaLaunchAttributeClusterDimension;
+            at.val.clusterDim = {1u << n, 1, 1};
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(1u << n);
+            cfg.blockDim = dim3(32 * (held8 ? SrSmem<DP, true>::TEAM : SrSmem<DP, false>::TEAM));
+            cfg.dynamicSmemBytes = held8 ? SrSmem<DP, true>::JOIN_BYTES : SrSmem<DP, false>::JOIN_BYTES;
+            cfg.attrs = &at;
+            cfg.numAttrs = 1;
+            JPI_CUDA_TRY(cudaOccupancyMaxActiveClusters(&h->span_clusters[held8][n], held8 ? k_kv_span_rows<DP, true, true> : k_kv_span_rows<DP, false, true>, &cfg));
+        }
     return JPI_OK;
 }
 
