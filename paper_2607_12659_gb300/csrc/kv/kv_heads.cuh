@@ -6,6 +6,7 @@
 #pragma once
 
 #include "kv_code.cuh"
+#include "kv_pair.cuh"
 #include "../ptx.h"
 
 #include <algorithm>
@@ -60,18 +61,6 @@ struct HeadLane {
             raw[i] = in && live[i] ? *reinterpret_cast<const uint4*>(head + c[i] * V) : make_uint4(0, 0, 0, 0);
     }
 };
-
-// Two fp32 numbers by one instruction.
-__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
-    uint64_t r, a = *reinterpret_cast<uint64_t*>(&x), b = *reinterpret_cast<uint64_t*>(&y);
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return *reinterpret_cast<float2*>(&r);
-}
-__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
-    uint64_t r, a = *reinterpret_cast<uint64_t*>(&x), b = *reinterpret_cast<uint64_t*>(&y), c = *reinterpret_cast<uint64_t*>(&z);
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return *reinterpret_cast<float2*>(&r);
-}
 
 __device__ __forceinline__ float group_sum(float x, int lanes_log2) {
     for (int i = 0; i < lanes_log2; ++i) x += __shfl_xor_sync(0xffffffffu, x, 1 << i);

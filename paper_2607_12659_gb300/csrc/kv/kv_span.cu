@@ -10,6 +10,7 @@
 #include "kv_attend.h"
 #include "kv_parts.cuh"
 #include "kv8.cuh"
+#include "kv_pair.cuh"
 #include "kv_span.cuh"
 
 #include <algorithm>
@@ -58,11 +59,123 @@ struct Held<Code8> {
     __device__ static __forceinline__ float4 part(const Run& r, int i) { return value(i == 0 ? r.x.x : i == 1 ? r.x.y : i == 2 ? r.x.z : r.x.w); }
 };
 
+constexpr int SR_RANKS = 8;   // most blocks of a cluster, as in the handle's table
+// Most blocks of keys for a warp of a cluster. Microseconds of one launch and of two, bf16 and 8 bits, single tokens over one KV head
+// of 256: 300 keys 6.7 and 8.4, 8.0 and 8.9 for one request, 8.4 and 8.9, 8.7 and 10.0 for 16; 867 keys 7.8 and 8.3, 8.5 and 9.3 for one; 2000
+// keys (four blocks, two) 9.3 and 9.1, 9.6 and 10.6 for one, 9.6 and 11.1, 9.9 and 12.2 for eight; 4000 keys (eight, four) 12.0 and 9.6, 11.8 and
+// 11.0 for one, 12.1 and 11.7, 11.9 and 13.1 for four. (On the host a launch less is 2 us less.)
+constexpr int SR_JOIN_BLOCKS = 4;
+
+// Joins the parts of a tile of 8 query rows that the warps of a cluster's blocks hold in shared memory, and writes the result: each
+// block its own warps' first, then every block some of the rows over all blocks. A warp's part is laid out as in MergeSmem, PART bytes
+// from the one before; behind them lie the block's joined rows and their (m, l).
+template <int DP, typename E, int TEAM, int PART>
+struct JoinSmem {
+    static constexpr int ROWS = TEAM * PART, ML = ROWS + KR_ROWS * DP * 4, BYTES = ML + KR_ROWS * 8;
+    static_assert(PART % 16 == 0 && BYTES <= 227 * 1024, "fits an SM");
+};
+template <int DP, typename E, int TEAM, int PART>
+__device__ __forceinline__ void join_cluster(const AttendArgs& a, const Piece& x, int ranks, uint8_t* block, int warp, int lane) {
+    using L = JoinSmem<DP, E, TEAM, PART>;
+    constexpr int LD = MergeSmem<DP>::LD, NI = (DP + 127) / 128;
+    float* const joined = reinterpret_cast<float*>(block + L::ROWS);
+    float2* const ml = reinterpret_cast<float2*>(block + L::ML);
+    auto part = [&](int k) { return reinterpret_cast<const float*>(block + k * PART); };
+    auto weight = [&](float m, float most) { return m == -INFINITY ? 0.f : kr_ex2((m - most) * a.c2); };
+    for (int r = warp; r < KR_ROWS; r += TEAM) {
+        float2 p[TEAM];
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int k = 0; k < TEAM; ++k) {
+            p[k] = *(const float2*)(part(k) + KR_ROWS * LD + 2 * r);
+            m = fmaxf(m, p[k].x);
+        }
+        float4 o[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < TEAM; ++k) {
+            if (p[k].y == 0.f) continue;
+            const float w = weight(p[k].x, m);
+            l = fmaf(w, p[k].y, l);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int d = 4 * lane + 128 * i;
+                if (d >= DP) continue;
+                const float4 v = *(const float4*)(part(k) + r * LD + d);
+                o[i] = make_float4(fmaf(w, v.x, o[i].x), fmaf(w, v.y, o[i].y), fmaf(w, v.z, o[i].z), fmaf(w, v.w, o[i].w));
+            }
+        }
+        if (ranks == 1) {
+            if (x.t.r0 + r < x.t.R) {
+                RowAcc<DP> row;
+#pragma unroll
+                for (int i = 0; i < NI; ++i) row.o[i] = o[i];
+                row.m = m;
+                row.l = l;
+                write_row<DP, E>(a, row, row_index(a.c, x.t, x.t.r0 + r), 0, lane);
+            }
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int d = 4 * lane + 128 * i;
+            if (d < DP) *(float4*)(joined + r * DP + d) = o[i];
+        }
+        if (lane == 0) ml[r] = make_float2(m, l);
+    }
+    if (ranks == 1) return;
+    __syncwarp();
+    ptx::cluster_sync_all();
+    for (int r = (int)ptx::cluster_rank(); r < KR_ROWS; r += ranks) {
+        if (x.t.r0 + r >= x.t.R) continue;
+        const long long row = row_index(a.c, x.t, x.t.r0 + r);
+        for (int d = 2 * (int)threadIdx.x; d < a.c.D; d += 64 * TEAM) {
+            float2 p[SR_RANKS], v[SR_RANKS];
+            float m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int k = 0; k < SR_RANKS; ++k) {
+                p[k] = make_float2(-INFINITY, 0.f);
+                v[k] = make_float2(0.f, 0.f);
+                if (k < ranks) {
+                    p[k] = ptx::dsmem_ld_f2(ptx::dsmem_map(ptx::smem_u32(ml + r), (uint32_t)k));
+                    v[k] = ptx::dsmem_ld_f2(ptx::dsmem_map(ptx::smem_u32(joined + r * DP + d), (uint32_t)k));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < SR_RANKS; ++k) m = fmaxf(m, p[k].x);
+            float2 o = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < SR_RANKS; ++k) {
+                if (p[k].y == 0.f) continue;
+                const float w = weight(p[k].x, m);
+                l = fmaf(w, p[k].y, l);
+                o = make_float2(fmaf(w, v[k].x, o.x), fmaf(w, v[k].y, o.y));
+            }
+            const float inv = inverse_sum(l);
+            E* const out = static_cast<E*>(a.out) + row * a.c.D + d;
+            if constexpr (sizeof(E) == 2) *(uint32_t*)out = kr_pack(o.x * inv, o.y * inv);
+            else *(float2*)out = make_float2(o.x * inv, o.y * inv);
+            if (d == 0 && a.lse) a.lse[row] = log_sum(m, l, a.c.scale);
+        }
+    }
+    __syncwarp();
+    ptx::cluster_sync_all();   // every block's rows have been read
+}
+
 // fp32, on CUDA cores: a warp takes 8 query rows over blocks of 32 keys, scores with a key per lane, values with a lane per four
 // elements of d; the warps of a block take different row tiles or different keys of one. What bounds it is latency: a block's
 // loads, its products and 2^x follow one another. So a key's next elements, and the next values, are on their way while these
-// are used: 4 requests of 9 tokens with windows of 300 keys took 22 us with loads one by one.
-template <int DP, typename T>
+// are used (4 requests of 9 tokens with windows of 300 keys took 22 us with loads one by one), and the values' product reads a key's eight
+// probabilities from shared memory and tests nothing where all that a row is given is finite (17 us, and 12 in one launch).
+template <int DP>
+using CcJoin = JoinSmem<DP, float, AT_WARPS, MergeSmem<DP>::WARP_FLOATS * 4>;
+template <int DP, bool JOIN>
+struct CcSmem {
+    static constexpr int P_OFF = JOIN ? CcJoin<DP>::BYTES : MergeSmem<DP>::BYTES;   // [warp][32 keys][8 rows] probabilities
+    static constexpr int BYTES = P_OFF + AT_WARPS * 32 * KR_ROWS * 4;
+};
+template <int DP, typename T, bool JOIN>
 __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(const __grid_constant__ SpanArgs g) {
     extern __shared__ __align__(16) float kv_smem[];
     using Hd = Held<T>;
@@ -75,6 +188,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
     const int D = a.c.D;
     float* qs = kv_smem + warp / sp.wk * (KR_ROWS * DP);
     const int wk = warp % sp.wk;
+    float* ps = kv_smem + CcSmem<DP, JOIN>::P_OFF / 4 + warp * (32 * KR_ROWS);
     if (wk == 0) {
         for (int e0 = lane; e0 < KR_ROWS * (DP / 4); e0 += 4 * 32) {
             float4 v[4];
@@ -114,9 +228,9 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
     }
     for (int blk = b0 + wk; blk < b1; blk += sp.wk) {
         const int key0 = blocks.row(blk), key = key0 + lane;
-        float p[KR_ROWS];
+        float2 p2[KR_ROWS];
 #pragma unroll
-        for (int r = 0; r < KR_ROWS; ++r) p[r] = 0.f;
+        for (int r = 0; r < KR_ROWS; ++r) p2[r] = make_float2(0.f, 0.f);
         const bool live = span_sees(g.s, key, lim, first);   // by some row of the tile
         const T* kp = kbase + (live ? key * s.rs : 0);
         float ks = 1.f, vs = 1.f;
@@ -148,16 +262,22 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
 #pragma unroll
                     for (int r = 0; r < KR_ROWS; ++r) {
                         const float4 q = *(const float4*)(qs + r * DP + d0 + 4 * i);
-                        p[r] = fmaf(q.x, y.x, fmaf(q.y, y.y, fmaf(q.z, y.z, fmaf(q.w, y.w, p[r]))));
+                        // (to D = 128 pairs would take registers that the loads ahead need)
+                        if constexpr (DP == 256) p2[r] = fma2(make_float2(q.x, q.y), make_float2(y.x, y.y), fma2(make_float2(q.z, q.w), make_float2(y.z, y.w), p2[r]));
+                        else p2[r].x = fmaf(q.x, y.x, fmaf(q.y, y.y, fmaf(q.z, y.z, fmaf(q.w, y.w, p2[r].x))));
                     }
                 }
                 k = k2;
             }
         }
-        __syncwarp();
+        __syncwarp();   // (and the last block's probabilities have been read)
+        float p[KR_ROWS];
+        bool cut = false;   // some row does not see all of the block's keys
 #pragma unroll
         for (int r = 0; r < KR_ROWS; ++r) {
-            const float sc = span_sees(g.s, key, n[r], span_first(g.s, n[r])) ? p[r] * ks : -INFINITY;
+            const bool in = span_sees(g.s, key, n[r], span_first(g.s, n[r]));
+            cut = cut || !in;
+            const float sc = in ? (p2[r].x + p2[r].y) * ks : -INFINITY;
             float mx = sc;
 #pragma unroll
             for (int e = 16; e > 0; e >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, e));
@@ -171,6 +291,10 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
             p[r] = exp2f((sc - (m[r] == -INFINITY ? 0.f : m[r])) * a.c2);   // (of -inf 0, of NaN NaN)
             l[r] += p[r];
         }
+        cut = __any_sync(0xffffffffu, cut);
+        *(float4*)(ps + 8 * lane) = make_float4(p[0], p[1], p[2], p[3]);
+        *(float4*)(ps + 8 * lane + 4) = make_float4(p[4], p[5], p[6], p[7]);
+        __syncwarp();
         for (int t0 = 0; t0 < 32 && key0 + t0 < lim; t0 += VL) {
             float4 v[VL][NI];
 #pragma unroll
@@ -178,26 +302,44 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
 #pragma unroll
                 for (int i = 0; i < NI; ++i) v[t][i] = Hd::value(next[t][i]);
             if (t0 + VL < 32) load(t0 + VL);
+            if constexpr (HELD8) {
 #pragma unroll
-            for (int t = 0; t < VL; ++t) {
-                if (HELD8) {
+                for (int t = 0; t < VL; ++t) {
                     const float by = __shfl_sync(0xffffffffu, vs, t0 + t);
 #pragma unroll
                     for (int i = 0; i < NI; ++i) v[t][i] = make_float4(v[t][i].x * by, v[t][i].y * by, v[t][i].z * by, v[t][i].w * by);
                 }
+            }
+            // A hidden value is multiplied by a probability of zero where it is finite, else by nothing.
+            bool bad = false;
+            if (cut) {
+                float z = 0.f;
 #pragma unroll
-                for (int r = 0; r < KR_ROWS; ++r) {
-                    const float w = __shfl_sync(0xffffffffu, p[r], t0 + t);
-                    if (!span_sees(g.s, key0 + t0 + t, n[r], span_first(g.s, n[r]))) continue;   // a hidden value is not even multiplied by zero
+                for (int t = 0; t < VL; ++t)
 #pragma unroll
-                    for (int i = 0; i < NI; ++i) {
-                        o[r][i].x = fmaf(w, v[t][i].x, o[r][i].x);
-                        o[r][i].y = fmaf(w, v[t][i].y, o[r][i].y);
-                        o[r][i].z = fmaf(w, v[t][i].z, o[r][i].z);
-                        o[r][i].w = fmaf(w, v[t][i].w, o[r][i].w);
+                    for (int i = 0; i < NI; ++i) z = fmaf(v[t][i].x, 0.f, fmaf(v[t][i].y, 0.f, fmaf(v[t][i].z, 0.f, fmaf(v[t][i].w, 0.f, z))));
+                bad = __any_sync(0xffffffffu, !(z == 0.f));
+            }
+            // (Apart from each other: with the test in one path, 4 requests of 40 tokens over 2000 keys of 64 took 55 us for 46.)
+            auto add = [&](auto check) {
+#pragma unroll
+                for (int t = 0; t < VL; ++t) {
+                    const float4 wa = *(const float4*)(ps + 8 * (t0 + t)), wb = *(const float4*)(ps + 8 * (t0 + t) + 4);
+                    const float w[KR_ROWS] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+#pragma unroll
+                    for (int r = 0; r < KR_ROWS; ++r) {
+                        if (check.value && !span_sees(g.s, key0 + t0 + t, n[r], span_first(g.s, n[r]))) continue;
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) {
+                            const float2 xy = fma2(make_float2(w[r], w[r]), make_float2(v[t][i].x, v[t][i].y), make_float2(o[r][i].x, o[r][i].y));
+                            const float2 zw = fma2(make_float2(w[r], w[r]), make_float2(v[t][i].z, v[t][i].w), make_float2(o[r][i].z, o[r][i].w));
+                            o[r][i] = make_float4(xy.x, xy.y, zw.x, zw.y);
+                        }
                     }
                 }
-            }
+            };
+            if (bad) add(std::true_type{});
+            else add(std::false_type{});
         }
     }
     __syncthreads();   // the queries have been read
@@ -216,7 +358,12 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
             f[KR_ROWS * MergeSmem<DP>::LD + 2 * r + 1] = l[r];
         }
     }
-    merge_and_write<DP, float>(a, x, sp, kv_smem, warp, lane);
+    if constexpr (JOIN) {
+        __syncthreads();
+        join_cluster<DP, float, AT_WARPS, MergeSmem<DP>::WARP_FLOATS * 4>(a, x, sp.splits, reinterpret_cast<uint8_t*>(kv_smem), warp, lane);
+    } else {
+        merge_and_write<DP, float>(a, x, sp, kv_smem, warp, lane);
+    }
 }
 
 // bf16 queries. A warp works alone: it takes pieces (8 query rows over a range of the blocks that they see) in turn and streams
@@ -250,20 +397,10 @@ struct SrSmem {
     static constexpr int BYTES = SEEN_OFF + AHEAD * KR_ROWS * 4;
     static constexpr int ALONE = Q8 ? (DP == 256 ? 8 : DP == 128 ? 10 : 11) : DP == 256 ? 5 : 6;   // blocks of an SM
     static constexpr int REGS = 65536 / 32 / ALONE / 8 * 8 < 255 ? 65536 / 32 / ALONE / 8 * 8 : 255;
-    // Joined in a cluster: warps of a block, each with what is above for itself, and then the block's joined rows and their (m, l).
-    static constexpr int TEAM = Q8 ? 8 : 4;
-    static constexpr int JOIN_OFF = TEAM * BYTES, JOIN_ML = JOIN_OFF + KR_ROWS * DP * 4;
-    static constexpr int JOIN_BYTES = JOIN_ML + KR_ROWS * 8;
-    static_assert(BYTES % 128 == 0 && JOIN_BYTES <= 227 * 1024, "fits an SM");
-    static_assert(KR_ROWS * (DP + 4) * 4 + KR_ROWS * 8 <= 2 * STAGE, "a warp's rows fit its stages");
+    static constexpr int TEAM = Q8 ? 8 : 4;   // JOIN: warps of a block, each with all of this for itself
+    static constexpr int JOIN_BYTES = JoinSmem<DP, __nv_bfloat16, TEAM, BYTES>::BYTES;
+    static_assert(BYTES % 128 == 0 && MergeSmem<DP>::WARP_FLOATS * 4 <= 2 * STAGE, "a warp's rows fit its stages");
 };
-constexpr int SR_RANKS = 8;   // most blocks of a cluster, as in the handle's table
-// Most blocks of keys for a warp of a cluster. Microseconds of one launch and of two, bf16 and 8 bits, single tokens over one KV head
-// of 256: 300 keys 6.7 and 8.4, 8.0 and 8.9 for one request, 8.4 and 8.9, 8.7 and 10.0 for 16; 867 keys 7.8 and 8.3, 8.5 and 9.3 for one; 2000
-// keys (four blocks, two) 9.3 and 9.1, 9.6 and 10.6 for one, 9.6 and 11.1, 9.9 and 12.2 for eight; 4000 keys (eight, four) 12.0 and 9.6, 11.8 and
-// 11.0 for one, 12.1 and 11.7, 11.9 and 13.1 for four. (On the host a launch less is 2 us less.)
-constexpr int SR_JOIN_BLOCKS = 4;
-
 __device__ __forceinline__ void sr_ldsm4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -290,96 +427,6 @@ __device__ __forceinline__ uint32_t sr_half2(float lo, float hi) {
 }
 
 constexpr int SR_NONE = -4096;   // no scale seen yet
-
-// Joins the parts of a tile of 8 query rows that the warps of a cluster's blocks hold in shared memory, and writes the result: each
-// block its own warps' first, then every block some of the rows over all blocks.
-template <int DP, bool Q8>
-__device__ __forceinline__ void join_cluster(const AttendArgs& a, const Piece& x, uint8_t* block, int warp, int lane) {
-    using L = SrSmem<DP, Q8>;
-    constexpr int LD = DP + 4, NI = (DP + 127) / 128;
-    float* const joined = reinterpret_cast<float*>(block + L::JOIN_OFF);
-    float2* const ml = reinterpret_cast<float2*>(block + L::JOIN_ML);
-    auto part = [&](int k) { return reinterpret_cast<const float*>(block + k * L::BYTES); };
-    const int ranks = a.o.splits / L::TEAM;
-    auto weight = [&](float m, float most) { return m == -INFINITY ? 0.f : kr_ex2((m - most) * a.c2); };
-    for (int r = warp; r < KR_ROWS; r += L::TEAM) {
-        float2 p[L::TEAM];
-        float m = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int k = 0; k < L::TEAM; ++k) {
-            p[k] = *(const float2*)(part(k) + KR_ROWS * LD + 2 * r);
-            m = fmaxf(m, p[k].x);
-        }
-        float4 o[NI];
-#pragma unroll
-        for (int i = 0; i < NI; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < L::TEAM; ++k) {
-            if (p[k].y == 0.f) continue;
-            const float w = weight(p[k].x, m);
-            l = fmaf(w, p[k].y, l);
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int d = 4 * lane + 128 * i;
-                if (d >= DP) continue;
-                const float4 v = *(const float4*)(part(k) + r * LD + d);
-                o[i] = make_float4(fmaf(w, v.x, o[i].x), fmaf(w, v.y, o[i].y), fmaf(w, v.z, o[i].z), fmaf(w, v.w, o[i].w));
-            }
-        }
-        if (ranks == 1) {
-            if (x.t.r0 + r < x.t.R) {
-                RowAcc<DP> row;
-#pragma unroll
-                for (int i = 0; i < NI; ++i) row.o[i] = o[i];
-                row.m = m;
-                row.l = l;
-                write_row<DP, __nv_bfloat16>(a, row, row_index(a.c, x.t, x.t.r0 + r), 0, lane);
-            }
-            continue;
-        }
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int d = 4 * lane + 128 * i;
-            if (d < DP) *(float4*)(joined + r * DP + d) = o[i];
-        }
-        if (lane == 0) ml[r] = make_float2(m, l);
-    }
-    if (ranks == 1) return;
-    __syncwarp();
-    ptx::cluster_sync_all();
-    for (int r = (int)ptx::cluster_rank(); r < KR_ROWS; r += ranks) {
-        if (x.t.r0 + r >= x.t.R) continue;
-        const long long row = row_index(a.c, x.t, x.t.r0 + r);
-        for (int d = 2 * (int)threadIdx.x; d < a.c.D; d += 64 * L::TEAM) {
-            float2 p[SR_RANKS], v[SR_RANKS];
-            float m = -INFINITY, l = 0.f;
-#pragma unroll
-            for (int k = 0; k < SR_RANKS; ++k) {
-                p[k] = make_float2(-INFINITY, 0.f);
-                v[k] = make_float2(0.f, 0.f);
-                if (k < ranks) {
-                    p[k] = ptx::dsmem_ld_f2(ptx::dsmem_map(ptx::smem_u32(ml + r), (uint32_t)k));
-                    v[k] = ptx::dsmem_ld_f2(ptx::dsmem_map(ptx::smem_u32(joined + r * DP + d), (uint32_t)k));
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < SR_RANKS; ++k) m = fmaxf(m, p[k].x);
-            float2 o = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < SR_RANKS; ++k) {
-                if (p[k].y == 0.f) continue;
-                const float w = weight(p[k].x, m);
-                l = fmaf(w, p[k].y, l);
-                o = make_float2(fmaf(w, v[k].x, o.x), fmaf(w, v[k].y, o.y));
-            }
-            const float inv = inverse_sum(l);
-            *(uint32_t*)(static_cast<__nv_bfloat16*>(a.out) + row * a.c.D + d) = kr_pack(o.x * inv, o.y * inv);
-            if (d == 0 && a.lse) a.lse[row] = log_sum(m, l, a.c.scale);
-        }
-    }
-    __syncwarp();
-    ptx::cluster_sync_all();   // every block's rows have been read
-}
 
 template <int DP, bool Q8, bool JOIN>
 __global__ void __maxnreg__((JOIN ? 248 : SrSmem<DP, Q8>::REGS)) k_kv_span_rows(const __grid_constant__ SpanArgs g_) {
@@ -827,7 +874,7 @@ __global__ void __maxnreg__((JOIN ? 248 : SrSmem<DP, Q8>::REGS)) k_kv_span_rows(
         }
         if constexpr (JOIN) {
             // The warp's rows go where its stages were, whose copies have all been read.
-            constexpr int LD = DP + 4;
+            constexpr int LD = MergeSmem<DP>::LD;
             float* f = reinterpret_cast<float*>(sr_smem);
             __syncwarp();
 #pragma unroll
@@ -842,7 +889,7 @@ __global__ void __maxnreg__((JOIN ? 248 : SrSmem<DP, Q8>::REGS)) k_kv_span_rows(
                 *(float2*)(f + KR_ROWS * LD + 4 * j + 2) = make_float2(m1, l1);
             }
             __syncthreads();
-            join_cluster<DP, Q8>(a, x, sr_block, warp, lane);
+            join_cluster<DP, __nv_bfloat16, L::TEAM, L::BYTES>(a, x, a.o.splits / L::TEAM, sr_block, warp, lane);
             return;
         }
         const long long row0 = in0 ? row_index(a.c, x.t, rj) : 0, row1 = in1 ? row_index(a.c, x.t, rj + 1) : 0;
@@ -898,6 +945,32 @@ __global__ void __maxnreg__((JOIN ? 248 : SrSmem<DP, Q8>::REGS)) k_kv_span_rows(
     }
 }
 
+// The kernels of a handle and their shared memory: on its own, and joined in clusters of blocks of `team` warps.
+template <int DP>
+struct SpanKernel {
+    using Rows8 = SrSmem<DP, true>;
+    using Rows = SrSmem<DP, false>;
+    void (*alone)(SpanArgs), (*joined)(SpanArgs);
+    int bytes, joined_bytes, keys, team;
+    SpanKernel(const jpi_kv_handle* h, bool held8) {
+        if (!h->bf16) {
+            alone = held8 ? k_kv_span_cc<DP, Code8, false> : k_kv_span_cc<DP, float, false>;
+            joined = held8 ? k_kv_span_cc<DP, Code8, true> : k_kv_span_cc<DP, float, true>;
+            bytes = CcSmem<DP, false>::BYTES;
+            joined_bytes = CcSmem<DP, true>::BYTES;
+            keys = 32;
+            team = AT_WARPS;
+        } else {
+            alone = held8 ? k_kv_span_rows<DP, true, false> : k_kv_span_rows<DP, false, false>;
+            joined = held8 ? k_kv_span_rows<DP, true, true> : k_kv_span_rows<DP, false, true>;
+            bytes = held8 ? Rows8::BYTES : Rows::BYTES;
+            joined_bytes = held8 ? Rows8::JOIN_BYTES : Rows::JOIN_BYTES;
+            keys = held8 ? Rows8::KEYS : Rows::KEYS;
+            team = held8 ? Rows8::TEAM : Rows::TEAM;
+        }
+    }
+};
+
 // Rows of the cache that the tokens of a tile of 8 query rows see, with the ends of their blocks.
 long long rows_span(const KvCall& c, const KvSpan& sn, int step) {
     const long long toks = std::min<long long>(c.tokens, (KR_ROWS + c.gq - 1) / c.gq + 1);
@@ -929,13 +1002,15 @@ SidePlan plan_span(const jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, in
 // 0: more tiles than fit one block each, or more blocks of keys for a warp than a second launch takes.
 template <int DP>
 int join_ranks(const jpi_kv_handle* h, const KvCall& c, const KvSpan& sn) {
-    if (!h->bf16) return 0;
-    const int keys = sn.ks ? SrSmem<DP, true>::KEYS : SrSmem<DP, false>::KEYS, team = sn.ks ? SrSmem<DP, true>::TEAM : SrSmem<DP, false>::TEAM;
+    // (The fp32 kernel's blocks of one tile take the same time alone; with more than one they hold four tiles each there: 4 requests of 9
+    // tokens over 300 keys of one KV head of 64 17 us, 14 joined, over 867 of 256 48 and 28.)
+    if (!h->bf16 && (long long)c.tokens * c.gq <= KR_ROWS) return 0;
+    const SpanKernel<DP> k(h, sn.ks != nullptr);
     const long long tiles = (long long)c.batch * c.K * (((long long)c.tokens * c.gq + KR_ROWS - 1) / KR_ROWS);
-    const long long nb = (rows_span(c, sn, keys) + keys - 1) / keys;
+    const long long nb = (rows_span(c, sn, k.keys) + k.keys - 1) / k.keys;
     int n = 3;
     while (n >= 0 && tiles > h->span_clusters[sn.ks != nullptr][n]) --n;
-    return n >= 0 && nb <= (long long)SR_JOIN_BLOCKS * team << n ? 1 << n : 0;
+    return n >= 0 && nb <= (long long)SR_JOIN_BLOCKS * k.team << n ? 1 << n : 0;
 }
 
 template <int DP>
@@ -954,23 +1029,21 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
         return splits == 1 ? JPI_OK : launch_kv_combine(h, c, splits, out, lse, st);
     }
     if (const int ranks = join_ranks<DP>(h, c, sn)) {
-        const int team = sn.ks ? SrSmem<DP, true>::TEAM : SrSmem<DP, false>::TEAM;
+        const SpanKernel<DP> k(h, sn.ks != nullptr);
         a.o.tiles = (int)(((long long)c.tokens * c.gq + KR_ROWS - 1) / KR_ROWS);
-        a.o.splits = ranks * team;
+        a.o.wk = k.team;
+        a.o.splits = h->bf16 ? ranks * k.team : ranks;   // (a block of the fp32 kernel is one split, whose keys its warps share)
         a.o.blocks = (long long)c.batch * c.K * a.o.tiles * a.o.splits;
         a.o.by_splits = KvDiv((uint32_t)a.o.splits);
         a.o.by_tiles = KvDiv((uint32_t)a.o.tiles);
         a.out = out;
-        return kv_start_clusters(sn.ks ? k_kv_span_rows<DP, true, true> : k_kv_span_rows<DP, false, true>, dim3((unsigned)(a.o.blocks / team)),
-                                 (unsigned)ranks, 32 * team, sn.ks ? SrSmem<DP, true>::JOIN_BYTES : SrSmem<DP, false>::JOIN_BYTES, false, st, g);
+        return kv_start_clusters(k.joined, dim3((unsigned)((long long)c.batch * c.K * a.o.tiles * ranks)), (unsigned)ranks, 32 * k.team,
+                                 (size_t)k.joined_bytes, false, st, g);
     }
+    const SpanKernel<DP> k(h, sn.ks != nullptr);
     const long long most = (long long)(sn.ks ? SrSmem<DP, true>::ALONE : SrSmem<DP, false>::ALONE) * h->num_sms;   // resident warps of the row kernel
-    if (h->bf16) {
-        const int keys = sn.ks ? SrSmem<DP, true>::KEYS : SrSmem<DP, false>::KEYS;
-        a.o = plan_span(h, c, sn, 1, keys, 4 * keys, most);
-    } else {
-        a.o = plan_span(h, c, sn, AT_WARPS, 32, 32, 2ll * h->num_sms);
-    }
+    if (h->bf16) a.o = plan_span(h, c, sn, 1, k.keys, 4 * k.keys, most);
+    else a.o = plan_span(h, c, sn, AT_WARPS, 32, 32, 2ll * h->num_sms);
     a.p.splits = 0;
     a.parts = a.o.splits;
     if (a.o.blocks > 0x7fffffffll) {
@@ -978,41 +1051,32 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
         return JPI_ERR_SHAPE;
     }
     if (a.parts == 1) a.out = out;
-    if (h->bf16)
-        JPI_TRY(kv_start(sn.ks ? k_kv_span_rows<DP, true, false> : k_kv_span_rows<DP, false, false>, dim3((unsigned)std::min(a.o.blocks, most)), 32,
-                         sn.ks ? SrSmem<DP, true>::BYTES : SrSmem<DP, false>::BYTES, false, st, g));
-    else
-        JPI_TRY(kv_start(sn.ks ? k_kv_span_cc<DP, Code8> : k_kv_span_cc<DP, float>, dim3((unsigned)a.o.blocks), AT_THREADS,
-                         MergeSmem<DP>::BYTES, false, st, g));
+    const long long blocks = h->bf16 ? std::min(a.o.blocks, most) : a.o.blocks;   // (the row kernel's take pieces in turn)
+    JPI_TRY(kv_start(k.alone, dim3((unsigned)blocks), h->bf16 ? 32 : AT_THREADS, (size_t)k.bytes, false, st, g));
     return a.parts == 1 ? JPI_OK : launch_kv_combine(h, c, a.parts, out, lse, st);
 }
 
 template <int DP>
 jpi_status prepare_dim(jpi_kv_handle* h) {
-    if (!h->bf16) {
-        for (auto* kernel : {k_kv_span_cc<DP, float>, k_kv_span_cc<DP, Code8>})
-            JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MergeSmem<DP>::BYTES));
-        return JPI_OK;
-    }
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, false>::BYTES));
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, true>::BYTES));
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, false>::JOIN_BYTES));
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_rows<DP, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SrSmem<DP, true>::JOIN_BYTES));
-    for (auto* kernel : {k_kv_span_rows<DP, false, false>, k_kv_span_rows<DP, true, false>})   // all of its loads go to shared memory
-        JPI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
-    for (int held8 = 0; held8 < 2; ++held8)
+    for (int held8 = 0; held8 < 2; ++held8) {
+        const SpanKernel<DP> k(h, held8 != 0);
+        JPI_CUDA_TRY(cudaFuncSetAttribute(k.alone, cudaFuncAttributeMaxDynamicSharedMemorySize, k.bytes));
+        JPI_CUDA_TRY(cudaFuncSetAttribute(k.joined, cudaFuncAttributeMaxDynamicSharedMemorySize, k.joined_bytes));
+        if (h->bf16)   // all of its loads go to shared memory
+            JPI_CUDA_TRY(cudaFuncSetAttribute(k.alone, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
         for (int n = 0; n < 4; ++n) {
             cudaLaunchAttribute at = {};
             at.id = cudaLaunchAttributeClusterDimension;
             at.val.clusterDim = {1u << n, 1, 1};
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(1u << n);
-            cfg.blockDim = dim3(32 * (held8 ? SrSmem<DP, true>::TEAM : SrSmem<DP, false>::TEAM));
-            cfg.dynamicSmemBytes = held8 ? SrSmem<DP, true>::JOIN_BYTES : SrSmem<DP, false>::JOIN_BYTES;
+            cfg.blockDim = dim3(32u * k.team);
+            cfg.dynamicSmemBytes = k.joined_bytes;
             cfg.attrs = &at;
             cfg.numAttrs = 1;
-            JPI_CUDA_TRY(cudaOccupancyMaxActiveClusters(&h->span_clusters[held8][n], held8 ? k_kv_span_rows<DP, true, true> : k_kv_span_rows<DP, false, true>, &cfg));
+            JPI_CUDA_TRY(cudaOccupancyMaxActiveClusters(&h->span_clusters[held8][n], k.joined, &cfg));
         }
+    }
     return JPI_OK;
 }
 
