@@ -19,6 +19,7 @@ struct jpi_kv_handle {
     bool pdl = true;             // kernels of one call may start before the one before them has finished
     int tiles = -1;              // attend, weigh: the tensor-core tiles never, (1) wherever they fit, (-1) by size
     int span_clusters[2][4] = {};   // attend_window, kv8_attend: clusters of 1, 2, 4 and 8 joining blocks that are resident together
+    int tile_pairs[2] = {};         // likewise pairs of blocks of their 128-row tiles
     size_t device_bytes = 0;
     std::vector<void*> allocations;
 };
@@ -106,6 +107,21 @@ jpi_status kv_start_clusters(void (*kernel)(Params...), dim3 grid, unsigned rank
         at[cfg.numAttrs++].val.clusterDim.z = 1;
     }
     JPI_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    return JPI_OK;
+}
+// Clusters of `ranks` blocks that are resident together.
+template <typename... Params>
+jpi_status kv_resident_clusters(void (*kernel)(Params...), unsigned ranks, int threads, size_t smem, int* n) {
+    cudaLaunchAttribute at = {};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim = {ranks, 1, 1};
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ranks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    JPI_CUDA_TRY(cudaOccupancyMaxActiveClusters(n, kernel, &cfg));
     return JPI_OK;
 }
 template <typename... Params, typename... Args>

@@ -1024,9 +1024,10 @@ jpi_status launch_dim(jpi_kv_handle* h, const KvCall& c, const KvSpan& sn, void*
     a.po = static_cast<float*>(h->ws);
     a.pml = reinterpret_cast<float2*>(a.po + (size_t)ws_rows(h) * c.D);
     a.lse = lse;
-    if (const int splits = kv_span_tiles_plan(h, c, sn, std::max(1ll, ws_rows(h) / a.rows))) {
-        JPI_TRY(launch_kv_span_tiles(h, c, sn, splits, a.po, a.pml, out, lse, st));
-        return splits == 1 ? JPI_OK : launch_kv_combine(h, c, splits, out, lse, st);
+    bool joined;
+    if (const int splits = kv_span_tiles_plan(h, c, sn, std::max(1ll, ws_rows(h) / a.rows), &joined)) {
+        JPI_TRY(launch_kv_span_tiles(h, c, sn, splits, joined, a.po, a.pml, out, lse, st));
+        return splits == 1 || joined ? JPI_OK : launch_kv_combine(h, c, splits, out, lse, st);
     }
     if (const int ranks = join_ranks<DP>(h, c, sn)) {
         const SpanKernel<DP> k(h, sn.ks != nullptr);
@@ -1064,18 +1065,8 @@ jpi_status prepare_dim(jpi_kv_handle* h) {
         JPI_CUDA_TRY(cudaFuncSetAttribute(k.joined, cudaFuncAttributeMaxDynamicSharedMemorySize, k.joined_bytes));
         if (h->bf16)   // all of its loads go to shared memory
             JPI_CUDA_TRY(cudaFuncSetAttribute(k.alone, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
-        for (int n = 0; n < 4; ++n) {
-            cudaLaunchAttribute at = {};
-            at.id = cudaLaunchAttributeClusterDimension;
-            at.val.clusterDim = {1u << n, 1, 1};
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(1u << n);
-            cfg.blockDim = dim3(32u * k.team);
-            cfg.dynamicSmemBytes = k.joined_bytes;
-            cfg.attrs = &at;
-            cfg.numAttrs = 1;
-            JPI_CUDA_TRY(cudaOccupancyMaxActiveClusters(&h->span_clusters[held8][n], k.joined, &cfg));
-        }
+        for (int n = 0; n < 4; ++n)
+            JPI_TRY(kv_resident_clusters(k.joined, 1u << n, 32 * k.team, (size_t)k.joined_bytes, &h->span_clusters[held8][n]));
     }
     return JPI_OK;
 }

@@ -16,10 +16,11 @@ jpi_status kv_span_prepare(jpi_kv_handle* h);
 jpi_status launch_kv_span(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, void* out, float* lse, cudaStream_t st);
 
 // On tensor-core tiles of 128 query rows (kv_span_t5.cu): the key splits, of at most `room`, that a call takes there; 0: it does not.
-jpi_status kv_span_tiles_prepare(const jpi_kv_handle* h);
-int kv_span_tiles_plan(const jpi_kv_handle* h, const KvCall& c, const KvSpan& s, long long room);
-// Its parts in `po` [splits][rows][D] and `pml` [rows][splits], or of one the result itself.
-jpi_status launch_kv_span_tiles(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, int splits, float* po, float2* pml, void* out, float* lse,
-                                cudaStream_t st);
+// `joined`: the launch joins them itself.
+jpi_status kv_span_tiles_prepare(jpi_kv_handle* h);
+int kv_span_tiles_plan(const jpi_kv_handle* h, const KvCall& c, const KvSpan& s, long long room, bool* joined);
+// Its parts in `po` [splits][rows][D] and `pml` [rows][splits], or of one, or joined, the result itself.
+jpi_status launch_kv_span_tiles(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, int splits, bool joined, float* po, float2* pml, void* out,
+                                float* lse, cudaStream_t st);
 
 }  // namespace jpi

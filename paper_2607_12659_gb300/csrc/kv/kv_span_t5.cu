@@ -24,7 +24,9 @@
 // its own keys), and the product adds nothing. A row that sees nothing has l = 0, and what its outputs hold is not used.
 //
 // Each block leaves a part (unnormalised fp32 rows, (m, l)) for the combine, or the result: rows pass through shared
-// memory (the ring, free by then).
+// memory (the ring, free by then). Of two parts whose pairs of blocks are all resident together (JOIN) the pair is a cluster, and each of
+// its blocks joins and writes half of the rows from both shared memories: 16 x 51 tokens over 867 rows in 8 bits 31.6 us with the
+// combine, 23.7 so; 256 tokens of 32 heads on 8 over 2100 keys 28.4 and 20.4.
 //
 // Every wait is bounded; a wait that gives up records an error in the handle's word, and its thread waits for
 // nothing more.
@@ -51,6 +53,7 @@ constexpr float ST_RESCALE = 24.f, ST_RESCALE8 = 11.f;
 constexpr int ST_BOOST = 4;         // log2 of what probabilities of fp16 are multiplied by
 constexpr int ST_NONE = -4096;      // no scale seen yet
 constexpr int ST_RUN = 32;          // blocks of a group whose scales are read together
+constexpr int ST_RANKS = 2;         // parts that are joined in a cluster
 // Query rows of a request and KV head from which a call takes the tiles, and the elements of keys up to which it stays with the row
 // kernel all the same, which reads a key once for every 8 query rows. Microseconds of row kernel and tiles, bf16: 1 KV head at D = 256,
 // 128 rows over 1024 keys (4 M elements) 13.6 and 13.3, over 4096 18.0 and 14.8; 8 KV heads at D = 128, 128 rows over 256 keys
@@ -60,9 +63,10 @@ constexpr int ST_RUN = 32;          // blocks of a group whose scales are read t
 // D = 64 over 4096 (64 M) 45.1 and 48.7.
 constexpr int ST_LEAST = 32;
 constexpr long long st_row_elements(bool held8, long long R, int D) { return (held8 ? (R < 64 && D <= 128 ? 60ll : 12ll) : 4ll) << 20; }
-// Cycles of a key block of D elements, of a block's start and end, of the combine's launch, and bytes a cycle to and from the workspace.
+// Cycles of a key block of D elements, of a block's start and end, of the combine's launch, of a pair's meeting, and bytes a cycle to and from
+// the workspace.
 constexpr long long st_block(bool held8, int D) { return held8 ? 1000 + 8 * D : 500 + 4 * D; }
-constexpr long long ST_ENDS = 10000, ST_JOIN = 8000, ST_BYTES = 2600;
+constexpr long long ST_ENDS = 10000, ST_JOIN = 8000, ST_MEET = 6500, ST_BYTES = 2600;
 
 struct SpanMaps {
     CUtensorMap k, v;
@@ -79,6 +83,7 @@ struct SpanTileArgs {
     float2* pml;           // [rows][parts]
     long long rows;
     __nv_bfloat16* out;    // of a call of one part: the result, else null
+    __nv_bfloat16* joined; // of one whose two parts are joined in clusters: the result, else null
     float* lse;
     int* err;
 };
@@ -116,7 +121,62 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <int DP, bool Q8>
+// Joins the parts of a tile, staged in the shared memories of the cluster's blocks, and writes the rows of block `rank`. What
+// bounds it is the latency of reads from the other block, so that eight of 16 bytes a lane, of several rows, are on their way together.
+template <int DP, int LD, int WARPS>
+__device__ __forceinline__ void join_tile(const SpanTileArgs& a, const RowTile& t, int rank, const uint8_t* rows, const float2* ml, int warp, int lane) {
+    constexpr int RANKS = ST_RANKS, CH = DP > 128 ? 2 : 1, RW = 8 / RANKS / CH;   // 128-element parts of a row; rows together
+    constexpr int step = RANKS * WARPS;
+    for (int r0 = rank + RANKS * warp; r0 < ST_ROWS; r0 += RW * step) {
+        float2 part[RW][RANKS];
+        float4 v[RW][CH][RANKS];
+#pragma unroll
+        for (int u = 0; u < RW; ++u)
+#pragma unroll
+            for (int k = 0; k < RANKS; ++k) {
+                const int r = r0 + u * step;
+                part[u][k] = make_float2(-INFINITY, 0.f);
+                if (r >= ST_ROWS || t.r0 + r >= t.R) continue;
+                part[u][k] = ptx::dsmem_ld_f2(ptx::dsmem_map(ptx::smem_u32(ml + r), (uint32_t)k));
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    v[u][c][k] = ptx::dsmem_ld_f4(ptx::dsmem_map(ptx::smem_u32(rows + r * LD + 16 * min(lane + 32 * c, DP / 4 - 1)), (uint32_t)k));
+            }
+#pragma unroll
+        for (int u = 0; u < RW; ++u) {
+            const int r = r0 + u * step;
+            if (r >= ST_ROWS || t.r0 + r >= t.R) continue;
+            const long long row_at = row_index(a.c, t, t.r0 + r);
+            float m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int k = 0; k < RANKS; ++k) m = fmaxf(m, part[u][k].x);
+            float4 x[CH];
+#pragma unroll
+            for (int c = 0; c < CH; ++c) x[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < RANKS; ++k) {
+                if (part[u][k].y == 0.f) continue;   // a part without a sum holds nothing
+                const float w = part[u][k].x == -INFINITY ? 0.f : kr_ex2((part[u][k].x - m) * a.c2);
+                l = fmaf(w, part[u][k].y, l);
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const float4 y = v[u][c][k];
+                    x[c] = make_float4(fmaf(w, y.x, x[c].x), fmaf(w, y.y, x[c].y), fmaf(w, y.z, x[c].z), fmaf(w, y.w, x[c].w));
+                }
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int d = 4 * (lane + 32 * c);
+                if (d < a.c.D)
+                    *(uint2*)(a.joined + row_at * a.c.D + d) = make_uint2(kr_pack(x[c].x * inv, x[c].y * inv), kr_pack(x[c].z * inv, x[c].w * inv));
+            }
+            if (lane == 0 && a.lse) a.lse[row_at] = l == 0.f ? -INFINITY : fmaf(m, a.c.scale, logf(l));
+        }
+    }
+}
+
+template <int DP, bool Q8, bool JOIN>
 __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_constant__ SpanMaps maps,
                                                                const __grid_constant__ SpanTileArgs a) {
     using L = StSmem<DP, Q8>;
@@ -776,44 +836,61 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         }
         if (grp == NG - 1 && half == 0 && valid) {
             const long long row_at = row_index(a.c, t, r);
-            if (!a.out) a.pml[row_at * a.splits + split] = make_float2(m_used, l);
+            if constexpr (JOIN) ml[row] = make_float2(m_used, l);   // (the groups' have been read)
+            else if (!a.out) a.pml[row_at * a.splits + split] = make_float2(m_used, l);
             else if (a.lse) a.lse[row_at] = l == 0.f ? -INFINITY : fmaf(m_used, a.c.scale, logf(l));
         }
         // Rows leave by whole warps. (A bulk copy a row, 128 of them, took 3 thousand cycles longer.)
         ptx::named_bar_sync(9, NG * ST_SOFT);
+        if constexpr (!JOIN) {
 #pragma unroll 4
-        for (int rr = warp - 4; rr < ST_ROWS; rr += 8 * NG) {
-            if (!good || t.r0 + rr >= t.R) continue;
-            const long long row_at = row_index(a.c, t, t.r0 + rr);
-            const uint8_t* from = st_smem + rr * L::OUT_LD;
-            if (a.out) {
-                const int d = 8 * lane, h = d >= DP / 2;
-                if (d < a.c.D)
-                    *(uint4*)(a.out + row_at * a.c.D + d) = nb == 0 ? make_uint4(0, 0, 0, 0) : *(const uint4*)(from + h * (DP * 2) + (d - h * (DP / 2)) * 2);
-            } else if (nb > 0) {
-                for (int d = 4 * lane; d < a.c.D; d += 128)
-                    *(uint4*)(a.po + ((long long)split * a.rows + row_at) * a.c.D + d) = *(const uint4*)(from + 4 * d);
+            for (int rr = warp - 4; rr < ST_ROWS; rr += 8 * NG) {
+                if (!good || t.r0 + rr >= t.R) continue;
+                const long long row_at = row_index(a.c, t, t.r0 + rr);
+                const uint8_t* from = st_smem + rr * L::OUT_LD;
+                if (a.out) {
+                    const int d = 8 * lane, h = d >= DP / 2;
+                    if (d < a.c.D)
+                        *(uint4*)(a.out + row_at * a.c.D + d) = nb == 0 ? make_uint4(0, 0, 0, 0) : *(const uint4*)(from + h * (DP * 2) + (d - h * (DP / 2)) * 2);
+                } else if (nb > 0) {
+                    for (int d = 4 * lane; d < a.c.D; d += 128)
+                        *(uint4*)(a.po + ((long long)split * a.rows + row_at) * a.c.D + d) = *(const uint4*)(from + 4 * d);
+                }
             }
         }
     }
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
+    if constexpr (JOIN) {
+        // The parts of the tile are in the shared memories of the cluster's blocks, each of which writes some of the rows.
+        ptx::cluster_sync_all();
+        bool whole = true;
+        for (int k = 0; k < ST_RANKS; ++k) whole = whole && __float_as_int(ptx::dsmem_ld_f32(ptx::dsmem_map(ptx::smem_u32(flag), (uint32_t)k))) == 0;
+        if (whole) join_tile<DP, L::OUT_LD, L::THREADS / 32>(a, t, (int)split, st_smem, ml, tid >> 5, lane);
+        __syncwarp();
+        ptx::cluster_sync_all();   // every block's rows have been read
+    }
     if (tid == 0 && *flag != 0) atomicCAS(a.err, 0, *flag);
     if (warp == 1) ptx::tmem_dealloc(tmem, L::TMEM_COLS);
 }
 
 template <int DP>
 jpi_status launch_dim(const SpanTileArgs& a, const SpanMaps& m, unsigned blocks, cudaStream_t st) {
-    return a.s.ks ? kv_start(k_kv_span_t5<DP, true>, dim3(blocks), StSmem<DP, true>::THREADS, StSmem<DP, true>::BYTES, false, st, m, a)
-                  : kv_start(k_kv_span_t5<DP, false>, dim3(blocks), StSmem<DP, false>::THREADS, StSmem<DP, false>::BYTES, false, st, m, a);
+    auto* const kernel = a.s.ks ? (a.joined ? k_kv_span_t5<DP, true, true> : k_kv_span_t5<DP, true, false>)
+                                : (a.joined ? k_kv_span_t5<DP, false, true> : k_kv_span_t5<DP, false, false>);
+    return kv_start_clusters(kernel, dim3(blocks), a.joined ? ST_RANKS : 1, a.s.ks ? StSmem<DP, true>::THREADS : StSmem<DP, false>::THREADS,
+                             (size_t)(a.s.ks ? StSmem<DP, true>::BYTES : StSmem<DP, false>::BYTES), false, st, m, a);
 }
 
 template <int DP>
-jpi_status prepare_dim() {
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_t5<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, StSmem<DP, false>::BYTES));
-    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_t5<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, StSmem<DP, true>::BYTES));
-    return JPI_OK;
+jpi_status prepare_dim(jpi_kv_handle* h) {
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_t5<DP, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, StSmem<DP, false>::BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_t5<DP, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, StSmem<DP, true>::BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_t5<DP, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, StSmem<DP, false>::BYTES));
+    JPI_CUDA_TRY(cudaFuncSetAttribute(k_kv_span_t5<DP, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, StSmem<DP, true>::BYTES));
+    JPI_TRY(kv_resident_clusters(k_kv_span_t5<DP, false, true>, ST_RANKS, StSmem<DP, false>::THREADS, StSmem<DP, false>::BYTES, &h->tile_pairs[0]));
+    return kv_resident_clusters(k_kv_span_t5<DP, true, true>, ST_RANKS, StSmem<DP, true>::THREADS, StSmem<DP, true>::BYTES, &h->tile_pairs[1]);
 }
 
 // Rows of the cache that the tokens of a tile see at most.
@@ -824,12 +901,13 @@ long long tile_span(const KvCall& c, const KvSpan& s) {
 
 }  // namespace
 
-jpi_status kv_span_tiles_prepare(const jpi_kv_handle* h) {
+jpi_status kv_span_tiles_prepare(jpi_kv_handle* h) {
     if (!h->bf16 || h->D < 64) return JPI_OK;
-    return h->D <= 64 ? prepare_dim<64>() : h->D <= 128 ? prepare_dim<128>() : prepare_dim<256>();
+    return h->D <= 64 ? prepare_dim<64>(h) : h->D <= 128 ? prepare_dim<128>(h) : prepare_dim<256>(h);
 }
 
-int kv_span_tiles_plan(const jpi_kv_handle* h, const KvCall& c, const KvSpan& s, long long room) {
+int kv_span_tiles_plan(const jpi_kv_handle* h, const KvCall& c, const KvSpan& s, long long room, bool* joined) {
+    *joined = false;
     if (!h->bf16 || c.D < 64 || h->tiles == 0) return 0;
     const long long R = (long long)c.tokens * c.gq, tiles = (R + ST_ROWS - 1) / ST_ROWS, blocks = tiles * c.K * c.batch;
     const long long span = tile_span(c, s), nb = (span + ST_KEYS - 1) / ST_KEYS;
@@ -837,21 +915,26 @@ int kv_span_tiles_plan(const jpi_kv_handle* h, const KvCall& c, const KvSpan& s,
     if (!s.ks && !kv_map_dims(c.own, c.K, c.D, c.batch, &m)) return 0;
     if (blocks * nb >= 1ll << 31) return 0;
     if (h->tiles < 0 && (R < ST_LEAST || (R + KR_ROWS - 1) / KR_ROWS * c.K * c.batch * span * c.D <= st_row_elements(s.ks, R, c.D))) return 0;
-    // Splits by which the waves of blocks end first; a result in parts has its combine, and its rows to and from the workspace.
+    // Splits by which the waves of blocks end first; a result in parts has its combine, and its rows to and from the workspace, or, of two
+    // parts in clusters that are all resident together, their meeting. (In clusters of four the meeting takes what the combine does: 64
+    // tokens of 8 heads over 2100 keys of 256 17.2 us for 15.5.)
     long long best = 1, best_time = -1;
-    for (long long n = 1; n <= std::min({nb, room, std::max(1ll, 2ll * h->num_sms / blocks)}); ++n) {
+    for (long long n = 1; n <= std::min(nb, std::max(1ll, 2ll * h->num_sms / blocks)); ++n) {
+        const bool meet = n == ST_RANKS && blocks <= h->tile_pairs[s.ks != nullptr];
+        if (!meet && n > room) continue;
         const long long time = (blocks * n + h->num_sms - 1) / h->num_sms * ((nb + n - 1) / n * st_block(s.ks, c.D) + ST_ENDS) +
-                               (n > 1 ? ST_JOIN + 2 * n * c.batch * c.tokens * c.H * c.D * 4 / ST_BYTES : 0);
+                               (meet ? ST_MEET : n > 1 ? ST_JOIN + 2 * n * c.batch * c.tokens * c.H * c.D * 4 / ST_BYTES : 0);
         if (best_time < 0 || time < best_time) {
             best_time = time;
             best = n;
+            *joined = meet;
         }
     }
     return (int)best;
 }
 
-jpi_status launch_kv_span_tiles(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, int splits, float* po, float2* pml, void* out, float* lse,
-                                cudaStream_t st) {
+jpi_status launch_kv_span_tiles(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, int splits, bool joined, float* po, float2* pml, void* out,
+                                float* lse, cudaStream_t st) {
     SpanTileArgs a = {};
     SpanMaps maps = {};
     a.c = c;
@@ -867,6 +950,8 @@ jpi_status launch_kv_span_tiles(jpi_kv_handle* h, const KvCall& c, const KvSpan&
     a.pml = pml;
     a.rows = (long long)c.batch * c.tokens * c.H;
     a.out = splits == 1 ? static_cast<__nv_bfloat16*>(out) : nullptr;
+    a.joined = joined ? static_cast<__nv_bfloat16*>(out) : nullptr;
+    if (joined) a.tiles_outer = true;   // (a cluster's blocks are the splits of one tile)
     a.lse = lse;
     a.err = h->dev_err;
     if (!s.ks) {
