@@ -397,7 +397,9 @@ struct SrSmem {
     static constexpr int BYTES = SEEN_OFF + AHEAD * KR_ROWS * 4;
     static constexpr int ALONE = Q8 ? (DP == 256 ? 8 : DP == 128 ? 10 : 11) : DP == 256 ? 5 : 6;   // blocks of an SM
     static constexpr int REGS = 65536 / 32 / ALONE / 8 * 8 < 255 ? 65536 / 32 / ALONE / 8 * 8 : 255;
-    static constexpr int TEAM = Q8 ? 8 : 4;   // JOIN: warps of a block, each with all of this for itself
+    // JOIN: warps of a block, each with all of this for itself; in 8 bits by the registers, else as many as fit (one token over windows of 1024
+    // rows of 256 8.1 us; with four warps 9.0).
+    static constexpr int TEAM = Q8 ? 8 : DP == 256 ? 5 : 6;
     static constexpr int JOIN_BYTES = JoinSmem<DP, __nv_bfloat16, TEAM, BYTES>::BYTES;
     static_assert(BYTES % 128 == 0 && MergeSmem<DP>::WARP_FLOATS * 4 <= 2 * STAGE, "a warp's rows fit its stages");
 };
