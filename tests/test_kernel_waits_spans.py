@@ -51,3 +51,20 @@ def test_barriers_of_a_ring_are_committed_only_where_a_block_follows():
     body = kernel()
     for ring, behind in (("kempty[sl]", "NS"), ("vempty[sl]", "NS"), ("odone[i % NB]", "NB"), ("gdone[i % NG]", "NG")):
         assert f"if (i + {behind} < nb) ptx::mma_commit(&{ring});" in body
+
+
+def test_blocks_of_a_cluster_meet_before_their_parts_are_read_and_after():
+    body = kernel()
+    meets = [m.start() for m in re.finditer(r"ptx::cluster_sync_all\(\);", body)]
+    read = body.index("join_tile<")
+    assert len(meets) == 2 and meets[0] < read < meets[1] and "if constexpr (JOIN) {" in body[:meets[0]]
+    # Nothing is written where a wait gave up in any block of the cluster.
+    assert meets[0] < body.index("dsmem_map(ptx::smem_u32(flag)") < body.index("if (whole) join_tile<")
+    with open(SOURCE.replace("kv_span_t5.cu", "kv_span.cu")) as f:
+        rows = f.read()
+    join = rows[rows.index("void join_cluster("):]
+    join = join[:join.index("\n}\n")]
+    meets = [m.start() for m in re.finditer(r"ptx::cluster_sync_all\(\);", join)]
+    reads = [m.start() for m in re.finditer(r"ptx::dsmem_ld_", join)]
+    assert len(meets) == 2 and all(meets[0] < r < meets[1] for r in reads) and len(reads) == 2
+    assert join.count("return;") == 1 and "if (ranks == 1) return;" in join   # the same for all blocks
