@@ -66,7 +66,8 @@ constexpr long long st_row_elements(bool held8, long long R, int D) { return (he
 // Cycles of a key block of D elements, of a block's start and end, of the combine's launch, of a pair's meeting, and bytes a cycle to and from
 // the workspace.
 constexpr long long st_block(bool held8, int D) { return held8 ? 1000 + 8 * D : 500 + 4 * D; }
-constexpr long long ST_ENDS = 10000, ST_JOIN = 8000, ST_MEET = 6500, ST_BYTES = 2600;
+constexpr long long ST_ENDS = 10000, ST_JOIN = 8000, ST_BYTES = 2600;
+constexpr long long st_meet(int D) { return 3000 + 14 * D; }
 
 struct SpanMaps {
     CUtensorMap k, v;
@@ -923,7 +924,7 @@ int kv_span_tiles_plan(const jpi_kv_handle* h, const KvCall& c, const KvSpan& s,
         const bool meet = n == ST_RANKS && blocks <= h->tile_pairs[s.ks != nullptr];
         if (!meet && n > room) continue;
         const long long time = (blocks * n + h->num_sms - 1) / h->num_sms * ((nb + n - 1) / n * st_block(s.ks, c.D) + ST_ENDS) +
-                               (meet ? ST_MEET : n > 1 ? ST_JOIN + 2 * n * c.batch * c.tokens * c.H * c.D * 4 / ST_BYTES : 0);
+                               (meet ? st_meet(c.D) : n > 1 ? ST_JOIN + 2 * n * c.batch * c.tokens * c.H * c.D * 4 / ST_BYTES : 0);
         if (best_time < 0 || time < best_time) {
             best_time = time;
             best = n;
