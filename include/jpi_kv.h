@@ -261,7 +261,7 @@ JPI_API jpi_status jpi_kv8_append(jpi_kv_handle* h, const void* q, long long q_s
  * Scores, softmax and sums in fp32, codes and scales taken as they are. JPI_BF16 mode: queries enter the first product as fp16,
  * scaled by a power of two (bf16's eight bits whole; an element below 2^-14 of its head's largest is off by at most 2^-25 of
  * that), the probabilities the second as fp16 (each off by at most 2^-11 of itself, or 2^-28 of what the largest value of the
- * blocks seen would weigh).
+ * blocks seen would weigh). JPI_KV_TILES holds here too.
  */
 JPI_API jpi_status jpi_kv8_attend(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
                                   const jpi_kv8_cache* cache, const int* seen, int window, int sink, void* out,

@@ -54,7 +54,7 @@ constexpr int ST_BOOST = 4;         // log2 of what probabilities of fp16 are mu
 constexpr int ST_NONE = -4096;      // no scale seen yet
 constexpr int ST_RUN = 32;          // blocks of a group whose scales are read together
 constexpr int ST_RANKS = 2;         // parts that are joined in a cluster
-// Query rows of a request and KV head from which a call takes the tiles, and the elements of keys up to which it stays with the row
+// Query rows of a request and KV head from which a call that has no room in clusters (kv_span.cu) takes the tiles, and the elements of keys up to which it stays with the row
 // kernel all the same, which reads a key once for every 8 query rows. Microseconds of row kernel and tiles, bf16: 1 KV head at D = 256,
 // 128 rows over 1024 keys (4 M elements) 13.6 and 13.3, over 4096 18.0 and 14.8; 8 KV heads at D = 128, 128 rows over 256 keys
 // (4.5 M) 11.4 and 12.3, over 1024 (16 M) 15.8 and 13.7. 8 bits: 128 rows at D = 256 over 1024 (4 M) 12.9 and 15.6, 4 times 64
