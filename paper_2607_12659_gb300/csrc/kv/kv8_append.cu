@@ -118,7 +118,7 @@ __device__ __forceinline__ void store8(const Append8Args& a, uint32_t unit, int 
         __syncwarp();
     }
     const int e = max(kv8_exponent(top), e_old);
-    const float inv = kv8_pow2(254 - e);
+    const float inv = kv8_scale((uint32_t)max(254 - e, 0));   // (of a kept scale of 254 it is 2^-127, no normal number)
     if (t == 0) *scale = (uint8_t)e;
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
