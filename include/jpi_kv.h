@@ -195,8 +195,8 @@ typedef struct jpi_kv_norm {
 
 /*
  * jpi_kv_append after a norm of each head of q and k, in one pass; v is copied. Arguments and what is written as there.
- * Squares are summed in fp32 (a head whose squares pass fp32's range is summed again at 2^-70 of its values, so that finite
- * values give finite norms); everything up to the one rounding to E is fp32.
+ * Squares are summed in fp32 (where the mean of a head's squares with eps passes 1e38 they are summed again at 2^-70 of its values,
+ * and eps is taken at 2^-140, so that finite values give finite norms); everything up to the one rounding to E is fp32.
  */
 JPI_API jpi_status jpi_kv_append_normed(jpi_kv_handle* h, const void* q, long long q_stride, const void* k,
                                         long long k_stride, const void* v, long long v_stride, const jpi_kv_norm* norm,

@@ -73,25 +73,26 @@ __device__ __forceinline__ float inverse_root(float v) {
     return v < INFINITY ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
-// Makes a head's elements x (those of one lane) x / sqrt(mean(x^2) + eps); returns the factors that did it, one after the other. Of heads
-// whose squares pass fp32's range the first is 2^-70, else it is 1. Every lane of the warp calls.
+// Makes a head's elements x (those of one lane) x / sqrt(mean(x^2) + eps); returns the factors that did it, one after the other. Where
+// that sum passes 1e38, and may pass fp32's range, the first is 2^-70 (the mean and eps are then 2^-140 of theirs), else it is 1. Every
+// lane of the warp calls.
 template <int N>
 __device__ __forceinline__ float2 head_norm(float2 (&x)[N], float inv_d, float eps, int lanes_log2) {
     float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < N; ++i) s2 = fma2(x[i], x[i], s2);
-    const float s = group_sum(s2.x + s2.y, lanes_log2);
-    float2 r = make_float2(1.f, inverse_root(fmaf(s, inv_d, eps)));
-    if (__any_sync(0xffffffffu, s > 1e38f)) {
+    const float v = fmaf(group_sum(s2.x + s2.y, lanes_log2), inv_d, eps);
+    float2 r = make_float2(1.f, inverse_root(v));
+    if (__any_sync(0xffffffffu, v > 1e38f)) {
         float z = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float2 y = make_float2(x[i].x * 0x1p-70f, x[i].y * 0x1p-70f);
             z = fmaf(y.x, y.x, fmaf(y.y, y.y, z));
-            if (s > 1e38f) x[i] = y;
+            if (v > 1e38f) x[i] = y;
         }
         z = group_sum(z, lanes_log2);
-        if (s > 1e38f) r = make_float2(0x1p-70f, inverse_root(z * inv_d));   // (eps is less than a rounding here)
+        if (v > 1e38f) r = make_float2(0x1p-70f, inverse_root(fmaf(z, inv_d, eps * 0x1p-140f)));
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = mul2(x[i], make_float2(r.y, r.y));

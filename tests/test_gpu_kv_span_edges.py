@@ -4,8 +4,8 @@ import numpy as np
 import pytest
 
 from oracle import kv as okv
-from test_gpu_kv import DT, i32, kv, np64, rand  # noqa: F401
-from test_gpu_kv_heads import bits
+from test_gpu_kv import DT, HALF_EPS, i32, kv, np64, rand, within  # noqa: F401
+from test_gpu_kv_heads import bits, norm_tol
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,17 @@ def test_append8_under_the_largest_scales(kv, dtype, byte):
     for (codes, scales), t, s in zip(want, (c.k, c.v), (c.k_scale, c.v_scale)):
         assert np.array_equal(bits(s), scales) and scales[0, 0, 0] == max(byte, okv.scale8(np64(x)))
         assert np.array_equal(np64(t), codes) and np.any(codes[0, 4])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [8, 64, 248])
+@pytest.mark.parametrize("eps", [1e-6, 1e30, 3e37, 1e38, 3.4e38])
+def test_norms_of_large_heads_under_any_eps(kv, dtype, D, eps):
+    """Mean squares and eps on both sides of where their sum passes fp32's range."""
+    size = np.array([1e-3, 1.0, 3e17, 1e18, 2e18, 5e18, 1.3e19, 2.0 ** 64, 2.0 ** 100, 2.0 ** 126])
+    T = len(size)
+    x = rand(D, 1, T, 2, D, dtype=dtype).clamp(-1.9, 1.9) * torch.tensor(size, device="cuda").to(DT[dtype])[None, :, None, None]
+    i = i32([[0] * T])
+    got = kv.KV(2, 1, D, max_tokens=T, precision=dtype).append(x, None, None, i, i, norm=kv.Norm(eps=eps))
+    want = okv.norm(np64(x), None, eps)
+    within(got, want, HALF_EPS[dtype] * np.abs(want) + norm_tol(want, D) * np.abs(want) + 2.0 ** -125, "norm")
