@@ -258,7 +258,9 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
 #pragma unroll
                 for (int i = 0; i < Hd::RUN / 4; ++i) {
                     if (d0 + 4 * i >= D) break;
-                    const float4 y = Hd::part(k, i);
+                    float4 y = Hd::part(k, i);
+                    // (a key by itself: its products with a query may pass fp32's range where those with it do not)
+                    if (HELD8) y = make_float4(y.x * ks, y.y * ks, y.z * ks, y.w * ks);
 #pragma unroll
                     for (int r = 0; r < KR_ROWS; ++r) {
                         const float4 q = *(const float4*)(qs + r * DP + d0 + 4 * i);
@@ -277,7 +279,7 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
         for (int r = 0; r < KR_ROWS; ++r) {
             const bool in = span_sees(g.s, key, n[r], span_first(g.s, n[r]));
             cut = cut || !in;
-            const float sc = in ? (p2[r].x + p2[r].y) * ks : -INFINITY;
+            const float sc = in ? p2[r].x + p2[r].y : -INFINITY;
             float mx = sc;
 #pragma unroll
             for (int e = 16; e > 0; e >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, e));
@@ -666,12 +668,14 @@ __global__ void __maxnreg__((JOIN ? 248 : SrSmem<DP, Q8>::REGS)) k_kv_span_rows(
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 const float by = Q8 ? __shfl_sync(0xffffffffu, mine, t) : 1.f;
+                // A row's factor below 1 first: the product with the other may pass fp32's range where the score does not.
+                const float a0 = qs0 < 1.f ? qs0 : by, b0 = qs0 < 1.f ? by : qs0, a1 = qs1 < 1.f ? qs1 : by, b1 = qs1 < 1.f ? by : qs1;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     sc[t][e] = part[0][t][e];
 #pragma unroll
                     for (int c = 1; c < NCH; ++c) sc[t][e] += part[c][t][e];
-                    if (Q8) sc[t][e] = sc[t][e] * by * (e & 1 ? qs1 : qs0);
+                    if (Q8) sc[t][e] = sc[t][e] * (e & 1 ? a1 : a0) * (e & 1 ? b1 : b0);
                 }
             }
             // Keys g, g + 8 of each tile, rows 2 j, 2 j + 1; hidden scores are replaced, whatever they hold.
@@ -850,17 +854,16 @@ __global__ void __maxnreg__((JOIN ? 248 : SrSmem<DP, Q8>::REGS)) k_kv_span_rows(
                 const int key = blocks.row(e / L::KEYS) + e % L::KEYS;
                 if (!span_sees(sn, key, n, span_first(sn, n))) continue;
                 const T *k = static_cast<const T*>(s.k) + base + key * s.rs, *v = static_cast<const T*>(s.v) + base + key * s.rs;
-                float dot = 0.f;
-#pragma unroll
-                for (int i = 0; i < NL; ++i)
-                    if (lane + 32 * i < D) dot = fmaf(qr[i], value(k[lane + 32 * i]), dot);
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
-                float vsc = 1.f;
+                float dot = 0.f, ksc = 1.f, vsc = 1.f;
                 if (Q8) {
-                    dot *= kv8_scale(sn.ks[sb + (key >> sn.n_log2)]);
+                    ksc = kv8_scale(sn.ks[sb + (key >> sn.n_log2)]);
                     vsc = kv8_scale(sn.vs[sb + (key >> sn.n_log2)]);
                 }
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    if (lane + 32 * i < D) dot = fmaf(qr[i], value(k[lane + 32 * i]) * ksc, dot);
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
                 const float pr = kr_ex2((dot - m) * a.c2);
 #pragma unroll
                 for (int i = 0; i < NL; ++i)

@@ -5,7 +5,8 @@ import pytest
 
 from oracle import kv as okv
 from test_gpu_kv import DT, HALF_EPS, i32, kv, np64, rand, within  # noqa: F401
-from test_gpu_kv_heads import bits, norm_tol
+from test_gpu_kv_heads import bits, fill8, norm_tol
+from test_gpu_kv_spans import finish, tols
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,30 @@ def test_norms_of_large_heads_under_any_eps(kv, dtype, D, eps):
     got = kv.KV(2, 1, D, max_tokens=T, precision=dtype).append(x, None, None, i, i, norm=kv.Norm(eps=eps))
     want = okv.norm(np64(x), None, eps)
     within(got, want, HALF_EPS[dtype] * np.abs(want) + norm_tol(want, D) * np.abs(want) + 2.0 ** -125, "norm")
+
+
+def wide_cache(kv, h, B, R, block, seed, k_byte):
+    """An 8-bit cache with its keys under one scale, and the numbers that it holds."""
+    c = fill8(kv, h, B, R, block, seed)
+    c.k_scale.view(torch.uint8).fill_(k_byte)
+    return c, [okv.values8(np64(x), bits(s), block) for x, s in ((c.k, c.k_scale), (c.v, c.v_scale))]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tiles", ["0", "1"])
+@pytest.mark.parametrize("k_byte,q_log2", [(245, -121), (228, -104), (10, 120), (30, 100)])
+@pytest.mark.parametrize("B,T", [(1, 1), (3, 20), (200, 1)])
+def test_attend8_where_scores_are_in_range_and_their_factors_far_from_it(kv, monkeypatch, dtype, tiles, k_byte, q_log2, B, T):
+    """Keys of 2^118 under queries of 2^-121 and the other way round."""
+    monkeypatch.setenv("JPI_KV_TILES", tiles)
+    H, K, D, R, block = 8, 1, 64, 150, 16
+    h = kv.KV(H, K, D, max_batch=B, max_tokens=T, precision=dtype)
+    c, (k, v) = wide_cache(kv, h, B, R, block, 3, k_byte)
+    q = rand(5, B, T, H, D, dtype=dtype) * 2.0 ** q_log2
+    assert torch.isfinite(q).all() and np.abs(k).max() < 3e38
+    seen = np.clip(R - 10 * np.arange(T), 0, None)[None].repeat(B, 0)
+    out, lse = h.attend8(q, c, i32(seen))
+    again = h.attend8(q, c, i32(seen))
+    h.device_status()
+    ref = okv.attend_window(np64(q), k, v, seen, 0, 0, 1 / 8)
+    finish(out, lse, again, ref, tols(np64(q), k, v, R, dtype, *ref[:1], ref[2], ref[3], ref[1], 1 / 8))
