@@ -865,6 +865,8 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
+    // Before the pair meets: another block's allocation may wait for these columns, and its partner for that one.
+    if (warp == 1) ptx::tmem_dealloc(tmem, L::TMEM_COLS);
     if constexpr (JOIN) {
         // The parts of the tile are in the shared memories of the cluster's blocks, each of which writes some of the rows.
         ptx::cluster_sync_all();
@@ -875,7 +877,6 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         ptx::cluster_sync_all();   // every block's rows have been read
     }
     if (tid == 0 && *flag != 0) atomicCAS(a.err, 0, *flag);
-    if (warp == 1) ptx::tmem_dealloc(tmem, L::TMEM_COLS);
 }
 
 template <int DP>
