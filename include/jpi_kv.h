@@ -213,7 +213,8 @@ JPI_API jpi_status jpi_kv_append_normed(jpi_kv_handle* h, const void* q, long lo
  * see, and rows that no token of a call sees are not read. The work follows the windows, not the cache's length. In
  * JPI_BF16 mode the probabilities enter the second product as there: calls of many query rows on the 128-row
  * tiles round each to bf16 once, the others carry what the rounding left. JPI_KV_TILES holds here too. Sums of p v are formed at up to
- * 2^24 times their size (2^8 outside the tiles): finite values of 2^100 and more may come out infinite.
+ * 2^24 times their size (2^8 outside the tiles): finite values of 2^100 and more may come out infinite. A handle's first call here or of
+ * jpi_kv8_attend looks up what the device holds of their kernels (2 ms in a process, 0.4 ms for a further head width); it may be captured.
  */
 JPI_API jpi_status jpi_kv_attend_window(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
                                         const jpi_kv_cache* cache, const int* seen, int window, int sink, void* out,

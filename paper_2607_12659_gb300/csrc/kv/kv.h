@@ -18,6 +18,7 @@ struct jpi_kv_handle {
     int* dev_err = nullptr;
     bool pdl = true;             // kernels of one call may start before the one before them has finished
     int tiles = -1;              // attend, weigh: the tensor-core tiles never, (1) wherever they fit, (-1) by size
+    bool span_ready = false;        // of attend_window and kv8_attend: what follows is known (their first call looks it up)
     int span_clusters[2][4] = {};   // attend_window, kv8_attend: clusters of 1, 2, 4 and 8 joining blocks that are resident together
     int tile_pairs[2] = {};         // likewise pairs of blocks of their 128-row tiles
     size_t device_bytes = 0;

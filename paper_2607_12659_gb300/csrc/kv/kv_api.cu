@@ -264,7 +264,6 @@ JPI_API jpi_status jpi_kv_create(const jpi_kv_config* cfg, const jpi_kv_rope* ro
         JPI_TRY(kv_alloc(h, &h->ws, h->ws_bytes));
         JPI_TRY(kv_append_prepare());
         JPI_TRY(kv_weigh_prepare(h));
-        JPI_TRY(kv_span_prepare(h));
         return kv_attend_prepare(h);
     };
     jpi_status s;

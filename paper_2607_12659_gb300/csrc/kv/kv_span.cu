@@ -1078,14 +1078,19 @@ jpi_status prepare_dim(jpi_kv_handle* h) {
     return JPI_OK;
 }
 
-}  // namespace
-
+// The kernels' shared memory and the clusters that are resident together: by a handle's first call here, so that one that only appends, or
+// attends over whole caches, does not load these kernels.
 jpi_status kv_span_prepare(jpi_kv_handle* h) {
     JPI_TRY(kv_span_tiles_prepare(h));
-    return h->D <= 64 ? prepare_dim<64>(h) : h->D <= 128 ? prepare_dim<128>(h) : prepare_dim<256>(h);
+    JPI_TRY(h->D <= 64 ? prepare_dim<64>(h) : h->D <= 128 ? prepare_dim<128>(h) : prepare_dim<256>(h));
+    h->span_ready = true;
+    return JPI_OK;
 }
 
+}  // namespace
+
 jpi_status launch_kv_span(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, void* out, float* lse, cudaStream_t st) {
+    if (!h->span_ready) JPI_TRY(kv_span_prepare(h));
     return h->D <= 64 ? launch_dim<64>(h, c, s, out, lse, st)
                       : h->D <= 128 ? launch_dim<128>(h, c, s, out, lse, st) : launch_dim<256>(h, c, s, out, lse, st);
 }

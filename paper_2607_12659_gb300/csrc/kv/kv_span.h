@@ -12,7 +12,6 @@ struct KvSpan {
     int n_log2 = 0, nblk = 0;                     // rows of a block (log2), blocks of a cache
 };
 
-jpi_status kv_span_prepare(jpi_kv_handle* h);
 jpi_status launch_kv_span(jpi_kv_handle* h, const KvCall& c, const KvSpan& s, void* out, float* lse, cudaStream_t st);
 
 // On tensor-core tiles of 128 query rows (kv_span_t5.cu): the key splits, of at most `room`, that a call takes there; 0: it does not.

@@ -72,3 +72,26 @@ def test_attend8_where_scores_are_in_range_and_their_factors_far_from_it(kv, mon
     h.device_status()
     ref = okv.attend_window(np64(q), k, v, seen, 0, 0, 1 / 8)
     finish(out, lse, again, ref, tols(np64(q), k, v, R, dtype, *ref[:1], ref[2], ref[3], ref[1], 1 / 8))
+
+
+# ------------------------------------------------------------------ the first call of a handle
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("held8", [False, True])
+@pytest.mark.parametrize("T", [1, 40])
+def test_the_first_attention_of_a_handle_may_be_captured(kv, dtype, held8, T):
+    H, K, D, R = 8, 1, 128, 200
+    q, k, v, s = rand(1, 1, T, H, D, dtype=dtype), rand(2, 1, R, K, D, dtype=dtype), rand(3, 1, R, K, D, dtype=dtype), i32([list(range(R - T + 1, R + 1))])
+    h, h2 = (kv.KV(H, K, D, max_tokens=T, precision=dtype) for _ in range(2))
+    c = fill8(kv, h, 1, R, 32, 5)
+    call = lambda x: x.attend8(q, c, s, window=77) if held8 else x.attend_window(q, (k, v), s, 77)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = call(h)
+    g.replay()
+    want = call(h2)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.equal(call(h)[0], want[0])
+    h.device_status()
