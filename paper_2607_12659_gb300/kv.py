@@ -257,13 +257,13 @@ class KV:
             elif q_out is None:
                 q_out = self._torch.zeros((*q.shape[:2], self.heads, self.head_dim), dtype=self.dtype, device=self.device)
                 returns = (q_out,)
-            args = reads = (q, k, v, positions, rows, cache_k, cache_v)
-            args += (q_out,)
-            if norm is not None:
-                args += (norm.q_weight, norm.k_weight, norm.eps)
-                reads += (norm.q_weight, norm.k_weight)
-            self._call("append" if norm is None else "append_normed", on, stream, args,
-                       reads + (None if returns else q_out,), returns)
+            if norm is None:
+                self._call("append", on, stream, (q, k, v, positions, rows, cache_k, cache_v, q_out),
+                           (q, k, v, positions, rows, cache_k, cache_v, None if returns else q_out), returns)
+            else:
+                self._call("append_normed", on, stream,
+                           (q, k, v, positions, rows, cache_k, cache_v, q_out, norm.q_weight, norm.k_weight, norm.eps),
+                           (q, k, v, positions, rows, cache_k, cache_v, norm.q_weight, norm.k_weight, None if returns else q_out), returns)
         return q_out
 
     def cache8(self, caches: int, rows: int, block: int = 32) -> Cache8:
