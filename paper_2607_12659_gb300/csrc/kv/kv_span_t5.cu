@@ -514,8 +514,8 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             ptx::mbar_arrive(qready);
         }
         constexpr int HK = ST_KEYS / 2;   // keys per thread
-        // In 8 bits scores are those of the scaled query, qs of them the true ones; maxima, which have their keys' scales in them, are 2^-20
-        // of those where qs is below 1: with a scale of up to 2^127 they may pass fp32's range where the true ones do not.
+        // In 8 bits scores are those of the scaled query, qs of them the true ones; maxima are those of the scores in log2 units, with their
+        // keys' scales (a score times either factor alone may pass fp32's range).
         float qs = 1.f;
         if constexpr (Q8) {
             if (grp > 0) good = ptx::mbar_wait_bounded(qready, 0, ST_WAIT_NS);
@@ -523,8 +523,8 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
         }
         const float c2s = fminf(a.c2 * qs, 3e38f);
         const uint64_t c2 = pair2(c2s);
-        const float held = Q8 && qs < 1.f ? 0x1p-20f : 1.f, c2m = Q8 && qs < 1.f ? c2s * 0x1p20f : c2s;
-        const float rescale = fminf((Q8 ? ST_RESCALE8 : ST_RESCALE) / c2m, 3e38f);
+        const float unit = Q8 ? 1.f : c2s;   // log2 units of a maximum's
+        const float rescale = Q8 ? ST_RESCALE8 : fminf(ST_RESCALE / c2s, 3e38f);
         // Scales of the group's next blocks, a byte a thread (of a tile that no row sees: 127).
         uint8_t* const sc = st_smem + L::SC_OFF + grp * ST_RUN * 8;
         auto scales = [&](int i0) {
@@ -574,8 +574,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                 for (int j = 0; j < 16; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[e][j]));
                 mt[e] = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
             }
-            // 8 bits: scores are the products times the scale of their tile's keys, which multiplies the maximum, and what the scores are
-            // multiplied by.
+            // 8 bits: scores are the products times the scale of their tile's keys, which is in what scores and maximum are multiplied by.
             float kc[2] = {c2s, c2s};
             if constexpr (Q8) {
 #pragma unroll
@@ -586,8 +585,8 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                         for (int j = 0; j < 16; ++j) s[e][j] = sees(16 * e + j) ? 0x7fffffffu : __float_as_uint(-INFINITY);
                         mt[e] = -INFINITY;
                     } else {
-                        mt[e] *= kv8_scale(k) * held;
                         kc[e] = fminf(fmaxf(c2s * kv8_scale(k), 0x1p-126f), 3e38f);   // (0 times a hidden score would be NaN, as infinity times 0)
+                        mt[e] *= kc[e];
                     }
                 }
             }
@@ -597,7 +596,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             ptx::named_bar_sync(pair_bar, 64);
             mb = fmaxf(mb, xm[(1 - half) * ST_ROWS]);
             const bool move = mb > m_used + rescale;
-            const float alpha = !move ? 1.f : m_used == -INFINITY ? 0.f : kr_ex2((m_used - mb) * c2m);
+            const float alpha = !move ? 1.f : m_used == -INFINITY ? 0.f : kr_ex2((m_used - mb) * unit);
             float beta = alpha;               // what the outputs are multiplied by: in units of the largest scale, too
             bool grown = false;
             float pv[2] = {1.f, 1.f};         // what the probabilities of the half's tiles are multiplied by
@@ -647,7 +646,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             }
             // 2^((s - m) c): a hidden key's -inf gives 0, also while the row has seen none at all (m taken as 0).
             const uint64_t neg_m = pair2(m_used == -INFINITY ? 0.f : -m_used);
-            const float neg_mc = m_used == -INFINITY ? 0.f : -m_used * c2m;
+            const float neg_mc = m_used == -INFINITY ? 0.f : -m_used;   // (8 bits)
             float l4[4] = {0.f, 0.f, 0.f, 0.f};
             uint32_t pk[HK / 2];
 #pragma unroll
@@ -780,13 +779,13 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             ptx::named_bar_sync(9, NG * ST_SOFT);
             const float2 other = ml[(1 - grp) * ST_ROWS + row];
             const float M = fmaxf(m_used, other.x);
-            w = m_used == -INFINITY ? 0.f : kr_ex2((m_used - M) * c2m);
-            l = w * l + (other.x == -INFINITY ? 0.f : kr_ex2((other.x - M) * c2m)) * other.y;   // (0 times a NaN sum is NaN)
+            w = m_used == -INFINITY ? 0.f : kr_ex2((m_used - M) * unit);
+            l = w * l + (other.x == -INFINITY ? 0.f : kr_ex2((other.x - M) * unit)) * other.y;   // (0 times a NaN sum is NaN)
             m_used = M;
         }
         float vscale = 1.f;
         if constexpr (Q8) {
-            m_used *= qs < 1.f ? qs * 0x1p20f : qs;
+            m_used *= 1.f / a.c2;
             w *= 1.f / (1 << ST_BOOST);
             vscale = v_used == ST_NONE ? 1.f : kv8_scale((uint32_t)v_used);
         }
