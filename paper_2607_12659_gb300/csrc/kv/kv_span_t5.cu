@@ -54,15 +54,27 @@ constexpr int ST_BOOST = 4;         // log2 of what probabilities of fp16 are mu
 constexpr int ST_NONE = -4096;      // no scale seen yet
 constexpr int ST_RUN = 32;          // blocks of a group whose scales are read together
 constexpr int ST_RANKS = 2;         // parts that are joined in a cluster
-// Query rows of a request and KV head from which a call that has no room in clusters (kv_span.cu) takes the tiles, and the elements of keys up to which it stays with the row
-// kernel all the same, which reads a key once for every 8 query rows. Microseconds of row kernel and tiles, bf16: 1 KV head at D = 256,
-// 128 rows over 1024 keys (4 M elements) 13.6 and 13.3, over 4096 18.0 and 14.8; 8 KV heads at D = 128, 128 rows over 256 keys
-// (4.5 M) 11.4 and 12.3, over 1024 (16 M) 15.8 and 13.7. 8 bits: 128 rows at D = 256 over 1024 (4 M) 12.9 and 15.6, 4 times 64
-// rows over 1024 (8 M) 17.8 and 15.1; 8 KV heads at D = 128, 128 rows over 1024 (16 M) 17.7 and 16.0; where a tile's rows are a
-// quarter of it, 32 rows of 32 KV heads at D = 128 over 1024 (16 M) 17.2 and 17.5, over 4096 (64 M) 33.9 and 31.5, of 64 KV heads at
-// D = 64 over 4096 (64 M) 45.1 and 48.7.
+// Query rows of a request and KV head from which a call that has no room in clusters (kv_span.cu) takes the tiles, and the elements of keys up
+// to which it stays with the row kernel all the same, which reads a key once for every 8 query rows: what the row kernel takes grows with
+// both, what a tile takes by its keys alone, however few of its rows there are and however narrow the heads. Microseconds of row kernel
+// and tiles, 8 bits, 32 KV heads to D = 128 and 8 at 256:
+//   D = 64   64 rows over 4096 keys (64 M elements) 27.3 and 29.0, over 16384 (256 M) 78 and 82, 32 rows 43 and 85; 96 rows over 1024
+//            (24 M) 17.6 and 18.6, over 2048 24.2 and 22.4; 128 rows over 512 (16 M) 15.8 and 14.8
+//   D = 128  32 rows over 2048 (32 M) 19.3 and 21.0, over 16384 81 and 88; 40 rows over 1024 (20 M) 15.7 and 16.7; 56 rows over 1024 (28 M)
+//            18.7 and 17.0; 64 rows over 512 (16 M) 13.6 and 15.4, over 1024 20.0 and 16.9
+//   D = 256  40 rows over 1024 (10 M) 13.5 and 14.4, over 2048 16.5 and 15.9; 64 rows of one KV head over 4096 (8 M) 12.4 and 14.3, over 16384
+//            19.4 and 16.7
+// and bf16:
+//   D = 64   32 rows over 2048 (16 M) 12.8 and 15.0, over 16384 42 and 54; 48 rows over 1024 (12 M) 12.1 and 13.5, over 2048 15.7 and 15.4
+//   D = 128  48 rows over 512 (12 M) 12.4 and 13.6, over 1024 15.8 and 14.8; 64 rows of 8 KV heads over 1024 (8 M) 10.6 and 11.8, over 4096
+//            17.5 and 13.9
+//   D = 256  128 rows of one KV head over 1024 (4 M) 10.9 and 12.1, 64 over 4096 (8 M) 12.1 and 11.9, over 16384 19.8 and 14.3
 constexpr int ST_LEAST = 32;
-constexpr long long st_row_elements(bool held8, long long R, int D) { return (held8 ? (R < 64 && D <= 128 ? 60ll : 12ll) : 4ll) << 20; }
+constexpr long long ST_NEVER = 1ll << 62;
+constexpr long long st_row_elements(bool held8, long long R, int D) {
+    if (held8) return D > 128 ? 12ll << 20 : D > 64 ? (R < 36 ? ST_NEVER : (R < 64 ? 20ll : 16ll) << 20) : R < 72 ? ST_NEVER : (R < 128 ? 24ll : 12ll) << 20;
+    return D > 128 ? 4ll << 20 : D <= 64 && R < 44 ? ST_NEVER : 12ll << 20;
+}
 // Cycles of a key block of D elements, of a block's start and end, of the combine's launch, of a pair's meeting, and bytes a cycle to and from
 // the workspace.
 constexpr long long st_block(bool held8, int D) { return held8 ? 1000 + 8 * D : 500 + 4 * D; }
