@@ -607,7 +607,7 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
             xm[half * ST_ROWS] = mb;
             ptx::named_bar_sync(pair_bar, 64);
             mb = fmaxf(mb, xm[(1 - half) * ST_ROWS]);
-            const bool move = mb > m_used + rescale;
+            const bool move = mb - m_used > rescale;   // (of -infinities NaN: no)
             const float alpha = !move ? 1.f : m_used == -INFINITY ? 0.f : kr_ex2((m_used - mb) * unit);
             float beta = alpha;               // what the outputs are multiplied by: in units of the largest scale, too
             bool grown = false;
@@ -657,16 +657,16 @@ __global__ void __maxnreg__((StSmem<DP, Q8>::REGS)) k_kv_span_t5(const __grid_co
                 m_used = mb;
             }
             // 2^((s - m) c): a hidden key's -inf gives 0, also while the row has seen none at all (m taken as 0).
-            const uint64_t neg_m = pair2(m_used == -INFINITY ? 0.f : -m_used);
-            const float neg_mc = m_used == -INFINITY ? 0.f : -m_used;   // (8 bits)
+            const float m_now = m_used == -INFINITY ? 0.f : m_used;
+            const uint64_t neg_m = pair2(-m_now), k2[2] = {pair2(kc[0]), pair2(kc[1])};   // (k2: 8 bits)
             float l4[4] = {0.f, 0.f, 0.f, 0.f};
             uint32_t pk[HK / 2];
 #pragma unroll
             for (int k = 0; k < HK; k += 2) {
                 float p0, p1;
                 if constexpr (Q8) {
-                    p0 = fmaf(__uint_as_float(s[k >> 4][k & 15]), kc[k >> 4], neg_mc);
-                    p1 = fmaf(__uint_as_float(s[k >> 4][(k + 1) & 15]), kc[k >> 4], neg_mc);
+                    // (as a product and a sum in one rounding the maximum's own would be what its rounding left: above 2^27 much more than 0)
+                    scale_sub2(__uint_as_float(s[k >> 4][k & 15]), __uint_as_float(s[k >> 4][(k + 1) & 15]), k2[k >> 4], m_now, p0, p1);
                 } else {
                     sub_scale2(__uint_as_float(s[k >> 4][k & 15]), __uint_as_float(s[k >> 4][(k + 1) & 15]), neg_m, c2, p0, p1);
                 }

@@ -14,6 +14,16 @@ __device__ __forceinline__ void sub_scale2(float a, float b, uint64_t neg_m2, ui
     asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(c2));
     asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
 }
+// a c - m likewise, the products rounded: 0 for the a that m is the product of. (The sums one at a time: the assembler makes one
+// instruction of a product and a sum of pairs, with one rounding, .rn or not.)
+__device__ __forceinline__ void scale_sub2(float a, float b, uint64_t c2, float m, float& x, float& y) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(c2));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+    x = __fsub_rn(x, m);
+    y = __fsub_rn(y, m);
+}
 __device__ __forceinline__ uint64_t pair2(float a) {
     uint64_t v;
     asm("mov.b64 %0, {%1, %1};" : "=l"(v) : "f"(a));

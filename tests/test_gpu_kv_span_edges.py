@@ -7,6 +7,7 @@ from oracle import kv as okv
 from test_gpu_kv import DT, HALF_EPS, i32, kv, np64, rand, within  # noqa: F401
 from test_gpu_kv_heads import bits, fill8, norm_tol
 from test_gpu_kv_spans import finish, tols
+from test_kv_span_rounding_host import bound
 
 pytestmark = pytest.mark.gpu
 
@@ -72,6 +73,38 @@ def test_attend8_where_scores_are_in_range_and_their_factors_far_from_it(kv, mon
     h.device_status()
     ref = okv.attend_window(np64(q), k, v, seen, 0, 0, 1 / 8)
     finish(out, lse, again, ref, tols(np64(q), k, v, R, dtype, *ref[:1], ref[2], ref[3], ref[1], 1 / 8))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tiles", ["0", "1"])
+def test_attend8_of_queries_far_from_each_other(kv, monkeypatch, dtype, tiles):
+    """Tokens of one tile whose queries are 0, below fp32's normal numbers, or up to 2^100: each as by itself."""
+    monkeypatch.setenv("JPI_KV_TILES", tiles)
+    H, K, D, R, block = 8, 1, 64, 150, 16
+    size = [0.0, 2.0 ** -130, 2.0 ** -60, 2.0 ** -8, 1.0, 2.0 ** 20, 2.0 ** 60, 2.0 ** 100]
+    T = len(size)
+    h = kv.KV(H, K, D, max_tokens=T, precision=dtype)
+    c = fill8(kv, h, 1, R, block, 3)
+    k, v = (okv.values8(np64(x), bits(s), block) for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    q = rand(5, 1, T, H, D, dtype="fp32") * torch.tensor(size, device="cuda")[None, :, None, None]
+    q = q.to(DT[dtype])
+    seen = np.full((1, T), R)
+    out, lse = h.attend8(q, c, i32(seen))
+    h.device_status()
+    ref, rlse, dot, mass = okv.attend_window(np64(q), k, v, seen, 0, 0, 1 / 8)
+    small = slice(0, 5)
+    bound = tols(np64(q[:, small]), k, v, R, dtype, ref[:, small], dot[:, small], mass[:, small], rlse[:, small], 1 / 8)
+    within(out[:, small], ref[:, small], bound[0], "out")
+    within(lse[:, small], rlse[:, small], bound[1], "lse")
+    # The large ones see one key, where the next is far enough below the first.
+    score = np.einsum("thd,jd->thj", np64(q)[0], k[0, :, 0]) / 8
+    top = np.sort(score, -1)
+    clear = (top[..., -1] - top[..., -2] > 2.0 ** -12 * dot[0] + 50) & (np.arange(T)[:, None] >= 5)
+    assert clear.sum() > 2 * H
+    got = np64(out)[0]
+    best = v[0, score.argmax(-1), 0]
+    assert np.all(np.abs(got - best)[clear] <= HALF_EPS[dtype] * np.abs(best[clear]) + 2.0 ** -10 * np.abs(v).max())
+    assert np.all(np.abs(np64(lse)[0] - top[..., -1])[clear] <= 2.0 ** -14 * dot[0][clear])
 
 
 # ------------------------------------------------------------------ the first call of a handle
