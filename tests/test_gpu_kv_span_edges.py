@@ -6,8 +6,8 @@ import pytest
 from oracle import kv as okv
 from test_gpu_kv import DT, HALF_EPS, i32, kv, np64, rand, within  # noqa: F401
 from test_gpu_kv_heads import bits, fill8, norm_tol
-from test_gpu_kv_spans import finish, tols
-from test_kv_span_rounding_host import bound
+from test_gpu_kv_spans import finish, hidden, tols
+from test_kv_span_rounding_host import bound, crafted
 
 pytestmark = pytest.mark.gpu
 
@@ -105,6 +105,124 @@ def test_attend8_of_queries_far_from_each_other(kv, monkeypatch, dtype, tiles):
     best = v[0, score.argmax(-1), 0]
     assert np.all(np.abs(got - best)[clear] <= HALF_EPS[dtype] * np.abs(best[clear]) + 2.0 ** -10 * np.abs(v).max())
     assert np.all(np.abs(np64(lse)[0] - top[..., -1])[clear] <= 2.0 ** -14 * dot[0][clear])
+
+
+# ------------------------------------------------------------------ what the probabilities are rounded to
+
+def crafted_call(seed, B, K, R, D, dtype, held8):
+    """Queries whose first element is 1 and nothing else, keys and values of `crafted`."""
+    rng = np.random.default_rng(seed)
+    scale = D ** -0.5
+    k, v = np.zeros((B, R, K, D)), np.zeros((B, R, K, D))
+    for b in range(B):
+        for h in range(K):
+            x, s = crafted(rng, R, scale, held8)
+            k[b, :, h, 0], v[b, :, h] = x, s[:, None] * np.where(np.arange(D) % 3 == 0, -1, 1)
+    k[..., 1:] = rng.integers(-3, 4, k[..., 1:].shape)      # (under queries of 0)
+    return [torch.tensor(t, device="cuda").to(DT[dtype]) for t in (k, v)]
+
+
+ROUNDED = [(8, 8, 64, 1, 1, 512), (8, 1, 64, 1, 3, 512), (32, 8, 128, 64, 1, 256), (8, 1, 256, 1, 1, 512), (8, 8, 64, 64, 1, 256),
+           (8, 1, 64, 2, 40, 512), (16, 2, 128, 2, 30, 512), (8, 1, 256, 3, 51, 256), (8, 1, 256, 40, 51, 256)]
+
+
+@pytest.mark.parametrize("tiles", ["0", "by size", "1"])
+@pytest.mark.parametrize("H,K,D,B,T,R", ROUNDED)
+@pytest.mark.parametrize("held8", [False, True])
+def test_rounding_of_the_probabilities(kv, monkeypatch, tiles, held8, H, K, D, B, T, R):
+    """Over bf16 caches two bf16 terms (2^-16) outside the tiles, one (2^-8) on them; over 8-bit caches one of fp16 (2^-11)."""
+    if tiles != "by size":
+        monkeypatch.setenv("JPI_KV_TILES", tiles)
+    h = kv.KV(H, K, D, max_batch=B, max_tokens=T)
+    k, v = crafted_call(D + T, B, K, R, D, "bf16", held8)
+    q = torch.zeros((B, T, H, D), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1
+    seen = i32(np.full((B, T), R))
+    if held8:
+        c = h.cache8(B, R, 32)
+        c.k.copy_(k.to(torch.float8_e4m3fn)), c.v.copy_(v.to(torch.float8_e4m3fn))
+        assert torch.equal(c.k.float(), k.float()) and torch.equal(c.v.float(), v.float())
+        out, lse = h.attend8(q, c, seen)
+    else:
+        out, lse = h.attend_window(q, (k, v), seen, R)
+    h.device_status()
+    ref, rlse, _, mass = okv.attend_window(np64(q), np64(k), np64(v), np.full((B, T), R), R, 0, D ** -0.5)
+    prob = 2.0 ** -11 if held8 else 2.0 ** -16 if tiles == "0" or T == 1 and tiles != "1" else 2.0 ** -8
+    within(out, ref, bound(ref, mass, R, prob, 2.0 ** -8), "out")
+    within(lse, rlse, 2.0 ** -18 + (R / 8 + 16) * 2.0 ** -23, "lse")
+
+
+# ------------------------------------------------------------------ values of 8 bits far apart
+
+@pytest.mark.parametrize("tiles", ["0", "1"])
+@pytest.mark.parametrize("std", [2.0 ** -20, 30.0])
+@pytest.mark.parametrize("T", [1, 20])
+def test_values_far_apart_by_what_each_row_sees(kv, monkeypatch, tiles, std, T):
+    """A probability is an fp16 number in units of 2^-7 of a probability (the tiles: 2^-4) times the largest scale that its row
+    sees: off by half of fp16's least step, 2^-25, for a value of at most 448 of its scale."""
+    monkeypatch.setenv("JPI_KV_TILES", tiles)
+    H, K, D, R, block = 8, 1, 64, 160, 16
+    hd = kv.KV(H, K, D, max_tokens=T)
+    c = fill8(kv, hd, 1, R, block, 1)
+    vs, ks = [120, 100, 119, 140, 90, 121, 118, 1, 60, 122], [120, 110, 119, 115, 90, 121, 118, 1, 60, 119]
+    c.v_scale.view(torch.uint8)[0, 0] = torch.tensor(vs, dtype=torch.uint8, device="cuda")
+    c.k_scale.view(torch.uint8)[0, 0] = torch.tensor(ks, dtype=torch.uint8, device="cuda")
+    q = rand(2, 1, T, H, D, std=std)
+    seen = np.linspace(1, R, T).astype(int)[None] if T > 1 else np.array([[48]])
+    k, v = (okv.values8(np64(x), bits(s), block) for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    out, lse = hd.attend8(q, c, i32(seen))
+    again = hd.attend8(q, c, i32(seen))
+    ref, rlse, dot, mass = okv.attend_window(np64(q), k, v, seen, 0, 0, 1 / 8)
+    rel = (D + 2) * 2.0 ** -22 * dot + 2.0 ** -20 + R * 2.0 ** -23 + 2.0 ** -22 * np.abs(rlse)
+    far = np.zeros((1, T, H, 1))
+    for t, n in enumerate(seen[0]):
+        rel[0, t] += 2.0 ** -24 / 8 * np.abs(np64(q)[0, t]).max(-1) * np.abs(k[0, :n]).sum(-1).max()
+        far[0, t] = n * 448 * 2.0 ** (max(vs[:-(-n // block)]) - 127) * 2.0 ** (-29 if tiles == "1" else -32)
+    # Rows that do not see the largest block would show it if they took its scale for theirs.
+    assert np.all(far[0, seen[0] <= 48] < 2.0 ** -4 * np.abs(ref[0, seen[0] <= 48]).max(-1, keepdims=True))
+    finish(out, lse, again, (ref, rlse, None, None), (2.0 ** -8 * np.abs(ref) + (2 * rel[..., None] + 2.0 ** -11) * mass + far, rel + 1e-6))
+
+
+# ------------------------------------------------------------------ counts far apart
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tiles", ["0", "1"])
+@pytest.mark.parametrize("held8", [False, True])
+def test_counts_far_apart_in_one_request(kv, monkeypatch, dtype, tiles, held8):
+    """Tokens whose windows are thousands of rows from each other: each has its own, whatever lies between."""
+    monkeypatch.setenv("JPI_KV_TILES", tiles)
+    H, K, D, B, T, R, window, sink = 8, 1, 64, 2, 6, 5000, 33, 2
+    seen = np.array([[100, 4990, 0, 2500, 101, 5000], [5000, 40, 41, 3000, 3100, 1]])
+    h = kv.KV(H, K, D, max_batch=B, max_tokens=T, precision=dtype)
+    none = torch.tensor(hidden(seen, R, window, sink), device="cuda")
+    q = rand(1, B, T, H, D, dtype=dtype)
+    if held8:
+        c = fill8(kv, h, B, R, 32, 3)
+        k, v = (okv.values8(np64(x), bits(s), 32) for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+        c.k.view(torch.uint8)[none], c.v.view(torch.uint8)[none] = 0x7f, 0xff
+        call = lambda: h.attend8(q, c, i32(seen), window=window, sink=sink)
+    else:
+        kc, vc = rand(2, B, R, K, D, dtype=dtype), rand(3, B, R, K, D, dtype=dtype)
+        k, v = np64(kc), np64(vc)
+        kc[none], vc[none] = float("nan"), float("inf")
+        call = lambda: h.attend_window(q, (kc, vc), i32(seen), window, sink=sink)
+    (out, lse), again = call(), call()
+    h.device_status()
+    ref = okv.attend_window(np64(q), k, v, seen, window, sink, 1 / 8)
+    finish(out, lse, again, ref, tols(np64(q), k, v, window + sink, dtype, *ref[:1], ref[2], ref[3], ref[1], 1 / 8))
+
+
+def test_a_window_over_everything_has_the_sums_of_attend(kv):
+    """The sums' logarithms agree, and both are -infinity where nothing is seen, and nowhere else."""
+    q, k, v = rand(1, 4, 9, 8, 128), rand(2, 4, 300, 2, 128), rand(3, 4, 300, 2, 128)
+    seen = np.random.default_rng(0).integers(0, 301, (4, 9))
+    seen[1, 3] = seen[2, 0] = 0
+    h = kv.KV(8, 2, 128, max_batch=4, max_tokens=9)
+    la, lb = h.attend(q, own=(k, v), seen=i32(seen))[1], h.attend_window(q, (k, v), i32(seen), 300)[1]
+    la, lb = np64(la), np64(lb)
+    assert np.array_equal(la == -np.inf, np.broadcast_to((seen == 0)[..., None], la.shape)) and np.array_equal(la == -np.inf, lb == -np.inf)
+    some = seen > 0
+    assert np.all(np.isfinite(lb[some])) and np.abs(la[some] - lb[some]).max() < 1e-5
 
 
 # ------------------------------------------------------------------ the first call of a handle
