@@ -210,9 +210,11 @@ JPI_API jpi_status jpi_kv_append_normed(jpi_kv_handle* h, const void* q, long lo
  *   seen:    device int [batch][tokens]; taken as 0 .. cache->rows (0: padding, which sees nothing)
  *   window:  >= 1;  sink: >= 0
  * q, out, lse, empty rows, NaN and infinities as in jpi_kv_attend; rows outside a token's window are rows that it does not
- * see, and rows that no token of a call sees are not read. The work follows the windows, not the cache's length. In
- * JPI_BF16 mode the probabilities enter the second product as there: calls of many query rows on the 128-row
- * tiles round each to bf16 once, the others carry what the rounding left. JPI_KV_TILES holds here too. Sums of p v are formed at up to
+ * see. The tokens of a request whose rows run together (8 rows, tokens x heads of a KV head, or 128 on the tiles) read the first
+ * `sink` rows and all from the lowest row of their windows to their largest count, the tiles in whole blocks of 64: for tokens that
+ * follow one another the work goes by the windows, not by the cache's length, but tokens of one call with counts far apart also
+ * cost what lies between their windows. In JPI_BF16 mode the probabilities enter the second product as there: calls of many query rows on
+ * the 128-row tiles round each to bf16 once, the others carry what the rounding left. JPI_KV_TILES holds here too. Sums of p v are formed at up to
  * 2^24 times their size (2^8 outside the tiles): finite values of 2^100 and more may come out infinite. A handle's first call here or of
  * jpi_kv8_attend looks up what the device holds of their kernels (2 ms in a process, 0.4 ms for a further head width); it may be captured.
  */
@@ -262,7 +264,8 @@ JPI_API jpi_status jpi_kv8_append(jpi_kv_handle* h, const void* q, long long q_s
  * Scores, softmax and sums in fp32, codes and scales taken as they are. JPI_BF16 mode: queries enter the first product as fp16,
  * scaled by a power of two (bf16's eight bits whole; an element below 2^-14 of its head's largest is off by at most 2^-25 of
  * that), the probabilities the second as fp16 (each off by at most 2^-11 of itself, or 2^-28 of what the largest value of the
- * blocks seen would weigh). JPI_KV_TILES holds here too.
+ * blocks seen would weigh). JPI_KV_TILES holds here too, and what jpi_kv_attend_window says of the rows that are read. Sums of p v are formed at
+ * up to 2^11 times their size (2^8 outside the tiles): finite values of 2^100 and more may come out infinite.
  */
 JPI_API jpi_status jpi_kv8_attend(jpi_kv_handle* h, const void* q, long long q_stride, int batch, int tokens,
                                   const jpi_kv8_cache* cache, const int* seen, int window, int sink, void* out,

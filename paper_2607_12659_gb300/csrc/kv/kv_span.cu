@@ -4,8 +4,8 @@
 // j over the rows that the token of query row r sees (kv_span.h); in 8 bits k_j and v_j are codes times the power of two of
 // their block and head.
 //
-// Query rows of one request and KV head form tiles of 8 (kv_rows.cuh), a tile's rows of the cache are those that one of
-// its tokens sees, and every part (a range of them) leaves partial rows that are joined as in kv_attend.cu.
+// Query rows of one request and KV head form tiles of 8 (kv_rows.cuh), a tile's rows of the cache are the first `sink` and those from its
+// windows' lowest row to its largest count (SpanBlocks), and every part (a range of them) leaves partial rows that are joined as in kv_attend.cu.
 
 #include "kv_attend.h"
 #include "kv_parts.cuh"
@@ -370,8 +370,8 @@ __global__ void __launch_bounds__(AT_THREADS, DP == 256 ? 2 : 3) k_kv_span_cc(co
 
 // bf16 queries. A warp works alone: it takes pieces (8 query rows over a range of the blocks that they see) in turn and streams
 // their blocks of keys, 16 KB with their values (8 of codes), through two stages of shared memory of its own by 16-byte asynchronous
-// copies, the next piece's first blocks and query rows behind this one's last; rows that no token of the piece sees arrive as zeros and
-// are not read. Keys are the 16 rows of mma.sync m16n8k16 and query rows its 8 columns; the values' product runs over keys
+// copies, the next piece's first blocks and query rows behind this one's last; rows behind the piece's largest count, or before
+// its windows and behind the first `sink`, arrive as zeros and are not read. Keys are the 16 rows of mma.sync m16n8k16 and query rows its 8 columns; the values' product runs over keys
 // with d as its rows, the probabilities turned from one's result into the other's operand by 8 x 8 transposes.
 //
 // In 8 bits the codes become fp16 numbers on their way from shared memory into the fragments, two by one instruction: e4m3 is a

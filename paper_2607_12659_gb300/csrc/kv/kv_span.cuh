@@ -13,7 +13,8 @@ __device__ __forceinline__ bool span_sees(const KvSpan& s, int row, int n, int f
 }
 
 // The blocks of KEYS rows that a tile reads: those of the first `sink` rows, and those from the lowest first row of its windows to
-// its largest count. The rows between are no block of the tile.
+// its largest count. The rows between are no block of the tile. (Where the counts lie far apart, rows that none of its tokens sees are
+// among them: a test of every block against every count would cost the calls whose tokens follow one another, which is nearly all.)
 template <int KEYS>
 struct SpanBlocks {
     int head, skip, count;   // blocks of the first rows, blocks left out behind them, blocks in all
